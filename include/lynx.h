@@ -281,6 +281,85 @@ lynx_status lynx_split_quantize_bits(const void* src_bf16, int64_t n_rows, int32
 lynx_status lynx_recombine_bits(const uint8_t* anchor, const uint8_t* residual, const float* meta, int64_t n_rows,
                                 int32_t anchor_bits, uint8_t* codes_u8, void* dequant_bf16, void* stream);
 
+/* Around the cache: rotary positions, tokens written into the planes and read back, and attention of a tree of drafted
+ * tokens (the paper speculates on chains, Section 4.3; these serve decode nodes that draft trees, or that quantise the
+ * tokens they accept instead of keeping them in BF16). */
+
+/* The planes a call writes; as lynx_plane otherwise. */
+typedef struct {
+  uint8_t* anchor;
+  uint8_t* residual;
+  float* meta;
+} lynx_plane_out;
+
+/* Rotary positions on n_pairs pairs of channels, each turned by the angle of its axis' position: text has one axis, images
+ * and video have time, height and width.  Pair i is (x[i], x[i + n_pairs]), or (x[2i], x[2i + 1]) if interleaved; with
+ * p = positions[pair_axis[i]][token], c = cos_sin[p][i] and s = cos_sin[p][n_pairs + i]
+ *     y1 = x1 c - x2 s,   y2 = x2 c + x1 s      (FP32);
+ * channels from 2 n_pairs on stay as they are.  A position outside [0, n_positions) is taken as the nearest one inside. */
+typedef struct {
+  const int32_t* positions;   /* DEVICE int32 [n_axes][positions_stride]: positions[a * positions_stride + token] */
+  const float* cos_sin;       /* DEVICE float [n_positions][2 n_pairs], 16-byte aligned */
+  int64_t positions_stride;   /* at least the number of tokens */
+  int32_t n_axes;             /* 1..8 */
+  int32_t n_positions;        /* at least 1 */
+  int32_t n_pairs;            /* 8, 16, ... 64 */
+  int32_t interleaved;
+  uint8_t pair_axis[64];      /* (read on the host) axis of each pair, below n_axes */
+} lynx_rotary_spec;
+
+/* q : BF16 [n_tokens][num_q_heads][128], k : BF16 [n_tokens][num_kv_heads][128], either may be NULL with 0 heads.  Strides
+ * are elements from a token to the next, multiples of 8 and at least heads * 128: views of a fused projection's output can be
+ * given.  The outputs have strides of their own and may be the inputs (with their strides: in place).  One rounding to BF16.
+ * All pointers 16-byte aligned (positions: 4). */
+lynx_status lynx_rotary(const lynx_rotary_spec* spec, const void* q, int64_t q_stride, int32_t num_q_heads, const void* k,
+                        int64_t k_stride, int32_t num_kv_heads, int64_t n_tokens, void* q_out, int64_t q_out_stride,
+                        void* k_out, int64_t k_out_stride, void* stream);
+
+/* Quantises tokens' keys and values into a paged cache: the codes, planes and scalars that lynx_split_quantize gives, each
+ * row in its place.  k, v : BF16 [n_src][num_kv_heads][128] with strides as for lynx_rotary.  Token i of n_tokens is source row
+ * rows[i] (int32, e.g. the accepted nodes of a tree) or, with rows NULL, row i (n_src >= n_tokens); it goes to
+ * slots[i] = block * block_tokens + offset (int64).  A token whose slot is outside [0, num_blocks * block_tokens) -- -1 for
+ * padding -- or whose source row is outside [0, n_src) is left out.  Of several tokens with one slot, any one's values may
+ * remain (K, V and planes not necessarily the same one's).  spec : NULL, or rotary positions (indexed by source row) for the
+ * keys, which are turned in FP32 and quantised without a rounding in between.  Of the shape, num_kv_heads, head_dim (128),
+ * block_tokens (any) and num_blocks are used.  n_tokens == 0 is a valid no-op. */
+lynx_status lynx_cache_append(const lynx_shape* shape, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                              int64_t n_src, const int32_t* rows, int64_t n_tokens, const int64_t* slots,
+                              const lynx_rotary_spec* spec, lynx_plane_out K, lynx_plane_out V, void* stream);
+
+/* Reads ranges of tokens back: output row i, offsets[b] <= i < offsets[b + 1], is token starts[b] + i - offsets[b] of sequence b,
+ * BF16 bf16_rne(fl(fma(code, scale, zero))) as lynx_recombine writes it, but ordered by token:
+ * k_out, v_out : BF16 [n_rows][num_kv_heads][128].  offsets : int32 [batch + 1], non-decreasing from 0; starts : int32 [batch], or
+ * NULL (all 0).  Where K.residual and V.residual are NULL, the middle of the Anchor's bucket, 16 a + 8, stands for the code.
+ * Rows from offsets[batch] on, tokens outside [0, max_blocks_per_seq * block_tokens) and tokens of a block id outside
+ * [0, num_blocks) are zeros.  Any block_tokens.  n_rows == 0 is a valid no-op. */
+lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, lynx_plane V, const int32_t* block_table, int32_t batch,
+                            const int32_t* starts, const int32_t* offsets, int64_t n_rows, void* k_out, void* v_out,
+                            void* stream);
+
+/* Attention of drafted tokens that form a tree, over a quantised prefix and over each other, in one pass over the planes.
+ * Node j of sequence b attends the tokens [0, seq_lens[b]) of the planes and the nodes i whose bit i is set in
+ * tree_mask[b][j] (itself and its ancestors, say; bits from n_nodes on are ignored); a row that sees nothing gives zeros and
+ * a log-sum-exp of -inf.  n_nodes <= 64, Hq/Hkv <= 16; sequences with fewer nodes leave the rest of their masks empty and
+ * referenced by none (then nothing of those nodes but their queries is read into a result).  A chain is a tree; n_nodes = 1 is a
+ * plain decode step.
+ * q_bf16 : BF16 [batch][n_nodes][Hq][128];  k_nodes, v_nodes : BF16 [batch * n_nodes][Hkv][128], k_stride / v_stride elements from
+ * a node to the next (multiples of 8, at least Hkv * 128: views of a fused projection's output);  tree_mask : uint64 [batch][n_nodes].
+ * K, V with both residuals: the full codes; with both NULL: the Anchor's state.
+ * out : [batch][n_nodes][Hq][128], BF16, or float where out_float is set (for lynx_lse_merge); lse : float [batch][n_nodes][Hq]
+ * or NULL.  Scores are FP32 sums of exact products; weights and values enter the second product as FP16 relative to exponents of
+ * their own (2^-12 of a term; value rows below 2^-29 of the largest of their 128 tokens lose bits), sums are FP32.
+ * workspace : lynx_tree_workspace_bytes(shape, batch, n_nodes) bytes (0: unsupported shape), its first 256 zeroed once
+ * (lynx_workspace_init); calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of range are
+ * clamped and recorded there.  block_tokens a multiple of 16; seq_lens[b] is clamped to the table's capacity. */
+size_t lynx_tree_workspace_bytes(const lynx_shape* shape, int32_t batch, int32_t n_nodes);
+lynx_status lynx_tree_attention(const lynx_shape* shape, const void* q_bf16, int32_t batch, int32_t n_nodes, lynx_plane K,
+                                lynx_plane V, const int32_t* block_table, const int32_t* seq_lens, const void* k_nodes,
+                                int64_t k_stride, const void* v_nodes, int64_t v_stride, const uint64_t* tree_mask,
+                                float softmax_scale, int32_t out_float, void* out, float* lse, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream`, reads and clears the workspace's status word.  Test / debug use. */
 lynx_status lynx_check(void* workspace, void* stream);
 

@@ -32,6 +32,12 @@ class _Plane(ctypes.Structure):
     _fields_ = [("anchor", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("meta", ctypes.c_void_p)]
 
 
+class _RotarySpec(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("cos_sin", ctypes.c_void_p), ("positions_stride", ctypes.c_int64),
+                ("n_axes", ctypes.c_int32), ("n_positions", ctypes.c_int32), ("n_pairs", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("pair_axis", ctypes.c_uint8 * 64)]
+
+
 class _Shape(ctypes.Structure):
     _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
@@ -42,6 +48,7 @@ EXPORTS = ["lynx_split_quantize", "lynx_recombine", "lynx_workspace_bytes", "lyn
            "lynx_anchor_attention", "lynx_merge_verify_attention", "lynx_anchor_attention_static",
            "lynx_bf16_workspace_bytes", "lynx_bf16_attention", "lynx_hier_quantize", "lynx_hier_dequantize",
            "lynx_token_verify", "lynx_workspace_lse", "lynx_bf16_workspace_lse", "lynx_lse_merge", "lynx_verify_decision", "lynx_split_quantize_bits", "lynx_recombine_bits",
+           "lynx_rotary", "lynx_cache_append", "lynx_cache_read", "lynx_tree_workspace_bytes", "lynx_tree_attention",
            "lynx_check",
            "lynx_status_string", "lynx_version"]
 
@@ -101,6 +108,18 @@ def load():
     lib.lynx_split_quantize_bits.restype = ctypes.c_int
     lib.lynx_recombine_bits.argtypes = [vp, vp, vp, i64, i32, vp, vp, vp]
     lib.lynx_recombine_bits.restype = ctypes.c_int
+    lib.lynx_rotary.argtypes = [ctypes.POINTER(_RotarySpec), vp, i64, i32, vp, i64, i32, i64, vp, i64, vp, i64, vp]
+    lib.lynx_rotary.restype = ctypes.c_int
+    lib.lynx_cache_append.argtypes = [ctypes.POINTER(_Shape), vp, i64, vp, i64, i64, vp, i64, vp, ctypes.POINTER(_RotarySpec),
+                                      _Plane, _Plane, vp]
+    lib.lynx_cache_append.restype = ctypes.c_int
+    lib.lynx_cache_read.argtypes = [ctypes.POINTER(_Shape), _Plane, _Plane, vp, i32, vp, vp, i64, vp, vp, vp]
+    lib.lynx_cache_read.restype = ctypes.c_int
+    lib.lynx_tree_workspace_bytes.argtypes = [ctypes.POINTER(_Shape), i32, i32]
+    lib.lynx_tree_workspace_bytes.restype = ctypes.c_size_t
+    lib.lynx_tree_attention.argtypes = [ctypes.POINTER(_Shape), vp, i32, i32, _Plane, _Plane, vp, vp, vp, i64, vp, i64, vp, f32, i32,
+                                        vp, vp, vp, ctypes.c_size_t, vp]
+    lib.lynx_tree_attention.restype = ctypes.c_int
     lib.lynx_check.argtypes = [vp, vp]
     lib.lynx_check.restype = ctypes.c_int
     lib.lynx_status_string.argtypes = [ctypes.c_int]
@@ -516,3 +535,178 @@ def token_verify(p_probs: torch.Tensor, q_probs: torch.Tensor, draft_tokens: tor
     _ok(load().lynx_token_verify(_ptr(p_probs), _ptr(q_probs), _ptr(draft_tokens), _ptr(u), _ptr(r), B, k, V,
                                  _ptr(n_acc), _ptr(nxt), _stream()), "lynx_token_verify")
     return n_acc, nxt
+
+
+# ---------------------------------------------------------------------------------------------- around the cache
+@dataclass
+class Rotary:
+    """Rotary positions: positions i32 [T] or [axes][T], cos_sin f32 [n_positions][2 P] (P cosines, P sines; P = 8, 16, ... 64
+    pairs of channels), pair_axis: the axis of each pair (P ints; None: one axis).  Pairs are channels (i, i + P), or
+    (2 i, 2 i + 1) if interleaved.  Made once per table and step, and used by any number of calls."""
+    positions: torch.Tensor
+    cos_sin: torch.Tensor
+    pair_axis: tuple | list | None = None
+    interleaved: bool = False
+
+    def _c(self, tokens: int):
+        pos, table = self.positions, self.cos_sin
+        if pos.dtype != torch.int32 or pos.dim() not in (1, 2) or pos.shape[-1] < tokens:
+            raise LynxError("positions must be int32 [tokens] or [axes][tokens]")
+        if table.dtype != torch.float32 or table.dim() != 2 or table.shape[1] % 2:
+            raise LynxError("cos_sin must be float32 [positions][2 pairs]")
+        axes, pairs = 1 if pos.dim() == 1 else pos.shape[0], table.shape[1] // 2
+        axis = self.pair_axis if self.pair_axis is not None else [0] * pairs
+        if len(axis) != pairs or pairs > 64 or not all(0 <= a < axes for a in axis):
+            raise LynxError("pair_axis must name one of the positions' axes for each pair, of at most 64")
+        return ctypes.byref(_RotarySpec(_ptr(pos), _ptr(table), pos.shape[-1], axes, table.shape[0], pairs, int(self.interleaved),
+                                        (ctypes.c_uint8 * 64)(*axis)))
+
+
+def rotary_table(n_positions: int, pairs: int = 64, base: float = 10000.0, device=None) -> torch.Tensor:
+    """A cos_sin table f32 [n_positions][2 pairs] of angles position * base^(-i / pairs), computed in 64 bits."""
+    angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * \
+        float(base) ** (-torch.arange(pairs, dtype=torch.float64, device=device) / pairs)
+    return torch.cat((angle.cos(), angle.sin()), 1).float()
+
+
+def _token_rows(t: torch.Tensor, what: str):
+    """Pointer, token stride and heads of BF16 [tokens][heads][128] whose tokens may lie apart (a view of a fused projection)."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != D:
+        raise LynxError(f"{what} must be BF16 [tokens][heads][128]")
+    if not t.is_cuda:
+        raise LynxError("device tensors required")
+    T, H = t.shape[:2]
+    if T and (t.stride(2) != 1 or (H > 1 and t.stride(1) != D)):
+        raise LynxError(f"{what}: the heads of a token must lie one behind the other")
+    return t.data_ptr(), t.stride(0) if T > 1 else H * D, H
+
+
+def rotary(q: torch.Tensor | None, k: torch.Tensor | None, spec: Rotary, q_out: torch.Tensor | None = None,
+           k_out: torch.Tensor | None = None):
+    """lynx_rotary: q BF16 [T][Hq][128], k BF16 [T][Hkv][128] (either may be None; tokens may lie apart) -> (q_out, k_out), which may
+    be the inputs."""
+    if q is None and k is None:
+        raise LynxError("q or k is needed")
+    T = (q if q is not None else k).shape[0]
+    rows = []
+    for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            rows.append((None, (None, 0, 0), (None, 0, 0)))
+            continue
+        if x.shape[0] != T or (out is not None and out.shape != x.shape):
+            raise LynxError("q and k must have as many tokens, and the outputs their shapes")
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        rows.append((out, _token_rows(x, what), _token_rows(out, what + "_out")))
+    (qo, qi, qw), (ko, ki, kw) = rows
+    _ok(load().lynx_rotary(spec._c(T), qi[0], qi[1], qi[2], ki[0], ki[1], ki[2], T, qw[0], qw[1], kw[0], kw[1], _stream()), "lynx_rotary")
+    return qo, ko
+
+
+def _planes_fit(geo: Geometry, *planes: Planes):
+    rows = geo.num_blocks * geo.num_kv_heads * geo.block_tokens
+    for p in planes:
+        if p.anchor.dtype != torch.uint8 or p.anchor.numel() < rows * 64 or p.meta.dtype != torch.float32 or p.meta.numel() < rows * 2 or \
+                (p.residual is not None and (p.residual.dtype != torch.uint8 or p.residual.numel() < rows * 64)):
+            raise LynxError("planes must be u8 [num_blocks][Hkv][block_tokens][64] and f32 [...][2] of the geometry")
+
+
+def cache_append(geo: Geometry, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, K: Planes, V: Planes,
+                 rows: torch.Tensor | None = None, rotary: Rotary | None = None):
+    """lynx_cache_append: quantises tokens' keys and values BF16 [T][Hkv][128] (tokens may lie apart) into the planes K and V.  slots
+    i64 [n]: block * block_tokens + offset of each token written, negative for none; rows i32 [n]: the source row of each
+    (None: row i); rotary: positions for the keys, by source row."""
+    (kp, ks, kh), (vp, vs, vh) = _token_rows(k, "k"), _token_rows(v, "v")
+    if kh != geo.num_kv_heads or vh != kh or v.shape[0] != k.shape[0]:
+        raise LynxError("k and v must be BF16 [tokens][num_kv_heads][128]")
+    if slots.dtype != torch.int64 or slots.dim() != 1 or (rows is not None and (rows.dtype != torch.int32 or rows.shape != slots.shape)):
+        raise LynxError("slots must be int64 [n], rows int32 [n]")
+    _planes_fit(geo, K, V)
+    T = k.shape[0]
+    _ok(load().lynx_cache_append(ctypes.byref(geo._c()), kp, ks, vp, vs, T, _ptr(rows), slots.numel(), _ptr(slots),
+                                 None if rotary is None else rotary._c(T), K._c(), V._c(), _stream()), "lynx_cache_append")
+
+
+def cache_read(geo: Geometry, K: Planes, V: Planes, block_table: torch.Tensor, starts: torch.Tensor | None, offsets: torch.Tensor,
+               n_rows: int, anchor_only: bool = False, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None):
+    """lynx_cache_read: tokens [starts[b], starts[b] + offsets[b + 1] - offsets[b]) of each sequence (starts i32 [B] or None for 0,
+    offsets i32 [B + 1], n_rows = offsets[B]) -> k, v BF16 [n_rows][Hkv][128], from the full codes or from the Anchor alone."""
+    B = block_table.shape[0]
+    if block_table.dtype != torch.int32 or tuple(block_table.shape) != (B, geo.max_blocks_per_seq):
+        raise LynxError("block_table must be int32 [B][max_blocks_per_seq]")
+    if offsets.dtype != torch.int32 or tuple(offsets.shape) != (B + 1,) or \
+            (starts is not None and (starts.dtype != torch.int32 or tuple(starts.shape) != (B,))):
+        raise LynxError("offsets must be int32 [B + 1], starts int32 [B]")
+    _planes_fit(geo, K, V)
+    if not anchor_only and (K.residual is None or V.residual is None):
+        raise LynxError("the Residual planes are needed unless anchor_only")
+    shape = (n_rows, geo.num_kv_heads, D)
+    outs = []
+    for o in (k_out, v_out):
+        if o is None:
+            o = torch.empty(shape, dtype=torch.bfloat16, device=block_table.device)
+        elif o.dtype != torch.bfloat16 or tuple(o.shape) != shape:
+            raise LynxError("k_out, v_out must be BF16 [n_rows][num_kv_heads][128]")
+        outs.append(o)
+    planes = [_Plane(_ptr(p.anchor), None if anchor_only else _ptr(p.residual), _ptr(p.meta)) for p in (K, V)]
+    _ok(load().lynx_cache_read(ctypes.byref(geo._c()), planes[0], planes[1], _ptr(block_table), B, _ptr(starts), _ptr(offsets), n_rows,
+                               _ptr(outs[0]), _ptr(outs[1]), _stream()), "lynx_cache_read")
+    return outs[0], outs[1]
+
+
+def tree_workspace_bytes(geo: Geometry, batch: int, n_nodes: int) -> int:
+    return int(load().lynx_tree_workspace_bytes(ctypes.byref(geo._c()), batch, n_nodes))
+
+
+def make_tree_workspace(geo: Geometry, batch: int, n_nodes: int, device) -> torch.Tensor:
+    """Allocate a workspace for tree_attention calls of (batch, n_nodes) and clear its status word."""
+    n = tree_workspace_bytes(geo, batch, n_nodes)
+    if n == 0:
+        raise LynxError("unsupported tree attention shape")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    _ok(load().lynx_workspace_init(_ptr(ws), 256, _stream()), "lynx_workspace_init")
+    return ws
+
+
+def _nodes(t: torch.Tensor, B: int, n: int, H: int, what: str):
+    """Pointer and node stride of BF16 [B][n][Hkv][128] whose nodes may lie apart, evenly."""
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != (B, n, H, D):
+        raise LynxError(f"{what} must be BF16 [B][n][Hkv][128]")
+    if n > 1 and B > 1 and t.stride(0) != n * t.stride(1):
+        raise LynxError(f"{what}: nodes must lie evenly apart")
+    p, stride, _ = _token_rows(t[:, 0] if n == 1 else t[0], what)
+    return p, stride
+
+
+def tree_attention(geo: Geometry, q: torch.Tensor, K: Planes, V: Planes, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                   k_nodes: torch.Tensor, v_nodes: torch.Tensor, tree_mask: torch.Tensor, workspace: torch.Tensor,
+                   anchor_only: bool = False, softmax_scale: float = 0.0, out: torch.Tensor | None = None,
+                   lse: torch.Tensor | None = None) -> torch.Tensor:
+    """lynx_tree_attention: q BF16 [B][n][Hq][128] of a tree's nodes over the planes' tokens [0, seq_lens[b]) and the nodes i with bit i
+    of tree_mask i64 [B][n]; k_nodes, v_nodes BF16 [B][n][Hkv][128] (nodes may lie apart).  -> BF16 [B][n][Hq][128], or what `out`
+    (BF16 or float32) is; lse: float32 [B][n][Hq] to be filled.  anchor_only: the Anchor's state of the planes."""
+    if q.dim() != 4 or q.dtype != torch.bfloat16 or q.shape[2:] != (geo.num_q_heads, D):
+        raise LynxError("q must be BF16 [B][n][Hq][128]")
+    B, n, Hq, _ = q.shape
+    if block_table.dtype != torch.int32 or tuple(block_table.shape) != (B, geo.max_blocks_per_seq) or seq_lens.dtype != torch.int32 or \
+            tuple(seq_lens.shape) != (B,):
+        raise LynxError("block_table must be int32 [B][max_blocks_per_seq], seq_lens int32 [B]")
+    if tree_mask.dtype != torch.int64 or tuple(tree_mask.shape) != (B, n):
+        raise LynxError("tree_mask must be int64 [B][n]")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != q.shape or out.dtype not in (torch.bfloat16, torch.float32):
+        raise LynxError("out must be BF16 or float32 [B][n][Hq][128]")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, n, Hq)):
+        raise LynxError("lse must be float32 [B][n][Hq]")
+    if not anchor_only and (K.residual is None or V.residual is None):
+        raise LynxError("the Residual planes are needed unless anchor_only")
+    _planes_fit(geo, K, V)
+    if B == 0:
+        return out
+    (kp, ks), (vp, vs) = _nodes(k_nodes, B, n, geo.num_kv_heads, "k_nodes"), _nodes(v_nodes, B, n, geo.num_kv_heads, "v_nodes")
+    planes = [_Plane(_ptr(p.anchor), None if anchor_only else _ptr(p.residual), _ptr(p.meta)) for p in (K, V)]
+    _ok(load().lynx_tree_attention(ctypes.byref(geo._c()), _ptr(q), B, n, planes[0], planes[1], _ptr(block_table), _ptr(seq_lens), kp, ks,
+                                   vp, vs, _ptr(tree_mask), softmax_scale, int(out.dtype == torch.float32), _ptr(out), _ptr(lse),
+                                   _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()), "lynx_tree_attention")
+    return out

@@ -1,0 +1,1065 @@
+// lynx_tree_attention: attention of a tree of drafted tokens over the quantised cache and over each other (sm_100a).
+//
+// For every (sequence, KV head) the n nodes' G = Hq / Hkv query heads are n * G rows; they share the head's keys and values:
+//   S = Q K^T,   p = 2^(a_r S + e - ref_r),   O += P V,   l += sum p,   out = O / l
+// over the prefix (planes, 128 tokens a tile) and one last tile of the nodes' own BF16 keys and values under the tree's mask.
+//
+// Keys enter as their codes less 128, which FP16 holds exactly, and queries scaled by a power of two per row, exactly too:
+//   q . K^_t = scale_t (q . (c_t - 128)) + mid_t sum(q),   mid = zero + 128 scale,
+// so scores have FP32 sums and no rounding of an operand.  Values enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15
+// (rows 2^29 times smaller keep all 11 bits), weights as FP16 relative to a reference that keeps each row's largest between 2^8 and
+// 2^15.5: both roundings are 2^-12 of a term, an eighth of the output's own rounding to BF16.  2^e goes into the weight's exponent and out
+// of l's terms again, so that it costs nothing per weight.  Sums l, references and O are FP32.
+//
+// Layout: rows are the M = 128 lanes of tensor memory (n * G > 128 rows: more row blocks), tokens the N of the scores and the K of
+// P V.  A thread owns a row: no exchange between threads for maxima and sums; P goes from registers to tensor memory, where P V takes it
+// as its A operand.  One CTA per SM; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
+//   warps 0-3, 4-7   two softmax warpgroups, alternating over the tiles with accumulators of their own, joined at the end of a piece
+//   warps 8-11       K codes to FP16 into the K tile, and a piece's queries
+//   warps 12-15      V codes to FP16 values into the V tiles
+//   warps 16, 17     bulk copies of 16-token sub-blocks of the K and V planes into rings; warp 16 deals out the pieces
+//   warp 18          issues every tcgen05.mma: Q K^T two tiles ahead of P V
+// Work is cut in stream-K form: the (sequence, KV head, row block, tile) list into equal ranges, a piece being a range's part of one
+// segment.  A segment within one CTA is written by it; otherwise partial (ref, l, O) go to the workspace and a dependent
+// kernel joins them.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "block_division.cuh"
+#include "bounded_wait.cuh"
+#include "lynx_common.cuh"
+
+namespace lynx {
+namespace {
+
+#include "tc_common.cuh"
+
+constexpr int kTile = 128;          // tokens of a tile, rows of a row block
+constexpr int kMaxNodes = 64;
+constexpr int kPartRow = 132;       // floats of a partial row: O[128], reference, sum, pad
+constexpr int kThreads = 640;
+constexpr int kDoneThreads = 256 + 3 * 32;   // softmax warpgroups, copies, products
+constexpr float kTop = 8.0f, kRaise = 15.5f; // log2 of a row's largest weight when its reference is set, and before it is set anew
+constexpr int kMinExp = -80;        // smallest exponent of a tile's values
+
+struct TreeParams {
+  const uint4* q;                   // [B][n][Hq][16 chunks]
+  const uint8_t *ka, *kr, *va, *vr;
+  const float2 *km, *vm;
+  const int32_t *table, *lens;
+  const uint4 *kt, *vt;             // [B * n] tokens, `kt_stride` / `vt_stride` chunks apart
+  int64_t kt_stride, vt_stride;
+  const unsigned long long* mask;   // [B][n]
+  void* out;                        // [B][n][Hq][128] BF16 or FP32
+  float* lse;                       // [B][n][Hq] or NULL
+  uint32_t* flags;
+  uint32_t* seg;                    // [segments] first CTA << 16 | CTAs
+  float* part;                      // [segments + CTAs][part_rows][kPartRow], slot = segment + CTA
+  float sm_log2;
+  int B, n, Hq, Hkv, G, bt, num_blocks, max_blocks, cols, RB, part_rows, out_f32;
+  int whole;                        // CTA i takes segment i
+  int per_seg;                      // CTAs per segment where all have as many tiles (else 0)
+  BlockDiv bt_div;
+};
+
+template <bool FULL>
+struct Cfg {
+  static constexpr int kStage = FULL ? 16384 : 8192;                 // planes of one tensor and tile: [planes][128 tokens][64 B]
+  static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 5;
+  static constexpr int kOffQ = 0, kOffK = 32768, kOffV = kOffK + 32768, kOffRK = kOffV + 65536, kOffRV = kOffRK + kRingK * kStage,
+                       kOffTok = kOffRV + kRingV * kStage;           // [2][64 token pairs] {scale, scale, mid, mid}
+  static constexpr int kOffRow = kOffTok + 2 * 1024;                 // [2][128] {a, sum of q}
+  static constexpr int kOffVm = kOffRow + 2 * 1024;                  // [2][128] half2 {scale, mid}
+  static constexpr int kOffMl = kOffVm + 2 * 512;                    // [2][128] {ref, l}
+  static constexpr int kOffItems = kOffMl + 2 * 1024;                // [2] Item
+  static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
+  static constexpr int kOffBars = kOffMisc + 128;
+  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 16;
+  static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
+  static_assert(kSmem <= 227 * 1024, "shared memory");
+  // registers a thread after the split (launched with 96 each): 256 * 152 + 256 * 72 + 128 * 32 = 640 * 96
+  static constexpr int kRegSoft = 152, kRegExp = 72, kRegRest = 32;
+  static constexpr int kTmS = 0, kTmO = 256;                         // [2][128] scores, weights in their place; [2][128] accumulators
+};
+
+struct Item {  // a piece: tiles u0 .. u0 + n - 1 of segment (b, h, rb), none: the end
+  int b, h, rb, len, u0, n, first_cta, n_contrib;
+};
+
+// ------------------------------------------------------------------ PTX
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ uint64_t globaltimer_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// Gives up after two seconds (see bounded_wait.cuh); the caller carries on without the data, so that all loops end, and the
+// host is told through the status word.  (Inlined: ptxas does not split the registers of a kernel that has calls.)
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_word) {
+  if (mbar_test(bar, parity)) return true;
+  return bounded_wait([=] { return mbar_try_wait(bar, parity); }, [] { return globaltimer_ns(); }, abort_word);
+}
+__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void named_bar(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }   // -126 <= e <= 127
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Operand descriptors in shared memory, 128-byte swizzle: rows of 128 bytes in groups of eight (1024 bytes).
+__host__ __device__ constexpr uint32_t desc_hi() { return (1024u >> 4) | (1u << 14) | (2u << 29); }
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return ((addr >> 4) & 0x3FFFu) | (((lbo >> 4) & 0x3FFFu) << 16); }
+__device__ __forceinline__ uint64_t desc(uint32_t lo) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(desc_hi()));
+  return d;
+}
+
+// ------------------------------------------------------------------ codes to FP16
+// Channels of a group of 8 in the order in which the nibbles come apart, 0 4 2 6 1 5 3 7 (its own inverse): all tiles have it.
+__device__ __forceinline__ uint32_t centred(uint32_t x) {   // 1024 + code -> code - 128
+  uint32_t d;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(0xE480E480u));
+  return d;
+}
+__device__ __forceinline__ uint32_t bit_select(uint32_t a, uint32_t b, uint32_t mask) {   // (a & mask) | (b & ~mask)
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xE4;" : "=r"(d) : "r"(a), "r"(b), "r"(mask));
+  return d;
+}
+// Eight codes less 128 from a word of Anchor and a word of Residual nibbles (Anchor alone: residual word 0x88888888, the buckets' middles).
+__device__ __forceinline__ void codes8(uint32_t xa, uint32_t xr, uint32_t* o) {
+  const uint32_t ev = bit_select(xa << 4, xr, 0xF0F0F0F0u), od = bit_select(xa, xr >> 4, 0xF0F0F0F0u);
+  o[0] = centred((ev & 0x00FF00FFu) | 0x64006400u);
+  o[1] = centred(__byte_perm(ev, 0x64646464u, 0x4341));
+  o[2] = centred((od & 0x00FF00FFu) | 0x64006400u);
+  o[3] = centred(__byte_perm(od, 0x64646464u, 0x4341));
+}
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+// Eight BF16 values times a power of two, as FP16.
+__device__ __forceinline__ uint4 scaled8(const uint4& w, float f) {
+  return make_uint4(pack_f16x2(bf_lo(w.x) * f, bf_lo(w.z) * f), pack_f16x2(bf_lo(w.y) * f, bf_lo(w.w) * f),
+                    pack_f16x2(bf_hi(w.x) * f, bf_hi(w.z) * f), pack_f16x2(bf_hi(w.y) * f, bf_hi(w.w) * f));
+}
+__device__ __forceinline__ float absmax8(const uint4& w) {
+  uint32_t m = 0u;
+  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v[i] & 0x7FFF7FFFu));
+  return fmaxf(bf_lo(m), bf_hi(m));
+}
+// Exponent that brings the largest of a set to [2^14, 2^15).
+__device__ __forceinline__ int exponent_of(float amax) { return ((__float_as_int(amax) >> 23) & 0xFF) - 127 - 14; }
+
+// A tile's codes by 128 threads: thread i takes the 16-byte chunk i & 3 (32 channels) of rows (i >> 2) + 32 j.  Half of the threads take a
+// chunk's 8-byte halves in the other order: the eight threads of a store's phase then have eight chunk positions, and rows that share
+// their banks in the raw stage are read in different halves.
+template <bool FULL, bool VALUES>
+__device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t vmeta, int i) {
+  const int cc = i & 3, row0 = i >> 2;
+  const uint32_t sw = (uint32_t)(((cc >> 1) ^ (row0 >> 1)) & 1) * 2u;
+  uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16);
+  uint32_t dst = tile + (uint32_t)(cc >> 1) * 16384u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
+  vmeta += (uint32_t)row0 * 4u;
+#pragma unroll 1
+  for (int j = 0; j < 4; ++j, a += 2048u, dst += 4096u, vmeta += 128u) {
+    const uint2 x0 = lds64(a + sw * 4u), x1 = lds64(a + (sw ^ 2u) * 4u);
+    uint2 r0 = make_uint2(0x88888888u, 0x88888888u), r1 = r0;
+    if (FULL) {
+      r0 = lds64(a + 8192u + sw * 4u);
+      r1 = lds64(a + 8192u + (sw ^ 2u) * 4u);
+    }
+    uint32_t s2 = 0u, m2 = 0u;
+    if (VALUES) {
+      const uint32_t sm = lds32(vmeta);
+      s2 = __byte_perm(sm, sm, 0x1010);
+      m2 = __byte_perm(sm, sm, 0x3232);
+    }
+    const uint32_t wa[4] = {x0.x, x0.y, x1.x, x1.y}, wr[4] = {r0.x, r0.y, r1.x, r1.y};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {   // register k holds word k ^ sw of the chunk
+      uint32_t o[4];
+      codes8(wa[k], wr[k], o);
+      if (VALUES) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[x] = fma_f16x2(o[x], s2, m2);
+      }
+      sts128(dst ^ (uint32_t)(k * 16), o[0], o[1], o[2], o[3]);
+    }
+  }
+}
+__device__ __forceinline__ uint32_t chunk_at(uint32_t tile, int row, int ch) {   // 16-byte chunk ch (8 channels) of a row
+  return tile + (uint32_t)(ch >> 3) * 16384u + (uint32_t)row * 128u + (uint32_t)(((ch & 7) ^ (row & 7)) * 16);
+}
+
+// ------------------------------------------------------------------ the cut
+struct Cursor {   // where a CTA's range begins, and how much of it there is
+  int left, q, before;   // units (fewer than 2^31 in all); units a CTA; units in front of sequence b
+  int b, s, u;           // sequence, segment of it, tile
+};
+__device__ __forceinline__ int seq_len(const TreeParams& p, int b) {
+  const int len = ld_dep(p.lens + b);
+  return min(max(len, 0), p.max_blocks * p.bt);
+}
+__device__ __forceinline__ int tiles_of(int len) { return (len + kTile - 1) / kTile + 1; }   // the prefix's and the nodes' own
+// By one warp.
+__device__ __forceinline__ Cursor first_unit(const TreeParams& p, int cta, int n_cta, int lane) {
+  Cursor c = {0, 0, 0, 0, 0, 0};
+  const int S = p.Hkv * p.RB;
+  if (p.whole) {
+    c.b = cta / S;
+    c.s = cta - c.b * S;
+    c.left = c.q = tiles_of(seq_len(p, c.b));
+    return c;
+  }
+  int tot = 0;
+  int lo = 0x7FFFFFFF, hi = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 32) {
+    const int u = b0 + lane < p.B ? tiles_of(seq_len(p, b0 + lane)) : 0;
+    tot += (int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)u);
+    if (u) { lo = min(lo, u); hi = max(hi, u); }
+  }
+  lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+  hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+  if (p.per_seg > 0 && lo == hi) {   // equal segments: each has CTAs of its own
+    const int seg = cta / p.per_seg, part = cta - seg * p.per_seg, q = (hi + p.per_seg - 1) / p.per_seg;
+    c.q = q;
+    c.b = seg / S;
+    c.s = seg - c.b * S;
+    c.u = part * q;
+    c.left = c.b < p.B && c.u < hi ? min(q, hi - c.u) : 0;
+    c.before = -1;
+    return c;
+  }
+  const int T = tot * S;
+  c.q = (T - 1) / n_cta + 1;
+  const int at = min((long long)cta * c.q, (long long)T);
+  c.left = min(c.q, T - at);
+  if (c.left == 0) return c;
+  int running = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 32) {
+    const int u = b0 + lane < p.B ? tiles_of(seq_len(p, b0 + lane)) * S : 0;
+    int incl = u;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    const int excl = running + incl - u;
+    const unsigned hit = __ballot_sync(0xFFFFFFFFu, u > 0 && at >= excl && at < excl + u);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      c.b = b0 + src;
+      c.before = __shfl_sync(0xFFFFFFFFu, excl, src);
+      const int U = tiles_of(seq_len(p, c.b));
+      c.s = (at - c.before) / U;
+      c.u = at - c.before - c.s * U;
+      break;
+    }
+    running += __shfl_sync(0xFFFFFFFFu, incl, 31);
+  }
+  return c;
+}
+// The piece at the cursor, which moves behind it.
+__device__ __forceinline__ Item next_piece(const TreeParams& p, Cursor& c, int cta) {
+  Item it = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (c.left <= 0 || c.b >= p.B) return it;
+  const int S = p.Hkv * p.RB, len = seq_len(p, c.b), U = tiles_of(len);
+  it.b = c.b;
+  it.h = c.s / p.RB;
+  it.rb = c.s - it.h * p.RB;
+  it.len = len;
+  it.u0 = c.u;
+  it.n = min(c.left, U - c.u);
+  if (p.whole) {
+    it.first_cta = cta;
+    it.n_contrib = 1;
+  } else if (c.before < 0) {
+    it.first_cta = (c.b * S + c.s) * p.per_seg;
+    it.n_contrib = (U + c.q - 1) / c.q;
+  } else {
+    const int g0 = c.before + c.s * U;
+    it.first_cta = g0 / c.q;
+    it.n_contrib = (g0 + U - 1) / c.q - it.first_cta + 1;
+  }
+  c.left -= it.n;
+  c.u = 0;
+  if (++c.s == S) {
+    c.s = 0;
+    if (c.before >= 0) c.before += U * S;
+    ++c.b;
+  }
+  return it;
+}
+
+// Which row of memory token `tok` of a sequence is in: (block * Hkv + h) * bt + offset.  Block ids out of range are clamped and recorded.
+__device__ __forceinline__ int block_id(const TreeParams& p, int b, int tok) {
+  return ld_dep(p.table + (int64_t)b * p.max_blocks + quotient(tok, p.bt_div));
+}
+__device__ __forceinline__ int64_t row_at(const TreeParams& p, int id, int h, int tok) {
+  if ((unsigned)id >= (unsigned)p.num_blocks) {
+    atomicOr(p.flags, kFlagBadBlock);
+    id = id < 0 ? 0 : p.num_blocks - 1;
+  }
+  return ((int64_t)id * p.Hkv + h) * p.bt + (tok - quotient(tok, p.bt_div) * p.bt);
+}
+
+// ------------------------------------------------------------------ the kernel
+template <bool FULL>
+__global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __grid_constant__ TreeParams p) {
+  using C = Cfg<FULL>;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t sbase = smem_u32(smem);
+  const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
+  int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
+  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + g] exponents, [8..15] V maxima
+  volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
+  const uint32_t bars = sbase + C::kOffBars;
+  const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
+  const uint32_t kready = vempty + 8 * C::kRingV, sfull = kready + 16, eready = sfull + 16, vready = eready + 16, pready = vready + 16,
+                 pvdone = pready + 16, ifull = pvdone + 16, iempty = ifull + 16;
+  volatile int* ab = misc;        // (waits for data)
+  volatile int* iab = misc + 1;   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
+
+  if (tid == 0) {
+    for (int i = 0; i < C::kRingK; ++i) { mbar_init(kfull + i * 8, 1); mbar_init(kempty + i * 8, 4); }
+    for (int i = 0; i < C::kRingV; ++i) { mbar_init(vfull + i * 8, 1); mbar_init(vempty + i * 8, 4); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(kready + i * 8, 4);
+      mbar_init(sfull + i * 8, 1);
+      mbar_init(eready + i * 8, 4);
+      mbar_init(vready + i * 8, 4);
+      mbar_init(pready + i * 8, 4);
+      mbar_init(pvdone + i * 8, 1);
+      mbar_init(ifull + i * 8, 1);
+      mbar_init(iempty + i * 8, 8 + 4 + 4 + 1 + 1);   // softmax, K, V, V copies, products
+    }
+    for (int i = 0; i < 32; ++i) misc_s[i] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc_s + 2)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem0 = __shfl_sync(0xFFFFFFFFu, misc[2], 0);
+  pdl_wait();
+
+  // ================================================================================== softmax
+  if (warp < 8) {
+    reg_inc<C::kRegSoft>();
+    const int g = warp >> 2, w4 = warp & 3, r = tid & 127;
+    const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
+    const uint32_t tm_s = tmem0 + C::kTmS + g * 128 + lanes, tm_o = tmem0 + C::kTmO + g * 128 + lanes;
+    const uint32_t tok = sbase + C::kOffTok + (uint32_t)g * 1024u;
+    float2* ml = reinterpret_cast<float2*>(smem + C::kOffMl);
+    int gs = 0;
+    for (int ic = 0;; ++ic) {
+      const int qi = ic & 1;
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
+      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
+      if (n == 0) break;
+      const int first_cta = items[qi].first_cta, n_contrib = items[qi].n_contrib;
+      const int c = rb * kTile + r, rows = min(kTile, p.cols - rb * kTile), j = c / p.G, hq = h * p.G + (c - j * p.G);
+      const int n_prefix = (len + kTile - 1) / kTile;
+      bool fresh = true;
+      float ref = 0.0f, l = 0.0f, a = 0.0f, qs = 0.0f;
+      int own = 0;
+      for (int u = 0; u < n; ++u, ++gs) {
+        if ((gs & 1) != g) continue;
+        const uint32_t ph = (gs >> 1) & 1;
+        wait(kready + g * 8, ph, ab);
+        wait(eready + g * 8, ph, ab);
+        wait(sfull + g * 8, ph, ab);
+        tc_fence_after();
+        if (w4 * 32 < rows) {
+          if (own == 0) {
+            const float2 x = reinterpret_cast<const float2*>(smem + C::kOffRow)[qi * 128 + r];
+            a = x.x;
+            qs = x.y;
+          }
+          const int ut = u0 + u;
+          const bool tree = ut == n_prefix;
+          const int valid = tree ? p.n : min(kTile, len - ut * kTile);
+          unsigned long long bits = ~0ull;   // (tree) nodes that this row sees
+          if (tree) bits = c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) : 0ull;
+          const int e = misc[4 + g];
+          const uint64_t qs2 = f2_pack(qs, qs), a2 = f2_pack(a, a);
+          float bias = (float)e - ref;
+          uint64_t sum2 = 0ull;
+#pragma unroll 1
+          for (int ch = 0; ch * 32 < valid; ++ch) {
+            uint32_t s[32];
+            asm volatile("" ::: "memory");
+            TmemRegs<16>::ld(tm_s + ch * 32, s);
+            TmemRegs<16>::ld(tm_s + ch * 32 + 16, s + 16);
+            tc_wait_ld();
+            const uint64_t b2 = f2_pack(bias, bias);
+            float x[32];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const uint4 t = lds128(tok + ch * 256 + k * 16);
+              const uint64_t sk = (uint64_t)t.y << 32 | t.x, mk = (uint64_t)t.w << 32 | t.z;
+              const uint64_t y = f2_fma(f2_pack(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), sk, f2_mul(mk, qs2));
+              f2_unpack(f2_fma(y, a2, b2), x[2 * k], x[2 * k + 1]);
+            }
+            const int room = valid - ch * 32;
+            if (tree || room < 32) {
+              uint32_t see = (uint32_t)(bits >> (tree && ch ? 32 : 0));
+              if (room < 32) see &= (1u << room) - 1u;
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (!((see >> k) & 1u)) x[k] = -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) mx = max3(mx, x[k], x[k + 1]);
+            const bool need = fresh ? mx > -INFINITY : mx > kRaise;
+            if (__any_sync(0xFFFFFFFFu, need)) {
+              // a first reference, or one that a weight would outgrow: what the tile and the piece have so far is scaled
+              const float delta = need ? mx - kTop : 0.0f, f = fresh ? 1.0f : ex2(-delta);
+              if (need) { ref += delta; fresh = false; }
+              bias -= delta;
+#pragma unroll
+              for (int k = 0; k < 32; ++k) x[k] -= delta;
+              l *= f;
+              sum2 = f2_mul(sum2, f2_pack(f, f));
+#pragma unroll 1
+              for (int i = 0; i < ch; ++i) {
+                uint32_t w[16];
+                TmemRegs<16>::ld(tm_s + i * 16, w);
+                tc_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                  const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+                  w[k] = pack_f16x2(v.x * f, v.y * f);
+                }
+                TmemRegs<16>::st(tm_s + i * 16, w);
+              }
+              if (own > 0) {
+                wait(pvdone + g * 8, ph ^ 1u, ab);
+                tc_fence_after();
+#pragma unroll 1
+                for (int i = 0; i < 128; i += 16) {
+                  uint32_t w[16];
+                  TmemRegs<16>::ld(tm_o + i, w);
+                  tc_wait_ld();
+#pragma unroll
+                  for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
+                  TmemRegs<16>::st(tm_o + i, w);
+                }
+              }
+              tc_wait_st();
+            }
+            uint32_t w[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float x0 = ex2(x[2 * k]), x1 = ex2(x[2 * k + 1]);
+              sum2 = f2_add(sum2, f2_pack(x0, x1));
+              w[k] = pack_f16x2(x0, x1);
+            }
+            TmemRegs<16>::st(tm_s + ch * 16, w);
+          }
+          float s0, s1;
+          f2_unpack(sum2, s0, s1);
+          l = fmaf(s0 + s1, pow2(-e), l);
+          tc_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(pready + g * 8);
+        ++own;
+      }
+      // ---- end of the piece: both warpgroups' sums, half of the channels each
+      if (own > 0) {
+        const int last = (gs - 1 & 1) == g ? gs - 1 : gs - 2;
+        wait(pvdone + g * 8, (last >> 1) & 1, ab);
+      }
+      tc_fence_after();
+      const float2 mine = own > 0 && !fresh ? make_float2(ref, l) : make_float2(-INFINITY, 0.0f);
+      ml[g * 128 + r] = mine;
+      named_bar(1, 256);
+      if (w4 * 32 < rows) {
+        const float2 other = ml[(g ^ 1) * 128 + r];
+        const float M = fmaxf(mine.x, other.x);
+        const float fm = mine.x == -INFINITY ? 0.0f : ex2(mine.x - M), fo = other.x == -INFINITY ? 0.0f : ex2(other.x - M);
+        const float L = mine.y * fm + other.y * fo;
+        const bool direct = n_contrib == 1;
+        const float inv = direct ? (L > 0.0f ? 1.0f / L : 0.0f) : 1.0f;
+        const float w0 = (g ? fo : fm) * inv, w1 = (g ? fm : fo) * inv;   // of accumulators 0 and 1
+        const int64_t orow = ((int64_t)b * p.n + j) * p.Hq + hq;
+        const int segment = (b * p.Hkv + h) * p.RB + rb;
+        float* part = p.part + ((int64_t)(segment + (int)blockIdx.x) * p.part_rows + r) * kPartRow;
+#pragma unroll 1
+        for (int i = 64 * g; i < 64 * g + 64; i += 8) {
+          uint32_t o0[8], o1[8];
+          TmemRegs<8>::ld(tmem0 + C::kTmO + lanes + i, o0);
+          TmemRegs<8>::ld(tmem0 + C::kTmO + 128 + lanes + i, o1);
+          tc_wait_ld();
+          float v[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {   // (channel k of the group is at position 0 4 2 6 1 5 3 7)
+            const int at = ((k & 1) << 2) | (k & 2) | (k >> 2);
+            v[k] = (w0 > 0.0f ? __uint_as_float(o0[at]) * w0 : 0.0f) + (w1 > 0.0f ? __uint_as_float(o1[at]) * w1 : 0.0f);
+          }
+          if (r < rows) {
+            if (direct && !p.out_f32) {
+              uint32_t w[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+                w[k] = *reinterpret_cast<const uint32_t*>(&t);
+              }
+              *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + orow * LYNX_D + i) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+              float4* d = reinterpret_cast<float4*>((direct ? static_cast<float*>(p.out) + orow * LYNX_D : part) + i);
+              d[0] = make_float4(v[0], v[1], v[2], v[3]);
+              d[1] = make_float4(v[4], v[5], v[6], v[7]);
+            }
+          }
+        }
+        if (g == 0 && r < rows) {
+          if (!direct) *reinterpret_cast<float2*>(part + 128) = make_float2(M, L);
+          else if (p.lse) p.lse[orow] = L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
+        }
+        if (g == 0 && r == 0 && u0 == 0 && !p.whole) p.seg[segment] = (uint32_t)first_cta << 16 | (uint32_t)n_contrib;
+      }
+      tc_fence_before();
+      named_bar(1, 256);   // (both have read both accumulators and sums)
+      if (lane == 0) mbar_arrive(iempty + qi * 8);
+    }
+    pdl_trigger();
+    // ---- every product has been waited for, and the warps that issue copies and products are done
+    tc_fence_before();
+    named_bar(2, kDoneThreads);
+    if (warp == 0) {
+      land_after_abort([] { return globaltimer_ns(); }, ab);
+      tc_fence_after();
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem0), "r"(512u) : "memory");
+    }
+    if (tid == 0 && (misc[0] || misc[1])) atomicOr(p.flags, kFlagTimeout);
+    return;
+  }
+  // ================================================================================== K tile and queries
+  if (warp < 12) {
+    reg_dec<C::kRegExp>();
+    const int kt = tid - 256;
+    float* tok = reinterpret_cast<float*>(smem + C::kOffTok) + (kt >> 1) * 4 + (kt & 1);
+    int gs = 0, slot = 0;
+    uint32_t phase = 0;
+    for (int ic = 0;; ++ic) {
+      const int qi = ic & 1;
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
+      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
+      if (n == 0) break;
+      const int n_prefix = (len + kTile - 1) / kTile;
+      {   // queries: a thread a row
+        const int c = rb * kTile + kt, j = c / p.G;
+        const uint4* src = p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (c - j * p.G)) * 16;
+        const bool in = c < p.cols;
+        float amax = 0.0f, sum = 0.0f;
+        if (in) {
+#pragma unroll 4
+          for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
+        }
+        const int e = amax > 0.0f ? max(-100, min(100, exponent_of(amax))) : 0;
+        const float f = pow2(-e);
+        if (gs > 0) wait(sfull + ((gs - 1) & 1) * 8, ((gs - 1) >> 1) & 1, ab);   // the previous piece's last Q K^T
+#pragma unroll 4
+        for (int ch = 0; ch < 16; ++ch) {
+          uint4 w = make_uint4(0u, 0u, 0u, 0u);
+          if (in) {
+            w = ld_dep(src + ch);
+            sum += ((bf_lo(w.x) + bf_hi(w.x)) + (bf_lo(w.y) + bf_hi(w.y))) + ((bf_lo(w.z) + bf_hi(w.z)) + (bf_lo(w.w) + bf_hi(w.w)));
+            w = scaled8(w, f);
+          }
+          sts128(chunk_at(sbase + C::kOffQ, kt, ch), w.x, w.y, w.z, w.w);
+        }
+        reinterpret_cast<float2*>(smem + C::kOffRow)[qi * 128 + kt] = make_float2(p.sm_log2 * pow2(e), sum * f);
+      }
+      float2 m = make_float2(0.0f, 0.0f);
+      auto fetch = [&](int ut) {   // scale and zero point of this thread's token of a tile
+        const int t = ut * kTile + kt;
+        m = make_float2(0.0f, 0.0f);
+        if (t < len) m = ld_dep(p.km + row_at(p, block_id(p, b, t), h, t));
+      };
+      fetch(u0);
+      for (int u = 0; u < n; ++u, ++gs) {
+        const int g = gs & 1, ut = u0 + u;
+        const float2 cur = m;
+        fetch(ut + 1);   // (nothing beyond the prefix)
+        wait(pready + g * 8, ((gs >> 1) - 1) & 1, ab);                                    // this place's scalars have been used
+        if (gs > 0) wait(sfull + (g ^ 1) * 8, ((gs - 1) >> 1) & 1, ab);                   // the tile has been used
+        if (ut < n_prefix) {
+          wait(kfull + slot * 8, phase, ab);
+          expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, sbase + C::kOffK, 0u, kt);
+          tok[g * 256] = cur.x;
+          tok[g * 256 + 2] = fmaf(128.0f, cur.x, cur.y);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(kempty + slot * 8);
+          if (++slot == C::kRingK) { slot = 0; phase ^= 1; }
+        } else {   // the nodes' keys: a thread a row, scaled like the queries
+          float f = 0.0f;
+          if (kt < p.n) {
+            const uint4* src = p.kt + ((int64_t)b * p.n + kt) * p.kt_stride + h * 16;
+            float amax = 0.0f;
+#pragma unroll 4
+            for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
+            const int e = amax > 0.0f ? max(-100, min(100, exponent_of(amax))) : 0;
+            f = pow2(e);
+#pragma unroll 4
+            for (int ch = 0; ch < 16; ++ch) {
+              const uint4 w = scaled8(ld_dep(src + ch), pow2(-e));
+              sts128(chunk_at(sbase + C::kOffK, kt, ch), w.x, w.y, w.z, w.w);
+            }
+          }
+          tok[g * 256] = f;
+          tok[g * 256 + 2] = 0.0f;
+        }
+        proxy_fence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(kready + g * 8);
+      }
+      if (lane == 0) mbar_arrive(iempty + qi * 8);
+    }
+    return;
+  }
+  // ================================================================================== V tiles
+  if (warp < 16) {
+    reg_dec<C::kRegExp>();
+    const int vt = tid - 384, w4 = warp & 3;
+    int gs = 0, slot = 0;
+    uint32_t phase = 0;
+    for (int ic = 0;; ++ic) {
+      const int qi = ic & 1;
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
+      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h;
+      if (n == 0) break;
+      const int n_prefix = (len + kTile - 1) / kTile;
+      float2 m = make_float2(0.0f, 0.0f);
+      auto fetch = [&](int ut) {
+        const int t = ut * kTile + vt;
+        m = make_float2(0.0f, 0.0f);
+        if (t < len) m = ld_dep(p.vm + row_at(p, block_id(p, b, t), h, t));
+      };
+      fetch(u0);
+      for (int u = 0; u < n; ++u, ++gs) {
+        const int g = gs & 1, ut = u0 + u;
+        const bool tree = ut == n_prefix;
+        const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u, vmeta = sbase + C::kOffVm + (uint32_t)g * 512u;
+        const float mid = fmaf(128.0f, m.x, m.y), scale = m.x;
+        fetch(ut + 1);
+        // the largest magnitude of the tile, and with it the exponent
+        float amax = fabsf(mid) + 128.0f * fabsf(scale);
+        bool used = false;
+        const uint4* src = p.vt + ((int64_t)b * p.n + vt) * p.vt_stride + h * 16;
+        if (tree) {
+          uint32_t lo = 0u, hi = 0u;   // nodes that some row sees (the others' values may be anything)
+          for (int i = lane; i < p.n; i += 32) {
+            const unsigned long long x = ld_dep(p.mask + (int64_t)b * p.n + i);
+            lo |= (uint32_t)x;
+            hi |= (uint32_t)(x >> 32);
+          }
+          lo = __reduce_or_sync(0xFFFFFFFFu, lo);
+          hi = __reduce_or_sync(0xFFFFFFFFu, hi);
+          used = vt < p.n && (((vt < 32 ? lo : hi) >> (vt & 31)) & 1u);
+          amax = 0.0f;
+          if (used) {
+#pragma unroll 4
+            for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
+          }
+        }
+        const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
+        if (lane == 0) misc[8 + 4 * g + w4] = (int)wmax;
+        named_bar(3, 128);
+        const int top = max(max(misc[8 + 4 * g], misc[9 + 4 * g]), max(misc[10 + 4 * g], misc[11 + 4 * g]));
+        const int e = min(max(exponent_of(__int_as_float(top)), kMinExp), 113);
+        const float f = pow2(-e);
+        wait(pvdone + g * 8, ((gs >> 1) - 1) & 1, ab);   // the tile, and the exponent with it, has been used
+        if (vt == 0) misc[4 + g] = e;
+        if (!tree)
+          *reinterpret_cast<uint32_t*>(smem + C::kOffVm + g * 512 + vt * 4) = pack_f16x2(scale * f, mid * f);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(eready + g * 8);
+        if (!tree) {
+          named_bar(3, 128);
+          wait(vfull + slot * 8, phase, ab);
+          expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, vmeta, vt);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(vempty + slot * 8);
+          if (++slot == C::kRingV) { slot = 0; phase ^= 1; }
+        } else if (vt < ((p.n + 15) & ~15)) {
+#pragma unroll 4
+          for (int ch = 0; ch < 16; ++ch) {
+            const uint4 w = used ? scaled8(ld_dep(src + ch), f) : make_uint4(0u, 0u, 0u, 0u);
+            sts128(chunk_at(tile, vt, ch), w.x, w.y, w.z, w.w);
+          }
+        }
+        proxy_fence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(vready + g * 8);
+      }
+      if (lane == 0) mbar_arrive(iempty + qi * 8);
+    }
+    return;
+  }
+  reg_dec<C::kRegRest>();
+  // ================================================================================== copies
+  if (warp < 18) {
+    const bool k_side = warp == 16;
+    const int ring = k_side ? C::kRingK : C::kRingV;
+    const uint32_t full = k_side ? kfull : vfull, empty = k_side ? kempty : vempty, stages = sbase + (k_side ? C::kOffRK : C::kOffRV);
+    const uint8_t* plane = k_side ? (lane < 8 ? p.ka : p.kr) : (lane < 8 ? p.va : p.vr);
+    Cursor cur = {0, 0, 0, 0, 0, 0};
+    if (k_side) cur = first_unit(p, blockIdx.x, gridDim.x, lane);
+    int slot = 0;
+    uint32_t phase = 1;   // (an empty ring)
+    for (int ic = 0;; ++ic) {
+      const int qi = ic & 1;
+      Item it;
+      if (k_side) {
+        it = next_piece(p, cur, blockIdx.x);
+        wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
+        if (lane == 0) {
+          volatile Item* d = items + qi;
+          d->b = it.b; d->h = it.h; d->rb = it.rb; d->len = it.len;
+          d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib;
+          mbar_arrive(ifull + qi * 8);
+        }
+        __syncwarp();
+      } else {
+        wait(ifull + qi * 8, (ic >> 1) & 1, iab);
+        it.n = items[qi].n; it.len = items[qi].len; it.u0 = items[qi].u0; it.b = items[qi].b; it.h = items[qi].h;
+      }
+      if (it.n == 0) break;
+      const int n_prefix = (it.len + kTile - 1) / kTile, last = min(it.u0 + it.n, n_prefix), off = (lane & 7) * 16;
+      const bool copies = lane < (FULL ? 16 : 8);
+      int id = 0;
+      if (copies && it.u0 * kTile + off < it.len) id = block_id(p, it.b, it.u0 * kTile + off);
+      for (int ut = it.u0; ut < last; ++ut) {
+        const int t = ut * kTile + off, now = id;
+        if (copies && t + kTile < it.len) id = block_id(p, it.b, t + kTile);
+        wait(empty + slot * 8, phase, ab);
+        const int subs = min(8, (it.len - ut * kTile + 15) / 16);   // sub-blocks of 16 tokens with a token of the sequence
+        if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)subs * (FULL ? 2048u : 1024u));
+        __syncwarp();
+        if (copies && (lane & 7) < subs)
+          bulk_g2s(stages + (uint32_t)slot * C::kStage + (uint32_t)(lane >> 3) * 8192u + (uint32_t)(lane & 7) * 1024u,
+                   plane + row_at(p, now, it.h, t) * 64, 1024u, full + slot * 8);
+        if (++slot == ring) { slot = 0; phase ^= 1; }
+      }
+      if (!k_side && lane == 0) mbar_arrive(iempty + qi * 8);
+    }
+    bar_arrive(2, kDoneThreads);
+    return;
+  }
+  // ================================================================================== products
+  if (warp == 18) {
+    constexpr uint32_t kIdescS = tc_idesc(128, false), kIdescO = tc_idesc(128, true);
+    const uint32_t q_lo = desc_lo(sbase + C::kOffQ, 16u), k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 16384u);
+    struct { int ic, n, u, gs; } s = {0, 0, 0, 0};   // the next Q K^T
+    bool more = true;
+    auto qk = [&]() {
+      if (s.u == s.n) {   // the next piece
+        wait(ifull + (s.ic & 1) * 8, (s.ic >> 1) & 1, iab);
+        s.n = items[s.ic & 1].n;
+        s.u = 0;
+        ++s.ic;
+        if (s.n == 0) { more = false; return; }
+      }
+      const int g = s.gs & 1;
+      wait(kready + g * 8, (s.gs >> 1) & 1, ab);
+      tc_fence_after();
+      if (tc_elect()) {
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          const uint32_t o = (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4);
+          tc_mma_ss(tmem0 + C::kTmS + g * 128, desc(q_lo + o), desc(k_lo + o), kIdescS, ks > 0 ? 1u : 0u);
+        }
+        tc_commit(sfull + g * 8);
+      }
+      __syncwarp();
+      ++s.u;
+      ++s.gs;
+    };
+    qk();
+    if (more) qk();
+    int gs = 0;
+    for (int ic = 0;; ++ic) {
+      const int qi = ic & 1;
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
+      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0;
+      if (n == 0) break;
+      const int n_prefix = (len + kTile - 1) / kTile;
+      for (int u = 0; u < n; ++u, ++gs) {
+        const int g = gs & 1, ut = u0 + u;
+        const int steps = ((ut == n_prefix ? p.n : min(kTile, len - ut * kTile)) + 15) / 16;
+        wait(vready + g * 8, (gs >> 1) & 1, ab);
+        wait(pready + g * 8, (gs >> 1) & 1, ab);
+        tc_fence_after();
+        if (tc_elect()) {
+          for (int ks = 0; ks < steps; ++ks)
+            tc_mma_ts(tmem0 + C::kTmO + g * 128, tmem0 + C::kTmS + g * 128 + ks * 8, desc(v_lo + g * 2048u + ks * 128u), kIdescO,
+                      u > 1 || ks > 0 ? 1u : 0u);
+          tc_commit(pvdone + g * 8);
+        }
+        __syncwarp();
+        if (u == n - 1 && lane == 0) mbar_arrive(iempty + qi * 8);   // (in front of a wait for the piece after next)
+        if (more) qk();
+      }
+    }
+    bar_arrive(2, kDoneThreads);
+  }
+}
+
+// Joins the partial results of the CTAs that share a segment, a warp per output row, a lane four channels.
+__global__ void __launch_bounds__(128) tree_combine_kernel(const __grid_constant__ TreeParams p, int n_cta) {
+  pdl_trigger();
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  pdl_wait();
+  if (row >= (int64_t)p.B * p.n * p.Hq) return;
+  const int64_t bj = row / p.Hq;
+  const int hq = (int)(row - bj * p.Hq), b = (int)(bj / p.n), j = (int)(bj - (int64_t)b * p.n), h = hq / p.G;
+  const int c = j * p.G + (hq - h * p.G), rb = c / kTile, r = c - rb * kTile;
+  const int segment = (b * p.Hkv + h) * p.RB + rb;
+  const uint32_t info = ld_dep(p.seg + segment);
+  const int first = min((int)(info >> 16), n_cta - 1), n = min((int)(info & 0xFFFFu), n_cta - first);
+  if (n == 1) return;   // written by the attention kernel
+  const int64_t slot = (int64_t)p.part_rows * kPartRow;
+  const float* src = p.part + (int64_t)(segment + first) * slot + (int64_t)r * kPartRow;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float M = -INFINITY, L = 0.0f;
+  constexpr int kFly = 6;
+  for (int i0 = 0; i0 < n; i0 += kFly) {
+    float4 o[kFly];
+    float2 ml[kFly];
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+      ml[u] = make_float2(-INFINITY, 0.0f);
+      o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i0 + u < n) {
+        ml[u] = ld_dep(reinterpret_cast<const float2*>(src + (i0 + u) * slot + 128));
+        o[u] = ld_dep(reinterpret_cast<const float4*>(src + (i0 + u) * slot) + lane);
+      }
+    }
+    const float m0 = M;
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) M = fmaxf(M, ml[u].x);
+    const float f0 = m0 == -INFINITY ? 0.0f : ex2(m0 - M);
+    L *= f0;
+    acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+      const float f = ml[u].x == -INFINITY ? 0.0f : ex2(ml[u].x - M);
+      L = fmaf(ml[u].y, f, L);
+      acc.x = fmaf(o[u].x, f, acc.x);
+      acc.y = fmaf(o[u].y, f, acc.y);
+      acc.z = fmaf(o[u].z, f, acc.z);
+      acc.w = fmaf(o[u].w, f, acc.w);
+    }
+  }
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+  if (p.out_f32) {
+    reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * LYNX_D)[lane] = acc;
+  } else {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
+    reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * LYNX_D)[lane] =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  }
+  if (p.lse && lane == 0) p.lse[row] = L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
+}
+
+// ------------------------------------------------------------------ host side
+constexpr int kWholeTiles = 3;   // up to so many tiles a CTA takes a whole segment
+
+struct TreePlan {
+  int cols, RB, part_rows, whole, grid, per_seg;
+  int64_t segs;
+  size_t off_seg, off_part, bytes;
+};
+lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
+  if (s->num_kv_heads <= 0 || s->num_q_heads <= 0 || s->num_q_heads % s->num_kv_heads || s->block_tokens <= 0 || s->num_blocks <= 0 ||
+      s->max_blocks_per_seq <= 0 || B <= 0 || n <= 0)
+    return LYNX_ERR_SHAPE;
+  const int G = s->num_q_heads / s->num_kv_heads;
+  const int64_t cap = (int64_t)s->max_blocks_per_seq * s->block_tokens;
+  if (s->head_dim != LYNX_D || s->block_tokens % 16 || G > 16 || n > kMaxNodes || cap >= (1ll << 30)) return LYNX_ERR_UNSUPPORTED;
+  pl->cols = n * G;
+  pl->RB = (pl->cols + kTile - 1) / kTile;
+  pl->part_rows = pl->cols < kTile ? pl->cols : kTile;
+  pl->segs = (int64_t)B * s->num_kv_heads * pl->RB;
+  const int64_t tiles = (cap + kTile - 1) / kTile + 1, sms = sm_count();
+  if (pl->segs >= (1 << 24) || pl->segs * tiles >= (1ll << 31)) return LYNX_ERR_UNSUPPORTED;
+  pl->whole = tiles <= kWholeTiles;
+  pl->per_seg = 0;
+  if (pl->whole) {
+    pl->grid = (int)pl->segs;
+  } else {
+    pl->grid = (int)(pl->segs * tiles < sms ? pl->segs * tiles : sms);
+    if (pl->segs <= pl->grid && pl->grid / pl->segs * pl->segs * 100 >= 85ll * pl->grid) pl->per_seg = (int)(pl->grid / pl->segs);
+  }
+  const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  pl->off_seg = kWsHeaderBytes;
+  pl->off_part = up(pl->off_seg + (size_t)pl->segs * 4);
+  pl->bytes = pl->off_part + (pl->whole ? 0 : (size_t)(pl->segs + pl->grid) * pl->part_rows * kPartRow * 4);
+  return LYNX_OK;
+}
+
+template <bool FULL>
+lynx_status launch_tree(const TreeParams& p, int grid, void* stream) {
+  using C = Cfg<FULL>;
+  if (cudaFuncSetAttribute(tree_attention_kernel<FULL>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
+    launch_status();
+    return LYNX_ERR_CUDA;
+  }
+  return launch_pdl(tree_attention_kernel<FULL>, (unsigned)grid, kThreads, C::kSmem, stream, p);
+}
+
+}  // namespace
+}  // namespace lynx
+
+extern "C" size_t lynx_tree_workspace_bytes(const lynx_shape* shape, int32_t batch, int32_t n_nodes) {
+  lynx::TreePlan pl;
+  if (!shape || lynx::tree_plan(shape, batch, n_nodes, &pl) != LYNX_OK) return 0;
+  return pl.bytes;
+}
+
+extern "C" lynx_status lynx_tree_attention(const lynx_shape* shape, const void* q_bf16, int32_t batch, int32_t n_nodes, lynx_plane K,
+                                           lynx_plane V, const int32_t* block_table, const int32_t* seq_lens, const void* k_nodes,
+                                           int64_t k_stride, const void* v_nodes, int64_t v_stride, const uint64_t* tree_mask,
+                                           float softmax_scale, int32_t out_float, void* out, float* lse, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
+  using namespace lynx;
+  if (batch == 0) return LYNX_OK;
+  if (!shape) return LYNX_ERR_NULL;
+  TreePlan pl;
+  const lynx_status rc = tree_plan(shape, batch, n_nodes, &pl);
+  if (rc != LYNX_OK) return rc;
+  if (!q_bf16 || !K.anchor || !K.meta || !V.anchor || !V.meta || !K.residual != !V.residual || !block_table || !seq_lens || !k_nodes ||
+      !v_nodes || !tree_mask || !out || !workspace)
+    return LYNX_ERR_NULL;
+  const int64_t least = (int64_t)shape->num_kv_heads * LYNX_D;
+  if (k_stride < least || v_stride < least || k_stride % 8 || v_stride % 8) return LYNX_ERR_SHAPE;
+  const auto at = [](const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; };
+  if (!aligned16(q_bf16) || !aligned16(K.anchor) || !aligned16(V.anchor) || !aligned16(K.residual) || !aligned16(V.residual) ||
+      !at(K.meta, 8) || !at(V.meta, 8) || !aligned16(k_nodes) || !aligned16(v_nodes) || !at(tree_mask, 8) || !aligned16(out) || !at(lse, 4) ||
+      !at(block_table, 4) || !at(seq_lens, 4) || !aligned16(workspace))
+    return LYNX_ERR_ALIGN;
+  if (workspace_bytes < pl.bytes) return LYNX_ERR_WORKSPACE;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  TreeParams p;
+  p.q = static_cast<const uint4*>(q_bf16);
+  p.ka = K.anchor; p.kr = K.residual; p.va = V.anchor; p.vr = V.residual;
+  p.km = reinterpret_cast<const float2*>(K.meta); p.vm = reinterpret_cast<const float2*>(V.meta);
+  p.table = block_table; p.lens = seq_lens;
+  p.kt = static_cast<const uint4*>(k_nodes); p.vt = static_cast<const uint4*>(v_nodes);
+  p.kt_stride = k_stride / 8; p.vt_stride = v_stride / 8;
+  p.mask = reinterpret_cast<const unsigned long long*>(tree_mask);
+  p.out = out; p.lse = lse;
+  p.flags = reinterpret_cast<uint32_t*>(ws);
+  p.seg = reinterpret_cast<uint32_t*>(ws + pl.off_seg);
+  p.part = reinterpret_cast<float*>(ws + pl.off_part);
+  p.sm_log2 = (softmax_scale == 0.0f ? 0.08838834764831845f : softmax_scale) * 1.4426950408889634f;
+  p.B = batch; p.n = n_nodes; p.Hq = shape->num_q_heads; p.Hkv = shape->num_kv_heads; p.G = p.Hq / p.Hkv;
+  p.bt = shape->block_tokens; p.num_blocks = shape->num_blocks; p.max_blocks = shape->max_blocks_per_seq;
+  p.cols = pl.cols; p.RB = pl.RB; p.part_rows = pl.part_rows; p.out_f32 = out_float ? 1 : 0;
+  p.whole = pl.whole; p.per_seg = pl.per_seg;
+  p.bt_div = block_div(p.bt);
+  const lynx_status st = K.residual ? launch_tree<true>(p, pl.grid, stream) : launch_tree<false>(p, pl.grid, stream);
+  if (st != LYNX_OK || pl.whole) return st;
+  const int64_t rows = (int64_t)batch * n_nodes * p.Hq;
+  return launch_pdl(tree_combine_kernel, (unsigned)((rows + 3) / 4), 128, 0, stream, p, pl.grid);
+}
