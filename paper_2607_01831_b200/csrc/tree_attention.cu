@@ -12,13 +12,14 @@
 // of l's terms again, so that it costs nothing per weight.  Sums l, references and O are FP32.
 //
 // Layout: rows are the M = 128 lanes of tensor memory (n * G > 128 rows: more row blocks), tokens the N of the scores and the K of
-// P V.  A thread owns a row: no exchange between threads for maxima and sums; P goes from registers to tensor memory, where P V takes it
-// as its A operand.  One CTA per SM; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
-//   warps 0-3, 4-7   two softmax warpgroups, alternating over the tiles with accumulators of their own, joined at the end of a piece
-//   warps 8-11       K codes to FP16 into the K tile, and a piece's queries
+// P V.  Two threads share a row, one for each half of a tile's tokens; they exchange a vote per tile and their sums at the end.  Queries
+// are the A operand of the scores in tensor memory, P goes from registers to tensor memory, over the scores, as the A operand of P V.
+// One CTA per SM; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
+//   warps 0-3, 4-7   softmax, tokens 0..63 and 64..127 of every tile
+//   warps 8-11       K codes to FP16 into the K tiles, and a piece's queries
 //   warps 12-15      V codes to FP16 values into the V tiles
 //   warps 16, 17     bulk copies of 16-token sub-blocks of the K and V planes into rings; warp 16 deals out the pieces
-//   warp 18          issues every tcgen05.mma: Q K^T two tiles ahead of P V
+//   warp 18          issues every tcgen05.mma: Q K^T a tile ahead of P V
 // Work is cut in stream-K form: the (sequence, KV head, row block, tile) list into equal ranges, a piece being a range's part of one
 // segment.  A segment within one CTA is written by it; otherwise partial (ref, l, O) go to the workspace and a dependent
 // kernel joins them.
@@ -66,12 +67,12 @@ template <bool FULL>
 struct Cfg {
   static constexpr int kStage = FULL ? 16384 : 8192;                 // planes of one tensor and tile: [planes][128 tokens][64 B]
   static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 5;
-  static constexpr int kOffQ = 0, kOffK = 32768, kOffV = kOffK + 32768, kOffRK = kOffV + 65536, kOffRV = kOffRK + kRingK * kStage,
+  static constexpr int kOffK = 0, kOffV = kOffK + 65536, kOffRK = kOffV + 65536, kOffRV = kOffRK + kRingK * kStage,
                        kOffTok = kOffRV + kRingV * kStage;           // [2][64 token pairs] {scale, scale, mid, mid}
-  static constexpr int kOffRow = kOffTok + 2 * 1024;                 // [2][128] {a, sum of q}
-  static constexpr int kOffVm = kOffRow + 2 * 1024;                  // [2][128] half2 {scale, mid}
-  static constexpr int kOffMl = kOffVm + 2 * 512;                    // [2][128] {ref, l}
-  static constexpr int kOffItems = kOffMl + 2 * 1024;                // [2] Item
+  static constexpr int kOffRow = kOffTok + 2 * 1024;                 // [2][128] sum of q
+  static constexpr int kOffVm = kOffRow + 2 * 512;                   // [2][128] half2 {scale, mid}
+  static constexpr int kOffX = kOffVm + 2 * 512;                     // [2][128] maxima, [2][128] sums of the halves of a row
+  static constexpr int kOffItems = kOffX + 4 * 512;                  // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
   static constexpr int kOffBars = kOffMisc + 128;
   static constexpr int kBars = 2 * kRingK + 2 * kRingV + 16;
@@ -79,7 +80,7 @@ struct Cfg {
   static_assert(kSmem <= 227 * 1024, "shared memory");
   // registers a thread after the split (launched with 96 each): 256 * 152 + 256 * 72 + 128 * 32 = 640 * 96
   static constexpr int kRegSoft = 152, kRegExp = 72, kRegRest = 32;
-  static constexpr int kTmS = 0, kTmO = 256;                         // [2][128] scores, weights in their place; [2][128] accumulators
+  static constexpr int kTmS = 0, kTmO = 256, kTmQ = 384;             // [2][128] scores, weights in their place; accumulators; queries
 };
 
 struct Item {  // a piece: tiles u0 .. u0 + n - 1 of segment (b, h, rb), none: the end
@@ -127,6 +128,12 @@ __device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t
 }
 __device__ __forceinline__ void named_bar(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+__device__ __forceinline__ bool bar_or(int id, int n, bool pred) {
+  uint32_t res;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(res) : "r"(pred ? 1u : 0u), "r"(id), "r"(n) : "memory");
+  return res != 0;
+}
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -174,11 +181,6 @@ __device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
 __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -250,29 +252,32 @@ __device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t vme
   uint32_t dst = tile + (uint32_t)(cc >> 1) * 16384u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
   vmeta += (uint32_t)row0 * 4u;
 #pragma unroll 1
-  for (int j = 0; j < 4; ++j, a += 2048u, dst += 4096u, vmeta += 128u) {
-    const uint2 x0 = lds64(a + sw * 4u), x1 = lds64(a + (sw ^ 2u) * 4u);
-    uint2 r0 = make_uint2(0x88888888u, 0x88888888u), r1 = r0;
-    if (FULL) {
-      r0 = lds64(a + 8192u + sw * 4u);
-      r1 = lds64(a + 8192u + (sw ^ 2u) * 4u);
-    }
-    uint32_t s2 = 0u, m2 = 0u;
-    if (VALUES) {
-      const uint32_t sm = lds32(vmeta);
-      s2 = __byte_perm(sm, sm, 0x1010);
-      m2 = __byte_perm(sm, sm, 0x3232);
-    }
-    const uint32_t wa[4] = {x0.x, x0.y, x1.x, x1.y}, wr[4] = {r0.x, r0.y, r1.x, r1.y};
+  for (int j = 0; j < 4; j += 2, a += 4096u, dst += 8192u, vmeta += 256u) {
+    uint2 x[2][2], y[2][2];
+    uint32_t sm[2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {   // register k holds word k ^ sw of the chunk
-      uint32_t o[4];
-      codes8(wa[k], wr[k], o);
-      if (VALUES) {
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) o[x] = fma_f16x2(o[x], s2, m2);
+      for (int z = 0; z < 2; ++z) {
+        x[i][z] = lds64(a + i * 2048u + (sw ^ (uint32_t)(2 * z)) * 4u);
+        y[i][z] = FULL ? lds64(a + i * 2048u + 8192u + (sw ^ (uint32_t)(2 * z)) * 4u) : make_uint2(0x88888888u, 0x88888888u);
       }
-      sts128(dst ^ (uint32_t)(k * 16), o[0], o[1], o[2], o[3]);
+      sm[i] = VALUES ? lds32(vmeta + i * 128u) : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t s2 = __byte_perm(sm[i], sm[i], 0x1010), m2 = __byte_perm(sm[i], sm[i], 0x3232);
+      const uint32_t wa[4] = {x[i][0].x, x[i][0].y, x[i][1].x, x[i][1].y}, wr[4] = {y[i][0].x, y[i][0].y, y[i][1].x, y[i][1].y};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {   // register k holds word k ^ sw of the chunk
+        uint32_t o[4];
+        codes8(wa[k], wr[k], o);
+        if (VALUES) {
+#pragma unroll
+          for (int z = 0; z < 4; ++z) o[z] = fma_f16x2(o[z], s2, m2);
+        }
+        sts128((dst ^ (uint32_t)(k * 16)) + i * 4096u, o[0], o[1], o[2], o[3]);
+      }
     }
   }
 }
@@ -401,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   const uint32_t sbase = smem_u32(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
-  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + g] exponents, [8..15] V maxima
+  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + g] exponents, [8..15] V maxima, [16 + 4 piece + i] q maxima
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
@@ -418,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       mbar_init(sfull + i * 8, 1);
       mbar_init(eready + i * 8, 4);
       mbar_init(vready + i * 8, 4);
-      mbar_init(pready + i * 8, 4);
+      mbar_init(pready + i * 8, 8);
       mbar_init(pvdone + i * 8, 1);
       mbar_init(ifull + i * 8, 1);
       mbar_init(iempty + i * 8, 8 + 4 + 4 + 1 + 1);   // softmax, K, V, V copies, products
@@ -439,11 +444,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   // ================================================================================== softmax
   if (warp < 8) {
     reg_inc<C::kRegSoft>();
-    const int g = warp >> 2, w4 = warp & 3, r = tid & 127;
+    const int half = warp >> 2, w4 = warp & 3, r = tid & 127, bar = 4 + w4;   // (a warp's rows are shared with warp ^ 4)
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
-    const uint32_t tm_s = tmem0 + C::kTmS + g * 128 + lanes, tm_o = tmem0 + C::kTmO + g * 128 + lanes;
-    const uint32_t tok = sbase + C::kOffTok + (uint32_t)g * 1024u;
-    float2* ml = reinterpret_cast<float2*>(smem + C::kOffMl);
+    const uint32_t tm_o = tmem0 + C::kTmO + lanes + half * 64;
+    float* xs = reinterpret_cast<float*>(smem + C::kOffX);
     int gs = 0;
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
@@ -453,170 +457,151 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int first_cta = items[qi].first_cta, n_contrib = items[qi].n_contrib;
       const int c = rb * kTile + r, rows = min(kTile, p.cols - rb * kTile), j = c / p.G, hq = h * p.G + (c - j * p.G);
       const int n_prefix = (len + kTile - 1) / kTile;
+      const bool works = w4 * 32 < rows;
       bool fresh = true;
-      float ref = 0.0f, l = 0.0f, a = 0.0f, qs = 0.0f;
-      int own = 0;
+      float ref = 0.0f, l = 0.0f, qs = 0.0f;
+#pragma unroll 1
       for (int u = 0; u < n; ++u, ++gs) {
-        if ((gs & 1) != g) continue;
+        const int g = gs & 1;
         const uint32_t ph = (gs >> 1) & 1;
         wait(kready + g * 8, ph, ab);
         wait(eready + g * 8, ph, ab);
         wait(sfull + g * 8, ph, ab);
         tc_fence_after();
-        if (w4 * 32 < rows) {
-          if (own == 0) {
-            const float2 x = reinterpret_cast<const float2*>(smem + C::kOffRow)[qi * 128 + r];
-            a = x.x;
-            qs = x.y;
-          }
+        if (works) {
+          if (u == 0) qs = reinterpret_cast<const float*>(smem + C::kOffRow)[qi * 128 + r];
           const int ut = u0 + u;
           const bool tree = ut == n_prefix;
-          const int valid = tree ? p.n : min(kTile, len - ut * kTile);
-          unsigned long long bits = ~0ull;   // (tree) nodes that this row sees
-          if (tree) bits = c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) : 0ull;
+          const int valid = (tree ? p.n : min(kTile, len - ut * kTile)) - 64 * half;   // of this half
           const int e = misc[4 + g];
-          const uint64_t qs2 = f2_pack(qs, qs), a2 = f2_pack(a, a);
-          float bias = (float)e - ref;
-          uint64_t sum2 = 0ull;
-#pragma unroll 1
-          for (int ch = 0; ch * 32 < valid; ++ch) {
-            uint32_t s[32];
-            asm volatile("" ::: "memory");
-            TmemRegs<16>::ld(tm_s + ch * 32, s);
-            TmemRegs<16>::ld(tm_s + ch * 32 + 16, s + 16);
+          const float bias = (float)e - ref;
+          const uint32_t tm_s = tmem0 + C::kTmS + g * 128 + lanes, tok = sbase + C::kOffTok + (uint32_t)(g * 1024 + half * 512);
+          float x[64];
+          float mx = -INFINITY;
+          if (valid > 0) {
+            const uint64_t qs2 = f2_pack(qs, qs), b2 = f2_pack(bias, bias);
+            uint32_t* sx = reinterpret_cast<uint32_t*>(x);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) TmemRegs<16>::ld(tm_s + half * 64 + k * 16, sx + 16 * k);
             tc_wait_ld();
-            const uint64_t b2 = f2_pack(bias, bias);
-            float x[32];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const uint4 t = lds128(tok + ch * 256 + k * 16);
+            for (int k = 0; k < 32; ++k) {
+              const uint4 t = lds128(tok + k * 16);
               const uint64_t sk = (uint64_t)t.y << 32 | t.x, mk = (uint64_t)t.w << 32 | t.z;
-              const uint64_t y = f2_fma(f2_pack(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), sk, f2_mul(mk, qs2));
-              f2_unpack(f2_fma(y, a2, b2), x[2 * k], x[2 * k + 1]);
+              f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), sk, f2_fma(mk, qs2, b2)), x[2 * k], x[2 * k + 1]);
             }
-            const int room = valid - ch * 32;
-            if (tree || room < 32) {
-              uint32_t see = (uint32_t)(bits >> (tree && ch ? 32 : 0));
-              if (room < 32) see &= (1u << room) - 1u;
+            if (tree || valid < 64) {
+              unsigned long long see = tree ? (c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) : 0ull) : ~0ull;
+              if (valid < 64) see &= (1ull << valid) - 1ull;
 #pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (!((see >> k) & 1u)) x[k] = -INFINITY;
+              for (int k = 0; k < 64; ++k)
+                if (!((see >> k) & 1ull)) x[k] = -INFINITY;
             }
-            float mx = -INFINITY;
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int k = 0; k < 32; k += 2) mx = max3(mx, x[k], x[k + 1]);
+            for (int k = 0; k < 32; ++k) m4[k & 3] = max3(m4[k & 3], x[2 * k], x[2 * k + 1]);
+            mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
+          }
+          // (behind the vote both halves' scores are in registers: weights may go over them)
+          if (bar_or(bar, 64, fresh ? mx > -INFINITY : mx > kRaise)) {
+            // a first reference, or one that a weight would outgrow: what the piece has so far is scaled
+            xs[half * 128 + r] = mx;
+            named_bar(bar, 64);
+            mx = fmaxf(mx, xs[(half ^ 1) * 128 + r]);
             const bool need = fresh ? mx > -INFINITY : mx > kRaise;
-            if (__any_sync(0xFFFFFFFFu, need)) {
-              // a first reference, or one that a weight would outgrow: what the tile and the piece have so far is scaled
-              const float delta = need ? mx - kTop : 0.0f, f = fresh ? 1.0f : ex2(-delta);
-              if (need) { ref += delta; fresh = false; }
-              bias -= delta;
+            const float delta = need ? mx - kTop : 0.0f, f = fresh ? 1.0f : ex2(-delta);
+            if (need) { ref += delta; fresh = false; }
 #pragma unroll
-              for (int k = 0; k < 32; ++k) x[k] -= delta;
-              l *= f;
-              sum2 = f2_mul(sum2, f2_pack(f, f));
+            for (int k = 0; k < 64; ++k) x[k] -= delta;
+            l *= f;
+            if (u > 0) {
+              wait(pvdone + (g ^ 1) * 8, ((gs - 1) >> 1) & 1, ab);
+              tc_fence_after();
 #pragma unroll 1
-              for (int i = 0; i < ch; ++i) {
+              for (int i = 0; i < 64; i += 16) {
                 uint32_t w[16];
-                TmemRegs<16>::ld(tm_s + i * 16, w);
+                TmemRegs<16>::ld(tm_o + i, w);
                 tc_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                  const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
-                  w[k] = pack_f16x2(v.x * f, v.y * f);
-                }
-                TmemRegs<16>::st(tm_s + i * 16, w);
+                for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
+                TmemRegs<16>::st(tm_o + i, w);
               }
-              if (own > 0) {
-                wait(pvdone + g * 8, ph ^ 1u, ab);
-                tc_fence_after();
-#pragma unroll 1
-                for (int i = 0; i < 128; i += 16) {
-                  uint32_t w[16];
-                  TmemRegs<16>::ld(tm_o + i, w);
-                  tc_wait_ld();
-#pragma unroll
-                  for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
-                  TmemRegs<16>::st(tm_o + i, w);
-                }
-              }
-              tc_wait_st();
             }
-            uint32_t w[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float x0 = ex2(x[2 * k]), x1 = ex2(x[2 * k + 1]);
-              sum2 = f2_add(sum2, f2_pack(x0, x1));
-              w[k] = pack_f16x2(x0, x1);
-            }
-            TmemRegs<16>::st(tm_s + ch * 16, w);
           }
-          float s0, s1;
-          f2_unpack(sum2, s0, s1);
-          l = fmaf(s0 + s1, pow2(-e), l);
+          if (valid > 0) {
+            uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              uint32_t w[16];
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                const float x0 = ex2(x[32 * i + 2 * k]), x1 = ex2(x[32 * i + 2 * k + 1]);
+                sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(x0, x1));
+                w[k] = pack_f16x2(x0, x1);
+              }
+              TmemRegs<16>::st(tm_s + half * 32 + i * 16, w);
+            }
+            float s0, s1;
+            f2_unpack(f2_add(sum2[0], sum2[1]), s0, s1);
+            l = fmaf(s0 + s1, pow2(-e), l);
+          }
           tc_wait_st();
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(pready + g * 8);
-        ++own;
       }
-      // ---- end of the piece: both warpgroups' sums, half of the channels each
-      if (own > 0) {
-        const int last = (gs - 1 & 1) == g ? gs - 1 : gs - 2;
-        wait(pvdone + g * 8, (last >> 1) & 1, ab);
-      }
+      // ---- end of the piece: both halves' sums, half of the channels each
+      wait(pvdone + ((gs - 1) & 1) * 8, ((gs - 1) >> 1) & 1, ab);
       tc_fence_after();
-      const float2 mine = own > 0 && !fresh ? make_float2(ref, l) : make_float2(-INFINITY, 0.0f);
-      ml[g * 128 + r] = mine;
-      named_bar(1, 256);
-      if (w4 * 32 < rows) {
-        const float2 other = ml[(g ^ 1) * 128 + r];
-        const float M = fmaxf(mine.x, other.x);
-        const float fm = mine.x == -INFINITY ? 0.0f : ex2(mine.x - M), fo = other.x == -INFINITY ? 0.0f : ex2(other.x - M);
-        const float L = mine.y * fm + other.y * fo;
+      if (works) {
+        xs[256 + half * 128 + r] = l;
+        named_bar(bar, 64);
+        const float L = l + xs[256 + (half ^ 1) * 128 + r], M = fresh ? -INFINITY : ref;
         const bool direct = n_contrib == 1;
-        const float inv = direct ? (L > 0.0f ? 1.0f / L : 0.0f) : 1.0f;
-        const float w0 = (g ? fo : fm) * inv, w1 = (g ? fm : fo) * inv;   // of accumulators 0 and 1
+        const float w = L > 0.0f ? (direct ? 1.0f / L : 1.0f) : 0.0f;
         const int64_t orow = ((int64_t)b * p.n + j) * p.Hq + hq;
         const int segment = (b * p.Hkv + h) * p.RB + rb;
         float* part = p.part + ((int64_t)(segment + (int)blockIdx.x) * p.part_rows + r) * kPartRow;
 #pragma unroll 1
-        for (int i = 64 * g; i < 64 * g + 64; i += 8) {
-          uint32_t o0[8], o1[8];
-          TmemRegs<8>::ld(tmem0 + C::kTmO + lanes + i, o0);
-          TmemRegs<8>::ld(tmem0 + C::kTmO + 128 + lanes + i, o1);
+        for (int i = 0; i < 64; i += 16) {
+          uint32_t o[16];
+          TmemRegs<16>::ld(tm_o + i, o);
           tc_wait_ld();
-          float v[8];
+          float v[16];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {   // (channel k of the group is at position 0 4 2 6 1 5 3 7)
-            const int at = ((k & 1) << 2) | (k & 2) | (k >> 2);
-            v[k] = (w0 > 0.0f ? __uint_as_float(o0[at]) * w0 : 0.0f) + (w1 > 0.0f ? __uint_as_float(o1[at]) * w1 : 0.0f);
+          for (int k = 0; k < 16; ++k) {   // (channel k of a group of 8 is at position 0 4 2 6 1 5 3 7)
+            const int at = (k & 8) | ((k & 1) << 2) | (k & 2) | ((k >> 2) & 1);
+            v[k] = __uint_as_float(o[at]) * w;
           }
           if (r < rows) {
+            const int d = half * 64 + i;
             if (direct && !p.out_f32) {
-              uint32_t w[4];
+              uint32_t x[8];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
+              for (int k = 0; k < 8; ++k) {
                 const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-                w[k] = *reinterpret_cast<const uint32_t*>(&t);
+                x[k] = *reinterpret_cast<const uint32_t*>(&t);
               }
-              *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + orow * LYNX_D + i) = make_uint4(w[0], w[1], w[2], w[3]);
+              uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + orow * LYNX_D + d);
+              dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
+              dst[1] = make_uint4(x[4], x[5], x[6], x[7]);
             } else {
-              float4* d = reinterpret_cast<float4*>((direct ? static_cast<float*>(p.out) + orow * LYNX_D : part) + i);
-              d[0] = make_float4(v[0], v[1], v[2], v[3]);
-              d[1] = make_float4(v[4], v[5], v[6], v[7]);
+              float4* dst = reinterpret_cast<float4*>((direct ? static_cast<float*>(p.out) + orow * LYNX_D : part) + d);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) dst[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
             }
           }
         }
-        if (g == 0 && r < rows) {
+        if (half == 0 && r < rows) {
           if (!direct) *reinterpret_cast<float2*>(part + 128) = make_float2(M, L);
           else if (p.lse) p.lse[orow] = L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
         }
-        if (g == 0 && r == 0 && u0 == 0 && !p.whole) p.seg[segment] = (uint32_t)first_cta << 16 | (uint32_t)n_contrib;
+        if (tid == 0 && u0 == 0 && !p.whole) p.seg[segment] = (uint32_t)first_cta << 16 | (uint32_t)n_contrib;
       }
+      // (the next piece's first product may take the accumulators once all have given it weights)
       tc_fence_before();
-      named_bar(1, 256);   // (both have read both accumulators and sums)
+      __syncwarp();
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
     pdl_trigger();
@@ -644,7 +629,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
-      {   // queries: a thread a row
+      float a;
+      {   // queries: a thread a row, all rows scaled by one power of two
         const int c = rb * kTile + kt, j = c / p.G;
         const uint4* src = p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (c - j * p.G)) * 16;
         const bool in = c < p.cols;
@@ -653,61 +639,78 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
 #pragma unroll 4
           for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
         }
-        const int e = amax > 0.0f ? max(-100, min(100, exponent_of(amax))) : 0;
+        const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
+        if (lane == 0) misc[16 + 4 * qi + (warp & 3)] = (int)wmax;
+        named_bar(8, 128);
+        volatile int* qm = misc + 16 + 4 * qi;
+        const int top = max(max(qm[0], qm[1]), max(qm[2], qm[3]));
+        const int e = top > 0 ? max(-100, min(100, exponent_of(__int_as_float(top)))) : 0;
         const float f = pow2(-e);
+        a = p.sm_log2 * pow2(e);
         if (gs > 0) wait(sfull + ((gs - 1) & 1) * 8, ((gs - 1) >> 1) & 1, ab);   // the previous piece's last Q K^T
-#pragma unroll 4
-        for (int ch = 0; ch < 16; ++ch) {
-          uint4 w = make_uint4(0u, 0u, 0u, 0u);
-          if (in) {
-            w = ld_dep(src + ch);
-            sum += ((bf_lo(w.x) + bf_hi(w.x)) + (bf_lo(w.y) + bf_hi(w.y))) + ((bf_lo(w.z) + bf_hi(w.z)) + (bf_lo(w.w) + bf_hi(w.w)));
-            w = scaled8(w, f);
+        tc_fence_after();
+        const uint32_t tm_q = tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16);
+#pragma unroll 1
+        for (int ch = 0; ch < 16; ch += 4) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            if (in) x = ld_dep(src + ch + i);
+            sum += ((bf_lo(x.x) + bf_hi(x.x)) + (bf_lo(x.y) + bf_hi(x.y))) + ((bf_lo(x.z) + bf_hi(x.z)) + (bf_lo(x.w) + bf_hi(x.w)));
+            x = scaled8(x, f);
+            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
           }
-          sts128(chunk_at(sbase + C::kOffQ, kt, ch), w.x, w.y, w.z, w.w);
+          TmemRegs<16>::st(tm_q + ch * 4, w);
         }
-        reinterpret_cast<float2*>(smem + C::kOffRow)[qi * 128 + kt] = make_float2(p.sm_log2 * pow2(e), sum * f);
+        tc_wait_st();
+        reinterpret_cast<float*>(smem + C::kOffRow)[qi * 128 + kt] = sum * f;
       }
-      float2 m = make_float2(0.0f, 0.0f);
-      auto fetch = [&](int ut) {   // scale and zero point of this thread's token of a tile
+      // scale and zero point of this thread's token, a tile ahead, and its block, two ahead
+      const int64_t ids = (int64_t)b * p.max_blocks;
+      auto id_of = [&](int ut) { const int t = ut * kTile + kt; return t < len ? ld_dep(p.table + ids + quotient(t, p.bt_div)) : 0; };
+      auto meta_of = [&](int ut, int id) {
         const int t = ut * kTile + kt;
-        m = make_float2(0.0f, 0.0f);
-        if (t < len) m = ld_dep(p.km + row_at(p, block_id(p, b, t), h, t));
+        return t < len ? ld_dep(p.km + row_at(p, id, h, t)) : make_float2(0.0f, 0.0f);
       };
-      fetch(u0);
+      float2 m = meta_of(u0, id_of(u0));
+      int id = id_of(u0 + 1);
+#pragma unroll 1
       for (int u = 0; u < n; ++u, ++gs) {
         const int g = gs & 1, ut = u0 + u;
+        const uint32_t tile = sbase + C::kOffK + (uint32_t)g * 32768u;
         const float2 cur = m;
-        fetch(ut + 1);   // (nothing beyond the prefix)
-        wait(pready + g * 8, ((gs >> 1) - 1) & 1, ab);                                    // this place's scalars have been used
-        if (gs > 0) wait(sfull + (g ^ 1) * 8, ((gs - 1) >> 1) & 1, ab);                   // the tile has been used
+        m = meta_of(ut + 1, id);
+        id = id_of(ut + 2);
+        float sk = cur.x, mk = fmaf(128.0f, cur.x, cur.y);
+        wait(sfull + g * 8, ((gs >> 1) - 1) & 1, ab);                                     // the tile has been used
         if (ut < n_prefix) {
           wait(kfull + slot * 8, phase, ab);
-          expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, sbase + C::kOffK, 0u, kt);
-          tok[g * 256] = cur.x;
-          tok[g * 256 + 2] = fmaf(128.0f, cur.x, cur.y);
+          expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, 0u, kt);
           __syncwarp();
           if (lane == 0) mbar_arrive(kempty + slot * 8);
           if (++slot == C::kRingK) { slot = 0; phase ^= 1; }
-        } else {   // the nodes' keys: a thread a row, scaled like the queries
-          float f = 0.0f;
+        } else {   // the nodes' keys: a thread a row, scaled by a power of two
+          sk = mk = 0.0f;
           if (kt < p.n) {
             const uint4* src = p.kt + ((int64_t)b * p.n + kt) * p.kt_stride + h * 16;
             float amax = 0.0f;
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
             const int e = amax > 0.0f ? max(-100, min(100, exponent_of(amax))) : 0;
-            f = pow2(e);
+            sk = pow2(e);
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
               const uint4 w = scaled8(ld_dep(src + ch), pow2(-e));
-              sts128(chunk_at(sbase + C::kOffK, kt, ch), w.x, w.y, w.z, w.w);
+              sts128(chunk_at(tile, kt, ch), w.x, w.y, w.z, w.w);
             }
           }
-          tok[g * 256] = f;
-          tok[g * 256 + 2] = 0.0f;
         }
+        wait(pready + g * 8, ((gs >> 1) - 1) & 1, ab);                                    // this place's scalars have been used
+        tok[g * 256] = sk * a;
+        tok[g * 256 + 2] = mk * a;
         proxy_fence();
+        tc_fence_before();   // (the queries)
         __syncwarp();
         if (lane == 0) mbar_arrive(kready + g * 8);
       }
@@ -727,19 +730,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h;
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
-      float2 m = make_float2(0.0f, 0.0f);
-      auto fetch = [&](int ut) {
+      const int64_t ids = (int64_t)b * p.max_blocks;   // (as for K)
+      auto id_of = [&](int ut) { const int t = ut * kTile + vt; return t < len ? ld_dep(p.table + ids + quotient(t, p.bt_div)) : 0; };
+      auto meta_of = [&](int ut, int id) {
         const int t = ut * kTile + vt;
-        m = make_float2(0.0f, 0.0f);
-        if (t < len) m = ld_dep(p.vm + row_at(p, block_id(p, b, t), h, t));
+        return t < len ? ld_dep(p.vm + row_at(p, id, h, t)) : make_float2(0.0f, 0.0f);
       };
-      fetch(u0);
+      float2 m = meta_of(u0, id_of(u0));
+      int id = id_of(u0 + 1);
+#pragma unroll 1
       for (int u = 0; u < n; ++u, ++gs) {
         const int g = gs & 1, ut = u0 + u;
         const bool tree = ut == n_prefix;
         const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u, vmeta = sbase + C::kOffVm + (uint32_t)g * 512u;
         const float mid = fmaf(128.0f, m.x, m.y), scale = m.x;
-        fetch(ut + 1);
+        m = meta_of(ut + 1, id);
+        id = id_of(ut + 2);
         // the largest magnitude of the tile, and with it the exponent
         float amax = fabsf(mid) + 128.0f * fabsf(scale);
         bool used = false;
@@ -847,7 +853,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   // ================================================================================== products
   if (warp == 18) {
     constexpr uint32_t kIdescS = tc_idesc(128, false), kIdescO = tc_idesc(128, true);
-    const uint32_t q_lo = desc_lo(sbase + C::kOffQ, 16u), k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 16384u);
+    const uint32_t k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 16384u);
     struct { int ic, n, u, gs; } s = {0, 0, 0, 0};   // the next Q K^T
     bool more = true;
     auto qk = [&]() {
@@ -859,14 +865,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         if (s.n == 0) { more = false; return; }
       }
       const int g = s.gs & 1;
-      wait(kready + g * 8, (s.gs >> 1) & 1, ab);
+      wait(kready + g * 8, (s.gs >> 1) & 1, ab);   // (and with it the weights that lay in the scores' place: see pready)
       tc_fence_after();
       if (tc_elect()) {
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          const uint32_t o = (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4);
-          tc_mma_ss(tmem0 + C::kTmS + g * 128, desc(q_lo + o), desc(k_lo + o), kIdescS, ks > 0 ? 1u : 0u);
-        }
+        for (int ks = 0; ks < 8; ++ks)
+          tc_mma_ts(tmem0 + C::kTmS + g * 128, tmem0 + C::kTmQ + ks * 8, desc(k_lo + g * 2048u + (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4)),
+                    kIdescS, ks > 0 ? 1u : 0u);
         tc_commit(sfull + g * 8);
       }
       __syncwarp();
@@ -874,30 +879,31 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       ++s.gs;
     };
     qk();
-    if (more) qk();
     int gs = 0;
+#pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0;
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
+#pragma unroll 1
       for (int u = 0; u < n; ++u, ++gs) {
         const int g = gs & 1, ut = u0 + u;
         const int steps = ((ut == n_prefix ? p.n : min(kTile, len - ut * kTile)) + 15) / 16;
+        if (more && s.u < s.n) qk();   // (the piece's next scores; the next piece's behind this one's last product)
         wait(vready + g * 8, (gs >> 1) & 1, ab);
         wait(pready + g * 8, (gs >> 1) & 1, ab);
         tc_fence_after();
         if (tc_elect()) {
           for (int ks = 0; ks < steps; ++ks)
-            tc_mma_ts(tmem0 + C::kTmO + g * 128, tmem0 + C::kTmS + g * 128 + ks * 8, desc(v_lo + g * 2048u + ks * 128u), kIdescO,
-                      u > 1 || ks > 0 ? 1u : 0u);
+            tc_mma_ts(tmem0 + C::kTmO, tmem0 + C::kTmS + g * 128 + ks * 8, desc(v_lo + g * 2048u + ks * 128u), kIdescO, u > 0 || ks > 0 ? 1u : 0u);
           tc_commit(pvdone + g * 8);
         }
         __syncwarp();
-        if (u == n - 1 && lane == 0) mbar_arrive(iempty + qi * 8);   // (in front of a wait for the piece after next)
-        if (more) qk();
       }
+      if (lane == 0) mbar_arrive(iempty + qi * 8);
+      if (more) qk();
     }
     bar_arrive(2, kDoneThreads);
   }
