@@ -20,6 +20,7 @@
 //   warps 12-15      V codes to FP16 values into the V tiles
 //   warps 16, 17     bulk copies of 16-token sub-blocks of the K and V planes into rings; warp 16 deals out the pieces
 //   warp 18          issues every tcgen05.mma: Q K^T a tile ahead of P V
+//   warp 19          scales and zero points of a tile: what the softmax and the V tile need of them
 // Work is cut in stream-K form: the (sequence, KV head, row block, tile) list into equal ranges, a piece being a range's part of one
 // segment.  A segment within one CTA is written by it; otherwise partial (ref, l, O) go to the workspace and a dependent
 // kernel joins them.
@@ -55,7 +56,7 @@ struct TreeParams {
   float* lse;                       // [B][n][Hq] or NULL
   uint32_t* flags;
   uint32_t* seg;                    // [segments] first CTA << 16 | CTAs
-  float* part;                      // [segments + CTAs][part_rows][kPartRow], slot = segment + CTA
+  float* part;                      // [segments + CTAs][part_rows][kPartRow], slot = segment + CTA (see TS)
   float sm_log2;
   int B, n, Hq, Hkv, G, bt, num_blocks, max_blocks, cols, RB, part_rows, out_f32;
   int whole;                        // CTA i takes segment i
@@ -63,9 +64,13 @@ struct TreeParams {
   BlockDiv bt_div;
 };
 
-template <bool FULL>
+// TS: where there are no more than 128 / TS rows, a row lies in TS lanes of tensor memory, which take the tokens of a tile in TS parts, with
+// references, sums and accumulators of their own; the joining kernel adds them up.  The softmax of a tile is then spread over all warps.
+template <bool FULL, int TS>
 struct Cfg {
-  static constexpr int kStage = FULL ? 16384 : 8192;                 // planes of one tensor and tile: [planes][128 tokens][64 B]
+  static constexpr int kRows = kTile / TS, kW = 64 / TS;             // rows of a row block; scores of a thread and tile
+  static constexpr int kPlanes = FULL ? 16384 : 8192;                // of one tensor and tile: [planes][128 tokens][64 B]
+  static constexpr int kStage = kPlanes + 1024;                      // and [128] {scale, zero}
   static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 5;
   static constexpr int kOffK = 0, kOffV = kOffK + 65536, kOffRK = kOffV + 65536, kOffRV = kOffRK + kRingK * kStage,
                        kOffTok = kOffRV + kRingV * kStage;           // [2][64 token pairs] {scale, scale, mid, mid}
@@ -75,11 +80,11 @@ struct Cfg {
   static constexpr int kOffItems = kOffX + 4 * 512;                  // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
   static constexpr int kOffBars = kOffMisc + 128;
-  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 16;
+  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 20;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024, "shared memory");
-  // registers a thread after the split (launched with 96 each): 256 * 152 + 256 * 72 + 128 * 32 = 640 * 96
-  static constexpr int kRegSoft = 152, kRegExp = 72, kRegRest = 32;
+  // registers a thread after the split (launched with 96 each): 256 * 144 + 256 * 72 + 128 * 48 = 640 * 96
+  static constexpr int kRegSoft = 144, kRegExp = 72, kRegRest = 48;
   static constexpr int kTmS = 0, kTmO = 256, kTmQ = 384;             // [2][128] scores, weights in their place; accumulators; queries
 };
 
@@ -238,8 +243,10 @@ __device__ __forceinline__ float absmax8(const uint4& w) {
   for (int i = 0; i < 4; ++i) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v[i] & 0x7FFF7FFFu));
   return fmaxf(bf_lo(m), bf_hi(m));
 }
-// Exponent that brings the largest of a set to [2^14, 2^15).
+// Exponent that brings the largest of a set to [2^14, 2^15); of a tile's values, from the bits of the largest.
 __device__ __forceinline__ int exponent_of(float amax) { return ((__float_as_int(amax) >> 23) & 0xFF) - 127 - 14; }
+
+__device__ __forceinline__ int value_exponent(int bits) { return min(max(exponent_of(__int_as_float(bits)), kMinExp), 113); }
 
 // A tile's codes by 128 threads: thread i takes the 16-byte chunk i & 3 (32 channels) of rows (i >> 2) + 32 j.  Half of the threads take a
 // chunk's 8-byte halves in the other order: the eight threads of a store's phase then have eight chunk positions, and rows that share
@@ -398,35 +405,37 @@ __device__ __forceinline__ int64_t row_at(const TreeParams& p, int id, int h, in
 }
 
 // ------------------------------------------------------------------ the kernel
-template <bool FULL>
+template <bool FULL, int TS>
 __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __grid_constant__ TreeParams p) {
-  using C = Cfg<FULL>;
+  using C = Cfg<FULL, TS>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t sbase = smem_u32(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
-  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + g] exponents, [8..15] V maxima, [16 + 4 piece + i] q maxima
+  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + g] exponents, [8 + i] V maxima, [16 + 4 piece + i] q maxima, [24 + piece] scores' factor
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
-  const uint32_t kready = vempty + 8 * C::kRingV, sfull = kready + 16, eready = sfull + 16, vready = eready + 16, pready = vready + 16,
-                 pvdone = pready + 16, ifull = pvdone + 16, iempty = ifull + 16;
+  const uint32_t kready = vempty + 8 * C::kRingV, sfull = kready + 16, mready = sfull + 16, vready = mready + 16, pready = vready + 16,
+                 pvdone = pready + 16, ifull = pvdone + 16, iempty = ifull + 16, qready = iempty + 16, kdone = qready + 16;
   volatile int* ab = misc;        // (waits for data)
   volatile int* iab = misc + 1;   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
 
   if (tid == 0) {
-    for (int i = 0; i < C::kRingK; ++i) { mbar_init(kfull + i * 8, 1); mbar_init(kempty + i * 8, 4); }
-    for (int i = 0; i < C::kRingV; ++i) { mbar_init(vfull + i * 8, 1); mbar_init(vempty + i * 8, 4); }
+    for (int i = 0; i < C::kRingK; ++i) { mbar_init(kfull + i * 8, 1); mbar_init(kempty + i * 8, 5); }
+    for (int i = 0; i < C::kRingV; ++i) { mbar_init(vfull + i * 8, 1); mbar_init(vempty + i * 8, 5); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(kready + i * 8, 4);
       mbar_init(sfull + i * 8, 1);
-      mbar_init(eready + i * 8, 4);
+      mbar_init(mready + i * 8, 1);
+      mbar_init(qready + i * 8, 4);
+      mbar_init(kdone + i * 8, 4);
       mbar_init(vready + i * 8, 4);
       mbar_init(pready + i * 8, 8);
       mbar_init(pvdone + i * 8, 1);
       mbar_init(ifull + i * 8, 1);
-      mbar_init(iempty + i * 8, 8 + 4 + 4 + 1 + 1);   // softmax, K, V, V copies, products
+      mbar_init(iempty + i * 8, 8 + 4 + 4 + 3);   // softmax, K, V, V copies, products, scales
     }
     for (int i = 0; i < 32; ++i) misc_s[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -455,51 +464,58 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
       if (n == 0) break;
       const int first_cta = items[qi].first_cta, n_contrib = items[qi].n_contrib;
-      const int c = rb * kTile + r, rows = min(kTile, p.cols - rb * kTile), j = c / p.G, hq = h * p.G + (c - j * p.G);
+      const int c = rb * kTile + (r & (C::kRows - 1)), j = c / p.G, hq = h * p.G + (c - j * p.G);
       const int n_prefix = (len + kTile - 1) / kTile;
-      const bool works = w4 * 32 < rows;
+      const bool works = rb * kTile + ((w4 * 32) & (C::kRows - 1)) < p.cols;
       bool fresh = true;
       float ref = 0.0f, l = 0.0f, qs = 0.0f;
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gs) {
         const int g = gs & 1;
         const uint32_t ph = (gs >> 1) & 1;
-        wait(kready + g * 8, ph, ab);
-        wait(eready + g * 8, ph, ab);
+        // (No barrier may be more than a phase further than a wait expects: kready, say, which the K warps give again as soon as the
+        // scores are there, is not waited for here.)
+        if (u == 0) wait(qready + qi * 8, (ic >> 1) & 1, ab);
+        wait(mready + g * 8, ph, ab);
+        if (u0 + u == n_prefix) {   // the nodes' scalars, the exponent of their values
+          wait(kdone + qi * 8, (ic >> 1) & 1, ab);
+          wait(vready + g * 8, ph, ab);
+        }
         wait(sfull + g * 8, ph, ab);
         tc_fence_after();
         if (works) {
           if (u == 0) qs = reinterpret_cast<const float*>(smem + C::kOffRow)[qi * 128 + r];
           const int ut = u0 + u;
           const bool tree = ut == n_prefix;
-          const int valid = (tree ? p.n : min(kTile, len - ut * kTile)) - 64 * half;   // of this half
+          const int t0 = (r / C::kRows) * (kTile / TS) + half * C::kW;                 // this thread's first token
+          const int valid = (tree ? p.n : min(kTile, len - ut * kTile)) - t0;
           const int e = misc[4 + g];
           const float bias = (float)e - ref;
-          const uint32_t tm_s = tmem0 + C::kTmS + g * 128 + lanes, tok = sbase + C::kOffTok + (uint32_t)(g * 1024 + half * 512);
-          float x[64];
+          const uint32_t tm_s = tmem0 + C::kTmS + g * 128 + lanes, tok = sbase + C::kOffTok + (uint32_t)(g * 1024 + t0 * 8);
+          float x[C::kW];
           float mx = -INFINITY;
           if (valid > 0) {
             const uint64_t qs2 = f2_pack(qs, qs), b2 = f2_pack(bias, bias);
             uint32_t* sx = reinterpret_cast<uint32_t*>(x);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) TmemRegs<16>::ld(tm_s + half * 64 + k * 16, sx + 16 * k);
+            for (int k = 0; k < C::kW / 16; ++k) TmemRegs<16>::ld(tm_s + t0 + k * 16, sx + 16 * k);
             tc_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
+            for (int k = 0; k < C::kW / 2; ++k) {
               const uint4 t = lds128(tok + k * 16);
               const uint64_t sk = (uint64_t)t.y << 32 | t.x, mk = (uint64_t)t.w << 32 | t.z;
               f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), sk, f2_fma(mk, qs2, b2)), x[2 * k], x[2 * k + 1]);
             }
-            if (tree || valid < 64) {
-              unsigned long long see = tree ? (c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) : 0ull) : ~0ull;
+            if (tree || valid < C::kW) {   // (nodes: valid > 0, so t0 < 64)
+              unsigned long long see = tree ? (c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) >> t0 : 0ull) : ~0ull;
               if (valid < 64) see &= (1ull << valid) - 1ull;
 #pragma unroll
-              for (int k = 0; k < 64; ++k)
+              for (int k = 0; k < C::kW; ++k)
                 if (!((see >> k) & 1ull)) x[k] = -INFINITY;
             }
             float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int k = 0; k < 32; ++k) m4[k & 3] = max3(m4[k & 3], x[2 * k], x[2 * k + 1]);
+            for (int k = 0; k < C::kW / 2; ++k) m4[k & 3] = max3(m4[k & 3], x[2 * k], x[2 * k + 1]);
             mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
           }
           // (behind the vote both halves' scores are in registers: weights may go over them)
@@ -512,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             const float delta = need ? mx - kTop : 0.0f, f = fresh ? 1.0f : ex2(-delta);
             if (need) { ref += delta; fresh = false; }
 #pragma unroll
-            for (int k = 0; k < 64; ++k) x[k] -= delta;
+            for (int k = 0; k < C::kW; ++k) x[k] -= delta;
             l *= f;
             if (u > 0) {
               wait(pvdone + (g ^ 1) * 8, ((gs - 1) >> 1) & 1, ab);
@@ -528,22 +544,32 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               }
             }
           }
+          uint32_t w[C::kW / 2] = {};
           if (valid > 0) {
             uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              uint32_t w[16];
-#pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const float x0 = ex2(x[32 * i + 2 * k]), x1 = ex2(x[32 * i + 2 * k + 1]);
-                sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(x0, x1));
-                w[k] = pack_f16x2(x0, x1);
-              }
-              TmemRegs<16>::st(tm_s + half * 32 + i * 16, w);
+            for (int k = 0; k < C::kW / 2; ++k) {
+              const float x0 = ex2(x[2 * k]), x1 = ex2(x[2 * k + 1]);
+              sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(x0, x1));
+              w[k] = pack_f16x2(x0, x1);
+              if constexpr (TS == 1)
+                if (k == 15) TmemRegs<16>::st(tm_s + half * 32, w);
             }
             float s0, s1;
             f2_unpack(f2_add(sum2[0], sum2[1]), s0, s1);
             l = fmaf(s0 + s1, pow2(-e), l);
+          }
+          // (the lanes' other parts of the tile have no weight)
+          if constexpr (TS == 1) {
+            if (valid > 0) TmemRegs<16>::st(tm_s + half * 32 + 16, w + 16);
+          } else {
+#pragma unroll
+            for (int i = 0; i < TS; ++i) {
+              uint32_t z[C::kW / 2];
+#pragma unroll
+              for (int k = 0; k < C::kW / 2; ++k) z[k] = i == r / C::kRows ? w[k] : 0u;
+              TmemRegs<C::kW / 2>::st(tm_s + i * (64 / TS) + half * (32 / TS), z);
+            }
           }
           tc_wait_st();
         }
@@ -558,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         xs[256 + half * 128 + r] = l;
         named_bar(bar, 64);
         const float L = l + xs[256 + (half ^ 1) * 128 + r], M = fresh ? -INFINITY : ref;
-        const bool direct = n_contrib == 1;
+        const bool direct = TS == 1 && n_contrib == 1;
         const float w = L > 0.0f ? (direct ? 1.0f / L : 1.0f) : 0.0f;
         const int64_t orow = ((int64_t)b * p.n + j) * p.Hq + hq;
         const int segment = (b * p.Hkv + h) * p.RB + rb;
@@ -574,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             const int at = (k & 8) | ((k & 1) << 2) | (k & 2) | ((k >> 2) & 1);
             v[k] = __uint_as_float(o[at]) * w;
           }
-          if (r < rows) {
+          if (c < p.cols) {
             const int d = half * 64 + i;
             if (direct && !p.out_f32) {
               uint32_t x[8];
@@ -593,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             }
           }
         }
-        if (half == 0 && r < rows) {
+        if (half == 0 && c < p.cols) {
           if (!direct) *reinterpret_cast<float2*>(part + 128) = make_float2(M, L);
           else if (p.lse) p.lse[orow] = L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
         }
@@ -631,7 +657,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n_prefix = (len + kTile - 1) / kTile;
       float a;
       {   // queries: a thread a row, all rows scaled by one power of two
-        const int c = rb * kTile + kt, j = c / p.G;
+        const int c = rb * kTile + (kt & (C::kRows - 1)), j = c / p.G;
         const uint4* src = p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (c - j * p.G)) * 16;
         const bool in = c < p.cols;
         float amax = 0.0f, sum = 0.0f;
@@ -647,6 +673,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         const int e = top > 0 ? max(-100, min(100, exponent_of(__int_as_float(top)))) : 0;
         const float f = pow2(-e);
         a = p.sm_log2 * pow2(e);
+        if (kt == 0) misc[24 + qi] = __float_as_int(a);
         if (gs > 0) wait(sfull + ((gs - 1) & 1) * 8, ((gs - 1) >> 1) & 1, ab);   // the previous piece's last Q K^T
         tc_fence_after();
         const uint32_t tm_q = tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16);
@@ -665,24 +692,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
         tc_wait_st();
         reinterpret_cast<float*>(smem + C::kOffRow)[qi * 128 + kt] = sum * f;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(qready + qi * 8);
       }
-      // scale and zero point of this thread's token, a tile ahead, and its block, two ahead
-      const int64_t ids = (int64_t)b * p.max_blocks;
-      auto id_of = [&](int ut) { const int t = ut * kTile + kt; return t < len ? ld_dep(p.table + ids + quotient(t, p.bt_div)) : 0; };
-      auto meta_of = [&](int ut, int id) {
-        const int t = ut * kTile + kt;
-        return t < len ? ld_dep(p.km + row_at(p, id, h, t)) : make_float2(0.0f, 0.0f);
-      };
-      float2 m = meta_of(u0, id_of(u0));
-      int id = id_of(u0 + 1);
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gs) {
         const int g = gs & 1, ut = u0 + u;
         const uint32_t tile = sbase + C::kOffK + (uint32_t)g * 32768u;
-        const float2 cur = m;
-        m = meta_of(ut + 1, id);
-        id = id_of(ut + 2);
-        float sk = cur.x, mk = fmaf(128.0f, cur.x, cur.y);
         wait(sfull + g * 8, ((gs >> 1) - 1) & 1, ab);                                     // the tile has been used
         if (ut < n_prefix) {
           wait(kfull + slot * 8, phase, ab);
@@ -691,7 +707,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           if (lane == 0) mbar_arrive(kempty + slot * 8);
           if (++slot == C::kRingK) { slot = 0; phase ^= 1; }
         } else {   // the nodes' keys: a thread a row, scaled by a power of two
-          sk = mk = 0.0f;
+          float sk = 0.0f;
           if (kt < p.n) {
             const uint4* src = p.kt + ((int64_t)b * p.n + kt) * p.kt_stride + h * 16;
             float amax = 0.0f;
@@ -705,16 +721,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               sts128(chunk_at(tile, kt, ch), w.x, w.y, w.z, w.w);
             }
           }
+          wait(pready + g * 8, ((gs >> 1) - 1) & 1, ab);                                  // this place's scalars have been used
+          tok[g * 256] = sk * a;
+          tok[g * 256 + 2] = 0.0f;
         }
-        wait(pready + g * 8, ((gs >> 1) - 1) & 1, ab);                                    // this place's scalars have been used
-        tok[g * 256] = sk * a;
-        tok[g * 256 + 2] = mk * a;
         proxy_fence();
         tc_fence_before();   // (the queries)
         __syncwarp();
         if (lane == 0) mbar_arrive(kready + g * 8);
       }
-      if (lane == 0) mbar_arrive(iempty + qi * 8);
+      if (lane == 0) { mbar_arrive(kdone + qi * 8); mbar_arrive(iempty + qi * 8); }
     }
     return;
   }
@@ -730,27 +746,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h;
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
-      const int64_t ids = (int64_t)b * p.max_blocks;   // (as for K)
-      auto id_of = [&](int ut) { const int t = ut * kTile + vt; return t < len ? ld_dep(p.table + ids + quotient(t, p.bt_div)) : 0; };
-      auto meta_of = [&](int ut, int id) {
-        const int t = ut * kTile + vt;
-        return t < len ? ld_dep(p.vm + row_at(p, id, h, t)) : make_float2(0.0f, 0.0f);
-      };
-      float2 m = meta_of(u0, id_of(u0));
-      int id = id_of(u0 + 1);
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gs) {
         const int g = gs & 1, ut = u0 + u;
-        const bool tree = ut == n_prefix;
         const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u, vmeta = sbase + C::kOffVm + (uint32_t)g * 512u;
-        const float mid = fmaf(128.0f, m.x, m.y), scale = m.x;
-        m = meta_of(ut + 1, id);
-        id = id_of(ut + 2);
-        // the largest magnitude of the tile, and with it the exponent
-        float amax = fabsf(mid) + 128.0f * fabsf(scale);
-        bool used = false;
-        const uint4* src = p.vt + ((int64_t)b * p.n + vt) * p.vt_stride + h * 16;
-        if (tree) {
+        wait(mready + g * 8, (gs >> 1) & 1, ab);
+        if (ut < n_prefix) {
+          wait(vfull + slot * 8, phase, ab);
+          wait(pvdone + g * 8, ((gs >> 1) - 1) & 1, ab);   // the tile has been used
+          expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, vmeta, vt);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(vempty + slot * 8);
+          if (++slot == C::kRingV) { slot = 0; phase ^= 1; }
+        } else {
           uint32_t lo = 0u, hi = 0u;   // nodes that some row sees (the others' values may be anything)
           for (int i = lane; i < p.n; i += 32) {
             const unsigned long long x = ld_dep(p.mask + (int64_t)b * p.n + i);
@@ -759,37 +767,26 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           }
           lo = __reduce_or_sync(0xFFFFFFFFu, lo);
           hi = __reduce_or_sync(0xFFFFFFFFu, hi);
-          used = vt < p.n && (((vt < 32 ? lo : hi) >> (vt & 31)) & 1u);
-          amax = 0.0f;
+          const bool used = vt < p.n && (((vt < 32 ? lo : hi) >> (vt & 31)) & 1u);
+          const uint4* src = p.vt + ((int64_t)b * p.n + vt) * p.vt_stride + h * 16;
+          float amax = 0.0f;
           if (used) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
           }
-        }
-        const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
-        if (lane == 0) misc[8 + 4 * g + w4] = (int)wmax;
-        named_bar(3, 128);
-        const int top = max(max(misc[8 + 4 * g], misc[9 + 4 * g]), max(misc[10 + 4 * g], misc[11 + 4 * g]));
-        const int e = min(max(exponent_of(__int_as_float(top)), kMinExp), 113);
-        const float f = pow2(-e);
-        wait(pvdone + g * 8, ((gs >> 1) - 1) & 1, ab);   // the tile, and the exponent with it, has been used
-        if (vt == 0) misc[4 + g] = e;
-        if (!tree)
-          *reinterpret_cast<uint32_t*>(smem + C::kOffVm + g * 512 + vt * 4) = pack_f16x2(scale * f, mid * f);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(eready + g * 8);
-        if (!tree) {
+          const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
+          if (lane == 0) misc[8 + w4] = (int)wmax;
           named_bar(3, 128);
-          wait(vfull + slot * 8, phase, ab);
-          expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, vmeta, vt);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(vempty + slot * 8);
-          if (++slot == C::kRingV) { slot = 0; phase ^= 1; }
-        } else if (vt < ((p.n + 15) & ~15)) {
+          const int e = value_exponent(max(max(misc[8], misc[9]), max(misc[10], misc[11])));
+          named_bar(3, 128);   // (read by all)
+          wait(pvdone + g * 8, ((gs >> 1) - 1) & 1, ab);   // the tile, and the exponent with it, has been used
+          if (vt == 0) misc[4 + g] = e;
+          if (vt < ((p.n + 15) & ~15)) {
 #pragma unroll 4
-          for (int ch = 0; ch < 16; ++ch) {
-            const uint4 w = used ? scaled8(ld_dep(src + ch), f) : make_uint4(0u, 0u, 0u, 0u);
-            sts128(chunk_at(tile, vt, ch), w.x, w.y, w.z, w.w);
+            for (int ch = 0; ch < 16; ++ch) {
+              const uint4 w = used ? scaled8(ld_dep(src + ch), pow2(-e)) : make_uint4(0u, 0u, 0u, 0u);
+              sts128(chunk_at(tile, vt, ch), w.x, w.y, w.z, w.w);
+            }
           }
         }
         proxy_fence();
@@ -806,7 +803,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     const bool k_side = warp == 16;
     const int ring = k_side ? C::kRingK : C::kRingV;
     const uint32_t full = k_side ? kfull : vfull, empty = k_side ? kempty : vempty, stages = sbase + (k_side ? C::kOffRK : C::kOffRV);
-    const uint8_t* plane = k_side ? (lane < 8 ? p.ka : p.kr) : (lane < 8 ? p.va : p.vr);
+    // lane: sub-block lane & 7 of the Anchor, the Residual or the scalars
+    const int what = lane >> 3, kind = !FULL && what == 1 ? 2 : what;
+    const uint8_t* plane = kind == 0 ? (k_side ? p.ka : p.va) : kind == 1 ? (k_side ? p.kr : p.vr) : reinterpret_cast<const uint8_t*>(k_side ? p.km : p.vm);
+    const uint32_t row_bytes = kind == 2 ? 8u : 64u, at = (kind == 2 ? (uint32_t)C::kPlanes : (uint32_t)kind * 8192u) + (uint32_t)(lane & 7) * 16u * row_bytes;
     Cursor cur = {0, 0, 0, 0, 0, 0};
     if (k_side) cur = first_unit(p, blockIdx.x, gridDim.x, lane);
     int slot = 0;
@@ -830,7 +830,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       }
       if (it.n == 0) break;
       const int n_prefix = (it.len + kTile - 1) / kTile, last = min(it.u0 + it.n, n_prefix), off = (lane & 7) * 16;
-      const bool copies = lane < (FULL ? 16 : 8);
+      const bool copies = lane < (FULL ? 24 : 16);
       int id = 0;
       if (copies && it.u0 * kTile + off < it.len) id = block_id(p, it.b, it.u0 * kTile + off);
       for (int ut = it.u0; ut < last; ++ut) {
@@ -838,16 +838,83 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         if (copies && t + kTile < it.len) id = block_id(p, it.b, t + kTile);
         wait(empty + slot * 8, phase, ab);
         const int subs = min(8, (it.len - ut * kTile + 15) / 16);   // sub-blocks of 16 tokens with a token of the sequence
-        if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)subs * (FULL ? 2048u : 1024u));
+        if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)subs * (FULL ? 2048u + 128u : 1024u + 128u));
         __syncwarp();
         if (copies && (lane & 7) < subs)
-          bulk_g2s(stages + (uint32_t)slot * C::kStage + (uint32_t)(lane >> 3) * 8192u + (uint32_t)(lane & 7) * 1024u,
-                   plane + row_at(p, now, it.h, t) * 64, 1024u, full + slot * 8);
+          bulk_g2s(stages + (uint32_t)slot * C::kStage + at, plane + row_at(p, now, it.h, t) * row_bytes, 16u * row_bytes, full + slot * 8);
         if (++slot == ring) { slot = 0; phase ^= 1; }
       }
       if (!k_side && lane == 0) mbar_arrive(iempty + qi * 8);
     }
     bar_arrive(2, kDoneThreads);
+    return;
+  }
+  // ================================================================================== scales and zero points
+  if (warp == 19) {
+    int gs = 0, kslot = 0, vslot = 0;
+    uint32_t kphase = 0, vphase = 0;
+#pragma unroll 1
+    for (int ic = 0;; ++ic) {
+      const int qi = ic & 1;
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
+      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0;
+      if (n == 0) break;
+      wait(qready + qi * 8, (ic >> 1) & 1, ab);
+      const float a = __int_as_float(misc[24 + qi]);
+      const int n_prefix = (len + kTile - 1) / kTile;
+#pragma unroll 1
+      for (int u = 0; u < n; ++u, ++gs) {
+        const int g = gs & 1, ut = u0 + u;
+        const uint32_t before = ((gs >> 1) - 1) & 1;
+        if (ut < n_prefix) {
+          // a lane takes four tokens, {scale, zero} of two in a register quadruple
+          wait(kfull + kslot * 8, kphase, ab);
+          wait(vfull + vslot * 8, vphase, ab);
+          const uint32_t ka = sbase + C::kOffRK + (uint32_t)kslot * C::kStage + C::kPlanes + (uint32_t)lane * 32u,
+                         va = sbase + C::kOffRV + (uint32_t)vslot * C::kStage + C::kPlanes + (uint32_t)lane * 32u;
+          uint4 k2[2] = {lds128(ka), lds128(ka + 16)}, v2[2] = {lds128(va), lds128(va + 16)};
+          const int room = len - ut * kTile - lane * 4;   // (what lies behind the sequence's end may be anything)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (room <= 2 * i) k2[i].x = k2[i].y = v2[i].x = v2[i].y = 0u;
+            if (room <= 2 * i + 1) k2[i].z = k2[i].w = v2[i].z = v2[i].w = 0u;
+          }
+          __syncwarp();
+          if (lane == 0) { mbar_arrive(kempty + kslot * 8); mbar_arrive(vempty + vslot * 8); }
+          if (++kslot == C::kRingK) { kslot = 0; kphase ^= 1; }
+          if (++vslot == C::kRingV) { vslot = 0; vphase ^= 1; }
+          float vs[4], vm[4], amax = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            vs[2 * i] = __uint_as_float(v2[i].x);
+            vs[2 * i + 1] = __uint_as_float(v2[i].z);
+            vm[2 * i] = fmaf(128.0f, vs[2 * i], __uint_as_float(v2[i].y));
+            vm[2 * i + 1] = fmaf(128.0f, vs[2 * i + 1], __uint_as_float(v2[i].w));
+            amax = max3(amax, fabsf(vm[2 * i]) + 128.0f * fabsf(vs[2 * i]), fabsf(vm[2 * i + 1]) + 128.0f * fabsf(vs[2 * i + 1]));
+          }
+          const int e = value_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax)));
+          const float f = pow2(-e);
+          wait(pready + g * 8, before, ab);   // these places have been read
+          wait(vready + g * 8, before, ab);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float s0 = __uint_as_float(k2[i].x) * a, s1 = __uint_as_float(k2[i].z) * a;
+            sts128(sbase + C::kOffTok + (uint32_t)(g * 1024 + lane * 32 + i * 16), __float_as_uint(s0), __float_as_uint(s1),
+                   __float_as_uint(fmaf(128.0f, s0, __uint_as_float(k2[i].y) * a)), __float_as_uint(fmaf(128.0f, s1, __uint_as_float(k2[i].w) * a)));
+          }
+          sts128(sbase + C::kOffVm + (uint32_t)(g * 512 + lane * 16), pack_f16x2(vs[0] * f, vm[0] * f), pack_f16x2(vs[1] * f, vm[1] * f),
+                 pack_f16x2(vs[2] * f, vm[2] * f), pack_f16x2(vs[3] * f, vm[3] * f));
+          if (lane == 0) misc[4 + g] = e;
+        } else {   // (the nodes': by the warps that have their keys and values.  They and the softmax wait for this warp all the same, so
+                   // that no barrier is a phase further than what a wait for it expects)
+          wait(pready + g * 8, before, ab);
+          wait(vready + g * 8, before, ab);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(mready + g * 8);
+      }
+      if (lane == 0) mbar_arrive(iempty + qi * 8);
+    }
     return;
   }
   // ================================================================================== products
@@ -910,7 +977,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
 }
 
 // Joins the partial results of the CTAs that share a segment, a warp per output row, a lane four channels.
-__global__ void __launch_bounds__(128) tree_combine_kernel(const __grid_constant__ TreeParams p, int n_cta) {
+__global__ void __launch_bounds__(128) tree_combine_kernel(const __grid_constant__ TreeParams p, int n_cta, int log_ts) {
   pdl_trigger();
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
@@ -921,10 +988,11 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(const __grid_constant
   const int c = j * p.G + (hq - h * p.G), rb = c / kTile, r = c - rb * kTile;
   const int segment = (b * p.Hkv + h) * p.RB + rb;
   const uint32_t info = ld_dep(p.seg + segment);
-  const int first = min((int)(info >> 16), n_cta - 1), n = min((int)(info & 0xFFFFu), n_cta - first);
+  const int first = min((int)(info >> 16), n_cta - 1), n = min((int)(info & 0xFFFFu), n_cta - first) << log_ts, ts = (1 << log_ts) - 1;
   if (n == 1) return;   // written by the attention kernel
   const int64_t slot = (int64_t)p.part_rows * kPartRow;
   const float* src = p.part + (int64_t)(segment + first) * slot + (int64_t)r * kPartRow;
+  const int64_t part = (int64_t)(kTile >> log_ts) * kPartRow;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float M = -INFINITY, L = 0.0f;
   constexpr int kFly = 6;
@@ -936,8 +1004,9 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(const __grid_constant
       ml[u] = make_float2(-INFINITY, 0.0f);
       o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (i0 + u < n) {
-        ml[u] = ld_dep(reinterpret_cast<const float2*>(src + (i0 + u) * slot + 128));
-        o[u] = ld_dep(reinterpret_cast<const float4*>(src + (i0 + u) * slot) + lane);
+        const float* x = src + ((i0 + u) >> log_ts) * slot + ((i0 + u) & ts) * part;
+        ml[u] = ld_dep(reinterpret_cast<const float2*>(x + 128));
+        o[u] = ld_dep(reinterpret_cast<const float4*>(x) + lane);
       }
     }
     const float m0 = M;
@@ -972,7 +1041,7 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(const __grid_constant
 constexpr int kWholeTiles = 3;   // up to so many tiles a CTA takes a whole segment
 
 struct TreePlan {
-  int cols, RB, part_rows, whole, grid, per_seg;
+  int cols, RB, part_rows, whole, grid, per_seg, log_ts;
   int64_t segs;
   size_t off_seg, off_part, bytes;
 };
@@ -985,11 +1054,12 @@ lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
   if (s->head_dim != LYNX_D || s->block_tokens % 16 || G > 16 || n > kMaxNodes || cap >= (1ll << 30)) return LYNX_ERR_UNSUPPORTED;
   pl->cols = n * G;
   pl->RB = (pl->cols + kTile - 1) / kTile;
-  pl->part_rows = pl->cols < kTile ? pl->cols : kTile;
   pl->segs = (int64_t)B * s->num_kv_heads * pl->RB;
   const int64_t tiles = (cap + kTile - 1) / kTile + 1, sms = sm_count();
   if (pl->segs >= (1 << 24) || pl->segs * tiles >= (1ll << 31)) return LYNX_ERR_UNSUPPORTED;
   pl->whole = tiles <= kWholeTiles;
+  pl->log_ts = pl->whole || pl->cols > 64 ? 0 : pl->cols > 32 ? 1 : 2;
+  pl->part_rows = pl->log_ts == 0 && pl->cols < kTile ? pl->cols : kTile;
   pl->per_seg = 0;
   if (pl->whole) {
     pl->grid = (int)pl->segs;
@@ -1004,14 +1074,14 @@ lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
   return LYNX_OK;
 }
 
-template <bool FULL>
+template <bool FULL, int TS>
 lynx_status launch_tree(const TreeParams& p, int grid, void* stream) {
-  using C = Cfg<FULL>;
-  if (cudaFuncSetAttribute(tree_attention_kernel<FULL>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
+  using C = Cfg<FULL, TS>;
+  if (cudaFuncSetAttribute(tree_attention_kernel<FULL, TS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
     launch_status();
     return LYNX_ERR_CUDA;
   }
-  return launch_pdl(tree_attention_kernel<FULL>, (unsigned)grid, kThreads, C::kSmem, stream, p);
+  return launch_pdl(tree_attention_kernel<FULL, TS>, (unsigned)grid, kThreads, C::kSmem, stream, p);
 }
 
 }  // namespace
@@ -1041,7 +1111,7 @@ extern "C" lynx_status lynx_tree_attention(const lynx_shape* shape, const void* 
   if (k_stride < least || v_stride < least || k_stride % 8 || v_stride % 8) return LYNX_ERR_SHAPE;
   const auto at = [](const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; };
   if (!aligned16(q_bf16) || !aligned16(K.anchor) || !aligned16(V.anchor) || !aligned16(K.residual) || !aligned16(V.residual) ||
-      !at(K.meta, 8) || !at(V.meta, 8) || !aligned16(k_nodes) || !aligned16(v_nodes) || !at(tree_mask, 8) || !aligned16(out) || !at(lse, 4) ||
+      !aligned16(K.meta) || !aligned16(V.meta) || !aligned16(k_nodes) || !aligned16(v_nodes) || !at(tree_mask, 8) || !aligned16(out) || !at(lse, 4) ||
       !at(block_table, 4) || !at(seq_lens, 4) || !aligned16(workspace))
     return LYNX_ERR_ALIGN;
   if (workspace_bytes < pl.bytes) return LYNX_ERR_WORKSPACE;
@@ -1064,8 +1134,10 @@ extern "C" lynx_status lynx_tree_attention(const lynx_shape* shape, const void* 
   p.cols = pl.cols; p.RB = pl.RB; p.part_rows = pl.part_rows; p.out_f32 = out_float ? 1 : 0;
   p.whole = pl.whole; p.per_seg = pl.per_seg;
   p.bt_div = block_div(p.bt);
-  const lynx_status st = K.residual ? launch_tree<true>(p, pl.grid, stream) : launch_tree<false>(p, pl.grid, stream);
+  const lynx_status st = pl.log_ts == 0 ? (K.residual ? launch_tree<true, 1>(p, pl.grid, stream) : launch_tree<false, 1>(p, pl.grid, stream))
+                         : pl.log_ts == 1 ? (K.residual ? launch_tree<true, 2>(p, pl.grid, stream) : launch_tree<false, 2>(p, pl.grid, stream))
+                                          : (K.residual ? launch_tree<true, 4>(p, pl.grid, stream) : launch_tree<false, 4>(p, pl.grid, stream));
   if (st != LYNX_OK || pl.whole) return st;
   const int64_t rows = (int64_t)batch * n_nodes * p.Hq;
-  return launch_pdl(tree_combine_kernel, (unsigned)((rows + 3) / 4), 128, 0, stream, p, pl.grid);
+  return launch_pdl(tree_combine_kernel, (unsigned)((rows + 3) / 4), 128, 0, stream, p, pl.grid, pl.log_ts);
 }
