@@ -1,15 +1,18 @@
 // lynx_tree_attention: attention of a tree of drafted tokens over the quantised cache and over each other (sm_100a).
 //
 // For every (sequence, KV head) the n nodes' G = Hq / Hkv query heads are n * G rows; they share the head's keys and values:
-//   S = Q K^T,   p = 2^(a_r S + e - ref_r),   O += P V,   l += sum p,   out = O / l
+//   S = Q K^T,   p = 2^(a S + e - ref_r),   O += P V,   l += sum p,   out = O / l
 // over the prefix (planes, 128 tokens a tile) and one last tile of the nodes' own BF16 keys and values under the tree's mask.
 //
-// Keys enter as their codes less 128, which FP16 holds exactly, and queries scaled by a power of two per row, exactly too:
-//   q . K^_t = scale_t (q . (c_t - 128)) + mid_t sum(q),   mid = zero + 128 scale,
-// so scores have FP32 sums and no rounding of an operand.  Values enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15
-// (rows 2^29 times smaller keep all 11 bits), weights as FP16 relative to a reference that keeps each row's largest between 2^8 and
-// 2^15.5: both roundings are 2^-12 of a term, an eighth of the output's own rounding to BF16.  2^e goes into the weight's exponent and out
-// of l's terms again, so that it costs nothing per weight.  Sums l, references and O are FP32.
+// A row of codes c is mid + scale (c - 128), mid = zero + 128 scale.  Keys enter as FP16 of scale (c - 128), an error of 2^-12 of a
+// key's deviation from the row's middle (an eighth of a code's step at most), and the middles, which may be far larger, as
+// rank-1 terms in 16 more elements of the contraction: mid x sum(q), both in two FP16 parts (2^-22).  Queries are scaled by a power of two, exact
+// down to 2^-24 of the row block's largest.  So a score needs one multiply-add in the softmax, with a factor that its whole tile shares
+// (per-token scales there are loads of shared memory for every score: 140 us instead of 112 for 128 rows over 131072 tokens).  Values
+// enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15 (rows 2^29 times smaller keep all 11 bits; keys 2^26), weights as
+// FP16 relative to a reference that keeps each row's largest between 2^8 and 2^15.5: both roundings are 2^-12 of a term, an eighth of the
+// output's own rounding to BF16.  2^e goes into the weight's exponent and out of l's terms again, so that it costs nothing per weight.  Sums
+// l, references and O are FP32.
 //
 // Layout: rows are the M = 128 lanes of tensor memory (n * G > 128 rows: more row blocks), tokens the N of the scores and the K of
 // P V.  Two threads share a row, one for each half of a tile's tokens; they exchange a vote per tile and their sums at the end.  Queries
@@ -42,7 +45,7 @@ constexpr int kPartRow = 132;       // floats of a partial row: O[128], referenc
 constexpr int kThreads = 640;
 constexpr int kDoneThreads = 256 + 3 * 32;   // softmax warpgroups, copies, products
 constexpr float kTop = 8.0f, kRaise = 15.5f; // log2 of a row's largest weight when its reference is set, and before it is set anew
-constexpr int kMinExp = -80;        // smallest exponent of a tile's values
+constexpr int kMinExp = -80;        // smallest exponent of a tile's keys or values
 
 struct TreeParams {
   const uint4* q;                   // [B][n][Hq][16 chunks]
@@ -71,16 +74,16 @@ struct Cfg {
   static constexpr int kRows = kTile / TS, kW = 64 / TS;             // rows of a row block; scores of a thread and tile
   static constexpr int kPlanes = FULL ? 16384 : 8192;                // of one tensor and tile: [planes][128 tokens][64 B]
   static constexpr int kStage = kPlanes + 1024;                      // and [128] {scale, zero}
-  static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 5;
+  static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 4;
   static constexpr int kOffK = 0, kOffV = kOffK + 65536, kOffRK = kOffV + 65536, kOffRV = kOffRK + kRingK * kStage,
-                       kOffTok = kOffRV + kRingV * kStage;           // [2][64 token pairs] {scale, scale, mid, mid}
-  static constexpr int kOffRow = kOffTok + 2 * 1024;                 // [2][128] sum of q
-  static constexpr int kOffVm = kOffRow + 2 * 512;                   // [2][128] half2 {scale, mid}
+                       kOffMid = kOffRV + kRingV * kStage;           // [2][128] the middles' 8 FP16, and 128 x 8 zeros
+  static constexpr int kOffKm = kOffMid + 3 * 2048;                  // [2][128] half2 {scale, - 1152 scale}
+  static constexpr int kOffVm = kOffKm + 2 * 512;                    // [2][128] half2 {scale, mid}
   static constexpr int kOffX = kOffVm + 2 * 512;                     // [2][128] maxima, [2][128] sums of the halves of a row
   static constexpr int kOffItems = kOffX + 4 * 512;                  // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
   static constexpr int kOffBars = kOffMisc + 128;
-  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 20;
+  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 22;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024, "shared memory");
   // registers a thread after the split (launched with 96 each): 256 * 144 + 256 * 72 + 128 * 48 = 640 * 96
@@ -206,6 +209,13 @@ __device__ __forceinline__ uint64_t desc(uint32_t lo) {
   return d;
 }
 
+// Without a swizzle: groups of eight rows of 16 bytes, 128 bytes apart.
+__device__ __forceinline__ uint64_t desc_plain(uint32_t lo) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"((128u >> 4) | (1u << 14)));
+  return d;
+}
+
 // ------------------------------------------------------------------ codes to FP16
 // Channels of a group of 8 in the order in which the nibbles come apart, 0 4 2 6 1 5 3 7 (its own inverse): all tiles have it.
 __device__ __forceinline__ uint32_t centred(uint32_t x) {   // 1024 + code -> code - 128
@@ -218,13 +228,13 @@ __device__ __forceinline__ uint32_t bit_select(uint32_t a, uint32_t b, uint32_t 
   asm("lop3.b32 %0, %1, %2, %3, 0xE4;" : "=r"(d) : "r"(a), "r"(b), "r"(mask));
   return d;
 }
-// Eight codes less 128 from a word of Anchor and a word of Residual nibbles (Anchor alone: residual word 0x88888888, the buckets' middles).
+// 1024 + eight codes from a word of Anchor and a word of Residual nibbles (Anchor alone: residual word 0x88888888, the buckets' middles).
 __device__ __forceinline__ void codes8(uint32_t xa, uint32_t xr, uint32_t* o) {
   const uint32_t ev = bit_select(xa << 4, xr, 0xF0F0F0F0u), od = bit_select(xa, xr >> 4, 0xF0F0F0F0u);
-  o[0] = centred((ev & 0x00FF00FFu) | 0x64006400u);
-  o[1] = centred(__byte_perm(ev, 0x64646464u, 0x4341));
-  o[2] = centred((od & 0x00FF00FFu) | 0x64006400u);
-  o[3] = centred(__byte_perm(od, 0x64646464u, 0x4341));
+  o[0] = (ev & 0x00FF00FFu) | 0x64006400u;
+  o[1] = __byte_perm(ev, 0x64646464u, 0x4341);
+  o[2] = (od & 0x00FF00FFu) | 0x64006400u;
+  o[3] = __byte_perm(od, 0x64646464u, 0x4341);
 }
 __device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d;
@@ -243,23 +253,32 @@ __device__ __forceinline__ float absmax8(const uint4& w) {
   for (int i = 0; i < 4; ++i) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v[i] & 0x7FFF7FFFu));
   return fmaxf(bf_lo(m), bf_hi(m));
 }
-// Exponent that brings the largest of a set to [2^14, 2^15); of a tile's values, from the bits of the largest.
+// Exponent that brings the largest of a set to [2^14, 2^15); of a tile, from the bits of the largest.
 __device__ __forceinline__ int exponent_of(float amax) { return ((__float_as_int(amax) >> 23) & 0xFF) - 127 - 14; }
 
-__device__ __forceinline__ int value_exponent(int bits) { return min(max(exponent_of(__int_as_float(bits)), kMinExp), 113); }
+__device__ __forceinline__ int tile_exponent(int bits) { return min(max(exponent_of(__int_as_float(bits)), kMinExp), 113); }
+
+// a 2^e, without infinities in between.
+__device__ __forceinline__ float times_pow2(float a, int e) { return a * pow2(max(e >> 1, -126)) * pow2(max(e - (e >> 1), -126)); }
+// Two FP16 parts of a value below 2^16: the nearest, and what is left.
+__device__ __forceinline__ uint32_t two_parts(float x) {
+  const float hi = __half2float(__float2half_rn(x));
+  return pack_f16x2(hi, x - hi);
+}
 
 // A tile's codes by 128 threads: thread i takes the 16-byte chunk i & 3 (32 channels) of rows (i >> 2) + 32 j.  Half of the threads take a
 // chunk's 8-byte halves in the other order: the eight threads of a store's phase then have eight chunk positions, and rows that share
 // their banks in the raw stage are read in different halves.
+// meta: per row, keys {scale, -1152 scale (rounded)} -> (1024 + c) scale - 1152 scale, values {scale, mid} -> (c - 128) scale + mid.
 template <bool FULL, bool VALUES>
-__device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t vmeta, int i) {
+__device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t meta, int i) {
   const int cc = i & 3, row0 = i >> 2;
   const uint32_t sw = (uint32_t)(((cc >> 1) ^ (row0 >> 1)) & 1) * 2u;
   uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16);
   uint32_t dst = tile + (uint32_t)(cc >> 1) * 16384u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
-  vmeta += (uint32_t)row0 * 4u;
+  meta += (uint32_t)row0 * 4u;
 #pragma unroll 1
-  for (int j = 0; j < 4; j += 2, a += 4096u, dst += 8192u, vmeta += 256u) {
+  for (int j = 0; j < 4; j += 2, a += 4096u, dst += 8192u, meta += 256u) {
     uint2 x[2][2], y[2][2];
     uint32_t sm[2];
 #pragma unroll
@@ -269,7 +288,7 @@ __device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t vme
         x[i][z] = lds64(a + i * 2048u + (sw ^ (uint32_t)(2 * z)) * 4u);
         y[i][z] = FULL ? lds64(a + i * 2048u + 8192u + (sw ^ (uint32_t)(2 * z)) * 4u) : make_uint2(0x88888888u, 0x88888888u);
       }
-      sm[i] = VALUES ? lds32(vmeta + i * 128u) : 0u;
+      sm[i] = lds32(meta + i * 128u);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -279,10 +298,8 @@ __device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t vme
       for (int k = 0; k < 4; ++k) {   // register k holds word k ^ sw of the chunk
         uint32_t o[4];
         codes8(wa[k], wr[k], o);
-        if (VALUES) {
 #pragma unroll
-          for (int z = 0; z < 4; ++z) o[z] = fma_f16x2(o[z], s2, m2);
-        }
+        for (int z = 0; z < 4; ++z) o[z] = fma_f16x2(VALUES ? centred(o[z]) : o[z], s2, m2);
         sts128((dst ^ (uint32_t)(k * 16)) + i * 4096u, o[0], o[1], o[2], o[3]);
       }
     }
@@ -404,6 +421,19 @@ __device__ __forceinline__ int64_t row_at(const TreeParams& p, int id, int h, in
   return ((int64_t)id * p.Hkv + h) * p.bt + (tok - quotient(tok, p.bt_div) * p.bt);
 }
 
+// Whether node i (of 128) is seen by some row, by a warp: the others' keys and values may be anything.
+__device__ __forceinline__ bool node_used(const TreeParams& p, int b, int i, int lane) {
+  uint32_t lo = 0u, hi = 0u;
+  for (int j = lane; j < p.n; j += 32) {
+    const unsigned long long x = ld_dep(p.mask + (int64_t)b * p.n + j);
+    lo |= (uint32_t)x;
+    hi |= (uint32_t)(x >> 32);
+  }
+  lo = __reduce_or_sync(0xFFFFFFFFu, lo);
+  hi = __reduce_or_sync(0xFFFFFFFFu, hi);
+  return i < p.n && (((i < 32 ? lo : hi) >> (i & 31)) & 1u);
+}
+
 // ------------------------------------------------------------------ the kernel
 template <bool FULL, int TS>
 __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __grid_constant__ TreeParams p) {
@@ -413,11 +443,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   const uint32_t sbase = smem_u32(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
-  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + g] exponents, [8 + i] V maxima, [16 + 4 piece + i] q maxima, [24 + piece] scores' factor
+  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + tile % 4] exponents of values, [8 + i] V maxima, [12 + i] K maxima,
+                                             // [16 + 4 piece + i] q maxima, [24 + tile % 4] factors of scores, [28 + piece] the queries' part of them
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
-  const uint32_t kready = vempty + 8 * C::kRingV, sfull = kready + 16, mready = sfull + 16, vready = mready + 16, pready = vready + 16,
+  const uint32_t kready = vempty + 8 * C::kRingV, sfull = kready + 16, mready = sfull + 16, vready = mready + 32, pready = vready + 16,
                  pvdone = pready + 16, ifull = pvdone + 16, iempty = ifull + 16, qready = iempty + 16, kdone = qready + 16;
   volatile int* ab = misc;        // (waits for data)
   volatile int* iab = misc + 1;   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
@@ -429,6 +460,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       mbar_init(kready + i * 8, 4);
       mbar_init(sfull + i * 8, 1);
       mbar_init(mready + i * 8, 1);
+      mbar_init(mready + 16 + i * 8, 1);
       mbar_init(qready + i * 8, 4);
       mbar_init(kdone + i * 8, 4);
       mbar_init(vready + i * 8, 4);
@@ -440,6 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     for (int i = 0; i < 32; ++i) misc_s[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  for (int i = tid; i < 2048 / 4; i += kThreads) reinterpret_cast<uint32_t*>(smem + C::kOffMid + 4096)[i] = 0u;
+  proxy_fence();
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc_s + 2)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -468,44 +502,38 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n_prefix = (len + kTile - 1) / kTile;
       const bool works = rb * kTile + ((w4 * 32) & (C::kRows - 1)) < p.cols;
       bool fresh = true;
-      float ref = 0.0f, l = 0.0f, qs = 0.0f;
+      float ref = 0.0f, l = 0.0f;
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gs) {
         const int g = gs & 1;
         const uint32_t ph = (gs >> 1) & 1;
-        // (No barrier may be more than a phase further than a wait expects: kready, say, which the K warps give again as soon as the
-        // scores are there, is not waited for here.)
-        if (u == 0) wait(qready + qi * 8, (ic >> 1) & 1, ab);
-        wait(mready + g * 8, ph, ab);
-        if (u0 + u == n_prefix) {   // the nodes' scalars, the exponent of their values
+        // (No barrier may be more than a phase further than a wait expects: see tests/test_tree_handoffs.py.)
+        wait(mready + (gs & 3) * 8, (gs >> 2) & 1, ab);
+        if (u0 + u == n_prefix) {   // the factor and the exponent of the nodes
           wait(kdone + qi * 8, (ic >> 1) & 1, ab);
           wait(vready + g * 8, ph, ab);
         }
         wait(sfull + g * 8, ph, ab);
         tc_fence_after();
         if (works) {
-          if (u == 0) qs = reinterpret_cast<const float*>(smem + C::kOffRow)[qi * 128 + r];
           const int ut = u0 + u;
           const bool tree = ut == n_prefix;
           const int t0 = (r / C::kRows) * (kTile / TS) + half * C::kW;                 // this thread's first token
           const int valid = (tree ? p.n : min(kTile, len - ut * kTile)) - t0;
-          const int e = misc[4 + g];
+          const int e = misc[4 + (gs & 3)];
+          const float a = __int_as_float(misc[24 + (gs & 3)]);
           const float bias = (float)e - ref;
-          const uint32_t tm_s = tmem0 + C::kTmS + g * 128 + lanes, tok = sbase + C::kOffTok + (uint32_t)(g * 1024 + t0 * 8);
+          const uint32_t tm_s = tmem0 + C::kTmS + g * 128 + lanes;
           float x[C::kW];
           float mx = -INFINITY;
           if (valid > 0) {
-            const uint64_t qs2 = f2_pack(qs, qs), b2 = f2_pack(bias, bias);
+            const uint64_t a2 = f2_pack(a, a), b2 = f2_pack(bias, bias);
             uint32_t* sx = reinterpret_cast<uint32_t*>(x);
 #pragma unroll
             for (int k = 0; k < C::kW / 16; ++k) TmemRegs<16>::ld(tm_s + t0 + k * 16, sx + 16 * k);
             tc_wait_ld();
 #pragma unroll
-            for (int k = 0; k < C::kW / 2; ++k) {
-              const uint4 t = lds128(tok + k * 16);
-              const uint64_t sk = (uint64_t)t.y << 32 | t.x, mk = (uint64_t)t.w << 32 | t.z;
-              f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), sk, f2_fma(mk, qs2, b2)), x[2 * k], x[2 * k + 1]);
-            }
+            for (int k = 0; k < C::kW / 2; ++k) f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), a2, b2), x[2 * k], x[2 * k + 1]);
             if (tree || valid < C::kW) {   // (nodes: valid > 0, so t0 < 64)
               unsigned long long see = tree ? (c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) >> t0 : 0ull) : ~0ull;
               if (valid < 64) see &= (1ull << valid) - 1ull;
@@ -646,7 +674,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   if (warp < 12) {
     reg_dec<C::kRegExp>();
     const int kt = tid - 256;
-    float* tok = reinterpret_cast<float*>(smem + C::kOffTok) + (kt >> 1) * 4 + (kt & 1);
     int gs = 0, slot = 0;
     uint32_t phase = 0;
     for (int ic = 0;; ++ic) {
@@ -655,8 +682,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
-      float a;
-      {   // queries: a thread a row, all rows scaled by one power of two
+      float a;   // factor of the scores, but for the keys' exponent
+      {   // queries: a thread a row, all rows scaled by one power of two, the largest below 2^7 (their sums below 2^14)
         const int c = rb * kTile + (kt & (C::kRows - 1)), j = c / p.G;
         const uint4* src = p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (c - j * p.G)) * 16;
         const bool in = c < p.cols;
@@ -670,10 +697,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         named_bar(8, 128);
         volatile int* qm = misc + 16 + 4 * qi;
         const int top = max(max(qm[0], qm[1]), max(qm[2], qm[3]));
-        const int e = top > 0 ? max(-100, min(100, exponent_of(__int_as_float(top)))) : 0;
+        const int e = top > 0 ? max(-100, min(100, exponent_of(__int_as_float(top)) + 8)) : 0;
         const float f = pow2(-e);
         a = p.sm_log2 * pow2(e);
-        if (kt == 0) misc[24 + qi] = __float_as_int(a);
+        if (kt == 0) misc[28 + qi] = __float_as_int(a);
         if (gs > 0) wait(sfull + ((gs - 1) & 1) * 8, ((gs - 1) >> 1) & 1, ab);   // the previous piece's last Q K^T
         tc_fence_after();
         const uint32_t tm_q = tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16);
@@ -690,8 +717,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           }
           TmemRegs<16>::st(tm_q + ch * 4, w);
         }
+        {   // against a token's {mid hi, mid lo, mid hi}: sum hi, sum hi, sum lo
+          const uint32_t both = two_parts(sum * f);
+          uint32_t w[8] = {__byte_perm(both, both, 0x1010), both >> 16};
+          TmemRegs<8>::st(tm_q + 64, w);
+        }
         tc_wait_st();
-        reinterpret_cast<float*>(smem + C::kOffRow)[qi * 128 + kt] = sum * f;
         __syncwarp();
         if (lane == 0) mbar_arrive(qready + qi * 8);
       }
@@ -699,31 +730,36 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       for (int u = 0; u < n; ++u, ++gs) {
         const int g = gs & 1, ut = u0 + u;
         const uint32_t tile = sbase + C::kOffK + (uint32_t)g * 32768u;
+        wait(mready + (gs & 3) * 8, (gs >> 2) & 1, ab);
         wait(sfull + g * 8, ((gs >> 1) - 1) & 1, ab);                                     // the tile has been used
         if (ut < n_prefix) {
           wait(kfull + slot * 8, phase, ab);
-          expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, 0u, kt);
+          expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, sbase + C::kOffKm + (uint32_t)g * 512u, kt);
           __syncwarp();
           if (lane == 0) mbar_arrive(kempty + slot * 8);
           if (++slot == C::kRingK) { slot = 0; phase ^= 1; }
         } else {   // the nodes' keys: a thread a row, scaled by a power of two
-          float sk = 0.0f;
-          if (kt < p.n) {
-            const uint4* src = p.kt + ((int64_t)b * p.n + kt) * p.kt_stride + h * 16;
-            float amax = 0.0f;
+          const uint4* src = p.kt + ((int64_t)b * p.n + kt) * p.kt_stride + h * 16;
+          const bool used = node_used(p, b, kt, lane);
+          float amax = 0.0f;
+          if (used) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
-            const int e = amax > 0.0f ? max(-100, min(100, exponent_of(amax))) : 0;
-            sk = pow2(e);
+          }
+          const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
+          if (lane == 0) misc[12 + (warp & 3)] = (int)wmax;
+          named_bar(8, 128);
+          const int e = tile_exponent(max(max(misc[12], misc[13]), max(misc[14], misc[15])));
+          named_bar(8, 128);   // (read by all)
+          if (kt == 0) misc[24 + (gs & 3)] = __float_as_int(times_pow2(a, e));
+          if (kt < kMaxNodes) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
-              const uint4 w = scaled8(ld_dep(src + ch), pow2(-e));
+              const uint4 w = used ? scaled8(ld_dep(src + ch), pow2(-e)) : make_uint4(0u, 0u, 0u, 0u);
               sts128(chunk_at(tile, kt, ch), w.x, w.y, w.z, w.w);
             }
           }
-          wait(pready + g * 8, ((gs >> 1) - 1) & 1, ab);                                  // this place's scalars have been used
-          tok[g * 256] = sk * a;
-          tok[g * 256 + 2] = 0.0f;
+          sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + kt * 16), 0u, 0u, 0u, 0u);
         }
         proxy_fence();
         tc_fence_before();   // (the queries)
@@ -750,7 +786,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       for (int u = 0; u < n; ++u, ++gs) {
         const int g = gs & 1, ut = u0 + u;
         const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u, vmeta = sbase + C::kOffVm + (uint32_t)g * 512u;
-        wait(mready + g * 8, (gs >> 1) & 1, ab);
+        wait(mready + (gs & 3) * 8, (gs >> 2) & 1, ab);
         if (ut < n_prefix) {
           wait(vfull + slot * 8, phase, ab);
           wait(pvdone + g * 8, ((gs >> 1) - 1) & 1, ab);   // the tile has been used
@@ -759,15 +795,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           if (lane == 0) mbar_arrive(vempty + slot * 8);
           if (++slot == C::kRingV) { slot = 0; phase ^= 1; }
         } else {
-          uint32_t lo = 0u, hi = 0u;   // nodes that some row sees (the others' values may be anything)
-          for (int i = lane; i < p.n; i += 32) {
-            const unsigned long long x = ld_dep(p.mask + (int64_t)b * p.n + i);
-            lo |= (uint32_t)x;
-            hi |= (uint32_t)(x >> 32);
-          }
-          lo = __reduce_or_sync(0xFFFFFFFFu, lo);
-          hi = __reduce_or_sync(0xFFFFFFFFu, hi);
-          const bool used = vt < p.n && (((vt < 32 ? lo : hi) >> (vt & 31)) & 1u);
+          const bool used = node_used(p, b, vt, lane);
           const uint4* src = p.vt + ((int64_t)b * p.n + vt) * p.vt_stride + h * 16;
           float amax = 0.0f;
           if (used) {
@@ -777,10 +805,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
           if (lane == 0) misc[8 + w4] = (int)wmax;
           named_bar(3, 128);
-          const int e = value_exponent(max(max(misc[8], misc[9]), max(misc[10], misc[11])));
+          const int e = tile_exponent(max(max(misc[8], misc[9]), max(misc[10], misc[11])));
           named_bar(3, 128);   // (read by all)
-          wait(pvdone + g * 8, ((gs >> 1) - 1) & 1, ab);   // the tile, and the exponent with it, has been used
-          if (vt == 0) misc[4 + g] = e;
+          wait(pvdone + g * 8, ((gs >> 1) - 1) & 1, ab);   // the tile has been used
+          if (vt == 0) misc[4 + (gs & 3)] = e;
           if (vt < ((p.n + 15) & ~15)) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
@@ -860,7 +888,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0;
       if (n == 0) break;
       wait(qready + qi * 8, (ic >> 1) & 1, ab);
-      const float a = __int_as_float(misc[24 + qi]);
+      const float a = __int_as_float(misc[28 + qi]);
       const int n_prefix = (len + kTile - 1) / kTile;
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gs) {
@@ -883,35 +911,48 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           if (lane == 0) { mbar_arrive(kempty + kslot * 8); mbar_arrive(vempty + vslot * 8); }
           if (++kslot == C::kRingK) { kslot = 0; kphase ^= 1; }
           if (++vslot == C::kRingV) { vslot = 0; vphase ^= 1; }
-          float vs[4], vm[4], amax = 0.0f;
+          float ks[4], km[4], vs[4], vm[4], kmax = 0.0f, vmax = 0.0f;
+          auto mids = [](const uint4 (&x)[2], float* sc, float* mid, float& top) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            vs[2 * i] = __uint_as_float(v2[i].x);
-            vs[2 * i + 1] = __uint_as_float(v2[i].z);
-            vm[2 * i] = fmaf(128.0f, vs[2 * i], __uint_as_float(v2[i].y));
-            vm[2 * i + 1] = fmaf(128.0f, vs[2 * i + 1], __uint_as_float(v2[i].w));
-            amax = max3(amax, fabsf(vm[2 * i]) + 128.0f * fabsf(vs[2 * i]), fabsf(vm[2 * i + 1]) + 128.0f * fabsf(vs[2 * i + 1]));
-          }
-          const int e = value_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax)));
-          const float f = pow2(-e);
-          wait(pready + g * 8, before, ab);   // these places have been read
+            for (int i = 0; i < 2; ++i) {
+              sc[2 * i] = __uint_as_float(x[i].x);
+              sc[2 * i + 1] = __uint_as_float(x[i].z);
+              mid[2 * i] = fmaf(128.0f, sc[2 * i], __uint_as_float(x[i].y));
+              mid[2 * i + 1] = fmaf(128.0f, sc[2 * i + 1], __uint_as_float(x[i].w));
+              top = max3(top, fabsf(mid[2 * i]) + 128.0f * fabsf(sc[2 * i]), fabsf(mid[2 * i + 1]) + 128.0f * fabsf(sc[2 * i + 1]));
+            }
+          };
+          mids(k2, ks, km, kmax);
+          mids(v2, vs, vm, vmax);
+          const int ek = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(kmax))) + 3;   // (1152 scales below 2^15.2)
+          const int ev = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(vmax)));
+          const float fk = pow2(-ek), fv = pow2(-ev);
+          wait(sfull + g * 8, before, ab);    // these places have been read (the softmax's of four tiles before: in front of that Q K^T)
           wait(vready + g * 8, before, ab);
+          uint32_t kw[4], vw[4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float s0 = __uint_as_float(k2[i].x) * a, s1 = __uint_as_float(k2[i].z) * a;
-            sts128(sbase + C::kOffTok + (uint32_t)(g * 1024 + lane * 32 + i * 16), __float_as_uint(s0), __float_as_uint(s1),
-                   __float_as_uint(fmaf(128.0f, s0, __uint_as_float(k2[i].y) * a)), __float_as_uint(fmaf(128.0f, s1, __uint_as_float(k2[i].w) * a)));
+          for (int i = 0; i < 4; ++i) {
+            // what rounding -1152 scale adds to all of a row's keys is taken off their middle
+            const float s16 = __half2float(__float2half_rn(ks[i] * fk)), m16 = __half2float(__float2half_rn(-1152.0f * s16));
+            kw[i] = pack_f16x2(s16, m16);
+            vw[i] = pack_f16x2(vs[i] * fv, vm[i] * fv);
+            const uint32_t both = two_parts(km[i] * fk - (m16 + 1152.0f * s16));
+            sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + lane * 64 + i * 16), both, both & 0xFFFFu, 0u, 0u);
           }
-          sts128(sbase + C::kOffVm + (uint32_t)(g * 512 + lane * 16), pack_f16x2(vs[0] * f, vm[0] * f), pack_f16x2(vs[1] * f, vm[1] * f),
-                 pack_f16x2(vs[2] * f, vm[2] * f), pack_f16x2(vs[3] * f, vm[3] * f));
-          if (lane == 0) misc[4 + g] = e;
-        } else {   // (the nodes': by the warps that have their keys and values.  They and the softmax wait for this warp all the same, so
-                   // that no barrier is a phase further than what a wait for it expects)
-          wait(pready + g * 8, before, ab);
+          sts128(sbase + C::kOffKm + (uint32_t)(g * 512 + lane * 16), kw[0], kw[1], kw[2], kw[3]);
+          sts128(sbase + C::kOffVm + (uint32_t)(g * 512 + lane * 16), vw[0], vw[1], vw[2], vw[3]);
+          if (lane == 0) {
+            misc[4 + (gs & 3)] = ev;
+            misc[24 + (gs & 3)] = __float_as_int(times_pow2(a, ek));
+          }
+          proxy_fence();
+        } else {   // (the nodes': by the warps that have their keys and values.  They wait for this warp all the same, so that no barrier is a
+                   // phase further than what a wait for it expects)
+          wait(sfull + g * 8, before, ab);
           wait(vready + g * 8, before, ab);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(mready + g * 8);
+        if (lane == 0) mbar_arrive(mready + (gs & 3) * 8);
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
@@ -921,6 +962,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   if (warp == 18) {
     constexpr uint32_t kIdescS = tc_idesc(128, false), kIdescO = tc_idesc(128, true);
     const uint32_t k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 16384u);
+    const uint32_t mid_lo[2] = {desc_lo(sbase + C::kOffMid, 4096u), desc_lo(sbase + C::kOffMid + 2048u, 2048u)};   // (zeros behind both)
     struct { int ic, n, u, gs; } s = {0, 0, 0, 0};   // the next Q K^T
     bool more = true;
     auto qk = [&]() {
@@ -939,6 +981,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         for (int ks = 0; ks < 8; ++ks)
           tc_mma_ts(tmem0 + C::kTmS + g * 128, tmem0 + C::kTmQ + ks * 8, desc(k_lo + g * 2048u + (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4)),
                     kIdescS, ks > 0 ? 1u : 0u);
+        tc_mma_ts(tmem0 + C::kTmS + g * 128, tmem0 + C::kTmQ + 64, desc_plain(g ? mid_lo[1] : mid_lo[0]), kIdescS, 1u);
         tc_commit(sfull + g * 8);
       }
       __syncwarp();

@@ -2,10 +2,11 @@
 
 Bounds.  Weights and values enter the second product as FP16: a weight is off by 2^-11 of itself at most, a value
 mid + scale (c - 128) by 2^-11 of each of its factors' and its own magnitude, 2^-9 of A in all, A = sum_t w_t (|mid_t| + 128 |scale_t|) over a
-row's weights w (nodes: their largest |v|).  Scores are FP32 sums over 128 channels of scale x (q . (c - 128)) and mid x sum(q), off by
-2^-16 of S, the largest sum of magnitudes that enters one; a weight follows relatively and the output by twice that of A.  The last
-rounding to BF16 is 2^-8 of the output; log-sum-exps are off by the scores' error, the sum's rounding and the approximations of
-exp2 and log2 (2^-18)."""
+row's weights w (nodes: their largest |v|).  Scores: FP32 sums over 128 channels of FP16 deviations and of mid x sum(q), off by 2^-16 of S,
+the largest sum of magnitudes that enters one, and by the rounding of the deviations, 2^-11 of each at most, independent of each
+other: 2^-9 of R = max_t |q x (k_t - mid_t)|_2 is five standard deviations of their sum and more.  A weight follows relatively and the
+output by twice that of A.  The last rounding to BF16 is 2^-8 of the output; log-sum-exps are off by the scores' error, the sum's
+rounding and the approximations of exp2 and log2 (2^-18)."""
 import math
 
 import numpy as np
@@ -92,21 +93,22 @@ class Problem:
                     workspace=lynx.make_tree_workspace(self.geo, self.B, self.n, "cuda"))
 
     def exact(self, anchor=False, scale=None):
-        """(out, lse, A, S) in 64 bits, on the GPU for the larger ones."""
+        """(out, lse, A, E) in 64 bits; E: bound of a score's error."""
         scale = 128 ** -0.5 if scale is None else scale
         B, n, Hkv, G, bt = self.B, self.n, self.Hkv, self.G, self.bt
         out = torch.zeros(B, n, Hkv * G, 128, dtype=torch.float64, device="cuda")
-        lse, A, S = (torch.zeros(B, n, Hkv * G, dtype=torch.float64, device="cuda") for _ in range(3))
+        lse, A, E = (torch.zeros(B, n, Hkv * G, dtype=torch.float64, device="cuda") for _ in range(3))
         for b, L in enumerate(self.lens):
             t = torch.arange(L)
             blk, off = self.table[b, t // bt].long(), t % bt
-            vals, mags = [], []
+            vals, mags, devs = [], [], []
             for p, x in zip(self.planes, (self.kn, self.vn)):
                 a, r, m = (y[blk, :, off].cuda() for y in p)                         # [L][Hkv][..]
                 level = 16 * _nibbles(a) + (8 if anchor else _nibbles(r))
                 m = m.double()
                 node = torch.where(self.sees[b].any(0)[:, None, None], x[b].double(), 0.0).cuda()
                 vals.append(torch.cat((m[..., 1:] + m[..., :1] * level, node)))
+                devs.append(torch.cat((m[..., :1] * (level - 128), node)))
                 mags.append(torch.cat(((m[..., 1] + 128 * m[..., 0]).abs() + 128 * m[..., 0], node.abs().amax(-1))))
             allowed = torch.cat((torch.ones(n, L, dtype=torch.bool), self.sees[b]), 1).cuda()
             for h in range(Hkv):
@@ -121,8 +123,10 @@ class Problem:
                 out[b, :, sl] = w @ vals[1][:, h]
                 lse[b, :, sl] = (den.log() + top)[..., 0]
                 A[b, :, sl] = w @ mags[1][:, h]
-                S[b, :, sl] = abs(scale) * q.abs().sum(-1) * (mags[0][:, h].max() if mags[0].numel() else 0.0)
-        return out, lse, A, S
+                S = abs(scale) * q.abs().sum(-1) * mags[0][:, h].max()
+                R = abs(scale) * torch.einsum("jgd,td->jgt", q * q, devs[0][:, h] ** 2).amax(-1).sqrt()
+                E[b, :, sl] = 2.0 ** -9 * R + 2.0 ** -16 * S
+        return out, lse, A, E
 
 
 def _check(pr, anchor=False, scale=0.0, out_f32=False, dev=None):
@@ -132,8 +136,8 @@ def _check(pr, anchor=False, scale=0.0, out_f32=False, dev=None):
     given = torch.full((B, n, Hq, 128), 777.0, device="cuda") if out_f32 else None
     got = lynx.tree_attention(**d, anchor_only=anchor, softmax_scale=scale, lse=lse, out=given)
     lynx.check(d["workspace"])
-    out, want_lse, A, S = pr.exact(anchor, None if scale == 0.0 else scale)
-    tol = (2.0 ** -9 + 2.0 ** -15 * S) * A
+    out, want_lse, A, E = pr.exact(anchor, None if scale == 0.0 else scale)
+    tol = (2.0 ** -9 + 2 * E) * A
     tol = tol[..., None] + (0.0 if out_f32 else 2.0 ** -8) * out.abs() + 1e-30
     err = (got.double() - out).abs()
     assert torch.isfinite(got).all()
@@ -144,7 +148,7 @@ def _check(pr, anchor=False, scale=0.0, out_f32=False, dev=None):
     empty = want_lse == -math.inf
     assert torch.equal(lse == -math.inf, empty) and (got[empty] == 0).all()
     d_lse = (lse.double() - want_lse)[~empty].abs()
-    assert (d_lse <= (2.0 ** -16 * S)[~empty] + 2.0 ** -18 * (1 + want_lse[~empty].abs())).all(), d_lse.max().item()
+    assert (d_lse <= E[~empty] + 2.0 ** -18 * (1 + want_lse[~empty].abs())).all(), d_lse.max().item()
     return got
 
 
@@ -251,8 +255,8 @@ def test_a_chain_is_a_verification():
     tail = lynx.bf16_attention(tail_geo, d["q"], *pages, torch.zeros(1, 1, dtype=torch.int32, device="cuda"),
                                torch.tensor([n], dtype=torch.int32, device="cuda"), tws, causal=True)
     both = lynx.lse_merge(out, lse, tail, lynx.bf16_workspace_lse(tail_geo, 1, n, tws))
-    _, _, A, S = pr.exact()
-    assert ((a - both).abs().double() <= 2 * ((2.0 ** -9 + 2.0 ** -15 * S) * A)[..., None] + 2e-3).all()
+    _, _, A, E = pr.exact()
+    assert ((a - both).abs().double() <= 2 * ((2.0 ** -9 + 2 * E) * A)[..., None] + 2e-3).all()
 
 
 def test_bad_block_ids_are_reported():
