@@ -2,7 +2,7 @@
 //
 // For every (sequence, KV head) the n nodes' G = Hq / Hkv query heads are n * G rows; they share the head's keys and values:
 //   S = Q K^T,   p = 2^(a S + e - ref_r),   O += P V,   l += sum p,   out = O / l
-// over the prefix (planes, 128 tokens a tile) and one last tile of the nodes' own BF16 keys and values under the tree's mask.
+// over the prefix (planes, 64 tokens a tile) and one last tile of the nodes' own BF16 keys and values under the tree's mask.
 //
 // A row of codes c is mid + scale (c - 128), mid = zero + 128 scale.  Keys enter as FP16 of scale (c - 128), an error of 2^-12 of a
 // key's deviation from the row's middle (an eighth of a code's step at most), and the middles, which may be far larger, as
@@ -10,20 +10,24 @@
 // down to 2^-24 of the row block's largest.  So a score needs one multiply-add in the softmax, with a factor that its whole tile shares
 // (per-token scales there are loads of shared memory for every score: 140 us instead of 112 for 128 rows over 131072 tokens).  Values
 // enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15 (rows 2^29 times smaller keep all 11 bits; keys 2^26), weights as
-// FP16 relative to a reference that keeps each row's largest between 2^8 and 2^15.5: both roundings are 2^-12 of a term, an eighth of the
+// FP16 relative to a reference that keeps each row's largest between 2^8 and 2^16 (set when the sum of 32 weights, which is
+// there anyway, tells it: no maxima): both roundings are 2^-12 of a term, an eighth of the
 // output's own rounding to BF16.  2^e goes into the weight's exponent and out of l's terms again, so that it costs nothing per weight.  Sums
 // l, references and O are FP32.
 //
 // Layout: rows are the M = 128 lanes of tensor memory (n * G > 128 rows: more row blocks), tokens the N of the scores and the K of
-// P V.  Two threads share a row, one for each half of a tile's tokens; they exchange a vote per tile and their sums at the end.  Queries
-// are the A operand of the scores in tensor memory, P goes from registers to tensor memory, over the scores, as the A operand of P V.
+// P V.  A thread owns a row of a tile: no exchange between threads for maxima and sums.  Two warpgroups take the tiles in turn, each with
+// references, sums and accumulators of its own, joined at the end of a piece: while one waits for the special function unit, the other
+// loads, compares and stores.  (Two threads a row instead, half of a tile of 128 tokens each, went through the same phases at the same
+// time: 141 us for 128 rows over 131072 tokens.)  Queries are the A operand of the scores in tensor memory, P goes from registers to tensor
+// memory, over the scores, as the A operand of P V; three places for scores, so that Q K^T is never waited for.
 // One CTA per SM; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
-//   warps 0-3, 4-7   softmax, tokens 0..63 and 64..127 of every tile
+//   warps 0-3, 4-7   softmax, even and odd tiles
 //   warps 8-11       K codes to FP16 into the K tiles, and a piece's queries
 //   warps 12-15      V codes to FP16 values into the V tiles
 //   warps 16, 17     bulk copies of 16-token sub-blocks of the K and V planes into rings; warp 16 deals out the pieces
-//   warp 18          issues every tcgen05.mma: Q K^T a tile ahead of P V
-//   warp 19          scales and zero points of a tile: what the softmax and the V tile need of them
+//   warp 18          issues every tcgen05.mma: Q K^T three tiles ahead of P V
+//   warp 19          scales and zero points of a tile: what the K and V tiles and the softmax need of them
 // Work is cut in stream-K form: the (sequence, KV head, row block, tile) list into equal ranges, a piece being a range's part of one
 // segment.  A segment within one CTA is written by it; otherwise partial (ref, l, O) go to the workspace and a dependent
 // kernel joins them.
@@ -39,12 +43,15 @@ namespace {
 
 #include "tc_common.cuh"
 
-constexpr int kTile = 128;          // tokens of a tile, rows of a row block
+constexpr int kTile = 64;           // tokens of a tile
+constexpr int kM = 128;             // rows of a row block
+constexpr int kSlots = 3;           // places for scores, K and V tiles
 constexpr int kMaxNodes = 64;
 constexpr int kPartRow = 132;       // floats of a partial row: O[128], reference, sum, pad
 constexpr int kThreads = 640;
 constexpr int kDoneThreads = 256 + 3 * 32;   // softmax warpgroups, copies, products
-constexpr float kTop = 8.0f, kRaise = 15.5f; // log2 of a row's largest weight when its reference is set, and before it is set anew
+// log2 of the largest of a row's 32 weights when its reference is set; their sum that sets it anew (no weight above it, and FP16 holds 65504)
+constexpr float kTop = 8.0f, kMost = 65000.0f;
 constexpr int kMinExp = -80;        // smallest exponent of a tile's keys or values
 
 struct TreeParams {
@@ -67,28 +74,38 @@ struct TreeParams {
   BlockDiv bt_div;
 };
 
-// TS: where there are no more than 128 / TS rows, a row lies in TS lanes of tensor memory, which take the tokens of a tile in TS parts, with
+// TS: where there are no more than 128 / TS rows, a row lies in TS lanes of tensor memory, which take a tile's tokens in TS parts, with
 // references, sums and accumulators of their own; the joining kernel adds them up.  The softmax of a tile is then spread over all warps.
 template <bool FULL, int TS>
 struct Cfg {
-  static constexpr int kRows = kTile / TS, kW = 64 / TS;             // rows of a row block; scores of a thread and tile
-  static constexpr int kPlanes = FULL ? 16384 : 8192;                // of one tensor and tile: [planes][128 tokens][64 B]
-  static constexpr int kStage = kPlanes + 1024;                      // and [128] {scale, zero}
-  static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 4;
-  static constexpr int kOffK = 0, kOffV = kOffK + 65536, kOffRK = kOffV + 65536, kOffRV = kOffRK + kRingK * kStage,
-                       kOffMid = kOffRV + kRingV * kStage;           // [2][128] the middles' 8 FP16, and 128 x 8 zeros
-  static constexpr int kOffKm = kOffMid + 3 * 2048;                  // [2][128] half2 {scale, - 1152 scale}
-  static constexpr int kOffVm = kOffKm + 2 * 512;                    // [2][128] half2 {scale, mid}
-  static constexpr int kOffX = kOffVm + 2 * 512;                     // [2][128] maxima, [2][128] sums of the halves of a row
-  static constexpr int kOffItems = kOffX + 4 * 512;                  // [2] Item
+  static constexpr int kRows = kM / TS, kW = kTile / TS;             // rows of a row block; scores of a thread and tile
+  static constexpr int kPlanes = FULL ? 8192 : 4096;                 // of one tensor and tile: [planes][64 tokens][64 B]
+  static constexpr int kStage = kPlanes + 512;                       // and [64] {scale, zero}
+  static constexpr int kRingK = FULL ? 7 : 11, kRingV = FULL ? 6 : 10;
+  static constexpr int kOffK = 0, kOffV = kOffK + kSlots * 16384, kOffRK = kOffV + kSlots * 16384, kOffRV = kOffRK + kRingK * kStage,
+                       kOffMid = kOffRV + kRingV * kStage;           // [kSlots][64] the middles' 8 FP16, and 64 x 8 zeros
+  static constexpr int kOffSum = kOffMid + (kSlots + 1) * 1024;      // [128] the query sums' 8 FP16, and 128 x 8 zeros
+  static constexpr int kOffKm = kOffSum + 2 * 2048;                  // [kSlots][64] half2 {scale, - 1152 scale}
+  static constexpr int kOffVm = kOffKm + kSlots * 256;               // [kSlots][64] half2 {scale, mid}
+  static constexpr int kOffMl = kOffVm + kSlots * 256;               // [2][128] {reference, sum}
+  static constexpr int kOffItems = kOffMl + 2 * 1024;                // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
-  static constexpr int kOffBars = kOffMisc + 128;
-  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 22;
+  static constexpr int kOffBars = kOffMisc + 256;
+  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 5 * kSlots + 8 + 8;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024, "shared memory");
+  static_assert(kOffMid % 128 == 0 && kOffBars % 8 == 0, "alignment");
   // registers a thread after the split (launched with 96 each): 256 * 144 + 256 * 72 + 128 * 48 = 640 * 96
   static constexpr int kRegSoft = 144, kRegExp = 72, kRegRest = 48;
-  static constexpr int kTmS = 0, kTmO = 256, kTmQ = 384;             // [2][128] scores, weights in their place; accumulators; queries
+  static constexpr int kTmS = 0, kTmQ = 192, kTmO = 256;             // [kSlots][64] scores, weights in their place; queries; [2][128] accumulators
+};
+// A place of kSlots and the parity of its round.
+struct Slot {
+  int i = 0;
+  uint32_t ph = 0;
+  __device__ __forceinline__ void next() {
+    if (++i == kSlots) { i = 0; ph ^= 1; }
+  }
 };
 
 struct Item {  // a piece: tiles u0 .. u0 + n - 1 of segment (b, h, rb), none: the end
@@ -136,12 +153,6 @@ __device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t
 }
 __device__ __forceinline__ void named_bar(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
-__device__ __forceinline__ bool bar_or(int id, int n, bool pred) {
-  uint32_t res;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(res) : "r"(pred ? 1u : 0u), "r"(id), "r"(n) : "memory");
-  return res != 0;
-}
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -266,7 +277,7 @@ __device__ __forceinline__ uint32_t two_parts(float x) {
   return pack_f16x2(hi, x - hi);
 }
 
-// A tile's codes by 128 threads: thread i takes the 16-byte chunk i & 3 (32 channels) of rows (i >> 2) + 32 j.  Half of the threads take a
+// A tile's codes by 128 threads: thread i takes the 16-byte chunk i & 3 (32 channels) of rows i >> 2 and 32 on.  Half of the threads take a
 // chunk's 8-byte halves in the other order: the eight threads of a store's phase then have eight chunk positions, and rows that share
 // their banks in the raw stage are read in different halves.
 // meta: per row, keys {scale, -1152 scale (rounded)} -> (1024 + c) scale - 1152 scale, values {scale, mid} -> (c - 128) scale + mid.
@@ -274,39 +285,36 @@ template <bool FULL, bool VALUES>
 __device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t meta, int i) {
   const int cc = i & 3, row0 = i >> 2;
   const uint32_t sw = (uint32_t)(((cc >> 1) ^ (row0 >> 1)) & 1) * 2u;
-  uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16);
-  uint32_t dst = tile + (uint32_t)(cc >> 1) * 16384u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
+  const uint32_t dst = tile + (uint32_t)(cc >> 1) * 8192u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
+  const uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16);
   meta += (uint32_t)row0 * 4u;
-#pragma unroll 1
-  for (int j = 0; j < 4; j += 2, a += 4096u, dst += 8192u, meta += 256u) {
-    uint2 x[2][2], y[2][2];
-    uint32_t sm[2];
+  uint2 x[2][2], y[2][2];
+  uint32_t sm[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        x[i][z] = lds64(a + i * 2048u + (sw ^ (uint32_t)(2 * z)) * 4u);
-        y[i][z] = FULL ? lds64(a + i * 2048u + 8192u + (sw ^ (uint32_t)(2 * z)) * 4u) : make_uint2(0x88888888u, 0x88888888u);
-      }
-      sm[i] = lds32(meta + i * 128u);
+    for (int z = 0; z < 2; ++z) {
+      x[i][z] = lds64(a + i * 2048u + (sw ^ (uint32_t)(2 * z)) * 4u);
+      y[i][z] = FULL ? lds64(a + i * 2048u + 4096u + (sw ^ (uint32_t)(2 * z)) * 4u) : make_uint2(0x88888888u, 0x88888888u);
     }
+    sm[i] = lds32(meta + i * 128u);
+  }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t s2 = __byte_perm(sm[i], sm[i], 0x1010), m2 = __byte_perm(sm[i], sm[i], 0x3232);
-      const uint32_t wa[4] = {x[i][0].x, x[i][0].y, x[i][1].x, x[i][1].y}, wr[4] = {y[i][0].x, y[i][0].y, y[i][1].x, y[i][1].y};
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t s2 = __byte_perm(sm[i], sm[i], 0x1010), m2 = __byte_perm(sm[i], sm[i], 0x3232);
+    const uint32_t wa[4] = {x[i][0].x, x[i][0].y, x[i][1].x, x[i][1].y}, wr[4] = {y[i][0].x, y[i][0].y, y[i][1].x, y[i][1].y};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {   // register k holds word k ^ sw of the chunk
-        uint32_t o[4];
-        codes8(wa[k], wr[k], o);
+    for (int k = 0; k < 4; ++k) {   // register k holds word k ^ sw of the chunk
+      uint32_t o[4];
+      codes8(wa[k], wr[k], o);
 #pragma unroll
-        for (int z = 0; z < 4; ++z) o[z] = fma_f16x2(VALUES ? centred(o[z]) : o[z], s2, m2);
-        sts128((dst ^ (uint32_t)(k * 16)) + i * 4096u, o[0], o[1], o[2], o[3]);
-      }
+      for (int z = 0; z < 4; ++z) o[z] = fma_f16x2(VALUES ? centred(o[z]) : o[z], s2, m2);
+      sts128((dst ^ (uint32_t)(k * 16)) + i * 4096u, o[0], o[1], o[2], o[3]);
     }
   }
 }
 __device__ __forceinline__ uint32_t chunk_at(uint32_t tile, int row, int ch) {   // 16-byte chunk ch (8 channels) of a row
-  return tile + (uint32_t)(ch >> 3) * 16384u + (uint32_t)row * 128u + (uint32_t)(((ch & 7) ^ (row & 7)) * 16);
+  return tile + (uint32_t)(ch >> 3) * 8192u + (uint32_t)row * 128u + (uint32_t)(((ch & 7) ^ (row & 7)) * 16);
 }
 
 // ------------------------------------------------------------------ the cut
@@ -443,36 +451,41 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   const uint32_t sbase = smem_u32(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
-  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + tile % 4] exponents of values, [8 + i] V maxima, [12 + i] K maxima,
-                                             // [16 + 4 piece + i] q maxima, [24 + tile % 4] factors of scores, [28 + piece] the queries' part of them
+  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [8 + i] V maxima, [12 + i] K maxima, [16 + 4 piece + i]
+                                             // q maxima, [28 + piece] the queries' part of the scores' factor, [32 + tile % 8] that factor, [40 + tile % 8]
+                                             // exponent of the values
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
-  const uint32_t kready = vempty + 8 * C::kRingV, sfull = kready + 16, mready = sfull + 16, vready = mready + 32, pready = vready + 16,
-                 pvdone = pready + 16, ifull = pvdone + 16, iempty = ifull + 16, qready = iempty + 16, kdone = qready + 16;
+  constexpr uint32_t kRound = 8 * kSlots;
+  const uint32_t kready = vempty + 8 * C::kRingV, sfull = kready + kRound, vready = sfull + kRound, pready = vready + kRound,
+                 pvdone = pready + kRound, mready = pvdone + kRound, ifull = mready + 64, iempty = ifull + 16, qready = iempty + 16,
+                 kdone = qready + 16;
   volatile int* ab = misc;        // (waits for data)
   volatile int* iab = misc + 1;   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
 
   if (tid == 0) {
     for (int i = 0; i < C::kRingK; ++i) { mbar_init(kfull + i * 8, 1); mbar_init(kempty + i * 8, 5); }
     for (int i = 0; i < C::kRingV; ++i) { mbar_init(vfull + i * 8, 1); mbar_init(vempty + i * 8, 5); }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kSlots; ++i) {
       mbar_init(kready + i * 8, 4);
       mbar_init(sfull + i * 8, 1);
-      mbar_init(mready + i * 8, 1);
-      mbar_init(mready + 16 + i * 8, 1);
+      mbar_init(vready + i * 8, 4);
+      mbar_init(pready + i * 8, 4);
+      mbar_init(pvdone + i * 8, 1);
+    }
+    for (int i = 0; i < 8; ++i) mbar_init(mready + i * 8, 1);
+    for (int i = 0; i < 2; ++i) {
       mbar_init(qready + i * 8, 4);
       mbar_init(kdone + i * 8, 4);
-      mbar_init(vready + i * 8, 4);
-      mbar_init(pready + i * 8, 8);
-      mbar_init(pvdone + i * 8, 1);
       mbar_init(ifull + i * 8, 1);
       mbar_init(iempty + i * 8, 8 + 4 + 4 + 3);   // softmax, K, V, V copies, products, scales
     }
-    for (int i = 0; i < 32; ++i) misc_s[i] = 0;
+    for (int i = 0; i < 64; ++i) misc_s[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (int i = tid; i < 2048 / 4; i += kThreads) reinterpret_cast<uint32_t*>(smem + C::kOffMid + 4096)[i] = 0u;
+  for (int i = tid; i < 256; i += kThreads) reinterpret_cast<uint32_t*>(smem + C::kOffMid + kSlots * 1024)[i] = 0u;
+  for (int i = tid; i < 512; i += kThreads) reinterpret_cast<uint32_t*>(smem + C::kOffSum + 2048)[i] = 0u;
   proxy_fence();
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc_s + 2)), "r"(512u) : "memory");
@@ -487,149 +500,179 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   // ================================================================================== softmax
   if (warp < 8) {
     reg_inc<C::kRegSoft>();
-    const int half = warp >> 2, w4 = warp & 3, r = tid & 127, bar = 4 + w4;   // (a warp's rows are shared with warp ^ 4)
+    const int g = warp >> 2, w4 = warp & 3, r = tid & 127, bar = 4 + w4;   // (a warp's rows are shared with warp ^ 4)
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
-    const uint32_t tm_o = tmem0 + C::kTmO + lanes + half * 64;
-    float* xs = reinterpret_cast<float*>(smem + C::kOffX);
+    const uint32_t tm_o = tmem0 + C::kTmO + g * 128 + lanes;
+    const int t0 = (r / C::kRows) * C::kW;                                 // this thread's first token of a tile
+    constexpr int kCW = C::kW < 32 ? C::kW : 32;                           // scores at a time
+    float2* ml = reinterpret_cast<float2*>(smem + C::kOffMl);
     int gs = 0;
+    Slot s, s2;   // of tile gs, and of tile gs - 2
+    s2.i = 1;
+    s2.ph = 1;
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
       if (n == 0) break;
       const int first_cta = items[qi].first_cta, n_contrib = items[qi].n_contrib;
-      const int c = rb * kTile + (r & (C::kRows - 1)), j = c / p.G, hq = h * p.G + (c - j * p.G);
+      const int c = rb * kM + (r & (C::kRows - 1)), j = c / p.G, hq = h * p.G + (c - j * p.G);
       const int n_prefix = (len + kTile - 1) / kTile;
-      const bool works = rb * kTile + ((w4 * 32) & (C::kRows - 1)) < p.cols;
-      bool fresh = true;
+      const bool works = rb * kM + ((w4 * 32) & (C::kRows - 1)) < p.cols;
+      bool fresh = true, any = false;   // no reference yet; a tile of this warpgroup's
       float ref = 0.0f, l = 0.0f;
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs) {
-        const int g = gs & 1;
-        const uint32_t ph = (gs >> 1) & 1;
+      for (int u = 0; u < n; ++u, ++gs, s.next(), s2.next()) {
+        if ((gs & 1) != g) continue;
         // (No barrier may be more than a phase further than a wait expects: see tests/test_tree_handoffs.py.)
-        wait(mready + (gs & 3) * 8, (gs >> 2) & 1, ab);
-        if (u0 + u == n_prefix) {   // the factor and the exponent of the nodes
+        wait(mready + (gs & 7) * 8, (gs >> 3) & 1, ab);
+        const int ut = u0 + u;
+        const bool tree = ut == n_prefix;
+        if (tree) {   // the factor and the exponent of the nodes
           wait(kdone + qi * 8, (ic >> 1) & 1, ab);
-          wait(vready + g * 8, ph, ab);
+          wait(vready + s.i * 8, s.ph, ab);
         }
-        wait(sfull + g * 8, ph, ab);
+        wait(sfull + s.i * 8, s.ph, ab);
         tc_fence_after();
         if (works) {
-          const int ut = u0 + u;
-          const bool tree = ut == n_prefix;
-          const int t0 = (r / C::kRows) * (kTile / TS) + half * C::kW;                 // this thread's first token
           const int valid = (tree ? p.n : min(kTile, len - ut * kTile)) - t0;
-          const int e = misc[4 + (gs & 3)];
-          const float a = __int_as_float(misc[24 + (gs & 3)]);
-          const float bias = (float)e - ref;
-          const uint32_t tm_s = tmem0 + C::kTmS + g * 128 + lanes;
-          float x[C::kW];
-          float mx = -INFINITY;
-          if (valid > 0) {
-            const uint64_t a2 = f2_pack(a, a), b2 = f2_pack(bias, bias);
-            uint32_t* sx = reinterpret_cast<uint32_t*>(x);
-#pragma unroll
-            for (int k = 0; k < C::kW / 16; ++k) TmemRegs<16>::ld(tm_s + t0 + k * 16, sx + 16 * k);
-            tc_wait_ld();
-#pragma unroll
-            for (int k = 0; k < C::kW / 2; ++k) f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), a2, b2), x[2 * k], x[2 * k + 1]);
-            if (tree || valid < C::kW) {   // (nodes: valid > 0, so t0 < 64)
-              unsigned long long see = tree ? (c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) >> t0 : 0ull) : ~0ull;
-              if (valid < 64) see &= (1ull << valid) - 1ull;
-#pragma unroll
-              for (int k = 0; k < C::kW; ++k)
-                if (!((see >> k) & 1ull)) x[k] = -INFINITY;
-            }
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int k = 0; k < C::kW / 2; ++k) m4[k & 3] = max3(m4[k & 3], x[2 * k], x[2 * k + 1]);
-            mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
-          }
-          // (behind the vote both halves' scores are in registers: weights may go over them)
-          if (bar_or(bar, 64, fresh ? mx > -INFINITY : mx > kRaise)) {
-            // a first reference, or one that a weight would outgrow: what the piece has so far is scaled
-            xs[half * 128 + r] = mx;
-            named_bar(bar, 64);
-            mx = fmaxf(mx, xs[(half ^ 1) * 128 + r]);
-            const bool need = fresh ? mx > -INFINITY : mx > kRaise;
-            const float delta = need ? mx - kTop : 0.0f, f = fresh ? 1.0f : ex2(-delta);
-            if (need) { ref += delta; fresh = false; }
-#pragma unroll
-            for (int k = 0; k < C::kW; ++k) x[k] -= delta;
-            l *= f;
-            if (u > 0) {
-              wait(pvdone + (g ^ 1) * 8, ((gs - 1) >> 1) & 1, ab);
-              tc_fence_after();
+          const int e = misc[40 + (gs & 7)];
+          const float a = __int_as_float(misc[32 + (gs & 7)]);
+          const uint32_t tm_s = tmem0 + C::kTmS + s.i * 64 + lanes;
+          const uint64_t a2 = f2_pack(a, a);
+          const bool masked = tree || valid < C::kW;
+          float sum = 0.0f;
 #pragma unroll 1
-              for (int i = 0; i < 64; i += 16) {
-                uint32_t w[16];
-                TmemRegs<16>::ld(tm_o + i, w);
+          for (int ch = 0; ch < C::kW; ch += kCW) {
+            uint32_t w[kCW / 2];
+            float x[kCW];
+            // weights of the chunk, scores less `shift` (in units of a weight's exponent), and their sum
+            auto scores = [&](float shift) {
+              uint32_t* sx = reinterpret_cast<uint32_t*>(x);
+#pragma unroll
+              for (int k = 0; k < kCW / 16; ++k) TmemRegs<16>::ld(tm_s + t0 + ch + k * 16, sx + 16 * k);
+              tc_wait_ld();
+              const uint64_t b2 = f2_pack(shift, shift);
+#pragma unroll
+              for (int k = 0; k < kCW / 2; ++k) f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), a2, b2), x[2 * k], x[2 * k + 1]);
+              if (masked) {
+                const int room = valid - ch;
+                uint32_t see = room <= 0 ? 0u : room < 32 ? (1u << room) - 1u : ~0u;
+                if (tree && see) see &= c < p.cols ? (uint32_t)(ld_dep(p.mask + (int64_t)b * p.n + j) >> (t0 + ch)) : 0u;
+#pragma unroll
+                for (int k = 0; k < kCW; ++k)
+                  if (!((see >> k) & 1u)) x[k] = -INFINITY;
+              }
+            };
+            auto weights = [&]() {
+              uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+              for (int k = 0; k < kCW / 2; ++k) {
+                const float x0 = ex2(x[2 * k]), x1 = ex2(x[2 * k + 1]);
+                sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(x0, x1));
+                w[k] = pack_f16x2(x0, x1);
+              }
+              float s0, s1;
+              f2_unpack(f2_add(sum2[0], sum2[1]), s0, s1);
+              return s0 + s1;
+            };
+            scores((float)e - ref);
+            float part = weights();
+            if (__any_sync(0xFFFFFFFFu, fresh || !(part <= kMost))) {
+              // no reference yet, or weights that FP16 might not hold: a reference from the chunk's largest score, what the piece has so far
+              // is scaled (scores and weights once more: this is rare)
+              scores((float)e - ref);
+              float mx = -INFINITY;
+#pragma unroll
+              for (int k = 0; k < kCW; ++k) mx = fmaxf(mx, x[k]);
+              const bool need = fresh ? mx > -INFINITY : !(part <= kMost);
+              const float delta = need ? mx - kTop : 0.0f, f = fresh ? 1.0f : ex2(-delta);
+              if (need) { ref += delta; fresh = false; }
+              l *= f;
+              sum *= f;
+#pragma unroll 1
+              for (int i = 0; i < ch / 2; i += 8) {   // (a row's only part of the tile, then)
+                uint32_t o[8];
+                TmemRegs<8>::ld(tm_s + i, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(__uint_as_float(w[k]) * f);
-                TmemRegs<16>::st(tm_o + i, w);
+                for (int k = 0; k < 8; ++k) {
+                  const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&o[k]));
+                  o[k] = pack_f16x2(v.x * f, v.y * f);
+                }
+                TmemRegs<8>::st(tm_s + i, o);
+              }
+              if (any) {
+                wait(pvdone + s2.i * 8, s2.ph, ab);
+                tc_fence_after();
+#pragma unroll 1
+                for (int i = 0; i < 128; i += 8) {
+                  uint32_t o[8];
+                  TmemRegs<8>::ld(tm_o + i, o);
+                  tc_wait_ld();
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                  TmemRegs<8>::st(tm_o + i, o);
+                }
+              }
+#pragma unroll
+              for (int k = 0; k < kCW; ++k) x[k] -= delta;
+              part = weights();
+            }
+            sum += part;
+            if constexpr (TS == 1) {
+              TmemRegs<16>::st(tm_s + ch / 2, w);
+            } else {   // (the lanes' other parts of the tile have no weight)
+#pragma unroll
+              for (int i = 0; i < TS; ++i) {
+                uint32_t z[kCW / 2];
+#pragma unroll
+                for (int k = 0; k < kCW / 2; ++k) z[k] = i == r / C::kRows ? w[k] : 0u;
+                TmemRegs<kCW / 2>::st(tm_s + i * (kCW / 2), z);
               }
             }
           }
-          uint32_t w[C::kW / 2] = {};
-          if (valid > 0) {
-            uint64_t sum2[2] = {0ull, 0ull};
-#pragma unroll
-            for (int k = 0; k < C::kW / 2; ++k) {
-              const float x0 = ex2(x[2 * k]), x1 = ex2(x[2 * k + 1]);
-              sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(x0, x1));
-              w[k] = pack_f16x2(x0, x1);
-              if constexpr (TS == 1)
-                if (k == 15) TmemRegs<16>::st(tm_s + half * 32, w);
-            }
-            float s0, s1;
-            f2_unpack(f2_add(sum2[0], sum2[1]), s0, s1);
-            l = fmaf(s0 + s1, pow2(-e), l);
-          }
-          // (the lanes' other parts of the tile have no weight)
-          if constexpr (TS == 1) {
-            if (valid > 0) TmemRegs<16>::st(tm_s + half * 32 + 16, w + 16);
-          } else {
-#pragma unroll
-            for (int i = 0; i < TS; ++i) {
-              uint32_t z[C::kW / 2];
-#pragma unroll
-              for (int k = 0; k < C::kW / 2; ++k) z[k] = i == r / C::kRows ? w[k] : 0u;
-              TmemRegs<C::kW / 2>::st(tm_s + i * (64 / TS) + half * (32 / TS), z);
-            }
-          }
+          l = fmaf(sum, pow2(-e), l);
           tc_wait_st();
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(pready + g * 8);
+        if (lane == 0) mbar_arrive(pready + s.i * 8);
+        any = true;
       }
-      // ---- end of the piece: both halves' sums, half of the channels each
-      wait(pvdone + ((gs - 1) & 1) * 8, ((gs - 1) >> 1) & 1, ab);
+      // ---- end of the piece: both warpgroups' sums, half of the channels each
+      Slot s1 = s2;   // of tile gs - 1
+      s1.next();
+      wait(pvdone + s1.i * 8, s1.ph, ab);
+      if (n > 1) wait(pvdone + s2.i * 8, s2.ph, ab);
       tc_fence_after();
       if (works) {
-        xs[256 + half * 128 + r] = l;
+        const float2 mine = any && !fresh ? make_float2(ref, l) : make_float2(-INFINITY, 0.0f);
+        ml[g * 128 + r] = mine;
         named_bar(bar, 64);
-        const float L = l + xs[256 + (half ^ 1) * 128 + r], M = fresh ? -INFINITY : ref;
+        const float2 other = ml[(g ^ 1) * 128 + r];
+        const float M = fmaxf(mine.x, other.x);
+        const float fm = mine.x == -INFINITY ? 0.0f : ex2(mine.x - M), fo = other.x == -INFINITY ? 0.0f : ex2(other.x - M);
+        const float L = mine.y * fm + other.y * fo;
         const bool direct = TS == 1 && n_contrib == 1;
-        const float w = L > 0.0f ? (direct ? 1.0f / L : 1.0f) : 0.0f;
+        const float inv = direct ? (L > 0.0f ? 1.0f / L : 0.0f) : 1.0f;
+        const float w0 = (g ? fo : fm) * inv, w1 = (g ? fm : fo) * inv;   // of accumulators 0 and 1
         const int64_t orow = ((int64_t)b * p.n + j) * p.Hq + hq;
         const int segment = (b * p.Hkv + h) * p.RB + rb;
         float* part = p.part + ((int64_t)(segment + (int)blockIdx.x) * p.part_rows + r) * kPartRow;
 #pragma unroll 1
-        for (int i = 0; i < 64; i += 16) {
-          uint32_t o[16];
-          TmemRegs<16>::ld(tm_o + i, o);
+        for (int i = 64 * g; i < 64 * g + 64; i += 16) {
+          uint32_t o0[16], o1[16];
+          TmemRegs<16>::ld(tmem0 + C::kTmO + lanes + i, o0);
+          TmemRegs<16>::ld(tmem0 + C::kTmO + 128 + lanes + i, o1);
           tc_wait_ld();
           float v[16];
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {   // (channel k of a group of 8 is at position 0 4 2 6 1 5 3 7)
+          for (int k = 0; k < 16; ++k) {   // (channel k of a group of 8 is at position 0 4 2 6 1 5 3 7; what no tile wrote may be anything)
             const int at = (k & 8) | ((k & 1) << 2) | (k & 2) | ((k >> 2) & 1);
-            v[k] = __uint_as_float(o[at]) * w;
+            v[k] = (w0 > 0.0f ? __uint_as_float(o0[at]) * w0 : 0.0f) + (w1 > 0.0f ? __uint_as_float(o1[at]) * w1 : 0.0f);
           }
           if (c < p.cols) {
-            const int d = half * 64 + i;
             if (direct && !p.out_f32) {
               uint32_t x[8];
 #pragma unroll
@@ -637,24 +680,24 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
                 const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
                 x[k] = *reinterpret_cast<const uint32_t*>(&t);
               }
-              uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + orow * LYNX_D + d);
+              uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + orow * LYNX_D + i);
               dst[0] = make_uint4(x[0], x[1], x[2], x[3]);
               dst[1] = make_uint4(x[4], x[5], x[6], x[7]);
             } else {
-              float4* dst = reinterpret_cast<float4*>((direct ? static_cast<float*>(p.out) + orow * LYNX_D : part) + d);
+              float4* dst = reinterpret_cast<float4*>((direct ? static_cast<float*>(p.out) + orow * LYNX_D : part) + i);
 #pragma unroll
               for (int k = 0; k < 4; ++k) dst[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
             }
           }
         }
-        if (half == 0 && c < p.cols) {
+        if (g == 0 && c < p.cols) {
           if (!direct) *reinterpret_cast<float2*>(part + 128) = make_float2(M, L);
           else if (p.lse) p.lse[orow] = L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
         }
         if (tid == 0 && u0 == 0 && !p.whole) p.seg[segment] = (uint32_t)first_cta << 16 | (uint32_t)n_contrib;
+        tc_fence_before();
+        named_bar(bar, 64);   // (both have read both accumulators, and the sums)
       }
-      // (the next piece's first product may take the accumulators once all have given it weights)
-      tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
@@ -675,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     reg_dec<C::kRegExp>();
     const int kt = tid - 256;
     int gs = 0, slot = 0;
-    uint32_t phase = 0;
+    Slot s, last;   // of tile gs, and of tile gs - 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
@@ -684,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n_prefix = (len + kTile - 1) / kTile;
       float a;   // factor of the scores, but for the keys' exponent
       {   // queries: a thread a row, all rows scaled by one power of two, the largest below 2^7 (their sums below 2^14)
-        const int c = rb * kTile + (kt & (C::kRows - 1)), j = c / p.G;
+        const int c = rb * kM + (kt & (C::kRows - 1)), j = c / p.G;
         const uint4* src = p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (c - j * p.G)) * 16;
         const bool in = c < p.cols;
         float amax = 0.0f, sum = 0.0f;
@@ -701,7 +744,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         const float f = pow2(-e);
         a = p.sm_log2 * pow2(e);
         if (kt == 0) misc[28 + qi] = __float_as_int(a);
-        if (gs > 0) wait(sfull + ((gs - 1) & 1) * 8, ((gs - 1) >> 1) & 1, ab);   // the previous piece's last Q K^T
+        if (gs > 0) wait(sfull + last.i * 8, last.ph, ab);   // the previous piece's last Q K^T
         tc_fence_after();
         const uint32_t tm_q = tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16);
 #pragma unroll 1
@@ -717,27 +760,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           }
           TmemRegs<16>::st(tm_q + ch * 4, w);
         }
-        {   // against a token's {mid hi, mid lo, mid hi}: sum hi, sum hi, sum lo
-          const uint32_t both = two_parts(sum * f);
-          uint32_t w[8] = {__byte_perm(both, both, 0x1010), both >> 16};
-          TmemRegs<8>::st(tm_q + 64, w);
-        }
+        const uint32_t both = two_parts(sum * f);   // against a token's {mid hi, mid lo, mid hi}: sum hi, sum hi, sum lo
+        sts128(sbase + C::kOffSum + (uint32_t)kt * 16u, __byte_perm(both, both, 0x1010), both >> 16, 0u, 0u);
         tc_wait_st();
         __syncwarp();
         if (lane == 0) mbar_arrive(qready + qi * 8);
       }
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs) {
-        const int g = gs & 1, ut = u0 + u;
-        const uint32_t tile = sbase + C::kOffK + (uint32_t)g * 32768u;
-        wait(mready + (gs & 3) * 8, (gs >> 2) & 1, ab);
-        wait(sfull + g * 8, ((gs >> 1) - 1) & 1, ab);                                     // the tile has been used
+      for (int u = 0; u < n; ++u, ++gs, s.next()) {
+        const int ut = u0 + u;
+        const uint32_t tile = sbase + C::kOffK + (uint32_t)s.i * 16384u;
+        wait(mready + (gs & 7) * 8, (gs >> 3) & 1, ab);   // (the raw stage is there, the tile has been used: warp 19 has waited for both)
         if (ut < n_prefix) {
-          wait(kfull + slot * 8, phase, ab);
-          expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, sbase + C::kOffKm + (uint32_t)g * 512u, kt);
+          expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, sbase + C::kOffKm + (uint32_t)s.i * 256u, kt);
           __syncwarp();
           if (lane == 0) mbar_arrive(kempty + slot * 8);
-          if (++slot == C::kRingK) { slot = 0; phase ^= 1; }
+          if (++slot == C::kRingK) slot = 0;
         } else {   // the nodes' keys: a thread a row, scaled by a power of two
           const uint4* src = p.kt + ((int64_t)b * p.n + kt) * p.kt_stride + h * 16;
           const bool used = node_used(p, b, kt, lane);
@@ -751,7 +789,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           named_bar(8, 128);
           const int e = tile_exponent(max(max(misc[12], misc[13]), max(misc[14], misc[15])));
           named_bar(8, 128);   // (read by all)
-          if (kt == 0) misc[24 + (gs & 3)] = __float_as_int(times_pow2(a, e));
+          if (kt == 0) misc[32 + (gs & 7)] = __float_as_int(times_pow2(a, e));
           if (kt < kMaxNodes) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
@@ -759,12 +797,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               sts128(chunk_at(tile, kt, ch), w.x, w.y, w.z, w.w);
             }
           }
-          sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + kt * 16), 0u, 0u, 0u, 0u);
+          if (kt < kTile) sts128(sbase + C::kOffMid + (uint32_t)(s.i * 1024 + kt * 16), 0u, 0u, 0u, 0u);
         }
         proxy_fence();
         tc_fence_before();   // (the queries)
         __syncwarp();
-        if (lane == 0) mbar_arrive(kready + g * 8);
+        if (lane == 0) mbar_arrive(kready + s.i * 8);
+        last = s;
       }
       if (lane == 0) { mbar_arrive(kdone + qi * 8); mbar_arrive(iempty + qi * 8); }
     }
@@ -775,7 +814,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     reg_dec<C::kRegExp>();
     const int vt = tid - 384, w4 = warp & 3;
     int gs = 0, slot = 0;
-    uint32_t phase = 0;
+    Slot s;
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
@@ -783,17 +822,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs) {
-        const int g = gs & 1, ut = u0 + u;
-        const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u, vmeta = sbase + C::kOffVm + (uint32_t)g * 512u;
-        wait(mready + (gs & 3) * 8, (gs >> 2) & 1, ab);
+      for (int u = 0; u < n; ++u, ++gs, s.next()) {
+        const int ut = u0 + u;
+        const uint32_t tile = sbase + C::kOffV + (uint32_t)s.i * 16384u;
+        wait(mready + (gs & 7) * 8, (gs >> 3) & 1, ab);   // (and the raw stage)
         if (ut < n_prefix) {
-          wait(vfull + slot * 8, phase, ab);
-          wait(pvdone + g * 8, ((gs >> 1) - 1) & 1, ab);   // the tile has been used
-          expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, vmeta, vt);
+          wait(pvdone + s.i * 8, s.ph ^ 1u, ab);          // the tile has been used
+          expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, sbase + C::kOffVm + (uint32_t)s.i * 256u, vt);
           __syncwarp();
           if (lane == 0) mbar_arrive(vempty + slot * 8);
-          if (++slot == C::kRingV) { slot = 0; phase ^= 1; }
+          if (++slot == C::kRingV) slot = 0;
         } else {
           const bool used = node_used(p, b, vt, lane);
           const uint4* src = p.vt + ((int64_t)b * p.n + vt) * p.vt_stride + h * 16;
@@ -807,8 +845,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           named_bar(3, 128);
           const int e = tile_exponent(max(max(misc[8], misc[9]), max(misc[10], misc[11])));
           named_bar(3, 128);   // (read by all)
-          wait(pvdone + g * 8, ((gs >> 1) - 1) & 1, ab);   // the tile has been used
-          if (vt == 0) misc[4 + (gs & 3)] = e;
+          wait(pvdone + s.i * 8, s.ph ^ 1u, ab);
+          if (vt == 0) misc[40 + (gs & 7)] = e;
           if (vt < ((p.n + 15) & ~15)) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
@@ -819,7 +857,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
         proxy_fence();
         __syncwarp();
-        if (lane == 0) mbar_arrive(vready + g * 8);
+        if (lane == 0) mbar_arrive(vready + s.i * 8);
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
@@ -831,10 +869,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     const bool k_side = warp == 16;
     const int ring = k_side ? C::kRingK : C::kRingV;
     const uint32_t full = k_side ? kfull : vfull, empty = k_side ? kempty : vempty, stages = sbase + (k_side ? C::kOffRK : C::kOffRV);
-    // lane: sub-block lane & 7 of the Anchor, the Residual or the scalars
-    const int what = lane >> 3, kind = !FULL && what == 1 ? 2 : what;
+    // lane: sub-block lane & 3 of the Anchor, the Residual or the scalars
+    const int what = lane >> 2, kind = !FULL && what == 1 ? 2 : what;
     const uint8_t* plane = kind == 0 ? (k_side ? p.ka : p.va) : kind == 1 ? (k_side ? p.kr : p.vr) : reinterpret_cast<const uint8_t*>(k_side ? p.km : p.vm);
-    const uint32_t row_bytes = kind == 2 ? 8u : 64u, at = (kind == 2 ? (uint32_t)C::kPlanes : (uint32_t)kind * 8192u) + (uint32_t)(lane & 7) * 16u * row_bytes;
+    const uint32_t row_bytes = kind == 2 ? 8u : 64u, at = (kind == 2 ? (uint32_t)C::kPlanes : (uint32_t)kind * 4096u) + (uint32_t)(lane & 3) * 16u * row_bytes;
     Cursor cur = {0, 0, 0, 0, 0, 0};
     if (k_side) cur = first_unit(p, blockIdx.x, gridDim.x, lane);
     int slot = 0;
@@ -857,18 +895,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         it.n = items[qi].n; it.len = items[qi].len; it.u0 = items[qi].u0; it.b = items[qi].b; it.h = items[qi].h;
       }
       if (it.n == 0) break;
-      const int n_prefix = (it.len + kTile - 1) / kTile, last = min(it.u0 + it.n, n_prefix), off = (lane & 7) * 16;
-      const bool copies = lane < (FULL ? 24 : 16);
+      const int n_prefix = (it.len + kTile - 1) / kTile, last = min(it.u0 + it.n, n_prefix), off = (lane & 3) * 16;
+      const bool copies = lane < (FULL ? 12 : 8);
       int id = 0;
       if (copies && it.u0 * kTile + off < it.len) id = block_id(p, it.b, it.u0 * kTile + off);
       for (int ut = it.u0; ut < last; ++ut) {
         const int t = ut * kTile + off, now = id;
         if (copies && t + kTile < it.len) id = block_id(p, it.b, t + kTile);
         wait(empty + slot * 8, phase, ab);
-        const int subs = min(8, (it.len - ut * kTile + 15) / 16);   // sub-blocks of 16 tokens with a token of the sequence
+        const int subs = min(4, (it.len - ut * kTile + 15) / 16);   // sub-blocks of 16 tokens with a token of the sequence
         if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)subs * (FULL ? 2048u + 128u : 1024u + 128u));
         __syncwarp();
-        if (copies && (lane & 7) < subs)
+        if (copies && (lane & 3) < subs)
           bulk_g2s(stages + (uint32_t)slot * C::kStage + at, plane + row_at(p, now, it.h, t) * row_bytes, 16u * row_bytes, full + slot * 8);
         if (++slot == ring) { slot = 0; phase ^= 1; }
       }
@@ -881,6 +919,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   if (warp == 19) {
     int gs = 0, kslot = 0, vslot = 0;
     uint32_t kphase = 0, vphase = 0;
+    Slot s;
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
@@ -891,68 +930,59 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const float a = __int_as_float(misc[28 + qi]);
       const int n_prefix = (len + kTile - 1) / kTile;
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs) {
-        const int g = gs & 1, ut = u0 + u;
-        const uint32_t before = ((gs >> 1) - 1) & 1;
+      for (int u = 0; u < n; ++u, ++gs, s.next()) {
+        const int ut = u0 + u;
         if (ut < n_prefix) {
-          // a lane takes four tokens, {scale, zero} of two in a register quadruple
+          // a lane takes two tokens, {scale, zero} each
           wait(kfull + kslot * 8, kphase, ab);
           wait(vfull + vslot * 8, vphase, ab);
-          const uint32_t ka = sbase + C::kOffRK + (uint32_t)kslot * C::kStage + C::kPlanes + (uint32_t)lane * 32u,
-                         va = sbase + C::kOffRV + (uint32_t)vslot * C::kStage + C::kPlanes + (uint32_t)lane * 32u;
-          uint4 k2[2] = {lds128(ka), lds128(ka + 16)}, v2[2] = {lds128(va), lds128(va + 16)};
-          const int room = len - ut * kTile - lane * 4;   // (what lies behind the sequence's end may be anything)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (room <= 2 * i) k2[i].x = k2[i].y = v2[i].x = v2[i].y = 0u;
-            if (room <= 2 * i + 1) k2[i].z = k2[i].w = v2[i].z = v2[i].w = 0u;
-          }
+          uint4 k2 = lds128(sbase + C::kOffRK + (uint32_t)kslot * C::kStage + C::kPlanes + (uint32_t)lane * 16u),
+                v2 = lds128(sbase + C::kOffRV + (uint32_t)vslot * C::kStage + C::kPlanes + (uint32_t)lane * 16u);
+          const int room = len - ut * kTile - lane * 2;   // (what lies behind the sequence's end may be anything)
+          if (room <= 0) k2.x = k2.y = v2.x = v2.y = 0u;
+          if (room <= 1) k2.z = k2.w = v2.z = v2.w = 0u;
           __syncwarp();
           if (lane == 0) { mbar_arrive(kempty + kslot * 8); mbar_arrive(vempty + vslot * 8); }
           if (++kslot == C::kRingK) { kslot = 0; kphase ^= 1; }
           if (++vslot == C::kRingV) { vslot = 0; vphase ^= 1; }
-          float ks[4], km[4], vs[4], vm[4], kmax = 0.0f, vmax = 0.0f;
-          auto mids = [](const uint4 (&x)[2], float* sc, float* mid, float& top) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              sc[2 * i] = __uint_as_float(x[i].x);
-              sc[2 * i + 1] = __uint_as_float(x[i].z);
-              mid[2 * i] = fmaf(128.0f, sc[2 * i], __uint_as_float(x[i].y));
-              mid[2 * i + 1] = fmaf(128.0f, sc[2 * i + 1], __uint_as_float(x[i].w));
-              top = max3(top, fabsf(mid[2 * i]) + 128.0f * fabsf(sc[2 * i]), fabsf(mid[2 * i + 1]) + 128.0f * fabsf(sc[2 * i + 1]));
-            }
+          auto mids = [](const uint4& x, float* sc, float* mid) {   // and the larger magnitude of the two rows
+            sc[0] = __uint_as_float(x.x);
+            sc[1] = __uint_as_float(x.z);
+            mid[0] = fmaf(128.0f, sc[0], __uint_as_float(x.y));
+            mid[1] = fmaf(128.0f, sc[1], __uint_as_float(x.w));
+            return fmaxf(fabsf(mid[0]) + 128.0f * fabsf(sc[0]), fabsf(mid[1]) + 128.0f * fabsf(sc[1]));
           };
-          mids(k2, ks, km, kmax);
-          mids(v2, vs, vm, vmax);
+          float ks[2], km[2], vs[2], vm[2];
+          const float kmax = mids(k2, ks, km), vmax = mids(v2, vs, vm);
           const int ek = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(kmax))) + 3;   // (1152 scales below 2^15.2)
           const int ev = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(vmax)));
           const float fk = pow2(-ek), fv = pow2(-ev);
-          wait(sfull + g * 8, before, ab);    // these places have been read (the softmax's of four tiles before: in front of that Q K^T)
-          wait(vready + g * 8, before, ab);
-          uint32_t kw[4], vw[4];
+          wait(sfull + s.i * 8, s.ph ^ 1u, ab);    // these places have been read (the softmax's of eight tiles before, too)
+          wait(vready + s.i * 8, s.ph ^ 1u, ab);
+          uint32_t kw[2], vw[2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 2; ++i) {
             // what rounding -1152 scale adds to all of a row's keys is taken off their middle
             const float s16 = __half2float(__float2half_rn(ks[i] * fk)), m16 = __half2float(__float2half_rn(-1152.0f * s16));
             kw[i] = pack_f16x2(s16, m16);
             vw[i] = pack_f16x2(vs[i] * fv, vm[i] * fv);
             const uint32_t both = two_parts(km[i] * fk - (m16 + 1152.0f * s16));
-            sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + lane * 64 + i * 16), both, both & 0xFFFFu, 0u, 0u);
+            sts128(sbase + C::kOffMid + (uint32_t)(s.i * 1024 + lane * 32 + i * 16), both, both & 0xFFFFu, 0u, 0u);
           }
-          sts128(sbase + C::kOffKm + (uint32_t)(g * 512 + lane * 16), kw[0], kw[1], kw[2], kw[3]);
-          sts128(sbase + C::kOffVm + (uint32_t)(g * 512 + lane * 16), vw[0], vw[1], vw[2], vw[3]);
+          *reinterpret_cast<uint2*>(smem + C::kOffKm + s.i * 256 + lane * 8) = make_uint2(kw[0], kw[1]);
+          *reinterpret_cast<uint2*>(smem + C::kOffVm + s.i * 256 + lane * 8) = make_uint2(vw[0], vw[1]);
           if (lane == 0) {
-            misc[4 + (gs & 3)] = ev;
-            misc[24 + (gs & 3)] = __float_as_int(times_pow2(a, ek));
+            misc[40 + (gs & 7)] = ev;
+            misc[32 + (gs & 7)] = __float_as_int(times_pow2(a, ek));
           }
           proxy_fence();
         } else {   // (the nodes': by the warps that have their keys and values.  They wait for this warp all the same, so that no barrier is a
                    // phase further than what a wait for it expects)
-          wait(sfull + g * 8, before, ab);
-          wait(vready + g * 8, before, ab);
+          wait(sfull + s.i * 8, s.ph ^ 1u, ab);
+          wait(vready + s.i * 8, s.ph ^ 1u, ab);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(mready + (gs & 3) * 8);
+        if (lane == 0) mbar_arrive(mready + (gs & 7) * 8);
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
@@ -960,60 +990,55 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   }
   // ================================================================================== products
   if (warp == 18) {
-    constexpr uint32_t kIdescS = tc_idesc(128, false), kIdescO = tc_idesc(128, true);
-    const uint32_t k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 16384u);
-    const uint32_t mid_lo[2] = {desc_lo(sbase + C::kOffMid, 4096u), desc_lo(sbase + C::kOffMid + 2048u, 2048u)};   // (zeros behind both)
-    struct { int ic, n, u, gs; } s = {0, 0, 0, 0};   // the next Q K^T
-    bool more = true;
+    constexpr uint32_t kIdescS = tc_idesc(kTile, false), kIdescO = tc_idesc(128, true);
+    const uint32_t k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 8192u), sum_lo = desc_lo(sbase + C::kOffSum, 2048u);
+    Slot q, s;   // of the next Q K^T, of the next P V
     auto qk = [&]() {
-      if (s.u == s.n) {   // the next piece
-        wait(ifull + (s.ic & 1) * 8, (s.ic >> 1) & 1, iab);
-        s.n = items[s.ic & 1].n;
-        s.u = 0;
-        ++s.ic;
-        if (s.n == 0) { more = false; return; }
-      }
-      const int g = s.gs & 1;
-      wait(kready + g * 8, (s.gs >> 1) & 1, ab);   // (and with it the weights that lay in the scores' place: see pready)
+      wait(kready + q.i * 8, q.ph, ab);   // (and with it the queries; the weights that lay in the scores' place are in front of this in the pipe)
       tc_fence_after();
       if (tc_elect()) {
+        const uint32_t d = tmem0 + C::kTmS + q.i * 64, kl = k_lo + (uint32_t)q.i * 1024u;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks)
-          tc_mma_ts(tmem0 + C::kTmS + g * 128, tmem0 + C::kTmQ + ks * 8, desc(k_lo + g * 2048u + (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4)),
-                    kIdescS, ks > 0 ? 1u : 0u);
-        tc_mma_ts(tmem0 + C::kTmS + g * 128, tmem0 + C::kTmQ + 64, desc_plain(g ? mid_lo[1] : mid_lo[0]), kIdescS, 1u);
-        tc_commit(sfull + g * 8);
+          tc_mma_ts(d, tmem0 + C::kTmQ + ks * 8, desc(kl + (uint32_t)(((ks >> 2) * 8192 + (ks & 3) * 32) >> 4)), kIdescS, ks > 0 ? 1u : 0u);
+        tc_mma_ss(d, desc_plain(sum_lo), desc_plain(desc_lo(sbase + C::kOffMid + q.i * 1024, (uint32_t)(kSlots - q.i) * 1024u)), kIdescS, 1u);
+        tc_commit(sfull + q.i * 8);
       }
       __syncwarp();
-      ++s.u;
-      ++s.gs;
+      q.next();
     };
-    qk();
     int gs = 0;
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
-      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0;
+      // (broadcast, so that the compiler knows them to be uniform: products behind loops of lanes' own counts take three times as long to issue)
+      const int n = __shfl_sync(0xFFFFFFFFu, items[qi].n, 0), len = __shfl_sync(0xFFFFFFFFu, items[qi].len, 0), u0 = __shfl_sync(0xFFFFFFFFu, items[qi].u0, 0);
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
+      // (Not ahead into the next piece: its queries wait for this one's last scores, and a piece is dealt out when the one before the last
+      // has been left.)
+      int ahead = 0;
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs) {
+      for (; ahead < min(n, kSlots); ++ahead) qk();
+#pragma unroll 1
+      for (int u = 0; u < n; ++u, ++gs, s.next()) {
         const int g = gs & 1, ut = u0 + u;
         const int steps = ((ut == n_prefix ? p.n : min(kTile, len - ut * kTile)) + 15) / 16;
-        if (more && s.u < s.n) qk();   // (the piece's next scores; the next piece's behind this one's last product)
-        wait(vready + g * 8, (gs >> 1) & 1, ab);
-        wait(pready + g * 8, (gs >> 1) & 1, ab);
+        wait(vready + s.i * 8, s.ph, ab);
+        wait(pready + s.i * 8, s.ph, ab);
         tc_fence_after();
         if (tc_elect()) {
+#pragma unroll 1
           for (int ks = 0; ks < steps; ++ks)
-            tc_mma_ts(tmem0 + C::kTmO, tmem0 + C::kTmS + g * 128 + ks * 8, desc(v_lo + g * 2048u + ks * 128u), kIdescO, u > 0 || ks > 0 ? 1u : 0u);
-          tc_commit(pvdone + g * 8);
+            tc_mma_ts(tmem0 + C::kTmO + g * 128, tmem0 + C::kTmS + s.i * 64 + ks * 8, desc(v_lo + (uint32_t)s.i * 1024u + ks * 128u), kIdescO,
+                      u > 1 || ks > 0 ? 1u : 0u);
+          tc_commit(pvdone + s.i * 8);
         }
         __syncwarp();
+        if (ahead < n) { qk(); ++ahead; }
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
-      if (more) qk();
     }
     bar_arrive(2, kDoneThreads);
   }
@@ -1028,14 +1053,14 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(const __grid_constant
   if (row >= (int64_t)p.B * p.n * p.Hq) return;
   const int64_t bj = row / p.Hq;
   const int hq = (int)(row - bj * p.Hq), b = (int)(bj / p.n), j = (int)(bj - (int64_t)b * p.n), h = hq / p.G;
-  const int c = j * p.G + (hq - h * p.G), rb = c / kTile, r = c - rb * kTile;
+  const int c = j * p.G + (hq - h * p.G), rb = c / kM, r = c - rb * kM;
   const int segment = (b * p.Hkv + h) * p.RB + rb;
   const uint32_t info = ld_dep(p.seg + segment);
   const int first = min((int)(info >> 16), n_cta - 1), n = min((int)(info & 0xFFFFu), n_cta - first) << log_ts, ts = (1 << log_ts) - 1;
   if (n == 1) return;   // written by the attention kernel
   const int64_t slot = (int64_t)p.part_rows * kPartRow;
   const float* src = p.part + (int64_t)(segment + first) * slot + (int64_t)r * kPartRow;
-  const int64_t part = (int64_t)(kTile >> log_ts) * kPartRow;
+  const int64_t part = (int64_t)(kM >> log_ts) * kPartRow;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float M = -INFINITY, L = 0.0f;
   constexpr int kFly = 6;
@@ -1081,7 +1106,7 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(const __grid_constant
 }
 
 // ------------------------------------------------------------------ host side
-constexpr int kWholeTiles = 3;   // up to so many tiles a CTA takes a whole segment
+constexpr int kWholeTiles = 5;   // up to so many tiles a CTA takes a whole segment
 
 struct TreePlan {
   int cols, RB, part_rows, whole, grid, per_seg, log_ts;
@@ -1096,13 +1121,13 @@ lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
   const int64_t cap = (int64_t)s->max_blocks_per_seq * s->block_tokens;
   if (s->head_dim != LYNX_D || s->block_tokens % 16 || G > 16 || n > kMaxNodes || cap >= (1ll << 30)) return LYNX_ERR_UNSUPPORTED;
   pl->cols = n * G;
-  pl->RB = (pl->cols + kTile - 1) / kTile;
+  pl->RB = (pl->cols + kM - 1) / kM;
   pl->segs = (int64_t)B * s->num_kv_heads * pl->RB;
   const int64_t tiles = (cap + kTile - 1) / kTile + 1, sms = sm_count();
   if (pl->segs >= (1 << 24) || pl->segs * tiles >= (1ll << 31)) return LYNX_ERR_UNSUPPORTED;
   pl->whole = tiles <= kWholeTiles;
   pl->log_ts = pl->whole || pl->cols > 64 ? 0 : pl->cols > 32 ? 1 : 2;
-  pl->part_rows = pl->log_ts == 0 && pl->cols < kTile ? pl->cols : kTile;
+  pl->part_rows = pl->log_ts == 0 && pl->cols < kM ? pl->cols : kM;
   pl->per_seg = 0;
   if (pl->whole) {
     pl->grid = (int)pl->segs;
