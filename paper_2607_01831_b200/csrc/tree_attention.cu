@@ -2,7 +2,7 @@
 //
 // For every (sequence, KV head) the n nodes' G = Hq / Hkv query heads are n * G rows; they share the head's keys and values:
 //   S = Q K^T,   p = 2^(a S + e - ref_r),   O += P V,   l += sum p,   out = O / l
-// over the prefix (planes, 64 tokens a tile) and one last tile of the nodes' own BF16 keys and values under the tree's mask.
+// over the prefix (planes, 128 tokens a tile) and one last tile of the nodes' own BF16 keys and values under the tree's mask.
 //
 // A row of codes c is mid + scale (c - 128), mid = zero + 128 scale.  Keys enter as FP16 of scale (c - 128), an error of 2^-12 of a
 // key's deviation from the row's middle (an eighth of a code's step at most), and the middles, which may be far larger, as
@@ -16,18 +16,21 @@
 // l, references and O are FP32.
 //
 // Layout: rows are the M = 128 lanes of tensor memory (n * G > 128 rows: more row blocks), tokens the N of the scores and the K of
-// P V.  A thread owns a row of a tile: no exchange between threads for maxima and sums.  Two warpgroups take the tiles in turn, each with
+// P V.  A thread owns a row of half a tile: no exchange between threads for maxima and sums.  Two warpgroups take the halves in turn, each with
 // references, sums and accumulators of its own, joined at the end of a piece: while one waits for the special function unit, the other
 // loads, compares and stores.  (Two threads a row instead, half of a tile of 128 tokens each, went through the same phases at the same
 // time: 141 us for 128 rows over 131072 tokens.)  Queries are the A operand of the scores in tensor memory, P goes from registers to tensor
 // memory, over the scores, as the A operand of P V; three places for scores, so that Q K^T is never waited for.
 // One CTA per SM; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
-//   warps 0-3, 4-7   softmax, even and odd tiles
-//   warps 8-11       K codes to FP16 into the K tiles, and a piece's queries
-//   warps 12-15      V codes to FP16 values into the V tiles
-//   warps 16, 17     bulk copies of 16-token sub-blocks of the K and V planes into rings; warp 16 deals out the pieces
-//   warp 18          issues every tcgen05.mma: Q K^T three tiles ahead of P V
-//   warp 19          scales and zero points of a tile: what the K and V tiles and the softmax need of them
+//   warps 0-3, 4-7   softmax, even and odd half tiles
+//   warps 8-15       K codes to FP16 into the K tiles, and a piece's queries
+//   warps 16-23      V codes to FP16 values into the V tiles
+//   warp 24          bulk copies of 16-token sub-blocks of the planes into rings; deals out the pieces
+//   warps 25, 27     scales and zero points of a tile's values and keys: what the tiles and the softmax need of them
+//   warp 26          issues every tcgen05.mma: Q K^T three half tiles ahead of P V
+// A hand-off costs its roles some 500 cycles whatever it hands over, and each is in itself a chain of latencies: hence tiles of 128 tokens
+// between the warps that expand codes, of 64 where tensor memory has no room for more, and eight warps for either expansion (173 us by
+// four each and tiles of 64).
 // Work is cut in stream-K form: the (sequence, KV head, row block, tile) list into equal ranges, a piece being a range's part of one
 // segment.  A segment within one CTA is written by it; otherwise partial (ref, l, O) go to the workspace and a dependent
 // kernel joins them.
@@ -43,13 +46,14 @@ namespace {
 
 #include "tc_common.cuh"
 
-constexpr int kTile = 64;           // tokens of a tile
+constexpr int kTile = 128;          // tokens of a tile
+constexpr int kHalf = 64;           // of half a tile: what the softmax and the products take at a time
 constexpr int kM = 128;             // rows of a row block
-constexpr int kSlots = 3;           // places for scores, K and V tiles
+constexpr int kSlots = 3;           // places for scores
 constexpr int kMaxNodes = 64;
 constexpr int kPartRow = 132;       // floats of a partial row: O[128], reference, sum, pad
-constexpr int kThreads = 640;
-constexpr int kDoneThreads = 256 + 3 * 32;   // softmax warpgroups, copies, products
+constexpr int kThreads = 896;
+constexpr int kDoneThreads = 256 + 2 * 32;   // softmax warpgroups, copies, products
 // log2 of the largest of a row's 32 weights when its reference is set; their sum that sets it anew (no weight above it, and FP16 holds 65504)
 constexpr float kTop = 8.0f, kMost = 65000.0f;
 constexpr int kMinExp = -80;        // smallest exponent of a tile's keys or values
@@ -78,25 +82,26 @@ struct TreeParams {
 // references, sums and accumulators of their own; the joining kernel adds them up.  The softmax of a tile is then spread over all warps.
 template <bool FULL, int TS>
 struct Cfg {
-  static constexpr int kRows = kM / TS, kW = kTile / TS;             // rows of a row block; scores of a thread and tile
-  static constexpr int kPlanes = FULL ? 8192 : 4096;                 // of one tensor and tile: [planes][64 tokens][64 B]
-  static constexpr int kStage = kPlanes + 512;                       // and [64] {scale, zero}
-  static constexpr int kRingK = FULL ? 7 : 11, kRingV = FULL ? 6 : 10;
-  static constexpr int kOffK = 0, kOffV = kOffK + kSlots * 16384, kOffRK = kOffV + kSlots * 16384, kOffRV = kOffRK + kRingK * kStage,
-                       kOffMid = kOffRV + kRingV * kStage;           // [kSlots][64] the middles' 8 FP16, and 64 x 8 zeros
-  static constexpr int kOffSum = kOffMid + (kSlots + 1) * 1024;      // [128] the query sums' 8 FP16, and 128 x 8 zeros
-  static constexpr int kOffKm = kOffSum + 2 * 2048;                  // [kSlots][64] half2 {scale, - 1152 scale}
-  static constexpr int kOffVm = kOffKm + kSlots * 256;               // [kSlots][64] half2 {scale, mid}
-  static constexpr int kOffMl = kOffVm + kSlots * 256;               // [2][128] {reference, sum}
+  static constexpr int kRows = kM / TS, kW = kHalf / TS;             // rows of a row block; scores of a thread and half tile
+  static constexpr int kPlanes = FULL ? 16384 : 8192;                // of one tensor and tile: [planes][128 tokens][64 B]
+  static constexpr int kStage = kPlanes + 1024;                      // and [128] {scale, zero}
+  static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 4;
+  static constexpr int kOffK = 0, kOffV = kOffK + 2 * 32768, kOffRK = kOffV + 2 * 32768, kOffRV = kOffRK + kRingK * kStage,
+                       kOffSum = kOffRV + kRingV * kStage;           // [128] the query sums' 8 FP16
+  static constexpr int kOffMid = kOffSum + 2048;                     // [2][128] the middles' 8 FP16
+  static constexpr int kOffZero = kOffMid + 4096;                    // 128 x 8 zeros, the other half of both
+  static constexpr int kOffKm = kOffZero + 2048;                     // [2][128] half2 {scale, - 1152 scale}
+  static constexpr int kOffVm = kOffKm + 2 * 512;                    // [2][128] half2 {scale, mid}
+  static constexpr int kOffMl = kOffVm + 2 * 512;                    // [2][128] {reference, sum}
   static constexpr int kOffItems = kOffMl + 2 * 1024;                // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
   static constexpr int kOffBars = kOffMisc + 256;
-  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 5 * kSlots + 8 + 8;
+  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 3 * kSlots + 8 + 16;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024, "shared memory");
-  static_assert(kOffMid % 128 == 0 && kOffBars % 8 == 0, "alignment");
-  // registers a thread after the split (launched with 96 each): 256 * 144 + 256 * 72 + 128 * 48 = 640 * 96
-  static constexpr int kRegSoft = 144, kRegExp = 72, kRegRest = 48;
+  static_assert(kOffSum % 128 == 0 && kOffBars % 8 == 0, "alignment");
+  // registers a thread after the split (launched with 72 each): 256 * 112 + 512 * 56 + 128 * 56 = 896 * 72
+  static constexpr int kRegSoft = 112, kRegExp = 56, kRegRest = 56;
   static constexpr int kTmS = 0, kTmQ = 192, kTmO = 256;             // [kSlots][64] scores, weights in their place; queries; [2][128] accumulators
 };
 // A place of kSlots and the parity of its round.
@@ -110,6 +115,19 @@ struct Slot {
 
 struct Item {  // a piece: tiles u0 .. u0 + n - 1 of segment (b, h, rb), none: the end
   int b, h, rb, len, u0, n, first_cta, n_contrib;
+};
+
+// The half tiles of a piece: those of the prefix, each two tokens' tile but for the sequence's last, and the nodes', a tile of its own.
+struct Halves {
+  int prefix, n;
+  __device__ __forceinline__ Halves(int u0, int tiles, int len) {
+    const int first = u0 * kTile, end = min(len, (u0 + tiles) * kTile);
+    prefix = max(end - first + kHalf - 1, 0) / kHalf;
+    n = prefix + (u0 + tiles > (len + kTile - 1) / kTile ? 1 : 0);
+  }
+  __device__ __forceinline__ bool nodes(int s) const { return s >= prefix; }
+  __device__ __forceinline__ int side(int s) const { return nodes(s) ? 0 : s & 1; }
+  __device__ __forceinline__ bool last_of_tile(int s) const { return side(s) == 1 || s >= prefix - 1; }
 };
 
 // ------------------------------------------------------------------ PTX
@@ -202,11 +220,6 @@ __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }   // -126 <= e <= 127
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -277,15 +290,15 @@ __device__ __forceinline__ uint32_t two_parts(float x) {
   return pack_f16x2(hi, x - hi);
 }
 
-// A tile's codes by 128 threads: thread i takes the 16-byte chunk i & 3 (32 channels) of rows i >> 2 and 32 on.  Half of the threads take a
+// The codes of half a tile by 128 threads: thread i takes the 16-byte chunk i & 3 (32 channels) of rows i >> 2 and 32 on.  Half of the threads take a
 // chunk's 8-byte halves in the other order: the eight threads of a store's phase then have eight chunk positions, and rows that share
 // their banks in the raw stage are read in different halves.
 // meta: per row, keys {scale, -1152 scale (rounded)} -> (1024 + c) scale - 1152 scale, values {scale, mid} -> (c - 128) scale + mid.
 template <bool FULL, bool VALUES>
-__device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t meta, int i) {
-  const int cc = i & 3, row0 = i >> 2;
+__device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t meta, int i, int row_base) {
+  const int cc = i & 3, row0 = row_base + (i >> 2);
   const uint32_t sw = (uint32_t)(((cc >> 1) ^ (row0 >> 1)) & 1) * 2u;
-  const uint32_t dst = tile + (uint32_t)(cc >> 1) * 8192u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
+  const uint32_t dst = tile + (uint32_t)(cc >> 1) * 16384u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
   const uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16);
   meta += (uint32_t)row0 * 4u;
   uint2 x[2][2], y[2][2];
@@ -295,7 +308,7 @@ __device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t met
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
       x[i][z] = lds64(a + i * 2048u + (sw ^ (uint32_t)(2 * z)) * 4u);
-      y[i][z] = FULL ? lds64(a + i * 2048u + 4096u + (sw ^ (uint32_t)(2 * z)) * 4u) : make_uint2(0x88888888u, 0x88888888u);
+      y[i][z] = FULL ? lds64(a + i * 2048u + 8192u + (sw ^ (uint32_t)(2 * z)) * 4u) : make_uint2(0x88888888u, 0x88888888u);
     }
     sm[i] = lds32(meta + i * 128u);
   }
@@ -314,7 +327,7 @@ __device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t met
   }
 }
 __device__ __forceinline__ uint32_t chunk_at(uint32_t tile, int row, int ch) {   // 16-byte chunk ch (8 channels) of a row
-  return tile + (uint32_t)(ch >> 3) * 8192u + (uint32_t)row * 128u + (uint32_t)(((ch & 7) ^ (row & 7)) * 16);
+  return tile + (uint32_t)(ch >> 3) * 16384u + (uint32_t)row * 128u + (uint32_t)(((ch & 7) ^ (row & 7)) * 16);
 }
 
 // ------------------------------------------------------------------ the cut
@@ -457,35 +470,36 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
-  constexpr uint32_t kRound = 8 * kSlots;
-  const uint32_t kready = vempty + 8 * C::kRingV, sfull = kready + kRound, vready = sfull + kRound, pready = vready + kRound,
-                 pvdone = pready + kRound, mready = pvdone + kRound, ifull = mready + 64, iempty = ifull + 16, qready = iempty + 16,
-                 kdone = qready + 16;
+  // of a half tile: sfull, pready, pvdone; of a tile: kready, kfree, vready, vfree (in turn), mready; of a piece: ifull, iempty, qready, kdone
+  const uint32_t sfull = vempty + 8 * C::kRingV, pready = sfull + 8 * kSlots, pvdone = pready + 8 * kSlots, mready = pvdone + 8 * kSlots,
+                 kready = mready + 64, kfree = kready + 16, vready = kfree + 16, vfree = vready + 16, ifull = vfree + 16, iempty = ifull + 16,
+                 qready = iempty + 16, kdone = qready + 16;
   volatile int* ab = misc;        // (waits for data)
   volatile int* iab = misc + 1;   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
 
   if (tid == 0) {
-    for (int i = 0; i < C::kRingK; ++i) { mbar_init(kfull + i * 8, 1); mbar_init(kempty + i * 8, 5); }
-    for (int i = 0; i < C::kRingV; ++i) { mbar_init(vfull + i * 8, 1); mbar_init(vempty + i * 8, 5); }
+    for (int i = 0; i < C::kRingK; ++i) { mbar_init(kfull + i * 8, 1); mbar_init(kempty + i * 8, 9); }
+    for (int i = 0; i < C::kRingV; ++i) { mbar_init(vfull + i * 8, 1); mbar_init(vempty + i * 8, 9); }
     for (int i = 0; i < kSlots; ++i) {
-      mbar_init(kready + i * 8, 4);
       mbar_init(sfull + i * 8, 1);
-      mbar_init(vready + i * 8, 4);
       mbar_init(pready + i * 8, 4);
       mbar_init(pvdone + i * 8, 1);
     }
-    for (int i = 0; i < 8; ++i) mbar_init(mready + i * 8, 1);
+    for (int i = 0; i < 8; ++i) mbar_init(mready + i * 8, 2);
     for (int i = 0; i < 2; ++i) {
+      mbar_init(kready + i * 8, 8);
+      mbar_init(kfree + i * 8, 1);
+      mbar_init(vready + i * 8, 8);
+      mbar_init(vfree + i * 8, 1);
       mbar_init(qready + i * 8, 4);
       mbar_init(kdone + i * 8, 4);
       mbar_init(ifull + i * 8, 1);
-      mbar_init(iempty + i * 8, 8 + 4 + 4 + 3);   // softmax, K, V, V copies, products, scales
+      mbar_init(iempty + i * 8, 8 + 8 + 8 + 3);   // softmax, K, V, scales, products
     }
     for (int i = 0; i < 64; ++i) misc_s[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (int i = tid; i < 256; i += kThreads) reinterpret_cast<uint32_t*>(smem + C::kOffMid + kSlots * 1024)[i] = 0u;
-  for (int i = tid; i < 512; i += kThreads) reinterpret_cast<uint32_t*>(smem + C::kOffSum + 2048)[i] = 0u;
+  for (int i = tid; i < 512; i += kThreads) reinterpret_cast<uint32_t*>(smem + C::kOffZero)[i] = 0u;
   proxy_fence();
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(misc_s + 2)), "r"(512u) : "memory");
@@ -506,8 +520,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     const int t0 = (r / C::kRows) * C::kW;                                 // this thread's first token of a tile
     constexpr int kCW = C::kW < 32 ? C::kW : 32;                           // scores at a time
     float2* ml = reinterpret_cast<float2*>(smem + C::kOffMl);
-    int gs = 0;
-    Slot s, s2;   // of tile gs, and of tile gs - 2
+    int gt = 0, gs = 0;   // tiles and half tiles so far
+    Slot s, s2;           // of half tile gs, and of half tile gs - 2
     s2.i = 1;
     s2.ph = 1;
     for (int ic = 0;; ++ic) {
@@ -517,27 +531,27 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       if (n == 0) break;
       const int first_cta = items[qi].first_cta, n_contrib = items[qi].n_contrib;
       const int c = rb * kM + (r & (C::kRows - 1)), j = c / p.G, hq = h * p.G + (c - j * p.G);
-      const int n_prefix = (len + kTile - 1) / kTile;
+      const Halves hv(u0, n, len);
       const bool works = rb * kM + ((w4 * 32) & (C::kRows - 1)) < p.cols;
-      bool fresh = true, any = false;   // no reference yet; a tile of this warpgroup's
+      bool fresh = true, any = false;   // no reference yet; a half tile of this warpgroup's
       float ref = 0.0f, l = 0.0f;
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs, s.next(), s2.next()) {
+      for (int u = 0; u < hv.n; ++u, ++gs, s.next(), s2.next()) {
         if ((gs & 1) != g) continue;
         // (No barrier may be more than a phase further than a wait expects: see tests/test_tree_handoffs.py.)
-        wait(mready + (gs & 7) * 8, (gs >> 3) & 1, ab);
-        const int ut = u0 + u;
-        const bool tree = ut == n_prefix;
+        const bool tree = hv.nodes(u);
+        const int t = gt + (tree ? n - 1 : u >> 1);
+        wait(mready + (t & 7) * 8, (t >> 3) & 1, ab);
         if (tree) {   // the factor and the exponent of the nodes
           wait(kdone + qi * 8, (ic >> 1) & 1, ab);
-          wait(vready + s.i * 8, s.ph, ab);
+          wait(vready + (t & 1) * 8, (t >> 1) & 1, ab);
         }
         wait(sfull + s.i * 8, s.ph, ab);
         tc_fence_after();
         if (works) {
-          const int valid = (tree ? p.n : min(kTile, len - ut * kTile)) - t0;
-          const int e = misc[40 + (gs & 7)];
-          const float a = __int_as_float(misc[32 + (gs & 7)]);
+          const int valid = (tree ? p.n : min(kHalf, len - u0 * kTile - u * kHalf)) - t0;
+          const int e = misc[40 + (t & 7)];
+          const float a = __int_as_float(misc[32 + (t & 7)]);
           const uint32_t tm_s = tmem0 + C::kTmS + s.i * 64 + lanes;
           const uint64_t a2 = f2_pack(a, a);
           const bool masked = tree || valid < C::kW;
@@ -641,10 +655,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         any = true;
       }
       // ---- end of the piece: both warpgroups' sums, half of the channels each
-      Slot s1 = s2;   // of tile gs - 1
+      gt += n;
+      Slot s1 = s2;   // of half tile gs - 1
       s1.next();
       wait(pvdone + s1.i * 8, s1.ph, ab);
-      if (n > 1) wait(pvdone + s2.i * 8, s2.ph, ab);
+      if (hv.n > 1) wait(pvdone + s2.i * 8, s2.ph, ab);
       tc_fence_after();
       if (works) {
         const float2 mine = any && !fresh ? make_float2(ref, l) : make_float2(-INFINITY, 0.0f);
@@ -714,19 +729,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     return;
   }
   // ================================================================================== K tile and queries
-  if (warp < 12) {
+  if (warp < 16) {
     reg_dec<C::kRegExp>();
-    const int kt = tid - 256;
-    int gs = 0, slot = 0;
-    Slot s, last;   // of tile gs, and of tile gs - 1
+    const int kt = (tid - 256) & 127, side = (warp >> 2) & 1;   // (the second warpgroup has the tile's second half and no more)
+    int gt = 0, slot = 0;
+    float a = 0.0f;   // factor of the scores, but for the keys' exponent
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
-      float a;   // factor of the scores, but for the keys' exponent
-      {   // queries: a thread a row, all rows scaled by one power of two, the largest below 2^7 (their sums below 2^14)
+      if (side == 0) {   // queries: a thread a row, all rows scaled by one power of two, the largest below 2^7 (their sums below 2^14)
         const int c = rb * kM + (kt & (C::kRows - 1)), j = c / p.G;
         const uint4* src = p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (c - j * p.G)) * 16;
         const bool in = c < p.cols;
@@ -744,7 +758,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         const float f = pow2(-e);
         a = p.sm_log2 * pow2(e);
         if (kt == 0) misc[28 + qi] = __float_as_int(a);
-        if (gs > 0) wait(sfull + last.i * 8, last.ph, ab);   // the previous piece's last Q K^T
+        if (gt > 0) wait(kfree + ((gt - 1) & 1) * 8, ((gt - 1) >> 1) & 1, ab);   // the previous piece's last Q K^T
         tc_fence_after();
         const uint32_t tm_q = tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16);
 #pragma unroll 1
@@ -767,16 +781,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         if (lane == 0) mbar_arrive(qready + qi * 8);
       }
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs, s.next()) {
-        const int ut = u0 + u;
-        const uint32_t tile = sbase + C::kOffK + (uint32_t)s.i * 16384u;
-        wait(mready + (gs & 7) * 8, (gs >> 3) & 1, ab);   // (the raw stage is there, the tile has been used: warp 19 has waited for both)
+      for (int u = 0; u < n; ++u, ++gt) {
+        const int ut = u0 + u, g = gt & 1;
+        const uint32_t tile = sbase + C::kOffK + (uint32_t)g * 32768u;
+        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);   // (the raw stage is there, the tile has been used: warp 27 has waited for both)
         if (ut < n_prefix) {
-          expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, sbase + C::kOffKm + (uint32_t)s.i * 256u, kt);
+          if (len - ut * kTile > kHalf * side)
+            expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, sbase + C::kOffKm + (uint32_t)g * 512u, kt, kHalf * side);
           __syncwarp();
           if (lane == 0) mbar_arrive(kempty + slot * 8);
           if (++slot == C::kRingK) slot = 0;
-        } else {   // the nodes' keys: a thread a row, scaled by a power of two
+        } else if (side == 0) {   // the nodes' keys: a thread a row, scaled by a power of two
           const uint4* src = p.kt + ((int64_t)b * p.n + kt) * p.kt_stride + h * 16;
           const bool used = node_used(p, b, kt, lane);
           float amax = 0.0f;
@@ -789,7 +804,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           named_bar(8, 128);
           const int e = tile_exponent(max(max(misc[12], misc[13]), max(misc[14], misc[15])));
           named_bar(8, 128);   // (read by all)
-          if (kt == 0) misc[32 + (gs & 7)] = __float_as_int(times_pow2(a, e));
+          if (kt == 0) misc[32 + (gt & 7)] = __float_as_int(times_pow2(a, e));
           if (kt < kMaxNodes) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
@@ -797,24 +812,25 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               sts128(chunk_at(tile, kt, ch), w.x, w.y, w.z, w.w);
             }
           }
-          if (kt < kTile) sts128(sbase + C::kOffMid + (uint32_t)(s.i * 1024 + kt * 16), 0u, 0u, 0u, 0u);
+          if (kt < kMaxNodes) sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + kt * 16), 0u, 0u, 0u, 0u);
         }
         proxy_fence();
         tc_fence_before();   // (the queries)
         __syncwarp();
-        if (lane == 0) mbar_arrive(kready + s.i * 8);
-        last = s;
+        if (lane == 0) mbar_arrive(kready + g * 8);
       }
-      if (lane == 0) { mbar_arrive(kdone + qi * 8); mbar_arrive(iempty + qi * 8); }
+      if (lane == 0) {
+        if (side == 0) mbar_arrive(kdone + qi * 8);
+        mbar_arrive(iempty + qi * 8);
+      }
     }
     return;
   }
   // ================================================================================== V tiles
-  if (warp < 16) {
+  if (warp < 24) {
     reg_dec<C::kRegExp>();
-    const int vt = tid - 384, w4 = warp & 3;
-    int gs = 0, slot = 0;
-    Slot s;
+    const int vt = (tid - 512) & 127, w4 = warp & 3, side = (warp >> 2) & 1;
+    int gt = 0, slot = 0;
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
@@ -822,17 +838,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs, s.next()) {
-        const int ut = u0 + u;
-        const uint32_t tile = sbase + C::kOffV + (uint32_t)s.i * 16384u;
-        wait(mready + (gs & 7) * 8, (gs >> 3) & 1, ab);   // (and the raw stage)
+      for (int u = 0; u < n; ++u, ++gt) {
+        const int ut = u0 + u, g = gt & 1;
+        const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u;
+        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);         // (and the raw stage)
+        wait(vfree + g * 8, ((gt >> 1) - 1) & 1, ab);           // the tile has been used
         if (ut < n_prefix) {
-          wait(pvdone + s.i * 8, s.ph ^ 1u, ab);          // the tile has been used
-          expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, sbase + C::kOffVm + (uint32_t)s.i * 256u, vt);
+          if (len - ut * kTile > kHalf * side)
+            expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, sbase + C::kOffVm + (uint32_t)g * 512u, vt, kHalf * side);
           __syncwarp();
           if (lane == 0) mbar_arrive(vempty + slot * 8);
           if (++slot == C::kRingV) slot = 0;
-        } else {
+        } else if (side == 0) {
           const bool used = node_used(p, b, vt, lane);
           const uint4* src = p.vt + ((int64_t)b * p.n + vt) * p.vt_stride + h * 16;
           float amax = 0.0f;
@@ -845,8 +862,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           named_bar(3, 128);
           const int e = tile_exponent(max(max(misc[8], misc[9]), max(misc[10], misc[11])));
           named_bar(3, 128);   // (read by all)
-          wait(pvdone + s.i * 8, s.ph ^ 1u, ab);
-          if (vt == 0) misc[40 + (gs & 7)] = e;
+          if (vt == 0) misc[40 + (gt & 7)] = e;
           if (vt < ((p.n + 15) & ~15)) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
@@ -857,7 +873,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
         proxy_fence();
         __syncwarp();
-        if (lane == 0) mbar_arrive(vready + s.i * 8);
+        if (lane == 0) mbar_arrive(vready + g * 8);
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
@@ -865,149 +881,143 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   }
   reg_dec<C::kRegRest>();
   // ================================================================================== copies
-  if (warp < 18) {
-    const bool k_side = warp == 16;
-    const int ring = k_side ? C::kRingK : C::kRingV;
-    const uint32_t full = k_side ? kfull : vfull, empty = k_side ? kempty : vempty, stages = sbase + (k_side ? C::kOffRK : C::kOffRV);
-    // lane: sub-block lane & 3 of the Anchor, the Residual or the scalars
-    const int what = lane >> 2, kind = !FULL && what == 1 ? 2 : what;
-    const uint8_t* plane = kind == 0 ? (k_side ? p.ka : p.va) : kind == 1 ? (k_side ? p.kr : p.vr) : reinterpret_cast<const uint8_t*>(k_side ? p.km : p.vm);
-    const uint32_t row_bytes = kind == 2 ? 8u : 64u, at = (kind == 2 ? (uint32_t)C::kPlanes : (uint32_t)kind * 4096u) + (uint32_t)(lane & 3) * 16u * row_bytes;
-    Cursor cur = {0, 0, 0, 0, 0, 0};
-    if (k_side) cur = first_unit(p, blockIdx.x, gridDim.x, lane);
-    int slot = 0;
-    uint32_t phase = 1;   // (an empty ring)
+  if (warp == 24) {
+    // what a lane copies of a tile, once or twice: sub-block (lane & 7) of the Anchor, the Residual or the scalars of keys or values
+    struct Job { const uint8_t* src; uint32_t row_bytes, at; bool v, on; } job[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int what = (lane >> 3) + 4 * i;   // FULL: K Anchor, K Residual, V Anchor, V Residual, K scalars, V scalars; else without the Residuals
+      const bool v = FULL ? what == 2 || what == 3 || what == 5 : (what & 1), meta = FULL ? what >= 4 : what >= 2, res = FULL && !meta && (what & 1);
+      const float2* m = v ? p.vm : p.km;
+      job[i].src = meta ? reinterpret_cast<const uint8_t*>(m) : res ? (v ? p.vr : p.kr) : (v ? p.va : p.ka);
+      job[i].row_bytes = meta ? 8u : 64u;
+      job[i].at = (v ? C::kOffRV : C::kOffRK) + (meta ? C::kPlanes : res ? 8192 : 0) + (uint32_t)(lane & 7) * 16u * job[i].row_bytes;
+      job[i].v = v;
+      job[i].on = what < (FULL ? 6 : 4);
+    }
+    Cursor cur = first_unit(p, blockIdx.x, gridDim.x, lane);
+    int kslot = 0, vslot = 0;
+    uint32_t kphase = 1, vphase = 1;   // (empty rings)
+#pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
-      Item it;
-      if (k_side) {
-        it = next_piece(p, cur, blockIdx.x);
-        wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
-        if (lane == 0) {
-          volatile Item* d = items + qi;
-          d->b = it.b; d->h = it.h; d->rb = it.rb; d->len = it.len;
-          d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib;
-          mbar_arrive(ifull + qi * 8);
-        }
-        __syncwarp();
-      } else {
-        wait(ifull + qi * 8, (ic >> 1) & 1, iab);
-        it.n = items[qi].n; it.len = items[qi].len; it.u0 = items[qi].u0; it.b = items[qi].b; it.h = items[qi].h;
+      const Item it = next_piece(p, cur, blockIdx.x);
+      wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
+      if (lane == 0) {
+        volatile Item* d = items + qi;
+        d->b = it.b; d->h = it.h; d->rb = it.rb; d->len = it.len;
+        d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib;
+        mbar_arrive(ifull + qi * 8);
       }
+      __syncwarp();
       if (it.n == 0) break;
-      const int n_prefix = (it.len + kTile - 1) / kTile, last = min(it.u0 + it.n, n_prefix), off = (lane & 3) * 16;
-      const bool copies = lane < (FULL ? 12 : 8);
+      const int n_prefix = (it.len + kTile - 1) / kTile, last = min(it.u0 + it.n, n_prefix), off = (lane & 7) * 16;
       int id = 0;
-      if (copies && it.u0 * kTile + off < it.len) id = block_id(p, it.b, it.u0 * kTile + off);
+      if (it.u0 * kTile + off < it.len) id = block_id(p, it.b, it.u0 * kTile + off);
+#pragma unroll 1
       for (int ut = it.u0; ut < last; ++ut) {
         const int t = ut * kTile + off, now = id;
-        if (copies && t + kTile < it.len) id = block_id(p, it.b, t + kTile);
-        wait(empty + slot * 8, phase, ab);
-        const int subs = min(4, (it.len - ut * kTile + 15) / 16);   // sub-blocks of 16 tokens with a token of the sequence
-        if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)subs * (FULL ? 2048u + 128u : 1024u + 128u));
-        __syncwarp();
-        if (copies && (lane & 3) < subs)
-          bulk_g2s(stages + (uint32_t)slot * C::kStage + at, plane + row_at(p, now, it.h, t) * row_bytes, 16u * row_bytes, full + slot * 8);
-        if (++slot == ring) { slot = 0; phase ^= 1; }
+        if (t + kTile < it.len) id = block_id(p, it.b, t + kTile);
+        const int subs = min(8, (it.len - ut * kTile + 15) / 16);   // sub-blocks of 16 tokens with a token of the sequence
+        const uint32_t bytes = (uint32_t)subs * (FULL ? 2048u + 128u : 1024u + 128u);
+        const int64_t row = (lane & 7) < subs ? row_at(p, now, it.h, t) : 0;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const uint32_t full = v ? vfull + vslot * 8 : kfull + kslot * 8, stage = sbase + (uint32_t)((v ? vslot : kslot) * C::kStage);
+          wait(v ? vempty + vslot * 8 : kempty + kslot * 8, v ? vphase : kphase, ab);
+          if (lane == 0) mbar_expect_tx(full, bytes);
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (job[i].on && job[i].v == (v != 0) && (lane & 7) < subs)
+              bulk_g2s(stage + job[i].at, job[i].src + row * job[i].row_bytes, 16u * job[i].row_bytes, full);
+        }
+        if (++kslot == C::kRingK) { kslot = 0; kphase ^= 1; }
+        if (++vslot == C::kRingV) { vslot = 0; vphase ^= 1; }
       }
-      if (!k_side && lane == 0) mbar_arrive(iempty + qi * 8);
     }
     bar_arrive(2, kDoneThreads);
     return;
   }
   // ================================================================================== scales and zero points
-  if (warp == 19) {
-    int gs = 0, kslot = 0, vslot = 0;
-    uint32_t kphase = 0, vphase = 0;
-    Slot s;
+  if (warp == 25 || warp == 27) {
+    const bool values = warp == 25;
+    const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty;
+    const int ring = values ? C::kRingV : C::kRingK, stages = (values ? C::kOffRV : C::kOffRK) + C::kPlanes;
+    int gt = 0, slot = 0;
+    uint32_t phase = 0;
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0;
       if (n == 0) break;
-      wait(qready + qi * 8, (ic >> 1) & 1, ab);
-      const float a = __int_as_float(misc[28 + qi]);
+      float a = 0.0f;
+      if (!values) {
+        wait(qready + qi * 8, (ic >> 1) & 1, ab);
+        a = __int_as_float(misc[28 + qi]);
+      }
       const int n_prefix = (len + kTile - 1) / kTile;
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs, s.next()) {
-        const int ut = u0 + u;
+      for (int u = 0; u < n; ++u, ++gt) {
+        const int ut = u0 + u, g = gt & 1;
+        // (the nodes' are made by the warps that have their keys and values.  These wait for this warp all the same, so that no barrier is a
+        // phase further than what a wait for it expects)
+        const uint32_t used = values ? vready + g * 8 : kfree + g * 8, before = ((gt >> 1) - 1) & 1;
         if (ut < n_prefix) {
-          // a lane takes two tokens, {scale, zero} each
-          wait(kfull + kslot * 8, kphase, ab);
-          wait(vfull + vslot * 8, vphase, ab);
-          uint4 k2 = lds128(sbase + C::kOffRK + (uint32_t)kslot * C::kStage + C::kPlanes + (uint32_t)lane * 16u),
-                v2 = lds128(sbase + C::kOffRV + (uint32_t)vslot * C::kStage + C::kPlanes + (uint32_t)lane * 16u);
-          const int room = len - ut * kTile - lane * 2;   // (what lies behind the sequence's end may be anything)
-          if (room <= 0) k2.x = k2.y = v2.x = v2.y = 0u;
-          if (room <= 1) k2.z = k2.w = v2.z = v2.w = 0u;
-          __syncwarp();
-          if (lane == 0) { mbar_arrive(kempty + kslot * 8); mbar_arrive(vempty + vslot * 8); }
-          if (++kslot == C::kRingK) { kslot = 0; kphase ^= 1; }
-          if (++vslot == C::kRingV) { vslot = 0; vphase ^= 1; }
-          auto mids = [](const uint4& x, float* sc, float* mid) {   // and the larger magnitude of the two rows
-            sc[0] = __uint_as_float(x.x);
-            sc[1] = __uint_as_float(x.z);
-            mid[0] = fmaf(128.0f, sc[0], __uint_as_float(x.y));
-            mid[1] = fmaf(128.0f, sc[1], __uint_as_float(x.w));
-            return fmaxf(fabsf(mid[0]) + 128.0f * fabsf(sc[0]), fabsf(mid[1]) + 128.0f * fabsf(sc[1]));
-          };
-          float ks[2], km[2], vs[2], vm[2];
-          const float kmax = mids(k2, ks, km), vmax = mids(v2, vs, vm);
-          const int ek = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(kmax))) + 3;   // (1152 scales below 2^15.2)
-          const int ev = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(vmax)));
-          const float fk = pow2(-ek), fv = pow2(-ev);
-          wait(sfull + s.i * 8, s.ph ^ 1u, ab);    // these places have been read (the softmax's of eight tiles before, too)
-          wait(vready + s.i * 8, s.ph ^ 1u, ab);
-          uint32_t kw[2], vw[2];
+          // a lane takes four tokens, {scale, zero} each
+          wait(full + slot * 8, phase, ab);
+          const uint32_t src = sbase + (uint32_t)(stages + slot * C::kStage + lane * 32);
+          const uint4 x[2] = {lds128(src), lds128(src + 16)};
+          const int room = len - ut * kTile - lane * 4;   // (what lies behind the sequence's end may be anything)
+          const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+          float sc[4], mid[4], top = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            // what rounding -1152 scale adds to all of a row's keys is taken off their middle
-            const float s16 = __half2float(__float2half_rn(ks[i] * fk)), m16 = __half2float(__float2half_rn(-1152.0f * s16));
-            kw[i] = pack_f16x2(s16, m16);
-            vw[i] = pack_f16x2(vs[i] * fv, vm[i] * fv);
-            const uint32_t both = two_parts(km[i] * fk - (m16 + 1152.0f * s16));
-            sts128(sbase + C::kOffMid + (uint32_t)(s.i * 1024 + lane * 32 + i * 16), both, both & 0xFFFFu, 0u, 0u);
+          for (int i = 0; i < 4; ++i) {
+            sc[i] = room > i ? __uint_as_float(w[2 * i]) : 0.0f;
+            mid[i] = room > i ? fmaf(128.0f, sc[i], __uint_as_float(w[2 * i + 1])) : 0.0f;
+            top = fmaxf(top, fabsf(mid[i]) + 128.0f * fabsf(sc[i]));
           }
-          *reinterpret_cast<uint2*>(smem + C::kOffKm + s.i * 256 + lane * 8) = make_uint2(kw[0], kw[1]);
-          *reinterpret_cast<uint2*>(smem + C::kOffVm + s.i * 256 + lane * 8) = make_uint2(vw[0], vw[1]);
+          const int e = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top))) + (values ? 0 : 3);   // (1152 scales below 2^15.2)
+          if (lane == 0) mbar_arrive(empty + slot * 8);
+          if (++slot == ring) { slot = 0; phase ^= 1; }
+          const float f = pow2(-e);
+          wait(used, before, ab);    // these places have been read (the softmax's of eight tiles before, too)
+          uint32_t o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (values) {
+              o[i] = pack_f16x2(sc[i] * f, mid[i] * f);
+            } else {
+              // what rounding -1152 scale adds to all of a row's keys is taken off their middle
+              const float s16 = __half2float(__float2half_rn(sc[i] * f)), m16 = __half2float(__float2half_rn(-1152.0f * s16));
+              o[i] = pack_f16x2(s16, m16);
+              const uint32_t both = two_parts(mid[i] * f - (m16 + 1152.0f * s16));
+              sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + lane * 64 + i * 16), both, both & 0xFFFFu, 0u, 0u);
+            }
+          }
+          sts128(sbase + (values ? C::kOffVm : C::kOffKm) + (uint32_t)(g * 512 + lane * 16), o[0], o[1], o[2], o[3]);
           if (lane == 0) {
-            misc[40 + (gs & 7)] = ev;
-            misc[32 + (gs & 7)] = __float_as_int(times_pow2(a, ek));
+            if (values) misc[40 + (gt & 7)] = e;
+            else misc[32 + (gt & 7)] = __float_as_int(times_pow2(a, e));
           }
-          proxy_fence();
-        } else {   // (the nodes': by the warps that have their keys and values.  They wait for this warp all the same, so that no barrier is a
-                   // phase further than what a wait for it expects)
-          wait(sfull + s.i * 8, s.ph ^ 1u, ab);
-          wait(vready + s.i * 8, s.ph ^ 1u, ab);
+          if (!values) proxy_fence();
+        } else {
+          wait(used, before, ab);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(mready + (gs & 7) * 8);
+        if (lane == 0) mbar_arrive(mready + (gt & 7) * 8);
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
     return;
   }
   // ================================================================================== products
-  if (warp == 18) {
-    constexpr uint32_t kIdescS = tc_idesc(kTile, false), kIdescO = tc_idesc(128, true);
-    const uint32_t k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 8192u), sum_lo = desc_lo(sbase + C::kOffSum, 2048u);
+  if (warp == 26) {
+    constexpr uint32_t kIdescS = tc_idesc(kHalf, false), kIdescO = tc_idesc(128, true);
+    const uint32_t k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 16384u), sum_lo = desc_lo(sbase + C::kOffSum, C::kOffZero - C::kOffSum);
     Slot q, s;   // of the next Q K^T, of the next P V
-    auto qk = [&]() {
-      wait(kready + q.i * 8, q.ph, ab);   // (and with it the queries; the weights that lay in the scores' place are in front of this in the pipe)
-      tc_fence_after();
-      if (tc_elect()) {
-        const uint32_t d = tmem0 + C::kTmS + q.i * 64, kl = k_lo + (uint32_t)q.i * 1024u;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          tc_mma_ts(d, tmem0 + C::kTmQ + ks * 8, desc(kl + (uint32_t)(((ks >> 2) * 8192 + (ks & 3) * 32) >> 4)), kIdescS, ks > 0 ? 1u : 0u);
-        tc_mma_ss(d, desc_plain(sum_lo), desc_plain(desc_lo(sbase + C::kOffMid + q.i * 1024, (uint32_t)(kSlots - q.i) * 1024u)), kIdescS, 1u);
-        tc_commit(sfull + q.i * 8);
-      }
-      __syncwarp();
-      q.next();
-    };
-    int gs = 0;
+    int gt = 0, gs = 0;
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
@@ -1015,29 +1025,52 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       // (broadcast, so that the compiler knows them to be uniform: products behind loops of lanes' own counts take three times as long to issue)
       const int n = __shfl_sync(0xFFFFFFFFu, items[qi].n, 0), len = __shfl_sync(0xFFFFFFFFu, items[qi].len, 0), u0 = __shfl_sync(0xFFFFFFFFu, items[qi].u0, 0);
       if (n == 0) break;
-      const int n_prefix = (len + kTile - 1) / kTile;
+      const Halves hv(u0, n, len);
+      auto qk = [&](int u) {
+        const int t = gt + (hv.nodes(u) ? n - 1 : u >> 1), side = hv.side(u), at = (t & 1) * 2 + side;
+        if (side == 0) wait(kready + (t & 1) * 8, (t >> 1) & 1, ab);   // (and with it the queries; the weights that lay in the scores' place are in front in the pipe)
+        tc_fence_after();
+        if (tc_elect()) {
+          const uint32_t d = tmem0 + C::kTmS + q.i * 64, kl = k_lo + (uint32_t)((t & 1) * 2048 + side * 512);
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)
+            tc_mma_ts(d, tmem0 + C::kTmQ + ks * 8, desc(kl + (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4)), kIdescS, ks > 0 ? 1u : 0u);
+          tc_mma_ss(d, desc_plain(sum_lo), desc_plain(desc_lo(sbase + C::kOffMid + at * 1024, (uint32_t)(4 - at) * 1024u)), kIdescS, 1u);
+          tc_commit(sfull + q.i * 8);
+          if (hv.last_of_tile(u)) tc_commit(kfree + (t & 1) * 8);
+        }
+        __syncwarp();
+        q.next();
+      };
       // (Not ahead into the next piece: its queries wait for this one's last scores, and a piece is dealt out when the one before the last
       // has been left.)
       int ahead = 0;
 #pragma unroll 1
-      for (; ahead < min(n, kSlots); ++ahead) qk();
+      for (; ahead < min(hv.n, kSlots); ++ahead) qk(ahead);
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gs, s.next()) {
-        const int g = gs & 1, ut = u0 + u;
-        const int steps = ((ut == n_prefix ? p.n : min(kTile, len - ut * kTile)) + 15) / 16;
-        wait(vready + s.i * 8, s.ph, ab);
+      for (int u = 0; u < hv.n; ++u, ++gs, s.next()) {
+        const int t = gt + (hv.nodes(u) ? n - 1 : u >> 1), side = hv.side(u);
+        const int steps = ((hv.nodes(u) ? p.n : min(kHalf, len - u0 * kTile - u * kHalf)) + 15) / 16;
+        if (side == 0) wait(vready + (t & 1) * 8, (t >> 1) & 1, ab);
         wait(pready + s.i * 8, s.ph, ab);
         tc_fence_after();
         if (tc_elect()) {
+          const uint32_t d = tmem0 + C::kTmO + (gs & 1) * 128, a = tmem0 + C::kTmS + s.i * 64, vl = v_lo + (uint32_t)((t & 1) * 2048 + side * 512);
+          tc_mma_ts(d, a, desc(vl), kIdescO, u > 1 ? 1u : 0u);
+          if (steps == 4) {
+#pragma unroll
+            for (int ks = 1; ks < 4; ++ks) tc_mma_ts(d, a + ks * 8, desc(vl + ks * 128u), kIdescO, 1u);
+          } else {
 #pragma unroll 1
-          for (int ks = 0; ks < steps; ++ks)
-            tc_mma_ts(tmem0 + C::kTmO + g * 128, tmem0 + C::kTmS + s.i * 64 + ks * 8, desc(v_lo + (uint32_t)s.i * 1024u + ks * 128u), kIdescO,
-                      u > 1 || ks > 0 ? 1u : 0u);
+            for (int ks = 1; ks < steps; ++ks) tc_mma_ts(d, a + ks * 8, desc(vl + ks * 128u), kIdescO, 1u);
+          }
           tc_commit(pvdone + s.i * 8);
+          if (hv.last_of_tile(u)) tc_commit(vfree + (t & 1) * 8);
         }
         __syncwarp();
-        if (ahead < n) { qk(); ++ahead; }
+        if (ahead < hv.n) { qk(ahead); ++ahead; }
       }
+      gt += n;
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
     bar_arrive(2, kDoneThreads);
@@ -1106,7 +1139,7 @@ __global__ void __launch_bounds__(128) tree_combine_kernel(const __grid_constant
 }
 
 // ------------------------------------------------------------------ host side
-constexpr int kWholeTiles = 5;   // up to so many tiles a CTA takes a whole segment
+constexpr int kWholeTiles = 3;   // up to so many tiles a CTA takes a whole segment
 
 struct TreePlan {
   int cols, RB, part_rows, whole, grid, per_seg, log_ts;

@@ -37,18 +37,30 @@ class Place:
         assert self.tile == tile, f"{self.name}: {self.tile} instead of {tile}"
 
 
-N = 3       # places for scores and tiles
+N = 3       # places for scores
+
+
+def _halves(n, tree, short):
+    """Half tiles of a piece of n tiles: (tile, whether it is its tile's first, its last).  short: the prefix ends in a first half."""
+    out = []
+    for t in range(n - 1 if tree else n):
+        one = short and t == (n - 2 if tree else n - 1)
+        out += [(t, True, one)] + ([] if one else [(t, False, True)])
+    return out + ([(n - 1, True, True)] if tree else [])
 
 
 def _run(pieces, ring_k, ring_v, rng, softmax=4):
-    """pieces: (tiles, whether the last is the nodes').  Warps of a role that only arrive together are one here."""
+    """pieces: (tiles, whether the last is the nodes', whether the prefix ends in the first half of a tile).  Warps of a role that
+    only arrive together are one here."""
     B = {}
-    for name, n, count in (("kfull", ring_k, 1), ("kempty", ring_k, 2), ("vfull", ring_v, 1), ("vempty", ring_v, 2), ("kready", N, 1), ("sfull", N, 1),
-                           ("mready", 8, 1), ("vready", N, 1), ("pready", N, softmax), ("pvdone", N, 1), ("ifull", 2, 1),
-                           ("iempty", 2, 2 * softmax + 5), ("qready", 2, 1), ("kdone", 2, 1)):
+    for name, n, count in (("kfull", ring_k, 1), ("kempty", ring_k, 3), ("vfull", ring_v, 1), ("vempty", ring_v, 3), ("kready", 2, 2), ("sfull", N, 1),
+                           ("mready", 8, 2), ("vready", 2, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", 2, 1), ("vfree", 2, 1),
+                           ("ifull", 2, 1), ("iempty", 2, 2 * softmax + 7), ("qready", 2, 1), ("kdone", 2, 1)):
         B[name] = [Barrier(count) for _ in range(n)]
     rawk, rawv = [Place(f"raw K {i}") for i in range(ring_k)], [Place(f"raw V {i}") for i in range(ring_v)]
-    ktile, vtile, vm, km, mids, S = ([Place(f"{x} {i}") for i in range(N)] for x in ("K", "V", "vm", "km", "mid", "S"))
+    S = [Place(f"S {i}") for i in range(N)]
+    vm, km, mids = ([Place(f"{x} {i}") for i in range(2)] for x in ("vm", "km", "mid"))
+    ktile, vtile = ([[Place(f"{x} {i} {j}") for j in range(2)] for i in range(2)] for x in ("K", "V"))
     factor, exp = ([Place(f"{x} {i}") for i in range(8)] for x in ("a", "e"))
     item, O, Q = [Place("item 0"), Place("item 1")], [Place("O 0"), Place("O 1")], Place("Q")
     pair = [[0, 0] for _ in range(softmax)]         # arrivals of a row's two warps at the barriers at the end of a piece
@@ -62,144 +74,150 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
     def get(ic):
         yield from wait("ifull", ic & 1, ic >> 1)
         item[ic & 1].read(ic)
-        return pieces[ic] if ic < len(pieces) else (0, False)
+        return pieces[ic] if ic < len(pieces) else (0, False, False)
 
     def raw_tiles(n, tree):
         return n - 1 if tree else n
 
-    def copies(k_side):
-        full, empty, ring, place = ("kfull", "kempty", ring_k, rawk) if k_side else ("vfull", "vempty", ring_v, rawv)
-        slot, phase, t, gs = 0, 1, 0, 0
+    def copies():
+        ks, vs, kp, vp, gt = 0, 0, 1, 1, 0
         for ic in range(len(pieces) + 1):
-            if k_side:
-                yield from wait("iempty", ic & 1, (ic >> 1) - 1)
-                item[ic & 1].write(ic)
-                B["ifull"][ic & 1].arrive()
-                n, tree = pieces[ic] if ic < len(pieces) else (0, False)
-            else:
-                n, tree = yield from get(ic)
+            yield from wait("iempty", ic & 1, (ic >> 1) - 1)
+            item[ic & 1].write(ic)
+            B["ifull"][ic & 1].arrive()
+            n, tree, _ = pieces[ic] if ic < len(pieces) else (0, False, False)
             if n == 0:
                 return
             for _ in range(raw_tiles(n, tree)):
-                yield from wait(empty, slot, phase)
-                place[slot].write(gs)
-                B[full][slot].arrive()
-                gs += 1
-                slot, phase = (0, phase ^ 1) if slot + 1 == ring else (slot + 1, phase)
-            gs += tree
-            if not k_side:
-                B["iempty"][ic & 1].arrive()
+                yield from wait("kempty", ks, kp)
+                rawk[ks].write(gt)
+                B["kfull"][ks].arrive()
+                yield from wait("vempty", vs, vp)
+                rawv[vs].write(gt)
+                B["vfull"][vs].arrive()
+                gt += 1
+                ks, kp = (0, kp ^ 1) if ks + 1 == ring_k else (ks + 1, kp)
+                vs, vp = (0, vp ^ 1) if vs + 1 == ring_v else (vs + 1, vp)
+            gt += tree
 
-    def k_tiles():
-        gs = slot = 0
+    def k_tiles(side):
+        gt = slot = 0
         for ic in range(len(pieces) + 1):
-            n, tree = yield from get(ic)
+            n, tree, short = yield from get(ic)
             if n == 0:
                 return
-            if gs > 0:
-                yield from wait("sfull", (gs - 1) % N, (gs - 1) // N)
-            Q.write(ic)
-            B["qready"][ic & 1].arrive()
+            if side == 0:
+                if gt > 0:
+                    yield from wait("kfree", (gt - 1) & 1, (gt - 1) >> 1)
+                Q.write(ic)
+                B["qready"][ic & 1].arrive()
             for u in range(n):
-                g = gs % N
-                yield from wait("mready", gs & 7, gs >> 3)
-                ktile[g].write(gs)
+                g = gt & 1
+                yield from wait("mready", gt & 7, gt >> 3)
                 if u < raw_tiles(n, tree):
-                    rawk[slot].read(gs)
-                    km[g].read(gs)
+                    ktile[g][side].write(gt)
+                    rawk[slot].read(gt)
+                    km[g].read(gt)
                     km[g].readers += 1
                     yield
                     km[g].readers -= 1
                     B["kempty"][slot].arrive()
                     slot = (slot + 1) % ring_k
-                else:
-                    factor[gs & 7].write(gs)
-                    mids[g].write(gs)
+                elif side == 0:
+                    ktile[g][0].write(gt)
+                    factor[gt & 7].write(gt)
+                    mids[g].write(gt)
                 B["kready"][g].arrive()
-                gs += 1
-            B["kdone"][ic & 1].arrive()
+                gt += 1
+            if side == 0:
+                B["kdone"][ic & 1].arrive()
             B["iempty"][ic & 1].arrive()
 
-    def v_tiles():
-        gs = slot = 0
+    def v_tiles(side):
+        gt = slot = 0
         for ic in range(len(pieces) + 1):
-            n, tree = yield from get(ic)
+            n, tree, short = yield from get(ic)
             if n == 0:
                 return
             for u in range(n):
-                g = gs % N
-                yield from wait("mready", gs & 7, gs >> 3)
-                yield from wait("pvdone", g, gs // N - 1)
-                vtile[g].write(gs)
+                g = gt & 1
+                yield from wait("mready", gt & 7, gt >> 3)
+                yield from wait("vfree", g, (gt >> 1) - 1)
                 if u < raw_tiles(n, tree):
-                    rawv[slot].read(gs)
-                    vm[g].read(gs)
+                    vtile[g][side].write(gt)
+                    rawv[slot].read(gt)
+                    vm[g].read(gt)
                     vm[g].readers += 1
                     yield
                     vm[g].readers -= 1
                     B["vempty"][slot].arrive()
                     slot = (slot + 1) % ring_v
-                else:
-                    exp[gs & 7].write(gs)
+                elif side == 0:
+                    vtile[g][0].write(gt)
+                    exp[gt & 7].write(gt)
                 B["vready"][g].arrive()
-                gs += 1
+                gt += 1
             B["iempty"][ic & 1].arrive()
 
-    def scales():
-        gs = ks = kp = vs = vp = 0
+    def scales(values):
+        full, empty, ring, raw = ("vfull", "vempty", ring_v, rawv) if values else ("kfull", "kempty", ring_k, rawk)
+        gt = slot = phase = 0
         for ic in range(len(pieces) + 1):
-            n, tree = yield from get(ic)
+            n, tree, _ = yield from get(ic)
             if n == 0:
                 return
-            yield from wait("qready", ic & 1, ic >> 1)
+            if not values:
+                yield from wait("qready", ic & 1, ic >> 1)
             for u in range(n):
-                g = gs % N
+                g = gt & 1
                 prefix = u < raw_tiles(n, tree)
                 if prefix:
-                    yield from wait("kfull", ks, kp)
-                    yield from wait("vfull", vs, vp)
-                    rawk[ks].read(gs)
-                    rawv[vs].read(gs)
-                    B["kempty"][ks].arrive()
-                    B["vempty"][vs].arrive()
-                    ks, kp = (0, kp ^ 1) if ks + 1 == ring_k else (ks + 1, kp)
-                    vs, vp = (0, vp ^ 1) if vs + 1 == ring_v else (vs + 1, vp)
-                yield from wait("sfull", g, gs // N - 1)
-                yield from wait("vready", g, gs // N - 1)
+                    yield from wait(full, slot, phase)
+                    raw[slot].read(gt)
+                    B[empty][slot].arrive()
+                    slot, phase = (0, phase ^ 1) if slot + 1 == ring else (slot + 1, phase)
+                yield from wait("vready" if values else "kfree", g, (gt >> 1) - 1)
                 if prefix:
-                    for x in (km[g], vm[g], mids[g], exp[gs & 7], factor[gs & 7]):
-                        x.write(gs)
-                B["mready"][gs & 7].arrive()
-                gs += 1
+                    for x in (vm[g], exp[gt & 7]) if values else (km[g], mids[g], factor[gt & 7]):
+                        x.write(gt)
+                B["mready"][gt & 7].arrive()
+                gt += 1
             B["iempty"][ic & 1].arrive()
 
     def products():
-        ahead = gs = 0
+        gt = gs = ahead = 0
 
-        def qk(ic):
+        def qk(ic, half):
             nonlocal ahead
-            yield from wait("kready", ahead % N, ahead // N)
+            t, first, last = half
+            t += gt
+            if first:
+                yield from wait("kready", t & 1, t >> 1)
             Q.readers += 1
-            ktile[ahead % N].readers += 1
-            mids[ahead % N].readers += 1
-            issued.append(("qk", ahead, ic, False))
+            ktile[t & 1][not first].readers += 1
+            mids[t & 1].readers += 1
+            issued.append(("qk", ahead, ic, t, first, last, False))
             ahead += 1
 
         for ic in range(len(pieces) + 1):
-            n, _ = yield from get(ic)
+            n, tree, short = yield from get(ic)
             if n == 0:
                 return
-            end = gs + n
-            while ahead < min(end, gs + N):
-                yield from qk(ic)
-            for u in range(n):
-                yield from wait("vready", gs % N, gs // N)
+            halves = _halves(n, tree, short)
+            start = gs
+            while ahead - start < min(len(halves), N):
+                yield from qk(ic, halves[ahead - start])
+            for u, (t, first, last) in enumerate(halves):
+                t += gt
+                if first:
+                    yield from wait("vready", t & 1, t >> 1)
                 yield from wait("pready", gs % N, gs // N)
-                vtile[gs % N].readers += 1
-                issued.append(("pv", gs, ic, u < 2))
+                vtile[t & 1][not first].readers += 1
+                issued.append(("pv", gs, ic, t, first, last, u < 2))
                 gs += 1
-                if ahead < end:
-                    yield from qk(ic)
+                if ahead - start < len(halves):
+                    yield from qk(ic, halves[ahead - start])
+            gt += n
             B["iempty"][ic & 1].arrive()
 
     def tensor_core():
@@ -207,49 +225,54 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             if not issued:
                 yield
                 continue
-            kind, gs, ic, first = issued[0]      # (in order, one behind the other)
-            g = gs % N
+            kind, gs, ic, t, first, last, fresh = issued[0]      # (in order, one behind the other)
             if kind == "qk":
-                S[g].write(gs)
-            elif first:
+                S[gs % N].write(gs)
+            elif fresh:
                 O[gs & 1].write(ic)
             yield
             issued.pop(0)
             if kind == "qk":
                 Q.read(ic)
-                ktile[g].read(gs)
-                mids[g].read(gs)
-                mids[g].readers -= 1
+                ktile[t & 1][not first].read(t)
+                mids[t & 1].read(t)
+                mids[t & 1].readers -= 1
                 Q.readers -= 1
-                ktile[g].readers -= 1
-                B["sfull"][g].arrive()
+                ktile[t & 1][not first].readers -= 1
+                B["sfull"][gs % N].arrive()
+                if last:
+                    B["kfree"][t & 1].arrive()
             else:
-                S[g].read(gs)
-                vtile[g].read(gs)
+                S[gs % N].read(gs)
+                vtile[t & 1][not first].read(t)
                 O[gs & 1].read(ic)
-                vtile[g].readers -= 1
-                B["pvdone"][g].arrive()
+                vtile[t & 1][not first].readers -= 1
+                B["pvdone"][gs % N].arrive()
+                if last:
+                    B["vfree"][t & 1].arrive()
 
     def softmax_warp(group, w):
-        gs = turn = 0
+        gt = gs = turn = 0
         for ic in range(len(pieces) + 1):
-            n, tree = yield from get(ic)
+            n, tree, short = yield from get(ic)
             if n == 0:
                 return
-            first = True
-            for u in range(n):
+            first, halves = True, _halves(n, tree, short)
+            for u, (t, _, _) in enumerate(halves):
                 if gs & 1 != group:
                     gs += 1
                     continue
-                g = gs % N
-                yield from wait("mready", gs & 7, gs >> 3)
-                if tree and u == n - 1:
+                g, t = gs % N, t + gt
+                yield from wait("mready", t & 7, t >> 3)
+                if tree and u == len(halves) - 1:
                     yield from wait("kdone", ic & 1, ic >> 1)
-                    yield from wait("vready", g, gs // N)
+                    yield from wait("vready", t & 1, t >> 1)
                 yield from wait("sfull", g, gs // N)
-                places = (S[g], factor[gs & 7], exp[gs & 7])
+                S[g].read(gs)
+                for p in (factor[t & 7], exp[t & 7]):
+                    p.read(t)
+                places = (S[g], factor[t & 7], exp[t & 7])
                 for p in places:
-                    p.read(gs)
                     p.readers += 1
                 yield
                 if not first and rng.random() < 0.2:      # the reference is raised
@@ -260,9 +283,10 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 first = False
                 gs += 1
             yield from wait("pvdone", (gs - 1) % N, (gs - 1) // N)
-            if n > 1:
+            gt += n
+            if len(halves) > 1:
                 yield from wait("pvdone", (gs - 2) % N, (gs - 2) // N)
-            used = O[:] if n > 1 else [O[(gs - 1) & 1]]
+            used = O[:] if len(halves) > 1 else [O[(gs - 1) & 1]]
             for o in used:
                 o.read(ic)
                 o.readers += 1
@@ -275,7 +299,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 yield
             B["iempty"][ic & 1].arrive()
 
-    roles = [copies(True), copies(False), k_tiles(), v_tiles(), scales(), products()] + [softmax_warp(g, w) for g in range(2) for w in range(softmax)]
+    roles = [copies(), k_tiles(0), k_tiles(1), v_tiles(0), v_tiles(1), scales(False), scales(True), products()] + [softmax_warp(g, w) for g in range(2) for w in range(softmax)]
     core = tensor_core()
     speed = [rng.choice([1, 1, 1, 3, 30, 200]) for _ in roles]
     core_speed, idle = rng.choice([1, 3, 30]), 0
@@ -296,11 +320,11 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
     assert not issued
 
 
-@pytest.mark.parametrize("rings", [(7, 6), (2, 5), (1, 1)])
+@pytest.mark.parametrize("rings", [(3, 2), (5, 4), (1, 1)])
 def test_every_role_ends(rings):
     rng = random.Random(9)
     for _ in range(20):
-        pieces = [(rng.choice([1, 1, 2, 3, 4, 7, 12]), rng.random() < 0.5) for _ in range(rng.randint(1, 6))]
+        pieces = [(rng.choice([1, 1, 2, 3, 4, 7, 12]), rng.random() < 0.5, rng.random() < 0.5) for _ in range(rng.randint(1, 6))]
         _run(pieces, *rings, rng, softmax=rng.choice([1, 4]))
 
 
@@ -308,11 +332,10 @@ def test_the_kernel_waits_for_what_is_played():
     """The waits of the roles in the source, by barrier."""
     code = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "tree_attention.cu")).read())
     code = code[code.index("tree_attention_kernel("):code.index("tree_combine_kernel(")]
-    cuts = ["if (warp < 8) {", "if (warp < 12) {", "if (warp < 16) {", "if (warp < 18) {", "if (warp == 19) {", "if (warp == 18) {"]
+    cuts = ["if (warp < 8) {", "if (warp < 16) {", "if (warp < 24) {", "if (warp == 24) {", "if (warp == 25 || warp == 27) {", "if (warp == 26) {"]
     at = [code.index(x) for x in cuts] + [len(code)]
     waits = [sorted(set(re.findall(r"\bwait\((\w+)", code[a:b]))) for a, b in zip(at, at[1:])]
-    assert waits == [["ifull", "kdone", "mready", "pvdone", "sfull", "vready"], ["ifull", "mready", "sfull"],
-                     ["ifull", "mready", "pvdone"], ["empty", "iempty", "ifull"],
-                     ["ifull", "kfull", "qready", "sfull", "vfull", "vready"], ["ifull", "kready", "pready", "vready"]]
+    assert waits == [["ifull", "kdone", "mready", "pvdone", "sfull", "vready"], ["ifull", "kfree", "mready"], ["ifull", "mready", "vfree"],
+                     ["iempty", "v"], ["full", "ifull", "qready", "used"], ["ifull", "kready", "pready", "vready"]]
     land, done, free = (code.index(x) for x in ("land_after_abort(", "named_bar(2, kDoneThreads)", "tcgen05.dealloc"))
     assert done < land < free and len(re.findall(r"bar_arrive\(2, kDoneThreads\)", code)) == 2
