@@ -25,15 +25,19 @@
 //   warps 0-3, 4-7   softmax, even and odd half tiles
 //   warps 8-15       K codes to FP16 into the K tiles, and a piece's queries
 //   warps 16-23      V codes to FP16 values into the V tiles
-//   warp 24          bulk copies of 16-token sub-blocks of the planes into rings; deals out the pieces
-//   warps 25, 27     scales and zero points of a tile's values and keys: what the tiles and the softmax need of them
+//   warp 24          copies of K planes into a ring, four 16-token sub-blocks at a time; deals out the pieces
+//   warp 25          the same of V planes; the values' scales and zero points: what the V tiles and the softmax need of them
+//   warp 27          the same of the keys
 //   warp 26          issues every tcgen05.mma: Q K^T three half tiles ahead of P V
-// A hand-off costs its roles some 500 cycles whatever it hands over, and each is in itself a chain of latencies: hence tiles of 128 tokens
+// The copy engine takes some 35 cycles per row of a copy and a lane that issues copies of one sub-block each some 80: 48 of them a tile, planes
+// and scales, took 4000 cycles (140 us for 128 rows over 131072 tokens).  Hence gathers of four sub-blocks by two warps, and plain loads,
+// two tiles ahead, of the scales.  A hand-off costs its roles some 500 cycles whatever it hands over, and each is in itself a chain of latencies: hence tiles of 128 tokens
 // between the warps that expand codes, of 64 where tensor memory has no room for more, and eight warps for either expansion (173 us by
 // four each and tiles of 64).
 // Work is cut in stream-K form: the (sequence, KV head, row block, tile) list into equal ranges, a piece being a range's part of one
 // segment.  A segment within one CTA is written by it; otherwise partial (ref, l, O) go to the workspace and a dependent
 // kernel joins them.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -53,7 +57,7 @@ constexpr int kSlots = 3;           // places for scores
 constexpr int kMaxNodes = 64;
 constexpr int kPartRow = 132;       // floats of a partial row: O[128], reference, sum, pad
 constexpr int kThreads = 896;
-constexpr int kDoneThreads = 256 + 2 * 32;   // softmax warpgroups, copies, products
+constexpr int kDoneThreads = 256 + 3 * 32;   // softmax warpgroups, copies, products
 // log2 of the largest of a row's 32 weights when its reference is set; their sum that sets it anew (no weight above it, and FP16 holds 65504)
 constexpr float kTop = 8.0f, kMost = 65000.0f;
 constexpr int kMinExp = -80;        // smallest exponent of a tile's keys or values
@@ -78,14 +82,18 @@ struct TreeParams {
   BlockDiv bt_div;
 };
 
+// Tensor maps of the planes, a row a 16-token sub-block (1 KiB, contiguous): K Anchor, K Residual, V Anchor, V Residual.
+struct alignas(64) Maps {
+  CUtensorMap m[4];
+};
+
 // TS: where there are no more than 128 / TS rows, a row lies in TS lanes of tensor memory, which take a tile's tokens in TS parts, with
 // references, sums and accumulators of their own; the joining kernel adds them up.  The softmax of a tile is then spread over all warps.
 template <bool FULL, int TS>
 struct Cfg {
   static constexpr int kRows = kM / TS, kW = kHalf / TS;             // rows of a row block; scores of a thread and half tile
-  static constexpr int kPlanes = FULL ? 16384 : 8192;                // of one tensor and tile: [planes][128 tokens][64 B]
-  static constexpr int kStage = kPlanes + 1024;                      // and [128] {scale, zero}
-  static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 4;
+  static constexpr int kStage = FULL ? 16384 : 8192;                 // planes of one tensor and tile: [planes][128 tokens][64 B]
+  static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 5;
   static constexpr int kOffK = 0, kOffV = kOffK + 2 * 32768, kOffRK = kOffV + 2 * 32768, kOffRV = kOffRK + kRingK * kStage,
                        kOffSum = kOffRV + kRingV * kStage;           // [128] the query sums' 8 FP16
   static constexpr int kOffMid = kOffSum + 2048;                     // [2][128] the middles' 8 FP16
@@ -96,7 +104,7 @@ struct Cfg {
   static constexpr int kOffItems = kOffMl + 2 * 1024;                // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
   static constexpr int kOffBars = kOffMisc + 256;
-  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 3 * kSlots + 8 + 16;
+  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 3 * kSlots + 16 + 16;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024, "shared memory");
   static_assert(kOffSum % 128 == 0 && kOffBars % 8 == 0, "alignment");
@@ -165,9 +173,11 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
   if (mbar_test(bar, parity)) return true;
   return bounded_wait([=] { return mbar_try_wait(bar, parity); }, [] { return globaltimer_ns(); }, abort_word);
 }
-__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+// Four rows of a map one behind the other.
+__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void named_bar(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
@@ -176,11 +186,6 @@ template <int N>
 __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
   uint2 v;
   asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
@@ -457,7 +462,7 @@ __device__ __forceinline__ bool node_used(const TreeParams& p, int b, int i, int
 
 // ------------------------------------------------------------------ the kernel
 template <bool FULL, int TS>
-__global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __grid_constant__ TreeParams p) {
+__global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __grid_constant__ TreeParams p, const __grid_constant__ Maps maps) {
   using C = Cfg<FULL, TS>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -470,22 +475,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
-  // of a half tile: sfull, pready, pvdone; of a tile: kready, kfree, vready, vfree (in turn), mready; of a piece: ifull, iempty, qready, kdone
-  const uint32_t sfull = vempty + 8 * C::kRingV, pready = sfull + 8 * kSlots, pvdone = pready + 8 * kSlots, mready = pvdone + 8 * kSlots,
-                 kready = mready + 64, kfree = kready + 16, vready = kfree + 16, vfree = vready + 16, ifull = vfree + 16, iempty = ifull + 16,
+  // of a half tile: sfull, pready, pvdone; of a tile: kready, kfree, vready, vfree (in turn), mkready, mvready; of a piece: ifull, iempty, qready, kdone
+  const uint32_t sfull = vempty + 8 * C::kRingV, pready = sfull + 8 * kSlots, pvdone = pready + 8 * kSlots, mkready = pvdone + 8 * kSlots,
+                 mvready = mkready + 64, kready = mvready + 64, kfree = kready + 16, vready = kfree + 16, vfree = vready + 16, ifull = vfree + 16, iempty = ifull + 16,
                  qready = iempty + 16, kdone = qready + 16;
   volatile int* ab = misc;        // (waits for data)
   volatile int* iab = misc + 1;   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
 
   if (tid == 0) {
-    for (int i = 0; i < C::kRingK; ++i) { mbar_init(kfull + i * 8, 1); mbar_init(kempty + i * 8, 9); }
-    for (int i = 0; i < C::kRingV; ++i) { mbar_init(vfull + i * 8, 1); mbar_init(vempty + i * 8, 9); }
+    for (int i = 0; i < C::kRingK; ++i) { mbar_init(kfull + i * 8, 1); mbar_init(kempty + i * 8, 8); }
+    for (int i = 0; i < C::kRingV; ++i) { mbar_init(vfull + i * 8, 1); mbar_init(vempty + i * 8, 8); }
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(sfull + i * 8, 1);
       mbar_init(pready + i * 8, 4);
       mbar_init(pvdone + i * 8, 1);
     }
-    for (int i = 0; i < 8; ++i) mbar_init(mready + i * 8, 2);
+    for (int i = 0; i < 8; ++i) { mbar_init(mkready + i * 8, 1); mbar_init(mvready + i * 8, 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(kready + i * 8, 8);
       mbar_init(kfree + i * 8, 1);
@@ -541,7 +546,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         // (No barrier may be more than a phase further than a wait expects: see tests/test_tree_handoffs.py.)
         const bool tree = hv.nodes(u);
         const int t = gt + (tree ? n - 1 : u >> 1);
-        wait(mready + (t & 7) * 8, (t >> 3) & 1, ab);
+        wait(mkready + (t & 7) * 8, (t >> 3) & 1, ab);
+        wait(mvready + (t & 7) * 8, (t >> 3) & 1, ab);
         if (tree) {   // the factor and the exponent of the nodes
           wait(kdone + qi * 8, (ic >> 1) & 1, ab);
           wait(vready + (t & 1) * 8, (t >> 1) & 1, ab);
@@ -733,6 +739,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     reg_dec<C::kRegExp>();
     const int kt = (tid - 256) & 127, side = (warp >> 2) & 1;   // (the second warpgroup has the tile's second half and no more)
     int gt = 0, slot = 0;
+    uint32_t phase = 0;
     float a = 0.0f;   // factor of the scores, but for the keys' exponent
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
@@ -784,13 +791,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       for (int u = 0; u < n; ++u, ++gt) {
         const int ut = u0 + u, g = gt & 1;
         const uint32_t tile = sbase + C::kOffK + (uint32_t)g * 32768u;
-        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);   // (the raw stage is there, the tile has been used: warp 27 has waited for both)
+        wait(mkready + (gt & 7) * 8, (gt >> 3) & 1, ab);   // (and the tile has been used: warp 27 has waited for that)
         if (ut < n_prefix) {
+          wait(kfull + slot * 8, phase, ab);
           if (len - ut * kTile > kHalf * side)
             expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, sbase + C::kOffKm + (uint32_t)g * 512u, kt, kHalf * side);
           __syncwarp();
           if (lane == 0) mbar_arrive(kempty + slot * 8);
-          if (++slot == C::kRingK) slot = 0;
+          if (++slot == C::kRingK) { slot = 0; phase ^= 1; }
         } else if (side == 0) {   // the nodes' keys: a thread a row, scaled by a power of two
           const uint4* src = p.kt + ((int64_t)b * p.n + kt) * p.kt_stride + h * 16;
           const bool used = node_used(p, b, kt, lane);
@@ -831,6 +839,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     reg_dec<C::kRegExp>();
     const int vt = (tid - 512) & 127, w4 = warp & 3, side = (warp >> 2) & 1;
     int gt = 0, slot = 0;
+    uint32_t phase = 0;
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
@@ -841,14 +850,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       for (int u = 0; u < n; ++u, ++gt) {
         const int ut = u0 + u, g = gt & 1;
         const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u;
-        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);         // (and the raw stage)
+        wait(mvready + (gt & 7) * 8, (gt >> 3) & 1, ab);
         wait(vfree + g * 8, ((gt >> 1) - 1) & 1, ab);           // the tile has been used
         if (ut < n_prefix) {
+          wait(vfull + slot * 8, phase, ab);
           if (len - ut * kTile > kHalf * side)
             expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, sbase + C::kOffVm + (uint32_t)g * 512u, vt, kHalf * side);
           __syncwarp();
           if (lane == 0) mbar_arrive(vempty + slot * 8);
-          if (++slot == C::kRingV) slot = 0;
+          if (++slot == C::kRingV) { slot = 0; phase ^= 1; }
         } else if (side == 0) {
           const bool used = node_used(p, b, vt, lane);
           const uint4* src = p.vt + ((int64_t)b * p.n + vt) * p.vt_stride + h * 16;
@@ -880,96 +890,93 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     return;
   }
   reg_dec<C::kRegRest>();
-  // ================================================================================== copies
-  if (warp == 24) {
-    // what a lane copies of a tile, once or twice: sub-block (lane & 7) of the Anchor, the Residual or the scalars of keys or values
-    struct Job { const uint8_t* src; uint32_t row_bytes, at; bool v, on; } job[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int what = (lane >> 3) + 4 * i;   // FULL: K Anchor, K Residual, V Anchor, V Residual, K scalars, V scalars; else without the Residuals
-      const bool v = FULL ? what == 2 || what == 3 || what == 5 : (what & 1), meta = FULL ? what >= 4 : what >= 2, res = FULL && !meta && (what & 1);
-      const float2* m = v ? p.vm : p.km;
-      job[i].src = meta ? reinterpret_cast<const uint8_t*>(m) : res ? (v ? p.vr : p.kr) : (v ? p.va : p.ka);
-      job[i].row_bytes = meta ? 8u : 64u;
-      job[i].at = (v ? C::kOffRV : C::kOffRK) + (meta ? C::kPlanes : res ? 8192 : 0) + (uint32_t)(lane & 7) * 16u * job[i].row_bytes;
-      job[i].v = v;
-      job[i].on = what < (FULL ? 6 : 4);
-    }
-    Cursor cur = first_unit(p, blockIdx.x, gridDim.x, lane);
-    int kslot = 0, vslot = 0;
-    uint32_t kphase = 1, vphase = 1;   // (empty rings)
-#pragma unroll 1
-    for (int ic = 0;; ++ic) {
-      const int qi = ic & 1;
-      const Item it = next_piece(p, cur, blockIdx.x);
-      wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
-      if (lane == 0) {
-        volatile Item* d = items + qi;
-        d->b = it.b; d->h = it.h; d->rb = it.rb; d->len = it.len;
-        d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib;
-        mbar_arrive(ifull + qi * 8);
-      }
-      __syncwarp();
-      if (it.n == 0) break;
-      const int n_prefix = (it.len + kTile - 1) / kTile, last = min(it.u0 + it.n, n_prefix), off = (lane & 7) * 16;
-      int id = 0;
-      if (it.u0 * kTile + off < it.len) id = block_id(p, it.b, it.u0 * kTile + off);
-#pragma unroll 1
-      for (int ut = it.u0; ut < last; ++ut) {
-        const int t = ut * kTile + off, now = id;
-        if (t + kTile < it.len) id = block_id(p, it.b, t + kTile);
-        const int subs = min(8, (it.len - ut * kTile + 15) / 16);   // sub-blocks of 16 tokens with a token of the sequence
-        const uint32_t bytes = (uint32_t)subs * (FULL ? 2048u + 128u : 1024u + 128u);
-        const int64_t row = (lane & 7) < subs ? row_at(p, now, it.h, t) : 0;
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const uint32_t full = v ? vfull + vslot * 8 : kfull + kslot * 8, stage = sbase + (uint32_t)((v ? vslot : kslot) * C::kStage);
-          wait(v ? vempty + vslot * 8 : kempty + kslot * 8, v ? vphase : kphase, ab);
-          if (lane == 0) mbar_expect_tx(full, bytes);
-          __syncwarp();
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            if (job[i].on && job[i].v == (v != 0) && (lane & 7) < subs)
-              bulk_g2s(stage + job[i].at, job[i].src + row * job[i].row_bytes, 16u * job[i].row_bytes, full);
-        }
-        if (++kslot == C::kRingK) { kslot = 0; kphase ^= 1; }
-        if (++vslot == C::kRingV) { vslot = 0; vphase ^= 1; }
-      }
-    }
-    bar_arrive(2, kDoneThreads);
-    return;
-  }
-  // ================================================================================== scales and zero points
-  if (warp == 25 || warp == 27) {
-    const bool values = warp == 25;
-    const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty;
-    const int ring = values ? C::kRingV : C::kRingK, stages = (values ? C::kOffRV : C::kOffRK) + C::kPlanes;
+  // ================================================================================== copies, scales and zero points
+  if (warp != 26) {
+    const bool copies = warp != 27, values = warp == 25, scales = warp != 24;
+    const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty, mready = values ? mvready : mkready;
+    const int ring = values ? C::kRingV : C::kRingK, stages = values ? C::kOffRV : C::kOffRK;
+    const float2* meta = values ? p.vm : p.km;
+    Cursor cur = {0, 0, 0, 0, 0, 0};
+    if (warp == 24) cur = first_unit(p, blockIdx.x, gridDim.x, lane);
     int gt = 0, slot = 0;
-    uint32_t phase = 0;
+    uint32_t phase = 1;   // (an empty ring)
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
-      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
-      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0;
-      if (n == 0) break;
+      Item it;
+      if (warp == 24) {
+        it = next_piece(p, cur, blockIdx.x);
+        wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
+        if (lane == 0) {
+          volatile Item* d = items + qi;
+          d->b = it.b; d->h = it.h; d->rb = it.rb; d->len = it.len;
+          d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib;
+          mbar_arrive(ifull + qi * 8);
+        }
+        __syncwarp();
+      } else {
+        wait(ifull + qi * 8, (ic >> 1) & 1, iab);
+        it.n = items[qi].n; it.len = items[qi].len; it.u0 = items[qi].u0; it.b = items[qi].b; it.h = items[qi].h;
+      }
+      if (it.n == 0) break;
+      const int n_prefix = (it.len + kTile - 1) / kTile, last = min(it.u0 + it.n, n_prefix);
+      // Copies, a tile's: lane i < 8 knows sub-block i's row, four lanes gather (Anchor or Residual, sub-blocks 0..3 or 4..7).
+      int cid = 0, ct = it.u0;   // its block, a tile ahead; the next tile to copy
+      if (copies && ct * kTile + (lane & 7) * 16 < it.len) cid = block_id(p, it.b, ct * kTile + (lane & 7) * 16);
+      auto copy = [&]() {
+        const int t = ct * kTile + (lane & 7) * 16, subs = min(8, (it.len - ct * kTile + 15) / 16);   // sub-blocks with a token of the sequence
+        uint32_t row = (lane & 7) < subs ? (uint32_t)(row_at(p, cid, it.h, t) >> 4) : 0u;
+        if (t + kTile < it.len) cid = block_id(p, it.b, t + kTile);
+        row = __shfl_sync(0xFFFFFFFFu, row, min(lane & 7, subs - 1));   // (behind the end: the last one again)
+        uint32_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __shfl_sync(0xFFFFFFFFu, row, (lane & 1) * 4 + i);
+        const int groups = subs > 4 ? 2 : 1;
+        wait(empty + slot * 8, phase, ab);
+        if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)groups * (FULL ? 8192u : 4096u));
+        __syncwarp();
+        if (lane < (FULL ? 4 : 2) && (lane & 1) < groups)
+          gather4(sbase + (uint32_t)(stages + slot * C::kStage + (lane >> 1) * 8192 + (lane & 1) * 4096), &maps.m[(values ? 2 : 0) + (lane >> 1)], r[0], r[1],
+                  r[2], r[3], full + slot * 8);
+        if (++slot == ring) { slot = 0; phase ^= 1; }
+        ++ct;
+      };
+      if (!scales) {
+#pragma unroll 1
+        while (ct < last) copy();
+        continue;
+      }
       float a = 0.0f;
       if (!values) {
         wait(qready + qi * 8, (ic >> 1) & 1, ab);
         a = __int_as_float(misc[28 + qi]);
       }
-      const int n_prefix = (len + kTile - 1) / kTile;
+      // Scales: a lane takes four tokens, {scale, zero} each, a tile ahead, their block two.
+      int id = 0;
+      uint4 x[2] = {};
+      auto id_of = [&](int ut) { const int t = ut * kTile + lane * 4; return t < it.len ? block_id(p, it.b, t) : 0; };
+      auto fetch = [&](int ut, int blk) {
+        const int t = ut * kTile + lane * 4;
+        if (t < it.len) {
+          const uint4* src = reinterpret_cast<const uint4*>(meta + row_at(p, blk, it.h, t));
+          x[0] = ld_dep(src);
+          x[1] = ld_dep(src + 1);
+        }
+      };
+      fetch(it.u0, id_of(it.u0));
+      id = id_of(it.u0 + 1);
+      if (copies) {   // (the ring full but for one place)
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt) {
-        const int ut = u0 + u, g = gt & 1;
+        while (ct < min(last, it.u0 + ring - 1)) copy();
+      }
+#pragma unroll 1
+      for (int u = 0; u < it.n; ++u, ++gt) {
+        const int ut = it.u0 + u, g = gt & 1;
         // (the nodes' are made by the warps that have their keys and values.  These wait for this warp all the same, so that no barrier is a
         // phase further than what a wait for it expects)
         const uint32_t used = values ? vready + g * 8 : kfree + g * 8, before = ((gt >> 1) - 1) & 1;
         if (ut < n_prefix) {
-          // a lane takes four tokens, {scale, zero} each
-          wait(full + slot * 8, phase, ab);
-          const uint32_t src = sbase + (uint32_t)(stages + slot * C::kStage + lane * 32);
-          const uint4 x[2] = {lds128(src), lds128(src + 16)};
-          const int room = len - ut * kTile - lane * 4;   // (what lies behind the sequence's end may be anything)
+          const int room = it.len - ut * kTile - lane * 4;   // (what lies behind the sequence's end may be anything)
           const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
           float sc[4], mid[4], top = 0.0f;
 #pragma unroll
@@ -978,9 +985,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             mid[i] = room > i ? fmaf(128.0f, sc[i], __uint_as_float(w[2 * i + 1])) : 0.0f;
             top = fmaxf(top, fabsf(mid[i]) + 128.0f * fabsf(sc[i]));
           }
+          fetch(ut + 1, id);
+          id = id_of(ut + 2);
           const int e = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top))) + (values ? 0 : 3);   // (1152 scales below 2^15.2)
-          if (lane == 0) mbar_arrive(empty + slot * 8);
-          if (++slot == ring) { slot = 0; phase ^= 1; }
           const float f = pow2(-e);
           wait(used, before, ab);    // these places have been read (the softmax's of eight tiles before, too)
           uint32_t o[4];
@@ -1007,13 +1014,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(mready + (gt & 7) * 8);
+        if (copies && ct < last) copy();
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
+    if (copies) bar_arrive(2, kDoneThreads);
     return;
   }
   // ================================================================================== products
-  if (warp == 26) {
+  {
     constexpr uint32_t kIdescS = tc_idesc(kHalf, false), kIdescO = tc_idesc(128, true);
     const uint32_t k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 16384u), sum_lo = desc_lo(sbase + C::kOffSum, C::kOffZero - C::kOffSum);
     Slot q, s;   // of the next Q K^T, of the next P V
@@ -1152,7 +1161,9 @@ lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
     return LYNX_ERR_SHAPE;
   const int G = s->num_q_heads / s->num_kv_heads;
   const int64_t cap = (int64_t)s->max_blocks_per_seq * s->block_tokens;
-  if (s->head_dim != LYNX_D || s->block_tokens % 16 || G > 16 || n > kMaxNodes || cap >= (1ll << 30)) return LYNX_ERR_UNSUPPORTED;
+  if (s->head_dim != LYNX_D || s->block_tokens % 16 || G > 16 || n > kMaxNodes || cap >= (1ll << 30) ||
+      (int64_t)s->num_blocks * s->num_kv_heads * s->block_tokens >= (1ll << 32))
+    return LYNX_ERR_UNSUPPORTED;
   pl->cols = n * G;
   pl->RB = (pl->cols + kM - 1) / kM;
   pl->segs = (int64_t)B * s->num_kv_heads * pl->RB;
@@ -1175,14 +1186,40 @@ lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
   return LYNX_OK;
 }
 
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+bool plane_map(CUtensorMap* m, const uint8_t* base, uint64_t rows) {
+  static const EncodeTiled fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) f = nullptr;
+    return reinterpret_cast<EncodeTiled>(f);
+  }();
+  const cuuint64_t dims[2] = {256, rows / 16}, strides[1] = {1024};   // (32-bit words)
+  const cuuint32_t box[2] = {256, 1}, es[2] = {1, 1};
+  return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint8_t*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <bool FULL, int TS>
 lynx_status launch_tree(const TreeParams& p, int grid, void* stream) {
   using C = Cfg<FULL, TS>;
-  if (cudaFuncSetAttribute(tree_attention_kernel<FULL, TS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
-    launch_status();
-    return LYNX_ERR_CUDA;
+  static bool configured[64] = {false};
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev < 0 || dev >= 64 || !configured[dev]) {
+    if (cudaFuncSetAttribute(tree_attention_kernel<FULL, TS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
+      launch_status();
+      return LYNX_ERR_CUDA;
+    }
+    if (dev >= 0 && dev < 64) configured[dev] = true;
   }
-  return launch_pdl(tree_attention_kernel<FULL, TS>, (unsigned)grid, kThreads, C::kSmem, stream, p);
+  Maps maps;
+  const uint64_t rows = (uint64_t)p.num_blocks * p.Hkv * p.bt;
+  if (!plane_map(&maps.m[0], p.ka, rows) || !plane_map(&maps.m[1], FULL ? p.kr : p.ka, rows) || !plane_map(&maps.m[2], p.va, rows) ||
+      !plane_map(&maps.m[3], FULL ? p.vr : p.va, rows))
+    return LYNX_ERR_CUDA;
+  return launch_pdl(tree_attention_kernel<FULL, TS>, (unsigned)grid, kThreads, C::kSmem, stream, p, maps);
 }
 
 }  // namespace

@@ -53,8 +53,8 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
     """pieces: (tiles, whether the last is the nodes', whether the prefix ends in the first half of a tile).  Warps of a role that
     only arrive together are one here."""
     B = {}
-    for name, n, count in (("kfull", ring_k, 1), ("kempty", ring_k, 3), ("vfull", ring_v, 1), ("vempty", ring_v, 3), ("kready", 2, 2), ("sfull", N, 1),
-                           ("mready", 8, 2), ("vready", 2, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", 2, 1), ("vfree", 2, 1),
+    for name, n, count in (("kfull", ring_k, 1), ("kempty", ring_k, 2), ("vfull", ring_v, 1), ("vempty", ring_v, 2), ("kready", 2, 2), ("sfull", N, 1),
+                           ("mkready", 8, 1), ("mvready", 8, 1), ("vready", 2, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", 2, 1), ("vfree", 2, 1),
                            ("ifull", 2, 1), ("iempty", 2, 2 * softmax + 7), ("qready", 2, 1), ("kdone", 2, 1)):
         B[name] = [Barrier(count) for _ in range(n)]
     rawk, rawv = [Place(f"raw K {i}") for i in range(ring_k)], [Place(f"raw V {i}") for i in range(ring_v)]
@@ -80,7 +80,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
         return n - 1 if tree else n
 
     def copies():
-        ks, vs, kp, vp, gt = 0, 0, 1, 1, 0
+        slot, phase, gt = 0, 1, 0
         for ic in range(len(pieces) + 1):
             yield from wait("iempty", ic & 1, (ic >> 1) - 1)
             item[ic & 1].write(ic)
@@ -89,19 +89,15 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             if n == 0:
                 return
             for _ in range(raw_tiles(n, tree)):
-                yield from wait("kempty", ks, kp)
-                rawk[ks].write(gt)
-                B["kfull"][ks].arrive()
-                yield from wait("vempty", vs, vp)
-                rawv[vs].write(gt)
-                B["vfull"][vs].arrive()
+                yield from wait("kempty", slot, phase)
+                rawk[slot].write(gt)
+                B["kfull"][slot].arrive()
                 gt += 1
-                ks, kp = (0, kp ^ 1) if ks + 1 == ring_k else (ks + 1, kp)
-                vs, vp = (0, vp ^ 1) if vs + 1 == ring_v else (vs + 1, vp)
+                slot, phase = (0, phase ^ 1) if slot + 1 == ring_k else (slot + 1, phase)
             gt += tree
 
     def k_tiles(side):
-        gt = slot = 0
+        gt = slot = phase = 0
         for ic in range(len(pieces) + 1):
             n, tree, short = yield from get(ic)
             if n == 0:
@@ -113,8 +109,9 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 B["qready"][ic & 1].arrive()
             for u in range(n):
                 g = gt & 1
-                yield from wait("mready", gt & 7, gt >> 3)
+                yield from wait("mkready", gt & 7, gt >> 3)
                 if u < raw_tiles(n, tree):
+                    yield from wait("kfull", slot, phase)
                     ktile[g][side].write(gt)
                     rawk[slot].read(gt)
                     km[g].read(gt)
@@ -122,7 +119,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                     yield
                     km[g].readers -= 1
                     B["kempty"][slot].arrive()
-                    slot = (slot + 1) % ring_k
+                    slot, phase = (0, phase ^ 1) if slot + 1 == ring_k else (slot + 1, phase)
                 elif side == 0:
                     ktile[g][0].write(gt)
                     factor[gt & 7].write(gt)
@@ -134,16 +131,17 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             B["iempty"][ic & 1].arrive()
 
     def v_tiles(side):
-        gt = slot = 0
+        gt = slot = phase = 0
         for ic in range(len(pieces) + 1):
             n, tree, short = yield from get(ic)
             if n == 0:
                 return
             for u in range(n):
                 g = gt & 1
-                yield from wait("mready", gt & 7, gt >> 3)
+                yield from wait("mvready", gt & 7, gt >> 3)
                 yield from wait("vfree", g, (gt >> 1) - 1)
                 if u < raw_tiles(n, tree):
+                    yield from wait("vfull", slot, phase)
                     vtile[g][side].write(gt)
                     rawv[slot].read(gt)
                     vm[g].read(gt)
@@ -151,7 +149,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                     yield
                     vm[g].readers -= 1
                     B["vempty"][slot].arrive()
-                    slot = (slot + 1) % ring_v
+                    slot, phase = (0, phase ^ 1) if slot + 1 == ring_v else (slot + 1, phase)
                 elif side == 0:
                     vtile[g][0].write(gt)
                     exp[gt & 7].write(gt)
@@ -160,27 +158,37 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             B["iempty"][ic & 1].arrive()
 
     def scales(values):
-        full, empty, ring, raw = ("vfull", "vempty", ring_v, rawv) if values else ("kfull", "kempty", ring_k, rawk)
-        gt = slot = phase = 0
+        gt = slot = 0
+        phase = 1
         for ic in range(len(pieces) + 1):
             n, tree, _ = yield from get(ic)
             if n == 0:
                 return
-            if not values:
+            copied, raw = 0, raw_tiles(n, tree)
+            start = gt
+
+            def copy():
+                nonlocal slot, phase, copied
+                yield from wait("vempty", slot, phase)
+                rawv[slot].write(start + copied)
+                B["vfull"][slot].arrive()
+                copied += 1
+                slot, phase = (0, phase ^ 1) if slot + 1 == ring_v else (slot + 1, phase)
+
+            if values:
+                while copied < min(raw, ring_v - 1):
+                    yield from copy()
+            else:
                 yield from wait("qready", ic & 1, ic >> 1)
             for u in range(n):
                 g = gt & 1
-                prefix = u < raw_tiles(n, tree)
-                if prefix:
-                    yield from wait(full, slot, phase)
-                    raw[slot].read(gt)
-                    B[empty][slot].arrive()
-                    slot, phase = (0, phase ^ 1) if slot + 1 == ring else (slot + 1, phase)
                 yield from wait("vready" if values else "kfree", g, (gt >> 1) - 1)
-                if prefix:
+                if u < raw:
                     for x in (vm[g], exp[gt & 7]) if values else (km[g], mids[g], factor[gt & 7]):
                         x.write(gt)
-                B["mready"][gt & 7].arrive()
+                B["mvready" if values else "mkready"][gt & 7].arrive()
+                if values and copied < raw:
+                    yield from copy()
                 gt += 1
             B["iempty"][ic & 1].arrive()
 
@@ -263,7 +271,8 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                     gs += 1
                     continue
                 g, t = gs % N, t + gt
-                yield from wait("mready", t & 7, t >> 3)
+                yield from wait("mkready", t & 7, t >> 3)
+                yield from wait("mvready", t & 7, t >> 3)
                 if tree and u == len(halves) - 1:
                     yield from wait("kdone", ic & 1, ic >> 1)
                     yield from wait("vready", t & 1, t >> 1)
@@ -332,10 +341,10 @@ def test_the_kernel_waits_for_what_is_played():
     """The waits of the roles in the source, by barrier."""
     code = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "tree_attention.cu")).read())
     code = code[code.index("tree_attention_kernel("):code.index("tree_combine_kernel(")]
-    cuts = ["if (warp < 8) {", "if (warp < 16) {", "if (warp < 24) {", "if (warp == 24) {", "if (warp == 25 || warp == 27) {", "if (warp == 26) {"]
+    cuts = ["if (warp < 8) {", "if (warp < 16) {", "if (warp < 24) {", "if (warp != 26) {", "constexpr uint32_t kIdescS"]
     at = [code.index(x) for x in cuts] + [len(code)]
     waits = [sorted(set(re.findall(r"\bwait\((\w+)", code[a:b]))) for a, b in zip(at, at[1:])]
-    assert waits == [["ifull", "kdone", "mready", "pvdone", "sfull", "vready"], ["ifull", "kfree", "mready"], ["ifull", "mready", "vfree"],
-                     ["iempty", "v"], ["full", "ifull", "qready", "used"], ["ifull", "kready", "pready", "vready"]]
+    assert waits == [["ifull", "kdone", "mkready", "mvready", "pvdone", "sfull", "vready"], ["ifull", "kfree", "kfull", "mkready"],
+                     ["ifull", "mvready", "vfree", "vfull"], ["empty", "iempty", "ifull", "qready", "used"], ["ifull", "kready", "pready", "vready"]]
     land, done, free = (code.index(x) for x in ("land_after_abort(", "named_bar(2, kDoneThreads)", "tcgen05.dealloc"))
     assert done < land < free and len(re.findall(r"bar_arrive\(2, kDoneThreads\)", code)) == 2
