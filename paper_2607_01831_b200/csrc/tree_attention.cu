@@ -10,8 +10,8 @@
 // down to 2^-24 of the row block's largest.  So a score needs one multiply-add in the softmax, with a factor that its whole tile shares
 // (per-token scales there are loads of shared memory for every score: 140 us instead of 112 for 128 rows over 131072 tokens).  Values
 // enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15 (rows 2^29 times smaller keep all 11 bits; keys 2^26), weights as
-// FP16 relative to a reference that keeps each row's largest between 2^8 and 2^16 (set when the sum of 32 weights, which is
-// there anyway, tells it: no maxima): both roundings are 2^-12 of a term, an eighth of the
+// FP16 relative to a reference that keeps each row's largest between 2^7 and 2^16 (set anew when the sum of 64 weights,
+// which is there anyway, comes near it: no maxima): both roundings are 2^-12 of a term, an eighth of the
 // output's own rounding to BF16.  2^e goes into the weight's exponent and out of l's terms again, so that it costs nothing per weight.  Sums
 // l, references and O are FP32.
 //
@@ -25,9 +25,8 @@
 //   warps 0-3, 4-7   softmax, even and odd half tiles
 //   warps 8-15       K codes to FP16 into the K tiles, and a piece's queries
 //   warps 16-23      V codes to FP16 values into the V tiles
-//   warp 24          copies of K planes into a ring, four 16-token sub-blocks at a time; deals out the pieces
-//   warp 25          the same of V planes; the values' scales and zero points: what the V tiles and the softmax need of them
-//   warp 27          the same of the keys
+//   warps 24, 25     copies of K and V planes into rings, four 16-token sub-blocks at a time; warp 24 deals out the pieces
+//   warp 27          scales and zero points of a tile: what the K and V tiles and the softmax need of them
 //   warp 26          issues every tcgen05.mma: Q K^T three half tiles ahead of P V
 // The copy engine takes some 35 cycles per row of a copy and a lane that issues copies of one sub-block each some 80: 48 of them a tile, planes
 // and scales, took 4000 cycles (140 us for 128 rows over 131072 tokens).  Hence gathers of four sub-blocks by two warps, and plain loads,
@@ -58,8 +57,8 @@ constexpr int kMaxNodes = 64;
 constexpr int kPartRow = 132;       // floats of a partial row: O[128], reference, sum, pad
 constexpr int kThreads = 896;
 constexpr int kDoneThreads = 256 + 3 * 32;   // softmax warpgroups, copies, products
-// log2 of the largest of a row's 32 weights when its reference is set; their sum that sets it anew (no weight above it, and FP16 holds 65504)
-constexpr float kTop = 8.0f, kMost = 65000.0f;
+// log2 of the largest of a row's weights when its reference is set; a sum of them that sets it anew (none is above it, and FP16 holds 65504)
+constexpr float kTop = 7.0f, kMost = 65000.0f;
 constexpr int kMinExp = -80;        // smallest exponent of a tile's keys or values
 
 struct TreeParams {
@@ -104,7 +103,7 @@ struct Cfg {
   static constexpr int kOffItems = kOffMl + 2 * 1024;                // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
   static constexpr int kOffBars = kOffMisc + 256;
-  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 3 * kSlots + 16 + 16;
+  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 3 * kSlots + 8 + 16;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024, "shared memory");
   static_assert(kOffSum % 128 == 0 && kOffBars % 8 == 0, "alignment");
@@ -134,8 +133,6 @@ struct Halves {
     n = prefix + (u0 + tiles > (len + kTile - 1) / kTile ? 1 : 0);
   }
   __device__ __forceinline__ bool nodes(int s) const { return s >= prefix; }
-  __device__ __forceinline__ int side(int s) const { return nodes(s) ? 0 : s & 1; }
-  __device__ __forceinline__ bool last_of_tile(int s) const { return side(s) == 1 || s >= prefix - 1; }
 };
 
 // ------------------------------------------------------------------ PTX
@@ -265,6 +262,12 @@ __device__ __forceinline__ void codes8(uint32_t xa, uint32_t xr, uint32_t* o) {
   o[2] = (od & 0x00FF00FFu) | 0x64006400u;
   o[3] = __byte_perm(od, 0x64646464u, 0x4341);
 }
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ float2 half2_to_float2(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 __device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d;
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
@@ -439,12 +442,12 @@ __device__ __forceinline__ Item next_piece(const TreeParams& p, Cursor& c, int c
 __device__ __forceinline__ int block_id(const TreeParams& p, int b, int tok) {
   return ld_dep(p.table + (int64_t)b * p.max_blocks + quotient(tok, p.bt_div));
 }
-__device__ __forceinline__ int64_t row_at(const TreeParams& p, int id, int h, int tok) {
+__device__ __forceinline__ uint32_t row_at(const TreeParams& p, int id, int h, int tok) {   // (fewer than 2^32 rows)
   if ((unsigned)id >= (unsigned)p.num_blocks) {
     atomicOr(p.flags, kFlagBadBlock);
     id = id < 0 ? 0 : p.num_blocks - 1;
   }
-  return ((int64_t)id * p.Hkv + h) * p.bt + (tok - quotient(tok, p.bt_div) * p.bt);
+  return ((uint32_t)id * p.Hkv + h) * p.bt + (uint32_t)(tok - quotient(tok, p.bt_div) * p.bt);
 }
 
 // Whether node i (of 128) is seen by some row, by a warp: the others' keys and values may be anything.
@@ -470,14 +473,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
   volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [8 + i] V maxima, [12 + i] K maxima, [16 + 4 piece + i]
-                                             // q maxima, [28 + piece] the queries' part of the scores' factor, [32 + tile % 8] that factor, [40 + tile % 8]
+                                             // q maxima, [28 + piece] the queries' part of the scores' factor, [32 + 2 (tile % 8)] that factor, [33 + 2 (tile % 8)]
                                              // exponent of the values
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
-  // of a half tile: sfull, pready, pvdone; of a tile: kready, kfree, vready, vfree (in turn), mkready, mvready; of a piece: ifull, iempty, qready, kdone
-  const uint32_t sfull = vempty + 8 * C::kRingV, pready = sfull + 8 * kSlots, pvdone = pready + 8 * kSlots, mkready = pvdone + 8 * kSlots,
-                 mvready = mkready + 64, kready = mvready + 64, kfree = kready + 16, vready = kfree + 16, vfree = vready + 16, ifull = vfree + 16, iempty = ifull + 16,
+  // of a half tile: sfull, pready, pvdone; of a tile: kready, kfree, vready, vfree (in turn), mready; of a piece: ifull, iempty, qready, kdone
+  const uint32_t sfull = vempty + 8 * C::kRingV, pready = sfull + 8 * kSlots, pvdone = pready + 8 * kSlots, mready = pvdone + 8 * kSlots,
+                 kready = mready + 64, kfree = kready + 16, vready = kfree + 16, vfree = vready + 16, ifull = vfree + 16, iempty = ifull + 16,
                  qready = iempty + 16, kdone = qready + 16;
   volatile int* ab = misc;        // (waits for data)
   volatile int* iab = misc + 1;   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
@@ -490,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       mbar_init(pready + i * 8, 4);
       mbar_init(pvdone + i * 8, 1);
     }
-    for (int i = 0; i < 8; ++i) { mbar_init(mkready + i * 8, 1); mbar_init(mvready + i * 8, 1); }
+    for (int i = 0; i < 8; ++i) mbar_init(mready + i * 8, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(kready + i * 8, 8);
       mbar_init(kfree + i * 8, 1);
@@ -546,8 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         // (No barrier may be more than a phase further than a wait expects: see tests/test_tree_handoffs.py.)
         const bool tree = hv.nodes(u);
         const int t = gt + (tree ? n - 1 : u >> 1);
-        wait(mkready + (t & 7) * 8, (t >> 3) & 1, ab);
-        wait(mvready + (t & 7) * 8, (t >> 3) & 1, ab);
+        wait(mready + (t & 7) * 8, (t >> 3) & 1, ab);
         if (tree) {   // the factor and the exponent of the nodes
           wait(kdone + qi * 8, (ic >> 1) & 1, ab);
           wait(vready + (t & 1) * 8, (t >> 1) & 1, ab);
@@ -556,100 +558,105 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         tc_fence_after();
         if (works) {
           const int valid = (tree ? p.n : min(kHalf, len - u0 * kTile - u * kHalf)) - t0;
-          const int e = misc[40 + (t & 7)];
-          const float a = __int_as_float(misc[32 + (t & 7)]);
+          const float a = __int_as_float(misc[32 + 2 * (t & 7)]);
+          const int e = misc[33 + 2 * (t & 7)];
           const uint32_t tm_s = tmem0 + C::kTmS + s.i * 64 + lanes;
           const uint64_t a2 = f2_pack(a, a);
           const bool masked = tree || valid < C::kW;
-          float sum = 0.0f;
-#pragma unroll 1
-          for (int ch = 0; ch < C::kW; ch += kCW) {
-            uint32_t w[kCW / 2];
-            float x[kCW];
-            // weights of the chunk, scores less `shift` (in units of a weight's exponent), and their sum
-            auto scores = [&](float shift) {
-              uint32_t* sx = reinterpret_cast<uint32_t*>(x);
+          uint32_t w[C::kW / 2];
+          // scores of a chunk, less `shift`, in units of a weight's exponent
+          auto scores = [&](float* x, int ch, float shift) {
+            const uint64_t b2 = f2_pack(shift, shift);
 #pragma unroll
-              for (int k = 0; k < kCW / 16; ++k) TmemRegs<16>::ld(tm_s + t0 + ch + k * 16, sx + 16 * k);
+            for (int k = 0; k < kCW / 2; ++k) f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), a2, b2), x[2 * k], x[2 * k + 1]);
+            if (masked) {
+              const int room = valid - ch;
+              uint32_t see = room <= 0 ? 0u : room < 32 ? (1u << room) - 1u : ~0u;
+              if (tree && see) see &= c < p.cols ? (uint32_t)(ld_dep(p.mask + (int64_t)b * p.n + j) >> (t0 + ch)) : 0u;
+#pragma unroll
+              for (int k = 0; k < kCW; ++k)
+                if (!((see >> k) & 1u)) x[k] = -INFINITY;
+            }
+          };
+          auto load = [&](float* x, int ch) {
+#pragma unroll
+            for (int k = 0; k < kCW / 16; ++k) TmemRegs<16>::ld(tm_s + t0 + ch + k * 16, reinterpret_cast<uint32_t*>(x) + 16 * k);
+          };
+          auto weights = [&](const float* x, int ch) {   // and their sum
+            uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+            for (int k = 0; k < kCW / 2; ++k) {
+              const float x0 = ex2(x[2 * k]), x1 = ex2(x[2 * k + 1]);
+              sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(x0, x1));
+              w[ch / 2 + k] = pack_f16x2(x0, x1);
+            }
+            float s0, s1;
+            f2_unpack(f2_add(sum2[0], sum2[1]), s0, s1);
+            return s0 + s1;
+          };
+          float sum;
+          {
+            float x[kCW], y[kCW];   // (the second chunk is on its way during the first one's exponentials)
+            load(x, 0);
+            tc_wait_ld();
+            if (C::kW > kCW) load(y, kCW);
+            scores(x, 0, (float)e - ref);
+            sum = weights(x, 0);
+            if (C::kW > kCW) {
               tc_wait_ld();
-              const uint64_t b2 = f2_pack(shift, shift);
+              scores(y, kCW, (float)e - ref);
+              sum += weights(y, kCW);
+            }
+          }
+          if (__any_sync(0xFFFFFFFFu, fresh || !(sum <= kMost))) {
+            // no reference yet, or weights that FP16 might not hold: a reference from the largest score, what the piece has so far is scaled
+            // (scores and weights once more: this is rare)
+            float x[kCW], mx = -INFINITY;
 #pragma unroll
-              for (int k = 0; k < kCW / 2; ++k) f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), a2, b2), x[2 * k], x[2 * k + 1]);
-              if (masked) {
-                const int room = valid - ch;
-                uint32_t see = room <= 0 ? 0u : room < 32 ? (1u << room) - 1u : ~0u;
-                if (tree && see) see &= c < p.cols ? (uint32_t)(ld_dep(p.mask + (int64_t)b * p.n + j) >> (t0 + ch)) : 0u;
-#pragma unroll
-                for (int k = 0; k < kCW; ++k)
-                  if (!((see >> k) & 1u)) x[k] = -INFINITY;
-              }
-            };
-            auto weights = [&]() {
-              uint64_t sum2[2] = {0ull, 0ull};
-#pragma unroll
-              for (int k = 0; k < kCW / 2; ++k) {
-                const float x0 = ex2(x[2 * k]), x1 = ex2(x[2 * k + 1]);
-                sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(x0, x1));
-                w[k] = pack_f16x2(x0, x1);
-              }
-              float s0, s1;
-              f2_unpack(f2_add(sum2[0], sum2[1]), s0, s1);
-              return s0 + s1;
-            };
-            scores((float)e - ref);
-            float part = weights();
-            if (__any_sync(0xFFFFFFFFu, fresh || !(part <= kMost))) {
-              // no reference yet, or weights that FP16 might not hold: a reference from the chunk's largest score, what the piece has so far
-              // is scaled (scores and weights once more: this is rare)
-              scores((float)e - ref);
-              float mx = -INFINITY;
+            for (int ch = 0; ch < C::kW; ch += kCW) {
+              load(x, ch);
+              tc_wait_ld();
+              scores(x, ch, (float)e - ref);
 #pragma unroll
               for (int k = 0; k < kCW; ++k) mx = fmaxf(mx, x[k]);
-              const bool need = fresh ? mx > -INFINITY : !(part <= kMost);
-              const float delta = need ? mx - kTop : 0.0f, f = fresh ? 1.0f : ex2(-delta);
-              if (need) { ref += delta; fresh = false; }
-              l *= f;
-              sum *= f;
+            }
+            const bool need = fresh ? mx > -INFINITY : !(sum <= kMost);
+            const float delta = need ? mx - kTop : 0.0f, f = fresh ? 1.0f : ex2(-delta);
+            if (need) { ref += delta; fresh = false; }
+            l *= f;
+            if (any) {
+              wait(pvdone + s2.i * 8, s2.ph, ab);
+              tc_fence_after();
 #pragma unroll 1
-              for (int i = 0; i < ch / 2; i += 8) {   // (a row's only part of the tile, then)
+              for (int i = 0; i < 128; i += 8) {
                 uint32_t o[8];
-                TmemRegs<8>::ld(tm_s + i, o);
+                TmemRegs<8>::ld(tm_o + i, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                  const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&o[k]));
-                  o[k] = pack_f16x2(v.x * f, v.y * f);
-                }
-                TmemRegs<8>::st(tm_s + i, o);
+                for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                TmemRegs<8>::st(tm_o + i, o);
               }
-              if (any) {
-                wait(pvdone + s2.i * 8, s2.ph, ab);
-                tc_fence_after();
-#pragma unroll 1
-                for (int i = 0; i < 128; i += 8) {
-                  uint32_t o[8];
-                  TmemRegs<8>::ld(tm_o + i, o);
-                  tc_wait_ld();
-#pragma unroll
-                  for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                  TmemRegs<8>::st(tm_o + i, o);
-                }
-              }
-#pragma unroll
-              for (int k = 0; k < kCW; ++k) x[k] -= delta;
-              part = weights();
             }
-            sum += part;
-            if constexpr (TS == 1) {
-              TmemRegs<16>::st(tm_s + ch / 2, w);
-            } else {   // (the lanes' other parts of the tile have no weight)
+            sum = 0.0f;
 #pragma unroll
-              for (int i = 0; i < TS; ++i) {
-                uint32_t z[kCW / 2];
+            for (int ch = 0; ch < C::kW; ch += kCW) {
+              load(x, ch);
+              tc_wait_ld();
+              scores(x, ch, (float)e - ref);
+              sum += weights(x, ch);
+            }
+          }
+          // (over the scores; the lanes' other parts of the tile have no weight)
+          if constexpr (TS == 1) {
+            TmemRegs<16>::st(tm_s, w);
+            TmemRegs<16>::st(tm_s + 16, w + 16);
+          } else {
 #pragma unroll
-                for (int k = 0; k < kCW / 2; ++k) z[k] = i == r / C::kRows ? w[k] : 0u;
-                TmemRegs<kCW / 2>::st(tm_s + i * (kCW / 2), z);
-              }
+            for (int i = 0; i < TS; ++i) {
+              uint32_t z[C::kW / 2];
+#pragma unroll
+              for (int k = 0; k < C::kW / 2; ++k) z[k] = i == r / C::kRows ? w[k] : 0u;
+              TmemRegs<C::kW / 2>::st(tm_s + i * (C::kW / 2), z);
             }
           }
           l = fmaf(sum, pow2(-e), l);
@@ -791,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       for (int u = 0; u < n; ++u, ++gt) {
         const int ut = u0 + u, g = gt & 1;
         const uint32_t tile = sbase + C::kOffK + (uint32_t)g * 32768u;
-        wait(mkready + (gt & 7) * 8, (gt >> 3) & 1, ab);   // (and the tile has been used: warp 27 has waited for that)
+        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);   // (and the tile has been used: warp 27 has waited for that)
         if (ut < n_prefix) {
           wait(kfull + slot * 8, phase, ab);
           if (len - ut * kTile > kHalf * side)
@@ -812,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           named_bar(8, 128);
           const int e = tile_exponent(max(max(misc[12], misc[13]), max(misc[14], misc[15])));
           named_bar(8, 128);   // (read by all)
-          if (kt == 0) misc[32 + (gt & 7)] = __float_as_int(times_pow2(a, e));
+          if (kt == 0) misc[32 + 2 * (gt & 7)] = __float_as_int(times_pow2(a, e));
           if (kt < kMaxNodes) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
@@ -850,7 +857,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       for (int u = 0; u < n; ++u, ++gt) {
         const int ut = u0 + u, g = gt & 1;
         const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u;
-        wait(mvready + (gt & 7) * 8, (gt >> 3) & 1, ab);
+        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);
         wait(vfree + g * 8, ((gt >> 1) - 1) & 1, ab);           // the tile has been used
         if (ut < n_prefix) {
           wait(vfull + slot * 8, phase, ab);
@@ -872,7 +879,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           named_bar(3, 128);
           const int e = tile_exponent(max(max(misc[8], misc[9]), max(misc[10], misc[11])));
           named_bar(3, 128);   // (read by all)
-          if (vt == 0) misc[40 + (gt & 7)] = e;
+          if (vt == 0) misc[33 + 2 * (gt & 7)] = e;
           if (vt < ((p.n + 15) & ~15)) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
@@ -890,21 +897,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     return;
   }
   reg_dec<C::kRegRest>();
-  // ================================================================================== copies, scales and zero points
-  if (warp != 26) {
-    const bool copies = warp != 27, values = warp == 25, scales = warp != 24;
-    const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty, mready = values ? mvready : mkready;
+  // ================================================================================== copies
+  if (warp < 26) {
+    const bool values = warp == 25;
+    const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty;
     const int ring = values ? C::kRingV : C::kRingK, stages = values ? C::kOffRV : C::kOffRK;
-    const float2* meta = values ? p.vm : p.km;
     Cursor cur = {0, 0, 0, 0, 0, 0};
-    if (warp == 24) cur = first_unit(p, blockIdx.x, gridDim.x, lane);
-    int gt = 0, slot = 0;
+    if (!values) cur = first_unit(p, blockIdx.x, gridDim.x, lane);
+    int slot = 0;
     uint32_t phase = 1;   // (an empty ring)
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       Item it;
-      if (warp == 24) {
+      if (!values) {
         it = next_piece(p, cur, blockIdx.x);
         wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
         if (lane == 0) {
@@ -919,19 +925,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         it.n = items[qi].n; it.len = items[qi].len; it.u0 = items[qi].u0; it.b = items[qi].b; it.h = items[qi].h;
       }
       if (it.n == 0) break;
-      const int n_prefix = (it.len + kTile - 1) / kTile, last = min(it.u0 + it.n, n_prefix);
-      // Copies, a tile's: lane i < 8 knows sub-block i's row, four lanes gather (Anchor or Residual, sub-blocks 0..3 or 4..7).
-      int cid = 0, ct = it.u0;   // its block, a tile ahead; the next tile to copy
-      if (copies && ct * kTile + (lane & 7) * 16 < it.len) cid = block_id(p, it.b, ct * kTile + (lane & 7) * 16);
-      auto copy = [&]() {
-        const int t = ct * kTile + (lane & 7) * 16, subs = min(8, (it.len - ct * kTile + 15) / 16);   // sub-blocks with a token of the sequence
-        uint32_t row = (lane & 7) < subs ? (uint32_t)(row_at(p, cid, it.h, t) >> 4) : 0u;
-        if (t + kTile < it.len) cid = block_id(p, it.b, t + kTile);
-        row = __shfl_sync(0xFFFFFFFFu, row, min(lane & 7, subs - 1));   // (behind the end: the last one again)
+      // lane i < 8 knows sub-block i's row (those behind the sequence's end: its last one's), four lanes gather: Anchor or Residual, sub-blocks
+      // 0..3 or 4..7
+      const int last = min(it.u0 + it.n, (it.len + kTile - 1) / kTile);
+      int t = it.u0 * kTile + (lane & 7) * 16, id = it.u0 < last ? block_id(p, it.b, min(t, it.len - 1)) : 0;
+#pragma unroll 1
+      for (int ut = it.u0; ut < last; ++ut, t += kTile) {
+        const uint32_t row = row_at(p, id, it.h, min(t, (it.len - 1) & ~15)) >> 4;
+        id = block_id(p, it.b, min(t + kTile, it.len - 1));   // (a tile ahead)
         uint32_t r[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) r[i] = __shfl_sync(0xFFFFFFFFu, row, (lane & 1) * 4 + i);
-        const int groups = subs > 4 ? 2 : 1;
+        const int groups = it.len - ut * kTile > kHalf ? 2 : 1;
         wait(empty + slot * 8, phase, ab);
         if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)groups * (FULL ? 8192u : 4096u));
         __syncwarp();
@@ -939,86 +944,105 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           gather4(sbase + (uint32_t)(stages + slot * C::kStage + (lane >> 1) * 8192 + (lane & 1) * 4096), &maps.m[(values ? 2 : 0) + (lane >> 1)], r[0], r[1],
                   r[2], r[3], full + slot * 8);
         if (++slot == ring) { slot = 0; phase ^= 1; }
-        ++ct;
-      };
-      if (!scales) {
+      }
+      if (values && lane == 0) mbar_arrive(iempty + qi * 8);
+    }
+    bar_arrive(2, kDoneThreads);
+    return;
+  }
+  // ================================================================================== scales and zero points
+  if (warp == 27) {
+    int gt = 0;
 #pragma unroll 1
-        while (ct < last) copy();
-        continue;
-      }
-      float a = 0.0f;
-      if (!values) {
-        wait(qready + qi * 8, (ic >> 1) & 1, ab);
-        a = __int_as_float(misc[28 + qi]);
-      }
-      // Scales: a lane takes four tokens, {scale, zero} each, a tile ahead, their block two.
+    for (int ic = 0;; ++ic) {
+      const int qi = ic & 1;
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
+      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h;
+      if (n == 0) break;
+      wait(qready + qi * 8, (ic >> 1) & 1, ab);
+      const float a = __int_as_float(misc[28 + qi]);
+      // a lane takes four tokens, {scale, zero} each, a tile ahead, and their block, two.  (Behind the sequence's end its last four again: a load
+      // under a condition is waited for where the condition ends.)
+      const int n_prefix = (len + kTile - 1) / kTile, top = (len - 1) & ~3;
+      const bool any = u0 < n_prefix;
+      uint4 x[2][2] = {};   // of keys, of values
       int id = 0;
-      uint4 x[2] = {};
-      auto id_of = [&](int ut) { const int t = ut * kTile + lane * 4; return t < it.len ? block_id(p, it.b, t) : 0; };
-      auto fetch = [&](int ut, int blk) {
-        const int t = ut * kTile + lane * 4;
-        if (t < it.len) {
-          const uint4* src = reinterpret_cast<const uint4*>(meta + row_at(p, blk, it.h, t));
-          x[0] = ld_dep(src);
-          x[1] = ld_dep(src + 1);
-        }
+      auto fetch = [&](int t, int blk) {
+        const size_t row = row_at(p, blk, h, t);
+        const uint4 *k = reinterpret_cast<const uint4*>(p.km + row), *v = reinterpret_cast<const uint4*>(p.vm + row);
+        x[0][0] = ld_dep(k);
+        x[0][1] = ld_dep(k + 1);
+        x[1][0] = ld_dep(v);
+        x[1][1] = ld_dep(v + 1);
       };
-      fetch(it.u0, id_of(it.u0));
-      id = id_of(it.u0 + 1);
-      if (copies) {   // (the ring full but for one place)
-#pragma unroll 1
-        while (ct < min(last, it.u0 + ring - 1)) copy();
+      if (any) {
+        const int t = u0 * kTile + lane * 4;
+        const int first = block_id(p, b, min(t, top));
+        id = block_id(p, b, min(t + kTile, top));
+        fetch(min(t, top), first);
       }
 #pragma unroll 1
-      for (int u = 0; u < it.n; ++u, ++gt) {
-        const int ut = it.u0 + u, g = gt & 1;
-        // (the nodes' are made by the warps that have their keys and values.  These wait for this warp all the same, so that no barrier is a
-        // phase further than what a wait for it expects)
-        const uint32_t used = values ? vready + g * 8 : kfree + g * 8, before = ((gt >> 1) - 1) & 1;
+      for (int u = 0; u < n; ++u, ++gt) {
+        const int ut = u0 + u, g = gt & 1;
+        const uint32_t before = ((gt >> 1) - 1) & 1;
         if (ut < n_prefix) {
-          const int room = it.len - ut * kTile - lane * 4;   // (what lies behind the sequence's end may be anything)
-          const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
-          float sc[4], mid[4], top = 0.0f;
+          const int t = ut * kTile + lane * 4, room = len - t;   // (what lies behind the sequence's end may be anything)
+          float sc[2][4], mid[2][4], big[2] = {0.0f, 0.0f};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            sc[i] = room > i ? __uint_as_float(w[2 * i]) : 0.0f;
-            mid[i] = room > i ? fmaf(128.0f, sc[i], __uint_as_float(w[2 * i + 1])) : 0.0f;
-            top = fmaxf(top, fabsf(mid[i]) + 128.0f * fabsf(sc[i]));
-          }
-          fetch(ut + 1, id);
-          id = id_of(ut + 2);
-          const int e = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top))) + (values ? 0 : 3);   // (1152 scales below 2^15.2)
-          const float f = pow2(-e);
-          wait(used, before, ab);    // these places have been read (the softmax's of eight tiles before, too)
-          uint32_t o[4];
+          for (int v = 0; v < 2; ++v) {
+            const uint32_t w[8] = {x[v][0].x, x[v][0].y, x[v][0].z, x[v][0].w, x[v][1].x, x[v][1].y, x[v][1].z, x[v][1].w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (values) {
-              o[i] = pack_f16x2(sc[i] * f, mid[i] * f);
-            } else {
-              // what rounding -1152 scale adds to all of a row's keys is taken off their middle
-              const float s16 = __half2float(__float2half_rn(sc[i] * f)), m16 = __half2float(__float2half_rn(-1152.0f * s16));
-              o[i] = pack_f16x2(s16, m16);
-              const uint32_t both = two_parts(mid[i] * f - (m16 + 1152.0f * s16));
-              sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + lane * 64 + i * 16), both, both & 0xFFFFu, 0u, 0u);
+            for (int i = 0; i < 4; ++i) {
+              sc[v][i] = room > i ? __uint_as_float(w[2 * i]) : 0.0f;
+              mid[v][i] = room > i ? fmaf(128.0f, sc[v][i], __uint_as_float(w[2 * i + 1])) : 0.0f;
+              big[v] = fmaxf(big[v], fabsf(mid[v][i]) + 128.0f * fabsf(sc[v][i]));
             }
           }
-          sts128(sbase + (values ? C::kOffVm : C::kOffKm) + (uint32_t)(g * 512 + lane * 16), o[0], o[1], o[2], o[3]);
-          if (lane == 0) {
-            if (values) misc[40 + (gt & 7)] = e;
-            else misc[32 + (gt & 7)] = __float_as_int(times_pow2(a, e));
+          fetch(min(t + kTile, top), id);
+          id = block_id(p, b, min(t + 2 * kTile, top));
+          const int ek = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big[0]))) + 3;   // (1152 scales below 2^15.2)
+          const int ev = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big[1])));
+          const float fk = pow2(-ek), fv = pow2(-ev);
+          // keys: what rounding -1152 scale adds to all of a row is taken off its middle, which goes in two parts
+          uint32_t km[4], mids[4][2], vm[4];
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const uint32_t s2 = pack_f16x2(sc[0][i] * fk, sc[0][i + 1] * fk), m2 = mul_f16x2(s2, 0xE480E480u);
+            km[i] = __byte_perm(s2, m2, 0x5410);
+            km[i + 1] = __byte_perm(s2, m2, 0x7632);
+            const float2 s16 = half2_to_float2(s2), m16 = half2_to_float2(m2);
+            const float x0 = mid[0][i] * fk - fmaf(1152.0f, s16.x, m16.x), x1 = mid[0][i + 1] * fk - fmaf(1152.0f, s16.y, m16.y);
+            const uint32_t hi = pack_f16x2(x0, x1);
+            const float2 h2 = half2_to_float2(hi);
+            const uint32_t lo = pack_f16x2(x0 - h2.x, x1 - h2.y);
+            mids[i][0] = __byte_perm(hi, lo, 0x5410);
+            mids[i][1] = hi & 0xFFFFu;
+            mids[i + 1][0] = __byte_perm(hi, lo, 0x7632);
+            mids[i + 1][1] = hi >> 16;
           }
-          if (!values) proxy_fence();
-        } else {
-          wait(used, before, ab);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vm[i] = pack_f16x2(sc[1][i] * fv, mid[1][i] * fv);
+          wait(kfree + g * 8, before, ab);    // these places have been read (the softmax's of eight tiles before, too)
+          wait(vready + g * 8, before, ab);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + lane * 64 + i * 16), mids[i][0], mids[i][1], 0u, 0u);
+          sts128(sbase + C::kOffKm + (uint32_t)(g * 512 + lane * 16), km[0], km[1], km[2], km[3]);
+          sts128(sbase + C::kOffVm + (uint32_t)(g * 512 + lane * 16), vm[0], vm[1], vm[2], vm[3]);
+          if (lane == 0) {
+            misc[32 + 2 * (gt & 7)] = __float_as_int(times_pow2(a, ek));
+            misc[33 + 2 * (gt & 7)] = ev;
+          }
+          proxy_fence();
+        } else {   // the nodes' are made by the warps that have their keys and values.  These wait for this warp all the same, so that no barrier
+                   // is a phase further than what a wait for it expects
+          wait(kfree + g * 8, before, ab);
+          wait(vready + g * 8, before, ab);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(mready + (gt & 7) * 8);
-        if (copies && ct < last) copy();
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
-    if (copies) bar_arrive(2, kDoneThreads);
     return;
   }
   // ================================================================================== products
@@ -1035,36 +1059,42 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = __shfl_sync(0xFFFFFFFFu, items[qi].n, 0), len = __shfl_sync(0xFFFFFFFFu, items[qi].len, 0), u0 = __shfl_sync(0xFFFFFFFFu, items[qi].u0, 0);
       if (n == 0) break;
       const Halves hv(u0, n, len);
-      auto qk = [&](int u) {
-        const int t = gt + (hv.nodes(u) ? n - 1 : u >> 1), side = hv.side(u), at = (t & 1) * 2 + side;
-        if (side == 0) wait(kready + (t & 1) * 8, (t >> 1) & 1, ab);   // (and with it the queries; the weights that lay in the scores' place are in front in the pipe)
+      const int node_steps = (p.n + 15) / 16, end_steps = (min(len - u0 * kTile - (hv.prefix - 1) * kHalf, kHalf) + 15) / 16;   // of 16 tokens
+      // (Not ahead into the next piece: its queries wait for this one's last scores, and a piece is dealt out when the one before the last
+      // has been left.)
+      int ahead = 0;   // half tiles whose scores have been issued
+      auto qk = [&]() {
+        const bool nodes = ahead >= hv.prefix;
+        const uint32_t t = (uint32_t)(nodes ? gt + n - 1 : gt + (ahead >> 1)), side = nodes ? 0u : ahead & 1u, tb = (t & 1u) * 8u;
+        if (side == 0) wait(kready + tb, (t >> 1) & 1, ab);   // (and with it the queries; the weights that lay in the scores' place are in front in the pipe)
         tc_fence_after();
+        const bool last = side == 1 || ahead >= hv.prefix - 1;
         if (tc_elect()) {
-          const uint32_t d = tmem0 + C::kTmS + q.i * 64, kl = k_lo + (uint32_t)((t & 1) * 2048 + side * 512);
+          const uint32_t d = tmem0 + C::kTmS + q.i * 64, kl = k_lo + (tb * 256u + side * 512u), at = tb * 256u + side * 1024u;
 #pragma unroll
           for (int ks = 0; ks < 8; ++ks)
             tc_mma_ts(d, tmem0 + C::kTmQ + ks * 8, desc(kl + (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4)), kIdescS, ks > 0 ? 1u : 0u);
-          tc_mma_ss(d, desc_plain(sum_lo), desc_plain(desc_lo(sbase + C::kOffMid + at * 1024, (uint32_t)(4 - at) * 1024u)), kIdescS, 1u);
+          tc_mma_ss(d, desc_plain(sum_lo), desc_plain(desc_lo(sbase + C::kOffMid + at, 4096u - at)), kIdescS, 1u);
           tc_commit(sfull + q.i * 8);
-          if (hv.last_of_tile(u)) tc_commit(kfree + (t & 1) * 8);
+          if (last) tc_commit(kfree + tb);
         }
         __syncwarp();
         q.next();
+        ++ahead;
       };
-      // (Not ahead into the next piece: its queries wait for this one's last scores, and a piece is dealt out when the one before the last
-      // has been left.)
-      int ahead = 0;
 #pragma unroll 1
-      for (; ahead < min(hv.n, kSlots); ++ahead) qk(ahead);
+      while (ahead < min(hv.n, kSlots)) qk();
 #pragma unroll 1
-      for (int u = 0; u < hv.n; ++u, ++gs, s.next()) {
-        const int t = gt + (hv.nodes(u) ? n - 1 : u >> 1), side = hv.side(u);
-        const int steps = ((hv.nodes(u) ? p.n : min(kHalf, len - u0 * kTile - u * kHalf)) + 15) / 16;
-        if (side == 0) wait(vready + (t & 1) * 8, (t >> 1) & 1, ab);
+      for (int u = 0; u < hv.n; ++u, s.next()) {
+        const bool nodes = u >= hv.prefix;
+        const uint32_t t = (uint32_t)(nodes ? gt + n - 1 : gt + (u >> 1)), side = nodes ? 0u : u & 1u, tb = (t & 1u) * 8u;
+        if (side == 0) wait(vready + tb, (t >> 1) & 1, ab);
         wait(pready + s.i * 8, s.ph, ab);
         tc_fence_after();
+        const bool last = side == 1 || u >= hv.prefix - 1;
+        const int steps = nodes ? node_steps : u == hv.prefix - 1 ? end_steps : 4;
         if (tc_elect()) {
-          const uint32_t d = tmem0 + C::kTmO + (gs & 1) * 128, a = tmem0 + C::kTmS + s.i * 64, vl = v_lo + (uint32_t)((t & 1) * 2048 + side * 512);
+          const uint32_t d = tmem0 + C::kTmO + (gs & 1) * 128, a = tmem0 + C::kTmS + s.i * 64, vl = v_lo + (tb * 256u + side * 512u);
           tc_mma_ts(d, a, desc(vl), kIdescO, u > 1 ? 1u : 0u);
           if (steps == 4) {
 #pragma unroll
@@ -1074,10 +1104,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             for (int ks = 1; ks < steps; ++ks) tc_mma_ts(d, a + ks * 8, desc(vl + ks * 128u), kIdescO, 1u);
           }
           tc_commit(pvdone + s.i * 8);
-          if (hv.last_of_tile(u)) tc_commit(vfree + (t & 1) * 8);
+          if (last) tc_commit(vfree + tb);
         }
         __syncwarp();
-        if (ahead < hv.n) { qk(ahead); ++ahead; }
+        ++gs;
+        if (ahead < hv.n) qk();
       }
       gt += n;
       if (lane == 0) mbar_arrive(iempty + qi * 8);

@@ -54,7 +54,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
     only arrive together are one here."""
     B = {}
     for name, n, count in (("kfull", ring_k, 1), ("kempty", ring_k, 2), ("vfull", ring_v, 1), ("vempty", ring_v, 2), ("kready", 2, 2), ("sfull", N, 1),
-                           ("mkready", 8, 1), ("mvready", 8, 1), ("vready", 2, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", 2, 1), ("vfree", 2, 1),
+                           ("mready", 8, 1), ("vready", 2, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", 2, 1), ("vfree", 2, 1),
                            ("ifull", 2, 1), ("iempty", 2, 2 * softmax + 7), ("qready", 2, 1), ("kdone", 2, 1)):
         B[name] = [Barrier(count) for _ in range(n)]
     rawk, rawv = [Place(f"raw K {i}") for i in range(ring_k)], [Place(f"raw V {i}") for i in range(ring_v)]
@@ -79,22 +79,28 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
     def raw_tiles(n, tree):
         return n - 1 if tree else n
 
-    def copies():
+    def copies(values):
+        full, empty, ring, raw = ("vfull", "vempty", ring_v, rawv) if values else ("kfull", "kempty", ring_k, rawk)
         slot, phase, gt = 0, 1, 0
         for ic in range(len(pieces) + 1):
-            yield from wait("iempty", ic & 1, (ic >> 1) - 1)
-            item[ic & 1].write(ic)
-            B["ifull"][ic & 1].arrive()
-            n, tree, _ = pieces[ic] if ic < len(pieces) else (0, False, False)
+            if values:
+                n, tree, _ = yield from get(ic)
+            else:
+                yield from wait("iempty", ic & 1, (ic >> 1) - 1)
+                item[ic & 1].write(ic)
+                B["ifull"][ic & 1].arrive()
+                n, tree, _ = pieces[ic] if ic < len(pieces) else (0, False, False)
             if n == 0:
                 return
             for _ in range(raw_tiles(n, tree)):
-                yield from wait("kempty", slot, phase)
-                rawk[slot].write(gt)
-                B["kfull"][slot].arrive()
+                yield from wait(empty, slot, phase)
+                raw[slot].write(gt)
+                B[full][slot].arrive()
                 gt += 1
-                slot, phase = (0, phase ^ 1) if slot + 1 == ring_k else (slot + 1, phase)
+                slot, phase = (0, phase ^ 1) if slot + 1 == ring else (slot + 1, phase)
             gt += tree
+            if values:
+                B["iempty"][ic & 1].arrive()
 
     def k_tiles(side):
         gt = slot = phase = 0
@@ -109,7 +115,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 B["qready"][ic & 1].arrive()
             for u in range(n):
                 g = gt & 1
-                yield from wait("mkready", gt & 7, gt >> 3)
+                yield from wait("mready", gt & 7, gt >> 3)
                 if u < raw_tiles(n, tree):
                     yield from wait("kfull", slot, phase)
                     ktile[g][side].write(gt)
@@ -138,7 +144,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 return
             for u in range(n):
                 g = gt & 1
-                yield from wait("mvready", gt & 7, gt >> 3)
+                yield from wait("mready", gt & 7, gt >> 3)
                 yield from wait("vfree", g, (gt >> 1) - 1)
                 if u < raw_tiles(n, tree):
                     yield from wait("vfull", slot, phase)
@@ -157,38 +163,21 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 gt += 1
             B["iempty"][ic & 1].arrive()
 
-    def scales(values):
-        gt = slot = 0
-        phase = 1
+    def scales():
+        gt = 0
         for ic in range(len(pieces) + 1):
             n, tree, _ = yield from get(ic)
             if n == 0:
                 return
-            copied, raw = 0, raw_tiles(n, tree)
-            start = gt
-
-            def copy():
-                nonlocal slot, phase, copied
-                yield from wait("vempty", slot, phase)
-                rawv[slot].write(start + copied)
-                B["vfull"][slot].arrive()
-                copied += 1
-                slot, phase = (0, phase ^ 1) if slot + 1 == ring_v else (slot + 1, phase)
-
-            if values:
-                while copied < min(raw, ring_v - 1):
-                    yield from copy()
-            else:
-                yield from wait("qready", ic & 1, ic >> 1)
+            yield from wait("qready", ic & 1, ic >> 1)
             for u in range(n):
                 g = gt & 1
-                yield from wait("vready" if values else "kfree", g, (gt >> 1) - 1)
-                if u < raw:
-                    for x in (vm[g], exp[gt & 7]) if values else (km[g], mids[g], factor[gt & 7]):
+                yield from wait("kfree", g, (gt >> 1) - 1)
+                yield from wait("vready", g, (gt >> 1) - 1)
+                if u < raw_tiles(n, tree):
+                    for x in (vm[g], exp[gt & 7], km[g], mids[g], factor[gt & 7]):
                         x.write(gt)
-                B["mvready" if values else "mkready"][gt & 7].arrive()
-                if values and copied < raw:
-                    yield from copy()
+                B["mready"][gt & 7].arrive()
                 gt += 1
             B["iempty"][ic & 1].arrive()
 
@@ -271,8 +260,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                     gs += 1
                     continue
                 g, t = gs % N, t + gt
-                yield from wait("mkready", t & 7, t >> 3)
-                yield from wait("mvready", t & 7, t >> 3)
+                yield from wait("mready", t & 7, t >> 3)
                 if tree and u == len(halves) - 1:
                     yield from wait("kdone", ic & 1, ic >> 1)
                     yield from wait("vready", t & 1, t >> 1)
@@ -308,7 +296,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 yield
             B["iempty"][ic & 1].arrive()
 
-    roles = [copies(), k_tiles(0), k_tiles(1), v_tiles(0), v_tiles(1), scales(False), scales(True), products()] + [softmax_warp(g, w) for g in range(2) for w in range(softmax)]
+    roles = [copies(False), copies(True), k_tiles(0), k_tiles(1), v_tiles(0), v_tiles(1), scales(), products()] + [softmax_warp(g, w) for g in range(2) for w in range(softmax)]
     core = tensor_core()
     speed = [rng.choice([1, 1, 1, 3, 30, 200]) for _ in roles]
     core_speed, idle = rng.choice([1, 3, 30]), 0
@@ -341,10 +329,11 @@ def test_the_kernel_waits_for_what_is_played():
     """The waits of the roles in the source, by barrier."""
     code = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "tree_attention.cu")).read())
     code = code[code.index("tree_attention_kernel("):code.index("tree_combine_kernel(")]
-    cuts = ["if (warp < 8) {", "if (warp < 16) {", "if (warp < 24) {", "if (warp != 26) {", "constexpr uint32_t kIdescS"]
+    cuts = ["if (warp < 8) {", "if (warp < 16) {", "if (warp < 24) {", "if (warp < 26) {", "if (warp == 27) {", "constexpr uint32_t kIdescS"]
     at = [code.index(x) for x in cuts] + [len(code)]
     waits = [sorted(set(re.findall(r"\bwait\((\w+)", code[a:b]))) for a, b in zip(at, at[1:])]
-    assert waits == [["ifull", "kdone", "mkready", "mvready", "pvdone", "sfull", "vready"], ["ifull", "kfree", "kfull", "mkready"],
-                     ["ifull", "mvready", "vfree", "vfull"], ["empty", "iempty", "ifull", "qready", "used"], ["ifull", "kready", "pready", "vready"]]
+    assert waits == [["ifull", "kdone", "mready", "pvdone", "sfull", "vready"], ["ifull", "kfree", "kfull", "mready"],
+                     ["ifull", "mready", "vfree", "vfull"], ["empty", "iempty", "ifull"], ["ifull", "kfree", "qready", "vready"],
+                     ["ifull", "kready", "pready", "vready"]]
     land, done, free = (code.index(x) for x in ("land_after_abort(", "named_bar(2, kDoneThreads)", "tcgen05.dealloc"))
     assert done < land < free and len(re.findall(r"bar_arrive\(2, kDoneThreads\)", code)) == 2
