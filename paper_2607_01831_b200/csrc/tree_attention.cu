@@ -52,7 +52,7 @@ namespace {
 constexpr int kTile = 128;          // tokens of a tile
 constexpr int kHalf = 64;           // of half a tile: what the softmax and the products take at a time
 constexpr int kM = 128;             // rows of a row block
-constexpr int kSlots = 3;           // places for scores
+constexpr int kSlots = 3;           // places for scores; for the scales of a tile
 constexpr int kMaxNodes = 64;
 constexpr int kPartRow = 132;       // floats of a partial row: O[128], reference, sum, pad
 constexpr int kThreads = 896;
@@ -95,15 +95,15 @@ struct Cfg {
   static constexpr int kRingK = FULL ? 3 : 5, kRingV = FULL ? 2 : 5;
   static constexpr int kOffK = 0, kOffV = kOffK + 2 * 32768, kOffRK = kOffV + 2 * 32768, kOffRV = kOffRK + kRingK * kStage,
                        kOffSum = kOffRV + kRingV * kStage;           // [128] the query sums' 8 FP16
-  static constexpr int kOffMid = kOffSum + 2048;                     // [2][128] the middles' 8 FP16
-  static constexpr int kOffZero = kOffMid + 4096;                    // 128 x 8 zeros, the other half of both
-  static constexpr int kOffKm = kOffZero + 2048;                     // [2][128] half2 {scale, - 1152 scale}
-  static constexpr int kOffVm = kOffKm + 2 * 512;                    // [2][128] half2 {scale, mid}
-  static constexpr int kOffMl = kOffVm + 2 * 512;                    // [2][128] {reference, sum}
+  static constexpr int kOffMid = kOffSum + 2048;                     // [kSlots][128] the middles' 8 FP16
+  static constexpr int kOffZero = kOffMid + kSlots * 2048;                    // 128 x 8 zeros, the other half of both
+  static constexpr int kOffKm = kOffZero + 2048;                     // [kSlots][128] half2 {scale, - 1152 scale}
+  static constexpr int kOffVm = kOffKm + kSlots * 512;               // [kSlots][128] half2 {scale, mid}
+  static constexpr int kOffMl = kOffVm + kSlots * 512;                    // [2][128] {reference, sum}
   static constexpr int kOffItems = kOffMl + 2 * 1024;                // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
   static constexpr int kOffBars = kOffMisc + 256;
-  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 3 * kSlots + 8 + 16;
+  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 5 * kSlots + 8 + 12;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024, "shared memory");
   static_assert(kOffSum % 128 == 0 && kOffBars % 8 == 0, "alignment");
@@ -115,10 +115,24 @@ struct Cfg {
 struct Slot {
   int i = 0;
   uint32_t ph = 0;
-  __device__ __forceinline__ void next() {
-    if (++i == kSlots) { i = 0; ph ^= 1; }
+  __device__ __forceinline__ void next(int by = 1) {   // (by less than kSlots)
+    i += by;
+    if (i >= kSlots) { i -= kSlots; ph ^= 1; }
+  }
+  __device__ __forceinline__ Slot before(int by) const {
+    Slot s;
+    s.i = i - by;
+    s.ph = ph;
+    if (s.i < 0) { s.i += kSlots; s.ph ^= 1; }
+    return s;
   }
 };
+__device__ __forceinline__ Slot slot_of(int at) {   // of the at-th use
+  Slot s;
+  s.i = at % kSlots;
+  s.ph = (uint32_t)(at / kSlots) & 1u;
+  return s;
+}
 
 struct Item {  // a piece: tiles u0 .. u0 + n - 1 of segment (b, h, rb), none: the end
   int b, h, rb, len, u0, n, first_cta, n_contrib;
@@ -306,31 +320,27 @@ template <bool FULL, bool VALUES>
 __device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t meta, int i, int row_base) {
   const int cc = i & 3, row0 = row_base + (i >> 2);
   const uint32_t sw = (uint32_t)(((cc >> 1) ^ (row0 >> 1)) & 1) * 2u;
-  const uint32_t dst = tile + (uint32_t)(cc >> 1) * 16384u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
-  const uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16);
+  uint32_t dst = tile + (uint32_t)(cc >> 1) * 16384u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
+  uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16);
   meta += (uint32_t)row0 * 4u;
-  uint2 x[2][2], y[2][2];
-  uint32_t sm[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-#pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      x[i][z] = lds64(a + i * 2048u + (sw ^ (uint32_t)(2 * z)) * 4u);
-      y[i][z] = FULL ? lds64(a + i * 2048u + 8192u + (sw ^ (uint32_t)(2 * z)) * 4u) : make_uint2(0x88888888u, 0x88888888u);
+  // (a rolled loop: the roles of a scheduler share an instruction cache of some 12 KB)
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i, a += 2048u, dst += 4096u, meta += 128u) {
+    const uint2 x0 = lds64(a + sw * 4u), x1 = lds64(a + (sw ^ 2u) * 4u);
+    uint2 y0 = make_uint2(0x88888888u, 0x88888888u), y1 = y0;
+    if (FULL) {
+      y0 = lds64(a + 8192u + sw * 4u);
+      y1 = lds64(a + 8192u + (sw ^ 2u) * 4u);
     }
-    sm[i] = lds32(meta + i * 128u);
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t s2 = __byte_perm(sm[i], sm[i], 0x1010), m2 = __byte_perm(sm[i], sm[i], 0x3232);
-    const uint32_t wa[4] = {x[i][0].x, x[i][0].y, x[i][1].x, x[i][1].y}, wr[4] = {y[i][0].x, y[i][0].y, y[i][1].x, y[i][1].y};
+    const uint32_t sm = lds32(meta), s2 = __byte_perm(sm, sm, 0x1010), m2 = __byte_perm(sm, sm, 0x3232);
+    const uint32_t wa[4] = {x0.x, x0.y, x1.x, x1.y}, wr[4] = {y0.x, y0.y, y1.x, y1.y};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {   // register k holds word k ^ sw of the chunk
       uint32_t o[4];
       codes8(wa[k], wr[k], o);
 #pragma unroll
       for (int z = 0; z < 4; ++z) o[z] = fma_f16x2(VALUES ? centred(o[z]) : o[z], s2, m2);
-      sts128((dst ^ (uint32_t)(k * 16)) + i * 4096u, o[0], o[1], o[2], o[3]);
+      sts128(dst ^ (uint32_t)(k * 16), o[0], o[1], o[2], o[3]);
     }
   }
 }
@@ -478,9 +488,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
-  // of a half tile: sfull, pready, pvdone; of a tile: kready, kfree, vready, vfree (in turn), mready; of a piece: ifull, iempty, qready, kdone
+  // of a half tile: sfull, pready, pvdone; of a tile: kfree, vready (kSlots), kready, vfree (in turn), mready (8); of a piece: ifull, iempty, qready, kdone
   const uint32_t sfull = vempty + 8 * C::kRingV, pready = sfull + 8 * kSlots, pvdone = pready + 8 * kSlots, mready = pvdone + 8 * kSlots,
-                 kready = mready + 64, kfree = kready + 16, vready = kfree + 16, vfree = vready + 16, ifull = vfree + 16, iempty = ifull + 16,
+                 kready = mready + 64, kfree = kready + 16, vready = kfree + 8 * kSlots, vfree = vready + 8 * kSlots, ifull = vfree + 16, iempty = ifull + 16,
                  qready = iempty + 16, kdone = qready + 16;
   volatile int* ab = misc;        // (waits for data)
   volatile int* iab = misc + 1;   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
@@ -492,12 +502,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       mbar_init(sfull + i * 8, 1);
       mbar_init(pready + i * 8, 4);
       mbar_init(pvdone + i * 8, 1);
+      mbar_init(kfree + i * 8, 1);
+      mbar_init(vready + i * 8, 8);
     }
     for (int i = 0; i < 8; ++i) mbar_init(mready + i * 8, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(kready + i * 8, 8);
-      mbar_init(kfree + i * 8, 1);
-      mbar_init(vready + i * 8, 8);
       mbar_init(vfree + i * 8, 1);
       mbar_init(qready + i * 8, 4);
       mbar_init(kdone + i * 8, 4);
@@ -529,9 +539,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     constexpr int kCW = C::kW < 32 ? C::kW : 32;                           // scores at a time
     float2* ml = reinterpret_cast<float2*>(smem + C::kOffMl);
     int gt = 0, gs = 0;   // tiles and half tiles so far
-    Slot s, s2;           // of half tile gs, and of half tile gs - 2
-    s2.i = 1;
-    s2.ph = 1;
+    Slot s;               // of this warpgroup's next half tile
+    s.i = g;
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
@@ -544,15 +553,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       bool fresh = true, any = false;   // no reference yet; a half tile of this warpgroup's
       float ref = 0.0f, l = 0.0f;
 #pragma unroll 1
-      for (int u = 0; u < hv.n; ++u, ++gs, s.next(), s2.next()) {
-        if ((gs & 1) != g) continue;
+      for (int u = (gs & 1) ^ g; u < hv.n; u += 2) {
         // (No barrier may be more than a phase further than a wait expects: see tests/test_tree_handoffs.py.)
         const bool tree = hv.nodes(u);
         const int t = gt + (tree ? n - 1 : u >> 1);
         wait(mready + (t & 7) * 8, (t >> 3) & 1, ab);
         if (tree) {   // the factor and the exponent of the nodes
           wait(kdone + qi * 8, (ic >> 1) & 1, ab);
-          wait(vready + (t & 1) * 8, (t >> 1) & 1, ab);
+          const Slot v = slot_of(t);
+          wait(vready + v.i * 8, v.ph, ab);
         }
         wait(sfull + s.i * 8, s.ph, ab);
         tc_fence_after();
@@ -625,7 +634,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             if (need) { ref += delta; fresh = false; }
             l *= f;
             if (any) {
-              wait(pvdone + s2.i * 8, s2.ph, ab);
+              const Slot prev = s.before(2);
+              wait(pvdone + prev.i * 8, prev.ph, ab);
               tc_fence_after();
 #pragma unroll 1
               for (int i = 0; i < 128; i += 8) {
@@ -665,14 +675,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(pready + s.i * 8);
+        s.next(2);
         any = true;
       }
       // ---- end of the piece: both warpgroups' sums, half of the channels each
       gt += n;
-      Slot s1 = s2;   // of half tile gs - 1
-      s1.next();
-      wait(pvdone + s1.i * 8, s1.ph, ab);
-      if (hv.n > 1) wait(pvdone + s2.i * 8, s2.ph, ab);
+      gs += hv.n;
+      const Slot end = slot_of(gs - 1), other_end = end.before(1);
+      wait(pvdone + end.i * 8, end.ph, ab);
+      if (hv.n > 1) wait(pvdone + other_end.i * 8, other_end.ph, ab);
       tc_fence_after();
       if (works) {
         const float2 mine = any && !fresh ? make_float2(ref, l) : make_float2(-INFINITY, 0.0f);
@@ -747,6 +758,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     const int kt = (tid - 256) & 127, side = (warp >> 2) & 1;   // (the second warpgroup has the tile's second half and no more)
     int gt = 0, slot = 0;
     uint32_t phase = 0;
+    Slot ms;          // of tile gt among kSlots
     float a = 0.0f;   // factor of the scores, but for the keys' exponent
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
@@ -772,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         const float f = pow2(-e);
         a = p.sm_log2 * pow2(e);
         if (kt == 0) misc[28 + qi] = __float_as_int(a);
-        if (gt > 0) wait(kfree + ((gt - 1) & 1) * 8, ((gt - 1) >> 1) & 1, ab);   // the previous piece's last Q K^T
+        if (gt > 0) wait(kfree + ms.before(1).i * 8, ms.before(1).ph, ab);   // the previous piece's last Q K^T
         tc_fence_after();
         const uint32_t tm_q = tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16);
 #pragma unroll 1
@@ -795,14 +807,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         if (lane == 0) mbar_arrive(qready + qi * 8);
       }
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt) {
+      for (int u = 0; u < n; ++u, ++gt, ms.next()) {
         const int ut = u0 + u, g = gt & 1;
         const uint32_t tile = sbase + C::kOffK + (uint32_t)g * 32768u;
-        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);   // (and the tile has been used: warp 27 has waited for that)
+        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);
+        if (gt > 1) wait(kfree + ms.before(2).i * 8, ms.before(2).ph, ab);   // the tile has been used
         if (ut < n_prefix) {
           wait(kfull + slot * 8, phase, ab);
           if (len - ut * kTile > kHalf * side)
-            expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, sbase + C::kOffKm + (uint32_t)g * 512u, kt, kHalf * side);
+            expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, sbase + C::kOffKm + (uint32_t)ms.i * 512u, kt, kHalf * side);
           __syncwarp();
           if (lane == 0) mbar_arrive(kempty + slot * 8);
           if (++slot == C::kRingK) { slot = 0; phase ^= 1; }
@@ -827,7 +840,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               sts128(chunk_at(tile, kt, ch), w.x, w.y, w.z, w.w);
             }
           }
-          if (kt < kMaxNodes) sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + kt * 16), 0u, 0u, 0u, 0u);
+          if (kt < kMaxNodes) sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + kt * 16), 0u, 0u, 0u, 0u);
         }
         proxy_fence();
         tc_fence_before();   // (the queries)
@@ -847,6 +860,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     const int vt = (tid - 512) & 127, w4 = warp & 3, side = (warp >> 2) & 1;
     int gt = 0, slot = 0;
     uint32_t phase = 0;
+    Slot ms;
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
@@ -854,7 +868,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt) {
+      for (int u = 0; u < n; ++u, ++gt, ms.next()) {
         const int ut = u0 + u, g = gt & 1;
         const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u;
         wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);
@@ -862,7 +876,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         if (ut < n_prefix) {
           wait(vfull + slot * 8, phase, ab);
           if (len - ut * kTile > kHalf * side)
-            expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, sbase + C::kOffVm + (uint32_t)g * 512u, vt, kHalf * side);
+            expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, sbase + C::kOffVm + (uint32_t)ms.i * 512u, vt, kHalf * side);
           __syncwarp();
           if (lane == 0) mbar_arrive(vempty + slot * 8);
           if (++slot == C::kRingV) { slot = 0; phase ^= 1; }
@@ -890,7 +904,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
         proxy_fence();
         __syncwarp();
-        if (lane == 0) mbar_arrive(vready + g * 8);
+        if (lane == 0) mbar_arrive(vready + ms.i * 8);
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
@@ -953,6 +967,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   // ================================================================================== scales and zero points
   if (warp == 27) {
     int gt = 0;
+    Slot ms;
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
@@ -982,9 +997,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         fetch(min(t, top), first);
       }
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt) {
-        const int ut = u0 + u, g = gt & 1;
-        const uint32_t before = ((gt >> 1) - 1) & 1;
+      for (int u = 0; u < n; ++u, ++gt, ms.next()) {
+        const int ut = u0 + u;
         if (ut < n_prefix) {
           const int t = ut * kTile + lane * 4, room = len - t;   // (what lies behind the sequence's end may be anything)
           float sc[2][4], mid[2][4], big[2] = {0.0f, 0.0f};
@@ -998,8 +1012,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               big[v] = fmaxf(big[v], fabsf(mid[v][i]) + 128.0f * fabsf(sc[v][i]));
             }
           }
-          fetch(min(t + kTile, top), id);
-          id = block_id(p, b, min(t + 2 * kTile, top));
           const int ek = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big[0]))) + 3;   // (1152 scales below 2^15.2)
           const int ev = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big[1])));
           const float fk = pow2(-ek), fv = pow2(-ev);
@@ -1022,12 +1034,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) vm[i] = pack_f16x2(sc[1][i] * fv, mid[1][i] * fv);
-          wait(kfree + g * 8, before, ab);    // these places have been read (the softmax's of eight tiles before, too)
-          wait(vready + g * 8, before, ab);
+          if (gt >= kSlots) {   // these places have been read (the softmax's of eight tiles before, too)
+            wait(kfree + ms.i * 8, ms.ph ^ 1u, ab);
+            wait(vready + ms.i * 8, ms.ph ^ 1u, ab);
+          }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sts128(sbase + C::kOffMid + (uint32_t)(g * 2048 + lane * 64 + i * 16), mids[i][0], mids[i][1], 0u, 0u);
-          sts128(sbase + C::kOffKm + (uint32_t)(g * 512 + lane * 16), km[0], km[1], km[2], km[3]);
-          sts128(sbase + C::kOffVm + (uint32_t)(g * 512 + lane * 16), vm[0], vm[1], vm[2], vm[3]);
+          for (int i = 0; i < 4; ++i) sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + lane * 64 + i * 16), mids[i][0], mids[i][1], 0u, 0u);
+          sts128(sbase + C::kOffKm + (uint32_t)(ms.i * 512 + lane * 16), km[0], km[1], km[2], km[3]);
+          sts128(sbase + C::kOffVm + (uint32_t)(ms.i * 512 + lane * 16), vm[0], vm[1], vm[2], vm[3]);
           if (lane == 0) {
             misc[32 + 2 * (gt & 7)] = __float_as_int(times_pow2(a, ek));
             misc[33 + 2 * (gt & 7)] = ev;
@@ -1035,11 +1049,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           proxy_fence();
         } else {   // the nodes' are made by the warps that have their keys and values.  These wait for this warp all the same, so that no barrier
                    // is a phase further than what a wait for it expects
-          wait(kfree + g * 8, before, ab);
-          wait(vready + g * 8, before, ab);
+          if (gt >= kSlots) {
+            wait(kfree + ms.i * 8, ms.ph ^ 1u, ab);
+            wait(vready + ms.i * 8, ms.ph ^ 1u, ab);
+          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(mready + (gt & 7) * 8);
+        if (ut < n_prefix) {   // (behind the fence, which waits for loads on their way: 1100 cycles a tile in front of it)
+          const int t = (ut + 1) * kTile + lane * 4;
+          fetch(min(t, top), id);
+          id = block_id(p, b, min(t + kTile, top));
+        }
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
@@ -1050,6 +1071,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     constexpr uint32_t kIdescS = tc_idesc(kHalf, false), kIdescO = tc_idesc(128, true);
     const uint32_t k_lo = desc_lo(sbase + C::kOffK, 16u), v_lo = desc_lo(sbase + C::kOffV, 16384u), sum_lo = desc_lo(sbase + C::kOffSum, C::kOffZero - C::kOffSum);
     Slot q, s;   // of the next Q K^T, of the next P V
+    Slot ms, vs;   // of their tiles
     int gt = 0, gs = 0;
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
@@ -1070,16 +1092,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         tc_fence_after();
         const bool last = side == 1 || ahead >= hv.prefix - 1;
         if (tc_elect()) {
-          const uint32_t d = tmem0 + C::kTmS + q.i * 64, kl = k_lo + (tb * 256u + side * 512u), at = tb * 256u + side * 1024u;
+          const uint32_t d = tmem0 + C::kTmS + q.i * 64, kl = k_lo + (tb * 256u + side * 512u), at = (uint32_t)ms.i * 2048u + side * 1024u;
 #pragma unroll
           for (int ks = 0; ks < 8; ++ks)
             tc_mma_ts(d, tmem0 + C::kTmQ + ks * 8, desc(kl + (uint32_t)(((ks >> 2) * 16384 + (ks & 3) * 32) >> 4)), kIdescS, ks > 0 ? 1u : 0u);
-          tc_mma_ss(d, desc_plain(sum_lo), desc_plain(desc_lo(sbase + C::kOffMid + at, 4096u - at)), kIdescS, 1u);
+          tc_mma_ss(d, desc_plain(sum_lo), desc_plain(desc_lo(sbase + C::kOffMid + at, C::kOffZero - C::kOffMid - at)), kIdescS, 1u);
           tc_commit(sfull + q.i * 8);
-          if (last) tc_commit(kfree + tb);
+          if (last) tc_commit(kfree + ms.i * 8);
         }
         __syncwarp();
         q.next();
+        if (last) ms.next();
         ++ahead;
       };
 #pragma unroll 1
@@ -1088,7 +1111,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       for (int u = 0; u < hv.n; ++u, s.next()) {
         const bool nodes = u >= hv.prefix;
         const uint32_t t = (uint32_t)(nodes ? gt + n - 1 : gt + (u >> 1)), side = nodes ? 0u : u & 1u, tb = (t & 1u) * 8u;
-        if (side == 0) wait(vready + tb, (t >> 1) & 1, ab);
+        if (side == 0) wait(vready + vs.i * 8, vs.ph, ab);
         wait(pready + s.i * 8, s.ph, ab);
         tc_fence_after();
         const bool last = side == 1 || u >= hv.prefix - 1;
@@ -1107,6 +1130,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           if (last) tc_commit(vfree + tb);
         }
         __syncwarp();
+        if (last) vs.next();
         ++gs;
         if (ahead < hv.n) qk();
       }

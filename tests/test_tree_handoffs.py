@@ -37,7 +37,7 @@ class Place:
         assert self.tile == tile, f"{self.name}: {self.tile} instead of {tile}"
 
 
-N = 3       # places for scores
+N = 3       # places for scores, and for the scales of a tile
 
 
 def _halves(n, tree, short):
@@ -54,12 +54,12 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
     only arrive together are one here."""
     B = {}
     for name, n, count in (("kfull", ring_k, 1), ("kempty", ring_k, 2), ("vfull", ring_v, 1), ("vempty", ring_v, 2), ("kready", 2, 2), ("sfull", N, 1),
-                           ("mready", 8, 1), ("vready", 2, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", 2, 1), ("vfree", 2, 1),
+                           ("mready", 8, 1), ("vready", N, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", N, 1), ("vfree", 2, 1),
                            ("ifull", 2, 1), ("iempty", 2, 2 * softmax + 7), ("qready", 2, 1), ("kdone", 2, 1)):
         B[name] = [Barrier(count) for _ in range(n)]
     rawk, rawv = [Place(f"raw K {i}") for i in range(ring_k)], [Place(f"raw V {i}") for i in range(ring_v)]
     S = [Place(f"S {i}") for i in range(N)]
-    vm, km, mids = ([Place(f"{x} {i}") for i in range(2)] for x in ("vm", "km", "mid"))
+    vm, km, mids = ([Place(f"{x} {i}") for i in range(N)] for x in ("vm", "km", "mid"))
     ktile, vtile = ([[Place(f"{x} {i} {j}") for j in range(2)] for i in range(2)] for x in ("K", "V"))
     factor, exp = ([Place(f"{x} {i}") for i in range(8)] for x in ("a", "e"))
     item, O, Q = [Place("item 0"), Place("item 1")], [Place("O 0"), Place("O 1")], Place("Q")
@@ -110,26 +110,28 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 return
             if side == 0:
                 if gt > 0:
-                    yield from wait("kfree", (gt - 1) & 1, (gt - 1) >> 1)
+                    yield from wait("kfree", (gt - 1) % N, (gt - 1) // N)
                 Q.write(ic)
                 B["qready"][ic & 1].arrive()
             for u in range(n):
                 g = gt & 1
                 yield from wait("mready", gt & 7, gt >> 3)
+                if gt > 1:
+                    yield from wait("kfree", (gt - 2) % N, (gt - 2) // N)
                 if u < raw_tiles(n, tree):
                     yield from wait("kfull", slot, phase)
                     ktile[g][side].write(gt)
                     rawk[slot].read(gt)
-                    km[g].read(gt)
-                    km[g].readers += 1
+                    km[gt % N].read(gt)
+                    km[gt % N].readers += 1
                     yield
-                    km[g].readers -= 1
+                    km[gt % N].readers -= 1
                     B["kempty"][slot].arrive()
                     slot, phase = (0, phase ^ 1) if slot + 1 == ring_k else (slot + 1, phase)
                 elif side == 0:
                     ktile[g][0].write(gt)
                     factor[gt & 7].write(gt)
-                    mids[g].write(gt)
+                    mids[gt % N].write(gt)
                 B["kready"][g].arrive()
                 gt += 1
             if side == 0:
@@ -150,16 +152,16 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                     yield from wait("vfull", slot, phase)
                     vtile[g][side].write(gt)
                     rawv[slot].read(gt)
-                    vm[g].read(gt)
-                    vm[g].readers += 1
+                    vm[gt % N].read(gt)
+                    vm[gt % N].readers += 1
                     yield
-                    vm[g].readers -= 1
+                    vm[gt % N].readers -= 1
                     B["vempty"][slot].arrive()
                     slot, phase = (0, phase ^ 1) if slot + 1 == ring_v else (slot + 1, phase)
                 elif side == 0:
                     vtile[g][0].write(gt)
                     exp[gt & 7].write(gt)
-                B["vready"][g].arrive()
+                B["vready"][gt % N].arrive()
                 gt += 1
             B["iempty"][ic & 1].arrive()
 
@@ -171,11 +173,11 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 return
             yield from wait("qready", ic & 1, ic >> 1)
             for u in range(n):
-                g = gt & 1
-                yield from wait("kfree", g, (gt >> 1) - 1)
-                yield from wait("vready", g, (gt >> 1) - 1)
+                if gt >= N:
+                    yield from wait("kfree", gt % N, gt // N - 1)
+                    yield from wait("vready", gt % N, gt // N - 1)
                 if u < raw_tiles(n, tree):
-                    for x in (vm[g], exp[gt & 7], km[g], mids[g], factor[gt & 7]):
+                    for x in (vm[gt % N], exp[gt & 7], km[gt % N], mids[gt % N], factor[gt & 7]):
                         x.write(gt)
                 B["mready"][gt & 7].arrive()
                 gt += 1
@@ -192,7 +194,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 yield from wait("kready", t & 1, t >> 1)
             Q.readers += 1
             ktile[t & 1][not first].readers += 1
-            mids[t & 1].readers += 1
+            mids[t % N].readers += 1
             issued.append(("qk", ahead, ic, t, first, last, False))
             ahead += 1
 
@@ -207,7 +209,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             for u, (t, first, last) in enumerate(halves):
                 t += gt
                 if first:
-                    yield from wait("vready", t & 1, t >> 1)
+                    yield from wait("vready", t % N, t // N)
                 yield from wait("pready", gs % N, gs // N)
                 vtile[t & 1][not first].readers += 1
                 issued.append(("pv", gs, ic, t, first, last, u < 2))
@@ -232,13 +234,13 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             if kind == "qk":
                 Q.read(ic)
                 ktile[t & 1][not first].read(t)
-                mids[t & 1].read(t)
-                mids[t & 1].readers -= 1
+                mids[t % N].read(t)
+                mids[t % N].readers -= 1
                 Q.readers -= 1
                 ktile[t & 1][not first].readers -= 1
                 B["sfull"][gs % N].arrive()
                 if last:
-                    B["kfree"][t & 1].arrive()
+                    B["kfree"][t % N].arrive()
             else:
                 S[gs % N].read(gs)
                 vtile[t & 1][not first].read(t)
@@ -263,7 +265,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 yield from wait("mready", t & 7, t >> 3)
                 if tree and u == len(halves) - 1:
                     yield from wait("kdone", ic & 1, ic >> 1)
-                    yield from wait("vready", t & 1, t >> 1)
+                    yield from wait("vready", t % N, t // N)
                 yield from wait("sfull", g, gs // N)
                 S[g].read(gs)
                 for p in (factor[t & 7], exp[t & 7]):
