@@ -23,16 +23,16 @@
 // memory, over the scores, as the A operand of P V; three places for scores, so that Q K^T is never waited for.
 // One CTA per SM; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
 //   warps 0-3, 4-7   softmax, even and odd half tiles
-//   warps 8-15       K codes to FP16 into the K tiles, and a piece's queries
-//   warps 16-23      V codes to FP16 values into the V tiles
-//   warps 24, 25     copies of K and V planes into rings, four 16-token sub-blocks at a time; warp 24 deals out the pieces
-//   warp 27          scales and zero points of a tile: what the K and V tiles and the softmax need of them
+//   warps 8-23       codes to FP16: K tiles by those on the first two of the four schedulers, V tiles on the others (warp mod 4); a piece's
+//                    queries by the first four
+//   warp 24          copies of the planes into rings, four 16-token sub-blocks at a time; deals out the pieces
+//   warps 25, 27     scales and zero points of a tile's values and keys: what the tiles and the softmax need of them
 //   warp 26          issues every tcgen05.mma: Q K^T three half tiles ahead of P V
-// The copy engine takes some 35 cycles per row of a copy and a lane that issues copies of one sub-block each some 80: 48 of them a tile, planes
-// and scales, took 4000 cycles (140 us for 128 rows over 131072 tokens).  Hence gathers of four sub-blocks by two warps, and plain loads,
-// two tiles ahead, of the scales.  A hand-off costs its roles some 500 cycles whatever it hands over, and each is in itself a chain of latencies: hence tiles of 128 tokens
-// between the warps that expand codes, of 64 where tensor memory has no room for more, and eight warps for either expansion (173 us by
-// four each and tiles of 64).
+// What bounds it is the issue of instructions and how they come: the roles of a scheduler share an instruction cache of some 12 KB, hence rolled
+// loops, one copy of what is rare (masks, a new reference), few roles on a scheduler, and short loops where a barrier is waited for.  Between
+// the warps that expand codes tiles have 128 tokens, since a hand-off costs its roles some 500 cycles whatever it hands over; 64 where
+// tensor memory has no room for more.  The copy engine takes some 35 cycles per row of a copy, and a lane that issues copies of one
+// sub-block each some 80: hence gathers, and plain loads, a tile ahead, of the scales.
 // Work is cut in stream-K form: the (sequence, KV head, row block, tile) list into equal ranges, a piece being a range's part of one
 // segment.  A segment within one CTA is written by it; otherwise partial (ref, l, O) go to the workspace and a dependent
 // kernel joins them.
@@ -56,9 +56,9 @@ constexpr int kSlots = 3;           // places for scores; for the scales of a ti
 constexpr int kMaxNodes = 64;
 constexpr int kPartRow = 132;       // floats of a partial row: O[128], reference, sum, pad
 constexpr int kThreads = 896;
-constexpr int kDoneThreads = 256 + 3 * 32;   // softmax warpgroups, copies, products
+constexpr int kDoneThreads = 256 + 2 * 32;   // softmax warpgroups, copies, products
 // log2 of the largest of a row's weights when its reference is set; a sum of them that sets it anew (none is above it, and FP16 holds 65504)
-constexpr float kTop = 7.0f, kMost = 65000.0f;
+constexpr float kTop = 7.0f, kMost = 65000.0f, kRaise = 9.9f;   // (64 weights of 2^9.9: 61000)
 constexpr int kMinExp = -80;        // smallest exponent of a tile's keys or values
 
 struct TreeParams {
@@ -167,22 +167,19 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
       : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
 __device__ __forceinline__ uint64_t globaltimer_ns() {
   uint64_t t;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// Gives up after two seconds (see bounded_wait.cuh); the caller carries on without the data, so that all loops end, and the
-// host is told through the status word.  (Inlined: ptxas does not split the registers of a kernel that has calls.)
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_word) {
-  if (mbar_test(bar, parity)) return true;
-  return bounded_wait([=] { return mbar_try_wait(bar, parity); }, [] { return globaltimer_ns(); }, abort_word);
+// Gives up after 2^17 probes, each of which may park its thread for 20 us, or once another thread has; the caller carries on without the data,
+// so that all loops end, and the host is told through the status word.  (Inlined, and no longer than it must be: there are some thirty.)
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* abort_word) {
+  for (uint32_t i = 0; !mbar_try_wait(bar, parity); ++i)
+    if (i >= (1u << 17) || *abort_word) {
+      *abort_word = 1;
+      break;
+    }
 }
 // Four rows of a map one behind the other.
 __device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3, uint32_t bar) {
@@ -193,6 +190,11 @@ __device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, ui
 __device__ __forceinline__ void named_bar(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t a, float (&x)[N]) {
+#pragma unroll
+  for (int k = 0; k < N / 16; ++k) TmemRegs<16>::ld(a + k * 16, reinterpret_cast<uint32_t*>(x) + 16 * k);
+}
 template <int N>
 __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -312,25 +314,24 @@ __device__ __forceinline__ uint32_t two_parts(float x) {
   return pack_f16x2(hi, x - hi);
 }
 
-// The codes of half a tile by 128 threads: thread i takes the 16-byte chunk i & 3 (32 channels) of rows i >> 2 and 32 on.  Half of the threads take a
-// chunk's 8-byte halves in the other order: the eight threads of a store's phase then have eight chunk positions, and rows that share
-// their banks in the raw stage are read in different halves.
+// A tile's codes, 64 or 128 rows, by eight warps: lane i of warp w takes the 16-byte chunk i & 3 (32 channels) of rows 8 w + (i >> 2) and 64 on.
+// Half of the lanes take a chunk's 8-byte halves in the other order: the eight of a store's phase then have eight chunk positions, and rows
+// that share their banks in the raw stage are read in different halves.
 // meta: per row, keys {scale, -1152 scale (rounded)} -> (1024 + c) scale - 1152 scale, values {scale, mid} -> (c - 128) scale + mid.
 template <bool FULL, bool VALUES>
-__device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t meta, int i, int row_base) {
-  const int cc = i & 3, row0 = row_base + (i >> 2);
+__device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t meta, int w, int i, int rounds) {
+  const int cc = i & 3, row0 = 8 * w + (i >> 2);
   const uint32_t sw = (uint32_t)(((cc >> 1) ^ (row0 >> 1)) & 1) * 2u;
   uint32_t dst = tile + (uint32_t)(cc >> 1) * 16384u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
-  uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16);
+  uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16) + sw * 4u;
   meta += (uint32_t)row0 * 4u;
-  // (a rolled loop: the roles of a scheduler share an instruction cache of some 12 KB)
 #pragma unroll 1
-  for (int i = 0; i < 2; ++i, a += 2048u, dst += 4096u, meta += 128u) {
-    const uint2 x0 = lds64(a + sw * 4u), x1 = lds64(a + (sw ^ 2u) * 4u);
+  for (; rounds > 0; --rounds, a += 4096u, dst += 8192u, meta += 256u) {
+    const uint2 x0 = lds64(a), x1 = lds64(a ^ 8u);
     uint2 y0 = make_uint2(0x88888888u, 0x88888888u), y1 = y0;
     if (FULL) {
-      y0 = lds64(a + 8192u + sw * 4u);
-      y1 = lds64(a + 8192u + (sw ^ 2u) * 4u);
+      y0 = lds64(a + 8192u);
+      y1 = lds64((a ^ 8u) + 8192u);
     }
     const uint32_t sm = lds32(meta), s2 = __byte_perm(sm, sm, 0x1010), m2 = __byte_perm(sm, sm, 0x3232);
     const uint32_t wa[4] = {x0.x, x0.y, x1.x, x1.y}, wr[4] = {y0.x, y0.y, y1.x, y1.y};
@@ -482,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   const uint32_t sbase = smem_u32(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
-  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [8 + i] V maxima, [12 + i] K maxima, [16 + 4 piece + i]
+  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [8 + i] maxima of the nodes, [16 + 4 piece + i]
                                              // q maxima, [28 + piece] the queries' part of the scores' factor, [32 + 2 (tile % 8)] that factor, [33 + 2 (tile % 8)]
                                              // exponent of the values
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
@@ -505,14 +506,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       mbar_init(kfree + i * 8, 1);
       mbar_init(vready + i * 8, 8);
     }
-    for (int i = 0; i < 8; ++i) mbar_init(mready + i * 8, 1);
+    for (int i = 0; i < 8; ++i) mbar_init(mready + i * 8, 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(kready + i * 8, 8);
       mbar_init(vfree + i * 8, 1);
       mbar_init(qready + i * 8, 4);
-      mbar_init(kdone + i * 8, 4);
+      mbar_init(kdone + i * 8, 2);
       mbar_init(ifull + i * 8, 1);
-      mbar_init(iempty + i * 8, 8 + 8 + 8 + 3);   // softmax, K, V, scales, products
+      mbar_init(iempty + i * 8, 8 + 16 + 3);   // softmax, codes, scales, products
     }
     for (int i = 0; i < 64; ++i) misc_s[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -550,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int c = rb * kM + (r & (C::kRows - 1)), j = c / p.G, hq = h * p.G + (c - j * p.G);
       const Halves hv(u0, n, len);
       const bool works = rb * kM + ((w4 * 32) & (C::kRows - 1)) < p.cols;
-      bool fresh = true, any = false;   // no reference yet; a half tile of this warpgroup's
+      bool fresh = true, settled = false, any = false;   // no reference yet; none of the warp's rows without; a half tile of this warpgroup's
       float ref = 0.0f, l = 0.0f;
 #pragma unroll 1
       for (int u = (gs & 1) ^ g; u < hv.n; u += 2) {
@@ -571,70 +572,78 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           const int e = misc[33 + 2 * (t & 7)];
           const uint32_t tm_s = tmem0 + C::kTmS + s.i * 64 + lanes;
           const uint64_t a2 = f2_pack(a, a);
-          const bool masked = tree || valid < C::kW;
-          uint32_t w[C::kW / 2];
-          // scores of a chunk, less `shift`, in units of a weight's exponent
-          auto scores = [&](float* x, int ch, float shift) {
-            const uint64_t b2 = f2_pack(shift, shift);
+          const float shift = (float)e - ref;
+          // N scores from position `at` on, in units of a weight's exponent; the weights of scores, and their sum
+          auto scores = [&](auto& x, float less) {
+            constexpr int N = sizeof(x) / sizeof(x[0]);
+            const uint64_t b2 = f2_pack(less, less);
 #pragma unroll
-            for (int k = 0; k < kCW / 2; ++k) f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), a2, b2), x[2 * k], x[2 * k + 1]);
-            if (masked) {
-              const int room = valid - ch;
-              uint32_t see = room <= 0 ? 0u : room < 32 ? (1u << room) - 1u : ~0u;
-              if (tree && see) see &= c < p.cols ? (uint32_t)(ld_dep(p.mask + (int64_t)b * p.n + j) >> (t0 + ch)) : 0u;
-#pragma unroll
-              for (int k = 0; k < kCW; ++k)
-                if (!((see >> k) & 1u)) x[k] = -INFINITY;
-            }
+            for (int k = 0; k < N / 2; ++k) f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), a2, b2), x[2 * k], x[2 * k + 1]);
           };
-          auto load = [&](float* x, int ch) {
-#pragma unroll
-            for (int k = 0; k < kCW / 16; ++k) TmemRegs<16>::ld(tm_s + t0 + ch + k * 16, reinterpret_cast<uint32_t*>(x) + 16 * k);
-          };
-          auto weights = [&](const float* x, int ch) {   // and their sum
+          auto weights = [&](const auto& x, uint32_t* w) {
+            constexpr int N = sizeof(x) / sizeof(x[0]);
             uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll
-            for (int k = 0; k < kCW / 2; ++k) {
+            for (int k = 0; k < N / 2; ++k) {
               const float x0 = ex2(x[2 * k]), x1 = ex2(x[2 * k + 1]);
               sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(x0, x1));
-              w[ch / 2 + k] = pack_f16x2(x0, x1);
+              w[k] = pack_f16x2(x0, x1);
             }
             float s0, s1;
             f2_unpack(f2_add(sum2[0], sum2[1]), s0, s1);
             return s0 + s1;
           };
-          float sum;
-          {
+          constexpr int kP = C::kW / 2;                  // columns of a thread's weights, from position ts * kP on
+          const uint32_t tm_p = tm_s + (r / C::kRows) * kP;
+          float sum = 0.0f;
+          bool plain = settled && !tree && valid >= C::kW;
+          if (plain) {
+            uint32_t w[kP];
             float x[kCW], y[kCW];   // (the second chunk is on its way during the first one's exponentials)
-            load(x, 0);
+            tmem_load(tm_s + t0, x);
             tc_wait_ld();
-            if (C::kW > kCW) load(y, kCW);
-            scores(x, 0, (float)e - ref);
-            sum = weights(x, 0);
-            if (C::kW > kCW) {
+            if constexpr (C::kW > kCW) tmem_load(tm_s + t0 + kCW, y);
+            scores(x, shift);
+            sum = weights(x, w);
+            if constexpr (C::kW > kCW) {
               tc_wait_ld();
-              scores(y, kCW, (float)e - ref);
-              sum += weights(y, kCW);
+              scores(y, shift);
+              sum += weights(y, w + kCW / 2);
+            }
+            plain = !__any_sync(0xFFFFFFFFu, !(sum <= kMost));
+            if (plain) {
+#pragma unroll
+              for (int i = 0; i < kP; i += 8) TmemRegs<8>::st(tm_p + i, w + i);
             }
           }
-          if (__any_sync(0xFFFFFFFFu, fresh || !(sum <= kMost))) {
-            // no reference yet, or weights that FP16 might not hold: a reference from the largest score, what the piece has so far is scaled
-            // (scores and weights once more: this is rare)
-            float x[kCW], mx = -INFINITY;
-#pragma unroll
-            for (int ch = 0; ch < C::kW; ch += kCW) {
-              load(x, ch);
+          if (__builtin_expect(!plain, 0)) {
+            // A mask, no reference yet, or weights that FP16 might not hold: 16 scores at a time, first their largest; with a new reference
+            // what the piece has so far is scaled.
+            const unsigned long long see = tree ? (c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) >> t0 : 0ull) : ~0ull;
+            auto chunk = [&](float (&x)[16], int ch, float less) {
+              tmem_load(tm_s + t0 + ch, x);
               tc_wait_ld();
-              scores(x, ch, (float)e - ref);
+              scores(x, less);
+              const int room = valid - ch;
+              uint32_t bits = (uint32_t)(see >> ch) & (room >= 16 ? 0xFFFFu : room > 0 ? (1u << room) - 1u : 0u);
 #pragma unroll
-              for (int k = 0; k < kCW; ++k) mx = fmaxf(mx, x[k]);
+              for (int k = 0; k < 16; ++k, bits >>= 1)
+                if (!(bits & 1u)) x[k] = -INFINITY;
+            };
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (int ch = 0; ch < C::kW; ch += 16) {
+              float x[16];
+              chunk(x, ch, shift);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) mx = fmaxf(mx, x[k]);
             }
-            const bool need = fresh ? mx > -INFINITY : !(sum <= kMost);
+            const bool need = fresh ? mx > -INFINITY : mx > kRaise;
             const float delta = need ? mx - kTop : 0.0f, f = fresh ? 1.0f : ex2(-delta);
             if (need) { ref += delta; fresh = false; }
-            l *= f;
-            if (any) {
-              const Slot prev = s.before(2);
+            if (__any_sync(0xFFFFFFFFu, f != 1.0f)) {
+              l *= f;
+              const Slot prev = s.before(2);   // (a row that has a reference has had a half tile)
               wait(pvdone + prev.i * 8, prev.ph, ab);
               tc_fence_after();
 #pragma unroll 1
@@ -647,27 +656,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
                 TmemRegs<8>::st(tm_o + i, o);
               }
             }
+            settled = !__any_sync(0xFFFFFFFFu, fresh);
             sum = 0.0f;
-#pragma unroll
-            for (int ch = 0; ch < C::kW; ch += kCW) {
-              load(x, ch);
-              tc_wait_ld();
-              scores(x, ch, (float)e - ref);
-              sum += weights(x, ch);
+#pragma unroll 1
+            for (int ch = 0; ch < C::kW; ch += 16) {
+              float x[16];
+              uint32_t w[8];
+              chunk(x, ch, shift - delta);
+              sum += weights(x, w);
+              TmemRegs<8>::st(tm_p + ch / 2, w);   // (over scores that have been read)
             }
           }
-          // (over the scores; the lanes' other parts of the tile have no weight)
-          if constexpr (TS == 1) {
-            TmemRegs<16>::st(tm_s, w);
-            TmemRegs<16>::st(tm_s + 16, w + 16);
-          } else {
+          if constexpr (TS > 1) {   // (the lanes' other parts of the tile have no weight)
+            uint32_t z[8] = {};
 #pragma unroll
-            for (int i = 0; i < TS; ++i) {
-              uint32_t z[C::kW / 2];
-#pragma unroll
-              for (int k = 0; k < C::kW / 2; ++k) z[k] = i == r / C::kRows ? w[k] : 0u;
-              TmemRegs<C::kW / 2>::st(tm_s + i * (C::kW / 2), z);
-            }
+            for (int i = 0; i < 32; i += 8)
+              if (i / kP != r / C::kRows) TmemRegs<8>::st(tm_s + i, z);
           }
           l = fmaf(sum, pow2(-e), l);
           tc_wait_st();
@@ -752,10 +756,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     if (tid == 0 && (misc[0] || misc[1])) atomicOr(p.flags, kFlagTimeout);
     return;
   }
-  // ================================================================================== K tile and queries
-  if (warp < 16) {
+  // ================================================================================== codes to FP16, and queries
+  if (warp < 24) {
     reg_dec<C::kRegExp>();
-    const int kt = (tid - 256) & 127, side = (warp >> 2) & 1;   // (the second warpgroup has the tile's second half and no more)
+    const bool values = (warp & 2) != 0;
+    const int w8 = ((warp - 8) >> 2) * 2 + (warp & 1), row = w8 * 32 + lane, qr = tid - 256;
+    const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty;
+    const int ring = values ? C::kRingV : C::kRingK, stages = values ? C::kOffRV : C::kOffRK, tiles = values ? C::kOffV : C::kOffK,
+              metas = values ? C::kOffVm : C::kOffKm;
     int gt = 0, slot = 0;
     uint32_t phase = 0;
     Slot ms;          // of tile gt among kSlots
@@ -766,8 +774,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
-      if (side == 0) {   // queries: a thread a row, all rows scaled by one power of two, the largest below 2^7 (their sums below 2^14)
-        const int c = rb * kM + (kt & (C::kRows - 1)), j = c / p.G;
+      if (warp < 12) {   // queries: a thread a row, all rows scaled by one power of two, the largest below 2^7 (their sums below 2^14)
+        const int c = rb * kM + (qr & (C::kRows - 1)), j = c / p.G;
         const uint4* src = p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (c - j * p.G)) * 16;
         const bool in = c < p.cols;
         float amax = 0.0f, sum = 0.0f;
@@ -777,13 +785,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
         const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
         if (lane == 0) misc[16 + 4 * qi + (warp & 3)] = (int)wmax;
-        named_bar(8, 128);
+        named_bar(1, 128);
         volatile int* qm = misc + 16 + 4 * qi;
         const int top = max(max(qm[0], qm[1]), max(qm[2], qm[3]));
         const int e = top > 0 ? max(-100, min(100, exponent_of(__int_as_float(top)) + 8)) : 0;
         const float f = pow2(-e);
         a = p.sm_log2 * pow2(e);
-        if (kt == 0) misc[28 + qi] = __float_as_int(a);
+        if (qr == 0) misc[28 + qi] = __float_as_int(a);
         if (gt > 0) wait(kfree + ms.before(1).i * 8, ms.before(1).ph, ab);   // the previous piece's last Q K^T
         tc_fence_after();
         const uint32_t tm_q = tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16);
@@ -801,146 +809,86 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           TmemRegs<16>::st(tm_q + ch * 4, w);
         }
         const uint32_t both = two_parts(sum * f);   // against a token's {mid hi, mid lo, mid hi}: sum hi, sum hi, sum lo
-        sts128(sbase + C::kOffSum + (uint32_t)kt * 16u, __byte_perm(both, both, 0x1010), both >> 16, 0u, 0u);
+        sts128(sbase + C::kOffSum + (uint32_t)qr * 16u, __byte_perm(both, both, 0x1010), both >> 16, 0u, 0u);
         tc_wait_st();
+        proxy_fence();
+        tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(qready + qi * 8);
       }
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gt, ms.next()) {
         const int ut = u0 + u, g = gt & 1;
-        const uint32_t tile = sbase + C::kOffK + (uint32_t)g * 32768u;
+        const uint32_t tile = sbase + (uint32_t)(tiles + g * 32768);
         wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);
-        if (gt > 1) wait(kfree + ms.before(2).i * 8, ms.before(2).ph, ab);   // the tile has been used
+        if (values) wait(vfree + g * 8, ((gt >> 1) - 1) & 1, ab);                        // the tile has been used
+        else if (gt > 1) wait(kfree + ms.before(2).i * 8, ms.before(2).ph, ab);
         if (ut < n_prefix) {
-          wait(kfull + slot * 8, phase, ab);
-          if (len - ut * kTile > kHalf * side)
-            expand<FULL, false>(sbase + C::kOffRK + (uint32_t)slot * C::kStage, tile, sbase + C::kOffKm + (uint32_t)ms.i * 512u, kt, kHalf * side);
+          const int rounds = len - ut * kTile > kHalf ? 2 : 1;
+          const uint32_t raw = sbase + (uint32_t)(stages + slot * C::kStage), meta = sbase + (uint32_t)(metas + ms.i * 512);
+          wait(full + slot * 8, phase, ab);
+          if (values) expand<FULL, true>(raw, tile, meta, w8, lane, rounds);
+          else expand<FULL, false>(raw, tile, meta, w8, lane, rounds);
           __syncwarp();
-          if (lane == 0) mbar_arrive(kempty + slot * 8);
-          if (++slot == C::kRingK) { slot = 0; phase ^= 1; }
-        } else if (side == 0) {   // the nodes' keys: a thread a row, scaled by a power of two
-          const uint4* src = p.kt + ((int64_t)b * p.n + kt) * p.kt_stride + h * 16;
-          const bool used = node_used(p, b, kt, lane);
+          if (lane == 0) mbar_arrive(empty + slot * 8);
+          if (++slot == ring) { slot = 0; phase ^= 1; }
+        } else if (w8 < 2) {   // the nodes' keys or values: a thread a row, all scaled by one power of two
+          const uint4* src = (values ? p.vt + ((int64_t)b * p.n + row) * p.vt_stride : p.kt + ((int64_t)b * p.n + row) * p.kt_stride) + h * 16;
+          const bool used = node_used(p, b, row, lane);
           float amax = 0.0f;
           if (used) {
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
           }
           const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
-          if (lane == 0) misc[12 + (warp & 3)] = (int)wmax;
-          named_bar(8, 128);
-          const int e = tile_exponent(max(max(misc[12], misc[13]), max(misc[14], misc[15])));
-          named_bar(8, 128);   // (read by all)
-          if (kt == 0) misc[32 + 2 * (gt & 7)] = __float_as_int(times_pow2(a, e));
-          if (kt < kMaxNodes) {
-#pragma unroll 4
-            for (int ch = 0; ch < 16; ++ch) {
-              const uint4 w = used ? scaled8(ld_dep(src + ch), pow2(-e)) : make_uint4(0u, 0u, 0u, 0u);
-              sts128(chunk_at(tile, kt, ch), w.x, w.y, w.z, w.w);
-            }
+          volatile int* most = misc + 8 + 2 * (values ? 1 : 0);
+          if (lane == 0) most[w8] = (int)wmax;
+          named_bar(values ? 3 : 8, 64);
+          const int e = tile_exponent(max(most[0], most[1]));
+          named_bar(values ? 3 : 8, 64);   // (read by both)
+          if (row == 0) {
+            if (values) misc[33 + 2 * (gt & 7)] = e;
+            else misc[32 + 2 * (gt & 7)] = __float_as_int(times_pow2(a, e));
           }
-          if (kt < kMaxNodes) sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + kt * 16), 0u, 0u, 0u, 0u);
+#pragma unroll 2
+          for (int ch = 0; ch < 16; ++ch) {
+            const uint4 w = used ? scaled8(ld_dep(src + ch), pow2(-e)) : make_uint4(0u, 0u, 0u, 0u);
+            sts128(chunk_at(tile, row, ch), w.x, w.y, w.z, w.w);
+          }
+          if (!values) sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + row * 16), 0u, 0u, 0u, 0u);
         }
-        proxy_fence();
-        tc_fence_before();   // (the queries)
+        proxy_fence();   // (for the middles, too, which warp 27 has written)
         __syncwarp();
-        if (lane == 0) mbar_arrive(kready + g * 8);
+        if (lane == 0) mbar_arrive(values ? vready + ms.i * 8 : kready + g * 8);
       }
       if (lane == 0) {
-        if (side == 0) mbar_arrive(kdone + qi * 8);
+        if (!values && w8 < 2) mbar_arrive(kdone + qi * 8);
         mbar_arrive(iempty + qi * 8);
       }
     }
     return;
   }
-  // ================================================================================== V tiles
-  if (warp < 24) {
-    reg_dec<C::kRegExp>();
-    const int vt = (tid - 512) & 127, w4 = warp & 3, side = (warp >> 2) & 1;
-    int gt = 0, slot = 0;
-    uint32_t phase = 0;
-    Slot ms;
-    for (int ic = 0;; ++ic) {
-      const int qi = ic & 1;
-      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
-      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h;
-      if (n == 0) break;
-      const int n_prefix = (len + kTile - 1) / kTile;
-#pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt, ms.next()) {
-        const int ut = u0 + u, g = gt & 1;
-        const uint32_t tile = sbase + C::kOffV + (uint32_t)g * 32768u;
-        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);
-        wait(vfree + g * 8, ((gt >> 1) - 1) & 1, ab);           // the tile has been used
-        if (ut < n_prefix) {
-          wait(vfull + slot * 8, phase, ab);
-          if (len - ut * kTile > kHalf * side)
-            expand<FULL, true>(sbase + C::kOffRV + (uint32_t)slot * C::kStage, tile, sbase + C::kOffVm + (uint32_t)ms.i * 512u, vt, kHalf * side);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(vempty + slot * 8);
-          if (++slot == C::kRingV) { slot = 0; phase ^= 1; }
-        } else if (side == 0) {
-          const bool used = node_used(p, b, vt, lane);
-          const uint4* src = p.vt + ((int64_t)b * p.n + vt) * p.vt_stride + h * 16;
-          float amax = 0.0f;
-          if (used) {
-#pragma unroll 4
-            for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
-          }
-          const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
-          if (lane == 0) misc[8 + w4] = (int)wmax;
-          named_bar(3, 128);
-          const int e = tile_exponent(max(max(misc[8], misc[9]), max(misc[10], misc[11])));
-          named_bar(3, 128);   // (read by all)
-          if (vt == 0) misc[33 + 2 * (gt & 7)] = e;
-          if (vt < ((p.n + 15) & ~15)) {
-#pragma unroll 4
-            for (int ch = 0; ch < 16; ++ch) {
-              const uint4 w = used ? scaled8(ld_dep(src + ch), pow2(-e)) : make_uint4(0u, 0u, 0u, 0u);
-              sts128(chunk_at(tile, vt, ch), w.x, w.y, w.z, w.w);
-            }
-          }
-        }
-        proxy_fence();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(vready + ms.i * 8);
-      }
-      if (lane == 0) mbar_arrive(iempty + qi * 8);
-    }
-    return;
-  }
   reg_dec<C::kRegRest>();
   // ================================================================================== copies
-  if (warp < 26) {
-    const bool values = warp == 25;
-    const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty;
-    const int ring = values ? C::kRingV : C::kRingK, stages = values ? C::kOffRV : C::kOffRK;
-    Cursor cur = {0, 0, 0, 0, 0, 0};
-    if (!values) cur = first_unit(p, blockIdx.x, gridDim.x, lane);
-    int slot = 0;
-    uint32_t phase = 1;   // (an empty ring)
+  if (warp == 24) {
+    Cursor cur = first_unit(p, blockIdx.x, gridDim.x, lane);
+    int kslot = 0, vslot = 0;
+    uint32_t kphase = 1, vphase = 1;   // (empty rings)
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
-      Item it;
-      if (!values) {
-        it = next_piece(p, cur, blockIdx.x);
-        wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
-        if (lane == 0) {
-          volatile Item* d = items + qi;
-          d->b = it.b; d->h = it.h; d->rb = it.rb; d->len = it.len;
-          d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib;
-          mbar_arrive(ifull + qi * 8);
-        }
-        __syncwarp();
-      } else {
-        wait(ifull + qi * 8, (ic >> 1) & 1, iab);
-        it.n = items[qi].n; it.len = items[qi].len; it.u0 = items[qi].u0; it.b = items[qi].b; it.h = items[qi].h;
+      const Item it = next_piece(p, cur, blockIdx.x);
+      wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
+      if (lane == 0) {
+        volatile Item* d = items + qi;
+        d->b = it.b; d->h = it.h; d->rb = it.rb; d->len = it.len;
+        d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib;
+        mbar_arrive(ifull + qi * 8);
       }
+      __syncwarp();
       if (it.n == 0) break;
-      // lane i < 8 knows sub-block i's row (those behind the sequence's end: its last one's), four lanes gather: Anchor or Residual, sub-blocks
-      // 0..3 or 4..7
+      // lane i < 8 knows sub-block i's row (those behind the sequence's end: its last one's); lanes 0..3 gather keys, 4..7 values: Anchor or
+      // Residual, sub-blocks 0..3 or 4..7
       const int last = min(it.u0 + it.n, (it.len + kTile - 1) / kTile);
       int t = it.u0 * kTile + (lane & 7) * 16, id = it.u0 < last ? block_id(p, it.b, min(t, it.len - 1)) : 0;
 #pragma unroll 1
@@ -951,21 +899,29 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
 #pragma unroll
         for (int i = 0; i < 4; ++i) r[i] = __shfl_sync(0xFFFFFFFFu, row, (lane & 1) * 4 + i);
         const int groups = it.len - ut * kTile > kHalf ? 2 : 1;
-        wait(empty + slot * 8, phase, ab);
-        if (lane == 0) mbar_expect_tx(full + slot * 8, (uint32_t)groups * (FULL ? 8192u : 4096u));
+        const uint32_t bytes = (uint32_t)groups * (FULL ? 8192u : 4096u), at = (uint32_t)(((lane >> 1) & 1) * 8192 + (lane & 1) * 4096);
+        const bool mine = (lane & 1) < groups && (FULL || !(lane & 2));
+        wait(kempty + kslot * 8, kphase, ab);
+        if (lane == 0) mbar_expect_tx(kfull + kslot * 8, bytes);
         __syncwarp();
-        if (lane < (FULL ? 4 : 2) && (lane & 1) < groups)
-          gather4(sbase + (uint32_t)(stages + slot * C::kStage + (lane >> 1) * 8192 + (lane & 1) * 4096), &maps.m[(values ? 2 : 0) + (lane >> 1)], r[0], r[1],
-                  r[2], r[3], full + slot * 8);
-        if (++slot == ring) { slot = 0; phase ^= 1; }
+        if (lane < 4 && mine) gather4(sbase + (uint32_t)(C::kOffRK + kslot * C::kStage) + at, &maps.m[lane >> 1], r[0], r[1], r[2], r[3], kfull + kslot * 8);
+        wait(vempty + vslot * 8, vphase, ab);
+        if (lane == 0) mbar_expect_tx(vfull + vslot * 8, bytes);
+        __syncwarp();
+        if (lane >= 4 && lane < 8 && mine)
+          gather4(sbase + (uint32_t)(C::kOffRV + vslot * C::kStage) + at, &maps.m[lane >> 1], r[0], r[1], r[2], r[3], vfull + vslot * 8);
+        if (++kslot == C::kRingK) { kslot = 0; kphase ^= 1; }
+        if (++vslot == C::kRingV) { vslot = 0; vphase ^= 1; }
       }
-      if (values && lane == 0) mbar_arrive(iempty + qi * 8);
     }
     bar_arrive(2, kDoneThreads);
     return;
   }
   // ================================================================================== scales and zero points
-  if (warp == 27) {
+  if (warp != 26) {
+    const bool values = warp == 25;
+    const float2* meta = values ? p.vm : p.km;
+    const uint32_t used = values ? vready : kfree;
     int gt = 0;
     Slot ms;
 #pragma unroll 1
@@ -974,93 +930,75 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h;
       if (n == 0) break;
-      wait(qready + qi * 8, (ic >> 1) & 1, ab);
-      const float a = __int_as_float(misc[28 + qi]);
       // a lane takes four tokens, {scale, zero} each, a tile ahead, and their block, two.  (Behind the sequence's end its last four again: a load
       // under a condition is waited for where the condition ends.)
       const int n_prefix = (len + kTile - 1) / kTile, top = (len - 1) & ~3;
-      const bool any = u0 < n_prefix;
-      uint4 x[2][2] = {};   // of keys, of values
+      uint4 x[2] = {};
       int id = 0;
       auto fetch = [&](int t, int blk) {
-        const size_t row = row_at(p, blk, h, t);
-        const uint4 *k = reinterpret_cast<const uint4*>(p.km + row), *v = reinterpret_cast<const uint4*>(p.vm + row);
-        x[0][0] = ld_dep(k);
-        x[0][1] = ld_dep(k + 1);
-        x[1][0] = ld_dep(v);
-        x[1][1] = ld_dep(v + 1);
+        const uint4* src = reinterpret_cast<const uint4*>(meta + row_at(p, blk, h, t));
+        x[0] = ld_dep(src);
+        x[1] = ld_dep(src + 1);
       };
-      if (any) {
-        const int t = u0 * kTile + lane * 4;
-        const int first = block_id(p, b, min(t, top));
+      if (u0 < n_prefix) {
+        const int t = u0 * kTile + lane * 4, first = block_id(p, b, min(t, top));
         id = block_id(p, b, min(t + kTile, top));
         fetch(min(t, top), first);
+      }
+      float a = 0.0f;
+      if (!values) {
+        wait(qready + qi * 8, (ic >> 1) & 1, ab);
+        a = __int_as_float(misc[28 + qi]);
       }
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gt, ms.next()) {
         const int ut = u0 + u;
+        // (The nodes' are made by the warps that have their keys and values.  These wait for this one all the same, so that no barrier is a phase
+        // further than what a wait for it expects.)
+        if (gt >= kSlots) wait(used + ms.i * 8, ms.ph ^ 1u, ab);   // the place has been read (the softmax's of eight tiles before, too)
         if (ut < n_prefix) {
-          const int t = ut * kTile + lane * 4, room = len - t;   // (what lies behind the sequence's end may be anything)
-          float sc[2][4], mid[2][4], big[2] = {0.0f, 0.0f};
+          const int t = ut * kTile + lane * 4, room = len - t;     // (what lies behind the sequence's end may be anything)
+          const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+          float sc[4], mid[4], big = 0.0f;
 #pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const uint32_t w[8] = {x[v][0].x, x[v][0].y, x[v][0].z, x[v][0].w, x[v][1].x, x[v][1].y, x[v][1].z, x[v][1].w};
+          for (int i = 0; i < 4; ++i) {
+            sc[i] = room > i ? __uint_as_float(w[2 * i]) : 0.0f;
+            mid[i] = room > i ? fmaf(128.0f, sc[i], __uint_as_float(w[2 * i + 1])) : 0.0f;
+            big = fmaxf(big, fabsf(mid[i]) + 128.0f * fabsf(sc[i]));
+          }
+          fetch(min(t + kTile, top), id);
+          id = block_id(p, b, min(t + 2 * kTile, top));
+          const int e = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big))) + (values ? 0 : 3);   // (1152 scales below 2^15.2)
+          const float f = pow2(-e);
+          uint32_t o[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              sc[v][i] = room > i ? __uint_as_float(w[2 * i]) : 0.0f;
-              mid[v][i] = room > i ? fmaf(128.0f, sc[v][i], __uint_as_float(w[2 * i + 1])) : 0.0f;
-              big[v] = fmaxf(big[v], fabsf(mid[v][i]) + 128.0f * fabsf(sc[v][i]));
+          for (int i = 0; i < 4; ++i) {
+            sc[i] *= f;
+            mid[i] *= f;
+          }
+          if (values) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = pack_f16x2(sc[i], mid[i]);
+          } else {   // what rounding -1152 scale adds to all of a row is taken off its middle, which goes in two parts
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+              const uint32_t s2 = pack_f16x2(sc[i], sc[i + 1]), m2 = mul_f16x2(s2, 0xE480E480u);
+              o[i] = __byte_perm(s2, m2, 0x5410);
+              o[i + 1] = __byte_perm(s2, m2, 0x7632);
+              const float2 s16 = half2_to_float2(s2), m16 = half2_to_float2(m2);
+              const float x0 = mid[i] - fmaf(1152.0f, s16.x, m16.x), x1 = mid[i + 1] - fmaf(1152.0f, s16.y, m16.y);
+              const uint32_t hi = pack_f16x2(x0, x1);
+              const float2 h2 = half2_to_float2(hi);
+              const uint32_t lo = pack_f16x2(x0 - h2.x, x1 - h2.y), at = sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + lane * 64 + i * 16);
+              sts128(at, __byte_perm(hi, lo, 0x5410), hi & 0xFFFFu, 0u, 0u);
+              sts128(at + 16u, __byte_perm(hi, lo, 0x7632), hi >> 16, 0u, 0u);
             }
           }
-          const int ek = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big[0]))) + 3;   // (1152 scales below 2^15.2)
-          const int ev = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big[1])));
-          const float fk = pow2(-ek), fv = pow2(-ev);
-          // keys: what rounding -1152 scale adds to all of a row is taken off its middle, which goes in two parts
-          uint32_t km[4], mids[4][2], vm[4];
-#pragma unroll
-          for (int i = 0; i < 4; i += 2) {
-            const uint32_t s2 = pack_f16x2(sc[0][i] * fk, sc[0][i + 1] * fk), m2 = mul_f16x2(s2, 0xE480E480u);
-            km[i] = __byte_perm(s2, m2, 0x5410);
-            km[i + 1] = __byte_perm(s2, m2, 0x7632);
-            const float2 s16 = half2_to_float2(s2), m16 = half2_to_float2(m2);
-            const float x0 = mid[0][i] * fk - fmaf(1152.0f, s16.x, m16.x), x1 = mid[0][i + 1] * fk - fmaf(1152.0f, s16.y, m16.y);
-            const uint32_t hi = pack_f16x2(x0, x1);
-            const float2 h2 = half2_to_float2(hi);
-            const uint32_t lo = pack_f16x2(x0 - h2.x, x1 - h2.y);
-            mids[i][0] = __byte_perm(hi, lo, 0x5410);
-            mids[i][1] = hi & 0xFFFFu;
-            mids[i + 1][0] = __byte_perm(hi, lo, 0x7632);
-            mids[i + 1][1] = hi >> 16;
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) vm[i] = pack_f16x2(sc[1][i] * fv, mid[1][i] * fv);
-          if (gt >= kSlots) {   // these places have been read (the softmax's of eight tiles before, too)
-            wait(kfree + ms.i * 8, ms.ph ^ 1u, ab);
-            wait(vready + ms.i * 8, ms.ph ^ 1u, ab);
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + lane * 64 + i * 16), mids[i][0], mids[i][1], 0u, 0u);
-          sts128(sbase + C::kOffKm + (uint32_t)(ms.i * 512 + lane * 16), km[0], km[1], km[2], km[3]);
-          sts128(sbase + C::kOffVm + (uint32_t)(ms.i * 512 + lane * 16), vm[0], vm[1], vm[2], vm[3]);
-          if (lane == 0) {
-            misc[32 + 2 * (gt & 7)] = __float_as_int(times_pow2(a, ek));
-            misc[33 + 2 * (gt & 7)] = ev;
-          }
-          proxy_fence();
-        } else {   // the nodes' are made by the warps that have their keys and values.  These wait for this warp all the same, so that no barrier
-                   // is a phase further than what a wait for it expects
-          if (gt >= kSlots) {
-            wait(kfree + ms.i * 8, ms.ph ^ 1u, ab);
-            wait(vready + ms.i * 8, ms.ph ^ 1u, ab);
-          }
+          sts128(sbase + (uint32_t)((values ? C::kOffVm : C::kOffKm) + ms.i * 512 + lane * 16), o[0], o[1], o[2], o[3]);
+          if (lane == 0) misc[(values ? 33 : 32) + 2 * (gt & 7)] = values ? e : __float_as_int(times_pow2(a, e));
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(mready + (gt & 7) * 8);
-        if (ut < n_prefix) {   // (behind the fence, which waits for loads on their way: 1100 cycles a tile in front of it)
-          const int t = (ut + 1) * kTile + lane * 4;
-          fetch(min(t, top), id);
-          id = block_id(p, b, min(t + kTile, top));
-        }
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
@@ -1081,6 +1019,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = __shfl_sync(0xFFFFFFFFu, items[qi].n, 0), len = __shfl_sync(0xFFFFFFFFu, items[qi].len, 0), u0 = __shfl_sync(0xFFFFFFFFu, items[qi].u0, 0);
       if (n == 0) break;
       const Halves hv(u0, n, len);
+      wait(qready + qi * 8, (ic >> 1) & 1, ab);
       const int node_steps = (p.n + 15) / 16, end_steps = (min(len - u0 * kTile - (hv.prefix - 1) * kHalf, kHalf) + 15) / 16;   // of 16 tokens
       // (Not ahead into the next piece: its queries wait for this one's last scores, and a piece is dealt out when the one before the last
       // has been left.)
@@ -1088,7 +1027,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       auto qk = [&]() {
         const bool nodes = ahead >= hv.prefix;
         const uint32_t t = (uint32_t)(nodes ? gt + n - 1 : gt + (ahead >> 1)), side = nodes ? 0u : ahead & 1u, tb = (t & 1u) * 8u;
-        if (side == 0) wait(kready + tb, (t >> 1) & 1, ab);   // (and with it the queries; the weights that lay in the scores' place are in front in the pipe)
+        if (side == 0) wait(kready + tb, (t >> 1) & 1, ab);   // (the weights that lay in the scores' place are in front in the pipe)
         tc_fence_after();
         const bool last = side == 1 || ahead >= hv.prefix - 1;
         if (tc_elect()) {

@@ -54,15 +54,15 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
     only arrive together are one here."""
     B = {}
     for name, n, count in (("kfull", ring_k, 1), ("kempty", ring_k, 2), ("vfull", ring_v, 1), ("vempty", ring_v, 2), ("kready", 2, 2), ("sfull", N, 1),
-                           ("mready", 8, 1), ("vready", N, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", N, 1), ("vfree", 2, 1),
-                           ("ifull", 2, 1), ("iempty", 2, 2 * softmax + 7), ("qready", 2, 1), ("kdone", 2, 1)):
+                           ("mready", 8, 2), ("vready", N, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", N, 1), ("vfree", 2, 1),
+                           ("ifull", 2, 1), ("iempty", 2, 2 * softmax + 7), ("qready", 2, 2), ("kdone", 2, 1)):
         B[name] = [Barrier(count) for _ in range(n)]
     rawk, rawv = [Place(f"raw K {i}") for i in range(ring_k)], [Place(f"raw V {i}") for i in range(ring_v)]
     S = [Place(f"S {i}") for i in range(N)]
     vm, km, mids = ([Place(f"{x} {i}") for i in range(N)] for x in ("vm", "km", "mid"))
     ktile, vtile = ([[Place(f"{x} {i} {j}") for j in range(2)] for i in range(2)] for x in ("K", "V"))
     factor, exp = ([Place(f"{x} {i}") for i in range(8)] for x in ("a", "e"))
-    item, O, Q = [Place("item 0"), Place("item 1")], [Place("O 0"), Place("O 1")], Place("Q")
+    item, O, Q = [Place("item 0"), Place("item 1")], [Place("O 0"), Place("O 1")], [Place("Q 0"), Place("Q 1")]
     pair = [[0, 0] for _ in range(softmax)]         # arrivals of a row's two warps at the barriers at the end of a piece
     issued = []        # products, in order, completed in order
 
@@ -79,28 +79,26 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
     def raw_tiles(n, tree):
         return n - 1 if tree else n
 
-    def copies(values):
-        full, empty, ring, raw = ("vfull", "vempty", ring_v, rawv) if values else ("kfull", "kempty", ring_k, rawk)
-        slot, phase, gt = 0, 1, 0
+    def copies():
+        ks, vs, kp, vp, gt = 0, 0, 1, 1, 0
         for ic in range(len(pieces) + 1):
-            if values:
-                n, tree, _ = yield from get(ic)
-            else:
-                yield from wait("iempty", ic & 1, (ic >> 1) - 1)
-                item[ic & 1].write(ic)
-                B["ifull"][ic & 1].arrive()
-                n, tree, _ = pieces[ic] if ic < len(pieces) else (0, False, False)
+            yield from wait("iempty", ic & 1, (ic >> 1) - 1)
+            item[ic & 1].write(ic)
+            B["ifull"][ic & 1].arrive()
+            n, tree, _ = pieces[ic] if ic < len(pieces) else (0, False, False)
             if n == 0:
                 return
             for _ in range(raw_tiles(n, tree)):
-                yield from wait(empty, slot, phase)
-                raw[slot].write(gt)
-                B[full][slot].arrive()
+                yield from wait("kempty", ks, kp)
+                rawk[ks].write(gt)
+                B["kfull"][ks].arrive()
+                yield from wait("vempty", vs, vp)
+                rawv[vs].write(gt)
+                B["vfull"][vs].arrive()
                 gt += 1
-                slot, phase = (0, phase ^ 1) if slot + 1 == ring else (slot + 1, phase)
+                ks, kp = (0, kp ^ 1) if ks + 1 == ring_k else (ks + 1, kp)
+                vs, vp = (0, vp ^ 1) if vs + 1 == ring_v else (vs + 1, vp)
             gt += tree
-            if values:
-                B["iempty"][ic & 1].arrive()
 
     def k_tiles(side):
         gt = slot = phase = 0
@@ -111,7 +109,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             if side == 0:
                 if gt > 0:
                     yield from wait("kfree", (gt - 1) % N, (gt - 1) // N)
-                Q.write(ic)
+                Q[0].write(ic)
                 B["qready"][ic & 1].arrive()
             for u in range(n):
                 g = gt & 1
@@ -144,6 +142,11 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             n, tree, short = yield from get(ic)
             if n == 0:
                 return
+            if side == 0:                   # (half of the queries' rows)
+                if gt > 0:
+                    yield from wait("kfree", (gt - 1) % N, (gt - 1) // N)
+                Q[1].write(ic)
+                B["qready"][ic & 1].arrive()
             for u in range(n):
                 g = gt & 1
                 yield from wait("mready", gt & 7, gt >> 3)
@@ -165,19 +168,19 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 gt += 1
             B["iempty"][ic & 1].arrive()
 
-    def scales():
+    def scales(values):
         gt = 0
         for ic in range(len(pieces) + 1):
             n, tree, _ = yield from get(ic)
             if n == 0:
                 return
-            yield from wait("qready", ic & 1, ic >> 1)
+            if not values:
+                yield from wait("qready", ic & 1, ic >> 1)
             for u in range(n):
                 if gt >= N:
-                    yield from wait("kfree", gt % N, gt // N - 1)
-                    yield from wait("vready", gt % N, gt // N - 1)
+                    yield from wait("vready" if values else "kfree", gt % N, gt // N - 1)
                 if u < raw_tiles(n, tree):
-                    for x in (vm[gt % N], exp[gt & 7], km[gt % N], mids[gt % N], factor[gt & 7]):
+                    for x in (vm[gt % N], exp[gt & 7]) if values else (km[gt % N], mids[gt % N], factor[gt & 7]):
                         x.write(gt)
                 B["mready"][gt & 7].arrive()
                 gt += 1
@@ -192,7 +195,8 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             t += gt
             if first:
                 yield from wait("kready", t & 1, t >> 1)
-            Q.readers += 1
+            for x in Q:
+                x.readers += 1
             ktile[t & 1][not first].readers += 1
             mids[t % N].readers += 1
             issued.append(("qk", ahead, ic, t, first, last, False))
@@ -204,6 +208,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 return
             halves = _halves(n, tree, short)
             start = gs
+            yield from wait("qready", ic & 1, ic >> 1)
             while ahead - start < min(len(halves), N):
                 yield from qk(ic, halves[ahead - start])
             for u, (t, first, last) in enumerate(halves):
@@ -232,11 +237,12 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             yield
             issued.pop(0)
             if kind == "qk":
-                Q.read(ic)
+                for x in Q:
+                    x.read(ic)
+                    x.readers -= 1
                 ktile[t & 1][not first].read(t)
                 mids[t % N].read(t)
                 mids[t % N].readers -= 1
-                Q.readers -= 1
                 ktile[t & 1][not first].readers -= 1
                 B["sfull"][gs % N].arrive()
                 if last:
@@ -298,7 +304,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                 yield
             B["iempty"][ic & 1].arrive()
 
-    roles = [copies(False), copies(True), k_tiles(0), k_tiles(1), v_tiles(0), v_tiles(1), scales(), products()] + [softmax_warp(g, w) for g in range(2) for w in range(softmax)]
+    roles = [copies(), k_tiles(0), k_tiles(1), v_tiles(0), v_tiles(1), scales(False), scales(True), products()] + [softmax_warp(g, w) for g in range(2) for w in range(softmax)]
     core = tensor_core()
     speed = [rng.choice([1, 1, 1, 3, 30, 200]) for _ in roles]
     core_speed, idle = rng.choice([1, 3, 30]), 0
@@ -331,11 +337,10 @@ def test_the_kernel_waits_for_what_is_played():
     """The waits of the roles in the source, by barrier."""
     code = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "tree_attention.cu")).read())
     code = code[code.index("tree_attention_kernel("):code.index("tree_combine_kernel(")]
-    cuts = ["if (warp < 8) {", "if (warp < 16) {", "if (warp < 24) {", "if (warp < 26) {", "if (warp == 27) {", "constexpr uint32_t kIdescS"]
+    cuts = ["if (warp < 8) {", "if (warp < 24) {", "if (warp == 24) {", "if (warp != 26) {", "constexpr uint32_t kIdescS"]
     at = [code.index(x) for x in cuts] + [len(code)]
     waits = [sorted(set(re.findall(r"\bwait\((\w+)", code[a:b]))) for a, b in zip(at, at[1:])]
-    assert waits == [["ifull", "kdone", "mready", "pvdone", "sfull", "vready"], ["ifull", "kfree", "kfull", "mready"],
-                     ["ifull", "mready", "vfree", "vfull"], ["empty", "iempty", "ifull"], ["ifull", "kfree", "qready", "vready"],
-                     ["ifull", "kready", "pready", "vready"]]
+    assert waits == [["ifull", "kdone", "mready", "pvdone", "sfull", "vready"], ["full", "ifull", "kfree", "mready", "vfree"],
+                     ["iempty", "kempty", "vempty"], ["ifull", "qready", "used"], ["ifull", "kready", "pready", "qready", "vready"]]
     land, done, free = (code.index(x) for x in ("land_after_abort(", "named_bar(2, kDoneThreads)", "tcgen05.dealloc"))
     assert done < land < free and len(re.findall(r"bar_arrive\(2, kDoneThreads\)", code)) == 2
