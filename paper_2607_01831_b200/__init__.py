@@ -202,6 +202,8 @@ _fast_split_quantize, _fast_recombine = _fast("_fast_split_quantize", "split_qua
 _fast_anchor, _fast_verify = _fast("_fast_anchor", "anchor_attention"), _fast("_fast_verify", "merge_verify_attention")
 _fast_bf16, _fast_lse_view = _fast("_fast_bf16", "bf16_attention"), _fast("_fast_lse_view", "lse_view")
 _fast_lse_merge = _fast("_fast_lse_merge", "lse_merge")
+_fast_rotary, _fast_cache_append = _fast("_fast_rotary", "rotary"), _fast("_fast_cache_append", "cache_append")
+_fast_cache_read, _fast_tree_attention = _fast("_fast_cache_read", "cache_read"), _fast("_fast_tree_attention", "tree_attention")
 _fast_hier_quantize, _fast_hier_dequantize = _fast("_fast_hier_quantize", "hier_quantize"), _fast("_fast_hier_dequantize", "hier_dequantize")
 
 
@@ -538,7 +540,7 @@ def token_verify(p_probs: torch.Tensor, q_probs: torch.Tensor, draft_tokens: tor
 
 
 # ---------------------------------------------------------------------------------------------- around the cache
-@dataclass
+@dataclass(frozen=True)
 class Rotary:
     """Rotary positions: positions i32 [T] or [axes][T], cos_sin f32 [n_positions][2 P] (P cosines, P sines; P = 8, 16, ... 64
     pairs of channels), pair_axis: the axis of each pair (P ints; None: one axis).  Pairs are channels (i, i + P), or
@@ -548,18 +550,24 @@ class Rotary:
     pair_axis: tuple | list | None = None
     interleaved: bool = False
 
-    def _c(self, tokens: int):
+    def __post_init__(self):
         pos, table = self.positions, self.cos_sin
-        if pos.dtype != torch.int32 or pos.dim() not in (1, 2) or pos.shape[-1] < tokens:
+        if pos.dtype != torch.int32 or pos.dim() not in (1, 2):
             raise LynxError("positions must be int32 [tokens] or [axes][tokens]")
         if table.dtype != torch.float32 or table.dim() != 2 or table.shape[1] % 2:
             raise LynxError("cos_sin must be float32 [positions][2 pairs]")
         axes, pairs = 1 if pos.dim() == 1 else pos.shape[0], table.shape[1] // 2
         axis = self.pair_axis if self.pair_axis is not None else [0] * pairs
-        if len(axis) != pairs or pairs > 64 or not all(0 <= a < axes for a in axis):
+        if len(axis) != pairs or pairs > 64 or (pairs and not (min(axis) >= 0 and max(axis) < min(axes, 256))):
             raise LynxError("pair_axis must name one of the positions' axes for each pair, of at most 64")
-        return ctypes.byref(_RotarySpec(_ptr(pos), _ptr(table), pos.shape[-1], axes, table.shape[0], pairs, int(self.interleaved),
-                                        (ctypes.c_uint8 * 64)(*axis)))
+        object.__setattr__(self, "_axis", bytes(axis))
+
+    def _c(self, tokens: int):
+        pos, table = self.positions, self.cos_sin
+        if pos.shape[-1] < tokens:
+            raise LynxError("positions must be int32 [tokens] or [axes][tokens]")
+        return ctypes.byref(_RotarySpec(_ptr(pos), _ptr(table), pos.shape[-1], 1 if pos.dim() == 1 else pos.shape[0], table.shape[0],
+                                        len(self._axis), int(self.interleaved), (ctypes.c_uint8 * 64)(*self._axis)))
 
 
 def rotary_table(n_positions: int, pairs: int = 64, base: float = 10000.0, device=None) -> torch.Tensor:
@@ -585,6 +593,9 @@ def rotary(q: torch.Tensor | None, k: torch.Tensor | None, spec: Rotary, q_out: 
            k_out: torch.Tensor | None = None):
     """lynx_rotary: q BF16 [T][Hq][128], k BF16 [T][Hkv][128] (either may be None; tokens may lie apart) -> (q_out, k_out), which may
     be the inputs."""
+    r = _fast_rotary(q, k, spec, q_out, k_out)
+    if r is not None:
+        return _result(r, "lynx_rotary")
     if q is None and k is None:
         raise LynxError("q or k is needed")
     T = (q if q is not None else k).shape[0]
@@ -616,6 +627,9 @@ def cache_append(geo: Geometry, k: torch.Tensor, v: torch.Tensor, slots: torch.T
     """lynx_cache_append: quantises tokens' keys and values BF16 [T][Hkv][128] (tokens may lie apart) into the planes K and V.  slots
     i64 [n]: block * block_tokens + offset of each token written, negative for none; rows i32 [n]: the source row of each
     (None: row i); rotary: positions for the keys, by source row."""
+    r = _fast_cache_append(geo, k, v, slots, K, V, rows, rotary)
+    if r is not None:
+        return _ok(r, "lynx_cache_append")
     (kp, ks, kh), (vp, vs, vh) = _token_rows(k, "k"), _token_rows(v, "v")
     if kh != geo.num_kv_heads or vh != kh or v.shape[0] != k.shape[0]:
         raise LynxError("k and v must be BF16 [tokens][num_kv_heads][128]")
@@ -631,6 +645,9 @@ def cache_read(geo: Geometry, K: Planes, V: Planes, block_table: torch.Tensor, s
                n_rows: int, anchor_only: bool = False, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None):
     """lynx_cache_read: tokens [starts[b], starts[b] + offsets[b + 1] - offsets[b]) of each sequence (starts i32 [B] or None for 0,
     offsets i32 [B + 1], n_rows = offsets[B]) -> k, v BF16 [n_rows][Hkv][128], from the full codes or from the Anchor alone."""
+    r = _fast_cache_read(geo, K, V, block_table, starts, offsets, n_rows, anchor_only, k_out, v_out)
+    if r is not None:
+        return _result(r, "lynx_cache_read")
     B = block_table.shape[0]
     if block_table.dtype != torch.int32 or tuple(block_table.shape) != (B, geo.max_blocks_per_seq):
         raise LynxError("block_table must be int32 [B][max_blocks_per_seq]")
@@ -685,6 +702,9 @@ def tree_attention(geo: Geometry, q: torch.Tensor, K: Planes, V: Planes, block_t
     """lynx_tree_attention: q BF16 [B][n][Hq][128] of a tree's nodes over the planes' tokens [0, seq_lens[b]) and the nodes i with bit i
     of tree_mask i64 [B][n]; k_nodes, v_nodes BF16 [B][n][Hkv][128] (nodes may lie apart).  -> BF16 [B][n][Hq][128], or what `out`
     (BF16 or float32) is; lse: float32 [B][n][Hq] to be filled.  anchor_only: the Anchor's state of the planes."""
+    r = _fast_tree_attention(geo, q, K, V, block_table, seq_lens, k_nodes, v_nodes, tree_mask, workspace, anchor_only, softmax_scale, out, lse)
+    if r is not None:
+        return _result(r, "lynx_tree_attention")
     if q.dim() != 4 or q.dtype != torch.bfloat16 or q.shape[2:] != (geo.num_q_heads, D):
         raise LynxError("q must be BF16 [B][n][Hq][128]")
     B, n, Hq, _ = q.shape

@@ -12,6 +12,9 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cstring>
+
 #include "lynx.h"
 
 namespace {
@@ -41,6 +44,7 @@ bool float_of(PyObject* o, float* v) {
   *v = (float)PyFloat_AS_DOUBLE(o);
   return true;
 }
+PyObject *s_positions, *s_cos_sin, *s_axis, *s_interleaved;
 PyObject *s_hq, *s_hkv, *s_d, *s_bt, *s_nb, *s_mb, *s_anchor, *s_residual, *s_meta;
 
 bool int_attr(PyObject* o, PyObject* name, int32_t* v) {
@@ -322,9 +326,206 @@ PyObject* hier_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- around the cache: tokens' rows may lie apart
+// BF16 [..][heads][128] of a tensor that is not contiguous as a whole; stride: elements from a token to the next.
+const at::Tensor* rows_of(PyObject* o, int dim, int64_t* stride) {
+  if (!THPVariable_CheckExact(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.defined() || !t.is_cuda() || at::isTensorSubclassLike(t) || t.scalar_type() != at::kBFloat16 || t.dim() != dim || t.size(-1) != kD) return nullptr;
+  const int64_t H = t.size(-2), n = t.size(-3);
+  if (t.numel() == 0 || t.stride(-1) != 1 || (H > 1 && t.stride(-2) != kD)) return nullptr;
+  if (dim == 3) {
+    *stride = n > 1 ? t.stride(0) : H * kD;
+  } else {   // [batch][nodes][heads][128]: one stride for all nodes
+    const int64_t B = t.size(0);
+    if (n > 1 && B > 1 && t.stride(0) != n * t.stride(1)) return nullptr;
+    *stride = n > 1 ? t.stride(1) : B > 1 ? t.stride(0) : H * kD;
+  }
+  return &t;
+}
+const at::Tensor* typed(PyObject* o, at::ScalarType type) {
+  const at::Tensor* t = plain(o);
+  return t && t->scalar_type() == type ? t : nullptr;
+}
+// Planes that hold a geometry's rows.  The objects keep their tensors alive over the call.
+bool planes_fit(PyObject* o, const lynx_shape& s, bool residual, lynx_plane* pl) {
+  const int64_t rows = (int64_t)s.num_blocks * s.num_kv_heads * s.block_tokens;
+  PyObject* names[3] = {s_anchor, s_residual, s_meta};
+  void* p[3] = {nullptr, nullptr, nullptr};
+  for (int i = 0; i < 3; ++i) {
+    PyObject* a = PyObject_GetAttr(o, names[i]);
+    if (!a) { PyErr_Clear(); return false; }
+    const at::Tensor* t = plain(a);
+    const bool ok = (t && t->scalar_type() == (i == 2 ? at::kFloat : at::kByte) && t->numel() >= rows * (i == 2 ? 2 : 64)) ||
+                    (i == 1 && !residual && is_none(a));
+    p[i] = ptr(t);
+    Py_DECREF(a);
+    if (!ok) return false;
+  }
+  *pl = {(const uint8_t*)p[0], residual ? (const uint8_t*)p[1] : nullptr, (const float*)p[2]};
+  return true;
+}
+bool rotary_of(PyObject* o, int64_t tokens, lynx_rotary_spec* r) {
+  PyObject *pos = PyObject_GetAttr(o, s_positions), *table = PyObject_GetAttr(o, s_cos_sin), *axis = PyObject_GetAttr(o, s_axis),
+           *inter = PyObject_GetAttr(o, s_interleaved);
+  bool ok = pos && table && axis && inter;
+  if (ok) {
+    const at::Tensor *p = typed(pos, at::kInt), *t = typed(table, at::kFloat);
+    ok = p && t && (p->dim() == 1 || p->dim() == 2) && p->size(-1) >= tokens && t->dim() == 2 && t->size(1) % 2 == 0 && t->size(1) <= 128 &&
+         t->size(0) <= INT32_MAX && PyBool_Check(inter) && PyBytes_CheckExact(axis) && PyBytes_GET_SIZE(axis) == t->size(1) / 2;
+    if (ok) {
+      r->positions = (const int32_t*)p->data_ptr();
+      r->cos_sin = (const float*)t->data_ptr();
+      r->positions_stride = p->size(-1);
+      r->n_axes = p->dim() == 1 ? 1 : (int32_t)std::min<int64_t>(p->size(0), INT32_MAX);
+      r->n_positions = (int32_t)t->size(0);
+      r->n_pairs = (int32_t)(t->size(1) / 2);
+      r->interleaved = inter == Py_True;
+      memset(r->pair_axis, 0, sizeof(r->pair_axis));
+      memcpy(r->pair_axis, PyBytes_AS_STRING(axis), (size_t)PyBytes_GET_SIZE(axis));
+    }
+  }
+  PyErr_Clear();
+  Py_XDECREF(pos);
+  Py_XDECREF(table);
+  Py_XDECREF(axis);
+  Py_XDECREF(inter);
+  return ok;
+}
+
+// q or None, k or None, spec, q_out or None, k_out or None -> (q_out, k_out)
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 5) Py_RETURN_NONE;
+    const at::Tensor *in[2] = {nullptr, nullptr};
+    at::Tensor out[2];
+    int64_t si[2] = {0, 0}, so[2] = {0, 0}, T = -1;
+    for (int i = 0; i < 2; ++i) {
+      if (is_none(a[i])) continue;
+      in[i] = rows_of(a[i], 3, &si[i]);
+      if (!in[i] || in[i]->size(1) > INT32_MAX || (T >= 0 && in[i]->size(0) != T)) Py_RETURN_NONE;
+      T = in[i]->size(0);
+      if (is_none(a[3 + i])) {
+        out[i] = empty_like_device(in[i]->sizes(), at::kBFloat16, *in[i]);
+        so[i] = in[i]->size(1) * kD;
+      } else {
+        const at::Tensor* o = rows_of(a[3 + i], 3, &so[i]);
+        if (!o || o->sizes() != in[i]->sizes()) Py_RETURN_NONE;
+        out[i] = *o;
+      }
+    }
+    lynx_rotary_spec r;
+    if (T < 0 || !rotary_of(a[2], T, &r)) Py_RETURN_NONE;
+    void* st = stream();
+    const lynx_status rc = unlocked([&] {
+      return lynx_rotary(&r, ptr(in[0]), si[0], in[0] ? (int32_t)in[0]->size(1) : 0, ptr(in[1]), si[1], in[1] ? (int32_t)in[1]->size(1) : 0, T,
+                         out[0].defined() ? out[0].data_ptr() : nullptr, so[0], out[1].defined() ? out[1].data_ptr() : nullptr, so[1], st);
+    });
+    if (rc != LYNX_OK) return status(rc);
+    PyObject* res = PyTuple_New(2);
+    if (!res) return nullptr;
+    for (int i = 0; i < 2; ++i)
+      PyTuple_SET_ITEM(res, i, !in[i] ? Py_NewRef(Py_None) : is_none(a[3 + i]) ? THPVariable_Wrap(out[i]) : Py_NewRef(a[3 + i]));
+    return res;
+  });
+}
+
+// geo, k, v, slots, K, V, rows or None, rotary or None -> status
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    lynx_shape s;
+    lynx_plane K, V;
+    if (n != 8 || !shape_of(a[0], &s)) Py_RETURN_NONE;
+    int64_t sk = 0, sv = 0;
+    const at::Tensor *k = rows_of(a[1], 3, &sk), *v = rows_of(a[2], 3, &sv), *slots = typed(a[3], at::kLong), *rows = typed(a[6], at::kInt);
+    if (!k || !v || !slots || slots->dim() != 1 || (!rows && !is_none(a[6])) || (rows && (rows->dim() != 1 || rows->numel() != slots->numel())) ||
+        k->size(1) != s.num_kv_heads || v->sizes() != k->sizes() || !planes_fit(a[4], s, true, &K) || !planes_fit(a[5], s, true, &V))
+      Py_RETURN_NONE;
+    lynx_rotary_spec r;
+    const bool turn = !is_none(a[7]);
+    if (turn && !rotary_of(a[7], k->size(0), &r)) Py_RETURN_NONE;
+    const lynx_plane_out ko = {const_cast<uint8_t*>(K.anchor), const_cast<uint8_t*>(K.residual), const_cast<float*>(K.meta)},
+                         vo = {const_cast<uint8_t*>(V.anchor), const_cast<uint8_t*>(V.residual), const_cast<float*>(V.meta)};
+    void* st = stream();
+    return status(unlocked([&] {
+      return lynx_cache_append(&s, k->data_ptr(), sk, v->data_ptr(), sv, k->size(0), (const int32_t*)ptr(rows), slots->numel(),
+                               (const int64_t*)slots->data_ptr(), turn ? &r : nullptr, ko, vo, st);
+    }));
+  });
+}
+
+// geo, K, V, block_table, starts or None, offsets, n_rows, anchor_only, k_out or None, v_out or None -> (k, v)
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    lynx_shape s;
+    lynx_plane K, V;
+    int32_t n_rows;
+    if (n != 10 || !shape_of(a[0], &s) || !PyBool_Check(a[7]) || !int_of(a[6], &n_rows) || n_rows < 0) Py_RETURN_NONE;
+    const bool full = a[7] == Py_False;
+    const at::Tensor *table = typed(a[3], at::kInt), *starts = typed(a[4], at::kInt), *offsets = typed(a[5], at::kInt);
+    if (!table || table->dim() != 2 || table->size(1) != s.max_blocks_per_seq || table->size(0) >= INT32_MAX || !offsets || offsets->dim() != 1 ||
+        offsets->numel() != table->size(0) + 1 || (!starts && !is_none(a[4])) || (starts && (starts->dim() != 1 || starts->numel() != table->size(0))) ||
+        !planes_fit(a[1], s, full, &K) || !planes_fit(a[2], s, full, &V))
+      Py_RETURN_NONE;
+    at::Tensor out[2];
+    for (int i = 0; i < 2; ++i) {
+      if (is_none(a[8 + i])) {
+        out[i] = empty_like_device({n_rows, s.num_kv_heads, kD}, at::kBFloat16, *table);
+      } else {
+        const at::Tensor* o = typed(a[8 + i], at::kBFloat16);
+        if (!o || o->dim() != 3 || o->size(0) != n_rows || o->size(1) != s.num_kv_heads || o->size(2) != kD) Py_RETURN_NONE;
+        out[i] = *o;
+      }
+    }
+    void* st = stream();
+    const lynx_status rc = unlocked([&] {
+      return lynx_cache_read(&s, K, V, (const int32_t*)table->data_ptr(), (int32_t)table->size(0), (const int32_t*)ptr(starts),
+                             (const int32_t*)offsets->data_ptr(), n_rows, out[0].data_ptr(), out[1].data_ptr(), st);
+    });
+    if (rc != LYNX_OK) return status(rc);
+    PyObject* res = PyTuple_New(2);
+    if (!res) return nullptr;
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(res, i, is_none(a[8 + i]) ? THPVariable_Wrap(out[i]) : Py_NewRef(a[8 + i]));
+    return res;
+  });
+}
+
+// geo, q, K, V, block_table, seq_lens, k_nodes, v_nodes, tree_mask, workspace, anchor_only, softmax_scale, out or None, lse or None -> out
+PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    lynx_shape s;
+    lynx_plane K, V;
+    float scale;
+    if (n != 14 || !shape_of(a[0], &s) || !PyBool_Check(a[10]) || !float_of(a[11], &scale)) Py_RETURN_NONE;
+    const bool full = a[10] == Py_False;
+    int64_t sk = 0, sv = 0;
+    const at::Tensor *q = plain(a[1]), *table = typed(a[4], at::kInt), *lens = typed(a[5], at::kInt), *k = rows_of(a[6], 4, &sk), *v = rows_of(a[7], 4, &sv),
+                     *mask = typed(a[8], at::kLong), *ws = plain(a[9]), *given = plain(a[12]), *lse = typed(a[13], at::kFloat);
+    if (!queries(q, s) || q->numel() == 0 || !table || !lens || !k || !v || !mask || !ws || (!given && !is_none(a[12])) || (!lse && !is_none(a[13])))
+      Py_RETURN_NONE;
+    const int64_t B = q->size(0), N = q->size(1);
+    if (table->dim() != 2 || table->size(0) != B || table->size(1) != s.max_blocks_per_seq || lens->dim() != 1 || lens->numel() != B ||
+        mask->dim() != 2 || mask->size(0) != B || mask->size(1) != N || k->size(0) != B || k->size(1) != N || k->size(2) != s.num_kv_heads ||
+        v->sizes() != k->sizes() || !planes_fit(a[2], s, full, &K) || !planes_fit(a[3], s, full, &V) ||
+        (given && (given->sizes() != q->sizes() || (given->scalar_type() != at::kBFloat16 && given->scalar_type() != at::kFloat))) ||
+        (lse && (lse->dim() != 3 || lse->size(0) != B || lse->size(1) != N || lse->size(2) != s.num_q_heads)))
+      Py_RETURN_NONE;
+    at::Tensor out = given ? *given : empty_like_device(q->sizes(), at::kBFloat16, *q);
+    void* st = stream();
+    const lynx_status rc = unlocked([&] {
+      return lynx_tree_attention(&s, q->data_ptr(), (int32_t)B, (int32_t)N, K, V, (const int32_t*)table->data_ptr(), (const int32_t*)lens->data_ptr(),
+                                 k->data_ptr(), sk, v->data_ptr(), sv, (const uint64_t*)mask->data_ptr(), scale, out.scalar_type() == at::kFloat,
+                                 out.data_ptr(), (float*)ptr(lse), ws->data_ptr(), (size_t)ws->nbytes(), st);
+    });
+    if (rc != LYNX_OK) return status(rc);
+    return given ? Py_NewRef(a[12]) : THPVariable_Wrap(out);
+  });
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(anchor_attention), FAST(merge_verify_attention), FAST(bf16_attention), FAST(split_quantize), FAST(recombine),
-                         FAST(lse_view), FAST(lse_merge), FAST(hier_quantize), FAST(hier_dequantize), {nullptr, nullptr, 0, nullptr}};
+                         FAST(lse_view), FAST(lse_merge), FAST(hier_quantize), FAST(hier_dequantize),
+                         FAST(rotary), FAST(cache_append), FAST(cache_read), FAST(tree_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -332,7 +533,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nu
 PyMODINIT_FUNC PyInit__native() {
   struct { PyObject** s; const char* n; } names[] = {{&s_hq, "num_q_heads"}, {&s_hkv, "num_kv_heads"}, {&s_d, "head_dim"}, {&s_bt, "block_tokens"},
                                                      {&s_nb, "num_blocks"}, {&s_mb, "max_blocks_per_seq"}, {&s_anchor, "anchor"},
-                                                     {&s_residual, "residual"}, {&s_meta, "meta"}};
+                                                     {&s_residual, "residual"}, {&s_meta, "meta"}, {&s_positions, "positions"}, {&s_cos_sin, "cos_sin"},
+                                                     {&s_axis, "_axis"}, {&s_interleaved, "interleaved"}};
   for (auto& x : names)
     if (!(*x.s = PyUnicode_InternFromString(x.n))) return nullptr;
   PyObject* m = PyModule_Create(&module);

@@ -228,6 +228,30 @@ def test_on_another_stream_and_written_then_read():
         assert np.array_equal(bf16_bits(got), np.asarray(want).view(np.uint16).reshape(got.shape))
 
 
+def test_the_extension_and_the_python_bodies_agree(monkeypatch):
+    T, H, bt, nb = 37, 4, 16, 8
+    spec, _ = _spec(T, 64, 3, seed=5)
+    d = _bf16(T, 8 * H, 128, seed=6).cuda()
+    slots = torch.randperm(nb * bt, generator=_gen(1))[:T].cuda()
+    rows = torch.randint(0, T, (T,), generator=_gen(2), dtype=torch.int32).cuda()
+    geo = lynx.Geometry(H, H, bt, nb, nb)
+    table, offsets = torch.arange(nb, dtype=torch.int32).view(1, -1).cuda(), torch.tensor([0, nb * bt], dtype=torch.int32).cuda()
+
+    def calls():
+        K, V = _pool(nb, H, bt, 0), _pool(nb, H, bt, 0)
+        q, k = lynx.rotary(d[:, :6 * H], d[:, 6 * H:7 * H], spec)
+        own = torch.empty_like(k)
+        assert lynx.rotary(None, k, spec, k_out=own)[1] is own
+        lynx.cache_append(geo, k, d[:, 7 * H:], slots, K, V, rows=rows, rotary=spec)
+        lynx.cache_append(geo, k, d[:, 7 * H:], slots, V, K)
+        return [q, k, own, K.anchor, K.residual, K.meta, V.anchor, *lynx.cache_read(geo, K, V, table, None, offsets, nb * bt),
+                *lynx.cache_read(geo, K, V, table, offsets[:1], offsets, nb * bt, anchor_only=True)]
+    fast = calls()
+    for name in ("_fast_rotary", "_fast_cache_append", "_fast_cache_read"):
+        monkeypatch.setattr(lynx, name, lynx._python_only)
+    assert all(torch.equal(a, b) for a, b in zip(fast, calls()))
+
+
 def test_refusals():
     T, H, bt, nb = 4, 2, 16, 3
     geo = lynx.Geometry(H, H, bt, nb, 2)

@@ -259,6 +259,16 @@ def test_a_chain_is_a_verification():
     assert ((a - both).abs().double() <= 2 * ((2.0 ** -9 + 2 * E) * A)[..., None] + 2e-3).all()
 
 
+def test_the_extension_and_the_python_body_agree(monkeypatch):
+    pr = Problem((300, 0, 41), 6, 2, 4, seed=81)
+    d = pr.device()
+    lse = [torch.empty(3, 6, 8, device="cuda") for _ in range(2)]
+    fast = lynx.tree_attention(**d, lse=lse[0]), lynx.tree_attention(**d, anchor_only=True, out=torch.empty(d["q"].shape, device="cuda"))
+    monkeypatch.setattr(lynx, "_fast_tree_attention", lynx._python_only)
+    slow = lynx.tree_attention(**d, lse=lse[1]), lynx.tree_attention(**d, anchor_only=True, out=torch.empty(d["q"].shape, device="cuda"))
+    assert all(torch.equal(a, b) for a, b in zip(fast + (lse[0],), slow + (lse[1],)))
+
+
 def test_bad_block_ids_are_reported():
     pr = Problem((100, 50), 4, 1, 4, seed=61)
     d = pr.device()
