@@ -30,6 +30,12 @@ struct RotaryParams {
 struct Turn {
   float c[8], s[8];
 };
+__device__ __forceinline__ uint32_t axes_of(const RotaryParams& r, int l) {   // (selects: parameters indexed by a lane would go through local memory)
+  uint32_t a = r.axis[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) a = l == i ? r.axis[i] : a;
+  return a;
+}
 __device__ __forceinline__ const float* angle_row(const RotaryParams& r, int64_t token, uint32_t axis) {
   const int32_t p = ld_dep(r.positions + (int64_t)axis * r.stride + token);
   return r.cos_sin + (int64_t)min(max(p, 0), r.n_positions - 1) * (2 * r.n_pairs);
@@ -113,7 +119,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
   chunks_of(!r.interleaved, r.n_pairs, l, c0, c1);
   const bool turns = 8 * l < r.n_pairs;
   Turn t;
-  if (turns) load_turn(r, token, l, r.axis[l], t);
+  if (turns) load_turn(r, token, l, axes_of(r, l), t);
   for (int h0 = first; h0 < last; h0 += kFly) {
     uint4 a[kFly], b[kFly];
 #pragma unroll
@@ -147,20 +153,76 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
 __device__ __forceinline__ int64_t block_of(int64_t t, int bt, BlockDiv d) {
   return bt > 1 && t < (1ll << 31) ? quotient((int32_t)t, d) : t / bt;
 }
-// Codes of 8 consecutive channels -> 4 bytes of each nibble plane: (x - mn) rounded, then one rounding of the exact product
-// and sum to an integer, ties to even, as the whole-block quantiser does.
+// Codes of 8 channels, four register pairs of FP32 -> 4 bytes of each nibble plane: (x - mn) rounded, then one rounding of the exact product
+// and sum to an integer, ties to even (the low byte of 1.5 * 2^23 + code), as the whole-block quantiser does.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ void codes8(const float* x, float mn, float inv, uint32_t& a, uint32_t& r) {
   uint32_t c[8];
+  const uint64_t mn2 = pack2(mn, mn), inv2 = pack2(inv, inv), magic2 = pack2(12582912.0f, 12582912.0f);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) c[i] = __float_as_uint(__fmaf_rn(__fsub_rn(x[i], mn), inv, 12582912.0f));
-  // byte j holds channels 2 j (low half) and 2 j + 1
-  a = r = 0u;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t lo = c[2 * j] & 0xFFu, hi = c[2 * j + 1] & 0xFFu;
-    a |= ((lo >> 4) | (hi & 0xF0u)) << (8 * j);
-    r |= ((lo & 15u) | ((hi & 15u) << 4)) << (8 * j);
+  for (int i = 0; i < 4; ++i) {
+    uint64_t u2, y2;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(u2) : "l"(pack2(x[2 * i], x[2 * i + 1])), "l"(mn2));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y2) : "l"(u2), "l"(inv2), "l"(magic2));
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(c[2 * i]), "=r"(c[2 * i + 1]) : "l"(y2));
   }
+  // byte j of a plane holds channels 2 j (low half) and 2 j + 1: codes 0 1 2 3 | 4 5 6 7 in words, even and odd nibbles joined within
+  // 16 bits, bytes 0 and 2 kept
+  const uint32_t w0 = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+  const uint32_t w1 = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
+  const uint32_t s0 = w0 >> 4, s1 = w1 >> 4;
+  a = __byte_perm((s0 & 0x0F0F0F0Fu) | ((w0 >> 8) & 0xF0F0F0F0u), (s1 & 0x0F0F0F0Fu) | ((w1 >> 8) & 0xF0F0F0F0u), 0x6420);
+  r = __byte_perm((w0 & 0x0F0F0F0Fu) | (s0 & 0xF0F0F0F0u), (w1 & 0x0F0F0F0Fu) | (s1 & 0xF0F0F0F0u), 0x6420);
+}
+__device__ __forceinline__ uint32_t bf2min(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("min.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// Smallest and largest of a row by its eight lanes, of BF16 values and of turned ones: one register (min, -max), or two, through three
+// exchanges.
+__device__ __forceinline__ float2 row_range(const uint4& a, const uint4& b) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  uint32_t lo = w[0], hi = w[0] ^ 0x80008000u;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    lo = bf2min(lo, w[i]);
+    hi = bf2min(hi, w[i] ^ 0x80008000u);
+  }
+  uint32_t v = bf2min(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+#pragma unroll
+  for (int off = 4; off >= 1; off >>= 1) v = bf2min(v, __shfl_xor_sync(0xFFFFFFFFu, v, off));
+  return make_float2(__uint_as_float(v << 16), -__uint_as_float(v & 0xFFFF0000u));
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float2 row_range(const float* x) {
+  float mn = x[0], mx = x[0];
+#pragma unroll
+  for (int i = 1; i < 15; i += 2) {
+    mn = min3(mn, x[i], x[i + 1]);
+    mx = max3(mx, x[i], x[i + 1]);
+  }
+  mn = fminf(mn, x[15]);
+  mx = fmaxf(mx, x[15]);
+#pragma unroll
+  for (int off = 4; off >= 1; off >>= 1) {
+    mn = fminf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, off));
+    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, off));
+  }
+  return make_float2(mn, mx);
 }
 
 struct AppendParams {
@@ -176,9 +238,90 @@ struct AppendParams {
   BlockDiv bt_div;
 };
 
-// A warp: four tokens, `per` heads of K or of V.
+// A warp: four tokens, `per` heads of K or of V, kFly rows of a quarter-warp at a time.
+// 8 heads of 131072 tokens, K and V, out of a fused projection into scattered blocks (822 MB: 125 us at the copy rate): 148 us, 185 with
+// the keys rotated (67 MB more of angles; 206 and 234 with scalar arithmetic and two divisions a row in every lane).  Four rows of a
+// quarter-warp are in flight, two where they are kept turned in FP32; more, or the next ones during the arithmetic, cost more registers than
+// they hide (152 and 209).
+template <int kFly, bool TURN>
+__device__ __forceinline__ void append_rows(const RotaryParams& r, const AppendParams& p, int64_t row, int64_t slot, int v, int l, int first, int last) {
+  static_assert(kFly == 1 || kFly == 2 || kFly == 4, "a division per lane");
+  const bool turns = TURN && 8 * l < r.n_pairs, have = row >= 0 && row < p.n_src;
+  int c0 = 2 * l, c1 = 2 * l + 1;
+  if (TURN) chunks_of(!r.interleaved, r.n_pairs, l, c0, c1);
+  const uint4* src = (v ? p.src[1] : p.src[0]) + (have ? row * (v ? p.stride[1] : p.stride[0]) : 0);
+  uint4 a[kFly], b[kFly];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+      a[u] = b[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (have && h0 + u < last) {
+        a[u] = __ldcs(src + (h0 + u) * 16 + c0);
+        b[u] = __ldcs(src + (h0 + u) * 16 + c1);
+      }
+    }
+  };
+  Turn t;
+  if (have && turns) load_turn(r, row, l, axes_of(r, l), t);
+  const bool live = have && slot >= 0 && slot < p.n_slots;
+  const int64_t blk = live ? block_of(slot, p.bt, p.bt_div) : 0;
+  const int64_t dst0 = blk * p.heads * p.bt + (slot - blk * p.bt);
+  uint32_t *anchor = v ? p.anchor[1] : p.anchor[0], *residual = v ? p.residual[1] : p.residual[0];
+  float2* meta = v ? p.meta[1] : p.meta[0];
+#pragma unroll 1
+  for (int h0 = first; h0 < last; h0 += kFly) {
+    load(h0);
+    float2 range[kFly];   // (smallest, largest)
+    float y[TURN ? kFly : 1][16];
+    float mine = 0.0f;    // of row l mod kFly: its scale, or (the next kFly lanes) the reciprocal
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+      if constexpr (TURN) {
+        unpack8(a[u], y[u]);
+        unpack8(b[u], y[u] + 8);
+        if (turns) turn16(y[u], t, r.interleaved);
+        range[u] = row_range(y[u]);
+      } else {
+        range[u] = row_range(a[u], b[u]);
+      }
+      if ((l & (kFly - 1)) == u) mine = __fsub_rn(range[u].y, range[u].x);
+    }
+    {
+      const bool scale = !(l & kFly), flat = !(mine >= 0x1p-100f);
+      mine = __fdiv_rn(scale ? mine : 255.0f, scale ? 255.0f : mine);
+      if (flat) mine = 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+      if (h0 + u >= last) break;   // (the same for the whole warp)
+      const float scale = __shfl_sync(0xFFFFFFFFu, mine, u, 8), inv = __shfl_sync(0xFFFFFFFFu, mine, kFly + u, 8), mn = range[u].x;
+      float x[16];
+      if constexpr (!TURN) {
+        unpack8(a[u], x);
+        unpack8(b[u], x + 8);
+      }
+      uint32_t a0, r0, a1, r1;
+      codes8(TURN ? y[TURN ? u : 0] : x, mn, inv, a0, r0);
+      codes8((TURN ? y[TURN ? u : 0] : x) + 8, mn, inv, a1, r1);
+      if (live) {
+        const int64_t d = dst0 + (int64_t)(h0 + u) * p.bt;
+        if (!TURN) {
+          *reinterpret_cast<uint2*>(anchor + d * 16 + c0) = make_uint2(a0, a1);
+          *reinterpret_cast<uint2*>(residual + d * 16 + c0) = make_uint2(r0, r1);
+        } else {
+          anchor[d * 16 + c0] = a0;
+          anchor[d * 16 + c1] = a1;
+          residual[d * 16 + c0] = r0;
+          residual[d * 16 + c1] = r1;
+        }
+        if (l == 0) meta[d] = make_float2(scale, __fadd_rn(mn, 0.0f));   // (-0 -> +0)
+      }
+    }
+  }
+}
 template <int kFly>
-__global__ void __launch_bounds__(kThreads) cache_append_kernel(const __grid_constant__ RotaryParams r, const __grid_constant__ AppendParams p, int per, int groups) {
+__global__ void __launch_bounds__(kThreads, 4) cache_append_kernel(const __grid_constant__ RotaryParams r, const __grid_constant__ AppendParams p, int per,
+                                                                  int groups) {
   pdl_begin();
   const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31, l = lane & 7;
@@ -190,59 +333,8 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(const __grid_con
     slot = ld_dep(p.slots + token);
     row = p.rows ? (int64_t)ld_dep(p.rows + token) : token;
   }
-  const bool live = slot >= 0 && slot < p.n_slots && row >= 0 && row < p.n_src;
-  const bool rotate = p.rotate && !v, turns = rotate && 8 * l < r.n_pairs;
-  int c0, c1;
-  chunks_of(rotate && !r.interleaved, r.n_pairs, l, c0, c1);
-  Turn t;
-  if (live && turns) load_turn(r, row, l, r.axis[l], t);
-  const int64_t blk = live ? block_of(slot, p.bt, p.bt_div) : 0;
-  const int64_t dst0 = blk * p.heads * p.bt + (slot - blk * p.bt);
-  const uint4* src = p.src[v] + (live ? row * p.stride[v] : 0);
-  for (int h0 = first; h0 < last; h0 += kFly) {
-    uint4 a[kFly], b[kFly];
-#pragma unroll
-    for (int u = 0; u < kFly; ++u) {
-      a[u] = b[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (live && h0 + u < last) {
-        a[u] = ld_dep(src + (h0 + u) * 16 + c0);
-        b[u] = ld_dep(src + (h0 + u) * 16 + c1);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kFly; ++u) {
-      if (h0 + u >= last) break;   // (the same for the whole warp)
-      float x[16];
-      unpack8(a[u], x);
-      unpack8(b[u], x + 8);
-      if (live && turns) turn16(x, t, r.interleaved);
-      float mn = x[0], mx = x[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) {
-        mn = fminf(mn, x[i]);
-        mx = fmaxf(mx, x[i]);
-      }
-#pragma unroll
-      for (int off = 4; off >= 1; off >>= 1) {
-        mn = fminf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, off));
-        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, off));
-      }
-      const float range = __fsub_rn(mx, mn);
-      const bool flat = !(range >= 0x1p-100f);
-      const float scale = flat ? 0.0f : __fdiv_rn(range, 255.0f), inv = flat ? 0.0f : __fdiv_rn(255.0f, range);
-      uint32_t a0, r0, a1, r1;
-      codes8(x, mn, inv, a0, r0);
-      codes8(x + 8, mn, inv, a1, r1);
-      if (live) {
-        const int64_t d = dst0 + (int64_t)(h0 + u) * p.bt;
-        p.anchor[v][d * 16 + c0] = a0;
-        p.anchor[v][d * 16 + c1] = a1;
-        p.residual[v][d * 16 + c0] = r0;
-        p.residual[v][d * 16 + c1] = r1;
-        if (l == 0) p.meta[v][d] = make_float2(scale, __fadd_rn(mn, 0.0f));   // (-0 -> +0)
-      }
-    }
-  }
+  if (p.rotate && !v) append_rows<kFly == 4 ? 2 : 1, true>(r, p, row, slot, v, l, first, last);
+  else append_rows<kFly, false>(r, p, row, slot, v, l, first, last);
 }
 
 // ------------------------------------------------------------------ out of the planes
