@@ -173,13 +173,19 @@ __device__ __forceinline__ uint64_t globaltimer_ns() {
   return t;
 }
 // Gives up after 2^17 probes, each of which may park its thread for 20 us, or once another thread has; the caller carries on without the data,
-// so that all loops end, and the host is told through the status word.  (Inlined, and no longer than it must be: there are some thirty.)
+// so that all loops end, and the host is told through the status word.  (Inlined, and no longer than it must be: there are some thirty.  What
+// is waited for is some tiles away at most.)
 __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* abort_word) {
   for (uint32_t i = 0; !mbar_try_wait(bar, parity); ++i)
     if (i >= (1u << 17) || *abort_word) {
       *abort_word = 1;
       break;
     }
+}
+// The wait for a piece, which may be as far away as the piece before is long: gives up after two seconds (see bounded_wait.cuh).
+struct PieceWait { volatile int* abort_word; };
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, PieceWait w) {
+  bounded_wait([=] { return mbar_try_wait(bar, parity); }, [] { return globaltimer_ns(); }, w.abort_word);
 }
 // Four rows of a map one behind the other.
 __device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3, uint32_t bar) {
@@ -494,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
                  kready = mready + 64, kfree = kready + 16, vready = kfree + 8 * kSlots, vfree = vready + 8 * kSlots, ifull = vfree + 16, iempty = ifull + 16,
                  qready = iempty + 16, kdone = qready + 16;
   volatile int* ab = misc;        // (waits for data)
-  volatile int* iab = misc + 1;   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
+  const PieceWait iab = {misc + 1};   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
 
   if (tid == 0) {
     for (int i = 0; i < C::kRingK; ++i) { mbar_init(kfull + i * 8, 1); mbar_init(kempty + i * 8, 8); }
