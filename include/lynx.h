@@ -348,8 +348,10 @@ lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, lynx_plane V,
  * a node to the next (multiples of 8, at least Hkv * 128: views of a fused projection's output);  tree_mask : uint64 [batch][n_nodes].
  * K, V with both residuals: the full codes; with both NULL: the Anchor's state.
  * out : [batch][n_nodes][Hq][128], BF16, or float where out_float is set (for lynx_lse_merge); lse : float [batch][n_nodes][Hq]
- * or NULL.  Scores are FP32 sums of exact products; weights and values enter the second product as FP16 relative to exponents of
- * their own (2^-12 of a term; value rows below 2^-29 of the largest of their 128 tokens lose bits), sums are FP32.
+ * or NULL.  Scores are FP32 sums; keys enter them exactly, but for their middles zero +
+ * 128 scale (2^-22 of them) and rows whose scale is below 2^-22 of the largest of their 128 tokens.  Weights and values enter the second
+ * product as FP16 relative to exponents of their own (2^-12 of a term; value rows below 2^-29 of the largest of their 128 tokens lose
+ * bits), sums are FP32.  All pointers 16-byte aligned, the planes' meta among them (tree_mask: 8; block_table, seq_lens, lse: 4).
  * workspace : lynx_tree_workspace_bytes(shape, batch, n_nodes) bytes (0: unsupported shape), its first 256 zeroed once
  * (lynx_workspace_init); calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of range are
  * clamped and recorded there.  block_tokens a multiple of 16; seq_lens[b] is clamped to the table's capacity. */

@@ -4,12 +4,12 @@
 //   S = Q K^T,   p = 2^(a S + e - ref_r),   O += P V,   l += sum p,   out = O / l
 // over the prefix (planes, 128 tokens a tile) and one last tile of the nodes' own BF16 keys and values under the tree's mask.
 //
-// A row of codes c is mid + scale (c - 128), mid = zero + 128 scale.  Keys enter as FP16 of scale (c - 128), an error of 2^-12 of a
-// key's deviation from the row's middle (an eighth of a code's step at most), and the middles, which may be far larger, as
-// rank-1 terms in 16 more elements of the contraction: mid x sum(q), both in two FP16 parts (2^-22).  Queries are scaled by a power of two, exact
-// down to 2^-24 of the row block's largest.  So a score needs one multiply-add in the softmax, with a factor that its whole tile shares
-// (per-token scales there are loads of shared memory for every score: 140 us instead of 112 for 128 rows over 131072 tokens).  Values
-// enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15 (rows 2^29 times smaller keep all 11 bits; keys 2^26), weights as
+// A row of codes c is mid + scale (c - 128), mid = zero + 128 scale.  Keys enter as s4 (c - 128), s4 the scale rounded to 4 significant bits, which
+// is exact in FP16, and the middles, which may be far larger, as rank-1 terms in 16 more elements of the contraction: mid s4 / scale x
+// sum(q), both in two FP16 parts (2^-22).  What a score lacks, scale / s4, is a factor of its token in the softmax's one multiply-add per score, in FP32.
+// (FP16 of scale (c - 128) and one factor for the tile: 5 % less time for 512 rows and two contexts of 131072 tokens, but outputs 2.4 times as far off
+// where a few channels are ten times the others.)  Queries are scaled by a power of two, exact down to 2^-24 of the row block's largest.  Values
+// enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15 (rows 2^29 times smaller keep all 11 bits; keys 2^22 their 4), weights as
 // FP16 relative to a reference that keeps each row's largest between 2^7 and 2^16 (set anew when the sum of 64 weights,
 // which is there anyway, comes near it: no maxima): both roundings are 2^-12 of a term, an eighth of the
 // output's own rounding to BF16.  2^e goes into the weight's exponent and out of l's terms again, so that it costs nothing per weight.  Sums
@@ -97,9 +97,10 @@ struct Cfg {
                        kOffSum = kOffRV + kRingV * kStage;           // [128] the query sums' 8 FP16
   static constexpr int kOffMid = kOffSum + 2048;                     // [kSlots][128] the middles' 8 FP16
   static constexpr int kOffZero = kOffMid + kSlots * 2048;                    // 128 x 8 zeros, the other half of both
-  static constexpr int kOffKm = kOffZero + 2048;                     // [kSlots][128] half2 {scale, - 1152 scale}
-  static constexpr int kOffVm = kOffKm + kSlots * 512;               // [kSlots][128] half2 {scale, mid}
-  static constexpr int kOffMl = kOffVm + kSlots * 512;                    // [2][128] {reference, sum}
+  static constexpr int kOffKm = kOffZero + 2048;                     // [kSlots][128] FP16 scales of 4 bits
+  static constexpr int kOffVm = kOffKm + kSlots * 256;               // [kSlots][128] half2 {scale, mid}
+  static constexpr int kOffFactor = kOffVm + kSlots * 512;           // [2 kSlots][128] factors of the scores
+  static constexpr int kOffMl = kOffFactor + 2 * kSlots * 512;       // [2][128] {reference, sum}
   static constexpr int kOffItems = kOffMl + 2 * 1024;                // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
   static constexpr int kOffBars = kOffMisc + 256;
@@ -210,6 +211,12 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
   asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
   return v;
 }
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void lds_2x64(uint32_t a, uint64_t& x, uint64_t& y) { asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x), "=l"(y) : "r"(a)); }
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   uint32_t v;
   asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
@@ -218,6 +225,8 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
+__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t x) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(x) : "memory"); }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
@@ -312,6 +321,8 @@ __device__ __forceinline__ int exponent_of(float amax) { return ((__float_as_int
 
 __device__ __forceinline__ int tile_exponent(int bits) { return min(max(exponent_of(__int_as_float(bits)), kMinExp), 113); }
 
+// The nearest value of 4 significant bits.
+__device__ __forceinline__ float four_bits(float x) { return __uint_as_float((__float_as_uint(x) + 0x00080000u) & 0xFFF00000u); }
 // a 2^e, without infinities in between.
 __device__ __forceinline__ float times_pow2(float a, int e) { return a * pow2(max(e >> 1, -126)) * pow2(max(e - (e >> 1), -126)); }
 // Two FP16 parts of a value below 2^16: the nearest, and what is left.
@@ -323,23 +334,24 @@ __device__ __forceinline__ uint32_t two_parts(float x) {
 // A tile's codes, 64 or 128 rows, by eight warps: lane i of warp w takes the 16-byte chunk i & 3 (32 channels) of rows 8 w + (i >> 2) and 64 on.
 // Half of the lanes take a chunk's 8-byte halves in the other order: the eight of a store's phase then have eight chunk positions, and rows
 // that share their banks in the raw stage are read in different halves.
-// meta: per row, keys {scale, -1152 scale (rounded)} -> (1024 + c) scale - 1152 scale, values {scale, mid} -> (c - 128) scale + mid.
+// meta: per row, keys a scale of 4 bits -> (1024 + c) scale - 1152 scale, exact; values {scale, mid} -> (c - 128) scale + mid.
 template <bool FULL, bool VALUES>
 __device__ __forceinline__ void expand(uint32_t raw, uint32_t tile, uint32_t meta, int w, int i, int rounds) {
   const int cc = i & 3, row0 = 8 * w + (i >> 2);
   const uint32_t sw = (uint32_t)(((cc >> 1) ^ (row0 >> 1)) & 1) * 2u;
   uint32_t dst = tile + (uint32_t)(cc >> 1) * 16384u + (uint32_t)row0 * 128u + (uint32_t)((((cc & 1) * 4) ^ (row0 & 7) ^ (int)sw) * 16);
   uint32_t a = raw + (uint32_t)(row0 * 64 + cc * 16) + sw * 4u;
-  meta += (uint32_t)row0 * 4u;
+  meta += (uint32_t)row0 * (VALUES ? 4u : 2u);
 #pragma unroll 1
-  for (; rounds > 0; --rounds, a += 4096u, dst += 8192u, meta += 256u) {
+  for (; rounds > 0; --rounds, a += 4096u, dst += 8192u, meta += VALUES ? 256u : 128u) {
     const uint2 x0 = lds64(a), x1 = lds64(a ^ 8u);
     uint2 y0 = make_uint2(0x88888888u, 0x88888888u), y1 = y0;
     if (FULL) {
       y0 = lds64(a + 8192u);
       y1 = lds64((a ^ 8u) + 8192u);
     }
-    const uint32_t sm = lds32(meta), s2 = __byte_perm(sm, sm, 0x1010), m2 = __byte_perm(sm, sm, 0x3232);
+    const uint32_t sm = VALUES ? lds32(meta) : lds16(meta), s2 = __byte_perm(sm, sm, 0x1010),
+                   m2 = VALUES ? __byte_perm(sm, sm, 0x3232) : mul_f16x2(s2, 0xE480E480u);
     const uint32_t wa[4] = {x0.x, x0.y, x1.x, x1.y}, wr[4] = {y0.x, y0.y, y1.x, y1.y};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {   // register k holds word k ^ sw of the chunk
@@ -490,8 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
   volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [8 + i] maxima of the nodes, [16 + 4 piece + i]
-                                             // q maxima, [28 + piece] the queries' part of the scores' factor, [32 + 2 (tile % 8)] that factor, [33 + 2 (tile % 8)]
-                                             // exponent of the values
+                                             // q maxima, [28 + piece] the queries' part of the scores' factors, [32 + tile % 8] exponent of the values
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
@@ -574,17 +585,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         tc_fence_after();
         if (works) {
           const int valid = (tree ? p.n : min(kHalf, len - u0 * kTile - u * kHalf)) - t0;
-          const float a = __int_as_float(misc[32 + 2 * (t & 7)]);
-          const int e = misc[33 + 2 * (t & 7)];
+          const int e = misc[32 + (t & 7)];
+          const Slot f = slot_of(t);   // (two rounds of places: half of a tile may still be read when the scores of the next one are there)
+          const uint32_t factors = sbase + (uint32_t)(C::kOffFactor + (f.i + (int)f.ph * kSlots) * 512 + ((tree ? 0 : u & 1) * kHalf + t0) * 4);
           const uint32_t tm_s = tmem0 + C::kTmS + s.i * 64 + lanes;
-          const uint64_t a2 = f2_pack(a, a);
           const float shift = (float)e - ref;
           // N scores from position `at` on, in units of a weight's exponent; the weights of scores, and their sum
-          auto scores = [&](auto& x, float less) {
+          auto scores = [&](auto& x, int at, float less) {
             constexpr int N = sizeof(x) / sizeof(x[0]);
             const uint64_t b2 = f2_pack(less, less);
 #pragma unroll
-            for (int k = 0; k < N / 2; ++k) f2_unpack(f2_fma(f2_pack(x[2 * k], x[2 * k + 1]), a2, b2), x[2 * k], x[2 * k + 1]);
+            for (int k = 0; k < N; k += 4) {
+              uint64_t a0, a1;
+              lds_2x64(factors + (uint32_t)(at + k) * 4u, a0, a1);
+              f2_unpack(f2_fma(f2_pack(x[k], x[k + 1]), a0, b2), x[k], x[k + 1]);
+              f2_unpack(f2_fma(f2_pack(x[k + 2], x[k + 3]), a1, b2), x[k + 2], x[k + 3]);
+            }
           };
           auto weights = [&](const auto& x, uint32_t* w) {
             constexpr int N = sizeof(x) / sizeof(x[0]);
@@ -609,11 +625,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             tmem_load(tm_s + t0, x);
             tc_wait_ld();
             if constexpr (C::kW > kCW) tmem_load(tm_s + t0 + kCW, y);
-            scores(x, shift);
+            scores(x, 0, shift);
             sum = weights(x, w);
             if constexpr (C::kW > kCW) {
               tc_wait_ld();
-              scores(y, shift);
+              scores(y, kCW, shift);
               sum += weights(y, w + kCW / 2);
             }
             plain = !__any_sync(0xFFFFFFFFu, !(sum <= kMost));
@@ -629,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             auto chunk = [&](float (&x)[16], int ch, float less) {
               tmem_load(tm_s + t0 + ch, x);
               tc_wait_ld();
-              scores(x, less);
+              scores(x, ch, less);
               const int room = valid - ch;
               uint32_t bits = (uint32_t)(see >> ch) & (room >= 16 ? 0xFFFFu : room > 0 ? (1u << room) - 1u : 0u);
 #pragma unroll
@@ -831,7 +847,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         else if (gt > 1) wait(kfree + ms.before(2).i * 8, ms.before(2).ph, ab);
         if (ut < n_prefix) {
           const int rounds = len - ut * kTile > kHalf ? 2 : 1;
-          const uint32_t raw = sbase + (uint32_t)(stages + slot * C::kStage), meta = sbase + (uint32_t)(metas + ms.i * 512);
+          const uint32_t raw = sbase + (uint32_t)(stages + slot * C::kStage), meta = sbase + (uint32_t)(metas + ms.i * (values ? 512 : 256));
           wait(full + slot * 8, phase, ab);
           if (values) expand<FULL, true>(raw, tile, meta, w8, lane, rounds);
           else expand<FULL, false>(raw, tile, meta, w8, lane, rounds);
@@ -852,10 +868,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           named_bar(values ? 3 : 8, 64);
           const int e = tile_exponent(max(most[0], most[1]));
           named_bar(values ? 3 : 8, 64);   // (read by both)
-          if (row == 0) {
-            if (values) misc[33 + 2 * (gt & 7)] = e;
-            else misc[32 + 2 * (gt & 7)] = __float_as_int(times_pow2(a, e));
-          }
+          if (!values) sts32(sbase + (uint32_t)(C::kOffFactor + (ms.i + (int)ms.ph * kSlots) * 512 + row * 4), __float_as_uint(times_pow2(a, e)));
+          else if (row == 0) misc[32 + (gt & 7)] = e;
 #pragma unroll 2
           for (int ch = 0; ch < 16; ++ch) {
             const uint4 w = used ? scaled8(ld_dep(src + ch), pow2(-e)) : make_uint4(0u, 0u, 0u, 0u);
@@ -976,32 +990,35 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           id = block_id(p, b, min(t + 2 * kTile, top));
           const int e = tile_exponent((int)__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big))) + (values ? 0 : 3);   // (1152 scales below 2^15.2)
           const float f = pow2(-e);
-          uint32_t o[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             sc[i] *= f;
             mid[i] *= f;
           }
           if (values) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = pack_f16x2(sc[i], mid[i]);
-          } else {   // what rounding -1152 scale adds to all of a row is taken off its middle, which goes in two parts
+            sts128(sbase + (uint32_t)(C::kOffVm + ms.i * 512 + lane * 16), pack_f16x2(sc[0], mid[0]), pack_f16x2(sc[1], mid[1]), pack_f16x2(sc[2], mid[2]),
+                   pack_f16x2(sc[3], mid[3]));
+            if (lane == 0) misc[32 + (gt & 7)] = e;
+          } else {   // scales of 4 bits, so that products with codes are exact, and what the scores lack; middles in units of it, in two parts
+            const float tile = times_pow2(a, e);
+            uint32_t s2[2], r[4];
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
-              const uint32_t s2 = pack_f16x2(sc[i], sc[i + 1]), m2 = mul_f16x2(s2, 0xE480E480u);
-              o[i] = __byte_perm(s2, m2, 0x5410);
-              o[i + 1] = __byte_perm(s2, m2, 0x7632);
-              const float2 s16 = half2_to_float2(s2), m16 = half2_to_float2(m2);
-              const float x0 = mid[i] - fmaf(1152.0f, s16.x, m16.x), x1 = mid[i + 1] - fmaf(1152.0f, s16.y, m16.y);
+              s2[i >> 1] = pack_f16x2(four_bits(sc[i]), four_bits(sc[i + 1]));
+              const float2 s16 = half2_to_float2(s2[i >> 1]);
+              const float r0 = s16.x != 0.0f ? __fdividef(sc[i], s16.x) : 1.0f, r1 = s16.y != 0.0f ? __fdividef(sc[i + 1], s16.y) : 1.0f;
+              const float x0 = __fdividef(mid[i], r0), x1 = __fdividef(mid[i + 1], r1);
+              r[i] = __float_as_uint(tile * r0);
+              r[i + 1] = __float_as_uint(tile * r1);
               const uint32_t hi = pack_f16x2(x0, x1);
               const float2 h2 = half2_to_float2(hi);
               const uint32_t lo = pack_f16x2(x0 - h2.x, x1 - h2.y), at = sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + lane * 64 + i * 16);
               sts128(at, __byte_perm(hi, lo, 0x5410), hi & 0xFFFFu, 0u, 0u);
               sts128(at + 16u, __byte_perm(hi, lo, 0x7632), hi >> 16, 0u, 0u);
             }
+            sts64(sbase + (uint32_t)(C::kOffKm + ms.i * 256 + lane * 8), s2[0], s2[1]);
+            sts128(sbase + (uint32_t)(C::kOffFactor + (ms.i + (int)ms.ph * kSlots) * 512 + lane * 16), r[0], r[1], r[2], r[3]);
           }
-          sts128(sbase + (uint32_t)((values ? C::kOffVm : C::kOffKm) + ms.i * 512 + lane * 16), o[0], o[1], o[2], o[3]);
-          if (lane == 0) misc[(values ? 33 : 32) + 2 * (gt & 7)] = values ? e : __float_as_int(times_pow2(a, e));
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(mready + (gt & 7) * 8);

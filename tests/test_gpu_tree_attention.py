@@ -2,9 +2,9 @@
 
 Bounds.  Weights and values enter the second product as FP16: a weight is off by 2^-11 of itself at most, a value
 mid + scale (c - 128) by 2^-11 of each of its factors' and its own magnitude, 2^-9 of A in all, A = sum_t w_t (|mid_t| + 128 |scale_t|) over a
-row's weights w (nodes: their largest |v|).  Scores: FP32 sums over 128 channels of FP16 deviations and of mid x sum(q), off by 2^-16 of S,
-the largest sum of magnitudes that enters one, and by the rounding of the deviations, 2^-11 of each at most, independent of each
-other: 2^-9 of R = max_t |q x (k_t - mid_t)|_2 is five standard deviations of their sum and more.  A weight follows relatively and the
+row's weights w (nodes: their largest |v|).  Scores: keys' deviations from the middle of their row enter exactly, middles in two FP16
+parts (2^-22); FP32 sums over 128 channels of them and of mid x sum(q), and the factors of a row, are off by E = 2^-16 of S at most, S the
+largest sum of magnitudes that enters one.  A weight follows relatively and the
 output by twice that of A.  The last rounding to BF16 is 2^-8 of the output; log-sum-exps are off by the scores' error, the sum's
 rounding and the approximations of exp2 and log2 (2^-18)."""
 import math
@@ -101,14 +101,13 @@ class Problem:
         for b, L in enumerate(self.lens):
             t = torch.arange(L)
             blk, off = self.table[b, t // bt].long(), t % bt
-            vals, mags, devs = [], [], []
+            vals, mags = [], []
             for p, x in zip(self.planes, (self.kn, self.vn)):
                 a, r, m = (y[blk, :, off].cuda() for y in p)                         # [L][Hkv][..]
                 level = 16 * _nibbles(a) + (8 if anchor else _nibbles(r))
                 m = m.double()
                 node = torch.where(self.sees[b].any(0)[:, None, None], x[b].double(), 0.0).cuda()
                 vals.append(torch.cat((m[..., 1:] + m[..., :1] * level, node)))
-                devs.append(torch.cat((m[..., :1] * (level - 128), node)))
                 mags.append(torch.cat(((m[..., 1] + 128 * m[..., 0]).abs() + 128 * m[..., 0], node.abs().amax(-1))))
             allowed = torch.cat((torch.ones(n, L, dtype=torch.bool), self.sees[b]), 1).cuda()
             for h in range(Hkv):
@@ -124,8 +123,7 @@ class Problem:
                 lse[b, :, sl] = (den.log() + top)[..., 0]
                 A[b, :, sl] = w @ mags[1][:, h]
                 S = abs(scale) * q.abs().sum(-1) * mags[0][:, h].max()
-                R = abs(scale) * torch.einsum("jgd,td->jgt", q * q, devs[0][:, h] ** 2).amax(-1).sqrt()
-                E[b, :, sl] = 2.0 ** -9 * R + 2.0 ** -16 * S
+                E[b, :, sl] = 2.0 ** -16 * S
         return out, lse, A, E
 
 
