@@ -352,8 +352,9 @@ lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, lynx_plane V,
  * 128 scale (2^-22 of them) and rows whose scale is below 2^-22 of the largest of their 128 tokens.  Weights and values enter the second
  * product as FP16 relative to exponents of their own (2^-12 of a term; value rows below 2^-29 of the largest of their 128 tokens lose
  * bits), sums are FP32.  All pointers 16-byte aligned, the planes' meta among them (tree_mask: 8; block_table, seq_lens, lse: 4).
- * workspace : lynx_tree_workspace_bytes(shape, batch, n_nodes) bytes (0: unsupported shape), its first 256 zeroed once
- * (lynx_workspace_init); calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of range are
+ * workspace : lynx_tree_workspace_bytes(shape, batch, n_nodes) bytes (0: unsupported shape), zero-filled once before its first use
+ * (lynx_workspace_init); each call leaves it ready for the next, also of another batch, shape or number of nodes that it is large enough for.
+ * Calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of range are
  * clamped and recorded there.  block_tokens a multiple of 16; seq_lens[b] is clamped to the table's capacity. */
 size_t lynx_tree_workspace_bytes(const lynx_shape* shape, int32_t batch, int32_t n_nodes);
 lynx_status lynx_tree_attention(const lynx_shape* shape, const void* q_bf16, int32_t batch, int32_t n_nodes, lynx_plane K,

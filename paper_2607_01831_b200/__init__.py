@@ -676,12 +676,12 @@ def tree_workspace_bytes(geo: Geometry, batch: int, n_nodes: int) -> int:
 
 
 def make_tree_workspace(geo: Geometry, batch: int, n_nodes: int, device) -> torch.Tensor:
-    """Allocate a workspace for tree_attention calls of (batch, n_nodes) and clear its status word."""
+    """Allocate a workspace for tree_attention calls of (batch, n_nodes) and zero it."""
     n = tree_workspace_bytes(geo, batch, n_nodes)
     if n == 0:
         raise LynxError("unsupported tree attention shape")
     ws = torch.empty(n, dtype=torch.uint8, device=device)
-    _ok(load().lynx_workspace_init(_ptr(ws), 256, _stream()), "lynx_workspace_init")
+    _ok(load().lynx_workspace_init(_ptr(ws), n, _stream()), "lynx_workspace_init")
     return ws
 
 

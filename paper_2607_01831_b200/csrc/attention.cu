@@ -31,6 +31,7 @@
 #include "block_division.cuh"
 #include "bounded_wait.cuh"
 #include "lynx_common.cuh"
+#include "prefix_attention.cuh"
 #include "workspace_layout.cuh"
 
 namespace lynx {
@@ -650,7 +651,7 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
                           lynx_plane K, lynx_plane V, const int32_t* block_table,
                           const int32_t* seq_lens, float softmax_scale, const float* draft,
                           float atol, float rtol, float* out, int32_t* first_reject, float* dev,
-                          void* workspace, size_t workspace_bytes, void* stream, bool fixed_scratch = false) {
+                          void* workspace, size_t workspace_bytes, void* stream, bool fixed_scratch = false, int anchor_cols = 32) {
   if (B == 0) return LYNX_OK;
   if (!shape) return LYNX_ERR_NULL;
   if (B < 0 || nq <= 0) return LYNX_ERR_SHAPE;
@@ -706,7 +707,7 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
     // Anchor attention: the integer tcgen05 kernels take up to 32 columns, 16 as a pipeline of stages, above in teams.  A call with more (33..64) is
     // run as slices of whole query positions, each a pass of its own over the planes, one after the
     // other on the stream (they share the workspace).
-    const int per = nq * p.G <= 32 ? nq : (32 / p.G > 0 ? 32 / p.G : 1);
+    const int per = nq * p.G <= anchor_cols ? nq : (anchor_cols / p.G > 0 ? anchor_cols / p.G : 1);
     for (int j0 = 0; j0 < nq; j0 += per) {
       AttnParams ps = p;
       ps.nq = nq - j0 < per ? nq - j0 : per;
@@ -749,6 +750,13 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
 }
 
 }  // namespace
+
+lynx_status prefix_attention(bool full, const lynx_shape* shape, const void* q, int B, int n, lynx_plane K, lynx_plane V, const int32_t* block_table,
+                             const int32_t* seq_lens, float softmax_scale, float* out, void* workspace, size_t workspace_bytes, void* stream) {
+  return run_attention(full, shape, q, B, n, 0, K, V, block_table, seq_lens, softmax_scale, nullptr, 0.f, 0.f, out, nullptr, nullptr, workspace,
+                       workspace_bytes, stream, false, kPrefixCols);
+}
+
 }  // namespace lynx
 
 extern "C" size_t lynx_workspace_bytes(const lynx_shape* shape, int32_t batch, int32_t n_cols_q) {
