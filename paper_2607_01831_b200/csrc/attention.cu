@@ -30,8 +30,8 @@
 
 #include "block_division.cuh"
 #include "bounded_wait.cuh"
+#include "nodes_attention.cuh"
 #include "lynx_common.cuh"
-#include "prefix_attention.cuh"
 #include "workspace_layout.cuh"
 
 namespace lynx {
@@ -75,7 +75,13 @@ struct AttnParams {
   BlockDiv seg_div, hkv_div;
   int combine_single;   // the attention kernel leaves a segment of one CTA in its slot, too
   int inline_merge;     // the last CTA of a segment joins its slots, not attn_combine_kernel
+  float v_rel, v_least;    // see v_scale
+  const NodeArgs* nodes;   // (on the host) drafted nodes to be attended to as well, or NULL
 };
+// A value row's scale for logarithms and quotients: at least v_rel of its zero point and v_least, since it may be 0 (then the codes are, and any does).  Chains
+// have 0 and 2^-40, so that rows of smaller scales are off by up to 2^-32; trees 2^-24 and 2^-80: by 2^-16 of themselves, or 2^-72.  (Not smaller: weights
+// times scales are dropped below 2^-126 of the largest.)
+__device__ __forceinline__ float v_scale(const AttnParams& p, float scale, float zero) { return fmaxf(scale, fmaxf(fabsf(zero) * p.v_rel, p.v_least)); }
 // Block of token t of a sequence.  (No division: its code, at four places of the unit loops, costs more in the instruction caches
 // than its time.  Together with rolled drains and one copy of the 4-column kernel's restart, us: one layer of 131072 tokens 37.7 ->
 // 37.1, two sequences of 16000 at 8 columns 22.1 -> 21.2, 16 ragged sequences with a verification at 16 columns 276 -> 274, one layer
@@ -550,10 +556,22 @@ inline void plan_cut(AttnParams* p, int n_cta) {
   p->hkv_div = p->Hkv > 1 ? block_div(p->Hkv) : BlockDiv{0, 0};
 }
 
+#include "attention_nodes.cuh"
+
 // (Nothing to join where every segment is one unit and nothing to decide; anchor calls with many heads join in the attention
 // kernel.  bench.py counts kernels by this rule.)
 inline lynx_status launch_combine(const AttnParams& p, int part_cols, int st_tokens, int min_units, cudaStream_t st) {
   const long long cap_units = ((long long)p.max_blocks * p.bt + st_tokens - 1) / st_tokens;
+  if (p.nodes) {
+    // (segments of very different lengths, or joined by their last CTAs: the results as they are there then, see attn_combine_kernel)
+    const bool wide = p.B * p.Hkv * 4 < sm_count(), none = p.inline_merge || (!p.combine_single && cap_units <= 1);
+    if (none || wide || cap_units < kLongSegment)
+      return wide ? launch_nodes<kCombineWarps>(p, part_cols, none, st) : launch_nodes<1>(p, part_cols, none, st);
+    AttnParams joining = p;
+    joining.nodes = nullptr;
+    const lynx_status rc = launch_combine(joining, part_cols, st_tokens, min_units, st);
+    return rc != LYNX_OK ? rc : launch_nodes<1>(p, part_cols, 1, st);
+  }
   if (p.inline_merge || (!p.draft && !p.combine_single && cap_units <= 1)) return LYNX_OK;
   // a warp per row where a head has no more than a few CTAs on average (one layer: 18; 16 layers of two sequences: 0.6)
   const unsigned rows = (unsigned)(p.B * p.nq * p.Hq);
@@ -651,7 +669,8 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
                           lynx_plane K, lynx_plane V, const int32_t* block_table,
                           const int32_t* seq_lens, float softmax_scale, const float* draft,
                           float atol, float rtol, float* out, int32_t* first_reject, float* dev,
-                          void* workspace, size_t workspace_bytes, void* stream, bool fixed_scratch = false, int anchor_cols = 32) {
+                          void* workspace, size_t workspace_bytes, void* stream, bool fixed_scratch = false, int anchor_cols = 32,
+                          const NodeArgs* nodes = nullptr) {
   if (B == 0) return LYNX_OK;
   if (!shape) return LYNX_ERR_NULL;
   if (B < 0 || nq <= 0) return LYNX_ERR_SHAPE;
@@ -678,6 +697,9 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
   p.block_table = block_table; p.seq_lens = seq_lens;
   p.out = out; p.draft = full ? draft : nullptr; p.first_reject = first_reject; p.dev = dev;
   p.combine_single = 0;
+  p.nodes = nullptr;
+  p.v_rel = nodes ? 5.9604645e-8f : 0.0f;
+  p.v_least = nodes ? 8.2718061e-25f : 9.094947e-13f;
   // Who joins the partial results: attn_combine_kernel where few heads share the grid (and for verification, which needs it for
   // the decision), the last CTA of a head where a head has a CTA or two on average and its merge overlaps other heads' work (16
   // layers of two sequences of 131072 tokens, 8 columns: 1025 us, 1040 us by a kernel of its own; one layer of 4096 tokens, 4
@@ -716,6 +738,12 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
       ps.q = p.q + (size_t)j0 * p.Hq * LYNX_D;
       ps.out = p.out + (size_t)j0 * p.Hq * LYNX_D;
       ps.ws_lse = p.ws_lse + (size_t)j0 * p.Hq;
+      NodeArgs slice;
+      if (nodes) {
+        slice = *nodes;
+        slice.j0 = j0;
+        ps.nodes = &slice;
+      }
       const lynx_status rc = ps.ncols <= 4 ? launch_pipe<false, 4>(ps, st) : ps.ncols <= 8 ? launch_pipe<false, 8>(ps, st)
                            : ps.ncols <= 16 ? launch_pipe<false, 16>(ps, st) : launch_i8(ps, st);
       if (rc != LYNX_OK) return rc;
@@ -736,6 +764,12 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
     ps.q = p.q + (size_t)j0 * p.Hq * LYNX_D;
     ps.out = p.out + (size_t)j0 * p.Hq * LYNX_D;
     ps.ws_lse = p.ws_lse + (size_t)j0 * p.Hq;
+    NodeArgs slice;
+    if (nodes) {
+      slice = *nodes;
+      slice.j0 = j0;
+      ps.nodes = &slice;
+    }
     if (p.draft) { ps.draft = p.draft + (size_t)j0 * p.Hq * LYNX_D; ps.dev = p.dev + j0; }
     const lynx_status rc = ps.ncols <= 4 ? launch_pipe<true, 4>(ps, st) : ps.ncols <= 8 ? launch_pipe<true, 8>(ps, st)
                          : ps.ncols <= 16 ? launch_pipe<true, 16>(ps, st) : ps.ncols > 32 ? launch_f16<64, false>(ps, st)
@@ -751,10 +785,11 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
 
 }  // namespace
 
-lynx_status prefix_attention(bool full, const lynx_shape* shape, const void* q, int B, int n, lynx_plane K, lynx_plane V, const int32_t* block_table,
-                             const int32_t* seq_lens, float softmax_scale, float* out, void* workspace, size_t workspace_bytes, void* stream) {
-  return run_attention(full, shape, q, B, n, 0, K, V, block_table, seq_lens, softmax_scale, nullptr, 0.f, 0.f, out, nullptr, nullptr, workspace,
-                       workspace_bytes, stream, false, kPrefixCols);
+lynx_status nodes_attention(bool full, const lynx_shape* shape, const void* q, int B, lynx_plane K, lynx_plane V, const int32_t* block_table,
+                            const int32_t* seq_lens, float softmax_scale, const NodeArgs& nodes, float* scratch, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  return run_attention(full, shape, q, B, nodes.n, 0, K, V, block_table, seq_lens, softmax_scale, nullptr, 0.f, 0.f, scratch, nullptr, nullptr, workspace,
+                       workspace_bytes, stream, false, kNodesCols, &nodes);
 }
 
 }  // namespace lynx

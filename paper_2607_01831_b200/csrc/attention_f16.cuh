@@ -402,7 +402,7 @@ struct F16Meta {
     for (int i = 0; i < N; ++i) {
       const bool valid = (u0 + u) * C::kST + i0 + 32 * i < len;
       if (C::kSplit && valid && !(vm[i].x < 16.0f)) atomicOr(p.ws_flags, kFlagRange);   // beyond the stated range of this width
-      const float sve = fmaxf(vm[i].x, 9.094947e-13f);   // floor 2^-40
+      const float sve = v_scale(p, vm[i].x, vm[i].y);
       const float ia = valid ? rcp_approx(sve) : 0.0f;
       const int at = gs % C::kSlots * 128 + 32 * i;
       tok4[at] = make_float4(km[i].x * ca, fmaf(km[i].x, 128.0f, km[i].y) * p.sm_log2, lg2_approx(sve), ia);

@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
           float2 km = meta[mt * 256], vm = meta[mt * 256 + 128];
           const bool valid = tok < len;
           if (!valid) { km = make_float2(0.f, 0.f); vm = make_float2(0.f, 0.f); }
-          const float sve = fmaxf(FULL ? vm.x : 16.0f * vm.x, 9.094947e-13f);   // floor 2^-40
+          const float sve = v_scale(p, FULL ? vm.x : 16.0f * vm.x, vm.y);
           const float al = km.x * ca;
           const float be = fmaf(km.x, FULL ? 128.0f : 8.0f, km.y) * cb;
           const float lsv = lg2_approx(sve);

@@ -48,7 +48,7 @@
 #include "block_division.cuh"
 #include "bounded_wait.cuh"
 #include "lynx_common.cuh"
-#include "prefix_attention.cuh"
+#include "nodes_attention.cuh"
 #include "workspace_layout.cuh"
 
 namespace lynx {
@@ -1110,18 +1110,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   }
 }
 
-// Four channels of an output row, and its log-sum-exp: maximum M, sum L.
-__device__ __forceinline__ void write_row(void* out, float* lse, int out_f32, int64_t row, int lane, float4 acc, float M, float L) {
-  if (out_f32) {
-    reinterpret_cast<float4*>(static_cast<float*>(out) + row * LYNX_D)[lane] = acc;
-  } else {
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
-    reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + row * LYNX_D)[lane] =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-  }
-  if (lse && lane == 0) lse[row] = L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
-}
-
 // Joins the partial results of the CTAs that share a segment: W warps per output row, its slots dealt to them, six on their way each, a lane four
 // channels.  (Four warps where segments are few and have many slots each: 13 nodes of 4 heads over 4096 tokens, 34 slots, 18.6 us, 19.5 with a warp per row.)
 constexpr int kCombineWarps = 4;
@@ -1194,106 +1182,14 @@ __global__ void __launch_bounds__(kCombineWarps * 32) tree_combine_kernel(const 
   }
   const float inv = L > 0.0f ? 1.0f / L : 0.0f;
   acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
-  write_row(p.out, p.lse, p.out_f32, row, lane, acc, M, L);
-}
-
-// Few columns: the prefix by the kernels that chains of drafted tokens have (prefix_attention), then this one, a warp per output row, which attends to
-// the nodes and joins both by their log-sum-exps; a lane has four channels, CH nodes are on their way at a time.
-struct NodeParams {
-  const uint2* q;                   // [B][n][Hq][32]
-  const uint2 *kt, *vt;             // [B * n] tokens, `kt_stride` / `vt_stride` apart
-  int64_t kt_stride, vt_stride;
-  const unsigned long long* mask;   // [B][n]
-  const float4* prefix;             // [B][n][Hq][32]
-  const float* prefix_lse;          // [B][n][Hq]
-  void* out;
-  float* lse;
-  float sm_log2;
-  int n, Hq, G, out_f32;
-  int64_t rows;
-};
-struct Pairs { uint64_t x, y; };   // four channels
-__device__ __forceinline__ Pairs widen(const uint2& w) { return {f2_pack(bf_lo(w.x), bf_hi(w.x)), f2_pack(bf_lo(w.y), bf_hi(w.y))}; }
-// Latency bounds it, a round of loads and some hundred instructions in a row: all that a row may need is asked for at once, seen or not.
-template <int CH>
-__global__ void __launch_bounds__(128) tree_nodes_kernel(const __grid_constant__ NodeParams p) {
-  pdl_trigger();
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (row >= p.rows) return;
-  const int64_t bj = row / p.Hq, first = bj / p.n * p.n;   // of this node, of its sequence's first
-  const int h = (int)(row - bj * p.Hq) / p.G;
-  const uint2 *kt = p.kt + first * p.kt_stride + h * 32 + lane, *vt = p.vt + first * p.vt_stride + h * 32 + lane;
-  pdl_wait();
-  const uint2 qw = ld_dep(p.q + row * 32 + lane);
-  const unsigned long long see = ld_dep(p.mask + bj) & (p.n < 64 ? (1ull << p.n) - 1 : ~0ull);
-  Pairs acc = {0ull, 0ull};
-  float m = -INFINITY, l = 0.0f;
-  const float pm = ld_dep(p.prefix_lse + row) * 1.4426950408889634f;
-  const float4 o = ld_dep(p.prefix + row * 32 + lane);
-#pragma unroll 1
-  for (int i0 = 0; i0 < p.n; i0 += CH) {
-    uint2 k[CH], v[CH];
-#pragma unroll
-    for (int u = 0; u < CH; ++u) {
-      const int i = min(i0 + u, p.n - 1);
-      k[u] = ld_dep(kt + i * p.kt_stride);
-      v[u] = ld_dep(vt + i * p.vt_stride);
-    }
-    const uint32_t bits = (uint32_t)(see >> i0) & ((1u << CH) - 1);
-    if (bits == 0) continue;
-    // CH sums over the lanes, halved at every exchange: the 32 / CH lanes from 32 / CH x u on end with that of node u
-    float d[CH];
-    const Pairs q = widen(qw);
-#pragma unroll
-    for (int u = 0; u < CH; ++u) {
-      const Pairs x = widen(k[u]);
-      float a, b;
-      f2_unpack(f2_fma(q.x, x.x, f2_fma(q.y, x.y, 0ull)), a, b);
-      d[u] = a + b;
-    }
-#pragma unroll
-    for (int half = CH / 2; half >= 1; half >>= 1) {
-      const bool up = lane & (half * (32 / CH));
-#pragma unroll
-      for (int u = 0; u < half; ++u) {
-        const float other = __shfl_xor_sync(0xFFFFFFFFu, up ? d[u] : d[u + half], half * (32 / CH));
-        d[u] = (up ? d[u + half] : d[u]) + other;
-      }
-    }
-    float s = d[0];
-#pragma unroll
-    for (int x = 16 / CH; x >= 1; x >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, x);
-    s = (bits >> (lane / (32 / CH))) & 1u ? s * p.sm_log2 : -INFINITY;   // (what is not seen may be anything)
-    float top = s;
-#pragma unroll
-    for (int x = 32 / CH; x <= 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-    const float m1 = fmaxf(m, top), f = ex2(m - m1);   // (top is a number)
-    const float w = ex2(s - m1);
-    float sum = w;
-#pragma unroll
-    for (int x = 32 / CH; x <= 16; x <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-    l = fmaf(l, f, sum);
-    const uint64_t f2 = f2_pack(f, f);
-    acc.x = f2_fma(acc.x, f2, 0ull);
-    acc.y = f2_fma(acc.y, f2, 0ull);
-    m = m1;
-#pragma unroll
-    for (int u = 0; u < CH; ++u) {
-      const float wu = __shfl_sync(0xFFFFFFFFu, w, u * (32 / CH));
-      const Pairs x = widen((bits >> u) & 1u ? v[u] : make_uint2(0u, 0u));
-      const uint64_t w2 = f2_pack(wu, wu);
-      acc.x = f2_fma(w2, x.x, acc.x);
-      acc.y = f2_fma(w2, x.y, acc.y);
-    }
+  if (p.out_f32) {
+    reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * LYNX_D)[lane] = acc;
+  } else {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
+    reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * LYNX_D)[lane] =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
   }
-  const float M = fmaxf(m, pm), wn = m == -INFINITY ? 0.0f : ex2(m - M), wp = pm == -INFINITY ? 0.0f : ex2(pm - M);
-  const float L = fmaf(l, wn, wp), inv = L > 0.0f ? 1.0f / L : 0.0f, fn = wn * inv, fp = wp * inv;
-  float4 a;
-  f2_unpack(acc.x, a.x, a.y);
-  f2_unpack(acc.y, a.z, a.w);
-  a = make_float4(fmaf(a.x, fn, o.x * fp), fmaf(a.y, fn, o.y * fp), fmaf(a.z, fn, o.z * fp), fmaf(a.w, fn, o.w * fp));
-  write_row(p.out, p.lse, p.out_f32, row, lane, a, M, L);
+  if (p.lse && lane == 0) p.lse[row] = L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 // ------------------------------------------------------------------ host side
@@ -1302,8 +1198,8 @@ constexpr int kWholeTiles = 3;   // up to so many tiles a CTA takes a whole segm
 struct TreePlan {
   int cols, RB, part_rows, whole, grid, per_seg, log_ts;
   int64_t segs;
-  int prefix[2];         // Anchor, full: the prefix by prefix_attention
-  size_t off_prefix;     // its output; its own workspace lies in front
+  int few[2];            // Anchor, full: by nodes_attention
+  size_t off_scratch;    // its scratch; its workspace lies in front
   size_t off_seg, off_part, bytes;
 };
 lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
@@ -1333,18 +1229,18 @@ lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
   const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   // Few rows, where the kernels for chains take one pass over the planes, or two over the Anchor and there is enough of it, eight tiles per SM (us, 24
   // rows, two passes / the tree kernel: 16 sequences of 8192 to 65536 tokens 325 / 409, one of 131072 95 / 102, of 4096 29 / 19).
-  const int passes = (n + kPrefixCols / G - 1) / (kPrefixCols / G);
-  pl->prefix[0] = passes == 1 || (passes == 2 && (int64_t)B * s->num_kv_heads * (tiles - 1) >= 8 * sms);
-  pl->prefix[1] = pl->cols <= 32 && n <= kWsMaxQ;
+  const int passes = (n + kNodesCols / G - 1) / (kNodesCols / G);
+  pl->few[0] = passes == 1 || (passes == 2 && (int64_t)B * s->num_kv_heads * (tiles - 1) >= 8 * sms);
+  pl->few[1] = pl->cols <= 32 && n <= kWsMaxQ;
   const size_t own = lynx_workspace_bytes(s, B, n);
-  if (own == 0) pl->prefix[0] = pl->prefix[1] = 0;
-  pl->off_prefix = up(own);
+  if (own == 0) pl->few[0] = pl->few[1] = 0;
+  pl->off_scratch = up(own);
   // (what the kernels for chains keep at zero between calls lies in front and stays as it is)
   pl->off_seg = up(ws_layout((int)sms, B, n, s->num_q_heads, s->num_kv_heads, 8).end_kept);
   pl->off_part = up(pl->off_seg + (size_t)pl->segs * 4);
   size_t most = 0;
-  if (pl->prefix[0] || pl->prefix[1]) most = pl->off_prefix + (size_t)B * n * s->num_q_heads * LYNX_D * 4;
-  if (!pl->prefix[0] || !pl->prefix[1]) {
+  if (pl->few[0] || pl->few[1]) most = pl->off_scratch + (size_t)B * n * s->num_q_heads * LYNX_D * 4;
+  if (!pl->few[0] || !pl->few[1]) {
     const size_t tree = pl->off_part + (pl->whole ? 0 : (size_t)(pl->segs + pl->grid) * pl->part_rows * kPartRow * 4);
     if (tree > most) most = tree;
   }
@@ -1422,23 +1318,15 @@ extern "C" lynx_status lynx_tree_attention(const lynx_shape* shape, const void* 
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   const float sm_log2 = (softmax_scale == 0.0f ? 0.08838834764831845f : softmax_scale) * 1.4426950408889634f;
   const int64_t rows = (int64_t)batch * n_nodes * shape->num_q_heads;
-  if (pl.prefix[K.residual ? 1 : 0]) {
-    float* prefix = reinterpret_cast<float*>(ws + pl.off_prefix);
-    const lynx_status st = prefix_attention(K.residual != nullptr, shape, q_bf16, batch, n_nodes, K, V, block_table, seq_lens, softmax_scale, prefix, ws,
-                                            pl.off_prefix, stream);
-    if (st != LYNX_OK) return st;
-    NodeParams p;
-    p.q = static_cast<const uint2*>(q_bf16);
-    p.kt = static_cast<const uint2*>(k_nodes); p.vt = static_cast<const uint2*>(v_nodes);
-    p.kt_stride = k_stride / 4; p.vt_stride = v_stride / 4;
-    p.mask = reinterpret_cast<const unsigned long long*>(tree_mask);
-    p.prefix = reinterpret_cast<const float4*>(prefix);
-    p.prefix_lse = lynx_workspace_lse(shape, batch, n_nodes, ws);
-    p.out = out; p.lse = lse;
-    p.sm_log2 = sm_log2;
-    p.n = n_nodes; p.Hq = shape->num_q_heads; p.G = p.Hq / shape->num_kv_heads; p.out_f32 = out_float ? 1 : 0;
-    p.rows = rows;
-    return launch_pdl(n_nodes <= 4 ? tree_nodes_kernel<4> : tree_nodes_kernel<8>, (unsigned)((rows + 3) / 4), 128, 0, stream, p);
+  if (pl.few[K.residual ? 1 : 0]) {
+    NodeArgs nodes;
+    nodes.kt = static_cast<const uint2*>(k_nodes); nodes.vt = static_cast<const uint2*>(v_nodes);
+    nodes.kt_stride = k_stride / 4; nodes.vt_stride = v_stride / 4;
+    nodes.mask = reinterpret_cast<const unsigned long long*>(tree_mask);
+    nodes.out = out; nodes.lse = lse;
+    nodes.out_f32 = out_float ? 1 : 0; nodes.n = n_nodes; nodes.j0 = 0;
+    return nodes_attention(K.residual != nullptr, shape, q_bf16, batch, K, V, block_table, seq_lens, softmax_scale, nodes,
+                           reinterpret_cast<float*>(ws + pl.off_scratch), ws, pl.off_scratch, stream);
   }
   TreeParams p;
   p.q = static_cast<const uint4*>(q_bf16);
