@@ -28,8 +28,8 @@
 // memory, over the scores, as the A operand of P V; three places for scores, so that Q K^T is never waited for.
 // One CTA per SM; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
 //   warps 0-3, 4-7   softmax, even and odd half tiles
-//   warps 8-23       codes to FP16: K tiles by those on the first two of the four schedulers, V tiles on the others (warp mod 4); a piece's
-//                    queries by the first four
+//   warps 8-23       codes to FP16: K tiles by those on the first two of the four schedulers, V tiles on the others (warp mod 4); all of them a piece's
+//                    queries
 //   warp 24          copies of the planes into rings, four 16-token sub-blocks at a time; deals out the pieces
 //   warps 25, 27     scales and zero points of a tile's values and keys: what the tiles and the softmax need of them
 //   warp 26          issues every tcgen05.mma: Q K^T three half tiles ahead of P V
@@ -110,8 +110,8 @@ struct Cfg {
   static constexpr int kOffMl = kOffFactor + 2 * kSlots * 512;       // [2][128] {reference, sum}
   static constexpr int kOffItems = kOffMl + 2 * 1024;                // [2] Item
   static constexpr int kOffMisc = kOffItems + 2 * 32;                // ints
-  static constexpr int kOffBars = kOffMisc + 256;
-  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 5 * kSlots + 8 + 12;
+  static constexpr int kOffBars = kOffMisc + 192;
+  static constexpr int kBars = 2 * kRingK + 2 * kRingV + 7 * kSlots + 8 + 12;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024, "shared memory");
   static_assert(kOffSum % 128 == 0 && kOffBars % 8 == 0, "alignment");
@@ -330,6 +330,30 @@ __device__ __forceinline__ int tile_exponent(int bits) { return min(max(exponent
 
 // The nearest value of 4 significant bits.
 __device__ __forceinline__ float four_bits(float x) { return __uint_as_float((__float_as_uint(x) + 0x00080000u) & 0xFFF00000u); }
+// Four chunks of a row; what is not in use may be anything, and is zeros.
+__device__ __forceinline__ void load4(uint4 (&x)[4], const uint4* src, bool used) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = ld_dep(src + i);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (!used) x[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+// The largest magnitude of the BF16 values that N warps have, by 16 bits of each in shared memory; bar: a barrier of theirs.
+template <int N>
+__device__ __forceinline__ float largest(const uint4 (&x)[4], unsigned char* maxima, int w, int lane, int bar) {
+  const float most = fmaxf(fmaxf(absmax8(x[0]), absmax8(x[1])), fmaxf(absmax8(x[2]), absmax8(x[3])));
+  const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
+  if (lane == 0) reinterpret_cast<volatile uint16_t*>(maxima)[w] = (uint16_t)(bits >> 16);
+  named_bar(bar, N * 32);
+  uint32_t top = 0u;
+#pragma unroll
+  for (int i = 0; i < N / 2; i += 2) {
+    const uint2 m = lds64(smem_u32(maxima) + 4 * i);
+    asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(m.x));
+    asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(m.y));
+  }
+  return __uint_as_float(max(top & 0xFFFF0000u, top << 16));
+}
 // a 2^e, without infinities in between.
 __device__ __forceinline__ float times_pow2(float a, int e) { return a * pow2(max(e >> 1, -126)) * pow2(max(e - (e >> 1), -126)); }
 // Two FP16 parts of a value below 2^16: the nearest, and what is left.
@@ -508,15 +532,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   const uint32_t sbase = smem_u32(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
-  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [8 + i] maxima of the nodes, [16 + 4 piece + i]
-                                             // q maxima, [28 + piece] the queries' part of the scores' factors, [32 + tile % 8] exponent of the values
+  volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + piece] the queries' part of the scores' factors, [8 ..]
+                                             // maxima of the nodes' keys and values (16 bits a warp), [16 + 8 piece ..] of the queries, [40 + tile % 8] exponent of
+                                             // the values
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
-  // of a half tile: sfull, pready, pvdone; of a tile: kfree, vready (kSlots), kready, vfree (in turn), mready (8); of a piece: ifull, iempty, qready, kdone
+  // of a half tile: sfull, pready, pvdone; of a tile: kfree, vready, kscales, vscales (kSlots), kready, vfree (in turn), mready (8); of a piece: ifull, iempty, qready, kdone
   const uint32_t sfull = vempty + 8 * C::kRingV, pready = sfull + 8 * kSlots, pvdone = pready + 8 * kSlots, mready = pvdone + 8 * kSlots,
                  kready = mready + 64, kfree = kready + 16, vready = kfree + 8 * kSlots, vfree = vready + 8 * kSlots, ifull = vfree + 16, iempty = ifull + 16,
-                 qready = iempty + 16, kdone = qready + 16;
+                 qready = iempty + 16, kdone = qready + 16, kscales = kdone + 16, vscales = kscales + 8 * kSlots;
   volatile int* ab = misc;        // (waits for data)
   const PieceWait iab = {misc + 1};   // (waits for pieces: they need no data to arrive and stay in step after a wait for data has given up)
 
@@ -529,17 +554,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       mbar_init(pvdone + i * 8, 1);
       mbar_init(kfree + i * 8, 1);
       mbar_init(vready + i * 8, 8);
+      mbar_init(kscales + i * 8, 1);
+      mbar_init(vscales + i * 8, 1);
     }
     for (int i = 0; i < 8; ++i) mbar_init(mready + i * 8, 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(kready + i * 8, 8);
       mbar_init(vfree + i * 8, 1);
-      mbar_init(qready + i * 8, 4);
+      mbar_init(qready + i * 8, 16);
       mbar_init(kdone + i * 8, 2);
       mbar_init(ifull + i * 8, 1);
       mbar_init(iempty + i * 8, 8 + 16 + 3);   // softmax, codes, scales, products
     }
-    for (int i = 0; i < 64; ++i) misc_s[i] = 0;
+    for (int i = 0; i < 48; ++i) misc_s[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   for (int i = tid; i < 512; i += kThreads) reinterpret_cast<uint32_t*>(smem + C::kOffZero)[i] = 0u;
@@ -592,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         tc_fence_after();
         if (works) {
           const int valid = (tree ? p.n : min(kHalf, len - u0 * kTile - u * kHalf)) - t0;
-          const int e = misc[32 + (t & 7)];
+          const int e = misc[40 + (t & 7)];
           const Slot f = slot_of(t);   // (two rounds of places: half of a tile may still be read when the scores of the next one are there)
           const uint32_t factors = sbase + (uint32_t)(C::kOffFactor + (f.i + (int)f.ph * kSlots) * 512 + ((tree ? 0 : u & 1) * kHalf + t0) * 4);
           const uint32_t tm_s = tmem0 + C::kTmS + s.i * 64 + lanes;
@@ -789,8 +816,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   if (warp < 24) {
     reg_dec<C::kRegExp>();
     const bool values = (warp & 2) != 0;
-    const int w8 = ((warp - 8) >> 2) * 2 + (warp & 1), row = w8 * 32 + lane, qr = tid - 256;
-    const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty;
+    const int w8 = ((warp - 8) >> 2) * 2 + (warp & 1);
+    const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty, scaled = values ? vscales : kscales;
     const int ring = values ? C::kRingV : C::kRingK, stages = values ? C::kOffRV : C::kOffRK, tiles = values ? C::kOffV : C::kOffK,
               metas = values ? C::kOffVm : C::kOffKm;
     int gt = 0, slot = 0;
@@ -803,53 +830,46 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
-      if (warp < 12) {   // queries: a thread a row, all rows scaled by one power of two, the largest below 2^7 (their sums below 2^14)
-        const int c = rb * kM + (qr & (C::kRows - 1)), j = c / p.G;
-        const uint4* src = p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (c - j * p.G)) * 16;
-        const bool in = c < p.cols;
-        float amax = 0.0f, sum = 0.0f;
-        if (in) {
-#pragma unroll 4
-          for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
-        }
-        const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
-        if (lane == 0) misc[16 + 4 * qi + (warp & 3)] = (int)wmax;
-        named_bar(1, 128);
-        volatile int* qm = misc + 16 + 4 * qi;
-        const int top = max(max(qm[0], qm[1]), max(qm[2], qm[3]));
-        const int e = top > 0 ? max(-100, min(100, exponent_of(__int_as_float(top)) + 8)) : 0;
+      {   // queries: a row by a thread of each of the four warps of its part of tensor memory, 32 channels each; all rows scaled by one power of two, the
+          // largest below 2^7 (their sums below 2^14)
+        const int qr = (warp & 3) * 32 + lane, quarter = (warp - 8) >> 2, c = rb * kM + (qr & (C::kRows - 1)), in = min(c, p.cols - 1), j = in / p.G;
+        uint4 x[4];
+        load4(x, p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (in - j * p.G)) * 16 + quarter * 4, c < p.cols);
+        const float top = largest<16>(x, smem + C::kOffMisc + 64 + 32 * qi, warp - 8, lane, 1);
+        const int e = top > 0.0f ? max(-100, min(100, exponent_of(top) + 8)) : 0;
         const float f = pow2(-e);
         a = p.sm_log2 * pow2(e);
-        if (qr == 0) misc[28 + qi] = __float_as_int(a);
+        if (tid == 256) misc[4 + qi] = __float_as_int(a);
         if (gt > 0) wait(kfree + ms.before(1).i * 8, ms.before(1).ph, ab);   // the previous piece's last Q K^T
         tc_fence_after();
-        const uint32_t tm_q = tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16);
-#pragma unroll 1
-        for (int ch = 0; ch < 16; ch += 4) {
-          uint32_t w[16];
+        uint32_t w[16];
+        float sum = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (in) x = ld_dep(src + ch + i);
-            sum += ((bf_lo(x.x) + bf_hi(x.x)) + (bf_lo(x.y) + bf_hi(x.y))) + ((bf_lo(x.z) + bf_hi(x.z)) + (bf_lo(x.w) + bf_hi(x.w)));
-            x = scaled8(x, f);
-            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-          }
-          TmemRegs<16>::st(tm_q + ch * 4, w);
+        for (int i = 0; i < 4; ++i) {
+          sum += ((bf_lo(x[i].x) + bf_hi(x[i].x)) + (bf_lo(x[i].y) + bf_hi(x[i].y))) + ((bf_lo(x[i].z) + bf_hi(x[i].z)) + (bf_lo(x[i].w) + bf_hi(x[i].w)));
+          const uint4 y = scaled8(x[i], f);
+          w[4 * i] = y.x; w[4 * i + 1] = y.y; w[4 * i + 2] = y.z; w[4 * i + 3] = y.w;
         }
-        const uint32_t both = two_parts(sum * f);   // against a token's {mid hi, mid lo, mid hi}: sum hi, sum hi, sum lo
-        sts128(sbase + C::kOffSum + (uint32_t)qr * 16u, __byte_perm(both, both, 0x1010), both >> 16, 0u, 0u);
+        TmemRegs<16>::st(tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16) + quarter * 16, w);
+        const uint32_t sums = sbase + C::kOffSum + (uint32_t)qr * 16u;   // (the quarters' first, then what the products take)
+        sts32(sums + quarter * 4u, __float_as_uint(sum * f));
         tc_wait_st();
-        proxy_fence();
         tc_fence_before();
-        __syncwarp();
+        named_bar(1, 512);
+        if (quarter == 0) {
+          const uint2 s01 = lds64(sums), s23 = lds64(sums + 8u);
+          const uint32_t both = two_parts((__uint_as_float(s01.x) + __uint_as_float(s01.y)) + (__uint_as_float(s23.x) + __uint_as_float(s23.y)));
+          sts128(sums, __byte_perm(both, both, 0x1010), both >> 16, 0u, 0u);   // against a token's {mid hi, mid lo, mid hi}: sum hi, sum hi, sum lo
+          proxy_fence();
+          __syncwarp();
+        }
         if (lane == 0) mbar_arrive(qready + qi * 8);
       }
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gt, ms.next()) {
         const int ut = u0 + u, g = gt & 1;
         const uint32_t tile = sbase + (uint32_t)(tiles + g * 32768);
-        wait(mready + (gt & 7) * 8, (gt >> 3) & 1, ab);
+        wait(scaled + ms.i * 8, ms.ph, ab);
         if (values) wait(vfree + g * 8, ((gt >> 1) - 1) & 1, ab);                        // the tile has been used
         else if (gt > 1) wait(kfree + ms.before(2).i * 8, ms.before(2).ph, ab);
         if (ut < n_prefix) {
@@ -861,28 +881,25 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           __syncwarp();
           if (lane == 0) mbar_arrive(empty + slot * 8);
           if (++slot == ring) { slot = 0; phase ^= 1; }
-        } else if (w8 < 2) {   // the nodes' keys or values: a thread a row, all scaled by one power of two
-          const uint4* src = (values ? p.vt + ((int64_t)b * p.n + row) * p.vt_stride : p.kt + ((int64_t)b * p.n + row) * p.kt_stride) + h * 16;
-          const bool used = node_used(p, b, row, lane);
-          float amax = 0.0f;
-          if (used) {
-#pragma unroll 4
-            for (int ch = 0; ch < 16; ++ch) amax = fmaxf(amax, absmax8(ld_dep(src + ch)));
+        } else {   // the nodes' keys or values: a row by a thread of each of four warps, all rows scaled by one power of two
+          const int row = (w8 & 1) * 32 + lane, quarter = w8 >> 1, in = min(row, p.n - 1);
+          const int64_t node = (int64_t)b * p.n + in;
+          uint4 x[4];
+          load4(x, (values ? p.vt + node * p.vt_stride : p.kt + node * p.kt_stride) + h * 16 + quarter * 4, node_used(p, b, row, lane));
+          const int e = tile_exponent(__float_as_int(largest<8>(x, smem + C::kOffMisc + (values ? 48 : 32), w8, lane, values ? 3 : 8)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint4 w = scaled8(x[i], pow2(-e));
+            sts128(chunk_at(tile, row, quarter * 4 + i), w.x, w.y, w.z, w.w);
           }
-          const uint32_t wmax = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax));
-          volatile int* most = misc + 8 + 2 * (values ? 1 : 0);
-          if (lane == 0) most[w8] = (int)wmax;
-          named_bar(values ? 3 : 8, 64);
-          const int e = tile_exponent(max(most[0], most[1]));
-          named_bar(values ? 3 : 8, 64);   // (read by both)
-          if (!values) sts32(sbase + (uint32_t)(C::kOffFactor + (ms.i + (int)ms.ph * kSlots) * 512 + row * 4), __float_as_uint(times_pow2(a, e)));
-          else if (row == 0) misc[32 + (gt & 7)] = e;
-#pragma unroll 2
-          for (int ch = 0; ch < 16; ++ch) {
-            const uint4 w = used ? scaled8(ld_dep(src + ch), pow2(-e)) : make_uint4(0u, 0u, 0u, 0u);
-            sts128(chunk_at(tile, row, ch), w.x, w.y, w.z, w.w);
+          if (quarter == 0) {
+            if (!values) {
+              sts32(sbase + (uint32_t)(C::kOffFactor + (ms.i + (int)ms.ph * kSlots) * 512 + row * 4), __float_as_uint(times_pow2(a, e)));
+              sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + row * 16), 0u, 0u, 0u, 0u);
+            } else if (row == 0) {
+              misc[40 + (gt & 7)] = e;
+            }
           }
-          if (!values) sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + row * 16), 0u, 0u, 0u, 0u);
         }
         proxy_fence();   // (for the middles, too, which warp 27 has written)
         __syncwarp();
@@ -973,16 +990,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         fetch(min(t, top), first);
       }
       float a = 0.0f;
-      if (!values) {
-        wait(qready + qi * 8, (ic >> 1) & 1, ab);
-        a = __int_as_float(misc[28 + qi]);
-      }
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gt, ms.next()) {
         const int ut = u0 + u;
         // (The nodes' are made by the warps that have their keys and values.  These wait for this one all the same, so that no barrier is a phase
         // further than what a wait for it expects.)
         if (gt >= kSlots) wait(used + ms.i * 8, ms.ph ^ 1u, ab);   // the place has been read (the softmax's of eight tiles before, too)
+        uint32_t r[4] = {};
+        int exponent = 0;
         if (ut < n_prefix) {
           const int t = ut * kTile + lane * 4, room = len - t;     // (what lies behind the sequence's end may be anything)
           const uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
@@ -1005,18 +1020,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           if (values) {
             sts128(sbase + (uint32_t)(C::kOffVm + ms.i * 512 + lane * 16), pack_f16x2(sc[0], mid[0]), pack_f16x2(sc[1], mid[1]), pack_f16x2(sc[2], mid[2]),
                    pack_f16x2(sc[3], mid[3]));
-            if (lane == 0) misc[32 + (gt & 7)] = e;
+            if (lane == 0) misc[40 + (gt & 7)] = e;
           } else {   // scales of 4 bits, so that products with codes are exact, and what the scores lack; middles in units of it, in two parts
-            const float tile = times_pow2(a, e);
-            uint32_t s2[2], r[4];
+            exponent = e;
+            uint32_t s2[2];
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
               s2[i >> 1] = pack_f16x2(four_bits(sc[i]), four_bits(sc[i + 1]));
               const float2 s16 = half2_to_float2(s2[i >> 1]);
               const float r0 = s16.x != 0.0f ? __fdividef(sc[i], s16.x) : 1.0f, r1 = s16.y != 0.0f ? __fdividef(sc[i + 1], s16.y) : 1.0f;
               const float x0 = __fdividef(mid[i], r0), x1 = __fdividef(mid[i + 1], r1);
-              r[i] = __float_as_uint(tile * r0);
-              r[i + 1] = __float_as_uint(tile * r1);
+              r[i] = __float_as_uint(r0);
+              r[i + 1] = __float_as_uint(r1);
               const uint32_t hi = pack_f16x2(x0, x1);
               const float2 h2 = half2_to_float2(hi);
               const uint32_t lo = pack_f16x2(x0 - h2.x, x1 - h2.y), at = sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + lane * 64 + i * 16);
@@ -1024,6 +1039,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               sts128(at + 16u, __byte_perm(hi, lo, 0x7632), hi >> 16, 0u, 0u);
             }
             sts64(sbase + (uint32_t)(C::kOffKm + ms.i * 256 + lane * 8), s2[0], s2[1]);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive((values ? vscales : kscales) + ms.i * 8);
+        if (!values) {   // (behind the tile's scales, so that keys become a tile while the queries come)
+          if (u == 0) {
+            wait(qready + qi * 8, (ic >> 1) & 1, ab);
+            a = __int_as_float(misc[4 + qi]);
+          }
+          if (ut < n_prefix) {
+            const float f = times_pow2(a, exponent);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
             sts128(sbase + (uint32_t)(C::kOffFactor + (ms.i + (int)ms.ph * kSlots) * 512 + lane * 16), r[0], r[1], r[2], r[3]);
           }
         }

@@ -55,14 +55,15 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
     B = {}
     for name, n, count in (("kfull", ring_k, 1), ("kempty", ring_k, 2), ("vfull", ring_v, 1), ("vempty", ring_v, 2), ("kready", 2, 2), ("sfull", N, 1),
                            ("mready", 8, 2), ("vready", N, 2), ("pready", N, softmax), ("pvdone", N, 1), ("kfree", N, 1), ("vfree", 2, 1),
-                           ("ifull", 2, 1), ("iempty", 2, 2 * softmax + 7), ("qready", 2, 2), ("kdone", 2, 1)):
+                           ("ifull", 2, 1), ("iempty", 2, 2 * softmax + 7), ("qready", 2, 4), ("kdone", 2, 1), ("kscales", N, 1), ("vscales", N, 1)):
         B[name] = [Barrier(count) for _ in range(n)]
     rawk, rawv = [Place(f"raw K {i}") for i in range(ring_k)], [Place(f"raw V {i}") for i in range(ring_v)]
     S = [Place(f"S {i}") for i in range(N)]
     vm, km, mids = ([Place(f"{x} {i}") for i in range(N)] for x in ("vm", "km", "mid"))
     ktile, vtile = ([[Place(f"{x} {i} {j}") for j in range(2)] for i in range(2)] for x in ("K", "V"))
-    factor, exp = ([Place(f"{x} {i}") for i in range(8)] for x in ("a", "e"))
-    item, O, Q = [Place("item 0"), Place("item 1")], [Place("O 0"), Place("O 1")], [Place("Q 0"), Place("Q 1")]
+    factor, exp = ([Place(f"{x} {i}") for i in range(n)] for x, n in (("a", 2 * N), ("e", 8)))
+    item, O, Q = [Place("item 0"), Place("item 1")], [Place("O 0"), Place("O 1")], [Place(f"Q {i}") for i in range(4)]
+    maxima, met = [[Place(f"maxima {i} {j}") for j in range(4)] for i in range(2)], [0] * 4       # of the queries; barriers of the roles that have them
     pair = [[0, 0] for _ in range(softmax)]         # arrivals of a row's two warps at the barriers at the end of a piece
     issued = []        # products, in order, completed in order
 
@@ -75,6 +76,30 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
         yield from wait("ifull", ic & 1, ic >> 1)
         item[ic & 1].read(ic)
         return pieces[ic] if ic < len(pieces) else (0, False, False)
+
+    def meet(i):
+        met[i] += 1
+        while min(met) < met[i]:
+            yield
+
+    def queries(i, ic, gt):
+        maxima[ic & 1][i].write(ic)
+        yield from meet(i)
+        for m in maxima[ic & 1]:
+            m.read(ic)
+            m.readers += 1
+        yield
+        for m in maxima[ic & 1]:
+            m.readers -= 1
+        if gt > 0:
+            yield from wait("kfree", (gt - 1) % N, (gt - 1) // N)
+        Q[i].write(ic)
+        yield from meet(i)
+        if i == 0:
+            for q in Q:                     # (the sums of all quarters)
+                q.read(ic)
+            Q[0].write(ic)
+        B["qready"][ic & 1].arrive()
 
     def raw_tiles(n, tree):
         return n - 1 if tree else n
@@ -106,14 +131,10 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             n, tree, short = yield from get(ic)
             if n == 0:
                 return
-            if side == 0:
-                if gt > 0:
-                    yield from wait("kfree", (gt - 1) % N, (gt - 1) // N)
-                Q[0].write(ic)
-                B["qready"][ic & 1].arrive()
+            yield from queries(side, ic, gt)
             for u in range(n):
                 g = gt & 1
-                yield from wait("mready", gt & 7, gt >> 3)
+                yield from wait("kscales", gt % N, gt // N)
                 if gt > 1:
                     yield from wait("kfree", (gt - 2) % N, (gt - 2) // N)
                 if u < raw_tiles(n, tree):
@@ -128,7 +149,7 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                     slot, phase = (0, phase ^ 1) if slot + 1 == ring_k else (slot + 1, phase)
                 elif side == 0:
                     ktile[g][0].write(gt)
-                    factor[gt & 7].write(gt)
+                    factor[gt % (2 * N)].write(gt)
                     mids[gt % N].write(gt)
                 B["kready"][g].arrive()
                 gt += 1
@@ -142,14 +163,10 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             n, tree, short = yield from get(ic)
             if n == 0:
                 return
-            if side == 0:                   # (half of the queries' rows)
-                if gt > 0:
-                    yield from wait("kfree", (gt - 1) % N, (gt - 1) // N)
-                Q[1].write(ic)
-                B["qready"][ic & 1].arrive()
+            yield from queries(2 + side, ic, gt)
             for u in range(n):
                 g = gt & 1
-                yield from wait("mready", gt & 7, gt >> 3)
+                yield from wait("vscales", gt % N, gt // N)
                 yield from wait("vfree", g, (gt >> 1) - 1)
                 if u < raw_tiles(n, tree):
                     yield from wait("vfull", slot, phase)
@@ -174,14 +191,18 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
             n, tree, _ = yield from get(ic)
             if n == 0:
                 return
-            if not values:
-                yield from wait("qready", ic & 1, ic >> 1)
             for u in range(n):
                 if gt >= N:
                     yield from wait("vready" if values else "kfree", gt % N, gt // N - 1)
                 if u < raw_tiles(n, tree):
-                    for x in (vm[gt % N], exp[gt & 7]) if values else (km[gt % N], mids[gt % N], factor[gt & 7]):
+                    for x in (vm[gt % N], exp[gt & 7]) if values else (km[gt % N], mids[gt % N]):
                         x.write(gt)
+                B["vscales" if values else "kscales"][gt % N].arrive()
+                if not values:
+                    if u == 0:
+                        yield from wait("qready", ic & 1, ic >> 1)
+                    if u < raw_tiles(n, tree):
+                        factor[gt % (2 * N)].write(gt)
                 B["mready"][gt & 7].arrive()
                 gt += 1
             B["iempty"][ic & 1].arrive()
@@ -274,9 +295,9 @@ def _run(pieces, ring_k, ring_v, rng, softmax=4):
                     yield from wait("vready", t % N, t // N)
                 yield from wait("sfull", g, gs // N)
                 S[g].read(gs)
-                for p in (factor[t & 7], exp[t & 7]):
+                places = (S[g], factor[t % (2 * N)], exp[t & 7])
+                for p in places[1:]:
                     p.read(t)
-                places = (S[g], factor[t & 7], exp[t & 7])
                 for p in places:
                     p.readers += 1
                 yield
@@ -340,7 +361,7 @@ def test_the_kernel_waits_for_what_is_played():
     cuts = ["if (warp < 8) {", "if (warp < 24) {", "if (warp == 24) {", "if (warp != 26) {", "constexpr uint32_t kIdescS"]
     at = [code.index(x) for x in cuts] + [len(code)]
     waits = [sorted(set(re.findall(r"\bwait\((\w+)", code[a:b]))) for a, b in zip(at, at[1:])]
-    assert waits == [["ifull", "kdone", "mready", "pvdone", "sfull", "vready"], ["full", "ifull", "kfree", "mready", "vfree"],
+    assert waits == [["ifull", "kdone", "mready", "pvdone", "sfull", "vready"], ["full", "ifull", "kfree", "scaled", "vfree"],
                      ["iempty", "kempty", "vempty"], ["ifull", "qready", "used"], ["ifull", "kready", "pready", "qready", "vready"]]
     land, done, free = (code.index(x) for x in ("land_after_abort(", "named_bar(2, kDoneThreads)", "tcgen05.dealloc"))
     assert done < land < free and len(re.findall(r"bar_arrive\(2, kDoneThreads\)", code)) == 2
