@@ -15,7 +15,7 @@
 // (FP16 of scale (c - 128) and one factor for the tile: 5 % less time for 512 rows and two contexts of 131072 tokens, but outputs 2.4 times as far off
 // where a few channels are ten times the others.)  Queries are scaled by a power of two, exact down to 2^-24 of the row block's largest.  Values
 // enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15 (rows 2^29 times smaller keep all 11 bits; keys 2^22 their 4), weights as
-// FP16 relative to a reference that keeps each row's largest between 2^7 and 2^16 (set anew when the sum of 64 weights,
+// FP16 relative to a reference that keeps each row's largest between 2^7 and 2^16 (set anew when the sum of 16 weights,
 // which is there anyway, comes near it: no maxima): both roundings are 2^-12 of a term, an eighth of the
 // output's own rounding to BF16.  2^e goes into the weight's exponent and out of l's terms again, so that it costs nothing per weight.  Sums
 // l, references and O are FP32.
@@ -26,7 +26,8 @@
 // loads, compares and stores.  (Two threads a row instead, half of a tile of 128 tokens each, went through the same phases at the same
 // time: 141 us for 128 rows over 131072 tokens.)  Queries are the A operand of the scores in tensor memory, P goes from registers to tensor
 // memory, over the scores, as the A operand of P V; three places for scores, so that Q K^T is never waited for.
-// One CTA per SM; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
+// One CTA per SM, 72 registers a thread (16 scores at a time need no more; 32, and a split of 112 for the softmax, 56 for the others, took 541 instead of 480 us
+// for 96 rows of 16 sequences of 8192 to 65536 tokens); roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
 //   warps 0-3, 4-7   softmax, even and odd half tiles
 //   warps 8-23       codes to FP16: K tiles by those on the first two of the four schedulers, V tiles on the others (warp mod 4); all of them a piece's
 //                    queries
@@ -65,7 +66,7 @@ constexpr int kPartRow = 132;       // floats of a partial row: O[128], referenc
 constexpr int kThreads = 896;
 constexpr int kDoneThreads = 256 + 2 * 32;   // softmax warpgroups, copies, products
 // log2 of the largest of a row's weights when its reference is set; a sum of them that sets it anew (none is above it, and FP16 holds 65504)
-constexpr float kTop = 7.0f, kMost = 65000.0f, kRaise = 9.9f;   // (64 weights of 2^9.9: 61000)
+constexpr float kTop = 7.0f, kMost = 65000.0f, kRaise = 11.9f;   // (16 weights of 2^11.9: 61000)
 constexpr int kMinExp = -80;        // smallest exponent of a tile's keys or values
 
 struct TreeParams {
@@ -115,8 +116,6 @@ struct Cfg {
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024, "shared memory");
   static_assert(kOffSum % 128 == 0 && kOffBars % 8 == 0, "alignment");
-  // registers a thread after the split (launched with 72 each): 256 * 112 + 512 * 56 + 128 * 56 = 896 * 72
-  static constexpr int kRegSoft = 112, kRegExp = 56, kRegRest = 56;
   static constexpr int kTmS = 0, kTmQ = 192, kTmO = 256;             // [kSlots][64] scores, weights in their place; queries; [2][128] accumulators
 };
 // A place of kSlots and the parity of its round.
@@ -204,15 +203,6 @@ __device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, ui
 __device__ __forceinline__ void named_bar(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void tmem_load(uint32_t a, float (&x)[N]) {
-#pragma unroll
-  for (int k = 0; k < N / 16; ++k) TmemRegs<16>::ld(a + k * 16, reinterpret_cast<uint32_t*>(x) + 16 * k);
-}
-template <int N>
-__device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
   uint2 v;
   asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
@@ -583,12 +573,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
 
   // ================================================================================== softmax
   if (warp < 8) {
-    reg_inc<C::kRegSoft>();
     const int g = warp >> 2, w4 = warp & 3, r = tid & 127, bar = 4 + w4;   // (a warp's rows are shared with warp ^ 4)
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
     const uint32_t tm_o = tmem0 + C::kTmO + g * 128 + lanes;
     const int t0 = (r / C::kRows) * C::kW;                                 // this thread's first token of a tile
-    constexpr int kCW = C::kW < 32 ? C::kW : 32;                           // scores at a time
     float2* ml = reinterpret_cast<float2*>(smem + C::kOffMl);
     int gt = 0, gs = 0;   // tiles and half tiles so far
     Slot s;               // of this warpgroup's next half tile
@@ -652,32 +640,27 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           constexpr int kP = C::kW / 2;                  // columns of a thread's weights, from position ts * kP on
           const uint32_t tm_p = tm_s + (r / C::kRows) * kP;
           float sum = 0.0f;
-          bool plain = settled && !tree && valid >= C::kW;
-          if (plain) {
-            uint32_t w[kP];
-            float x[kCW], y[kCW];   // (the second chunk is on its way during the first one's exponentials)
-            tmem_load(tm_s + t0, x);
-            tc_wait_ld();
-            if constexpr (C::kW > kCW) tmem_load(tm_s + t0 + kCW, y);
-            scores(x, 0, shift);
-            sum = weights(x, w);
-            if constexpr (C::kW > kCW) {
+          int done = 0;   // scores whose weights lie in place: 16 at a time, over scores that have been read
+          if (settled && !tree && valid >= C::kW) {
+#pragma unroll 1
+            for (; done < C::kW; done += 16) {
+              float x[16];
+              uint32_t w[8];
+              TmemRegs<16>::ld(tm_s + t0 + done, reinterpret_cast<uint32_t*>(x));
               tc_wait_ld();
-              scores(y, kCW, shift);
-              sum += weights(y, w + kCW / 2);
-            }
-            plain = !__any_sync(0xFFFFFFFFu, !(sum <= kMost));
-            if (plain) {
-#pragma unroll
-              for (int i = 0; i < kP; i += 8) TmemRegs<8>::st(tm_p + i, w + i);
+              scores(x, done, shift);
+              const float part = weights(x, w);
+              if (__any_sync(0xFFFFFFFFu, !(part <= kMost))) break;
+              TmemRegs<8>::st(tm_p + done / 2, w);
+              sum += part;
             }
           }
-          if (__builtin_expect(!plain, 0)) {
-            // A mask, no reference yet, or weights that FP16 might not hold: 16 scores at a time, first their largest; with a new reference
-            // what the piece has so far is scaled.
+          if (__builtin_expect(done < C::kW, 0)) {
+            // A mask, no reference yet, or weights that FP16 might not hold: first the largest of the scores that are left; with a new reference
+            // what the piece has so far is scaled, and this half tile's weights.
             const unsigned long long see = tree ? (c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) >> t0 : 0ull) : ~0ull;
             auto chunk = [&](float (&x)[16], int ch, float less) {
-              tmem_load(tm_s + t0 + ch, x);
+              TmemRegs<16>::ld(tm_s + t0 + ch, reinterpret_cast<uint32_t*>(x));
               tc_wait_ld();
               scores(x, ch, less);
               const int room = valid - ch;
@@ -688,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             };
             float mx = -INFINITY;
 #pragma unroll 1
-            for (int ch = 0; ch < C::kW; ch += 16) {
+            for (int ch = done; ch < C::kW; ch += 16) {
               float x[16];
               chunk(x, ch, shift);
 #pragma unroll
@@ -699,6 +682,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             if (need) { ref += delta; fresh = false; }
             if (__any_sync(0xFFFFFFFFu, f != 1.0f)) {
               l *= f;
+              sum *= f;
+              tc_wait_st();
+#pragma unroll 1
+              for (int ch = 0; ch < done; ch += 16) {
+                uint32_t w[8];
+                TmemRegs<8>::ld(tm_p + ch / 2, w);
+                tc_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const float2 x = half2_to_float2(w[k]);
+                  w[k] = pack_f16x2(x.x * f, x.y * f);
+                }
+                TmemRegs<8>::st(tm_p + ch / 2, w);
+              }
               const Slot prev = s.before(2);   // (a row that has a reference has had a half tile)
               wait(pvdone + prev.i * 8, prev.ph, ab);
               tc_fence_after();
@@ -713,9 +710,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               }
             }
             settled = !__any_sync(0xFFFFFFFFu, fresh);
-            sum = 0.0f;
 #pragma unroll 1
-            for (int ch = 0; ch < C::kW; ch += 16) {
+            for (int ch = done; ch < C::kW; ch += 16) {
               float x[16];
               uint32_t w[8];
               chunk(x, ch, shift - delta);
@@ -814,7 +810,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   }
   // ================================================================================== codes to FP16, and queries
   if (warp < 24) {
-    reg_dec<C::kRegExp>();
     const bool values = (warp & 2) != 0;
     const int w8 = ((warp - 8) >> 2) * 2 + (warp & 1);
     const uint32_t full = values ? vfull : kfull, empty = values ? vempty : kempty, scaled = values ? vscales : kscales;
@@ -912,7 +907,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     }
     return;
   }
-  reg_dec<C::kRegRest>();
   // ================================================================================== copies
   if (warp == 24) {
     Cursor cur = first_unit(p, blockIdx.x, gridDim.x, lane);
