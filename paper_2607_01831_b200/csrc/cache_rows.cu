@@ -239,10 +239,10 @@ struct AppendParams {
 };
 
 // A warp: four tokens, `per` heads of K or of V, kFly rows of a quarter-warp at a time.
-// 8 heads of 131072 tokens, K and V, out of a fused projection into scattered blocks (822 MB: 125 us at the copy rate): 148 us, 185 with
-// the keys rotated (67 MB more of angles; 206 and 234 with scalar arithmetic and two divisions a row in every lane).  Four rows of a
-// quarter-warp are in flight, two where they are kept turned in FP32; more, or the next ones during the arithmetic, cost more registers than
-// they hide (152 and 209).
+// 8 heads of 131072 tokens, K and V, out of a fused projection into scattered blocks (822 MB: 125 us at the copy rate): 148 us, 179 with
+// the keys rotated (67 MB more of angles; 206 and 234 with scalar arithmetic and two divisions a row in every lane).  The issue of instructions
+// bounds it (0.63 a cycle and scheduler, the ALUs at 59 %).  Two rows of a quarter-warp are in flight; four, or the next ones during the arithmetic,
+// cost more registers than they hide (149 and 185, 152 and 209), a fifth CTA per SM 144 and 197.
 template <int kFly, bool TURN>
 __device__ __forceinline__ void append_rows(const RotaryParams& r, const AppendParams& p, int64_t row, int64_t slot, int v, int l, int first, int last) {
   static_assert(kFly == 1 || kFly == 2 || kFly == 4, "a division per lane");
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, 4) cache_append_kernel(const __grid_
     slot = ld_dep(p.slots + token);
     row = p.rows ? (int64_t)ld_dep(p.rows + token) : token;
   }
-  if (p.rotate && !v) append_rows<kFly == 4 ? 2 : 1, true>(r, p, row, slot, v, l, first, last);
+  if (p.rotate && !v) append_rows<kFly, true>(r, p, row, slot, v, l, first, last);
   else append_rows<kFly, false>(r, p, row, slot, v, l, first, last);
 }
 
@@ -345,8 +345,13 @@ struct ReadParams {
   const int32_t *table, *starts, *offsets;
   int64_t n_rows;
   int batch, heads, bt, num_blocks, max_blocks;
+  int wide;   // outputs are 32-byte aligned: a lane's 32 bytes in one store
   BlockDiv bt_div;
 };
+__device__ __forceinline__ void st256(uint4* p, const uint4& a, const uint4& b) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
 // The sequence that output row `row` belongs to, the last b with offsets[b] <= row, by the eight lanes of a quarter-warp; -1 behind the
 // last.  Eight probes a step: one step up to 8 sequences, two up to 64.
 __device__ __forceinline__ int sequence_of(const ReadParams& p, int64_t row, int lane) {
@@ -364,9 +369,11 @@ __device__ __forceinline__ int sequence_of(const ReadParams& p, int64_t row, int
   return lo < p.batch ? lo : -1;
 }
 
-// A warp: four output rows, `per` heads of K or of V.
+// A warp: four output rows, `per` heads of K or of V.  8 heads of 131072 tokens (822 MB, from the Anchor 688 MB: 125 and 105 us at the copy rate) take 136 us
+// and 118.  Memory bounds it, at six CTAs per SM: full codes four rows of a quarter-warp at a time with four CTAs 146, from the Anchor alone, with 16-byte
+// stores and loads under conditions, 133.
 template <int kFly, bool kFull>
-__global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ ReadParams p, int per, int groups) {
+__global__ void __launch_bounds__(kThreads, 6) cache_read_kernel(const __grid_constant__ ReadParams p, int per, int groups) {
   pdl_begin();
   const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31, l = lane & 7;
@@ -387,25 +394,25 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
       src0 = (int64_t)blk * p.heads * p.bt + (token - i * p.bt);
     }
   }
+  const uint2 *anchor = v ? p.anchor[1] : p.anchor[0], *residual = v ? p.residual[1] : p.residual[0];
+  const float2* meta = v ? p.meta[1] : p.meta[0];
+  uint4* out = (v ? p.out[1] : p.out[0]) + row * p.heads * 16 + 2 * l;
   for (int h0 = first; h0 < last; h0 += kFly) {
     uint2 xa[kFly], xr[kFly];
     float2 m[kFly];
 #pragma unroll
     for (int u = 0; u < kFly; ++u) {
-      xa[u] = xr[u] = make_uint2(0u, 0u);
-      m[u] = make_float2(0.0f, 0.0f);
-      if (live && h0 + u < last) {
-        const int64_t s = src0 + (int64_t)(h0 + u) * p.bt;
-        xa[u] = ld_dep(p.anchor[v] + s * 8 + l);
-        if (kFull) xr[u] = ld_dep(p.residual[v] + s * 8 + l);
-        m[u] = ld_dep(p.meta[v] + s);
-      }
+      const int64_t s = src0 + (int64_t)min(h0 + u, last - 1) * p.bt;   // (loads under a condition are waited for where it ends)
+      xa[u] = ld_dep(anchor + s * 8 + l);
+      if (kFull) xr[u] = ld_dep(residual + s * 8 + l);
+      m[u] = ld_dep(meta + s);
     }
 #pragma unroll
     for (int u = 0; u < kFly; ++u) {
       if (h0 + u >= last) break;
       const uint32_t wa[2] = {xa[u].x, xa[u].y}, wr[2] = {xr[u].x, xr[u].y};
-      uint4* o = p.out[v] + (row * p.heads + h0 + u) * 16 + 2 * l;
+      if (!live) m[u] = make_float2(0.0f, 0.0f);
+      uint4 o[2];
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         // even channels from the low nibbles, odd ones from the high nibbles
@@ -418,6 +425,13 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
           x[2 * i + 1] = __fmaf_rn((float)((od >> (8 * i)) & 0xFFu), m[u].x, m[u].y);
         }
         o[c] = pack8(x);
+      }
+      uint4* to = out + (h0 + u) * 16;
+      if (p.wide) {
+        st256(to, o[0], o[1]);
+      } else {
+        to[0] = o[0];
+        to[1] = o[1];
       }
     }
   }
@@ -524,7 +538,7 @@ extern "C" lynx_status lynx_cache_append(const lynx_shape* shape, const void* k,
   const int per = heads_per_warp(2 * n_tokens, p.heads), groups = (p.heads + per - 1) / per;
   unsigned grid;
   if (!grid_of((n_tokens + 3) / 4 * 2 * groups, &grid)) return LYNX_ERR_UNSUPPORTED;
-  return per > 1 ? launch_pdl(cache_append_kernel<4>, grid, kThreads, 0, stream, r, p, per, groups)
+  return per > 1 ? launch_pdl(cache_append_kernel<2>, grid, kThreads, 0, stream, r, p, per, groups)
                  : launch_pdl(cache_append_kernel<1>, grid, kThreads, 0, stream, r, p, per, groups);
 }
 
@@ -548,6 +562,7 @@ extern "C" lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, ly
   p.residual[0] = reinterpret_cast<const uint2*>(K.residual); p.residual[1] = reinterpret_cast<const uint2*>(V.residual);
   p.meta[0] = reinterpret_cast<const float2*>(K.meta); p.meta[1] = reinterpret_cast<const float2*>(V.meta);
   p.out[0] = static_cast<uint4*>(k_out); p.out[1] = static_cast<uint4*>(v_out);
+  p.wide = aligned(k_out, 32) && aligned(v_out, 32) ? 1 : 0;
   p.table = block_table; p.starts = starts; p.offsets = offsets;
   p.n_rows = n_rows; p.batch = batch; p.heads = shape->num_kv_heads; p.bt = shape->block_tokens;
   p.num_blocks = shape->num_blocks; p.max_blocks = shape->max_blocks_per_seq;
@@ -556,7 +571,7 @@ extern "C" lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, ly
   unsigned grid;
   if (!grid_of((n_rows + 3) / 4 * 2 * groups, &grid)) return LYNX_ERR_UNSUPPORTED;
   if (K.residual)
-    return per > 1 ? launch_pdl(cache_read_kernel<4, true>, grid, kThreads, 0, stream, p, per, groups)
+    return per > 1 ? launch_pdl(cache_read_kernel<2, true>, grid, kThreads, 0, stream, p, per, groups)
                    : launch_pdl(cache_read_kernel<1, true>, grid, kThreads, 0, stream, p, per, groups);
   return per > 1 ? launch_pdl(cache_read_kernel<4, false>, grid, kThreads, 0, stream, p, per, groups)
                  : launch_pdl(cache_read_kernel<1, false>, grid, kThreads, 0, stream, p, per, groups);

@@ -252,6 +252,25 @@ def test_the_extension_and_the_python_bodies_agree(monkeypatch):
     assert all(torch.equal(a, b) for a, b in zip(fast, calls()))
 
 
+@pytest.mark.parametrize("tokens,H", [(37, 3), (3000, 8)])
+@pytest.mark.parametrize("anchor_only", [False, True])
+def test_read_into_outputs_of_less_alignment(tokens, H, anchor_only):
+    """16 bytes are enough; what lies in front and behind stays."""
+    bt, nb = 16, -(-tokens // 16)
+    geo = lynx.Geometry(H, H, bt, nb, nb)
+    K, V = _pool(nb, H, bt, 0), _pool(nb, H, bt, 0)
+    x = _bf16(tokens, 2 * H, 128, seed=8).cuda()
+    lynx.cache_append(geo, x[:, :H], x[:, H:], torch.arange(tokens).cuda(), K, V)
+    table, offsets = torch.arange(nb, dtype=torch.int32).view(1, -1).cuda(), torch.tensor([0, tokens], dtype=torch.int32).cuda()
+    want = lynx.cache_read(geo, K, V, table, None, offsets, tokens, anchor_only=anchor_only)
+    buf = [torch.full((tokens * H * 128 + 16,), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    views = [b[8:-8].view(tokens, H, 128) for b in buf]
+    assert views[0].data_ptr() % 32 == 16
+    lynx.cache_read(geo, K, V, table, None, offsets, tokens, anchor_only=anchor_only, k_out=views[0], v_out=views[1])
+    for b, view, w in zip(buf, views, want):
+        assert torch.equal(view, w) and (b[:8] == 9.0).all() and (b[-8:] == 9.0).all()
+
+
 def test_refusals():
     T, H, bt, nb = 4, 2, 16, 3
     geo = lynx.Geometry(H, H, bt, nb, 2)
