@@ -1,9 +1,9 @@
 // lynx_tree_attention: attention of a tree of drafted tokens over the quantised cache and over each other (sm_100a).
 //
-// Up to 32 rows per (sequence, KV head) the prefix goes through the kernels for chains and a small one adds the nodes: those have a stage for each step and
-// exact integer products, and take a third to nine tenths of the time (us, 8 KV heads, full codes, rows 4 / 16 / 32, this kernel's in brackets: one
-// sequence of 4096 tokens 11.7 / 14.9 / 17.5 (19.2 / 21.0 / 23.3), 131072 tokens 56 / 60 / 89 (99 / 102 / 106), 16 sequences of 8192 to 65536
-// 217 / 232 / 331 (393 / 415 / 440)); from 33 rows on they take several passes, or more time for one (48 rows of that mix 497 against 452).  See tree_plan.
+// Up to 32 rows per (sequence, KV head) the work goes to the kernels for chains, whose joining kernel then attends to the nodes as well (attention_nodes.cuh):
+// they have a stage for each step and exact integer products (us, 8 KV heads, full codes, 4 / 16 / 32 rows, this kernel's in brackets: one sequence of
+// 4096 tokens 9.8 / 13.3 / 15.8 (15.3 / 16.5 / 18.5), of 131072 54 / 57 / 86 (89 / 92 / 101), 16 of 8192 to 65536 217 / 232 / 331 (390 / 404 / 422)).
+// From 33 rows on they take several passes, or more time for one (48 rows of that mix 510 against 433).  See tree_plan.
 //
 // For every (sequence, KV head) the n nodes' G = Hq / Hkv query heads are n * G rows; they share the head's keys and values:
 //   S = Q K^T,   p = 2^(a S + e - ref_r),   O += P V,   l += sum p,   out = O / l
@@ -14,7 +14,7 @@
 // sum(q), both in two FP16 parts (2^-22).  What a score lacks, scale / s4, is a factor of its token in the softmax's one multiply-add per score, in FP32.
 // (FP16 of scale (c - 128) and one factor for the tile: 5 % less time for 512 rows and two contexts of 131072 tokens, but outputs 2.4 times as far off
 // where a few channels are ten times the others.)  Queries are scaled by a power of two, exact down to 2^-24 of the row block's largest.  Values
-// enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15 (rows 2^29 times smaller keep all 11 bits; keys 2^22 their 4), weights as
+// enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15 (rows 2^29 times smaller keep all 11 bits; scales of keys 2^26 times smaller their 4), weights as
 // FP16 relative to a reference that keeps each row's largest between 2^7 and 2^16 (set anew when the sum of 16 weights,
 // which is there anyway, comes near it: no maxima): both roundings are 2^-12 of a term, an eighth of the
 // output's own rounding to BF16.  2^e goes into the weight's exponent and out of l's terms again, so that it costs nothing per weight.  Sums
@@ -23,7 +23,7 @@
 // Layout: rows are the M = 128 lanes of tensor memory (n * G > 128 rows: more row blocks), tokens the N of the scores and the K of
 // P V.  A thread owns a row of half a tile: no exchange between threads for maxima and sums.  Two warpgroups take the halves in turn, each with
 // references, sums and accumulators of its own, joined at the end of a piece: while one waits for the special function unit, the other
-// loads, compares and stores.  (Two threads a row instead, half of a tile of 128 tokens each, went through the same phases at the same
+// loads, compares and stores.  (In an early version two threads a row, half of a tile of 128 tokens each, went through the same phases at the same
 // time: 141 us for 128 rows over 131072 tokens.)  Queries are the A operand of the scores in tensor memory, P goes from registers to tensor
 // memory, over the scores, as the A operand of P V; three places for scores, so that Q K^T is never waited for.
 // One CTA per SM, 72 registers a thread (16 scores at a time need no more; 32, and a split of 112 for the softmax, 56 for the others, took 541 instead of 480 us
@@ -34,11 +34,15 @@
 //   warp 24          copies of the planes into rings, four 16-token sub-blocks at a time; deals out the pieces
 //   warps 25, 27     scales and zero points of a tile's values and keys: what the tiles and the softmax need of them
 //   warp 26          issues every tcgen05.mma: Q K^T three half tiles ahead of P V
-// What bounds it is the issue of instructions and how they come: the roles of a scheduler share an instruction cache of some 12 KB, hence rolled
-// loops, one copy of what is rare (masks, a new reference), few roles on a scheduler, and short loops where a barrier is waited for.  Between
+// Measured (32 nodes, 128 rows, 131072 tokens, 8 KV heads: 286 MB, 69 GFLOP): 110 us in a burst, 2.6 TB/s and 630 TFLOP/s, 123 among many, since the
+// chip then runs at its power limit, 992 W, at 1.67 GHz.  What bounds it is the issue of instructions and how they come: 8500 warp instructions a
+// tile, 0.67 a cycle and scheduler, the tensor pipe 32 % and the ALUs 41 % of the time.  The roles of a scheduler share an instruction cache of some
+// 12 KB, hence rolled loops, one copy of what is rare (masks, a new reference), few roles on a scheduler, and short loops where a barrier is
+// waited for: code that runs once a piece, unrolled beside them, cost up to 12 %.  Between
 // the warps that expand codes tiles have 128 tokens, since a hand-off costs its roles some 500 cycles whatever it hands over; 64 where
 // tensor memory has no room for more.  The copy engine takes some 35 cycles per row of a copy, and a lane that issues copies of one
-// sub-block each some 80: hence gathers, and plain loads, a tile ahead, of the scales.
+// sub-block each some 80: hence gathers, and plain loads, a tile ahead, of the scales.  A piece costs some 9 us besides its tiles, latencies in a row; a row
+// of queries or nodes is loaded once, a quarter by each of four warps.
 // Work is cut in stream-K form: the (sequence, KV head, row block, tile) list into equal ranges, a piece being a range's part of one
 // segment.  A segment within one CTA is written by it; otherwise partial (ref, l, O) go to the workspace and a dependent
 // kernel joins them.
@@ -1250,7 +1254,7 @@ lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
   }
   const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   // Few rows, where the kernels for chains take one pass over the planes, or two over the Anchor and there is enough of it, eight tiles per SM (us, 24
-  // rows, two passes / the tree kernel: 16 sequences of 8192 to 65536 tokens 325 / 409, one of 131072 95 / 102, of 4096 29 / 19).
+  // rows, two passes / the tree kernel: 16 sequences of 8192 to 65536 tokens 330 / 417, one of 131072 94 / 97, of 4096 29 / 17).
   const int passes = (n + kNodesCols / G - 1) / (kNodesCols / G);
   pl->few[0] = passes == 1 || (passes == 2 && (int64_t)B * s->num_kv_heads * (tiles - 1) >= 8 * sms);
   pl->few[1] = pl->cols <= 32 && n <= kWsMaxQ;
