@@ -1136,10 +1136,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   }
 }
 
-// Joins the partial results of the CTAs that share a segment: W warps per output row, its slots dealt to them, six on their way each, a lane four
-// channels.  (Four warps where segments are few and have many slots each: 13 nodes of 4 heads over 4096 tokens, 34 slots, 18.6 us, 19.5 with a warp per row.)
+// Joins the partial results of the CTAs that share a segment: W warps per output row, its slots dealt to them, FLY on their way each, a lane four
+// channels.  (Four warps where segments are few and have many slots each: 13 nodes of 4 heads over 4096 tokens, 34 slots, 18.6 us, 19.5 with a warp per row.
+// Where rows lie in several lanes and have as many parts a slot, nine on their way: 17.2 -> 16.1 us; 96 rows and two sequences of 16000 39.9 -> 40.2.)
 constexpr int kCombineWarps = 4;
-template <int W>
+template <int W, int FLY>
 __global__ void __launch_bounds__(kCombineWarps * 32) tree_combine_kernel(const __grid_constant__ TreeParams p, int n_cta, int log_ts) {
   pdl_trigger();
   const int64_t row = W == 1 ? (int64_t)blockIdx.x * kCombineWarps + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
@@ -1173,26 +1174,25 @@ __global__ void __launch_bounds__(kCombineWarps * 32) tree_combine_kernel(const 
     L *= f0;
     acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
   };
-  constexpr int kFly = 6;
-  for (int i0 = warp; i0 < n; i0 += W * kFly) {
-    float4 o[kFly];
-    float2 ml[kFly];
+  for (int i0 = warp; i0 < n; i0 += W * FLY) {
+    float4 o[FLY];
+    float2 ml[FLY];
 #pragma unroll
-    for (int u = 0; u < kFly; ++u) {
+    for (int u = 0; u < FLY; ++u) {
       const int i = min(i0 + u * W, n - 1);   // (loads under a condition are waited for where it ends)
       const float* x = src + (i >> log_ts) * slot + (i & ts) * part;
       ml[u] = ld_dep(reinterpret_cast<const float2*>(x + 128));
       o[u] = ld_dep(reinterpret_cast<const float4*>(x) + lane);
     }
 #pragma unroll
-    for (int u = 0; u < kFly; ++u)
+    for (int u = 0; u < FLY; ++u)
       if (i0 + u * W >= n) ml[u].x = -INFINITY;
     const float m0 = M;
 #pragma unroll
-    for (int u = 0; u < kFly; ++u) M = fmaxf(M, ml[u].x);
+    for (int u = 0; u < FLY; ++u) M = fmaxf(M, ml[u].x);
     raise(m0);
 #pragma unroll
-    for (int u = 0; u < kFly; ++u) join(ml[u], o[u]);
+    for (int u = 0; u < FLY; ++u) join(ml[u], o[u]);
   }
   if (W > 1) {
     if (warp > 0) o_s[warp][lane] = acc;
@@ -1376,6 +1376,8 @@ extern "C" lynx_status lynx_tree_attention(const lynx_shape* shape, const void* 
                          : pl.log_ts == 1 ? (K.residual ? launch_tree<true, 2>(p, pl.grid, stream) : launch_tree<false, 2>(p, pl.grid, stream))
                                           : (K.residual ? launch_tree<true, 4>(p, pl.grid, stream) : launch_tree<false, 4>(p, pl.grid, stream));
   if (st != LYNX_OK || pl.whole) return st;
-  if (pl.segs * 4 <= pl.grid) return launch_pdl(tree_combine_kernel<kCombineWarps>, (unsigned)rows, kCombineWarps * 32, 0, stream, p, pl.grid, pl.log_ts);
-  return launch_pdl(tree_combine_kernel<1>, (unsigned)((rows + kCombineWarps - 1) / kCombineWarps), kCombineWarps * 32, 0, stream, p, pl.grid, pl.log_ts);
+  if (pl.segs * 4 <= pl.grid)
+    return launch_pdl(pl.log_ts ? tree_combine_kernel<kCombineWarps, 9> : tree_combine_kernel<kCombineWarps, 6>, (unsigned)rows, kCombineWarps * 32, 0, stream, p,
+                      pl.grid, pl.log_ts);
+  return launch_pdl(tree_combine_kernel<1, 6>, (unsigned)((rows + kCombineWarps - 1) / kCombineWarps), kCombineWarps * 32, 0, stream, p, pl.grid, pl.log_ts);
 }
