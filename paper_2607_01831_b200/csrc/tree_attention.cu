@@ -1253,10 +1253,11 @@ lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
     if (pl->segs <= pl->grid && pl->grid / pl->segs * pl->segs * 100 >= 85ll * pl->grid) pl->per_seg = (int)(pl->grid / pl->segs);
   }
   const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  // Few rows, where the kernels for chains take one pass over the planes, or two over the Anchor and there is enough of it, eight tiles per SM (us, 24
-  // rows, two passes / the tree kernel: 16 sequences of 8192 to 65536 tokens 330 / 417, one of 131072 94 / 97, of 4096 29 / 17).
+  // Few rows, where the kernels for chains take one pass over the planes, or two over the Anchor and there is enough of it: 128 tiles per SM in the tables.
+  // (us, 20 rows, two passes / the tree kernel: 16 sequences of 8192 to 65536 tokens 325 / 417, 8 of 131072 512 / 751, one 92 / 95, 64 of 500 to 4096
+  // 176 / 168, one of 32768 40 / 34; 4 of 32768 95 / 104.)
   const int passes = (n + kNodesCols / G - 1) / (kNodesCols / G);
-  pl->few[0] = passes == 1 || (passes == 2 && (int64_t)B * s->num_kv_heads * (tiles - 1) >= 8 * sms);
+  pl->few[0] = passes == 1 || (passes == 2 && (int64_t)B * s->num_kv_heads * (tiles - 1) >= 128 * sms);
   pl->few[1] = pl->cols <= 32 && n <= kWsMaxQ;
   const size_t own = lynx_workspace_bytes(s, B, n);
   if (own == 0) pl->few[0] = pl->few[1] = 0;

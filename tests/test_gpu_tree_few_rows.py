@@ -14,7 +14,17 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("anchor", [False, True])
 def test_where_the_way_changes(n, G, anchor):
     _check(Problem((1000, 17), n, 2, G, seed=n * G), anchor=anchor)
-    _check(Problem((21000, 4000), n, 4, G, seed=n * G + 1), anchor=anchor)     # (enough tiles for two passes over the Anchor)
+    _check(Problem((21000, 4000), n, 4, G, seed=n * G + 1), anchor=anchor)     # (several tiles a CTA)
+
+
+@pytest.mark.parametrize("n,G", [(17, 1), (32, 1), (9, 2), (16, 2), (6, 3), (5, 4), (8, 4), (6, 5), (4, 7), (3, 8), (4, 8), (2, 11), (2, 16)])
+@pytest.mark.parametrize("lens,Hkv", [((3000, 700), 4), ((0, 1, 129, 16), 2), ((200,) * 50, 1)])
+def test_two_passes_over_the_anchor(n, G, lens, Hkv):
+    """17 to 32 rows where the tables have room for 128 tiles per SM."""
+    wide = 128 * 160 * 8 // (len(lens) * Hkv)
+    pr = Problem(lens, n, Hkv, G, seed=n * G, extra_blocks=wide)
+    _check(pr, anchor=True)
+    _check(pr, anchor=True, out_f32=True)
 
 
 @pytest.mark.parametrize("n,G", [(1, 4), (4, 4), (7, 4), (16, 1), (16, 2)])
