@@ -9,6 +9,7 @@
 #include <cuda_bf16.h>
 
 #include "block_division.cuh"
+#include "cache_place.cuh"
 #include "lynx_common.cuh"
 
 namespace lynx {
@@ -382,16 +383,12 @@ __global__ void __launch_bounds__(kThreads, 6) cache_read_kernel(const __grid_co
   const int g = (int)(w - quad * 2 * groups), v = g >= groups, first = (g - v * groups) * per, last = min(first + per, p.heads);
   const int b = sequence_of(p, row, lane);
   if (row >= p.n_rows) return;
-  bool live = b >= 0;
-  int64_t src0 = 0;
-  if (live) {
+  CacheRow src = {0, false};   // (the loads below have no condition: a dead row's go to row 0)
+  if (b >= 0) {
     const int64_t token = row - ld_dep(p.offsets + b) + (p.starts ? (int64_t)ld_dep(p.starts + b) : 0);
-    live = token >= 0 && token < (int64_t)p.max_blocks * p.bt;
-    if (live) {
+    if (in_table(token, p.max_blocks, p.bt)) {
       const int64_t i = block_of(token, p.bt, p.bt_div);
-      const int32_t blk = ld_dep(p.table + (int64_t)b * p.max_blocks + i);
-      live = blk >= 0 && blk < p.num_blocks;
-      src0 = (int64_t)blk * p.heads * p.bt + (token - i * p.bt);
+      src = cache_row(true, ld_dep(p.table + (int64_t)b * p.max_blocks + i), token - i * p.bt, p.num_blocks, p.heads, p.bt);
     }
   }
   const uint2 *anchor = v ? p.anchor[1] : p.anchor[0], *residual = v ? p.residual[1] : p.residual[0];
@@ -402,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, 6) cache_read_kernel(const __grid_co
     float2 m[kFly];
 #pragma unroll
     for (int u = 0; u < kFly; ++u) {
-      const int64_t s = src0 + (int64_t)min(h0 + u, last - 1) * p.bt;   // (loads under a condition are waited for where it ends)
+      const int64_t s = src.row + (int64_t)min(h0 + u, last - 1) * p.bt;   // (loads under a condition are waited for where it ends)
       xa[u] = ld_dep(anchor + s * 8 + l);
       if (kFull) xr[u] = ld_dep(residual + s * 8 + l);
       m[u] = ld_dep(meta + s);
@@ -411,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 6) cache_read_kernel(const __grid_co
     for (int u = 0; u < kFly; ++u) {
       if (h0 + u >= last) break;
       const uint32_t wa[2] = {xa[u].x, xa[u].y}, wr[2] = {xr[u].x, xr[u].y};
-      if (!live) m[u] = make_float2(0.0f, 0.0f);
+      if (!src.live) m[u] = make_float2(0.0f, 0.0f);
       uint4 o[2];
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
