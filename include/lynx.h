@@ -353,8 +353,8 @@ lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, lynx_plane V,
  * Precision: scores, statistics and sums are FP32 or exact integers.  With more than 32 rows n_nodes * Hq/Hkv (and where the Anchor is short)
  * keys enter the scores exactly but for their middles zero + 128 scale (2^-22 of them) and scales below 2^-36 of the largest magnitude of their
  * 128 tokens; weights and values enter the second product as FP16 relative to exponents of their own (2^-12 of a term; value rows below 2^-29 of
- * the largest of their 128 tokens lose bits).  With fewer rows queries are exact to 2^-22 of the largest and weights have 22 bits and more; a
- * value row's scale counts as 2^-80, and as 2^-24 of its zero point, at least.
+ * the largest of their 128 tokens lose bits).  With fewer rows queries are exact to 2^-22 of the largest among the rows that see a node (of
+ * their own, where that is larger) and weights have 22 bits and more; a value row's scale counts as 2^-80, and as 2^-24 of its zero point, at least.
  * workspace : lynx_tree_workspace_bytes(shape, batch, n_nodes) bytes (0: unsupported shape), zero-filled once before its first use
  * (lynx_workspace_init); each call leaves it ready for the next, also of another batch, shape or number of nodes that it is large enough for.
  * Calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of range are

@@ -28,6 +28,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "block_division.cuh"
 #include "bounded_wait.cuh"
 #include "nodes_attention.cuh"
@@ -77,7 +79,53 @@ struct AttnParams {
   int inline_merge;     // the last CTA of a segment joins its slots, not attn_combine_kernel
   float v_rel, v_least;    // see v_scale
   const NodeArgs* nodes;   // (on the host) drafted nodes to be attended to as well, or NULL
+  const unsigned long long* node_mask;   // (kernels with ROWS) [B][node_n] nodes that a query sees, from query node_j0 on
+  int node_n, node_j0;
 };
+// Queries enter as integers or FP16 parts, all columns of a piece scaled by the power of two of their largest entry.  Where they are rows of drafted trees (ROWS) some
+// may be padding, with anything in them: the largest is then that of the rows that see a node, and a row with larger entries -- one without nodes, which
+// still attends to the prefix and may be in earnest -- has a power of two of its own, its scores a factor.  Entries that are no numbers spoil their own row.
+// (BF16 maxima, two in a register: of the rows that see a node, and of all.)
+__device__ __forceinline__ uint32_t bf16x2_max(uint32_t a, uint32_t b) {
+  asm("max.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+  return a;
+}
+__device__ __forceinline__ uint32_t row_maxima(uint32_t seeing2, uint32_t all2) {
+  uint32_t m = __byte_perm(bf16x2_max(seeing2, seeing2 >> 16), bf16x2_max(all2, all2 >> 16), 0x5410);
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) m = bf16x2_max(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
+  return m;
+}
+// The largest entry of a row, a register quadruple in each of 16 lanes.
+__device__ __forceinline__ float row_largest(const uint4& w) {
+  const uint32_t m2 = bf16x2_max(bf16x2_max(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu), bf16x2_max(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu));
+  float top = fmaxf(__uint_as_float(m2 << 16), __uint_as_float(m2 & 0xFFFF0000u));
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, off));
+  return top;
+}
+// Takes a row with a power of two of its own, 2^own, to the common one and returns its scores' factor.  (Nothing is rounded but what is far below the row's largest.)
+__device__ __forceinline__ float row_to_common(uint4& w, float largest, int own, int common) {
+  const int d = largest < INFINITY ? min(common - own, 120) : 0;
+  if (d <= 0 || largest == 0.0f) return 1.0f;
+  const float f = __int_as_float((127 - d) << 23);
+  const __nv_bfloat162 f2 = __float2bfloat162_rn(f);
+  const auto times = [&](uint32_t x) {
+    const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), f2);
+    return *reinterpret_cast<const uint32_t*>(&y);
+  };
+  w = make_uint4(times(w.x), times(w.y), times(w.z), times(w.w));
+  return __int_as_float((127 + d) << 23);
+}
+// The nodes that column `lane`'s query sees (the last column's, behind it), from bits node_n on nothing; g_inv for quotients by G, see there.
+__device__ __forceinline__ unsigned long long nodes_seen(const AttnParams& p, int b, uint32_t g_inv, int lane) {
+  return ld_dep(p.node_mask + (size_t)b * p.node_n + p.node_j0 + ((uint32_t)min(lane, p.ncols - 1) * g_inv >> 16)) << (64 - p.node_n);
+}
+// The columns whose queries see a node, a bit each: all, where none does.
+__device__ __forceinline__ uint32_t columns_that_see(unsigned long long nodes) {
+  const uint32_t see = __ballot_sync(0xFFFFFFFFu, nodes != 0);
+  return see ? see : ~0u;
+}
 // A value row's scale for logarithms and quotients: at least v_rel of its zero point and v_least, since it may be 0 (then the codes are, and any does).  Chains
 // have 0 and 2^-40, so that rows of smaller scales are off by up to 2^-32; trees 2^-24 and 2^-80: by 2^-16 of themselves, or 2^-72.  (Not smaller: weights
 // times scales are dropped below 2^-126 of the largest.)
@@ -698,6 +746,9 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
   p.out = out; p.draft = full ? draft : nullptr; p.first_reject = first_reject; p.dev = dev;
   p.combine_single = 0;
   p.nodes = nullptr;
+  p.node_mask = nodes ? nodes->mask : nullptr;
+  p.node_n = nodes ? nodes->n : 0;
+  p.node_j0 = 0;
   p.v_rel = nodes ? 5.9604645e-8f : 0.0f;
   p.v_least = nodes ? 8.2718061e-25f : 9.094947e-13f;
   // Who joins the partial results: attn_combine_kernel where few heads share the grid (and for verification, which needs it for
@@ -741,7 +792,7 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
       NodeArgs slice;
       if (nodes) {
         slice = *nodes;
-        slice.j0 = j0;
+        slice.j0 = ps.node_j0 = j0;
         ps.nodes = &slice;
       }
       const lynx_status rc = ps.ncols <= 4 ? launch_pipe<false, 4>(ps, st) : ps.ncols <= 8 ? launch_pipe<false, 8>(ps, st)
@@ -767,7 +818,7 @@ lynx_status run_attention(bool full, const lynx_shape* shape, const void* q, int
     NodeArgs slice;
     if (nodes) {
       slice = *nodes;
-      slice.j0 = j0;
+      slice.j0 = ps.node_j0 = j0;
       ps.nodes = &slice;
     }
     if (p.draft) { ps.draft = p.draft + (size_t)j0 * p.Hq * LYNX_D; ps.dev = p.dev + j0; }

@@ -74,7 +74,7 @@ struct F16Cfg {
   static constexpr int kOFBytes = kIntPV ? 2 * kCG * 512 : 0;   // FP32 copy of O where tensor memory has no room for it: [group][column][128]
   static constexpr int kOffV = 0, kOffP = 2 * kVTile, kOffOF = kOffP + 2 * kPTile, kOffQ = kOffOF + kOFBytes, kOffRK = kOffQ + kQTile,
                        kOffRV = kOffRK + kRingK * kStageBytes, kOffScal = kOffRV + kRingV * kStageBytes;
-  // floats: qs[2][NC], limits[2][NC], exponents[2] (+ 2); per group: ref[32], fac[32], red[4][64], lz[64]
+  // floats: qs[2][NC], limits (ROWS: factors, see row_to_common) [2][NC], exponents[2] (+ 2); per group: ref[32], fac[32], red[4][64], lz[64]
   static constexpr int kGrpScal = 2 * 32 + 256 + 64;
   static constexpr int kOffGrp = kOffScal + (4 * NC + 4) * 4;
   // (Scalars stored as the packed pairs that the softmax takes, in two slots, spare it a tenth of its instructions and cost more in
@@ -152,6 +152,12 @@ __device__ __forceinline__ void f16_codes(uint32_t xa, uint32_t xr, uint32_t* o)
   o[1] = f16_centre(prmt(ev, 0x64646464u, 0x4341));
   o[2] = f16_centre((od & 0x00FF00FFu) | 0x64006400u);
   o[3] = f16_centre(prmt(od, 0x64646464u, 0x4341));
+}
+// Exponent of a piece's queries: the largest |q 2^e| lies in [2^14, 2^15).
+__device__ __forceinline__ int f16_q_exponent(float amax) {
+  int e = 0;
+  if (amax > 0.0f && amax < INFINITY) e = 14 - (((__float_as_int(amax) >> 23) & 0xFF) - 127);
+  return max(-100, min(100, e));
 }
 // A scaled query entry, |f| < 2^15, in two parts: f becomes a multiple of 32, lo what is left, |lo| <= 16.  The sum of 128
 // products of codes (|c - 128| <= 128) with multiples of 32 up to 2^15 stays below 2^24 times 32: exact in FP32 in any order.
@@ -418,7 +424,8 @@ struct F16Meta {
   }
 };
 
-template <int NC, bool INT>
+// ROWS: the queries are rows of drafted trees (see row_to_common).
+template <int NC, bool INT, bool ROWS = false>
 __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(const AttnParams p,
                                                                            const __grid_constant__ PlaneMaps maps) {
   using C = F16Cfg<NC, INT>;
@@ -608,6 +615,10 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
         mbar_wait_in(qready + qi * 8, (ic >> 1) & 1, abort_word);
 #pragma unroll
         for (int j = 0; j < NG; ++j) qs2[j] = *reinterpret_cast<const uint64_t*>(scal + qi * NC + col0 + 8 * j + c2);
+        const float* back_s = scal + 2 * NC + qi * NC + col0;   // (ROWS, in the place of the limits, which are all the sequence's length)
+        // APART: some column has a power of two of its own.  (A copy of the loop: a factor of 1, or a branch around it, costs 10 to 30 %.)
+        const auto units = [&](auto apart) {
+        constexpr bool APART = decltype(apart)::value;
         for (int u = u_first; u < n_piece; u += STEP, ++n_own) {
           const int gs = gs_base + u, sl = gs & 1;
           const int unit_t0 = (item.pad1 + u) * C::kST;
@@ -639,18 +650,20 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
               const uint32_t* sv = s[C::kQP == 2 ? 0 : k >> 1] + 4 * j + 2 * (k & 1);
+              uint64_t a2 = al2;
+              if constexpr (APART) a2 = f2_mul(al2, *reinterpret_cast<const uint64_t*>(back_s + 8 * j + c2));
               uint64_t rest = f2_fma(be2, qs2[j], f2_sub(lsv2, ref2[j]));
               if (C::kQP == 2) {
                 const uint32_t* lv = s[1] + 4 * j + 2 * (k & 1);
-                rest = f2_fma(f2_pack(__uint_as_float(lv[0]), __uint_as_float(lv[1])), al2, rest);
+                rest = f2_fma(f2_pack(__uint_as_float(lv[0]), __uint_as_float(lv[1])), a2, rest);
               }
-              y2[k][j] = f2_fma(f2_pack(__uint_as_float(sv[0]), __uint_as_float(sv[1])), al2, rest);
+              y2[k][j] = f2_fma(f2_pack(__uint_as_float(sv[0]), __uint_as_float(sv[1])), a2, rest);
             }
           }
           if (unit_t0 + C::kST > full_lim) {
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
-              const int la = lim_s[8 * j + c2] - unit_t0 - t0, lb = lim_s[8 * j + c2 + 1] - unit_t0 - t0;
+              const int la = (ROWS ? len : lim_s[8 * j + c2]) - unit_t0 - t0, lb = (ROWS ? len : lim_s[8 * j + c2 + 1]) - unit_t0 - t0;
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 float a, b;
@@ -764,6 +777,9 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
           if (lane == 0) { mbar_arrive(mfree + ms * 8); mbar_arrive(pready + g * 8); }
           ++units_in_acc;
         }
+        };
+        if (ROWS && __any_sync(0xFFFFFFFFu, back_s[lane] != 1.0f)) units(std::bool_constant<ROWS>());
+        else units(std::false_type());
         mbar_wait_in(pvdone + g * 8, (n_own - 1) & 1, abort_word);   // the last P.V
         drain(false);
       }
@@ -897,6 +913,8 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
         // At 64 columns they spill 72 bytes of these warps' registers, once per piece.)
         constexpr int NI = NC / 8;
         const uint32_t g_inv = 65536u / (uint32_t)p.G + 1u;   // c / G = c * g_inv >> 16 for c < 64, G <= 16
+        [[maybe_unused]] unsigned long long seen = 0;   // (ROWS)
+        if (ROWS) seen = nodes_seen(p, ib, g_inv, lane);
         uint4 qv[NI];
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
@@ -905,7 +923,10 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
           if ((int)c < p.ncols)
             qv[i] = ld_dep(reinterpret_cast<const uint4*>(p.q + (((size_t)ib * p.nq_stride + j) * p.Hq + (size_t)ih * p.G + hh) * LYNX_D) + (kt & 15));
         }
+        [[maybe_unused]] const uint32_t seeing = ROWS ? columns_that_see(seen) : 0u;
+        const auto sees = [&](int i) { return (seeing >> (i * 8 + (kt >> 4))) & 1u; };
         uint32_t amax2 = 0u;
+        [[maybe_unused]] uint32_t all2 = 0u;            // (ROWS) amax2: of the rows that see a node, all2: of all
         float sums[NI];
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
@@ -913,7 +934,8 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
           uint64_t s2 = 0ull;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            asm("max.bf16x2 %0, %0, %1;" : "+r"(amax2) : "r"(w[k] & 0x7FFF7FFFu));
+            asm("max.bf16x2 %0, %0, %1;" : "+r"(amax2) : "r"(w[k] & (!ROWS || sees(i) ? 0x7FFF7FFFu : 0u)));
+            if (ROWS) all2 = bf16x2_max(all2, w[k] & 0x7FFF7FFFu);
             s2 = f2_add(s2, f2_pack(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u)));
           }
           float lo, hi;
@@ -935,18 +957,43 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
           for (; off >= 1; off >>= 1) sums[0] += __shfl_xor_sync(0xFFFFFFFFu, sums[0], off);
           if ((lane & (16 / NI - 1)) == 0) scal[qi * NC + ((kt & 15) / (16 / NI)) * 8 + (kt >> 4)] = sums[0];
         }
-        amax = warp_max(amax);
+        amax = ROWS ? __uint_as_float(row_maxima(amax2, all2)) : warp_max(amax);
         if (lane == 0) amax_s[w4] = amax;
+        if (ROWS && kt < NC) scal[2 * NC + qi * NC + kt] = 1.0f;
         named_bar(4, 128);
-        amax = fmaxf(fmaxf(amax_s[0], amax_s[1]), fmaxf(amax_s[2], amax_s[3]));
-        // |q 2^e| in [2^14, 2^15) for the largest entry
-        int e = 0;
-        if (amax > 0.0f && amax < INFINITY) e = 14 - (((__float_as_int(amax) >> 23) & 0xFF) - 127);
-        e = max(-100, min(100, e));
+        int e;
+        if constexpr (ROWS) {
+          const uint32_t* x = reinterpret_cast<const uint32_t*>(amax_s);
+          const uint32_t m = bf16x2_max(bf16x2_max(x[0], x[1]), bf16x2_max(x[2], x[3]));
+          const float common = __uint_as_float(m << 16), all = __uint_as_float(m & 0xFFFF0000u);
+          e = f16_q_exponent(common);
+          if (!(all < INFINITY) || f16_q_exponent(all) < e) {   // (the same for all four warps)
+            if (!(common < INFINITY)) {   // of the rows that are numbers
+              float top = 0.0f;
+#pragma unroll
+              for (int i = 0; i < NI; ++i) {
+                const float t = row_largest(qv[i]);
+                if (sees(i) && t < INFINITY) top = fmaxf(top, t);
+              }
+              top = warp_max(top);
+              named_bar(4, 128);
+              if (lane == 0) amax_s[w4] = top;
+              named_bar(4, 128);
+              e = f16_q_exponent(fmaxf(fmaxf(amax_s[0], amax_s[1]), fmaxf(amax_s[2], amax_s[3])));
+            }
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+              const float t = row_largest(qv[i]), f = row_to_common(qv[i], t, f16_q_exponent(t), e);
+              if ((kt & 15) == 0) scal[2 * NC + qi * NC + i * 8 + (kt >> 4)] = f;
+            }
+          }
+        } else {
+          e = f16_q_exponent(fmaxf(fmaxf(amax_s[0], amax_s[1]), fmaxf(amax_s[2], amax_s[3])));
+        }
         const float up = __int_as_float((127 + e) << 23);
         if (C::kMetaK) ca = p.sm_log2 * __int_as_float((127 - e) << 23);
         else if (kt == 0) reinterpret_cast<int*>(scal)[4 * NC + qi] = e;
-        if (kt < NC) reinterpret_cast<int*>(scal)[2 * NC + qi * NC + kt] =
+        if (!ROWS && kt < NC) reinterpret_cast<int*>(scal)[2 * NC + qi * NC + kt] =
             kt < p.ncols ? (p.causal ? len - p.tail + kt / p.G + 1 : len) : 0;
         if (gs > 0) mbar_wait_in(sfull + ((gs - 1) & 1) * 8, ((gs - 1) >> 1) & 1, abort_word);   // the previous piece's last Q.K^T
 #pragma unroll
@@ -1135,7 +1182,9 @@ lynx_status launch_f16(AttnParams p, cudaStream_t st) {
   using C = F16Cfg<NC, INT>;
   p.combine_single = 1;
   constexpr int kMin = 1;
-  const lynx_status rc = launch_units<true, PlaneMaps, C::kSmem, C::kThreads, C::kST, kMin, attn_f16_kernel<NC, INT>>(p, st);
+  lynx_status rc;
+  if (NC == 32 && p.nodes) rc = launch_units<true, PlaneMaps, C::kSmem, C::kThreads, C::kST, kMin, attn_f16_kernel<NC, INT, NC == 32>>(p, st);
+  else rc = launch_units<true, PlaneMaps, C::kSmem, C::kThreads, C::kST, kMin, attn_f16_kernel<NC, INT>>(p, st);
   return rc != LYNX_OK ? rc : launch_combine(p, C::kPartCols, C::kST, kMin, st);
 }
 

@@ -55,7 +55,7 @@ struct PipeCfg {
   static constexpr int kPLayout = kPRow == 32 ? 6 : kPRow == 64 ? 4 : 2;   // descriptor swizzle mode of the P tile
   static constexpr int kQTile = (kNQK * 128 + 1023) / 1024 * 1024;
   static constexpr int kOffV = 0, kOffP = kNV * kVTile, kOffQ = kOffP + kSG * kPB * kPTile, kOffMeta = kOffQ + 2 * kQTile, kOffRK = kOffMeta + kNT * 2048;
-  // floats: qs[2][CP], limits[2][CP], exponents[2], maxima[2], zeros[CP]; per group: ref[CP], fac[CP], lz[2 CP], red[4][2 CP]
+  // floats: qs[2][CP], limits (ROWS: factors, see row_to_common) [2][CP], exponents[2], maxima[2], zeros[CP]; per group: ref[CP], fac[CP], lz[2 CP], red[4][2 CP]
   static constexpr int kScal = 5 * CP + 4, kGrpScal = 12 * CP;
   static constexpr int kTail = (kScal + kSG * kGrpScal) * 4 + 24 * kI8PieceUnits * 4 + 2 * 32 + 88 * 8 + 256;
   static constexpr int kAvail = 227 * 1024 - 1024 - kOffRK - kTail;
@@ -87,7 +87,8 @@ template <> struct TmemCols<4> : TmemRegs<4> {};
 template <> struct TmemCols<8> : TmemRegs<8> {};
 template <> struct TmemCols<16> : TmemRegs<16> {};
 
-template <bool FULL, int CP>
+// ROWS: the queries are rows of drafted trees (see row_to_common).
+template <bool FULL, int CP, bool ROWS = false>
 __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kernel(const AttnParams p, const __grid_constant__ PipeMaps maps) {
   using C = PipeCfg<FULL, CP>;
   constexpr int SG = C::kSG, NB = C::kNB, NV = C::kNV, NP = C::kNP, PB = C::kPB;
@@ -230,11 +231,15 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
         const int full_lim = p.causal ? len - p.tail + 1 : len;
         const float* qs_s = scal + qi * CP;
         const int* lim_s = reinterpret_cast<const int*>(scal + 2 * CP + qi * CP);
+        const float* back_s = scal + 2 * CP + qi * CP;   // (ROWS, in the place of the limits, which are all the sequence's length)
         bool fresh = true;
         mbar_wait_in(qready + qi * 8, (ic >> 1) & 1, abort_word);
         const int e = reinterpret_cast<const int*>(scal)[4 * CP + qi];
         const float ca = p.sm_log2 * __int_as_float((127 - e) << 23) * ((FULL || C::kRawK) ? 1.0f : 16.0f);
         int last = 0;
+        // APART: some column has a power of two of its own.  (A copy of the loop: a factor of 1, or a branch around it, costs 10 % at 16 columns.)
+        const auto units = [&](auto apart) {
+        constexpr bool APART = decltype(apart)::value;
         for (int u = u_first; u < n_piece; u += SG) {
           const int gs = gs_base + u, sb = gs % NB;
           last = gs;
@@ -279,7 +284,9 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
               }
               const uint64_t qs2 = *reinterpret_cast<const uint64_t*>(qs_s + 2 * c);
               const uint64_t rf2 = *reinterpret_cast<const uint64_t*>(ref_r + 2 * c);
-              y2[c] = f2_fma(f2_fma(hi, k256, lo), al2, f2_fma(be2, qs2, f2_sub(lsv2, rf2)));
+              uint64_t sum2 = f2_fma(hi, k256, lo);
+              if constexpr (APART) sum2 = f2_mul(sum2, *reinterpret_cast<const uint64_t*>(back_s + 2 * c));
+              y2[c] = f2_fma(sum2, al2, f2_fma(be2, qs2, f2_sub(lsv2, rf2)));
             }
           }
           if (unit_t0 + C::kST > full_lim) {
@@ -287,8 +294,8 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
             for (int c = 0; c < CP / 2; ++c) {
               float a, b;
               f2_unpack(y2[c], a, b);
-              if (tok >= lim_s[2 * c]) a = -INFINITY;
-              if (tok >= lim_s[2 * c + 1]) b = -INFINITY;
+              if (tok >= (ROWS ? len : lim_s[2 * c])) a = -INFINITY;
+              if (tok >= (ROWS ? len : lim_s[2 * c + 1])) b = -INFINITY;
               y2[c] = f2_pack(a, b);
             }
           }
@@ -376,6 +383,9 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
           if (lane == 0) mbar_arrive(pready + (g * PB + pb) * 8);
           ++units_in_acc;
         }
+        };
+        if (ROWS && __any_sync(0xFFFFFFFFu, back_s[lane & (CP - 1)] != 1.0f)) units(std::bool_constant<ROWS>());
+        else units(std::false_type());
         mbar_wait_in(pvdone + (last % NP) * 8, (last / NP) & 1, abort_word);   // the last P.V
         tc_fence_after();
       }
@@ -597,8 +607,11 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
       mbar_wait_in(qfull + qi * 8, (ic >> 1) & 1, abort_word + kItemAbort);
       const int ib = items[qi].b, ih = items[qi].hkv, len = items[qi].len;
       gs += items[qi].pad0;
+      [[maybe_unused]] unsigned long long seen = 0;   // (ROWS)
+      if (ROWS) seen = nodes_seen(p, ib, g_inv, lane);
       uint4 qv[NI];
       uint32_t amax2 = 0u;
+      [[maybe_unused]] uint32_t all2 = 0u;             // (ROWS) amax2: of the rows that see a node, all2: of all
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const uint32_t c = (uint32_t)(i * 4 + (qt >> 4)), j = c * g_inv >> 16, hh = c - j * (uint32_t)p.G;
@@ -606,26 +619,58 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
         if ((int)c < p.ncols)
           qv[i] = ld_dep(reinterpret_cast<const uint4*>(p.q + (((size_t)ib * p.nq_stride + j) * p.Hq + (size_t)ih * p.G + hh) * LYNX_D) + (qt & 15));
       }
+      [[maybe_unused]] const uint32_t seeing = ROWS ? columns_that_see(seen) : 0u;
+      const auto sees = [&](int i) { return (seeing >> (i * 4 + (qt >> 4))) & 1u; };
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const uint32_t w[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
         float sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          asm("max.bf16x2 %0, %0, %1;" : "+r"(amax2) : "r"(w[k] & 0x7FFF7FFFu));
+          asm("max.bf16x2 %0, %0, %1;" : "+r"(amax2) : "r"(w[k] & (!ROWS || sees(i) ? 0x7FFF7FFFu : 0u)));
+          if (ROWS) all2 = bf16x2_max(all2, w[k] & 0x7FFF7FFFu);
           sum += __uint_as_float(w[k] << 16) + __uint_as_float(w[k] & 0xFFFF0000u);
         }
 #pragma unroll
         for (int off = 8; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
         if ((qt & 15) == 0) scal[qi * CP + i * 4 + (qt >> 4)] = sum;
       }
-      const float am = warp_max(fmaxf(__uint_as_float(amax2 << 16), __uint_as_float(amax2 & 0xFFFF0000u)));
+      const float am = ROWS ? __uint_as_float(row_maxima(amax2, all2)) : warp_max(fmaxf(__uint_as_float(amax2 << 16), __uint_as_float(amax2 & 0xFFFF0000u)));
       if (lane == 0) scal[4 * CP + 2 + (warp & 1)] = am;
+      if (ROWS && qt < CP) scal[2 * CP + qi * CP + qt] = 1.0f;
       named_bar(6, 64);
-      const int e = i8_q_exponent(fmaxf(scal[4 * CP + 2], scal[4 * CP + 3]));
+      int e;
+      if constexpr (ROWS) {
+        const uint32_t m = bf16x2_max(__float_as_uint(scal[4 * CP + 2]), __float_as_uint(scal[4 * CP + 3]));
+        float common = __uint_as_float(m << 16);
+        const float all = __uint_as_float(m & 0xFFFF0000u);
+        e = i8_q_exponent(common);
+        if (!(all < INFINITY) || i8_q_exponent(all) < e) {   // (the same for both warps)
+          if (!(common < INFINITY)) {   // of the rows that are numbers
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+              const float t = row_largest(qv[i]);
+              if (sees(i) && t < INFINITY) top = fmaxf(top, t);
+            }
+            top = warp_max(top);
+            named_bar(6, 64);
+            if (lane == 0) scal[4 * CP + 2 + (warp & 1)] = top;
+            named_bar(6, 64);
+            e = i8_q_exponent(fmaxf(scal[4 * CP + 2], scal[4 * CP + 3]));
+          }
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const float t = row_largest(qv[i]), f = row_to_common(qv[i], t, i8_q_exponent(t), e);
+            if ((qt & 15) == 0) scal[2 * CP + qi * CP + i * 4 + (qt >> 4)] = f;
+          }
+        }
+      } else {
+        e = i8_q_exponent(fmaxf(scal[4 * CP + 2], scal[4 * CP + 3]));
+      }
       const float up = __int_as_float((127 + e) << 23);
       if (qt == 0) reinterpret_cast<int*>(scal)[4 * CP + qi] = e;
-      if (qt < CP) reinterpret_cast<int*>(scal)[2 * CP + qi * CP + qt] = qt < p.ncols ? (p.causal ? len - p.tail + qt / p.G + 1 : len) : 0;
+      if (!ROWS && qt < CP) reinterpret_cast<int*>(scal)[2 * CP + qi * CP + qt] = qt < p.ncols ? (p.causal ? len - p.tail + qt / p.G + 1 : len) : 0;
       // three balanced s8 digit planes of q_int = rint(q 2^e), rows plane * CP + column (four where K goes in as raw bytes)
       const uint32_t qtile = sbase + C::kOffQ + qi * C::kQTile;
 #pragma unroll
@@ -678,6 +723,7 @@ template <bool FULL, int CP>
 lynx_status launch_pipe(const AttnParams& p, cudaStream_t st) {
   using C = PipeCfg<FULL, CP>;
   constexpr int kMin = 2;
-  const lynx_status rc = launch_units<FULL, PipeMaps, C::kSmem, C::kThreads, C::kST, kMin, attn_pipe_kernel<FULL, CP>>(p, st);
+  const lynx_status rc = p.nodes ? launch_units<FULL, PipeMaps, C::kSmem, C::kThreads, C::kST, kMin, attn_pipe_kernel<FULL, CP, true>>(p, st)
+                                 : launch_units<FULL, PipeMaps, C::kSmem, C::kThreads, C::kST, kMin, attn_pipe_kernel<FULL, CP>>(p, st);
   return rc != LYNX_OK ? rc : launch_combine(p, C::kPartCols, C::kST, kMin, st);
 }
