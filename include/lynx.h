@@ -342,8 +342,9 @@ lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, lynx_plane V,
  * Node j of sequence b attends the tokens [0, seq_lens[b]) of the planes and the nodes i whose bit i is set in
  * tree_mask[b][j] (itself and its ancestors, say; bits from n_nodes on are ignored); a row that sees nothing gives zeros and
  * a log-sum-exp of -inf.  n_nodes <= 64, Hq/Hkv <= 16; sequences with fewer nodes leave the rest of their masks empty and
- * referenced by none (then nothing of those nodes but their queries is read into a result).  A chain is a tree; n_nodes = 1 is a
- * plain decode step.
+ * referenced by none: such a node's key and value enter no result, its rows attend to the prefix alone, and whatever its query holds the
+ * other rows' results are what they are without it.  An infinity or a NaN in a query spoils the results of that row alone.  A chain is
+ * a tree; n_nodes = 1 is a plain decode step.
  * q_bf16 : BF16 [batch][n_nodes][Hq][128];  k_nodes, v_nodes : BF16 [batch * n_nodes][Hkv][128], k_stride / v_stride elements from
  * a node to the next (multiples of 8, at least Hkv * 128: views of a fused projection's output);  tree_mask : uint64 [batch][n_nodes].
  * K, V with both residuals: the full codes; with both NULL: the Anchor's state.
@@ -353,8 +354,9 @@ lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, lynx_plane V,
  * Precision: scores, statistics and sums are FP32 or exact integers.  With more than 32 rows n_nodes * Hq/Hkv (and where the Anchor is short)
  * keys enter the scores exactly but for their middles zero + 128 scale (2^-22 of them) and scales below 2^-36 of the largest magnitude of their
  * 128 tokens; weights and values enter the second product as FP16 relative to exponents of their own (2^-12 of a term; value rows below 2^-29 of
- * the largest of their 128 tokens lose bits).  With fewer rows queries are exact to 2^-22 of the largest among the rows that see a node (of
- * their own, where that is larger) and weights have 22 bits and more; a value row's scale counts as 2^-80, and as 2^-24 of its zero point, at least.
+ * the largest of their 128 tokens lose bits).  Queries are exact to 2^-24 (with fewer rows 2^-22) of the largest among the KV head's rows that
+ * see a node, or of their own row's where that is larger.  With fewer rows weights have 22 bits and more; a value row's scale counts as 2^-80,
+ * and as 2^-24 of its zero point, at least.
  * workspace : lynx_tree_workspace_bytes(shape, batch, n_nodes) bytes (0: unsupported shape), zero-filled once before its first use
  * (lynx_workspace_init); each call leaves it ready for the next, also of another batch, shape or number of nodes that it is large enough for.
  * Calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of range are

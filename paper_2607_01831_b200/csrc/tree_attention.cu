@@ -13,7 +13,8 @@
 // is exact in FP16, and the middles, which may be far larger, as rank-1 terms in 16 more elements of the contraction: mid s4 / scale x
 // sum(q), both in two FP16 parts (2^-22).  What a score lacks, scale / s4, is a factor of its token in the softmax's one multiply-add per score, in FP32.
 // (FP16 of scale (c - 128) and one factor for the tile: 5 % less time for 512 rows and two contexts of 131072 tokens, but outputs 2.4 times as far off
-// where a few channels are ten times the others.)  Queries are scaled by a power of two, exact down to 2^-24 of the row block's largest.  Values
+// where a few channels are ten times the others.)  Queries are scaled by a power of two, exact down to 2^-24 of the
+// largest of the row block's rows that see a node; a row with larger entries, padding perhaps, by its own, its scores by a factor.  Values
 // enter as FP16 of V^ 2^-e, e so that the tile's largest lies below 2^15 (rows 2^29 times smaller keep all 11 bits; scales of keys 2^26 times smaller their 4), weights as
 // FP16 relative to a reference that keeps each row's largest between 2^7 and 2^16 (set anew when the sum of 16 weights,
 // which is there anyway, comes near it: no maxima): both roundings are 2^-12 of a term, an eighth of the
@@ -108,7 +109,9 @@ struct Cfg {
   static constexpr int kOffK = 0, kOffV = kOffK + 2 * 32768, kOffRK = kOffV + 2 * 32768, kOffRV = kOffRK + kRingK * kStage,
                        kOffSum = kOffRV + kRingV * kStage;           // [128] the query sums' 8 FP16
   static constexpr int kOffMid = kOffSum + 2048;                     // [kSlots][128] the middles' 8 FP16
-  static constexpr int kOffZero = kOffMid + kSlots * 2048;                    // 128 x 8 zeros, the other half of both
+  // 64 x 8 zeros, the other half of the middles; rows 64 to 127 of that of the sums, which multiply zeros, hold [2][128] factors of the rows' scores: powers of
+  // two, whose 16-bit halves are finite as FP16.  (They change while no product is under way.)
+  static constexpr int kOffZero = kOffMid + kSlots * 2048, kOffRow = kOffZero + 1024;
   static constexpr int kOffKm = kOffZero + 2048;                     // [kSlots][128] FP16 scales of 4 bits
   static constexpr int kOffVm = kOffKm + kSlots * 256;               // [kSlots][128] half2 {scale, mid}
   static constexpr int kOffFactor = kOffVm + kSlots * 512;           // [2 kSlots][128] factors of the scores
@@ -332,11 +335,11 @@ __device__ __forceinline__ void load4(uint4 (&x)[4], const uint4* src, bool used
   for (int i = 0; i < 4; ++i)
     if (!used) x[i] = make_uint4(0u, 0u, 0u, 0u);
 }
+__device__ __forceinline__ float absmax32(const uint4 (&x)[4]) { return fmaxf(fmaxf(absmax8(x[0]), absmax8(x[1])), fmaxf(absmax8(x[2]), absmax8(x[3]))); }
 // The largest magnitude of the BF16 values that N warps have, by 16 bits of each in shared memory; bar: a barrier of theirs.
 template <int N>
 __device__ __forceinline__ float largest(const uint4 (&x)[4], unsigned char* maxima, int w, int lane, int bar) {
-  const float most = fmaxf(fmaxf(absmax8(x[0]), absmax8(x[1])), fmaxf(absmax8(x[2]), absmax8(x[3])));
-  const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
+  const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(absmax32(x)));
   if (lane == 0) reinterpret_cast<volatile uint16_t*>(maxima)[w] = (uint16_t)(bits >> 16);
   named_bar(bar, N * 32);
   uint32_t top = 0u;
@@ -348,6 +351,26 @@ __device__ __forceinline__ float largest(const uint4 (&x)[4], unsigned char* max
   }
   return __uint_as_float(max(top & 0xFFFF0000u, top << 16));
 }
+// The largest magnitude of a piece's queries, of the rows that see a node and of all, by the 16 warps that have them: BF16 values, two in a word for each.
+struct RowMaxima { float seeing, all; };
+__device__ __forceinline__ RowMaxima row_maxima_of(float mine, bool sees, unsigned char* maxima, int w, int lane) {
+  const uint32_t all = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(mine)), seeing = __reduce_max_sync(0xFFFFFFFFu, sees ? __float_as_uint(mine) : 0u);
+  if (lane == 0) reinterpret_cast<volatile uint32_t*>(maxima)[w] = __byte_perm(seeing, all, 0x7632);
+  named_bar(1, 512);
+  uint32_t top = 0u;
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) {
+    const uint2 m = lds64(smem_u32(maxima) + 4 * i);
+    asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(m.x));
+    asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(m.y));
+  }
+  return {__uint_as_float(top << 16), __uint_as_float(top & 0xFFFF0000u)};
+}
+__device__ __forceinline__ RowMaxima row_maxima(const uint4 (&x)[4], bool sees, unsigned char* maxima, int w, int lane) {
+  return row_maxima_of(absmax32(x), sees, maxima, w, lane);
+}
+// Exponent by which queries are scaled: the largest below 2^7.
+__device__ __forceinline__ int query_exponent(float top) { return top > 0.0f ? max(-100, min(100, exponent_of(top) + 8)) : 0; }
 // a 2^e, without infinities in between.
 __device__ __forceinline__ float times_pow2(float a, int e) { return a * pow2(max(e >> 1, -126)) * pow2(max(e - (e >> 1), -126)); }
 // Two FP16 parts of a value below 2^16: the nearest, and what is left.
@@ -527,8 +550,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
   volatile int* misc = misc_s;               // [0] abort of data waits, [1] of item waits, [2] tensor memory, [4 + piece] the queries' part of the scores' factors, [8 ..]
-                                             // maxima of the nodes' keys and values (16 bits a warp), [16 + 8 piece ..] of the queries, [40 + tile % 8] exponent of
-                                             // the values
+                                             // maxima of the nodes' keys and values (16 bits a warp), [16 ..] of the queries (32), [40 + tile % 8] exponent of the
+                                             // values
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
   const uint32_t kfull = bars, kempty = kfull + 8 * C::kRingK, vfull = kempty + 8 * C::kRingK, vempty = vfull + 8 * C::kRingV;
@@ -594,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int c = rb * kM + (r & (C::kRows - 1)), j = c / p.G, hq = h * p.G + (c - j * p.G);
       const Halves hv(u0, n, len);
       const bool works = rb * kM + ((w4 * 32) & (C::kRows - 1)) < p.cols;
-      bool fresh = true, settled = false, any = false;   // no reference yet; none of the warp's rows without; a half tile of this warpgroup's
+      bool fresh = true, settled = false, any = false;   // no reference yet; none of the warp's rows without, or with a factor; a half tile of this warpgroup's
       float ref = 0.0f, l = 0.0f;
 #pragma unroll 1
       for (int u = (gs & 1) ^ g; u < hv.n; u += 2) {
@@ -663,9 +686,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             // A mask, no reference yet, or weights that FP16 might not hold: first the largest of the scores that are left; with a new reference
             // what the piece has so far is scaled, and this half tile's weights.
             const unsigned long long see = tree ? (c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) >> t0 : 0ull) : ~0ull;
+            const float row = __uint_as_float(lds32(sbase + C::kOffRow + (uint32_t)(qi * 512 + r * 4)));
             auto chunk = [&](float (&x)[16], int ch, float less) {
               TmemRegs<16>::ld(tm_s + t0 + ch, reinterpret_cast<uint32_t*>(x));
               tc_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 16; ++k) x[k] *= row;
               scores(x, ch, less);
               const int room = valid - ch;
               uint32_t bits = (uint32_t)(see >> ch) & (room >= 16 ? 0xFFFFu : room > 0 ? (1u << room) - 1u : 0u);
@@ -713,7 +739,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
                 TmemRegs<8>::st(tm_o + i, o);
               }
             }
-            settled = !__any_sync(0xFFFFFFFFu, fresh);
+            settled = !__any_sync(0xFFFFFFFFu, fresh || row != 1.0f);
 #pragma unroll 1
             for (int ch = done; ch < C::kW; ch += 16) {
               float x[16];
@@ -832,14 +858,28 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       {   // queries: a row by a thread of each of the four warps of its part of tensor memory, 32 channels each; all rows scaled by one power of two, the
           // largest below 2^7 (their sums below 2^14)
         const int qr = (warp & 3) * 32 + lane, quarter = (warp - 8) >> 2, c = rb * kM + (qr & (C::kRows - 1)), in = min(c, p.cols - 1), j = in / p.G;
+        const uint32_t sums = sbase + C::kOffSum + (uint32_t)qr * 16u;   // (the quarters' first, then what the products take)
         uint4 x[4];
+        const unsigned long long nodes = ld_dep(p.mask + (int64_t)b * p.n + j) << (64 - p.n);   // (bits from n on mean nothing)
         load4(x, p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (in - j * p.G)) * 16 + quarter * 4, c < p.cols);
-        const float top = largest<16>(x, smem + C::kOffMisc + 64 + 32 * qi, warp - 8, lane, 1);
-        const int e = top > 0.0f ? max(-100, min(100, exponent_of(top) + 8)) : 0;
-        const float f = pow2(-e);
+        const RowMaxima top = row_maxima(x, nodes != 0, smem + C::kOffMisc + 64, warp - 8, lane);
+        int e = query_exponent(top.seeing > 0.0f ? top.seeing : top.all), own = 0;   // (own: what a row's has more)
+        if (gt > 0) wait(kfree + ms.before(1).i * 8, ms.before(1).ph, ab);   // the previous piece's last Q K^T
+        if (!(top.all < INFINITY) || query_exponent(top.all) > e) {   // (the same for all threads)
+          // Rows that see no node may be padding, with anything in them: one with larger entries has a power of two of its own, and a factor for its scores.  An
+          // infinity, of whichever row, counts in none.
+          sts32(sums + quarter * 4u, __float_as_uint(absmax32(x)));
+          named_bar(1, 512);
+          const uint2 m01 = lds64(sums), m23 = lds64(sums + 8u);
+          const float row = __uint_as_float(max(max(m01.x, m01.y), max(m23.x, m23.y)));
+          const bool number = row < INFINITY;
+          const RowMaxima numbers = row_maxima_of(number ? row : 0.0f, nodes != 0, smem + C::kOffMisc + 64, warp - 8, lane);
+          e = query_exponent(numbers.seeing > 0.0f ? numbers.seeing : numbers.all);
+          own = number ? min(max(query_exponent(row) - e, 0), 120) : 0;
+        }
+        const float f = pow2(-e - own);
         a = p.sm_log2 * pow2(e);
         if (tid == 256) misc[4 + qi] = __float_as_int(a);
-        if (gt > 0) wait(kfree + ms.before(1).i * 8, ms.before(1).ph, ab);   // the previous piece's last Q K^T
         tc_fence_after();
         uint32_t w[16];
         float sum = 0.0f;
@@ -850,7 +890,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           w[4 * i] = y.x; w[4 * i + 1] = y.y; w[4 * i + 2] = y.z; w[4 * i + 3] = y.w;
         }
         TmemRegs<16>::st(tmem0 + C::kTmQ + ((uint32_t)((warp & 3) * 32) << 16) + quarter * 16, w);
-        const uint32_t sums = sbase + C::kOffSum + (uint32_t)qr * 16u;   // (the quarters' first, then what the products take)
         sts32(sums + quarter * 4u, __float_as_uint(sum * f));
         tc_wait_st();
         tc_fence_before();
@@ -859,6 +898,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           const uint2 s01 = lds64(sums), s23 = lds64(sums + 8u);
           const uint32_t both = two_parts((__uint_as_float(s01.x) + __uint_as_float(s01.y)) + (__uint_as_float(s23.x) + __uint_as_float(s23.y)));
           sts128(sums, __byte_perm(both, both, 0x1010), both >> 16, 0u, 0u);   // against a token's {mid hi, mid lo, mid hi}: sum hi, sum hi, sum lo
+          sts32(sbase + C::kOffRow + (uint32_t)(qi * 512 + qr * 4), __float_as_uint(pow2(own)));
           proxy_fence();
           __syncwarp();
         }

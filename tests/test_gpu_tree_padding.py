@@ -16,6 +16,9 @@ GARBAGE = [INF, -INF, NAN, 1e30, 3e38, -1e5, 2.0 ** 24]     # of queries
 # (nodes, heads, Anchor) whose prefix goes through the kernels for chains: up to 16 rows, 32 on the full codes
 FEW = [(4, 1, False), (4, 4, False), (7, 2, False), (16, 1, False), (8, 4, False), (5, 5, False), (2, 16, False), (10, 3, False),
        (4, 1, True), (4, 4, True), (7, 2, True), (16, 1, True), (2, 8, True), (3, 5, True)]
+# through tree_attention_kernel: up to 32 rows (four lanes of tensor memory each), 64 (two), 128, and row blocks
+MANY = [(31, 1, False), (8, 4, True), (5, 5, True), (9, 4, False), (16, 4, True), (32, 2, False), (17, 4, False), (32, 4, True), (32, 4, False), (40, 4, False),
+        (64, 8, True)]
 
 
 def _pad(pr, real):
@@ -73,7 +76,7 @@ def _padding(lens, real, n, G, Hkv, anchor, seed, extra_blocks=0):
     _compare(live, got, lse, want)
 
 
-@pytest.mark.parametrize("n,G,anchor", FEW)
+@pytest.mark.parametrize("n,G,anchor", FEW + MANY)
 def test_what_padding_holds(n, G, anchor):
     _padding((700, 40, 300), (max(1, n // 2), max(1, n - 1), 1), n, G, 2, anchor, seed=n + G)
     _padding((9000,), (n - 1,), n, G, 1, anchor, seed=n + G + 1)
@@ -99,7 +102,7 @@ def _magnitudes(n, G, anchor, lens, seed):
             _compare(rows, got, lse, want, out_f32)
 
 
-@pytest.mark.parametrize("n,G,anchor", FEW)
+@pytest.mark.parametrize("n,G,anchor", FEW + MANY)
 def test_larger_rows_without_nodes(n, G, anchor):
     _magnitudes(n, G, anchor, (500, 30), seed=n * G)
     _magnitudes(n, G, anchor, (6000,), seed=n * G + 1)
@@ -116,6 +119,6 @@ def _no_number(n, G, anchor, lens, seed):
         _compare(rows, got, lse, want)
 
 
-@pytest.mark.parametrize("n,G,anchor", FEW)
+@pytest.mark.parametrize("n,G,anchor", FEW + MANY)
 def test_a_row_that_is_no_number(n, G, anchor):
     _no_number(n, G, anchor, (700, 33), seed=n + G)
