@@ -19,7 +19,7 @@
 // FP16 relative to a reference that keeps each row's largest between 2^7 and 2^16 (set anew when the sum of 16 weights,
 // which is there anyway, comes near it: no maxima): both roundings are 2^-12 of a term, an eighth of the
 // output's own rounding to BF16.  2^e goes into the weight's exponent and out of l's terms again, so that it costs nothing per weight.  Sums
-// l, references and O are FP32.
+// l, references and O are FP32.  Nodes' keys are scaled row by row, and of their values only the largest number counts: what a row does not see cannot matter to it.
 //
 // Layout: rows are the M = 128 lanes of tensor memory (n * G > 128 rows: more row blocks), tokens the N of the scores and the K of
 // P V.  A thread owns a row of half a tile: no exchange between threads for maxima and sums.  Two warpgroups take the halves in turn, each with
@@ -215,6 +215,11 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
   asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
   return v;
 }
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
 __device__ __forceinline__ uint32_t lds16(uint32_t a) {
   uint16_t v;
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
@@ -336,20 +341,28 @@ __device__ __forceinline__ void load4(uint4 (&x)[4], const uint4* src, bool used
     if (!used) x[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 __device__ __forceinline__ float absmax32(const uint4 (&x)[4]) { return fmaxf(fmaxf(absmax8(x[0]), absmax8(x[1])), fmaxf(absmax8(x[2]), absmax8(x[3]))); }
-// The largest magnitude of the BF16 values that N warps have, by 16 bits of each in shared memory; bar: a barrier of theirs.
-template <int N>
-__device__ __forceinline__ float largest(const uint4 (&x)[4], unsigned char* maxima, int w, int lane, int bar) {
-  const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(absmax32(x)));
-  if (lane == 0) reinterpret_cast<volatile uint16_t*>(maxima)[w] = (uint16_t)(bits >> 16);
-  named_bar(bar, N * 32);
-  uint32_t top = 0u;
+// The largest magnitude of BF16 values, as bits: a NaN's lie above an infinity's.
+__device__ __forceinline__ uint32_t top_bits(const uint4 (&x)[4]) {
+  uint32_t m = 0u;
 #pragma unroll
-  for (int i = 0; i < N / 2; i += 2) {
-    const uint2 m = lds64(smem_u32(maxima) + 4 * i);
-    asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(m.x));
-    asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(m.y));
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) asm("max.u16x2 %0, %0, %1;" : "+r"(m) : "r"(v[k] & 0x7FFF7FFFu));
   }
-  return __uint_as_float(max(top & 0xFFFF0000u, top << 16));
+  return max(m & 0xFFFFu, m >> 16);
+}
+// The largest of such bits that the eight warps of the nodes' values have, by 16 bits of each in shared memory.
+__device__ __forceinline__ uint32_t largest_of_8(uint32_t mine, unsigned char* maxima, int w, int lane) {
+  const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, mine);
+  if (lane == 0) reinterpret_cast<volatile uint16_t*>(maxima)[w] = (uint16_t)bits;
+  named_bar(3, 256);
+  const uint2 a = lds64(smem_u32(maxima)), b = lds64(smem_u32(maxima) + 8);
+  uint32_t top = a.x;
+  asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(a.y));
+  asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(b.x));
+  asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(b.y));
+  return max(top & 0xFFFFu, top >> 16);
 }
 // The largest magnitude of a piece's queries, of the rows that see a node and of all, by the 16 warps that have them: BF16 values, two in a word for each.
 struct RowMaxima { float seeing, all; };
@@ -740,6 +753,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               }
             }
             settled = !__any_sync(0xFFFFFFFFu, fresh || row != 1.0f);
+            if (tree) {   // a node whose values are no numbers: neither are the results of who sees it
+              const uint32_t notes = sbase + (uint32_t)(C::kOffV + (t & 1) * 32768 + 8192);
+              const uint4 n0 = lds128(notes), n1 = lds128(notes + 16u);   // (of 32 rows each: first half, second half, for each quarter of the channels)
+              const unsigned long long none = (unsigned long long)(n0.y | n0.w | n1.y | n1.w) << 32 | (n0.x | n0.z | n1.x | n1.z);
+              if (see & (none >> t0)) sum = __int_as_float(0x7FFFFFFF);
+              if (sum != sum) fresh = false;
+            }
 #pragma unroll 1
             for (int ch = done; ch < C::kW; ch += 16) {
               float x[16];
@@ -780,7 +800,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         const float fm = mine.x == -INFINITY ? 0.0f : ex2(mine.x - M), fo = other.x == -INFINITY ? 0.0f : ex2(other.x - M);
         const float L = mine.y * fm + other.y * fo;
         const bool direct = TS == 1 && n_contrib == 1;
-        const float inv = direct ? (L > 0.0f ? 1.0f / L : 0.0f) : 1.0f;
+        const float inv = direct ? (L != 0.0f ? 1.0f / L : 0.0f) : 1.0f;   // (what is no number stays so)
         const float w0 = (g ? fo : fm) * inv, w1 = (g ? fm : fo) * inv;   // of accumulators 0 and 1
         const int64_t orow = ((int64_t)b * p.n + j) * p.Hq + hq;
         const int segment = (b * p.Hkv + h) * p.RB + rb;
@@ -795,7 +815,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
 #pragma unroll
           for (int k = 0; k < 16; ++k) {   // (channel k of a group of 8 is at position 0 4 2 6 1 5 3 7; what no tile wrote may be anything)
             const int at = (k & 8) | ((k & 1) << 2) | (k & 2) | ((k >> 2) & 1);
-            v[k] = (w0 > 0.0f ? __uint_as_float(o0[at]) * w0 : 0.0f) + (w1 > 0.0f ? __uint_as_float(o1[at]) * w1 : 0.0f);
+            v[k] = (w0 != 0.0f ? __uint_as_float(o0[at]) * w0 : 0.0f) + (w1 != 0.0f ? __uint_as_float(o1[at]) * w1 : 0.0f);
           }
           if (c < p.cols) {
             if (direct && !p.out_f32) {
@@ -817,7 +837,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
         if (g == 0 && c < p.cols) {
           if (!direct) *reinterpret_cast<float2*>(part + 128) = make_float2(M, L);
-          else if (p.lse) p.lse[orow] = L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
+          else if (p.lse) p.lse[orow] = L != 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
         }
         if (tid == 0 && u0 == 0 && !p.whole) p.seg[segment] = (uint32_t)first_cta << 16 | (uint32_t)n_contrib;
         tc_fence_before();
@@ -920,24 +940,39 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           __syncwarp();
           if (lane == 0) mbar_arrive(empty + slot * 8);
           if (++slot == ring) { slot = 0; phase ^= 1; }
-        } else {   // the nodes' keys or values: a row by a thread of each of four warps, all rows scaled by one power of two
+        } else {   // the nodes' keys or values: a row by a thread of each of four warps.  Rows 64 to 127 of the tile, which no product of nodes reads, pass on
+          // what the warps have to know of one another's.
           const int row = (w8 & 1) * 32 + lane, quarter = w8 >> 1, in = min(row, p.n - 1);
           const int64_t node = (int64_t)b * p.n + in;
+          const uint32_t notes = tile + 8192u;
           uint4 x[4];
           load4(x, (values ? p.vt + node * p.vt_stride : p.kt + node * p.kt_stride) + h * 16 + quarter * 4, node_used(p, b, row, lane));
-          const int e = tile_exponent(__float_as_int(largest<8>(x, smem + C::kOffMisc + (values ? 48 : 32), w8, lane, values ? 3 : 8)));
+          uint32_t most = top_bits(x);   // (the largest magnitude, an infinity or a NaN)
+          int e;
+          if (values) {   // all rows scaled by one power of two, the largest number's; what is none is zero here, and the softmax of who sees the row is told
+            const uint32_t none = __ballot_sync(0xFFFFFFFFu, most >= 0x7F80u);
+            if (lane == 0) sts32(notes + w8 * 4u, none);
+            if (most >= 0x7F80u) {
+              most = 0u;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            e = tile_exponent(largest_of_8(most, smem + C::kOffMisc + 48, w8, lane) << 16);
+            if (w8 == 0 && lane == 0) misc[40 + (gt & 7)] = e;
+          } else {        // each row by its own, so that none matters to who does not see it
+            sts32(notes + (uint32_t)row * 16u + quarter * 4u, most);
+            named_bar(8, 256);
+            const uint2 m01 = lds64(notes + (uint32_t)row * 16u), m23 = lds64(notes + (uint32_t)row * 16u + 8u);
+            e = tile_exponent((int)(max(max(m01.x, m01.y), max(m23.x, m23.y)) << 16));
+            if (quarter == 0) {
+              sts32(sbase + (uint32_t)(C::kOffFactor + (ms.i + (int)ms.ph * kSlots) * 512 + row * 4), __float_as_uint(times_pow2(a, e)));
+              sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + row * 16), 0u, 0u, 0u, 0u);
+            }
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint4 w = scaled8(x[i], pow2(-e));
             sts128(chunk_at(tile, row, quarter * 4 + i), w.x, w.y, w.z, w.w);
-          }
-          if (quarter == 0) {
-            if (!values) {
-              sts32(sbase + (uint32_t)(C::kOffFactor + (ms.i + (int)ms.ph * kSlots) * 512 + row * 4), __float_as_uint(times_pow2(a, e)));
-              sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + row * 16), 0u, 0u, 0u, 0u);
-            } else if (row == 0) {
-              misc[40 + (gt & 7)] = e;
-            }
           }
         }
         proxy_fence();   // (for the middles, too, which warp 27 has written)
@@ -1246,7 +1281,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) tree_combine_kernel(const 
 #pragma unroll
     for (int k = 1; k < W; ++k) join(ml_s[k], o_s[k][lane]);
   }
-  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  const float inv = L != 0.0f ? 1.0f / L : 0.0f;
   acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
   if (p.out_f32) {
     reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * LYNX_D)[lane] = acc;
@@ -1255,7 +1290,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) tree_combine_kernel(const 
     reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * LYNX_D)[lane] =
         make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
   }
-  if (p.lse && lane == 0) p.lse[row] = L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
+  if (p.lse && lane == 0) p.lse[row] = L != 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 // ------------------------------------------------------------------ host side

@@ -122,3 +122,30 @@ def _no_number(n, G, anchor, lens, seed):
 @pytest.mark.parametrize("n,G,anchor", FEW + MANY)
 def test_a_row_that_is_no_number(n, G, anchor):
     _no_number(n, G, anchor, (700, 33), seed=n + G)
+
+
+def _strange_node(n, G, anchor, lens, seed, kind):
+    """A node whose key or value holds what is no number, or the largest there is: rows that do not see it are what they are without it, and where a value is no
+    number, neither are the results of the rows that see it."""
+    for i, (key, value) in enumerate([(INF, None), (NAN, None), (3e38, None), (None, INF), (None, NAN), (-INF, NAN)]):
+        pr = Problem(lens, n, 2, G, seed=seed + i, kind=kind)
+        node = (i * 7 + n // 2) % n
+        pr.kn[:, node], pr.vn[:, node] = 0.0, 0.0       # (in what is compared with)
+        want = pr.exact(anchor)
+        pr.kn[:, node], pr.vn[:, node] = 0.5, 0.5
+        if key is not None:
+            pr.kn[:, node, :, 3::17] = key
+        if value is not None:
+            pr.vn[:, node, :, 100] = value
+        sees = pr.sees[:, :, node]
+        for out_f32 in (True, False):
+            got, lse = _call(pr, anchor, out_f32=out_f32)
+            _compare(~sees, got, lse, want, out_f32)
+            if value is not None and sees.any():
+                assert not torch.isfinite(got[sees.cuda()][..., 100]).any()
+
+
+@pytest.mark.parametrize("n,G,anchor", FEW + MANY)
+@pytest.mark.parametrize("kind", ["self", "tree"])
+def test_a_node_that_is_no_number(n, G, anchor, kind):
+    _strange_node(n, G, anchor, (150, 0, 33), n * G, kind)
