@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) attn_nodes_kernel(const At
     }
     M = mx;
   }
-  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  const float inv = L != 0.0f ? 1.0f / L : 0.0f;   // (what is no number stays so)
   acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
   const size_t orow = row + (size_t)a.j0 * p.Hq;
   if (a.out_f32) {
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) attn_nodes_kernel(const At
     reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + orow * LYNX_D)[lane] =
         make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
   }
-  if (a.lse && lane == 0) a.lse[orow] = lse_of(M, L);
+  if (a.lse && lane == 0) a.lse[orow] = L == L ? lse_of(M, L) : L;
 }
 
 template <int W>

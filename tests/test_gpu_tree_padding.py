@@ -145,7 +145,21 @@ def _strange_node(n, G, anchor, lens, seed, kind):
                 assert not torch.isfinite(got[sees.cuda()][..., 100]).any()
 
 
+def _no_lse(n, G, anchor, seed):
+    """The log-sum-exp of a row that sees a node with a NaN in its key is none, nor is it that of an empty row."""
+    pr = Problem((150, 0, 33), n, 2, G, seed=seed, kind="tree")
+    pr.kn[:, n // 2, :, 9] = NAN
+    sees = pr.sees[:, :, n // 2].cuda()
+    got, lse = _call(pr, anchor)
+    assert torch.isnan(got[sees]).all() and torch.isnan(lse[sees]).all() and torch.isfinite(lse[~sees]).all()
+
+
 @pytest.mark.parametrize("n,G,anchor", FEW + MANY)
 @pytest.mark.parametrize("kind", ["self", "tree"])
 def test_a_node_that_is_no_number(n, G, anchor, kind):
     _strange_node(n, G, anchor, (150, 0, 33), n * G, kind)
+
+
+@pytest.mark.parametrize("n,G,anchor", FEW + MANY)
+def test_no_log_sum_exp_of_what_is_no_number(n, G, anchor):
+    _no_lse(n, G, anchor, seed=n + G)
