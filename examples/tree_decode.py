@@ -68,7 +68,7 @@ class Decoder:
         self.lens = torch.zeros(batch, dtype=torch.int32, device=device)
         self.table = lynx.rotary_table(capacity, device=device)
         self.ends = [sum(map(len, LEVELS[:d + 1])) for d in range(len(LEVELS))]     # nodes up to each level; all of them are verified
-        self.workspaces = {n: lynx.make_tree_workspace(self.geo, batch, n, device) for n in self.ends}
+        self.workspace = lynx.make_tree_workspace(self.geo, batch, self.ends[-1], device)      # (for smaller trees, too)
         mask = []
         for j, p in enumerate(PARENTS):                                              # a node sees itself and its ancestors
             mask.append((mask[p] if p >= 0 else 0) | 1 << j)
@@ -96,7 +96,7 @@ class Decoder:
         positions = self.lens[:, None] + self.depth[:n]
         q, k = lynx.rotary(q, k, lynx.Rotary(positions.reshape(-1), self.table))
         q, k, v = (x.unflatten(0, (self.batch, n)) for x in (q, k, v))
-        o = lynx.tree_attention(self.geo, q, self.K, self.V, self.blocks, self.lens, k, v, self.mask[:, :n].contiguous(), self.workspaces[n],
+        o = lynx.tree_attention(self.geo, q, self.K, self.V, self.blocks, self.lens, k, v, self.mask[:, :n].contiguous(), self.workspace,
                                 anchor_only=anchor_only)
         return self.layer.logits(flat, o.flatten(0, 1).flatten(1)).view(self.batch, n, -1), k, v
 

@@ -359,7 +359,8 @@ lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, lynx_plane V,
  * see a node, or of their own row's where that is larger.  With fewer rows weights have 22 bits and more; a value row's scale counts as 2^-80,
  * and as 2^-24 of its zero point, at least.
  * workspace : lynx_tree_workspace_bytes(shape, batch, n_nodes) bytes (0: unsupported shape), zero-filled once before its first use
- * (lynx_workspace_init); each call leaves it ready for the next, also of another batch, shape or number of nodes that it is large enough for.
+ * (lynx_workspace_init); each call leaves it ready for the next, also of another batch, shape or number of nodes that it is large enough for:
+ * one for a batch and a number of nodes is for smaller ones of both, of the same shape.
  * Calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of range are
  * clamped and recorded there.  block_tokens a multiple of 16; seq_lens[b] is clamped to the table's capacity. */
 size_t lynx_tree_workspace_bytes(const lynx_shape* shape, int32_t batch, int32_t n_nodes);

@@ -683,7 +683,7 @@ def tree_workspace_bytes(geo: Geometry, batch: int, n_nodes: int) -> int:
 
 
 def make_tree_workspace(geo: Geometry, batch: int, n_nodes: int, device) -> torch.Tensor:
-    """Allocate a workspace for tree_attention calls of (batch, n_nodes) and zero it."""
+    """Allocate a workspace for tree_attention calls of up to (batch, n_nodes) and zero it."""
     n = tree_workspace_bytes(geo, batch, n_nodes)
     if n == 0:
         raise LynxError("unsupported tree attention shape")

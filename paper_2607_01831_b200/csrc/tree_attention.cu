@@ -1340,10 +1340,13 @@ lynx_status tree_plan(const lynx_shape* s, int B, int n, TreePlan* pl) {
   // (what the kernels for chains keep at zero between calls lies in front and stays as it is)
   pl->off_seg = up(ws_layout((int)sms, B, n, s->num_q_heads, s->num_kv_heads, 8).end_kept);
   pl->off_part = up(pl->off_seg + (size_t)pl->segs * 4);
+  // A workspace also serves calls of fewer sequences and nodes, whichever way those go: by the kernels for chains up to n_few nodes, by the tree kernel
+  // unless all of them are few rows, with up to kM rows of a partial result.  So the size never falls where batch or nodes grow.
+  const int by_full = 32 / G < kWsMaxQ ? 32 / G : kWsMaxQ, by_anchor = 2 * (kNodesCols / G), n_most = by_full > by_anchor ? by_full : by_anchor, n_few = n < n_most ? n : n_most;
   size_t most = 0;
-  if (pl->few[0] || pl->few[1]) most = pl->off_scratch + (size_t)B * n * s->num_q_heads * LYNX_D * 4;
-  if (!pl->few[0] || !pl->few[1]) {
-    const size_t tree = pl->off_part + (pl->whole ? 0 : (size_t)(pl->segs + pl->grid) * pl->part_rows * kPartRow * 4);
+  if (own != 0) most = up(lynx_workspace_bytes(s, B, n_few)) + (size_t)B * n_few * s->num_q_heads * LYNX_D * 4;
+  if (!pl->few[1] || passes > 1) {
+    const size_t tree = pl->off_part + (pl->whole ? 0 : (size_t)(pl->segs + pl->grid) * kM * kPartRow * 4);
     if (tree > most) most = tree;
   }
   pl->bytes = most;
