@@ -323,7 +323,7 @@ lynx_status lynx_rotary(const lynx_rotary_spec* spec, const void* q, int64_t q_s
  * padding -- or whose source row is outside [0, n_src) is left out.  Of several tokens with one slot, any one's values may
  * remain (K, V and planes not necessarily the same one's).  spec : NULL, or rotary positions (indexed by source row) for the
  * keys, which are turned in FP32 and quantised without a rounding in between.  Of the shape, num_kv_heads, head_dim (128),
- * block_tokens (any) and num_blocks are used.  n_tokens == 0 is a valid no-op. */
+ * block_tokens (any) and num_blocks are used.  n_tokens == 0 and, with rows, n_src == 0 are valid no-ops. */
 lynx_status lynx_cache_append(const lynx_shape* shape, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                               int64_t n_src, const int32_t* rows, int64_t n_tokens, const int64_t* slots,
                               const lynx_rotary_spec* spec, lynx_plane_out K, lynx_plane_out V, void* stream);

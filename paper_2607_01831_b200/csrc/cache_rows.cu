@@ -511,7 +511,7 @@ extern "C" lynx_status lynx_cache_append(const lynx_shape* shape, const void* k,
   if (n_tokens < 0 || n_src < 0 || (!rows && n_src < n_tokens)) return LYNX_ERR_SHAPE;
   if (shape->head_dim != LYNX_D) return LYNX_ERR_UNSUPPORTED;
   if (shape->num_kv_heads <= 0 || shape->num_kv_heads > 65536 || shape->block_tokens <= 0 || shape->num_blocks <= 0) return LYNX_ERR_SHAPE;
-  if (n_tokens == 0) return LYNX_OK;
+  if (n_tokens == 0 || n_src == 0) return LYNX_OK;   // (no token's source row is inside [0, 0))
   if (!k || !v || !slots || !K.anchor || !K.residual || !K.meta || !V.anchor || !V.residual || !V.meta) return LYNX_ERR_NULL;
   if (!stride_ok(k_stride, shape->num_kv_heads) || !stride_ok(v_stride, shape->num_kv_heads)) return LYNX_ERR_SHAPE;
   if (!aligned16(k) || !aligned16(v) || !aligned(slots, 8) || !aligned(rows, 4) || !aligned16(K.anchor) || !aligned16(K.residual) ||
