@@ -344,8 +344,8 @@ lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, lynx_plane V,
  * a log-sum-exp of -inf.  n_nodes <= 64, Hq/Hkv <= 16; sequences with fewer nodes leave the rest of their masks empty and
  * referenced by none: such a node's key and value enter no result, its rows attend to the prefix alone, and whatever its query holds the
  * other rows' results are what they are without it.  An infinity or a NaN in a query spoils the results of that row alone, one in a node's
- * key or value those of the rows that see the node (all of a row's channels may be NaN then).  A chain is a tree; n_nodes = 1 is a
- * plain decode step.
+ * key or value those of the rows that see the node, one in the scalars of a token of the prefix those of its sequence (all of a row's
+ * channels may be NaN then).  A chain is a tree; n_nodes = 1 is a plain decode step.
  * q_bf16 : BF16 [batch][n_nodes][Hq][128];  k_nodes, v_nodes : BF16 [batch * n_nodes][Hkv][128], k_stride / v_stride elements from
  * a node to the next (multiples of 8, at least Hkv * 128: views of a fused projection's output);  tree_mask : uint64 [batch][n_nodes].
  * K, V with both residuals: the full codes; with both NULL: the Anchor's state.

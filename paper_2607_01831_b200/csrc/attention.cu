@@ -250,6 +250,8 @@ __device__ __forceinline__ void merge_codes(uint32_t xa, uint32_t xr, uint32_t& 
 __device__ __forceinline__ float lse_of(float M, float L) {
   return L > 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
+// (Of rows of trees: what is no number is no empty row's.)
+__device__ __forceinline__ float lse_of(const AttnParams& p, float M, float L) { return p.node_n > 0 && L != L ? L : lse_of(M, L); }
 
 struct Item {  // one piece: a run of stage-units of one (sequence, KV head) given to one CTA
   int b, hkv, len, first_cta, n_contrib, pad0, pad1, pad2;  // pad0 = units, pad1 = first unit
@@ -546,7 +548,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) attn_combine_kernel(const 
     }
     const float inv = L > 0.0f ? 1.0f / L : 0.0f;
     acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
-    lse = lse_of(M, L);
+    lse = lse_of(p, M, L);
   } else {
     if (warp > 0) return;
     acc = ld_dep(reinterpret_cast<const float4*>(p.out + row * LYNX_D) + lane);

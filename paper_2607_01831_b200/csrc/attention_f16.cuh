@@ -366,7 +366,7 @@ __device__ __forceinline__ void plane_producer(const AttnParams& p, const SkRang
 // The per-token scalars of a unit, for N tokens (32 apart) of a thread: scale and offset of the scores, log2 of the value
 // scale, its reciprocal and the zero point in units of it.  Metadata is read two steps ahead: the block id of the unit after
 // next, the (scale, zero) pairs of the next unit.
-template <class C, int N>
+template <class C, int N, bool ROWS>
 struct F16Meta {
   float4* tok4;
   float* tok1;
@@ -411,7 +411,9 @@ struct F16Meta {
       const float sve = v_scale(p, vm[i].x, vm[i].y);
       const float ia = valid ? rcp_approx(sve) : 0.0f;
       const int at = gs % C::kSlots * 128 + 32 * i;
-      tok4[at] = make_float4(km[i].x * ca, fmaf(km[i].x, 128.0f, km[i].y) * p.sm_log2, lg2_approx(sve), ia);
+      float lsv = lg2_approx(sve);
+      if (ROWS) lsv += fmaf(km[i].x, 0.0f, fmaf(km[i].y, 0.0f, fmaf(vm[i].x, 0.0f, vm[i].y * 0.0f)));   // (a token that is no number makes all rows none)
+      tok4[at] = make_float4(km[i].x * ca, fmaf(km[i].x, 128.0f, km[i].y) * p.sm_log2, lsv, ia);
       tok1[at] = fmaf(sve, 128.0f, vm[i].y) * ia;
     }
   }
@@ -897,7 +899,7 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
     const int kt = tid - 256, w4 = warp & 3;
     const uint32_t tm_k = tmem0 + C::kTmK + ((uint32_t)(w4 * 32) << 16);
     float* amax_s = reinterpret_cast<float*>(misc + 48);
-    F16Meta<C, 1> meta;
+    F16Meta<C, 1, ROWS> meta;
     float ca = 0.0f;
     if (C::kMetaK) meta.init(p, smem, kt);
     int gs = 0, ic = 0, slot = 0;
@@ -1089,7 +1091,7 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
   reg_dec<C::kRegMma>();
   // ---- per-token scalars of the scores and weights (warps 21, 22: a lane has tokens 64 w + lane and 32 further on) ----
   if (!C::kMetaK && (warp == 21 || warp == 22)) {
-    F16Meta<C, 2> meta;
+    F16Meta<C, 2, ROWS> meta;
     meta.init(p, smem, (warp - 21) * 64 + lane);
     int gs = 0, ic = 0;
     while (gs < n_units) {

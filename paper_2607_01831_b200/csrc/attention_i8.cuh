@@ -569,7 +569,7 @@ __device__ __forceinline__ void i8_join(const AttnParams& p, const Item& item, i
     const int j = c / p.G;
     const size_t row = ((size_t)item.b * p.nq_stride + j) * p.Hq + (size_t)item.hkv * p.G + (c - j * p.G);
     reinterpret_cast<float4*>(p.out + row * LYNX_D)[lane] = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-    if (lane == 0) p.ws_lse[row] = lse_of(M, L);
+    if (lane == 0) p.ws_lse[row] = lse_of(p, M, L);
   }
 }
 // The segments that a CTA shares -- its first with the CTAs before it, its last with those behind -- once all of its slots have been

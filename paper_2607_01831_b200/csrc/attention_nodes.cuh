@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) attn_nodes_kernel(const At
     if (warp == 0) {
       const float lse = ld_dep(p.ws_lse + row);
       acc = ld_dep(reinterpret_cast<const float4*>(p.out + row * LYNX_D) + lane);
-      if (lse > -INFINITY) { M = lse * 1.4426950408889634f; L = 1.0f; }   // (else the row is zeros)
+      if (lse != -INFINITY) { M = lse * 1.4426950408889634f; L = 1.0f; }   // (else the row is zeros)
     }
   } else {
     const size_t sstride = (size_t)part_cols * kPartStride;
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) attn_nodes_kernel(const At
     reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + orow * LYNX_D)[lane] =
         make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
   }
-  if (a.lse && lane == 0) a.lse[orow] = L == L ? lse_of(M, L) : L;
+  if (a.lse && lane == 0) a.lse[orow] = lse_of(p, M, L);
 }
 
 template <int W>

@@ -254,7 +254,8 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
           const float sve = v_scale(p, FULL ? vm.x : 16.0f * vm.x, vm.y);
           const float al = km.x * ca;
           const float be = fmaf(km.x, FULL ? 128.0f : 8.0f, km.y) * cb;
-          const float lsv = lg2_approx(sve);
+          float lsv = lg2_approx(sve);
+          if (ROWS) lsv += fmaf(km.x, 0.0f, fmaf(km.y, 0.0f, fmaf(vm.x, 0.0f, vm.y * 0.0f)));   // (a token that is no number makes all rows none)
           const float ia = valid ? rcp_approx(sve) : 0.0f;
           const float ib = (FULL ? fmaf(sve, 128.0f, vm.y) : fmaf(vm.x, 8.0f, vm.y)) * ia;
           uint64_t y2[CP / 2];
@@ -440,7 +441,7 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
           if (direct) {
             const int j = c / p.G, hh = c - j * p.G;
             t.row = (uint32_t)((item.b * p.nq_stride + j) * p.Hq + item.hkv * p.G + hh);
-            if (leads) p.ws_lse[t.row] = lse_of(M, t.l);
+            if (leads) p.ws_lse[t.row] = lse_of(p, M, t.l);
           } else if (leads) {
             *reinterpret_cast<float2*>(part + (size_t)c * kPartStride + 128) = make_float2(M, t.l);
           }
@@ -450,7 +451,7 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
 #pragma unroll
           for (int i = 0; i < SG; ++i) o = fmaf(mails[i * (PB * C::kPTile / 4) + c * 128], t.f[i], o);
           const float v = o + t.z;
-          if (direct) p.out[(size_t)t.row * LYNX_D + dim_out] = t.l > 0.0f ? v / t.l : 0.0f;
+          if (direct) p.out[(size_t)t.row * LYNX_D + dim_out] = (ROWS ? t.l != 0.0f : t.l > 0.0f) ? v / t.l : 0.0f;
           else part[(size_t)c * kPartStride + dim_out] = v;
         };
         if constexpr (H > 1) {

@@ -163,3 +163,27 @@ def test_a_node_that_is_no_number(n, G, anchor, kind):
 @pytest.mark.parametrize("n,G,anchor", FEW + MANY)
 def test_no_log_sum_exp_of_what_is_no_number(n, G, anchor):
     _no_lse(n, G, anchor, seed=n + G)
+
+
+def _strange_prefix(n, G, anchor, lens, seed):
+    """A token of the prefix whose scale is infinite, as of a row that was quantised with an infinity in it: all rows of its sequence see it and are no numbers, the
+    other sequences' are what they are."""
+    for tensor in (0, 1):
+        pr = Problem(lens, n, 2, G, seed=seed + tensor, kind="tree")
+        want = pr.exact(anchor)
+        token = lens[0] // 2
+        pr.planes[tensor][2][pr.table[0, token // 16], :, token % 16] = torch.tensor([INF, 1.0])
+        got, lse = _call(pr, anchor)
+        assert not torch.isfinite(got[0]).any()
+        assert tensor == 1 or not torch.isfinite(lse[0]).any() and not (lse[0] == -INF).any()
+        rows = torch.ones(pr.B, n, dtype=torch.bool)
+        rows[0] = False
+        _compare(rows, got, lse, want)
+
+
+@pytest.mark.parametrize("n,G,anchor", FEW + MANY)
+def test_a_prefix_that_is_no_number(n, G, anchor):
+    _strange_prefix(n, G, anchor, (40, 90, 0), seed=n + G)
+    _strange_prefix(n, G, anchor, (7000, 300), seed=n + G)
+    _strange_prefix(n, G, anchor, (300,) * 50, seed=n + G)
+    _strange_prefix(n, G, anchor, (32768,) + (64,) * 39, seed=n + G)     # (joined by each of the ways there are)
