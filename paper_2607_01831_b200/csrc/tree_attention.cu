@@ -318,13 +318,6 @@ __device__ __forceinline__ uint4 scaled8(const uint4& w, float f) {
   return make_uint4(pack_f16x2(bf_lo(w.x) * f, bf_lo(w.z) * f), pack_f16x2(bf_lo(w.y) * f, bf_lo(w.w) * f),
                     pack_f16x2(bf_hi(w.x) * f, bf_hi(w.z) * f), pack_f16x2(bf_hi(w.y) * f, bf_hi(w.w) * f));
 }
-__device__ __forceinline__ float absmax8(const uint4& w) {
-  uint32_t m = 0u;
-  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v[i] & 0x7FFF7FFFu));
-  return fmaxf(bf_lo(m), bf_hi(m));
-}
 // Exponent that brings the largest of a set to [2^14, 2^15); of a tile, from the bits of the largest.
 __device__ __forceinline__ int exponent_of(float amax) { return ((__float_as_int(amax) >> 23) & 0xFF) - 127 - 14; }
 
@@ -340,7 +333,6 @@ __device__ __forceinline__ void load4(uint4 (&x)[4], const uint4* src, bool used
   for (int i = 0; i < 4; ++i)
     if (!used) x[i] = make_uint4(0u, 0u, 0u, 0u);
 }
-__device__ __forceinline__ float absmax32(const uint4 (&x)[4]) { return fmaxf(fmaxf(absmax8(x[0]), absmax8(x[1])), fmaxf(absmax8(x[2]), absmax8(x[3]))); }
 // The largest magnitude of BF16 values, as bits: a NaN's lie above an infinity's.
 __device__ __forceinline__ uint32_t top_bits(const uint4 (&x)[4]) {
   uint32_t m = 0u;
@@ -364,11 +356,12 @@ __device__ __forceinline__ uint32_t largest_of_8(uint32_t mine, unsigned char* m
   asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(b.y));
   return max(top & 0xFFFFu, top >> 16);
 }
-// The largest magnitude of a piece's queries, of the rows that see a node and of all, by the 16 warps that have them: BF16 values, two in a word for each.
+// The largest magnitude of a piece's queries that is a number, of the rows that see a node and of all, by the 16 warps that have them: BF16 values, two in a word for each.
 struct RowMaxima { float seeing, all; };
-__device__ __forceinline__ RowMaxima row_maxima_of(float mine, bool sees, unsigned char* maxima, int w, int lane) {
-  const uint32_t all = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(mine)), seeing = __reduce_max_sync(0xFFFFFFFFu, sees ? __float_as_uint(mine) : 0u);
-  if (lane == 0) reinterpret_cast<volatile uint32_t*>(maxima)[w] = __byte_perm(seeing, all, 0x7632);
+__device__ __forceinline__ RowMaxima row_maxima(uint32_t mine, bool sees, unsigned char* maxima, int w, int lane) {
+  if (mine >= 0x7F80u) mine = 0u;
+  const uint32_t all = __reduce_max_sync(0xFFFFFFFFu, mine), seeing = __reduce_max_sync(0xFFFFFFFFu, sees ? mine : 0u);
+  if (lane == 0) reinterpret_cast<volatile uint32_t*>(maxima)[w] = all << 16 | seeing;
   named_bar(1, 512);
   uint32_t top = 0u;
 #pragma unroll
@@ -378,9 +371,6 @@ __device__ __forceinline__ RowMaxima row_maxima_of(float mine, bool sees, unsign
     asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(m.y));
   }
   return {__uint_as_float(top << 16), __uint_as_float(top & 0xFFFF0000u)};
-}
-__device__ __forceinline__ RowMaxima row_maxima(const uint4 (&x)[4], bool sees, unsigned char* maxima, int w, int lane) {
-  return row_maxima_of(absmax32(x), sees, maxima, w, lane);
 }
 // Exponent by which queries are scaled: the largest below 2^7.
 __device__ __forceinline__ int query_exponent(float top) { return top > 0.0f ? max(-100, min(100, exponent_of(top) + 8)) : 0; }
@@ -700,11 +690,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             // what the piece has so far is scaled, and this half tile's weights.
             const unsigned long long see = tree ? (c < p.cols ? ld_dep(p.mask + (int64_t)b * p.n + j) >> t0 : 0ull) : ~0ull;
             const float row = __uint_as_float(lds32(sbase + C::kOffRow + (uint32_t)(qi * 512 + r * 4)));
+            const int apart = __any_sync(0xFFFFFFFFu, row != 1.0f);   // (some row has a factor)
             auto chunk = [&](float (&x)[16], int ch, float less) {
               TmemRegs<16>::ld(tm_s + t0 + ch, reinterpret_cast<uint32_t*>(x));
               tc_wait_ld();
+#pragma unroll 1
+              for (int once = apart; once > 0; --once) {   // (a loop, so that it is branched around and not predicated)
 #pragma unroll
-              for (int k = 0; k < 16; ++k) x[k] *= row;
+                for (int k = 0; k < 16; ++k) x[k] *= row;
+              }
               scores(x, ch, less);
               const int room = valid - ch;
               uint32_t bits = (uint32_t)(see >> ch) & (room >= 16 ? 0xFFFFu : room > 0 ? (1u << room) - 1u : 0u);
@@ -752,7 +746,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
                 TmemRegs<8>::st(tm_o + i, o);
               }
             }
-            settled = !__any_sync(0xFFFFFFFFu, fresh || row != 1.0f);
+            settled = !apart && !__any_sync(0xFFFFFFFFu, fresh);
             if (tree) {   // a node whose values are no numbers: neither are the results of who sees it
               const uint32_t notes = sbase + (uint32_t)(C::kOffV + (t & 1) * 32768 + 8192);
               const uint4 n0 = lds128(notes), n1 = lds128(notes + 16u);   // (of 32 rows each: first half, second half, for each quarter of the channels)
@@ -868,38 +862,36 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     int gt = 0, slot = 0;
     uint32_t phase = 0;
     Slot ms;          // of tile gt among kSlots
-    float a = 0.0f;   // factor of the scores, but for the keys' exponent
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
-      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
+      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0;
       if (n == 0) break;
       const int n_prefix = (len + kTile - 1) / kTile;
       {   // queries: a row by a thread of each of the four warps of its part of tensor memory, 32 channels each; all rows scaled by one power of two, the
           // largest below 2^7 (their sums below 2^14)
+        const int b = items[qi].b, h = items[qi].h, rb = items[qi].rb;
         const int qr = (warp & 3) * 32 + lane, quarter = (warp - 8) >> 2, c = rb * kM + (qr & (C::kRows - 1)), in = min(c, p.cols - 1), j = in / p.G;
         const uint32_t sums = sbase + C::kOffSum + (uint32_t)qr * 16u;   // (the quarters' first, then what the products take)
         uint4 x[4];
         const unsigned long long nodes = ld_dep(p.mask + (int64_t)b * p.n + j) << (64 - p.n);   // (bits from n on mean nothing)
         load4(x, p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (in - j * p.G)) * 16 + quarter * 4, c < p.cols);
-        const RowMaxima top = row_maxima(x, nodes != 0, smem + C::kOffMisc + 64, warp - 8, lane);
-        int e = query_exponent(top.seeing > 0.0f ? top.seeing : top.all), own = 0;   // (own: what a row's has more)
+        const uint32_t mine = top_bits(x);
+        const RowMaxima top = row_maxima(mine, nodes != 0, smem + C::kOffMisc + 64, warp - 8, lane);
+        const int e = query_exponent(top.seeing > 0.0f ? top.seeing : top.all);
+        int own = 0;   // what a row's has more
         if (gt > 0) wait(kfree + ms.before(1).i * 8, ms.before(1).ph, ab);   // the previous piece's last Q K^T
-        if (!(top.all < INFINITY) || query_exponent(top.all) > e) {   // (the same for all threads)
-          // Rows that see no node may be padding, with anything in them: one with larger entries has a power of two of its own, and a factor for its scores.  An
-          // infinity, of whichever row, counts in none.
-          sts32(sums + quarter * 4u, __float_as_uint(absmax32(x)));
+        if (__builtin_expect(query_exponent(top.all) > e, 0)) {   // (the same for all threads)
+          // Rows that see no node may be padding, with anything in them: one with larger entries has a power of two of its own, and a factor for its scores.
+          sts32(sums + quarter * 4u, mine);
           named_bar(1, 512);
           const uint2 m01 = lds64(sums), m23 = lds64(sums + 8u);
-          const float row = __uint_as_float(max(max(m01.x, m01.y), max(m23.x, m23.y)));
-          const bool number = row < INFINITY;
-          const RowMaxima numbers = row_maxima_of(number ? row : 0.0f, nodes != 0, smem + C::kOffMisc + 64, warp - 8, lane);
-          e = query_exponent(numbers.seeing > 0.0f ? numbers.seeing : numbers.all);
-          own = number ? min(max(query_exponent(row) - e, 0), 120) : 0;
+          const uint32_t row = max(max(m01.x, m01.y), max(m23.x, m23.y));
+          if (row < 0x7F80u) own = min(max(query_exponent(__uint_as_float(row << 16)) - e, 0), 120);
+          named_bar(1, 512);
         }
         const float f = pow2(-e - own);
-        a = p.sm_log2 * pow2(e);
-        if (tid == 256) misc[4 + qi] = __float_as_int(a);
+        if (tid == 256) misc[4 + qi] = __float_as_int(p.sm_log2 * pow2(e));
         tc_fence_after();
         uint32_t w[16];
         float sum = 0.0f;
@@ -942,22 +934,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           if (++slot == ring) { slot = 0; phase ^= 1; }
         } else {   // the nodes' keys or values: a row by a thread of each of four warps.  Rows 64 to 127 of the tile, which no product of nodes reads, pass on
           // what the warps have to know of one another's.
-          const int row = (w8 & 1) * 32 + lane, quarter = w8 >> 1, in = min(row, p.n - 1);
+          const int row = (w8 & 1) * 32 + lane, quarter = w8 >> 1, in = min(row, p.n - 1), b = items[qi].b, h = items[qi].h;
           const int64_t node = (int64_t)b * p.n + in;
           const uint32_t notes = tile + 8192u;
           uint4 x[4];
           load4(x, (values ? p.vt + node * p.vt_stride : p.kt + node * p.kt_stride) + h * 16 + quarter * 4, node_used(p, b, row, lane));
-          uint32_t most = top_bits(x);   // (the largest magnitude, an infinity or a NaN)
+          const uint32_t most = top_bits(x);   // (the largest magnitude, an infinity or a NaN)
+          const bool none = values && most >= 0x7F80u;
           int e;
           if (values) {   // all rows scaled by one power of two, the largest number's; what is none is zero here, and the softmax of who sees the row is told
-            const uint32_t none = __ballot_sync(0xFFFFFFFFu, most >= 0x7F80u);
-            if (lane == 0) sts32(notes + w8 * 4u, none);
-            if (most >= 0x7F80u) {
-              most = 0u;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
-            }
-            e = tile_exponent(largest_of_8(most, smem + C::kOffMisc + 48, w8, lane) << 16);
+            const uint32_t rows = __ballot_sync(0xFFFFFFFFu, none);
+            if (lane == 0) sts32(notes + w8 * 4u, rows);
+            e = tile_exponent(largest_of_8(none ? 0u : most, smem + C::kOffMisc + 48, w8, lane) << 16);
             if (w8 == 0 && lane == 0) misc[40 + (gt & 7)] = e;
           } else {        // each row by its own, so that none matters to who does not see it
             sts32(notes + (uint32_t)row * 16u + quarter * 4u, most);
@@ -965,13 +953,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             const uint2 m01 = lds64(notes + (uint32_t)row * 16u), m23 = lds64(notes + (uint32_t)row * 16u + 8u);
             e = tile_exponent((int)(max(max(m01.x, m01.y), max(m23.x, m23.y)) << 16));
             if (quarter == 0) {
-              sts32(sbase + (uint32_t)(C::kOffFactor + (ms.i + (int)ms.ph * kSlots) * 512 + row * 4), __float_as_uint(times_pow2(a, e)));
+              sts32(sbase + (uint32_t)(C::kOffFactor + (ms.i + (int)ms.ph * kSlots) * 512 + row * 4), __float_as_uint(times_pow2(__int_as_float(misc[4 + qi]), e)));
               sts128(sbase + C::kOffMid + (uint32_t)(ms.i * 2048 + row * 16), 0u, 0u, 0u, 0u);
             }
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint4 w = scaled8(x[i], pow2(-e));
+            uint4 w = scaled8(x[i], pow2(-e));
+            if (none) w = make_uint4(0u, 0u, 0u, 0u);
             sts128(chunk_at(tile, row, quarter * 4 + i), w.x, w.y, w.z, w.w);
           }
         }

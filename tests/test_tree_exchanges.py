@@ -75,18 +75,16 @@ def _run(pieces, rng, give_up=None):
             if n == 0:
                 return
             # queries
-            maxima[i].write((ic, 0))
+            maxima[i].write(ic)
             yield from meet("1", i, W)
-            yield from read(maxima, (ic, 0))
+            yield from read(maxima, ic)
             if gt > 0:
                 yield from wait("kfree", (gt - 1) % 3, (gt - 1) // 3)
             if apart:
                 sums[i].write((ic, "largest"))
                 yield from meet("1", i, W)
                 yield from read([sums[k] for k in own], (ic, "largest"))
-                maxima[i].write((ic, 1))
                 yield from meet("1", i, W)
-                yield from read(maxima, (ic, 1))
             if i == 0:
                 word[ic & 1].write(ic)
             Q[i].write(ic)
@@ -220,12 +218,12 @@ def test_the_kernel_exchanges_what_is_played():
     """The barriers of the warps with codes in the source, in order, and how often each is met."""
     code = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "tree_attention.cu")).read())
     body = code[code.index("if (warp < 24) {"):code.index("if (warp == 24) {")]
-    assert re.findall(r"named_bar\((\d+), \d+\)|\b(row_maxima|row_maxima_of|largest_of_8)\(", body) == [
-        ("", "row_maxima"), ("1", ""), ("", "row_maxima_of"), ("1", ""), ("", "largest_of_8"), ("8", "")]
-    for name, bar in (("RowMaxima row_maxima_of(", "named_bar(1, 512)"), ("uint32_t largest_of_8(", "named_bar(3, 256)")):
+    assert re.findall(r"named_bar\((\d+), \d+\)|\b(row_maxima|largest_of_8)\(", body) == [
+        ("", "row_maxima"), ("1", ""), ("1", ""), ("1", ""), ("", "largest_of_8"), ("8", "")]
+    for name, bar in (("RowMaxima row_maxima(", "named_bar(1, 512)"), ("uint32_t largest_of_8(", "named_bar(3, 256)")):
         f = code[code.index(name):]
         f = f[:f.index("\n}")]
         assert f.count("named_bar(") == 1 and bar in f
         assert f.index("volatile uint") < f.index("named_bar(") < f.index("lds64(")      # written, met, read
     # (the sums are free from the previous piece's last product on)
-    assert body.index("wait(kfree + ms.before(1)") < body.index("sts32(sums + quarter * 4u, __float_as_uint(absmax32(x)))")
+    assert body.index("wait(kfree + ms.before(1)") < body.index("sts32(sums + quarter * 4u, mine)")
