@@ -240,10 +240,11 @@ struct AppendParams {
 };
 
 // A warp: four tokens, `per` heads of K or of V, kFly rows of a quarter-warp at a time.
-// 8 heads of 131072 tokens, K and V, out of a fused projection into scattered blocks (822 MB: 125 us at the copy rate): 148 us, 179 with
+// 8 heads of 131072 tokens, K and V, out of a fused projection into scattered blocks (822 MB: 125 us at the copy rate): 148 us, 180 with
 // the keys rotated (67 MB more of angles; 206 and 234 with scalar arithmetic and two divisions a row in every lane).  The issue of instructions
-// bounds it (0.63 a cycle and scheduler, the ALUs at 59 %).  Two rows of a quarter-warp are in flight; four, or the next ones during the arithmetic,
-// cost more registers than they hide (149 and 185, 152 and 209), a fifth CTA per SM 144 and 197.
+// bounds it (0.62 a cycle and scheduler, the ALUs at 60 %).  Two rows of a quarter-warp are in flight; four, or the next ones during the arithmetic,
+// cost more registers than they hide (149 and 185, 152 and 209), a fifth CTA per SM 144 and 197.  Two turned rows in FP32 and their angles are too many
+// for the 64 registers that four CTAs leave: 60 bytes a thread are spilled (-Xptxas -v), which the rotated keys' time includes.
 template <int kFly, bool TURN>
 __device__ __forceinline__ void append_rows(const RotaryParams& r, const AppendParams& p, int64_t row, int64_t slot, int v, int l, int first, int last) {
   static_assert(kFly == 1 || kFly == 2 || kFly == 4, "a division per lane");
@@ -370,8 +371,8 @@ __device__ __forceinline__ int sequence_of(const ReadParams& p, int64_t row, int
   return lo < p.batch ? lo : -1;
 }
 
-// A warp: four output rows, `per` heads of K or of V.  8 heads of 131072 tokens (822 MB, from the Anchor 688 MB: 125 and 105 us at the copy rate) take 136 us
-// and 118.  Memory bounds it, at six CTAs per SM: full codes four rows of a quarter-warp at a time with four CTAs 146, from the Anchor alone, with 16-byte
+// A warp: four output rows, `per` heads of K or of V.  8 heads of 131072 tokens (822 MB, from the Anchor 688 MB: 125 and 105 us at the copy rate) take 137 us
+// and 117.  Memory bounds it, at six CTAs per SM: full codes four rows of a quarter-warp at a time with four CTAs 146, from the Anchor alone, with 16-byte
 // stores and loads under conditions, 133.
 template <int kFly, bool kFull>
 __global__ void __launch_bounds__(kThreads, 6) cache_read_kernel(const __grid_constant__ ReadParams p, int per, int groups) {
@@ -464,7 +465,7 @@ lynx_status rotary_params(const lynx_rotary_spec* s, int64_t n_tokens, RotaryPar
 }
 inline bool stride_ok(int64_t stride, int heads) { return stride >= (int64_t)heads * LYNX_D && stride % 8 == 0; }
 
-// Heads that a warp walks through: all of them where the tokens alone fill the GPU several times over, else one by one.
+// Heads that a warp walks through, with a token's angles in its registers: up to eight, halved until the warps fill the GPU several times over.
 inline int heads_per_warp(int64_t n_tokens, int heads) {
   const int64_t warps = (n_tokens + 3) / 4, full = (int64_t)sm_count() * 64;
   for (int per = heads < 8 ? heads : 8; per > 1; per /= 2)
