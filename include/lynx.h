@@ -356,8 +356,8 @@ lynx_status lynx_cache_read(const lynx_shape* shape, lynx_plane K, lynx_plane V,
  * keys enter the scores exactly but for their middles zero + 128 scale (2^-22 of them) and scales below 2^-36 of the largest magnitude of their
  * 128 tokens; weights and values enter the second product as FP16 relative to exponents of their own (2^-12 of a term; value rows below 2^-29 of
  * the largest of their 128 tokens lose bits).  Queries are exact to 2^-24 (with fewer rows 2^-22) of the largest among the KV head's rows that
- * see a node, or of their own row's where that is larger.  With fewer rows weights have 22 bits and more; a value row's scale counts as 2^-80,
- * and as 2^-24 of its zero point, at least.
+ * see a node, or of their own row's where that is larger; where no row sees a node, to 2^-14 and 2^-18 of their own row's at least.  With fewer rows
+ * weights have 22 bits and more; a value row's scale counts as 2^-80, and as 2^-24 of its zero point, at least.
  * workspace : lynx_tree_workspace_bytes(shape, batch, n_nodes) bytes (0: unsupported shape), zero-filled once before its first use
  * (lynx_workspace_init); each call leaves it ready for the next, also of another batch, shape or number of nodes that it is large enough for:
  * one for a batch and a number of nodes is for smaller ones of both, of the same shape.

@@ -123,10 +123,16 @@ __device__ __forceinline__ float row_to_common(uint4& w, float largest, int own,
 __device__ __forceinline__ unsigned long long nodes_seen(const AttnParams& p, int b, uint32_t g_inv, int lane) {
   return ld_dep(p.node_mask + (size_t)b * p.node_n + p.node_j0 + ((uint32_t)min(lane, p.ncols - 1) * g_inv >> 16)) << (64 - p.node_n);
 }
-// The columns whose queries see a node, a bit each: all, where none does.
-__device__ __forceinline__ uint32_t columns_that_see(unsigned long long nodes) {
-  const uint32_t see = __ballot_sync(0xFFFFFFFFu, nodes != 0);
-  return see ? see : ~0u;
+// The smallest and the largest entry of rows, as one word that maxima join: BF16, the smallest less than infinity by so much.
+__device__ __forceinline__ uint32_t range_word(float low, float top) { return __float_as_uint(top) | (0x7F80u - (__float_as_uint(low) >> 16)); }
+__device__ __forceinline__ float top_of(uint32_t range) { return __uint_as_float(range & 0xFFFF0000u); }
+__device__ __forceinline__ float low_of(uint32_t range) { return __uint_as_float((0x7F80u - (range & 0xFFFFu)) << 16); }
+// Where no row that sees a node has one, the common power of two is the largest row's if all are within 2^kRowShare of it, else the smallest's, so that each other has its own.
+constexpr int kRowShare = 4;
+template <class Exponent>
+__device__ __forceinline__ int common_exponent(uint32_t range, Exponent exponent) {
+  const int of_top = exponent(top_of(range)), of_low = exponent(low_of(range));
+  return of_low > of_top + kRowShare ? of_low : of_top;
 }
 // A value row's scale for logarithms and quotients: at least v_rel of its zero point and v_least, since it may be 0 (then the codes are, and any does).  Chains
 // have 0 and 2^-40, so that rows of smaller scales are off by up to 2^-32; trees 2^-24 and 2^-80: by 2^-16 of themselves, or 2^-72.  (Not smaller: weights

@@ -925,8 +925,8 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
           if ((int)c < p.ncols)
             qv[i] = ld_dep(reinterpret_cast<const uint4*>(p.q + (((size_t)ib * p.nq_stride + j) * p.Hq + (size_t)ih * p.G + hh) * LYNX_D) + (kt & 15));
         }
-        [[maybe_unused]] const uint32_t seeing = ROWS ? columns_that_see(seen) : 0u;
-        const auto sees = [&](int i) { return (seeing >> (i * 8 + (kt >> 4))) & 1u; };
+        [[maybe_unused]] const uint32_t see = __ballot_sync(0xFFFFFFFFu, seen != 0);   // (ROWS) the columns that see a node
+        const auto sees = [&](int i) { return (see >> (i * 8 + (kt >> 4))) & 1u; };
         uint32_t amax2 = 0u;
         [[maybe_unused]] uint32_t all2 = 0u;            // (ROWS) amax2: of the rows that see a node, all2: of all
         float sums[NI];
@@ -969,19 +969,21 @@ __global__ void __launch_bounds__(F16Cfg<NC, INT>::kThreads, 1) attn_f16_kernel(
           const uint32_t m = bf16x2_max(bf16x2_max(x[0], x[1]), bf16x2_max(x[2], x[3]));
           const float common = __uint_as_float(m << 16), all = __uint_as_float(m & 0xFFFF0000u);
           e = f16_q_exponent(common);
-          if (!(all < INFINITY) || f16_q_exponent(all) < e) {   // (the same for all four warps)
-            if (!(common < INFINITY)) {   // of the rows that are numbers
-              float top = 0.0f;
+          const bool none = !(common > 0.0f && common < INFINITY);   // (of those that see a node)
+          if (none || !(all < INFINITY) || f16_q_exponent(all) < e) {   // (the same for all four warps)
+            if (none) {   // of all rows that are numbers
+              float top = 0.0f, low = INFINITY;
 #pragma unroll
               for (int i = 0; i < NI; ++i) {
                 const float t = row_largest(qv[i]);
-                if (sees(i) && t < INFINITY) top = fmaxf(top, t);
+                if (t < INFINITY && t > 0.0f) { top = fmaxf(top, t); low = fminf(low, t); }
               }
               top = warp_max(top);
+              low = -warp_max(-low);
               named_bar(4, 128);
-              if (lane == 0) amax_s[w4] = top;
+              if (lane == 0) amax_s[w4] = __uint_as_float(range_word(low, top));
               named_bar(4, 128);
-              e = f16_q_exponent(fmaxf(fmaxf(amax_s[0], amax_s[1]), fmaxf(amax_s[2], amax_s[3])));
+              e = common_exponent(bf16x2_max(bf16x2_max(x[0], x[1]), bf16x2_max(x[2], x[3])), f16_q_exponent);
             }
 #pragma unroll
             for (int i = 0; i < NI; ++i) {

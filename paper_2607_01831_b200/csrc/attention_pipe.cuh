@@ -620,8 +620,8 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
         if ((int)c < p.ncols)
           qv[i] = ld_dep(reinterpret_cast<const uint4*>(p.q + (((size_t)ib * p.nq_stride + j) * p.Hq + (size_t)ih * p.G + hh) * LYNX_D) + (qt & 15));
       }
-      [[maybe_unused]] const uint32_t seeing = ROWS ? columns_that_see(seen) : 0u;
-      const auto sees = [&](int i) { return (seeing >> (i * 4 + (qt >> 4))) & 1u; };
+      [[maybe_unused]] const uint32_t see = __ballot_sync(0xFFFFFFFFu, seen != 0);   // (ROWS) the columns that see a node
+      const auto sees = [&](int i) { return (see >> (i * 4 + (qt >> 4))) & 1u; };
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const uint32_t w[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
@@ -646,19 +646,21 @@ __global__ void __launch_bounds__(PipeCfg<FULL, CP>::kThreads, 1) attn_pipe_kern
         float common = __uint_as_float(m << 16);
         const float all = __uint_as_float(m & 0xFFFF0000u);
         e = i8_q_exponent(common);
-        if (!(all < INFINITY) || i8_q_exponent(all) < e) {   // (the same for both warps)
-          if (!(common < INFINITY)) {   // of the rows that are numbers
-            float top = 0.0f;
+        const bool none = !(common > 0.0f && common < INFINITY);   // (of those that see a node)
+        if (none || !(all < INFINITY) || i8_q_exponent(all) < e) {   // (the same for both warps)
+          if (none) {   // of all rows that are numbers
+            float top = 0.0f, low = INFINITY;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
               const float t = row_largest(qv[i]);
-              if (sees(i) && t < INFINITY) top = fmaxf(top, t);
+              if (t < INFINITY && t > 0.0f) { top = fmaxf(top, t); low = fminf(low, t); }
             }
             top = warp_max(top);
+            low = -warp_max(-low);
             named_bar(6, 64);
-            if (lane == 0) scal[4 * CP + 2 + (warp & 1)] = top;
+            if (lane == 0) scal[4 * CP + 2 + (warp & 1)] = __uint_as_float(range_word(low, top));
             named_bar(6, 64);
-            e = i8_q_exponent(fmaxf(scal[4 * CP + 2], scal[4 * CP + 3]));
+            e = common_exponent(bf16x2_max(__float_as_uint(scal[4 * CP + 2]), __float_as_uint(scal[4 * CP + 3])), i8_q_exponent);
           }
 #pragma unroll
           for (int i = 0; i < NI; ++i) {

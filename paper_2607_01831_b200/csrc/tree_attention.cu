@@ -878,16 +878,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         load4(x, p.q + (((int64_t)b * p.n + j) * p.Hq + h * p.G + (in - j * p.G)) * 16 + quarter * 4, c < p.cols);
         const uint32_t mine = top_bits(x);
         const RowMaxima top = row_maxima(mine, nodes != 0, smem + C::kOffMisc + 64, warp - 8, lane);
-        const int e = query_exponent(top.seeing > 0.0f ? top.seeing : top.all);
-        int own = 0;   // what a row's has more
+        int e = query_exponent(top.seeing > 0.0f ? top.seeing : top.all), own = 0;   // (own: what a row's has more)
         if (gt > 0) wait(kfree + ms.before(1).i * 8, ms.before(1).ph, ab);   // the previous piece's last Q K^T
-        if (__builtin_expect(query_exponent(top.all) > e, 0)) {   // (the same for all threads)
+        if (__builtin_expect(query_exponent(top.all) > e || top.seeing == 0.0f, 0)) {   // (the same for all threads)
           // Rows that see no node may be padding, with anything in them: one with larger entries has a power of two of its own, and a factor for its scores.
           sts32(sums + quarter * 4u, mine);
           named_bar(1, 512);
           const uint2 m01 = lds64(sums), m23 = lds64(sums + 8u);
-          const uint32_t row = max(max(m01.x, m01.y), max(m23.x, m23.y));
-          if (row < 0x7F80u) own = min(max(query_exponent(__uint_as_float(row << 16)) - e, 0), 120);
+          uint32_t row = max(max(m01.x, m01.y), max(m23.x, m23.y));
+          if (row >= 0x7F80u) row = 0u;
+          if (top.seeing == 0.0f) {   // none sees a node: the common one is the smallest row's, unless all rows are within 2^10 of the largest
+            const RowMaxima low = row_maxima(row ? 0x7F7Fu - row : 0u, false, smem + C::kOffMisc + 64, warp - 8, lane);
+            const int of_low = query_exponent(__uint_as_float((0x7F7Fu << 16) - __float_as_uint(low.all)));
+            if (of_low < e - 10) e = of_low;
+          }
+          if (row > 0u) own = min(max(query_exponent(__uint_as_float(row << 16)) - e, 0), 120);
           named_bar(1, 512);
         }
         const float f = pow2(-e - own);

@@ -55,8 +55,8 @@ def _compare(rows, got, lse, want, out_f32=True):
     assert (off <= E + 2.0 ** -18 * (1 + want_lse.abs()))[full].all(), off[full].max().item()
 
 
-def _padding(lens, real, n, G, Hkv, anchor, seed, extra_blocks=0):
-    pr = Problem(lens, n, Hkv, G, seed=seed, extra_blocks=extra_blocks)
+def _padding(lens, real, n, G, Hkv, anchor, seed, extra_blocks=0, kind="tree"):
+    pr = Problem(lens, n, Hkv, G, seed=seed, extra_blocks=extra_blocks, kind=kind)
     live = _pad(pr, real)
     assert not live.all() and live.any()
     pads = [(b, j) for b in range(pr.B) for j in range(n) if not live[b, j]]
@@ -80,6 +80,13 @@ def _padding(lens, real, n, G, Hkv, anchor, seed, extra_blocks=0):
 def test_what_padding_holds(n, G, anchor):
     _padding((700, 40, 300), (max(1, n // 2), max(1, n - 1), 1), n, G, 2, anchor, seed=n + G)
     _padding((9000,), (n - 1,), n, G, 1, anchor, seed=n + G + 1)
+
+
+@pytest.mark.parametrize("n,G,anchor", FEW + MANY)
+def test_what_padding_holds_where_no_row_sees_a_node(n, G, anchor):
+    """The rows that are meant attend to the prefix alone, as the padding does: nothing tells them apart."""
+    _padding((700, 40, 300), (max(1, n // 2), max(1, n - 1), 1), n, G, 2, anchor, seed=n + G, kind="none")
+    _padding((5000,), (1,), n, G, 1, anchor, seed=n + G + 1, kind="none")
 
 
 @pytest.mark.parametrize("n,G", [(17, 1), (8, 4), (4, 8), (6, 5)])

@@ -24,7 +24,7 @@ class Abandoned:
 
 
 def _run(pieces, rng, give_up=None):
-    """pieces: (tiles, whether the last is the nodes', whether rows need a power of two of their own).  give_up: the number of waits after which all waits for
+    """pieces: (tiles, whether the last is the nodes', whether rows need a power of two of their own; 2: and none sees a node).  give_up: the number of waits after which all waits for
     data end at once."""
     place = (lambda name: Abandoned()) if give_up is not None else Place
     B = {name: [Barrier(count) for _ in range(n)] for name, n, count in
@@ -84,6 +84,10 @@ def _run(pieces, rng, give_up=None):
                 sums[i].write((ic, "largest"))
                 yield from meet("1", i, W)
                 yield from read([sums[k] for k in own], (ic, "largest"))
+                if apart == 2:                                         # (none sees a node: the smallest row)
+                    maxima[i].write((ic, "smallest"))
+                    yield from meet("1", i, W)
+                    yield from read(maxima, (ic, "smallest"))
                 yield from meet("1", i, W)
             if i == 0:
                 word[ic & 1].write(ic)
@@ -197,7 +201,7 @@ def _run(pieces, rng, give_up=None):
 
 
 def _pieces(rng):
-    return [(rng.choice([1, 1, 2, 3, 6]), rng.random() < 0.7, rng.random() < 0.5) for _ in range(rng.randint(1, 6))]
+    return [(rng.choice([1, 1, 2, 3, 6]), rng.random() < 0.7, rng.choice([0, 0, 1, 2])) for _ in range(rng.randint(1, 6))]
 
 
 @pytest.mark.parametrize("seed", range(4))
@@ -219,7 +223,7 @@ def test_the_kernel_exchanges_what_is_played():
     code = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "tree_attention.cu")).read())
     body = code[code.index("if (warp < 24) {"):code.index("if (warp == 24) {")]
     assert re.findall(r"named_bar\((\d+), \d+\)|\b(row_maxima|largest_of_8)\(", body) == [
-        ("", "row_maxima"), ("1", ""), ("1", ""), ("1", ""), ("", "largest_of_8"), ("8", "")]
+        ("", "row_maxima"), ("1", ""), ("", "row_maxima"), ("1", ""), ("1", ""), ("", "largest_of_8"), ("8", "")]
     for name, bar in (("RowMaxima row_maxima(", "named_bar(1, 512)"), ("uint32_t largest_of_8(", "named_bar(3, 256)")):
         f = code[code.index(name):]
         f = f[:f.index("\n}")]
