@@ -328,6 +328,30 @@ lynx_status lynx_cache_append(const lynx_shape* shape, const void* k, int64_t k_
                               int64_t n_src, const int32_t* rows, int64_t n_tokens, const int64_t* slots,
                               const lynx_rotary_spec* spec, lynx_plane_out K, lynx_plane_out V, void* stream);
 
+/* Norms of heads: y = x / sqrt(mean x^2 + eps) * weight over a head's channels, FP32.  A tensor without weights is not normed. */
+typedef struct {
+  const void* q_weight;   /* DEVICE [channels of a head], BF16 or (weight_float) float, 16-byte aligned; or NULL */
+  const void* k_weight;   /* likewise */
+  float eps;              /* at least 0 */
+  int32_t weight_float;
+} lynx_head_norm;
+
+/* Norms of queries and keys for each head and their rotary positions, in one pass: lynx_rotary's arguments, conventions and tensors
+ * (in place or not), each head normed before it is turned, one rounding to BF16 behind both.  head_width : 64, 128 or 256 channels (strides at least
+ * heads * head_width, weights of as many); 2 n_pairs <= head_width.  norm or spec may be NULL: the rotation alone (of 64-wide rotary keys
+ * and queries, say), the norm alone, a copy. */
+lynx_status lynx_norm_rotary(const lynx_head_norm* norm, const lynx_rotary_spec* spec, int32_t head_width, const void* q,
+                             int64_t q_stride, int32_t num_q_heads, const void* k, int64_t k_stride, int32_t num_kv_heads,
+                             int64_t n_tokens, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                             void* stream);
+
+/* lynx_cache_append of keys that are normed first, by norm's k_weight (NULL norm or weight: none), then turned, then quantised: FP32 all the way,
+ * no rounding in between. */
+lynx_status lynx_norm_cache_append(const lynx_shape* shape, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                   int64_t n_src, const int32_t* rows, int64_t n_tokens, const int64_t* slots,
+                                   const lynx_head_norm* norm, const lynx_rotary_spec* spec, lynx_plane_out K,
+                                   lynx_plane_out V, void* stream);
+
 /* Reads ranges of tokens back: output row i, offsets[b] <= i < offsets[b + 1], is token starts[b] + i - offsets[b] of sequence b,
  * BF16 bf16_rne(fl(fma(code, scale, zero))) as lynx_recombine writes it, but ordered by token:
  * k_out, v_out : BF16 [n_rows][num_kv_heads][128].  offsets : int32 [batch + 1], non-decreasing from 0; starts : int32 [batch], or
@@ -369,6 +393,46 @@ lynx_status lynx_tree_attention(const lynx_shape* shape, const void* q_bf16, int
                                 int64_t k_stride, const void* v_nodes, int64_t v_stride, const uint64_t* tree_mask,
                                 float softmax_scale, int32_t out_float, void* out, float* lse, void* workspace,
                                 size_t workspace_bytes, void* stream);
+
+/* Block tables, slots and positions from the lengths that requests have (old_lens) and are to have (new_lens), int32 [batch], on the device:
+ * requests that grow take blocks from the pool's free ones, those that shrink (to 0: that end) give blocks back.  With bt = block_tokens,
+ * have = ceil(old / bt) and want = ceil(new / bt) request b needs max(0, want - have) blocks.  It gets them where it needs none or where the sum
+ * of all requests' needs up to and with its own is at most the number of free blocks; else it stays as it is (preempt it, and plan again).
+ * block_table : int32 [batch][max_blocks_per_seq], of which entries [have, want) of a growing request are written and entries [want, have) of a
+ *   shrinking one are given back (and left as they stand).
+ * free_ring : int32 [num_blocks], pool_state : int32 [4] = {place of the first free block in the ring, number of free blocks, 0, 0}.  Free
+ *   blocks are taken from the front, in the requests' order, and given back behind the last, in the requests' order and each request's: results
+ *   do not depend on how the work is spread.  What is free and what requests hold must be at most num_blocks together, and a block held
+ *   by one request at most (a block shared by several is not to be given back through this call).
+ * lens : int32 [batch], the length each request has now: new_lens[b], or old_lens[b] where it did not get its blocks.  Not old_lens or new_lens.
+ * Tokens [old, new) of the requests, one behind the other (a request that did not get its blocks has its rows, too), are rows of
+ * offsets : int32 [batch + 1], or NULL: each request's first row, and their number;
+ * slots : int64 [max_tokens], or NULL: block * bt + offset as lynx_cache_append takes it, -1 for tokens without a block;
+ * positions : int32 [max_tokens], or NULL: the token's number in its sequence, as lynx_rotary_spec takes it.
+ * Rows behind the last have slot -1 and position 0; rows from max_tokens on are left out.  With offsets and old_lens as its starts lynx_cache_read
+ * reads the new tokens back.  Lengths are clamped to [0, max_blocks_per_seq * bt].  Any block_tokens; batch * max_blocks_per_seq * bt and
+ * max_tokens below 2^31 - 8192 (LYNX_ERR_UNSUPPORTED otherwise).  Calls that share a pool are ordered on a stream. */
+lynx_status lynx_plan_blocks(const lynx_shape* shape, const int32_t* old_lens, const int32_t* new_lens, int32_t batch,
+                             int32_t* block_table, int32_t* free_ring, int32_t* pool_state, int64_t max_tokens, int32_t* lens,
+                             int32_t* offsets, int64_t* slots, int32_t* positions, void* stream);
+
+/* Caches of latents: models whose keys and values are expanded from one vector of 512 channels a token, next to a rotary key of 64 that all heads
+ * share.  A latent is four rows of the planes -- num_kv_heads is 4 and head h holds channels [128 h, 128 (h + 1)) --, so that lynx_split_quantize,
+ * lynx_recombine and the transfer of the streams take it as it is.  Rotary keys stay BF16 : rope_pages [num_blocks][block_tokens][64].
+ *
+ * lynx_latent_append: latents BF16 [n_src][512] and rope_keys BF16 [n_src][64], strides as for lynx_rotary (views of one projection's output).
+ * rows, n_tokens, slots: as for lynx_cache_append (of several tokens with one slot, any one's rows and key may remain).  weight : NULL, or 512 BF16
+ * (weight_float: float) weights of a norm over the latent's 512 channels, y = x / sqrt(mean x^2 + eps) * weight, FP32, quantised without a rounding
+ * in between.  spec : NULL, or rotary positions of the keys, 2 n_pairs <= 64, one rounding to BF16.  Pointers 16-byte aligned (slots, meta: 8, rows: 4).
+ * lynx_latent_read: ranges of tokens as lynx_cache_read's, latents_out BF16 [n_rows][512] (residual NULL: the middles of the Anchor's buckets)
+ * and rope_out BF16 [n_rows][64]: what the expanded form of the attention multiplies by its projections.  Any block_tokens, both calls. */
+lynx_status lynx_latent_append(const lynx_shape* shape, const void* latents, int64_t latent_stride, const void* rope_keys,
+                               int64_t rope_stride, int64_t n_src, const int32_t* rows, int64_t n_tokens, const int64_t* slots,
+                               const void* weight, int32_t weight_float, float eps, const lynx_rotary_spec* spec,
+                               lynx_plane_out C, void* rope_pages, void* stream);
+lynx_status lynx_latent_read(const lynx_shape* shape, lynx_plane C, const void* rope_pages, const int32_t* block_table,
+                             int32_t batch, const int32_t* starts, const int32_t* offsets, int64_t n_rows, void* latents_out,
+                             void* rope_out, void* stream);
 
 /* Synchronises `stream`, reads and clears the workspace's status word.  Test / debug use. */
 lynx_status lynx_check(void* workspace, void* stream);

@@ -14,6 +14,7 @@ import functools
 import os
 import warnings
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -38,6 +39,10 @@ class _RotarySpec(ctypes.Structure):
                 ("interleaved", ctypes.c_int32), ("pair_axis", ctypes.c_uint8 * 64)]
 
 
+class _HeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float), ("weight_float", ctypes.c_int32)]
+
+
 class _Shape(ctypes.Structure):
     _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
@@ -49,6 +54,7 @@ EXPORTS = ["lynx_split_quantize", "lynx_recombine", "lynx_workspace_bytes", "lyn
            "lynx_bf16_workspace_bytes", "lynx_bf16_attention", "lynx_hier_quantize", "lynx_hier_dequantize",
            "lynx_token_verify", "lynx_workspace_lse", "lynx_bf16_workspace_lse", "lynx_lse_merge", "lynx_verify_decision", "lynx_split_quantize_bits", "lynx_recombine_bits",
            "lynx_rotary", "lynx_cache_append", "lynx_cache_read", "lynx_tree_workspace_bytes", "lynx_tree_attention",
+           "lynx_norm_rotary", "lynx_norm_cache_append", "lynx_plan_blocks", "lynx_latent_append", "lynx_latent_read",
            "lynx_check",
            "lynx_status_string", "lynx_version"]
 
@@ -120,6 +126,19 @@ def load():
     lib.lynx_tree_attention.argtypes = [ctypes.POINTER(_Shape), vp, i32, i32, _Plane, _Plane, vp, vp, vp, i64, vp, i64, vp, f32, i32,
                                         vp, vp, vp, ctypes.c_size_t, vp]
     lib.lynx_tree_attention.restype = ctypes.c_int
+    lib.lynx_norm_rotary.argtypes = [ctypes.POINTER(_HeadNorm), ctypes.POINTER(_RotarySpec), i32, vp, i64, i32, vp, i64, i32, i64, vp, i64, vp,
+                                     i64, vp]
+    lib.lynx_norm_rotary.restype = ctypes.c_int
+    lib.lynx_norm_cache_append.argtypes = [ctypes.POINTER(_Shape), vp, i64, vp, i64, i64, vp, i64, vp, ctypes.POINTER(_HeadNorm),
+                                           ctypes.POINTER(_RotarySpec), _Plane, _Plane, vp]
+    lib.lynx_norm_cache_append.restype = ctypes.c_int
+    lib.lynx_plan_blocks.argtypes = [ctypes.POINTER(_Shape), vp, vp, i32, vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    lib.lynx_plan_blocks.restype = ctypes.c_int
+    lib.lynx_latent_append.argtypes = [ctypes.POINTER(_Shape), vp, i64, vp, i64, i64, vp, i64, vp, vp, i32, f32, ctypes.POINTER(_RotarySpec),
+                                       _Plane, vp, vp]
+    lib.lynx_latent_append.restype = ctypes.c_int
+    lib.lynx_latent_read.argtypes = [ctypes.POINTER(_Shape), _Plane, vp, vp, i32, vp, vp, i64, vp, vp, vp]
+    lib.lynx_latent_read.restype = ctypes.c_int
     lib.lynx_check.argtypes = [vp, vp]
     lib.lynx_check.restype = ctypes.c_int
     lib.lynx_status_string.argtypes = [ctypes.c_int]
@@ -204,6 +223,9 @@ _fast_bf16, _fast_lse_view = _fast("_fast_bf16", "bf16_attention"), _fast("_fast
 _fast_lse_merge = _fast("_fast_lse_merge", "lse_merge")
 _fast_rotary, _fast_cache_append = _fast("_fast_rotary", "rotary"), _fast("_fast_cache_append", "cache_append")
 _fast_cache_read, _fast_tree_attention = _fast("_fast_cache_read", "cache_read"), _fast("_fast_tree_attention", "tree_attention")
+_fast_norm_rotary, _fast_norm_append = _fast("_fast_norm_rotary", "norm_rotary"), _fast("_fast_norm_append", "norm_cache_append")
+_fast_plan_blocks = _fast("_fast_plan_blocks", "plan_blocks")
+_fast_latent_append, _fast_latent_read = _fast("_fast_latent_append", "latent_append"), _fast("_fast_latent_read", "latent_read")
 _fast_hier_quantize, _fast_hier_dequantize = _fast("_fast_hier_quantize", "hier_quantize"), _fast("_fast_hier_dequantize", "hier_dequantize")
 
 
@@ -584,16 +606,16 @@ def rotary_table(n_positions: int, pairs: int = 64, base: float = 10000.0, devic
     return torch.cat((angle.cos(), angle.sin()), 1).float()
 
 
-def _token_rows(t: torch.Tensor, what: str):
-    """Pointer, token stride and heads of BF16 [tokens][heads][128] whose tokens may lie apart (a view of a fused projection)."""
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != D:
-        raise LynxError(f"{what} must be BF16 [tokens][heads][128]")
+def _token_rows(t: torch.Tensor, what: str, width: int = D):
+    """Pointer, token stride and heads of BF16 [tokens][heads][width] whose tokens may lie apart (a view of a fused projection)."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != width:
+        raise LynxError(f"{what} must be BF16 [tokens][heads][{width}]")
     if not t.is_cuda:
         raise LynxError("device tensors required")
     T, H = t.shape[:2]
-    if T and (t.stride(2) != 1 or (H > 1 and t.stride(1) != D)):
+    if T and (t.stride(2) != 1 or (H > 1 and t.stride(1) != width)):
         raise LynxError(f"{what}: the heads of a token must lie one behind the other")
-    return t.data_ptr(), t.stride(0) if T > 1 else H * D, H
+    return t.data_ptr(), t.stride(0) if T > 1 else H * width, H
 
 
 def rotary(q: torch.Tensor | None, k: torch.Tensor | None, spec: Rotary, q_out: torch.Tensor | None = None,
@@ -621,6 +643,75 @@ def rotary(q: torch.Tensor | None, k: torch.Tensor | None, spec: Rotary, q_out: 
     return qo, ko
 
 
+def _here(*tensors):
+    """Tensors (and planes) of a call must be on the current device, whose stream it uses."""
+    for t in tensors:
+        if isinstance(t, Planes):
+            _here(t.anchor, t.residual, t.meta)
+        elif isinstance(t, Rotary):
+            _here(t.positions, t.cos_sin)
+        elif isinstance(t, HeadNorm):
+            _here(t.q_weight, t.k_weight)
+        elif t is not None:
+            if not t.is_cuda:
+                raise LynxError("device tensors required")
+            if t.device.index != torch.cuda.current_device():
+                raise LynxError("tensors must be on the current device")
+
+
+@dataclass(frozen=True)
+class HeadNorm:
+    """Norms of heads, y = x / sqrt(mean x^2 + eps) * weight: weights BF16 or float32 (both alike) of as many values as a head has channels.  A
+    tensor whose weight is None is not normed."""
+    q_weight: torch.Tensor | None = None
+    k_weight: torch.Tensor | None = None
+    eps: float = 1e-6
+
+    def __post_init__(self):
+        given = [w for w in (self.q_weight, self.k_weight) if w is not None]
+        if any(w.dim() != 1 or w.dtype not in (torch.bfloat16, torch.float32) or w.dtype != given[0].dtype or w.shape != given[0].shape for w in given):
+            raise LynxError("a norm's weights must be BF16 or float32 [channels of a head], both alike")
+        object.__setattr__(self, "eps", float(self.eps))
+        if not self.eps >= 0.0:
+            raise LynxError("eps must be at least 0")
+
+    def _c(self, width: int):
+        some = self.k_weight if self.q_weight is None else self.q_weight
+        if some is not None and some.shape[0] != width:
+            raise LynxError(f"the norm's weights must be {width} values, as a head has channels")
+        return ctypes.byref(_HeadNorm(_ptr(self.q_weight), _ptr(self.k_weight), self.eps, int(some is not None and some.dtype == torch.float32)))
+
+
+def norm_rotary(q: torch.Tensor | None, k: torch.Tensor | None, norm: HeadNorm | None = None, spec: Rotary | None = None,
+                q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
+    """lynx_norm_rotary: q BF16 [T][Hq][W], k BF16 [T][Hkv][W], W = 64, 128 or 256 (either may be None; tokens may lie apart), each head normed
+    and turned in one pass -> (q_out, k_out), which may be the inputs.  norm or spec None: that part is left out."""
+    r = _fast_norm_rotary(q, k, norm, spec, q_out, k_out)
+    if r is not None:
+        return _result(r, "lynx_norm_rotary")
+    if q is None and k is None:
+        raise LynxError("q or k is needed")
+    some = q if q is not None else k
+    T, width = some.shape[0], some.shape[-1]
+    if width not in (64, 128, 256):
+        raise LynxError("heads must have 64, 128 or 256 channels")
+    rows = []
+    for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            rows.append((None, (None, 0, 0), (None, 0, 0)))
+            continue
+        if x.shape[0] != T or (out is not None and out.shape != x.shape):
+            raise LynxError("q and k must have as many tokens, and the outputs their shapes")
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        rows.append((out, _token_rows(x, what, width), _token_rows(out, what + "_out", width)))
+    _here(q, k, q_out, k_out, norm, spec)
+    (qo, qi, qw), (ko, ki, kw) = rows
+    _ok(load().lynx_norm_rotary(None if norm is None else norm._c(width), None if spec is None else spec._c(T), width, qi[0], qi[1], qi[2], ki[0],
+                                ki[1], ki[2], T, qw[0], qw[1], kw[0], kw[1], _stream()), "lynx_norm_rotary")
+    return qo, ko
+
+
 def _planes_fit(geo: Geometry, *planes: Planes):
     rows = geo.num_blocks * geo.num_kv_heads * geo.block_tokens
     for p in planes:
@@ -630,13 +721,14 @@ def _planes_fit(geo: Geometry, *planes: Planes):
 
 
 def cache_append(geo: Geometry, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, K: Planes, V: Planes,
-                 rows: torch.Tensor | None = None, rotary: Rotary | None = None):
-    """lynx_cache_append: quantises tokens' keys and values BF16 [T][Hkv][128] (tokens may lie apart) into the planes K and V.  slots
+                 rows: torch.Tensor | None = None, rotary: Rotary | None = None, norm: HeadNorm | None = None):
+    """lynx_cache_append, with a norm lynx_norm_cache_append: quantises tokens' keys and values BF16 [T][Hkv][128] (tokens may lie apart) into the planes K and V.  slots
     i64 [n]: block * block_tokens + offset of each token written, negative for none; rows i32 [n]: the source row of each
-    (None: row i); rotary: positions for the keys, by source row."""
-    r = _fast_cache_append(geo, k, v, slots, K, V, rows, rotary)
+    (None: row i); norm: its k_weight norms the keys first; rotary: positions for the keys, by source row."""
+    r = _fast_cache_append(geo, k, v, slots, K, V, rows, rotary) if norm is None else \
+        _fast_norm_append(geo, k, v, slots, K, V, rows, rotary, norm)
     if r is not None:
-        return _ok(r, "lynx_cache_append")
+        return _ok(r, "lynx_cache_append" if norm is None else "lynx_norm_cache_append")
     (kp, ks, kh), (vp, vs, vh) = _token_rows(k, "k"), _token_rows(v, "v")
     if kh != geo.num_kv_heads or vh != kh or v.shape[0] != k.shape[0]:
         raise LynxError("k and v must be BF16 [tokens][num_kv_heads][128]")
@@ -644,6 +736,11 @@ def cache_append(geo: Geometry, k: torch.Tensor, v: torch.Tensor, slots: torch.T
         raise LynxError("slots must be int64 [n], rows int32 [n]")
     _planes_fit(geo, K, V)
     T = k.shape[0]
+    if norm is not None:
+        _here(k, v, slots, rows, K, V, rotary, norm)
+        return _ok(load().lynx_norm_cache_append(ctypes.byref(geo._c()), kp, ks, vp, vs, T, _ptr(rows), slots.numel(), _ptr(slots),
+                                                 norm._c(D), None if rotary is None else rotary._c(T), K._c(), V._c(), _stream()),
+                   "lynx_norm_cache_append")
     _ok(load().lynx_cache_append(ctypes.byref(geo._c()), kp, ks, vp, vs, T, _ptr(rows), slots.numel(), _ptr(slots),
                                  None if rotary is None else rotary._c(T), K._c(), V._c(), _stream()), "lynx_cache_append")
 
@@ -676,6 +773,122 @@ def cache_read(geo: Geometry, K: Planes, V: Planes, block_table: torch.Tensor, s
     _ok(load().lynx_cache_read(ctypes.byref(geo._c()), planes[0], planes[1], _ptr(block_table), B, _ptr(starts), _ptr(offsets), n_rows,
                                _ptr(outs[0]), _ptr(outs[1]), _stream()), "lynx_cache_read")
     return outs[0], outs[1]
+
+
+@dataclass
+class BlockPool:
+    """Free blocks of a cache: ring i32 [num_blocks], state i32 [4] = {place of the first free block, number of free blocks, 0, 0}."""
+    ring: torch.Tensor
+    state: torch.Tensor
+
+
+def make_block_pool(num_blocks: int, device) -> BlockPool:
+    """All blocks free, in order."""
+    return BlockPool(torch.arange(num_blocks, dtype=torch.int32, device=device),
+                     torch.tensor([0, num_blocks, 0, 0], dtype=torch.int32, device=device))
+
+
+class BlockPlan(NamedTuple):
+    lens: torch.Tensor         # i32 [B] the length that each request has now
+    offsets: torch.Tensor      # i32 [B + 1] first row of each request's new tokens
+    slots: torch.Tensor        # i64 [max_tokens]
+    positions: torch.Tensor    # i32 [max_tokens]
+
+
+def plan_blocks(geo: Geometry, pool: BlockPool, block_table: torch.Tensor, old_lens: torch.Tensor, new_lens: torch.Tensor,
+                max_tokens: int) -> BlockPlan:
+    """lynx_plan_blocks: requests of old_lens i32 [B] tokens are to have new_lens i32 [B]; block_table i32 [B][max_blocks_per_seq] and the pool
+    are brought up to date, and each new token gets its slot (for cache_append) and position (for Rotary); starts of a cache_read are old_lens."""
+    r = _fast_plan_blocks(geo, pool.ring, pool.state, block_table, old_lens, new_lens, max_tokens)
+    if r is not None:
+        return BlockPlan(*_result(r, "lynx_plan_blocks"))
+    B = block_table.shape[0]
+    if block_table.dtype != torch.int32 or tuple(block_table.shape) != (B, geo.max_blocks_per_seq):
+        raise LynxError("block_table must be int32 [B][max_blocks_per_seq]")
+    if any(x.dtype != torch.int32 or tuple(x.shape) != (B,) for x in (old_lens, new_lens)):
+        raise LynxError("old_lens, new_lens must be int32 [B]")
+    if pool.ring.dtype != torch.int32 or tuple(pool.ring.shape) != (geo.num_blocks,) or pool.state.dtype != torch.int32 or \
+            tuple(pool.state.shape) != (4,):
+        raise LynxError("the pool must be int32 [num_blocks] and int32 [4]")
+    if max_tokens < 0:
+        raise LynxError("max_tokens must be at least 0")
+    _here(block_table, old_lens, new_lens, pool.ring, pool.state)
+    dev = block_table.device
+    out = BlockPlan(torch.empty(B, dtype=torch.int32, device=dev), torch.empty(B + 1, dtype=torch.int32, device=dev),
+                    torch.empty(max_tokens, dtype=torch.int64, device=dev), torch.empty(max_tokens, dtype=torch.int32, device=dev))
+    _ok(load().lynx_plan_blocks(ctypes.byref(geo._c()), _ptr(old_lens), _ptr(new_lens), B, _ptr(block_table), _ptr(pool.ring), _ptr(pool.state),
+                                max_tokens, _ptr(out.lens), _ptr(out.offsets), _ptr(out.slots), _ptr(out.positions), _stream()),
+        "lynx_plan_blocks")
+    return out
+
+
+# ---------------------------------------------------------------------------------------------- caches of latents
+LATENT, ROPE = 512, 64
+
+
+def _latent_rows(t: torch.Tensor, width: int, what: str):
+    """Pointer and token stride of BF16 [tokens][width] whose tokens may lie apart."""
+    if t.dtype != torch.bfloat16 or t.dim() != 2 or t.shape[1] != width:
+        raise LynxError(f"{what} must be BF16 [tokens][{width}]")
+    return _token_rows(t[:, None], what, width)[:2]
+
+
+def _latent_fit(geo: Geometry, C: Planes, pages: torch.Tensor):
+    if geo.num_kv_heads != 4:
+        raise LynxError("a latent is four rows of the planes: num_kv_heads must be 4")
+    _planes_fit(geo, C)
+    if pages.dtype != torch.bfloat16 or pages.numel() < geo.num_blocks * geo.block_tokens * ROPE:
+        raise LynxError("rope_pages must be BF16 [num_blocks][block_tokens][64]")
+
+
+def latent_append(geo: Geometry, latents: torch.Tensor, rope_keys: torch.Tensor, slots: torch.Tensor, C: Planes, rope_pages: torch.Tensor,
+                  weight: torch.Tensor | None = None, eps: float = 1e-6, rows: torch.Tensor | None = None, rotary: Rotary | None = None):
+    """lynx_latent_append: tokens' latents BF16 [T][512] (normed with weight BF16 or float32 [512], where given) into the planes C of a geometry with
+    num_kv_heads = 4, and rotary keys BF16 [T][64] (turned, where rotary is given) into rope_pages BF16 [num_blocks][block_tokens][64].  slots and
+    rows as for cache_append."""
+    eps = float(eps)
+    r = _fast_latent_append(geo, latents, rope_keys, slots, C, rope_pages, weight, eps, rows, rotary)
+    if r is not None:
+        return _ok(r, "lynx_latent_append")
+    (cp, cs), (kp, ks) = _latent_rows(latents, LATENT, "latents"), _latent_rows(rope_keys, ROPE, "rope_keys")
+    T = latents.shape[0]
+    if rope_keys.shape[0] != T:
+        raise LynxError("latents and rope_keys must have as many tokens")
+    if slots.dtype != torch.int64 or slots.dim() != 1 or (rows is not None and (rows.dtype != torch.int32 or rows.shape != slots.shape)):
+        raise LynxError("slots must be int64 [n], rows int32 [n]")
+    if weight is not None and (weight.dtype not in (torch.bfloat16, torch.float32) or tuple(weight.shape) != (LATENT,)):
+        raise LynxError("weight must be BF16 or float32 [512]")
+    _latent_fit(geo, C, rope_pages)
+    _here(latents, rope_keys, slots, C, rope_pages, weight, rows, rotary)
+    _ok(load().lynx_latent_append(ctypes.byref(geo._c()), cp, cs, kp, ks, T, _ptr(rows), slots.numel(), _ptr(slots), _ptr(weight),
+                                  int(weight is not None and weight.dtype == torch.float32), eps, None if rotary is None else rotary._c(T), C._c(),
+                                  _ptr(rope_pages), _stream()), "lynx_latent_append")
+
+
+def latent_read(geo: Geometry, C: Planes, rope_pages: torch.Tensor, block_table: torch.Tensor, starts: torch.Tensor | None, offsets: torch.Tensor,
+                n_rows: int, anchor_only: bool = False):
+    """lynx_latent_read: ranges of tokens as cache_read's -> latents BF16 [n_rows][512], rotary keys BF16 [n_rows][64]."""
+    r = _fast_latent_read(geo, C, rope_pages, block_table, starts, offsets, n_rows, anchor_only)
+    if r is not None:
+        return _result(r, "lynx_latent_read")
+    B = block_table.shape[0]
+    if block_table.dtype != torch.int32 or tuple(block_table.shape) != (B, geo.max_blocks_per_seq):
+        raise LynxError("block_table must be int32 [B][max_blocks_per_seq]")
+    if offsets.dtype != torch.int32 or tuple(offsets.shape) != (B + 1,) or \
+            (starts is not None and (starts.dtype != torch.int32 or tuple(starts.shape) != (B,))):
+        raise LynxError("offsets must be int32 [B + 1], starts int32 [B]")
+    _latent_fit(geo, C, rope_pages)
+    if not anchor_only and C.residual is None:
+        raise LynxError("the Residual plane is needed unless anchor_only")
+    if n_rows < 0:
+        raise LynxError("n_rows must be at least 0")
+    _here(C, rope_pages, block_table, starts, offsets)
+    out = torch.empty(n_rows, LATENT, dtype=torch.bfloat16, device=block_table.device)
+    keys = torch.empty(n_rows, ROPE, dtype=torch.bfloat16, device=block_table.device)
+    plane = _Plane(_ptr(C.anchor), None if anchor_only else _ptr(C.residual), _ptr(C.meta))
+    _ok(load().lynx_latent_read(ctypes.byref(geo._c()), plane, _ptr(rope_pages), _ptr(block_table), B, _ptr(starts), _ptr(offsets), n_rows,
+                                _ptr(out), _ptr(keys), _stream()), "lynx_latent_read")
+    return out, keys
 
 
 def tree_workspace_bytes(geo: Geometry, batch: int, n_nodes: int) -> int:

@@ -44,7 +44,7 @@ bool float_of(PyObject* o, float* v) {
   *v = (float)PyFloat_AS_DOUBLE(o);
   return true;
 }
-PyObject *s_positions, *s_cos_sin, *s_axis, *s_interleaved;
+PyObject *s_positions, *s_cos_sin, *s_axis, *s_interleaved, *s_q_weight, *s_k_weight, *s_eps;
 PyObject *s_hq, *s_hkv, *s_d, *s_bt, *s_nb, *s_mb, *s_anchor, *s_residual, *s_meta;
 
 bool int_attr(PyObject* o, PyObject* name, int32_t* v) {
@@ -328,18 +328,18 @@ PyObject* hier_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // ---- around the cache: tokens' rows may lie apart
 // BF16 [..][heads][128] of a tensor that is not contiguous as a whole; stride: elements from a token to the next.
-const at::Tensor* rows_of(PyObject* o, int dim, int64_t* stride) {
+const at::Tensor* rows_of(PyObject* o, int dim, int64_t* stride, int64_t width = kD) {
   if (!THPVariable_CheckExact(o)) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
-  if (!t.defined() || !t.is_cuda() || at::isTensorSubclassLike(t) || t.scalar_type() != at::kBFloat16 || t.dim() != dim || t.size(-1) != kD) return nullptr;
+  if (!t.defined() || !t.is_cuda() || at::isTensorSubclassLike(t) || t.scalar_type() != at::kBFloat16 || t.dim() != dim || t.size(-1) != width) return nullptr;
   const int64_t H = t.size(-2), n = t.size(-3);
-  if (t.numel() == 0 || t.stride(-1) != 1 || (H > 1 && t.stride(-2) != kD)) return nullptr;
+  if (t.numel() == 0 || t.stride(-1) != 1 || (H > 1 && t.stride(-2) != width)) return nullptr;
   if (dim == 3) {
-    *stride = n > 1 ? t.stride(0) : H * kD;
+    *stride = n > 1 ? t.stride(0) : H * width;
   } else {   // [batch][nodes][heads][128]: one stride for all nodes
     const int64_t B = t.size(0);
     if (n > 1 && B > 1 && t.stride(0) != n * t.stride(1)) return nullptr;
-    *stride = n > 1 ? t.stride(1) : B > 1 ? t.stride(0) : H * kD;
+    *stride = n > 1 ? t.stride(1) : B > 1 ? t.stride(0) : H * width;
   }
   return &t;
 }
@@ -348,7 +348,7 @@ const at::Tensor* typed(PyObject* o, at::ScalarType type) {
   return t && t->scalar_type() == type ? t : nullptr;
 }
 // Planes that hold a geometry's rows.  The objects keep their tensors alive over the call.
-bool planes_fit(PyObject* o, const lynx_shape& s, bool residual, lynx_plane* pl) {
+bool planes_fit(PyObject* o, const lynx_shape& s, bool residual, lynx_plane* pl, bool current = false) {   // (current: on the current device)
   const int64_t rows = (int64_t)s.num_blocks * s.num_kv_heads * s.block_tokens;
   PyObject* names[3] = {s_anchor, s_residual, s_meta};
   void* p[3] = {nullptr, nullptr, nullptr};
@@ -358,9 +358,10 @@ bool planes_fit(PyObject* o, const lynx_shape& s, bool residual, lynx_plane* pl)
     const at::Tensor* t = plain(a);
     const bool ok = (t && t->scalar_type() == (i == 2 ? at::kFloat : at::kByte) && t->numel() >= rows * (i == 2 ? 2 : 64)) ||
                     (i == 1 && !residual && is_none(a));
+    const bool elsewhere = current && t && t->get_device() != c10::cuda::current_device();
     p[i] = ptr(t);
     Py_DECREF(a);
-    if (!ok) return false;
+    if (!ok || elsewhere) return false;
   }
   *pl = {(const uint8_t*)p[0], residual ? (const uint8_t*)p[1] : nullptr, (const float*)p[2]};
   return true;
@@ -522,10 +523,214 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Whether all of the given tensors are on the current device, whose stream a call uses: else the Python bodies refuse them.
+bool here(std::initializer_list<const at::Tensor*> tensors) {
+  const auto dev = c10::cuda::current_device();
+  for (const at::Tensor* t : tensors)
+    if (t && t->get_device() != dev) return false;
+  return true;
+}
+// A norm's weights: BF16 or float, one type, as many as a head has channels; the object keeps them alive over the call.
+bool norm_of(PyObject* o, int64_t width, lynx_head_norm* n) {
+  *n = {nullptr, nullptr, 0.0f, 0};
+  if (is_none(o)) return true;
+  PyObject *w[2] = {PyObject_GetAttr(o, s_q_weight), PyObject_GetAttr(o, s_k_weight)}, *eps = PyObject_GetAttr(o, s_eps);
+  bool ok = w[0] && w[1] && eps && float_of(eps, &n->eps);
+  const at::Tensor* t[2] = {nullptr, nullptr};
+  for (int i = 0; ok && i < 2; ++i) {
+    if (is_none(w[i])) continue;
+    t[i] = plain(w[i]);
+    ok = t[i] && t[i]->dim() == 1 && t[i]->size(0) == width && (t[i]->scalar_type() == at::kBFloat16 || t[i]->scalar_type() == at::kFloat);
+  }
+  ok = ok && here({t[0], t[1]}) && (!t[0] || !t[1] || t[0]->scalar_type() == t[1]->scalar_type());
+  if (ok) {
+    n->q_weight = ptr(t[0]);
+    n->k_weight = ptr(t[1]);
+    const at::Tensor* some = t[0] ? t[0] : t[1];
+    n->weight_float = some && some->scalar_type() == at::kFloat;
+  }
+  PyErr_Clear();
+  Py_XDECREF(w[0]);
+  Py_XDECREF(w[1]);
+  Py_XDECREF(eps);
+  return ok;
+}
+
+// q, k, norm or None, spec or None, q_out, k_out -> (q_out, k_out)
+PyObject* norm_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 6) Py_RETURN_NONE;
+    const at::Tensor *in[2] = {nullptr, nullptr};
+    at::Tensor out[2];
+    int64_t si[2] = {0, 0}, so[2] = {0, 0}, T = -1, width = 0;
+    for (int i = 0; i < 2; ++i) {
+      if (is_none(a[i])) continue;
+      if (!THPVariable_CheckExact(a[i])) Py_RETURN_NONE;
+      const at::Tensor& t = THPVariable_Unpack(a[i]);
+      if (!t.defined() || t.dim() != 3 || (width && t.size(2) != width)) Py_RETURN_NONE;
+      width = t.size(2);
+      if (width != 64 && width != 128 && width != 256) Py_RETURN_NONE;
+      in[i] = rows_of(a[i], 3, &si[i], width);
+      if (!in[i] || in[i]->size(1) > INT32_MAX || (T >= 0 && in[i]->size(0) != T)) Py_RETURN_NONE;
+      T = in[i]->size(0);
+      if (is_none(a[4 + i])) {
+        out[i] = empty_like_device(in[i]->sizes(), at::kBFloat16, *in[i]);
+        so[i] = in[i]->size(1) * width;
+      } else {
+        const at::Tensor* o = rows_of(a[4 + i], 3, &so[i], width);
+        if (!o || o->sizes() != in[i]->sizes()) Py_RETURN_NONE;
+        out[i] = *o;
+      }
+    }
+    lynx_rotary_spec r;
+    lynx_head_norm norm;
+    const bool turn = !is_none(a[3]);
+    if (T < 0 || !here({in[0], in[1], out[0].defined() ? &out[0] : nullptr, out[1].defined() ? &out[1] : nullptr}) || !norm_of(a[2], width, &norm) || (turn && !rotary_of(a[3], T, &r))) Py_RETURN_NONE;
+    void* st = stream();
+    const lynx_status rc = unlocked([&] {
+      return lynx_norm_rotary(&norm, turn ? &r : nullptr, (int32_t)width, ptr(in[0]), si[0], in[0] ? (int32_t)in[0]->size(1) : 0, ptr(in[1]), si[1],
+                              in[1] ? (int32_t)in[1]->size(1) : 0, T, out[0].defined() ? out[0].data_ptr() : nullptr, so[0],
+                              out[1].defined() ? out[1].data_ptr() : nullptr, so[1], st);
+    });
+    if (rc != LYNX_OK) return status(rc);
+    PyObject* res = PyTuple_New(2);
+    if (!res) return nullptr;
+    for (int i = 0; i < 2; ++i)
+      PyTuple_SET_ITEM(res, i, !in[i] ? Py_NewRef(Py_None) : is_none(a[4 + i]) ? THPVariable_Wrap(out[i]) : Py_NewRef(a[4 + i]));
+    return res;
+  });
+}
+
+// geo, k, v, slots, K, V, rows or None, rotary or None, norm -> status
+PyObject* norm_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    lynx_shape s;
+    lynx_plane K, V;
+    if (n != 9 || !shape_of(a[0], &s)) Py_RETURN_NONE;
+    int64_t sk = 0, sv = 0;
+    const at::Tensor *k = rows_of(a[1], 3, &sk), *v = rows_of(a[2], 3, &sv), *slots = typed(a[3], at::kLong), *rows = typed(a[6], at::kInt);
+    if (!k || !v || !slots || slots->dim() != 1 || (!rows && !is_none(a[6])) || (rows && (rows->dim() != 1 || rows->numel() != slots->numel())) ||
+        k->size(1) != s.num_kv_heads || v->sizes() != k->sizes() || !planes_fit(a[4], s, true, &K, true) || !planes_fit(a[5], s, true, &V, true) || !here({k, v, slots, rows}))
+      Py_RETURN_NONE;
+    lynx_rotary_spec r;
+    lynx_head_norm norm;
+    const bool turn = !is_none(a[7]);
+    if ((turn && !rotary_of(a[7], k->size(0), &r)) || !norm_of(a[8], kD, &norm)) Py_RETURN_NONE;
+    const lynx_plane_out ko = {const_cast<uint8_t*>(K.anchor), const_cast<uint8_t*>(K.residual), const_cast<float*>(K.meta)},
+                         vo = {const_cast<uint8_t*>(V.anchor), const_cast<uint8_t*>(V.residual), const_cast<float*>(V.meta)};
+    void* st = stream();
+    return status(unlocked([&] {
+      return lynx_norm_cache_append(&s, k->data_ptr(), sk, v->data_ptr(), sv, k->size(0), (const int32_t*)ptr(rows), slots->numel(),
+                                    (const int64_t*)slots->data_ptr(), &norm, turn ? &r : nullptr, ko, vo, st);
+    }));
+  });
+}
+
+// geo, ring, state, block_table, old_lens, new_lens, max_tokens -> (lens, offsets, slots, positions)
+PyObject* plan_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    lynx_shape s;
+    int32_t rows;
+    if (n != 7 || !shape_of(a[0], &s) || !int_of(a[6], &rows) || rows < 0) Py_RETURN_NONE;
+    const at::Tensor *ring = typed(a[1], at::kInt), *state = typed(a[2], at::kInt), *table = typed(a[3], at::kInt), *from = typed(a[4], at::kInt),
+                     *to = typed(a[5], at::kInt);
+    if (!ring || !state || !table || !from || !to || ring->dim() != 1 || ring->numel() != s.num_blocks || state->dim() != 1 || state->numel() != 4 ||
+        table->dim() != 2 || table->size(1) != s.max_blocks_per_seq || table->size(0) > INT32_MAX || from->dim() != 1 || to->dim() != 1 ||
+        from->numel() != table->size(0) || to->numel() != from->numel() || !here({ring, state, table, from, to}))
+      Py_RETURN_NONE;
+    const int64_t B = from->numel();
+    at::Tensor t[4] = {empty_like_device({B}, at::kInt, *from), empty_like_device({B + 1}, at::kInt, *from), empty_like_device({rows}, at::kLong, *from),
+                       empty_like_device({rows}, at::kInt, *from)};
+    void* st = stream();
+    const lynx_status rc = unlocked([&] {
+      return lynx_plan_blocks(&s, (const int32_t*)from->data_ptr(), (const int32_t*)to->data_ptr(), (int32_t)B, (int32_t*)table->data_ptr(),
+                              (int32_t*)ring->data_ptr(), (int32_t*)state->data_ptr(), rows, (int32_t*)t[0].data_ptr(), (int32_t*)t[1].data_ptr(),
+                              (int64_t*)t[2].data_ptr(), (int32_t*)t[3].data_ptr(), st);
+    });
+    if (rc != LYNX_OK) return status(rc);
+    PyObject* r = PyTuple_New(4);
+    if (!r) return nullptr;
+    for (int i = 0; i < 4; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(t[i]));
+    return r;
+  });
+}
+
+// ---- latents
+constexpr int64_t kLatent = 512, kRope = 64;
+// BF16 [tokens][width], rows apart
+const at::Tensor* token_rows(PyObject* o, int64_t width, int64_t* stride) {
+  if (!THPVariable_CheckExact(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.defined() || !t.is_cuda() || at::isTensorSubclassLike(t) || t.scalar_type() != at::kBFloat16 || t.dim() != 2 || t.size(1) != width ||
+      t.size(0) == 0 || t.stride(1) != 1)
+    return nullptr;
+  *stride = t.size(0) > 1 ? t.stride(0) : width;
+  return &t;
+}
+const at::Tensor* rope_pages(PyObject* o, const lynx_shape& s) {
+  const at::Tensor* t = typed(o, at::kBFloat16);
+  return t && s.num_kv_heads == 4 && t->numel() >= (int64_t)s.num_blocks * s.block_tokens * kRope ? t : nullptr;
+}
+
+// geo, latents, rope_keys, slots, planes, pages, weight or None, eps, rows or None, rotary or None -> status
+PyObject* latent_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    lynx_shape s;
+    lynx_plane C;
+    float eps;
+    if (n != 10 || !shape_of(a[0], &s) || !float_of(a[7], &eps)) Py_RETURN_NONE;
+    int64_t sc = 0, sk = 0;
+    const at::Tensor *c = token_rows(a[1], kLatent, &sc), *k = token_rows(a[2], kRope, &sk), *slots = typed(a[3], at::kLong), *pages = rope_pages(a[5], s),
+                     *weight = plain(a[6]), *rows = typed(a[8], at::kInt);
+    if (!c || !k || !slots || !pages || slots->dim() != 1 || k->size(0) != c->size(0) || (!rows && !is_none(a[8])) ||
+        (rows && (rows->dim() != 1 || rows->numel() != slots->numel())) || (!weight && !is_none(a[6])) ||
+        (weight && (weight->dim() != 1 || weight->size(0) != kLatent || (weight->scalar_type() != at::kBFloat16 && weight->scalar_type() != at::kFloat))) ||
+        !planes_fit(a[4], s, true, &C, true) || !here({c, k, slots, pages, weight, rows}))
+      Py_RETURN_NONE;
+    lynx_rotary_spec r;
+    const bool turn = !is_none(a[9]);
+    if (turn && !rotary_of(a[9], c->size(0), &r)) Py_RETURN_NONE;
+    const lynx_plane_out o = {const_cast<uint8_t*>(C.anchor), const_cast<uint8_t*>(C.residual), const_cast<float*>(C.meta)};
+    void* st = stream();
+    return status(unlocked([&] {
+      return lynx_latent_append(&s, c->data_ptr(), sc, k->data_ptr(), sk, c->size(0), (const int32_t*)ptr(rows), slots->numel(),
+                                (const int64_t*)slots->data_ptr(), ptr(weight), weight && weight->scalar_type() == at::kFloat, eps, turn ? &r : nullptr, o,
+                                pages->data_ptr(), st);
+    }));
+  });
+}
+
+// geo, planes, pages, block_table, starts or None, offsets, n_rows, anchor_only -> (latents, rope keys)
+PyObject* latent_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    lynx_shape s;
+    lynx_plane C;
+    int32_t n_rows;
+    if (n != 8 || !shape_of(a[0], &s) || !PyBool_Check(a[7]) || !int_of(a[6], &n_rows) || n_rows < 0) Py_RETURN_NONE;
+    const at::Tensor *pages = rope_pages(a[2], s), *table = typed(a[3], at::kInt), *starts = typed(a[4], at::kInt), *offsets = typed(a[5], at::kInt);
+    if (!pages || !table || table->dim() != 2 || table->size(1) != s.max_blocks_per_seq || table->size(0) >= INT32_MAX || !offsets || offsets->dim() != 1 ||
+        offsets->numel() != table->size(0) + 1 || (!starts && !is_none(a[4])) || (starts && (starts->dim() != 1 || starts->numel() != table->size(0))) ||
+        !planes_fit(a[1], s, a[7] == Py_False, &C, true) || !here({pages, table, starts, offsets}))
+      Py_RETURN_NONE;
+    at::Tensor out[2] = {empty_like_device({n_rows, kLatent}, at::kBFloat16, *table), empty_like_device({n_rows, kRope}, at::kBFloat16, *table)};
+    void* st = stream();
+    const lynx_status rc = unlocked([&] {
+      return lynx_latent_read(&s, C, pages->data_ptr(), (const int32_t*)table->data_ptr(), (int32_t)table->size(0), (const int32_t*)ptr(starts),
+                              (const int32_t*)offsets->data_ptr(), n_rows, out[0].data_ptr(), out[1].data_ptr(), st);
+    });
+    if (rc != LYNX_OK) return status(rc);
+    PyObject* r = PyTuple_New(2);
+    if (!r) return nullptr;
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(out[i]));
+    return r;
+  });
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(anchor_attention), FAST(merge_verify_attention), FAST(bf16_attention), FAST(split_quantize), FAST(recombine),
                          FAST(lse_view), FAST(lse_merge), FAST(hier_quantize), FAST(hier_dequantize),
-                         FAST(rotary), FAST(cache_append), FAST(cache_read), FAST(tree_attention), {nullptr, nullptr, 0, nullptr}};
+                         FAST(rotary), FAST(cache_append), FAST(cache_read), FAST(tree_attention),
+                         FAST(norm_rotary), FAST(norm_cache_append), FAST(plan_blocks), FAST(latent_append), FAST(latent_read), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -534,7 +739,8 @@ PyMODINIT_FUNC PyInit__native() {
   struct { PyObject** s; const char* n; } names[] = {{&s_hq, "num_q_heads"}, {&s_hkv, "num_kv_heads"}, {&s_d, "head_dim"}, {&s_bt, "block_tokens"},
                                                      {&s_nb, "num_blocks"}, {&s_mb, "max_blocks_per_seq"}, {&s_anchor, "anchor"},
                                                      {&s_residual, "residual"}, {&s_meta, "meta"}, {&s_positions, "positions"}, {&s_cos_sin, "cos_sin"},
-                                                     {&s_axis, "_axis"}, {&s_interleaved, "interleaved"}};
+                                                     {&s_axis, "_axis"}, {&s_interleaved, "interleaved"}, {&s_q_weight, "q_weight"},
+                                                     {&s_k_weight, "k_weight"}, {&s_eps, "eps"}};
   for (auto& x : names)
     if (!(*x.s = PyUnicode_InternFromString(x.n))) return nullptr;
   PyObject* m = PyModule_Create(&module);
