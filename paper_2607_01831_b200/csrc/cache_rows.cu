@@ -250,6 +250,9 @@ __global__ void __launch_bounds__(kThreads, 6) cache_read_kernel(const __grid_co
   }
 }
 
+// ------------------------------------------------------------------ host side
+inline bool aligned(const void* p, uintptr_t n) { return aligned_to(p, n); }
+
 }  // namespace
 }  // namespace lynx
 

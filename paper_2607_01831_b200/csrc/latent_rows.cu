@@ -216,8 +216,8 @@ extern "C" lynx_status lynx_latent_append(const lynx_shape* shape, const void* l
   if (n_tokens == 0 || n_src == 0) return LYNX_OK;   // (no token's source row is inside [0, 0))
   if (!latents || !rope_keys || !slots || !C.anchor || !C.residual || !C.meta || !rope_pages) return LYNX_ERR_NULL;
   if (!stride_ok(latent_stride, 1, kLatent) || !stride_ok(rope_stride, 1, kRope)) return LYNX_ERR_SHAPE;
-  if (!aligned16(latents) || !aligned16(rope_keys) || !aligned(slots, 8) || !aligned(rows, 4) || !aligned16(C.anchor) || !aligned16(C.residual) ||
-      !aligned(C.meta, 8) || !aligned16(rope_pages))
+  if (!aligned16(latents) || !aligned16(rope_keys) || !aligned_to(slots, 8) || !aligned_to(rows, 4) || !aligned16(C.anchor) || !aligned16(C.residual) ||
+      !aligned_to(C.meta, 8) || !aligned16(rope_pages))
     return LYNX_ERR_ALIGN;
   RotaryParams r = {};
   if (spec) {
@@ -256,8 +256,8 @@ extern "C" lynx_status lynx_latent_read(const lynx_shape* shape, lynx_plane C, c
   if (shape->max_blocks_per_seq <= 0) return LYNX_ERR_SHAPE;
   if (n_rows == 0) return LYNX_OK;
   if (!C.anchor || !C.meta || !rope_pages || !block_table || !offsets || !latents_out || !rope_out) return LYNX_ERR_NULL;
-  if (!aligned16(C.anchor) || !aligned16(C.residual) || !aligned(C.meta, 8) || !aligned16(rope_pages) || !aligned(block_table, 4) || !aligned(starts, 4) ||
-      !aligned(offsets, 4) || !aligned16(latents_out) || !aligned16(rope_out))
+  if (!aligned16(C.anchor) || !aligned16(C.residual) || !aligned_to(C.meta, 8) || !aligned16(rope_pages) || !aligned_to(block_table, 4) || !aligned_to(starts, 4) ||
+      !aligned_to(offsets, 4) || !aligned16(latents_out) || !aligned16(rope_out))
     return LYNX_ERR_ALIGN;
   LatentReadParams p;
   p.anchor = reinterpret_cast<const uint2*>(C.anchor); p.residual = reinterpret_cast<const uint2*>(C.residual);
@@ -265,7 +265,7 @@ extern "C" lynx_status lynx_latent_read(const lynx_shape* shape, lynx_plane C, c
   p.out = static_cast<uint4*>(latents_out); p.key_out = static_cast<uint4*>(rope_out);
   p.table = block_table; p.starts = starts; p.offsets = offsets;
   p.n_rows = n_rows; p.batch = batch; p.bt = shape->block_tokens; p.num_blocks = shape->num_blocks; p.max_blocks = shape->max_blocks_per_seq;
-  p.wide = aligned(latents_out, 32) ? 1 : 0;
+  p.wide = aligned_to(latents_out, 32) ? 1 : 0;
   p.bt_div = p.bt > 1 ? block_div(p.bt) : BlockDiv{0, 0};
   unsigned grid;
   if (!grid_of(spread(n_rows) ? n_rows : (n_rows + 3) / 4, &grid)) return LYNX_ERR_UNSUPPORTED;

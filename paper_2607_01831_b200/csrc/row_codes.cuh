@@ -241,13 +241,13 @@ __device__ __forceinline__ int sequence_of(const int32_t* offsets, int batch, in
 }
 
 // ------------------------------------------------------------------ host side
-inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+inline bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 lynx_status rotary_params(const lynx_rotary_spec* s, int64_t n_tokens, RotaryParams* r) {
   if (s->n_axes < 1 || s->n_axes > 8 || s->n_positions < 1 || s->n_pairs < 1 || s->positions_stride < n_tokens) return LYNX_ERR_SHAPE;
   if (s->n_pairs > 64 || s->n_pairs % 8 != 0) return LYNX_ERR_UNSUPPORTED;
   if (!s->positions || !s->cos_sin) return LYNX_ERR_NULL;
-  if (!aligned(s->positions, 4) || !aligned16(s->cos_sin)) return LYNX_ERR_ALIGN;
+  if (!aligned_to(s->positions, 4) || !aligned16(s->cos_sin)) return LYNX_ERR_ALIGN;
   r->positions = s->positions;
   r->cos_sin = s->cos_sin;
   r->stride = s->positions_stride;
