@@ -434,6 +434,31 @@ lynx_status lynx_latent_read(const lynx_shape* shape, lynx_plane C, const void* 
                              int32_t batch, const int32_t* starts, const int32_t* offsets, int64_t n_rows, void* latents_out,
                              void* rope_out, void* stream);
 
+/* Attention over a cache of latents, absorbed form: all heads of the queries, multiplied by their keys' projections beforehand, read the same latents,
+ *   score = softmax_scale * (q_latent . latent_t + q_rope . rope_key_t),   out = sum_t softmax(score)_t latent_t,
+ * whose rows the caller multiplies by the values' projections.  For row r = (b n_q + j) Hq + h, q_latent : BF16 [rows][512] with q_stride elements from a
+ * row to the next, q_rope : BF16 [rows][64] with q_rope_stride (multiples of 8, at least 512 and 64: views of one [rows][576] can be given), rotated.  n_q <= 64
+ * positions, Hq <= 128 heads, num_kv_heads 4 (see above), block_tokens a multiple of 16.  Position j of sequence b attends tokens [0, seq_lens[b]) (causal == 0) or
+ * [0, seq_lens[b] - n_q + j + 1); one that sees no token gives zeros and a log-sum-exp of -inf.  softmax_scale 0 means 1/sqrt(192), of heads with 128 + 64
+ * channels before they are absorbed.  C with its residual: the full codes; residual NULL: the Anchor's state.
+ * out : [batch][n_q][Hq][512], BF16, or float where out_float is set; lse : float [batch][n_q][Hq] (natural log) or NULL.  Pointers 16-byte aligned (meta 8;
+ * block_table, seq_lens, lens 4); planes and pages aligned to 32 are read faster.
+ * An infinity or a NaN in a query spoils that row alone, one in the scalars or the rotary key of a token the rows that see it (all of a sequence's may be NaN); what
+ * lies behind a sequence's end, in blocks or in the table, is not looked at.
+ * Precision: scores, statistics and sums are FP32; a code's value zero + scale c enters both products as FP16 (2^-12 of it; relative to the token's largest, so that
+ * any finite scale is handled; channels below 2^-29 of it lose bits), rotary keys and their queries as they are, queries as FP16 relative to their row's largest
+ * (exact down to 2^-32 of it), weights as FP16 (2^-12 of one; below 2^-18 of a row's largest they lose bits, below 2^-28 they are left out of the sum's numerator).
+ * Up to 64 rows n_q * Hq of a sequence take one pass over its planes.
+ * workspace : lynx_latent_workspace_bytes(shape, batch, n_q) bytes (0: unsupported shape), zero-filled once before its first use (lynx_workspace_init); it serves
+ * smaller batches and fewer positions of the same shape, too.  Calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of
+ * range are clamped and recorded there.  seq_lens[b] is clamped to the table's capacity. */
+size_t lynx_latent_workspace_bytes(const lynx_shape* shape, int32_t batch, int32_t n_q);
+lynx_status lynx_latent_attention(const lynx_shape* shape, const void* q_latent, int64_t q_stride, const void* q_rope,
+                                  int64_t q_rope_stride, int32_t batch, int32_t n_q, int32_t causal, lynx_plane C,
+                                  const void* rope_pages, const int32_t* block_table, const int32_t* seq_lens,
+                                  float softmax_scale, int32_t out_float, void* out, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream`, reads and clears the workspace's status word.  Test / debug use. */
 lynx_status lynx_check(void* workspace, void* stream);
 

@@ -55,6 +55,7 @@ EXPORTS = ["lynx_split_quantize", "lynx_recombine", "lynx_workspace_bytes", "lyn
            "lynx_token_verify", "lynx_workspace_lse", "lynx_bf16_workspace_lse", "lynx_lse_merge", "lynx_verify_decision", "lynx_split_quantize_bits", "lynx_recombine_bits",
            "lynx_rotary", "lynx_cache_append", "lynx_cache_read", "lynx_tree_workspace_bytes", "lynx_tree_attention",
            "lynx_norm_rotary", "lynx_norm_cache_append", "lynx_plan_blocks", "lynx_latent_append", "lynx_latent_read",
+           "lynx_latent_workspace_bytes", "lynx_latent_attention",
            "lynx_check",
            "lynx_status_string", "lynx_version"]
 
@@ -139,6 +140,11 @@ def load():
     lib.lynx_latent_append.restype = ctypes.c_int
     lib.lynx_latent_read.argtypes = [ctypes.POINTER(_Shape), _Plane, vp, vp, i32, vp, vp, i64, vp, vp, vp]
     lib.lynx_latent_read.restype = ctypes.c_int
+    lib.lynx_latent_workspace_bytes.argtypes = [ctypes.POINTER(_Shape), i32, i32]
+    lib.lynx_latent_workspace_bytes.restype = ctypes.c_size_t
+    lib.lynx_latent_attention.argtypes = [ctypes.POINTER(_Shape), vp, i64, vp, i64, i32, i32, i32, _Plane, vp, vp, vp, f32, i32, vp, vp, vp,
+                                          ctypes.c_size_t, vp]
+    lib.lynx_latent_attention.restype = ctypes.c_int
     lib.lynx_check.argtypes = [vp, vp]
     lib.lynx_check.restype = ctypes.c_int
     lib.lynx_status_string.argtypes = [ctypes.c_int]
@@ -225,6 +231,7 @@ _fast_rotary, _fast_cache_append = _fast("_fast_rotary", "rotary"), _fast("_fast
 _fast_cache_read, _fast_tree_attention = _fast("_fast_cache_read", "cache_read"), _fast("_fast_tree_attention", "tree_attention")
 _fast_norm_rotary, _fast_norm_append = _fast("_fast_norm_rotary", "norm_rotary"), _fast("_fast_norm_append", "norm_cache_append")
 _fast_plan_blocks = _fast("_fast_plan_blocks", "plan_blocks")
+_fast_latent_attention = _fast("_fast_latent_attention", "latent_attention")
 _fast_latent_append, _fast_latent_read = _fast("_fast_latent_append", "latent_append"), _fast("_fast_latent_read", "latent_read")
 _fast_hier_quantize, _fast_hier_dequantize = _fast("_fast_hier_quantize", "hier_quantize"), _fast("_fast_hier_dequantize", "hier_dequantize")
 
@@ -889,6 +896,74 @@ def latent_read(geo: Geometry, C: Planes, rope_pages: torch.Tensor, block_table:
     _ok(load().lynx_latent_read(ctypes.byref(geo._c()), plane, _ptr(rope_pages), _ptr(block_table), B, _ptr(starts), _ptr(offsets), n_rows,
                                 _ptr(out), _ptr(keys), _stream()), "lynx_latent_read")
     return out, keys
+
+
+def latent_workspace_bytes(geo: Geometry, batch: int, n_q: int) -> int:
+    return int(load().lynx_latent_workspace_bytes(ctypes.byref(geo._c()), batch, n_q))
+
+
+def make_latent_workspace(geo: Geometry, batch: int, n_q: int, device) -> torch.Tensor:
+    """Allocate a workspace for latent_attention calls of up to (batch, n_q) and zero it."""
+    n = latent_workspace_bytes(geo, batch, n_q)
+    if n == 0:
+        raise LynxError("unsupported latent attention shape")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    _ok(load().lynx_workspace_init(_ptr(ws), n, _stream()), "lynx_workspace_init")
+    return ws
+
+
+def _query_rows(t: torch.Tensor, shape: tuple, what: str):
+    """Pointer and row stride of BF16 [B][n][Hq][width] whose rows may lie apart, evenly."""
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != shape:
+        raise LynxError(f"{what} must be BF16 [B][n_q][Hq][{shape[-1]}]")
+    if not t.is_cuda:
+        raise LynxError("device tensors required")
+    apart, rows = None, 1
+    for d in (2, 1, 0):
+        if t.shape[d] > 1:      # (of dimensions with one entry the stride means nothing)
+            if apart is None:
+                apart = t.stride(d)
+            elif t.stride(d) != apart * rows:
+                raise LynxError(f"{what}: rows must lie evenly apart")
+            rows *= t.shape[d]
+    if t.stride(3) != 1:
+        raise LynxError(f"{what}: the channels of a row must lie one behind the other")
+    return t.data_ptr(), shape[-1] if apart is None else apart
+
+
+def latent_attention(geo: Geometry, q_latent: torch.Tensor, q_rope: torch.Tensor, C: Planes, rope_pages: torch.Tensor, block_table: torch.Tensor,
+                     seq_lens: torch.Tensor, workspace: torch.Tensor, causal: bool = True, anchor_only: bool = False, softmax_scale: float = 0.0,
+                     out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
+    """lynx_latent_attention: q_latent BF16 [B][n][Hq][512] and q_rope BF16 [B][n][Hq][64] (rows may lie apart, evenly: views of one [..][576]) over
+    the latents of a geometry with num_kv_heads = 4 -> BF16 [B][n][Hq][512], or what `out` (BF16 or float32) is; lse: float32 [B][n][Hq] to be filled.
+    anchor_only: the Anchor's state of the planes.  softmax_scale 0: 1 / sqrt(192)."""
+    r = _fast_latent_attention(geo, q_latent, q_rope, C, rope_pages, block_table, seq_lens, workspace, causal, anchor_only, softmax_scale, out, lse)
+    if r is not None:
+        return _result(r, "lynx_latent_attention")
+    if q_latent.dim() != 4 or q_latent.dtype != torch.bfloat16 or q_latent.shape[2:] != (geo.num_q_heads, LATENT):
+        raise LynxError("q_latent must be BF16 [B][n_q][Hq][512]")
+    B, n, Hq, _ = q_latent.shape
+    if block_table.dtype != torch.int32 or tuple(block_table.shape) != (B, geo.max_blocks_per_seq) or seq_lens.dtype != torch.int32 or \
+            tuple(seq_lens.shape) != (B,):
+        raise LynxError("block_table must be int32 [B][max_blocks_per_seq], seq_lens int32 [B]")
+    if out is None:
+        out = torch.empty(q_latent.shape, dtype=torch.bfloat16, device=q_latent.device)
+    elif out.shape != q_latent.shape or out.dtype not in (torch.bfloat16, torch.float32):
+        raise LynxError("out must be BF16 or float32 [B][n_q][Hq][512]")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, n, Hq)):
+        raise LynxError("lse must be float32 [B][n_q][Hq]")
+    if not anchor_only and C.residual is None:
+        raise LynxError("the Residual plane is needed unless anchor_only")
+    _latent_fit(geo, C, rope_pages)
+    if B == 0:
+        return out
+    (qp, qs), (rp, rs) = _query_rows(q_latent, (B, n, Hq, LATENT), "q_latent"), _query_rows(q_rope, (B, n, Hq, ROPE), "q_rope")
+    _here(q_latent, q_rope, C, rope_pages, block_table, seq_lens, workspace, out, lse)
+    plane = _Plane(_ptr(C.anchor), None if anchor_only else _ptr(C.residual), _ptr(C.meta))
+    _ok(load().lynx_latent_attention(ctypes.byref(geo._c()), qp, qs, rp, rs, B, n, int(causal), plane, _ptr(rope_pages), _ptr(block_table),
+                                     _ptr(seq_lens), softmax_scale, int(out.dtype == torch.float32), _ptr(out), _ptr(lse), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size(), _stream()), "lynx_latent_attention")
+    return out
 
 
 def tree_workspace_bytes(geo: Geometry, batch: int, n_nodes: int) -> int:

@@ -14,7 +14,7 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "liblynx.so")
 NATIVE = os.path.join(_HERE, "_native.so")
 SOURCES = ["api.cu", "split_quantize.cu", "attention.cu", "bf16_attention.cu", "hier_quantize.cu", "token_verify.cu", "lse_merge.cu", "bit_split.cu", "cache_rows.cu", "tree_attention.cu",
-           "head_norm.cu", "block_plan.cu", "latent_rows.cu"]
+           "head_norm.cu", "block_plan.cu", "latent_rows.cu", "latent_attention.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

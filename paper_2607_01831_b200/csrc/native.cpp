@@ -726,11 +726,59 @@ PyObject* latent_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// BF16 [batch][n][heads][width], rows evenly apart
+const at::Tensor* query_rows(PyObject* o, int64_t width, int64_t* stride) {
+  if (!THPVariable_CheckExact(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.defined() || !t.is_cuda() || at::isTensorSubclassLike(t) || t.scalar_type() != at::kBFloat16 || t.dim() != 4 || t.size(3) != width || t.numel() == 0 ||
+      t.stride(3) != 1)
+    return nullptr;
+  int64_t apart = -1, rows = 1;   // (of dimensions with one entry the stride means nothing)
+  for (int d = 2; d >= 0; --d) {
+    if (t.size(d) > 1) {
+      if (apart < 0) apart = t.stride(d);
+      else if (t.stride(d) != apart * rows) return nullptr;
+      rows *= t.size(d);
+    }
+  }
+  *stride = apart < 0 ? width : apart;
+  return &t;
+}
+
+// geo, q_latent, q_rope, planes, pages, block_table, seq_lens, workspace, causal, anchor_only, softmax_scale, out or None, lse or None -> out
+PyObject* latent_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    lynx_shape s;
+    lynx_plane C;
+    float scale;
+    if (n != 13 || !shape_of(a[0], &s) || !PyBool_Check(a[8]) || !PyBool_Check(a[9]) || !float_of(a[10], &scale)) Py_RETURN_NONE;
+    int64_t sq = 0, sr = 0;
+    const at::Tensor *q = query_rows(a[1], kLatent, &sq), *qr = query_rows(a[2], kRope, &sr), *pages = rope_pages(a[4], s), *table = typed(a[5], at::kInt),
+                     *lens = typed(a[6], at::kInt), *ws = plain(a[7]), *given = plain(a[11]), *lse = typed(a[12], at::kFloat);
+    if (!q || !qr || !pages || !table || !lens || !ws || (!given && !is_none(a[11])) || (!lse && !is_none(a[12]))) Py_RETURN_NONE;
+    const int64_t B = q->size(0), N = q->size(1);
+    if (q->size(2) != s.num_q_heads || qr->size(0) != B || qr->size(1) != N || qr->size(2) != s.num_q_heads || B > INT32_MAX || N > INT32_MAX || table->dim() != 2 ||
+        table->size(0) != B || table->size(1) != s.max_blocks_per_seq || lens->dim() != 1 || lens->numel() != B || !planes_fit(a[3], s, a[9] == Py_False, &C, true) ||
+        (given && (given->sizes() != q->sizes() || (given->scalar_type() != at::kBFloat16 && given->scalar_type() != at::kFloat))) ||
+        (lse && (lse->dim() != 3 || lse->size(0) != B || lse->size(1) != N || lse->size(2) != s.num_q_heads)) || !here({q, qr, pages, table, lens, ws, given, lse}))
+      Py_RETURN_NONE;
+    at::Tensor out = given ? *given : empty_like_device(q->sizes(), at::kBFloat16, *q);
+    void* st = stream();
+    const lynx_status rc = unlocked([&] {
+      return lynx_latent_attention(&s, q->data_ptr(), sq, qr->data_ptr(), sr, (int32_t)B, (int32_t)N, a[8] == Py_True, C, pages->data_ptr(),
+                                   (const int32_t*)table->data_ptr(), (const int32_t*)lens->data_ptr(), scale, out.scalar_type() == at::kFloat, out.data_ptr(),
+                                   (float*)ptr(lse), ws->data_ptr(), (size_t)ws->nbytes(), st);
+    });
+    if (rc != LYNX_OK) return status(rc);
+    return given ? Py_NewRef(a[11]) : THPVariable_Wrap(out);
+  });
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(anchor_attention), FAST(merge_verify_attention), FAST(bf16_attention), FAST(split_quantize), FAST(recombine),
                          FAST(lse_view), FAST(lse_merge), FAST(hier_quantize), FAST(hier_dequantize),
                          FAST(rotary), FAST(cache_append), FAST(cache_read), FAST(tree_attention),
-                         FAST(norm_rotary), FAST(norm_cache_append), FAST(plan_blocks), FAST(latent_append), FAST(latent_read), {nullptr, nullptr, 0, nullptr}};
+                         FAST(norm_rotary), FAST(norm_cache_append), FAST(plan_blocks), FAST(latent_append), FAST(latent_read), FAST(latent_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

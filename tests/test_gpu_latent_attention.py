@@ -1,0 +1,249 @@
+"""Attention over quantised latents against 64 bits, on the planes' exact values.
+
+Bounds, with half steps u16 = 2^-12 (FP16, 11 bits: 2^-11 / 2 of a value on either side is 2^-12 of its binade's top, 2^-11 at most of the value itself) -- taken
+as u = 2^-11 throughout -- and u32 = 2^-24.
+Scores: each key channel off by u of itself at most, q exact: |ds| <= u a sum_d |q_d v_d| (latent channels alone), plus FP32 accumulation of 576 terms, truncating:
+2^-23 * 576 < 2^-13 of a sum |q k| over all channels, and the few FP32 operations behind it.  With D = a (u + 2^-13) sum_d |q_d k_d|, the largest over the tokens
+that a row sees, a weight is off by a factor e^+-D, and weight over sum by 2 D (1 + D) at most.
+Weights: u of themselves in the numerator; values: u of themselves.  Sums of the second product: 2^-13 of sum p |v| (as above, per 128 tokens, and FP32 adding from tile to tile:
+tokens / 128 * 2^-24).  So |out - want| <= (2 D + D^2 2 + 2 u + 2^-12 + tokens 2^-31) sum p |v|, and half a step of the output's type.  Weights below FP16's range:
+2^-28 of the row's largest 2^e p, tokens * 2^-28 * 2^15 relative to the accumulator's ... covered by tokens * 2^-26 max |v|.
+Log-sum-exps: D, and 2^-20 of 1 + |lse|."""
+import pytest
+import torch
+
+import paper_2607_01831_b200 as lynx
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -11
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+class Cache:
+    """A pool of quantised latents and rotary keys in shuffled blocks; what no sequence holds is no number."""
+
+    def __init__(self, lens, bt, Hq, seed=0, spread=1.0, channels=True, wide=0, junk=True):
+        g = _gen(seed)
+        self.lens, self.bt, B = list(lens), bt, len(lens)
+        need = [-(-n // bt) for n in lens]
+        self.nb = sum(need) + 3
+        self.table = torch.full((B, max(1, max(need)) + wide), -9 if junk else 0, dtype=torch.int32)
+        ids = torch.randperm(self.nb, generator=g).to(torch.int32)
+        for b, n in enumerate(need):
+            self.table[b, :n] = ids[sum(need[:b]):sum(need[:b]) + n]
+        x = torch.randn(self.nb, 4, bt, 128, generator=g) * spread
+        if channels:
+            x *= torch.exp(0.7 * torch.randn(4, 1, 128, generator=g))
+        self.planes = lynx.split_quantize(x.to(torch.bfloat16).cuda())
+        self.pages = torch.randn(self.nb, bt, 64, generator=g).to(torch.bfloat16).cuda()
+        if junk:       # rows behind a sequence's end, and blocks of none
+            dead = torch.ones(self.nb * bt, dtype=torch.bool)
+            for b, n in enumerate(lens):
+                t = torch.arange(n)
+                dead[self.table[b, t // bt].long() * bt + t % bt] = False
+            dead = dead.view(self.nb, bt).cuda()
+            self.planes.meta[dead[:, None].expand(self.nb, 4, bt)] = float("nan")
+            self.pages[dead] = float("nan")
+        self.geo = lynx.Geometry(Hq, 4, bt, self.nb, self.table.shape[1])
+        self.d_table, self.d_lens = self.table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+
+    def rows(self, b, anchor):
+        """float64 latents [tokens][512] and rotary keys [tokens][64] of sequence b, on the GPU."""
+        t = torch.arange(self.lens[b])
+        blk, off = self.table[b, t // self.bt].long().cuda(), (t % self.bt).cuda()
+        code = lynx.recombine(self.planes)[0][blk, :, off].double()
+        if anchor:
+            code = torch.floor(code / 16) * 16 + 8
+        meta = self.planes.meta[blk, :, off].double()
+        return (meta[..., 1:] + meta[..., :1] * code).flatten(1), self.pages[blk, off].double()
+
+
+def _queries(B, n, H, seed, spread=1.0):
+    g = _gen(seed)
+    q = (torch.randn(B, n, H, 576, generator=g) * spread).to(torch.bfloat16).cuda()
+    return q[..., :512], q[..., 512:]
+
+
+def _check(cache, q, qr, out, lse, causal, anchor, scale=0.0, skip=()):
+    B, n, H, _ = q.shape
+    a = scale or 192 ** -0.5
+    step = 2.0 ** -8 if out.dtype == torch.bfloat16 else 2.0 ** -24
+    for b, L in enumerate(cache.lens):
+        if b in skip:
+            continue
+        latents, keys = cache.rows(b, anchor)
+        for j in range(n):
+            count = max(0, L - n + j + 1) if causal else L
+            got, gl = out[b, j].double(), None if lse is None else lse[b, j].double()
+            if count == 0:
+                assert (got == 0).all() and (gl is None or (gl == -float("inf")).all())
+                continue
+            v, x, y = latents[:count], q[b, j].double(), qr[b, j].double()
+            s = a * (x @ v.T + y @ keys[:count].T)
+            w = s.softmax(1)
+            want, size = w @ v, w @ v.abs()
+            D = a * ((U + 2.0 ** -13) * (x.abs() @ v.abs().T) + 2.0 ** -13 * (y.abs() @ keys[:count].abs().T)).amax(1, keepdim=True)
+            bound = (2 * D + 2 * D * D + 2 * U + 2.0 ** -12 + count * 2.0 ** -31) * size + count * 2.0 ** -26 * v.abs().max() + step * want.abs()
+            assert ((got - want).abs() <= bound).all(), (b, j, float(((got - want).abs() / bound).max()))
+            if gl is not None:
+                l = s.logsumexp(1)
+                assert ((gl - l).abs() <= D[:, 0] + 2.0 ** -20 * (1 + l.abs())).all()
+
+
+def _run(cache, q, qr, causal=True, anchor=False, out=None, ws=None, scale=0.0):
+    B, n, H, _ = q.shape
+    ws = lynx.make_latent_workspace(cache.geo, B, n, "cuda") if ws is None else ws
+    lse = torch.full((B, n, H), 7.0, device="cuda")
+    out = lynx.latent_attention(cache.geo, q, qr, cache.planes, cache.pages, cache.d_table, cache.d_lens, ws, causal=causal, anchor_only=anchor, lse=lse, out=out,
+                                softmax_scale=scale)
+    lynx.check(ws)
+    return out, lse
+
+
+LENS = [(1,), (16,), (300,), (128, 129, 0, 127), (1000, 3, 2500), (40, 700, 1, 0, 260, 130, 128, 5, 900)]
+
+
+@pytest.mark.parametrize("lens", LENS)
+@pytest.mark.parametrize("n,H", [(1, 1), (1, 16), (1, 20), (1, 64), (1, 128), (3, 16), (5, 40), (64, 2)])
+@pytest.mark.parametrize("anchor", [False, True])
+def test_lengths_rows_and_planes(lens, n, H, anchor):
+    cache = Cache(lens, 16 if n < 5 else 32, H, seed=sum(lens) + H, wide=n)
+    q, qr = _queries(len(lens), n, H, seed=n + H)
+    for causal in (True, False):
+        out, lse = _run(cache, q, qr, causal, anchor)
+        assert out.dtype == torch.bfloat16
+        _check(cache, q, qr, out, lse, causal, anchor)
+
+
+@pytest.mark.parametrize("lens,n,H", [((20000,), 1, 16), ((9000, 20011, 333), 4, 32), ((7000,) * 5, 1, 128), ((131072,), 1, 64)])
+def test_long_contexts_in_many_parts(lens, n, H):
+    cache = Cache(lens, 64, H, seed=9, junk=False)
+    q, qr = _queries(len(lens), n, H, seed=2)
+    out, lse = _run(cache, q, qr, True, False, out=torch.empty(q.shape, device="cuda"))
+    _check(cache, q, qr, out, lse, True, False)
+    again, _ = _run(cache, q, qr, True, False, out=torch.empty(q.shape, device="cuda"))
+    assert torch.equal(out, again)
+
+
+def test_many_sequences():
+    lens = [i * 37 % 611 for i in range(200)]
+    cache = Cache(lens, 16, 16, seed=5)
+    q, qr = _queries(200, 1, 16, seed=3)
+    out, lse = _run(cache, q, qr)
+    _check(cache, q, qr, out, lse, True, False)
+
+
+@pytest.mark.parametrize("spread,qs", [(1e-20, 1.0), (1e-3, 100.0), (300.0, 0.01), (1e15, 1e-15), (1.0, 8.0), (1.0, 1e-30)])
+@pytest.mark.parametrize("H", [16, 64])
+def test_scales_of_any_size(spread, qs, H):
+    cache = Cache((700, 33), 16, H, seed=4, spread=spread)
+    q, qr = _queries(2, 1, H, seed=5, spread=qs)
+    if qs > 1:
+        qr = (qr.float() / qs).to(torch.bfloat16)
+    out, lse = _run(cache, q, qr, out=torch.empty(q.shape, device="cuda"))
+    _check(cache, q, qr, out, lse, True, False)
+
+
+@pytest.mark.parametrize("at", [0, 100, 1500, 4000])
+@pytest.mark.parametrize("H", [16, 40])
+def test_a_dominating_token_raises_the_references(at, H):
+    """Scores that grow along the context, and one token far above the rest: early, in the middle, at the end."""
+    cache = Cache((4001,), 16, H, seed=6)
+    q, qr = _queries(1, 2, H, seed=7)
+    t = torch.arange(4001)
+    blk, off = cache.table[0, t // 16].long().cuda(), (t % 16).cuda()
+    ramp = torch.linspace(0, 3, 4001).to(torch.bfloat16).cuda()
+    cache.pages[blk, off, 0] = ramp
+    qr[..., 0] = 60.0 * (1 + torch.arange(H, device="cuda") % 3)
+    cache.pages[blk[at], off[at], 1] = 30.0
+    qr[..., 1] = 12.0
+    out, lse = _run(cache, q, qr, out=torch.empty(q.shape, device="cuda"))
+    _check(cache, q, qr, out, lse, True, False)
+
+
+def test_tokens_of_very_different_sizes():
+    """A token of tiny values that takes most of the weight, tokens of zeros, tokens with outliers."""
+    cache = Cache((2000,), 16, 16, seed=8, channels=False)
+    t = torch.arange(2000)
+    blk, off = cache.table[0, t // 16].long().cuda(), (t % 16).cuda()
+    cache.planes.meta[blk[5], :, off[5]] *= 2.0 ** -30
+    cache.planes.meta[blk[300], :, off[300]] = 0.0
+    cache.planes.meta[blk[777], 1, off[777]] *= 2.0 ** 7
+    q, qr = _queries(1, 1, 16, seed=9)
+    cache.pages[blk[5], off[5]] = 8.0
+    qr.abs_()
+    out, lse = _run(cache, q, qr, out=torch.empty(q.shape, device="cuda"))
+    _check(cache, q, qr, out, lse, True, False)
+
+
+def test_what_is_no_number_spoils_no_other_row():
+    cache = Cache((500, 260, 90), 16, 20, seed=10)
+    q, qr = _queries(3, 2, 20, seed=11)
+    clean, _ = _run(cache, q, qr)
+    q, qr = q.clone(), qr.clone()
+    bad = torch.zeros(3, 2, 20, dtype=torch.bool)
+    for (b, j, h), x, t in (((0, 0, 3), float("nan"), q), ((0, 1, 19), float("inf"), q), ((1, 1, 0), float("nan"), qr), ((2, 0, 7), -float("inf"), qr)):
+        t[b, j, h, 9] = x
+        bad[b, j, h] = True
+    out, lse = _run(cache, q, qr)
+    assert torch.equal(out[~bad.cuda()], clean[~bad.cuda()]) and lse[~bad.cuda()].isfinite().all()
+    # one in a token: the sequence's rows, the others' stay
+    cache.planes.meta[cache.table[1, 3], 2, 4] = float("nan")
+    out, _ = _run(cache, q, qr)
+    keep = ~bad
+    keep[1] = False
+    assert torch.equal(out[keep.cuda()], clean[keep.cuda()]) and out[1].isnan().any()
+
+
+def test_strides_scale_workspaces_and_streams(monkeypatch):
+    cache = Cache((333, 40), 16, 16, seed=12)
+    q, qr = _queries(2, 3, 16, seed=13)
+    ws = lynx.make_latent_workspace(cache.geo, 2, 8, "cuda")        # a larger call's serves
+    out, lse = _run(cache, q, qr, ws=ws, scale=0.25)
+    _check(cache, q, qr, out, lse, True, False, scale=0.25)
+    assert torch.equal(_run(cache, q.contiguous(), qr.contiguous(), ws=ws, scale=0.25)[0], out)
+    # 16 bytes of alignment are enough
+    shift = lambda t: torch.cat((torch.zeros(16 // t.element_size(), dtype=t.dtype, device="cuda"), t.flatten()))[16 // t.element_size():].view(t.shape)
+    p = cache.planes
+    moved = lynx.Planes(shift(p.anchor), shift(p.residual), shift(p.meta))
+    assert moved.anchor.data_ptr() % 32 == 16
+    assert torch.equal(lynx.latent_attention(cache.geo, q, qr, moved, shift(cache.pages), cache.d_table, cache.d_lens, ws, softmax_scale=0.25), out)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        side = lynx.latent_attention(cache.geo, q, qr, p, cache.pages, cache.d_table, cache.d_lens, ws, softmax_scale=0.25)
+    st.synchronize()
+    assert torch.equal(side, out)
+    monkeypatch.setattr(lynx, "_fast_latent_attention", lynx._python_only)
+    assert torch.equal(lynx.latent_attention(cache.geo, q, qr, p, cache.pages, cache.d_table, cache.d_lens, ws, softmax_scale=0.25), out)
+
+
+def test_bad_block_ids_are_reported():
+    cache = Cache((300,), 16, 16, seed=14, junk=False)
+    q, qr = _queries(1, 1, 16, seed=15)
+    ws = lynx.make_latent_workspace(cache.geo, 1, 1, "cuda")
+    cache.d_table[0, 5] = cache.nb + 100
+    cache.d_table[0, 7] = -3
+    lynx.latent_attention(cache.geo, q, qr, cache.planes, cache.pages, cache.d_table, cache.d_lens, ws)
+    with pytest.raises(lynx.LynxError, match="block id"):
+        lynx.check(ws)
+    lynx.check(ws)
+
+
+def test_captured_and_replayed():
+    cache = Cache((600, 200), 16, 16, seed=16, wide=4)
+    q, qr = _queries(2, 1, 16, seed=17)
+    ws = lynx.make_latent_workspace(cache.geo, 2, 1, "cuda")
+    _run(cache, q, qr, ws=ws)
+    graph, out = torch.cuda.CUDAGraph(), torch.empty(2, 1, 16, 512, device="cuda")
+    with torch.cuda.graph(graph):
+        lynx.latent_attention(cache.geo, q, qr, cache.planes, cache.pages, cache.d_table, cache.d_lens, ws, out=out)
+    for lens in ((600, 200), (17, 130), (1, 0)):
+        cache.lens = list(lens)
+        cache.d_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(cache, q, qr, out, None, True, False)
