@@ -10,15 +10,19 @@
 // own.  Weights are FP16 relative to a reference per row, set from its first tile and raised (rare) before one would leave FP16; references, sums and
 // accumulators are FP32.
 //
-// Layout: tokens (scores) and channels (outputs) are the M = 128 lanes of tensor memory, up to 64 rows the N: O^T takes 4 x 64 columns of the 512, scores 2 x 64, two places for
-// 128 channels of a tile's keys the rest.  (Rows as lanes would need all 512 columns for O alone.)  More rows are more row tiles, each a pass over the planes.
+// Layout: tokens (scores) and channels (outputs) are the M = 128 lanes of tensor memory, up to 64 rows the N: O^T takes 4 x 64 columns of the 512, scores
+// 64, three places for 128 channels of a tile's keys the rest.  (Rows as lanes would need all 512 columns for O alone.)
+// More rows are more row tiles, each a pass over the planes.
 // One CTA per SM, a tile 128 tokens; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
 //   warps 0-3, 4-7   softmax, half of the rows each, whole tiles
-//   warps 8-15       codes to FP16: a thread has a token, 64 channels of each of its rows, loaded a tile ahead into registers; a piece's queries
-//   warp 16          issues every tcgen05.mma
-//   warp 17          deals out the pieces
-// The tile's values have one place (128 KB).  A row's 128 channels of it are given up by their part of P C, so that P C of tile i, the expansion of tile i + 1 and its
-// scores follow one another channel group by channel group.
+//   warps 8-23       codes to FP16, two sets of eight, in turn 128 channels each: a thread has 32 of two tokens, loaded a group ahead into registers; a piece's
+//                    queries
+//   warps 24, 25     issue every tcgen05.mma: scores, weights times values
+//   warp 26          the tokens' powers of two
+//   warp 27          deals out the pieces
+// The tile's values have one place in shared memory (128 KB, beside queries of 72): a group's 128 channels go there, and to tensor memory as keys, when the
+// same channels of the tile before have been multiplied, so that the products of a tile, the expansion of the next one and its scores follow one another
+// group by group.
 // Work is cut in stream-K form: the (sequence, row tile, tile) list into equal ranges, a piece being a range's part of one segment.  A segment within one
 // CTA is written by it; otherwise partial (O, ref, l) go to the workspace and a dependent kernel joins them.
 #include <cuda_bf16.h>
@@ -36,12 +40,14 @@ namespace {
 constexpr int kTile = 128, kGroups = 4, kLatent = 512, kRope = 64;
 constexpr int kMaxRows = 64;                // rows of a row tile
 constexpr int kPartRow = kLatent + 4;       // floats of a partial row: O[512], reference, sum, pad
-constexpr int kThreads = 640;
-constexpr int kRegSoft = 80, kRegCodes = 136, kRegRest = 40;   // per thread; the launch has 96 for each of five warpgroups
-static_assert(2 * kRegSoft + 2 * kRegCodes + kRegRest <= 5 * 96, "registers");
-constexpr int kDoneThreads = 256 + 2 * 32;  // softmax, products, pieces
-// log2 of a row's largest weight when its reference is set; of one that sets it anew (FP16 holds 65504); what sets others anew with it
-constexpr float kTop = 4.0f, kMost = 15.9f, kRaise = 9.0f;
+constexpr int kThreads = 896;
+constexpr int kRegSoft = 72, kRegCodes = 80, kRegRest = 40;   // per thread; the launch has 72 for each of seven warpgroups
+static_assert(2 * kRegSoft + 4 * kRegCodes + kRegRest <= 7 * 72, "registers");
+constexpr int kFac = 3;                     // places for the powers of two of a tile's tokens
+constexpr int kPlaces = 3;                  // for keys, of a rotary part or of 128 channels: five a tile, in turn
+constexpr int kDoneThreads = 256 + 4 * 32;  // softmax, products, powers of two, pieces
+// log2 of a row's largest weight when its reference is set; of what sets it anew when another row's weight has left FP16 (65504)
+constexpr float kTop = 4.0f, kRaise = 9.0f;
 constexpr int kMinExp = -80;                // smallest exponent of a token's values
 
 struct LatentParams {
@@ -60,7 +66,6 @@ struct LatentParams {
   int B, n, Hq, R, RT, bt, num_blocks, max_blocks, causal, out_f32;
   int whole;                                // CTA i takes segment i
   int per_seg;                              // CTAs per segment where all have as many tiles (else 0)
-  int wide;                                 // planes and pages are aligned to 32 bytes
   BlockDiv bt_div;
 };
 
@@ -68,23 +73,34 @@ template <int NR>
 struct Cfg {
   static constexpr int kPRow = 2 * NR, kPLayout = NR == 16 ? 6 : NR == 32 ? 4 : 2;   // bytes of a token's weights; the descriptor's swizzle of such rows
   static constexpr int kOffV = 0, kOffQ = 131072, kOffP = kOffQ + 9 * NR * 128, kOffFac = kOffP + kTile * kPRow;   // values [8 x 64 channels][128 tokens][128 B]
-  static constexpr int kOffRq = kOffFac + 2 * kTile * 8;             // [2][128] {2^e, e}; [2][NR] factors of the rows' scores
-  static constexpr int kOffScale = kOffRq + 2 * NR * 4, kOffSum = kOffScale + NR * 4, kOffMax = kOffSum + 4 * NR * 4;   // [NR], [4][NR], [4][NR]
+  static constexpr int kOffRq = kOffFac + kFac * kTile * 8;          // [kFac][128] {2^e, e}; [2][NR] factors of the rows' scores, tokens they see
+  static constexpr int kOffLim = kOffRq + 2 * NR * 4, kOffScale = kOffLim + 2 * NR * 4, kOffRef = kOffScale + NR * 4, kOffFinal = kOffRef + NR * 4;   // [NR] each
+  static constexpr int kOffSum = kOffFinal + NR * 4, kOffMax = kOffSum + 4 * NR * 4;                                  // [4][NR]
   static constexpr int kOffItems = kOffMax + 4 * NR * 4, kOffMisc = kOffItems + 2 * 32, kOffBars = kOffMisc + 64;
-  static constexpr int kBars = 25;
+  static constexpr int kBars = 2 * kPlaces + 2 * 4 + 2 * kFac + 4 + 7;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
-  static_assert(kSmem <= 227 * 1024 && kOffP % 1024 == 0 && kOffItems % 16 == 0, "shared memory");
-  static constexpr int kTmO = 0, kTmS = 4 * NR, kTmSr = 5 * NR, kTmK = 6 * NR;   // O^T [4][NR], scores of latents and of rotary keys, keys [2][64]
-  static_assert(kTmK + 128 <= 512, "tensor memory");
+  static_assert(kSmem <= 227 * 1024 && kOffP % 1024 == 0 && kOffItems % 16 == 0 && kOffBars % 8 == 0, "shared memory");
+  static constexpr int kTmO = 0, kTmS = 4 * NR, kTmK = 5 * NR;       // O^T [4][NR], scores [NR], keys [kPlaces][64]
+  static_assert(kTmK + kPlaces * 64 <= 512, "tensor memory");
 };
 
 struct Item {  // a piece: tiles u0 .. u0 + n - 1 of segment (b, rt), none: the end
   int b, rt, len, u0, n, first_cta, n_contrib, pad;
 };
 
+// A place among several in turn, and the parity of its round.
+struct Ring {
+  int i = 0;
+  uint32_t ph = 0;
+  __device__ __forceinline__ void next(int places, int by = 1) {   // (by no more than five times as many)
+    for (i += by; i >= places; ph ^= 1) i -= places;
+  }
+};
+
 // ------------------------------------------------------------------ PTX
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
+__device__ __forceinline__ void mbar_arrive2(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 2;" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
   uint32_t ok;
@@ -98,10 +114,19 @@ __device__ __forceinline__ uint64_t globaltimer_ns() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// Gives up after about two seconds, or soon after another thread has; the caller carries on without the data, so that all loops end, and the host is told
-// through the status word.
+// Gives up after 2^17 probes, each of which may park its thread for 20 us, or once another thread has; the caller carries on without the data, so that all
+// loops end, and the host is told through the status word.  (Inlined, and no longer than it must be: there are some twenty.)
 __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* abort_word) {
-  bounded_wait([=] { return mbar_try_wait(bar, parity); }, [] { return globaltimer_ns(); }, abort_word);
+  for (uint32_t i = 0; !mbar_try_wait(bar, parity); ++i)
+    if (i >= (1u << 17) || *abort_word) {
+      *abort_word = 1;
+      break;
+    }
+}
+// The wait for a piece, which may be as far away as the piece before is long: gives up after two seconds (see bounded_wait.cuh).
+struct PieceWait { volatile int* abort_word; };
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, PieceWait w) {
+  bounded_wait([=] { return mbar_try_wait(bar, parity); }, [] { return globaltimer_ns(); }, w.abort_word);
 }
 __device__ __forceinline__ void named_bar(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
@@ -116,6 +141,7 @@ template <int N>
 __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
@@ -129,6 +155,19 @@ __device__ __forceinline__ void ld_16x256(uint32_t a, uint32_t* r) {
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(a) : "memory");
   else
     tc_ld_16x256(a, r);
+}
+// Likewise into tensor memory: 16 and 64 columns.
+__device__ __forceinline__ void st_16x256(uint32_t a, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void st_16x256(uint32_t a, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,"
+      "%31,%32};"
+      ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   uint32_t d;
@@ -162,6 +201,11 @@ __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }   // -126 <= e <= 127
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -184,31 +228,30 @@ __device__ __forceinline__ uint32_t bit_select(uint32_t a, uint32_t b, uint32_t 
   asm("lop3.b32 %0, %1, %2, %3, 0xE4;" : "=r"(d) : "r"(a), "r"(b), "r"(mask));
   return d;
 }
-// Eight channels from a word of Anchor and a word of Residual nibbles, (2^15 + code) s + z in FP32, rounded to FP16.  A code in the second byte of
-// 2^15 is the number 2^15 + code; z has 2^15 s taken off, exact to 2^-9 of a code.
-__device__ __forceinline__ void values8(uint32_t xa, uint32_t xr, uint64_t s, uint64_t z, uint32_t* o) {
+// Eight channels' values from a word of Anchor and a word of Residual nibbles: code - 128 in FP16 (exact), times the scale and plus the middle, one rounding.
+// They come apart in the order 0 4 2 6 1 5 3 7 (its own inverse), which keys, queries and values have.  (In FP32, with one rounding at the end, the
+// arithmetic units take twice as long, and the scores wait for half of it.)
+__device__ __forceinline__ uint32_t value2(uint32_t x, uint32_t scale, uint32_t mid) {   // x: 1024 + code, twice
+  uint32_t d;
+  asm("{\n\t.reg .b32 c;\n\tadd.rn.f16x2 c, %1, %4;\n\tfma.rn.f16x2 %0, c, %2, %3;\n\t}" : "=r"(d) : "r"(x), "r"(scale), "r"(mid), "r"(0xE480E480u));
+  return d;
+}
+__device__ __forceinline__ void values8(uint32_t xa, uint32_t xr, uint32_t scale, uint32_t mid, uint32_t* o) {
   const uint32_t ev = bit_select(xa << 4, xr, 0xF0F0F0F0u), od = bit_select(xa, xr >> 4, 0xF0F0F0F0u);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    float a, b;
-    f2_unpack(f2_fma(u2_pack(__byte_perm(ev, 0x47000000u, 0x7404 | (k << 4)), __byte_perm(od, 0x47000000u, 0x7404 | (k << 4))), s, z), a, b);
-    o[k] = pack_f16x2(a, b);
-  }
+  o[0] = value2((ev & 0x00FF00FFu) | 0x64006400u, scale, mid);
+  o[1] = value2(__byte_perm(ev, 0x64646464u, 0x4341), scale, mid);
+  o[2] = value2((od & 0x00FF00FFu) | 0x64006400u, scale, mid);
+  o[3] = value2(__byte_perm(od, 0x64646464u, 0x4341), scale, mid);
 }
-struct Words8 { uint32_t w[8]; };
-// 32 bytes, in one load where they are aligned to that.
-__device__ __forceinline__ Words8 load32(const void* p, bool wide) {
-  Words8 v;
-  if (wide) {
-    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7]) : "l"(p));
-  } else {
-    const uint4 a = ld_dep(static_cast<const uint4*>(p)), b = ld_dep(static_cast<const uint4*>(p) + 1);
-    v.w[0] = a.x; v.w[1] = a.y; v.w[2] = a.z; v.w[3] = a.w;
-    v.w[4] = b.x; v.w[5] = b.y; v.w[6] = b.z; v.w[7] = b.w;
-  }
-  return v;
+
+// Where channels lie in the contraction of the scores.  Four threads load a token's 64 bytes of a row, 16 each (a warp 8 tokens at a time, 512 bytes), and
+// write what they hold into tensor memory in the accumulator layout of the warp-level products: thread q's channel pairs 2 j, 2 j + 1 are columns 8 j + 2 q, + 1, that
+// is positions 16 j + 4 q .. + 3.  (A thread a token and 32 bytes a load, whose 32 sectors lie in as many lines: 374 instead of 296 us for 128 rows and 16 sequences of 32768
+// tokens.)  q = 2, 3 take their words in the order 2 3 0 1, so that the stores of the values meet in no bank.
+__host__ __device__ constexpr int position_of(int chunk) {   // of the first four of 8 channels, chunk 0..15 of a group; the others are 16 further on
+  return 32 * ((chunk & 3) ^ ((chunk >> 3) << 1)) + 4 * (chunk >> 2);
 }
+__host__ __device__ constexpr int rope_position_of(int chunk) { return 32 * (chunk >> 2) + 4 * (chunk & 3); }   // likewise, chunk 0..7 of a rotary key
 
 // ------------------------------------------------------------------ the cut
 struct Cursor {   // where a CTA's range begins, and how much of it there is
@@ -324,22 +367,29 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
   const uint32_t sbase = smem_u32(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
   int* misc_s = reinterpret_cast<int*>(smem + C::kOffMisc);
-  volatile int* misc = misc_s;   // [0] abort of waits, [2] tensor memory
+  volatile int* misc = misc_s;   // [0] abort of data waits, [1] of waits for pieces, [2] tensor memory
   volatile int* ab = misc;
+  const PieceWait iab = {misc + 1};   // (pieces need no data to arrive and stay in step after a wait for data has given up)
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
-  // of 128 channels of keys (five a tile, in turn): kready, kfree (2); of a group of a tile's values: vready, vfree (4); of a tile: fready (2), sfull, sfree, pready, odone;
-  // of a piece: ifull, iempty, qready (2), qfree
-  const uint32_t kready = bars, kfree = bars + 16, vready = bars + 32, vfree = bars + 64, fready = bars + 96, sfull = bars + 112, sfree = bars + 120,
-                 pready = bars + 128, odone = bars + 136, ifull = bars + 144, iempty = bars + 160, qready = bars + 176, qfree = bars + 192;
+  // of a place for keys: kready, kfree; of a group of the values: vready, vfree (4); of the powers of two: fready, ffree (kFac); of a tile: sfull, sfree,
+  // pready, odone; of a piece: ifull, iempty, qready (2), qfree
+  const uint32_t kready = bars, kfree = kready + 8 * kPlaces, vready = kfree + 8 * kPlaces, vfree = vready + 32, fready = vfree + 32, ffree = fready + 8 * kFac,
+                 sfull = ffree + 8 * kFac, sfree = sfull + 8, pready = sfree + 8, odone = pready + 8, ifull = odone + 8, iempty = ifull + 16, qready = iempty + 16,
+                 qfree = qready + 16;
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(kready + i * 8, 8);
+    for (int i = 0; i < kPlaces; ++i) {
+      mbar_init(kready + i * 8, 16);   // (rotary keys by all, 128 channels by eight warps, twice each)
       mbar_init(kfree + i * 8, 1);
-      mbar_init(fready + i * 8, 4);
+    }
+    for (int i = 0; i < kFac; ++i) {
+      mbar_init(fready + i * 8, 1);
+      mbar_init(ffree + i * 8, 8 + 16);
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(ifull + i * 8, 1);
-      mbar_init(iempty + i * 8, 8 + 8 + 1);
-      mbar_init(qready + i * 8, 8);
+      mbar_init(iempty + i * 8, 8 + 16 + 2 + 1);   // softmax, codes, products, powers of two
+      mbar_init(qready + i * 8, 16);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(vready + i * 8, 8);
@@ -370,6 +420,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
     const int wg = warp >> 2, w4 = warp & 3, col0 = wg * NC + 2 * (lane & 3), tok0 = 32 * w4 + (lane >> 2);   // this thread's rows col0 + 8 j, + 1 and tokens tok0 + 8 i
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
     float* const rq_s = reinterpret_cast<float*>(smem + C::kOffRq);
+    float* const ref_s = reinterpret_cast<float*>(smem + C::kOffRef);
+    float* const final_s = reinterpret_cast<float*>(smem + C::kOffFinal);
     float* const scale_s = reinterpret_cast<float*>(smem + C::kOffScale);
     float* const sum_s = reinterpret_cast<float*>(smem + C::kOffSum);
     float* const max_s = reinterpret_cast<float*>(smem + C::kOffMax);
@@ -377,145 +429,161 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
     const int pr = lane & 7, pb = lane >> 3, swz = NR == 64 ? pr : NR == 32 ? pr >> 1 : pr >> 2;
     const uint32_t p_row = sbase + C::kOffP + (uint32_t)((32 * w4 + (NJ == 1 ? 8 * pb : 8 * (pb & 1)) + pr) * C::kPRow);
     int gt = 0;   // tiles so far
+    Ring fr;      // place of their powers of two
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
-      wait(ifull + qi * 8, (ic >> 1) & 1, ab);
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, rt = items[qi].rt;
       if (n == 0) break;
       wait(qready + qi * 8, (ic >> 1) & 1, ab);
-      uint64_t rq[NJ], ref[NJ], l[NJ];    // of pairs of rows
+      // (factors and references of pairs of rows stay in shared memory, for want of registers)
+      const uint64_t* const rq = reinterpret_cast<const uint64_t*>(rq_s + qi * NR + col0);
+      uint64_t* const ref = reinterpret_cast<uint64_t*>(ref_s + col0);
+      uint64_t l[NJ];
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        rq[j] = f2_pack(rq_s[qi * NR + col0 + 8 * j], rq_s[qi * NR + col0 + 8 * j + 1]);
-        ref[j] = l[j] = 0ull;
+        l[j] = 0ull;
+        if (w4 == 0 && lane < 4) ref[4 * j] = 0ull;
       }
-      const uint64_t c2 = f2_pack(p.sm_log2, p.sm_log2);
+      const int id = 1 + wg;
+      named_bar(id, 128);
       const int clear = p.causal ? len - p.n + 1 : len;   // tokens that every row sees
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt) {
-        wait(fready + (gt & 1) * 8, (gt >> 1) & 1, ab);
+      for (int u = 0; u < n; ++u, ++gt, fr.next(kFac)) {
+        wait(fready + fr.i * 8, fr.ph, ab);
         wait(sfull, gt & 1, ab);
         tc_fence_after();
-        const float2* fac = reinterpret_cast<const float2*>(smem + C::kOffFac) + (gt & 1) * kTile + tok0;
-        uint64_t x[4][NJ];   // [token][pair of rows]
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t s[4 * NJ], r[4 * NJ];
-          ld_16x256<NJ>(tmem0 + C::kTmS + wg * NC + lanes + ((uint32_t)(16 * h) << 16), s);
-          ld_16x256<NJ>(tmem0 + C::kTmSr + wg * NC + lanes + ((uint32_t)(16 * h) << 16), r);
-          tc_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float2 f = fac[16 * h + 8 * i];
-            const uint64_t f2 = f2_pack(f.x, f.x), e2 = f2_pack(f.y, f.y);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-              x[2 * h + i][j] = f2_fma(u2_pack(s[4 * j + 2 * i], s[4 * j + 2 * i + 1]), f2_mul(f2, rq[j]),
-                                       f2_fma(u2_pack(r[4 * j + 2 * i], r[4 * j + 2 * i + 1]), c2, e2));
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sfree);
+        const float2* fac = reinterpret_cast<const float2*>(smem + C::kOffFac) + fr.i * kTile + tok0;
+        const uint32_t tm_s = tmem0 + C::kTmS + wg * NC + lanes;
         const int first = (u0 + u) * kTile;
-        if (first + kTile > clear) {   // a mask: the sequence's end, and what lies behind a row's position
+        // Scores of this thread's tokens tok0 + 16 h, + 8 and all its pairs of rows, less their references
+        auto scores = [&](int h, const uint32_t* s, uint64_t (&x)[2][NJ]) {
+          float2 f[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) f[i] = fac[16 * h + 8 * i];
 #pragma unroll
           for (int j = 0; j < NJ; ++j) {
-            int limit[2];
+            const uint64_t q = rq[4 * j], minus = ref[4 * j] ^ 0x8000000080000000ull;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) limit[k] = (p.causal ? clear + min((rt * kMaxRows + col0 + 8 * j + k) / p.Hq, p.n - 1) : len) - first;
+            for (int i = 0; i < 2; ++i)
+              x[i][j] = f2_fma(u2_pack(s[4 * j + 2 * i], s[4 * j + 2 * i + 1]), f2_mul(f2_pack(f[i].x, f[i].x), q), f2_add(f2_pack(f[i].y, f[i].y), minus));
+          }
+          if (__builtin_expect(first + kTile > clear, 0)) {   // a mask: the sequence's end, and what lies behind a row's position
+            const int2* const lim = reinterpret_cast<const int2*>(smem + C::kOffLim) + (qi * NR + col0) / 2;
+            const int t = first + 16 * h + tok0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float a, c;
-              f2_unpack(x[i][j], a, c);
-              x[i][j] = f2_pack(tok0 + 8 * i < limit[0] ? a : -INFINITY, tok0 + 8 * i < limit[1] ? c : -INFINITY);
+            for (int j = 0; j < NJ; ++j) {
+              const int2 end = lim[4 * j];
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                float a, c;
+                f2_unpack(x[i][j], a, c);
+                x[i][j] = f2_pack(t + 8 * i < end.x ? a : -INFINITY, t + 8 * i < end.y ? c : -INFINITY);
+              }
             }
           }
-        }
-        float most = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const uint64_t minus = ref[j] ^ 0x8000000080000000ull;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float a, c;
-            f2_unpack(f2_add(x[i][j], minus), a, c);
-            most = fmaxf(most, fmaxf(a, c));
-          }
-        }
-        const int id = 1 + wg;
-        if (bar_or(id, 128, u == 0 || most > kMost)) {   // the rows' references: set, or raised
-          float* const mine = max_s + w4 * NR + col0;
-#pragma unroll
-          for (int j = 0; j < NJ; ++j) {
-            float m[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float a, c;
-              f2_unpack(x[i][j], a, c);
-              m[0] = fmaxf(m[0], a);
-              m[1] = fmaxf(m[1], c);
-            }
-#pragma unroll
-            for (int o = 4; o < 32; o <<= 1) {
-              m[0] = fmaxf(m[0], __shfl_xor_sync(0xFFFFFFFFu, m[0], o));
-              m[1] = fmaxf(m[1], __shfl_xor_sync(0xFFFFFFFFu, m[1], o));
-            }
-            if (lane < 4) {
-              mine[8 * j] = m[0];
-              mine[8 * j + 1] = m[1];
-            }
-          }
-          named_bar(id, 128);
-          bool rescale = false;
-#pragma unroll
-          for (int j = 0; j < NJ; ++j) {
-            float r[2], f[2];
-            f2_unpack(ref[j], r[0], r[1]);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float* m = max_s + col0 + 8 * j + k;
-              const float M = fmaxf(fmaxf(m[0], m[NR]), fmaxf(m[2 * NR], m[3 * NR]));
-              const float to = (u == 0 ? M > -INFINITY : M - r[k] > kRaise) ? M - kTop : r[k];
-              f[k] = u == 0 ? 1.0f : ex2(r[k] - to);
-              r[k] = to;
-              rescale = rescale || f[k] != 1.0f;
-              if (w4 == 0 && lane < 4) scale_s[col0 + 8 * j + k] = f[k];
-            }
-            ref[j] = f2_pack(r[0], r[1]);
-            l[j] = f2_mul(l[j], f2_pack(f[0], f[1]));
-          }
-          if (bar_or(id, 128, rescale)) {   // (not in a piece's first tile: f is 1)
-            wait(odone, (gt - 1) & 1, ab);
-            tc_fence_after();
-#pragma unroll 1
-            for (int i = 0; i < 4 * NC; i += 8) {
-              const int g = i / NC, c = wg * NC + (i - g * NC);
-              uint32_t o[8];
-              TmemRegs<8>::ld(tmem0 + C::kTmO + g * NR + c + lanes, o);
-              tc_wait_ld();
-#pragma unroll
-              for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * scale_s[c + k]);
-              TmemRegs<8>::st(tmem0 + C::kTmO + g * NR + c + lanes, o);
-            }
-            tc_wait_st();
-          }
-        }
+        };
+        bool anew = u == 0;   // references are to be set, or raised
         uint32_t w[4][NJ];
+        uint64_t sum[NJ];
+#pragma unroll 1
+        for (;;) {
+          if (__builtin_expect(anew, 0)) {
+            uint64_t top[NJ];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t back = 0x7F000000u - __float_as_uint(fac[8 * i].x);   // 2^-e
-          const uint64_t b2 = u2_pack(back, back);
+            for (int j = 0; j < NJ; ++j) top[j] = f2_pack(-INFINITY, -INFINITY);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+              uint32_t s[4 * NJ];
+              uint64_t x[2][NJ];
+              ld_16x256<NJ>(tm_s + ((uint32_t)(16 * h) << 16), s);
+              tc_wait_ld();
+              scores(h, s, x);
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) {
-            float a, c;
-            f2_unpack(f2_add(x[i][j], ref[j] ^ 0x8000000080000000ull), a, c);
-            a = ex2(a);
-            c = ex2(c);
-            l[j] = f2_fma(f2_pack(a, c), b2, l[j]);
-            w[i][j] = pack_f16x2(a, c);
+              for (int j = 0; j < NJ; ++j) {
+                float m[2], y[4];
+                f2_unpack(top[j], m[0], m[1]);
+                f2_unpack(x[0][j], y[0], y[1]);
+                f2_unpack(x[1][j], y[2], y[3]);
+                top[j] = f2_pack(fmaxf(m[0], fmaxf(y[0], y[2])), fmaxf(m[1], fmaxf(y[1], y[3])));
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+              float m[2];
+              f2_unpack(top[j], m[0], m[1]);
+#pragma unroll
+              for (int o = 4; o < 32; o <<= 1) {
+                m[0] = fmaxf(m[0], __shfl_xor_sync(0xFFFFFFFFu, m[0], o));
+                m[1] = fmaxf(m[1], __shfl_xor_sync(0xFFFFFFFFu, m[1], o));
+              }
+              if (lane < 4) *reinterpret_cast<float2*>(max_s + w4 * NR + col0 + 8 * j) = make_float2(m[0], m[1]);
+            }
+            named_bar(id, 128);
+            bool rescale = false;
+            if (w4 == 0 && lane < 4) {   // a warp for all
+#pragma unroll 1
+              for (int j = 0; j < 2 * NJ; ++j) {
+                const int c = col0 + 8 * (j >> 1) + (j & 1);
+                const float M = fmaxf(fmaxf(max_s[c], max_s[NR + c]), fmaxf(max_s[2 * NR + c], max_s[3 * NR + c]));   // (less the reference)
+                const float more = (u == 0 ? M > -INFINITY : M > kRaise) ? M - kTop : 0.0f, f = u == 0 ? 1.0f : ex2(-more);
+                ref_s[c] += more;
+                scale_s[c] = f;
+                rescale = rescale || f != 1.0f;
+              }
+            }
+            if (bar_or(id, 128, rescale)) {   // (not in a piece's first tile: f is 1)
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) l[j] = f2_mul(l[j], *reinterpret_cast<const uint64_t*>(scale_s + col0 + 8 * j));
+              wait(odone, (gt - 1) & 1, ab);
+              tc_fence_after();
+#pragma unroll 1
+              for (int i = 0; i < 4 * NC; i += 8) {
+                const int g = i / NC, c = wg * NC + (i - g * NC);
+                uint32_t o[8];
+                TmemRegs<8>::ld(tmem0 + C::kTmO + g * NR + c + lanes, o);
+                tc_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * scale_s[c + k]);
+                TmemRegs<8>::st(tmem0 + C::kTmO + g * NR + c + lanes, o);
+              }
+              tc_wait_st();
+            }
           }
+          uint32_t s0[4 * NJ], s1[4 * NJ];
+          ld_16x256<NJ>(tm_s, s0);
+          uint32_t most = 0u;   // the largest two weights' bits, so to say: FP16's infinity, and what is no number, are above all others
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) sum[j] = 0ull;
+          auto weights = [&](int h, const uint32_t (&s)[4 * NJ], uint32_t (&v)[4][NJ]) {
+            uint64_t x[2][NJ];
+            scores(h, s, x);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t back = 0x7F000000u - __float_as_uint(fac[16 * h + 8 * i].x);   // 2^-e
+              const uint64_t b2 = u2_pack(back, back);
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) {
+                float a, c;
+                f2_unpack(x[i][j], a, c);
+                a = ex2(a);
+                c = ex2(c);
+                sum[j] = f2_fma(f2_pack(a, c), b2, sum[j]);
+                v[2 * h + i][j] = pack_f16x2(a, c);
+                asm("max.u16x2 %0, %0, %1;" : "+r"(most) : "r"(v[2 * h + i][j]));
+              }
+            }
+          };
+          tc_wait_ld();
+          ld_16x256<NJ>(tm_s + (16u << 16), s1);
+          weights(0, s0, w);
+          tc_wait_ld();
+          weights(1, s1, w);
+          if (anew || !bar_or(id, 128, (most & 0xFFFFu) >= 0x7C00u || most >= 0x7C000000u)) break;
+          anew = true;
         }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) l[j] = f2_add(l[j], sum[j]);
         if (gt > 0) wait(odone, (gt - 1) & 1, ab);   // the weights before have been used
         if constexpr (NJ == 1) {
           stm_x4(p_row + (uint32_t)((wg ^ swz) << 4), w[0][0], w[1][0], w[2][0], w[3][0]);
@@ -531,14 +599,17 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         proxy_fence();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(pready);
+        if (lane == 0) {
+          mbar_arrive(pready);
+          mbar_arrive(sfree);
+          mbar_arrive(ffree + fr.i * 8);
+        }
       }
       // ---- end of the piece: sums over the warps, then a row's 512 channels by the lanes that hold them
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        float s[2], r[2];
+        float s[2];
         f2_unpack(l[j], s[0], s[1]);
-        f2_unpack(ref[j], r[0], r[1]);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) {
           s[0] += __shfl_xor_sync(0xFFFFFFFFu, s[0], o);
@@ -548,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             sum_s[w4 * NR + col0 + 8 * j + k] = s[k];
-            if (w4 == 0) max_s[col0 + 8 * j + k] = r[k];   // (another warp may still read factors in scale_s)
+            if (w4 == 0) final_s[col0 + 8 * j + k] = ref_s[col0 + 8 * j + k];   // (ref_s may be the next piece's while it is read)
           }
         }
       }
@@ -562,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       float* const part = p.part + (int64_t)(segment + (int)blockIdx.x) * NR * kPartRow;
 #pragma unroll 1
       for (int i = 0; i < 2 * NR; i += 8) {
-        const int g = 2 * wg + i / NR, c0 = i % NR, d = g * 128 + w4 * 32 + lane;
+        const int g = 2 * wg + i / NR, c0 = i % NR, d = g * 128 + w4 * 32 + (lane & 24) + ((lane & 1) << 2 | (lane & 2) | (lane & 4) >> 2);   // (see values8)
         if (c0 >= rows) continue;
         uint32_t o[8];
         TmemRegs<8>::ld(tmem0 + C::kTmO + g * NR + c0 + lanes, o);
@@ -582,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         }
       }
       if (tid < rows) {
-        const float L = (sum_s[tid] + sum_s[NR + tid]) + (sum_s[2 * NR + tid] + sum_s[3 * NR + tid]), M = max_s[tid];
+        const float L = (sum_s[tid] + sum_s[NR + tid]) + (sum_s[2 * NR + tid] + sum_s[3 * NR + tid]), M = final_s[tid];
         if (!direct) *reinterpret_cast<float2*>(part + tid * kPartRow + kLatent) = make_float2(L != 0.0f ? M : -INFINITY, L);
         else if (p.lse) p.lse[row0 + tid] = L != 0.0f ? (M + __log2f(L)) * 0.6931471805599453f : -INFINITY;
       }
@@ -600,156 +671,177 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       tc_fence_after();
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem0), "r"(512u) : "memory");
     }
-    if (tid == 0 && misc[0]) atomicOr(p.flags, kFlagTimeout);
+    if (tid == 0 && (misc[0] || misc[1])) atomicOr(p.flags, kFlagTimeout);
     return;
   }
   // ================================================================================== codes to FP16, and queries
-  if (warp < 16) {
+  if (warp < 24) {
     reg_inc<kRegCodes>();
-    const int half = (warp - 8) >> 2, tok = (warp & 3) * 32 + lane;   // 64 channels of each group's 128; token of a tile
-    const uint32_t tm_k = tmem0 + C::kTmK + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t v_row = sbase + C::kOffV + (uint32_t)(half * 16384 + tok * 128);
-    float2* const fac = reinterpret_cast<float2*>(smem + C::kOffFac);
-    int gt = 0, ku = 0;   // tiles, places for keys so far
+    const int set = (warp - 8) >> 3, q4 = lane & 3, lane0 = (warp & 3) * 32 + ((warp >> 2) & 1) * 16, tok = lane0 + (lane >> 2);   // tokens tok, tok + 8 of a tile
+    const uint32_t tm_k = tmem0 + C::kTmK + ((uint32_t)lane0 << 16);
+    const uint32_t v_row = sbase + C::kOffV + (uint32_t)(set * 32768 + (q4 >> 1) * 16384 + tok * 128), v_swz = (uint32_t)((((q4 & 1) * 4) ^ (q4 & 2) ^ (tok & 7)) << 4);
+    int gt = 0;          // tiles so far
+    Ring kp, fr;         // places of the tile's rotary keys, of the tokens' powers of two
+    kp.ph = 1;           // (empty: the first waits for them succeed)
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
-      wait(ifull + qi * 8, (ic >> 1) & 1, ab);
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b, rt = items[qi].rt;
       if (n == 0) break;
-      // what the first tile's loads need, on its way while the queries come
+      // the first tile's loads, on their way while the queries come
       const int top = max(len - 1, 0);
       int next_id = len > 0 ? block_id(p, b, min(u0 * kTile + tok, top)) : 0;
-      if (ic > 0) wait(qfree, (ic - 1) & 1, ab);
-      {   // queries: a row by TPR threads, chunks of 8 channels
-        constexpr int TPR = 256 / NR, kMine = 64 / TPR;
-        const int t = tid - 256, c = t / TPR, i = t % TPR, row = rt * kMaxRows + c;
-        const bool used = row < p.R;
-        const int64_t src = (int64_t)b * p.R + (used ? row : 0);
-        uint4 x[kMine];
-        uint32_t m = 0u;
+      uint4 a[2], r[2], key[2];    // of both tokens: codes of the set's next group, 16 bytes of the rotary key
+      float2 m[2][2];              // scalars of the set's groups
+      uint32_t row[2] = {0u, 0u};  // of the loads: group set's (fewer than 2^31)
+      auto place = [&](int u) {    // where tile u's tokens lie (in one block), their scalars and rotary keys; the block after it is looked up
+        const int t = min((u0 + u) * kTile + tok, top), t8 = min((u0 + u) * kTile + tok + 8, top), blk = in_pool(p, next_id), first = quotient(t, p.bt_div) * p.bt;
+        row[0] = (uint32_t)((blk * kGroups + set) * p.bt + t - first);
+        row[1] = row[0] + (uint32_t)(t8 - t);
 #pragma unroll
-        for (int k = 0; k < kMine; ++k) {
-          x[k] = ld_dep(p.q + src * p.q_stride + i + k * TPR);
-          if (!used) x[k] = make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t v[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
-#pragma unroll
-          for (int z = 0; z < 4; ++z) asm("max.u16x2 %0, %0, %1;" : "+r"(m) : "r"(v[z] & 0x7FFF7FFFu));
+        for (int i = 0; i < 2; ++i) {
+          m[i][0] = ld_dep(p.meta + row[i]);
+          m[i][1] = ld_dep(p.meta + row[i] + 2 * p.bt);
+          key[i] = ld_dep(p.pages + (int64_t)(blk * p.bt + (i ? t8 : t) - first) * 8 + set * 4 + q4);
         }
-        uint32_t best = max(m & 0xFFFFu, m >> 16);
+        if (u + 1 < n) next_id = block_id(p, b, min(t + kTile, top));
+      };
+      auto load_codes = [&](int i) {   // of group set + 2 i
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int64_t at = (int64_t)(row[k] + (uint32_t)(2 * i * p.bt)) * 4 + q4;
+          a[k] = ld_dep(reinterpret_cast<const uint4*>(p.anchor) + at);
+          if (FULL) r[k] = ld_dep(reinterpret_cast<const uint4*>(p.residual) + at);
+        }
+      };
+      place(0);
+      load_codes(0);
+      if (ic > 0) wait(qfree, (ic - 1) & 1, ab);
+      {   // queries: a row by TPR threads, chunks of 8 channels, 16 at a time
+        constexpr int TPR = 512 / NR, kMine = 64 / TPR;
+        const int t = tid - 256, c = t / TPR, i = t % TPR, qrow = rt * kMaxRows + c;
+        const bool used = qrow < p.R;
+        const int64_t src = (int64_t)b * p.R + (used ? qrow : 0);
+        const uint4 *q = p.q + src * p.q_stride, *qr = p.qr + src * p.qr_stride;
+        uint32_t top2 = 0u;
+#pragma unroll 4
+        for (int k = 0; k < kMine + (i < 8); ++k) {   // the largest of latent and rotary part
+          const uint4 x = k < kMine ? ld_dep(q + i + k * TPR) : ld_dep(qr + i + (k - kMine) * TPR);
+          const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int z = 0; z < 4; ++z) asm("max.u16x2 %0, %0, %1;" : "+r"(top2) : "r"(v[z] & 0x7FFF7FFFu));
+        }
+        uint32_t best = max(top2 & 0xFFFFu, top2 >> 16);
 #pragma unroll
         for (int o = TPR / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xFFFFFFFFu, best, o));
         const int e = best > 0u ? min(max(exponent_of(__uint_as_float(best << 16)), -100), 113) : 0;
-        const float f = pow2(-e);
-        const uint32_t dst = sbase + C::kOffQ + (uint32_t)(c * 128);
-#pragma unroll
-        for (int k = 0; k < kMine; ++k) {
-          const int ch = i + k * TPR;
-          sts128(dst + (uint32_t)((ch >> 3) * NR * 128 + (((ch & 7) ^ (c & 7)) << 4)), pack_f16x2(bf_lo(x[k].x) * f, bf_hi(x[k].x) * f),
-                 pack_f16x2(bf_lo(x[k].y) * f, bf_hi(x[k].y) * f), pack_f16x2(bf_lo(x[k].z) * f, bf_hi(x[k].z) * f),
-                 pack_f16x2(bf_lo(x[k].w) * f, bf_hi(x[k].w) * f));
+        const float f = used ? pow2(-e) : 0.0f;
+        // (four channels at a position of the scores' order: see position_of)
+        auto put = [&](int slab, int at, uint32_t x, uint32_t y) {
+          sts64(sbase + C::kOffQ + (uint32_t)((slab + (at >> 6)) * NR * 128 + c * 128 + ((((at & 63) >> 3) ^ (c & 7)) << 4) + ((at & 4) << 1)), x, y);
+        };
+#pragma unroll 4
+        for (int k = 0; k < kMine; ++k) {   // (again, out of a cache)
+          const int ch = i + k * TPR, at = position_of(ch & 15);
+          uint4 x = ld_dep(q + ch);
+          if (!used) x = make_uint4(0u, 0u, 0u, 0u);
+          put(2 * (ch >> 4), at, pack_f16x2(bf_lo(x.x) * f, bf_lo(x.z) * f), pack_f16x2(bf_lo(x.y) * f, bf_lo(x.w) * f));   // (0 4 2 6 | 1 5 3 7)
+          put(2 * (ch >> 4), at + 16, pack_f16x2(bf_hi(x.x) * f, bf_hi(x.z) * f), pack_f16x2(bf_hi(x.y) * f, bf_hi(x.w) * f));
         }
-        for (int ch = i; ch < 8; ch += TPR) {
-          uint4 y = ld_dep(p.qr + src * p.qr_stride + ch);
+        if (i < 8) {
+          uint4 y = ld_dep(qr + i);
           if (!used) y = make_uint4(0u, 0u, 0u, 0u);
-          sts128(dst + (uint32_t)(8 * NR * 128 + ((ch ^ (c & 7)) << 4)), y.x, y.y, y.z, y.w);
+          const uint32_t f2 = (uint32_t)((127 - e) << 7) * 0x10001u;
+          put(8, rope_position_of(i), mul_bf16x2(y.x, f2), mul_bf16x2(y.y, f2));
+          put(8, rope_position_of(i) + 16, mul_bf16x2(y.z, f2), mul_bf16x2(y.w, f2));
         }
-        if (i == 0) reinterpret_cast<float*>(smem + C::kOffRq)[qi * NR + c] = p.sm_log2 * pow2(e);
+        if (i == 0) {   // the factor of the row's scores; the tokens that it sees
+          reinterpret_cast<float*>(smem + C::kOffRq)[qi * NR + c] = p.sm_log2 * pow2(e);
+          reinterpret_cast<int*>(smem + C::kOffLim)[qi * NR + c] = p.causal ? len - p.n + 1 + min(qrow / p.Hq, p.n - 1) : len;
+        }
         proxy_fence();
         __syncwarp();
         if (lane == 0) mbar_arrive(qready + qi * 8);
       }
-      Words8 a[kGroups], r[kGroups], key[2];
-      float2 m[kGroups];
-      int64_t row = 0;     // of the loads: of group 0
-      int64_t page = 0;
-      auto place = [&](int u) {   // where tile u's token lies; the block after it is looked up
-        const int t = min((u0 + u) * kTile + tok, top), blk = in_pool(p, next_id), off = t - quotient(t, p.bt_div) * p.bt;
-        row = (int64_t)blk * kGroups * p.bt + off;
-        page = (int64_t)blk * p.bt + off;
-        if (u + 1 < n) next_id = block_id(p, b, min(t + kTile, top));
-      };
-      auto load_meta = [&]() {
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) m[g] = ld_dep(p.meta + row + g * p.bt);
-      };
-      auto load_key = [&]() {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) key[k] = load32(reinterpret_cast<const char*>(p.pages) + page * 128 + half * 64 + k * 32, p.wide);
-      };
-      auto load_codes = [&](int g) {
-        const int64_t at = (row + (int64_t)g * p.bt) * 64 + half * 32;
-        a[g] = load32(p.anchor + at, p.wide);
-        if (FULL) r[g] = load32(p.residual + at, p.wide);
-      };
-      place(0);
-      load_meta();
-      load_key();
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g) load_codes(g);
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt) {
-        const bool live = (u0 + u) * kTile + tok < len;   // (what lies behind the sequence's end may be anything)
-        float s[kGroups], z[kGroups], big = 0.0f;
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          s[g] = live ? m[g].x : 0.0f;
-          z[g] = live ? m[g].y : 0.0f;
-          big = fmaxf(big, fmaxf(fabsf(z[g]), fabsf(fmaf(255.0f, s[g], z[g]))));
-        }
-        const int e = min(max(exponent_of(big), kMinExp), 113);
-        const float f = pow2(-e);
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          s[g] *= f;
-          z[g] = fmaf(-32768.0f, s[g], z[g] * f);
-        }
-        if (half == 0) {
-          fac[(gt & 1) * kTile + tok] = make_float2(pow2(e), (float)e);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(fready + (gt & 1) * 8);
-        }
+      for (int u = 0; u < n; ++u, ++gt, fr.next(kFac)) {
         const bool more = u + 1 < n;
-        // ---- the rotary key
-        if (ku > 1) wait(kfree + (ku & 1) * 8, ((ku >> 1) - 1) & 1, ab);
-        tc_fence_after();
-        {
-          uint32_t o[16];
+        wait(fready + fr.i * 8, fr.ph, ab);
+        float back[2];     // 2^-e, of a token behind the sequence's end (whose rows may be anything) 0
+        bool live[2];
 #pragma unroll
-          for (int k = 0; k < 16; ++k) o[k] = live ? key[k >> 3].w[k & 7] : 0u;
-          TmemRegs<16>::st(tm_k + (ku & 1) * 64 + half * 16, o);
+        for (int i = 0; i < 2; ++i) {
+          live[i] = (u0 + u) * kTile + tok + 8 * i < len;
+          back[i] = pow2(-(int)reinterpret_cast<const float2*>(smem + C::kOffFac)[fr.i * kTile + tok + 8 * i].y);
         }
-        tc_wait_st();
-        tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(kready + (ku & 1) * 8);
-        ++ku;
-        if (more) {
-          place(u + 1);
-          load_meta();
-          load_key();
-        }
-        // ---- 128 channels at a time: keys, then values once their place is free
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          const uint64_t s2 = f2_pack(s[g], s[g]), z2 = f2_pack(z[g], z[g]);
-          uint32_t o[32];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) values8(a[g].w[k], FULL ? r[g].w[k] : 0x88888888u, s2, z2, o + 4 * k);
-          if (more) load_codes(g);
-          if (ku > 1) wait(kfree + (ku & 1) * 8, ((ku >> 1) - 1) & 1, ab);
-          tc_fence_after();
-          TmemRegs<32>::st(tm_k + (ku & 1) * 64 + half * 32, o);
+        if (lane == 0) mbar_arrive(ffree + fr.i * 8);
+        Ring k = kp;   // the place at hand
+        kp.next(kPlaces, 5);
+        auto keys_there = [&]() {
           tc_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(kready + (ku & 1) * 8);
-          ++ku;
+        };
+        // ---- the rotary key, BF16 times the power of two (exact), 32 channels by either set
+        {
+          uint32_t o[8];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t f2 = live[i] ? (__float_as_uint(back[i]) >> 16) * 0x10001u : 0u, w[4] = {key[i].x, key[i].y, key[i].z, key[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[(j >> 1) * 4 + 2 * i + (j & 1)] = live[i] ? mul_bf16x2(w[j], f2) : 0u;
+          }
+          wait(kfree + k.i * 8, k.ph, ab);
+          tc_fence_after();
+          st_16x256(tm_k + k.i * 64 + set * 16, o);
+          keys_there();
+          if (lane == 0) mbar_arrive(kready + k.i * 8);
+        }
+        k.next(kPlaces, 1 + set);
+        // ---- 128 channels at a time, ready before their places are
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int g = set + 2 * i;
+          uint32_t o[32];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float s = (live[h] ? m[h][i].x : 0.0f) * back[h], mid = fmaf(128.0f, s, (live[h] ? m[h][i].y : 0.0f) * back[h]);
+            const uint32_t s2 = pack_f16x2(s, s), m2 = pack_f16x2(mid, mid);
+            const bool turn = (q4 & 2) != 0;
+            const uint4 x = turn ? make_uint4(a[h].z, a[h].w, a[h].x, a[h].y) : a[h], y = turn ? make_uint4(r[h].z, r[h].w, r[h].x, r[h].y) : r[h];
+            const uint32_t wa[4] = {x.x, x.y, x.z, x.w}, wr[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              uint32_t v[4];
+              values8(wa[w], FULL ? wr[w] : 0x88888888u, s2, m2, v);
+              o[8 * w + 2 * h] = v[0];
+              o[8 * w + 2 * h + 1] = v[1];
+              o[8 * w + 4 + 2 * h] = v[2];
+              o[8 * w + 4 + 2 * h + 1] = v[3];
+            }
+          }
+          if (i == 0) load_codes(1);
+          wait(kfree + k.i * 8, k.ph, ab);
+          tc_fence_after();
+          st_16x256(tm_k + k.i * 64, o);
           if (gt > 0) wait(vfree + g * 8, (gt - 1) & 1, ab);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) sts128(v_row + (uint32_t)(g * 32768 + ((k ^ (tok & 7)) << 4)), o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-          proxy_fence();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(vready + g * 8);
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              sts128((v_row + (uint32_t)(i * 65536 + h * 1024)) + (v_swz ^ (uint32_t)(w << 4)), o[8 * w + 2 * h], o[8 * w + 2 * h + 1], o[8 * w + 4 + 2 * h], o[8 * w + 5 + 2 * h]);
+          }
+          keys_there();
+          if (lane == 0) {
+            mbar_arrive2(kready + k.i * 8);
+            mbar_arrive(vready + g * 8);
+          }
+          if (i == 1 && more) {   // (behind the hand-over: loads wait for room in the queue of those under way, which these fill)
+            place(u + 1);
+            load_codes(0);
+          }
+          k.next(kPlaces, 2);
         }
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
@@ -758,67 +850,71 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
   }
   reg_dec<kRegRest>();
   // ================================================================================== products
-  if (warp == 16) {
-    constexpr uint32_t kIdescS = tc_idesc(NR, false), kIdescO = tc_idesc(NR, true) | kChannelsMajor;
-    constexpr uint32_t kHi = desc_hi(128u, 2u), kPHi = desc_hi(C::kPRow, C::kPLayout);
-    const uint32_t q_lo = desc_lo(sbase + C::kOffQ, 16u), v_lo = desc_lo(sbase + C::kOffV, 16384u), p_lo = desc_lo(sbase + C::kOffP, 16384u);
-    int gt = 0, ku = 0;
-    // scores: the rotary keys' (g < 0), or of 128 channels; the last of a tile makes them full, the last of a piece gives up the queries
-    auto qk = [&](int g, bool end) {
-      wait(kready + (ku & 1) * 8, (ku >> 1) & 1, ab);
-      tc_fence_after();
-      if (tc_elect()) {
-        const uint32_t a = tmem0 + C::kTmK + (ku & 1) * 64;
-        if (g < 0) {
-#pragma unroll
-          for (int ks = 0; ks < 4; ++ks)
-            tc_mma_ts(tmem0 + C::kTmSr, a + ks * 8, desc(q_lo + (uint32_t)((8 * NR * 128 + ks * 32) >> 4), kHi), kIdescS | kBf16Operands, ks > 0 ? 1u : 0u);
-        } else {
-          const uint32_t q = q_lo + (uint32_t)((2 * g * NR * 128) >> 4);
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks)
-            tc_mma_ts(tmem0 + C::kTmS, a + ks * 8, desc(q + (uint32_t)(((ks >> 2) * NR * 128 + (ks & 3) * 32) >> 4), kHi), kIdescS, ks > 0 || g > 0 ? 1u : 0u);
-        }
-        tc_commit(kfree + (ku & 1) * 8);
-        if (g == kGroups - 1) tc_commit(sfull);
-        if (end) tc_commit(qfree);
-      }
-      __syncwarp();
-      ++ku;
-    };
+  if (warp < 26) {
+    constexpr uint32_t kHi = desc_hi(128u, 2u);
+    const bool scores = warp == 24;
+    int gt = 0;   // tiles so far
+    Ring kp;      // place of the next keys
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
-      wait(ifull + qi * 8, (ic >> 1) & 1, ab);
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
       const int n = __shfl_sync(0xFFFFFFFFu, items[qi].n, 0);   // (known to be uniform)
       if (n == 0) break;
-      wait(qready + qi * 8, (ic >> 1) & 1, ab);
-      if (gt > 0) wait(sfree, (gt - 1) & 1, ab);
+      if (scores) {
+        constexpr uint32_t kIdesc = tc_idesc(NR, false);
+        const uint32_t q_lo = desc_lo(sbase + C::kOffQ, 16u), d = tmem0 + C::kTmS;
+        wait(qready + qi * 8, (ic >> 1) & 1, ab);
 #pragma unroll 1
-      for (int g = -1; g < kGroups; ++g) qk(g, n == 1 && g == kGroups - 1);
+        for (int u = 0; u < n; ++u, ++gt) {
+          if (gt > 0) wait(sfree, (gt - 1) & 1, ab);
+          // The rotary keys', then of 128 channels at a time; the last of a tile makes its scores full, the last of a piece gives up the queries
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt) {
-        wait(pready, gt & 1, ab);
+          for (int g = -1; g < kGroups; ++g, kp.next(kPlaces)) {
+            wait(kready + kp.i * 8, kp.ph, ab);
+            tc_fence_after();
+            if (tc_elect()) {
+              const uint32_t a = tmem0 + C::kTmK + kp.i * 64;
+              if (g < 0) {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                  tc_mma_ts(d, a + ks * 8, desc(q_lo + (uint32_t)((8 * NR * 128 + ks * 32) >> 4), kHi), kIdesc | kBf16Operands, ks > 0 ? 1u : 0u);
+              } else {
+                const uint32_t q = q_lo + (uint32_t)((2 * g * NR * 128) >> 4);
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                  tc_mma_ts(d, a + ks * 8, desc(q + (uint32_t)(((ks >> 2) * NR * 128 + (ks & 3) * 32) >> 4), kHi), kIdesc, 1u);
+              }
+              tc_commit(kfree + kp.i * 8);
+              if (g == kGroups - 1) tc_commit(sfull);
+              if (g == kGroups - 1 && u == n - 1) tc_commit(qfree);
+            }
+            __syncwarp();
+          }
+        }
+      } else {
+        constexpr uint32_t kIdesc = tc_idesc(NR, true) | kChannelsMajor, kPHi = desc_hi(C::kPRow, C::kPLayout);
+        const uint32_t v_lo = desc_lo(sbase + C::kOffV, 16384u), p_lo = desc_lo(sbase + C::kOffP, 16384u);
 #pragma unroll 1
-        for (int g = 0; g < kGroups; ++g) {
-          wait(vready + g * 8, gt & 1, ab);
+        for (int u = 0; u < n; ++u, ++gt) {
+#pragma unroll 1
+          for (int g = 0; g < kGroups; ++g) wait(vready + g * 8, gt & 1, ab);
+          // (Not by the threads that write the values: there it would wait for their loads.)
+          proxy_fence();
+          wait(pready, gt & 1, ab);
           tc_fence_after();
           if (tc_elect()) {
-            const uint32_t v = v_lo + (uint32_t)((g * 32768) >> 4), d = tmem0 + C::kTmO + g * NR;
+#pragma unroll 1
+            for (int g = 0; g < kGroups; ++g) {
+              const uint32_t v = v_lo + (uint32_t)((g * 32768) >> 4), d = tmem0 + C::kTmO + g * NR;
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-              tc_mma_ss(d, desc(v + ks * 128u, kHi), desc(p_lo + (uint32_t)((ks * 16 * C::kPRow) >> 4), kPHi), kIdescO, ks > 0 || u > 0 ? 1u : 0u);
-            tc_commit(vfree + g * 8);
-            if (g == kGroups - 1) tc_commit(odone);
+              for (int ks = 0; ks < 8; ++ks)
+                tc_mma_ss(d, desc(v + ks * 128u, kHi), desc(p_lo + (uint32_t)((ks * 16 * C::kPRow) >> 4), kPHi), kIdesc, ks > 0 || u > 0 ? 1u : 0u);
+              tc_commit(vfree + g * 8);
+            }
+            tc_commit(odone);
           }
           __syncwarp();
-          if (u + 1 < n) {   // the next tile's scores, as its channels come
-            if (g == 0) {
-              wait(sfree, gt & 1, ab);
-              qk(-1, false);
-            }
-            qk(g, u + 2 == n && g == kGroups - 1);
-          }
         }
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
@@ -827,13 +923,13 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
     return;
   }
   // ================================================================================== pieces
-  if (warp == 17) {
+  if (warp == 27) {
     Cursor cur = first_unit(p, blockIdx.x, gridDim.x, lane);
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       const Item it = next_piece(p, cur, blockIdx.x);
-      if (ic > 1) wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, ab);
+      if (ic > 1) wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
       if (lane == 0) {
         volatile Item* d = items + qi;
         d->b = it.b; d->rt = it.rt; d->len = it.len; d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib;
@@ -841,6 +937,45 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       }
       __syncwarp();
       if (it.n == 0) break;
+    }
+    bar_arrive(4, kDoneThreads);
+    return;
+  }
+  // ================================================================================== the tokens' powers of two, four tokens a lane
+  {
+    Ring fr;
+    fr.ph = 1;   // (empty: the first waits succeed)
+#pragma unroll 1
+    for (int ic = 0;; ++ic) {
+      const int qi = ic & 1;
+      wait(ifull + qi * 8, (ic >> 1) & 1, iab);
+      const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b;
+      if (n == 0) break;
+      const int top = max(len - 1, 0);
+#pragma unroll 1
+      for (int u = 0; u < n; ++u, fr.next(kFac)) {
+        wait(ffree + fr.i * 8, fr.ph, ab);
+        int blk[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) blk[i] = len > 0 ? block_id(p, b, min((u0 + u) * kTile + lane + 32 * i, top)) : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int tok = (u0 + u) * kTile + lane + 32 * i, t = min(tok, top);
+          const float2* at = p.meta + (int64_t)min(max(blk[i], 0), p.num_blocks - 1) * kGroups * p.bt + (t - quotient(t, p.bt_div) * p.bt);
+          float big = 0.0f;
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            const float2 m = ld_dep(at + g * p.bt);
+            big = fmaxf(big, fmaxf(fabsf(m.y), fabsf(fmaf(255.0f, m.x, m.y))));
+          }
+          if (tok >= len) big = 0.0f;   // (what lies behind the sequence's end may be anything)
+          const int e = min(max(exponent_of(big), kMinExp), 113);
+          reinterpret_cast<float2*>(smem + C::kOffFac)[fr.i * kTile + lane + 32 * i] = make_float2(pow2(e), (float)e);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(fready + fr.i * 8);
+      }
+      if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
     bar_arrive(4, kDoneThreads);
   }
@@ -931,7 +1066,9 @@ lynx_status latent_plan(const lynx_shape* s, int B, int n, LatentPlan* pl) {
   if (s->num_kv_heads <= 0 || s->num_q_heads <= 0 || s->block_tokens <= 0 || s->num_blocks <= 0 || s->max_blocks_per_seq <= 0 || B <= 0 || n <= 0)
     return LYNX_ERR_SHAPE;
   const int64_t cap = (int64_t)s->max_blocks_per_seq * s->block_tokens;
-  if (s->head_dim != LYNX_D || s->num_kv_heads != kGroups || s->block_tokens % 16 || n > 64 || s->num_q_heads > 128 || cap >= (1ll << 30)) return LYNX_ERR_UNSUPPORTED;
+  if (s->head_dim != LYNX_D || s->num_kv_heads != kGroups || s->block_tokens % 16 || n > 64 || s->num_q_heads > 128 || cap >= (1ll << 30) ||
+      (int64_t)s->num_blocks * kGroups * s->block_tokens >= (1ll << 31))
+    return LYNX_ERR_UNSUPPORTED;
   pl->R = n * s->num_q_heads;
   pl->RT = (pl->R + kMaxRows - 1) / kMaxRows;
   pl->NR = pl->R <= 16 ? 16 : pl->R <= 32 ? 32 : 64;
@@ -1013,7 +1150,6 @@ extern "C" lynx_status lynx_latent_attention(const lynx_shape* shape, const void
   p.bt = shape->block_tokens; p.num_blocks = shape->num_blocks; p.max_blocks = shape->max_blocks_per_seq;
   p.causal = causal ? 1 : 0; p.out_f32 = out_float ? 1 : 0;
   p.whole = pl.whole; p.per_seg = pl.per_seg;
-  p.wide = at(C.anchor, 32) && at(C.residual, 32) && at(rope_pages, 32) ? 1 : 0;
   p.bt_div = block_div(p.bt);
   const lynx_status st = pl.NR == 16 ? launch_latent<16>(p, pl.grid, stream) : pl.NR == 32 ? launch_latent<32>(p, pl.grid, stream) : launch_latent<64>(p, pl.grid, stream);
   if (st != LYNX_OK || pl.whole) return st;

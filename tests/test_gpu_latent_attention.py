@@ -1,13 +1,14 @@
 """Attention over quantised latents against 64 bits, on the planes' exact values.
 
-Bounds, with half steps u16 = 2^-12 (FP16, 11 bits: 2^-11 / 2 of a value on either side is 2^-12 of its binade's top, 2^-11 at most of the value itself) -- taken
-as u = 2^-11 throughout -- and u32 = 2^-24.
-Scores: each key channel off by u of itself at most, q exact: |ds| <= u a sum_d |q_d v_d| (latent channels alone), plus FP32 accumulation of 576 terms, truncating:
-2^-23 * 576 < 2^-13 of a sum |q k| over all channels, and the few FP32 operations behind it.  With D = a (u + 2^-13) sum_d |q_d k_d|, the largest over the tokens
-that a row sees, a weight is off by a factor e^+-D, and weight over sum by 2 D (1 + D) at most.
-Weights: u of themselves in the numerator; values: u of themselves.  Sums of the second product: 2^-13 of sum p |v| (as above, per 128 tokens, and FP32 adding from tile to tile:
-tokens / 128 * 2^-24).  So |out - want| <= (2 D + D^2 2 + 2 u + 2^-12 + tokens 2^-31) sum p |v|, and half a step of the output's type.  Weights below FP16's range:
-2^-28 of the row's largest 2^e p, tokens * 2^-28 * 2^15 relative to the accumulator's ... covered by tokens * 2^-26 max |v|.
+Bounds, with U = 2^-11, FP16's eps / 2, and 2^-24 of FP32.
+Values: a row's scale and middle (zero + 128 scale) are rounded to FP16, then middle + scale (code - 128): U (|middle| + |code - 128| scale) + U |value|, at
+most 2 U M with M = |middle| + 128 scale, which no channel of the row exceeds.
+Scores: |ds| <= a sum_d |q_d| (2 U M_d) over the latent's channels (queries are exact), plus the accumulation of 576 terms, truncating: 2^-23 * 576 < 2^-13 of a sum of
+|q| M and |q_r k_r|, and the few FP32 operations behind it.  With D the largest of that over the tokens that a row sees, a weight is off by a factor e^+-D, and weight over
+sum by 2 D (1 + D) at most.
+Outputs: weights are rounded (U), values as above, the second product's sums truncate (2^-13 of sum p |v|, as above, per 128 tokens, and FP32 from tile to tile: tokens / 128 *
+2^-24), so |out - want| <= (2 D + 2 D^2 + 3 U + 2^-12 + tokens 2^-31) sum p M, and half a step of the output's type.  Weights below FP16's range are 2^-28 of the row's largest
+2^e p, an absolute 2^-25 of it: covered by tokens * 2^-26 max M.
 Log-sum-exps: D, and 2^-20 of 1 + |lse|."""
 import pytest
 import torch
@@ -51,14 +52,15 @@ class Cache:
         self.d_table, self.d_lens = self.table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
 
     def rows(self, b, anchor):
-        """float64 latents [tokens][512] and rotary keys [tokens][64] of sequence b, on the GPU."""
+        """float64 latents [tokens][512], the most that a channel of their rows can be, and rotary keys [tokens][64] of sequence b, on the GPU."""
         t = torch.arange(self.lens[b])
         blk, off = self.table[b, t // self.bt].long().cuda(), (t % self.bt).cuda()
         code = lynx.recombine(self.planes)[0][blk, :, off].double()
         if anchor:
             code = torch.floor(code / 16) * 16 + 8
         meta = self.planes.meta[blk, :, off].double()
-        return (meta[..., 1:] + meta[..., :1] * code).flatten(1), self.pages[blk, off].double()
+        size = (meta[..., 1:] + 128 * meta[..., :1]).abs() + 128 * meta[..., :1]
+        return (meta[..., 1:] + meta[..., :1] * code).flatten(1), size.expand(-1, -1, 128).flatten(1), self.pages[blk, off].double()
 
 
 def _queries(B, n, H, seed, spread=1.0):
@@ -74,19 +76,19 @@ def _check(cache, q, qr, out, lse, causal, anchor, scale=0.0, skip=()):
     for b, L in enumerate(cache.lens):
         if b in skip:
             continue
-        latents, keys = cache.rows(b, anchor)
+        latents, sizes, keys = cache.rows(b, anchor)
         for j in range(n):
             count = max(0, L - n + j + 1) if causal else L
             got, gl = out[b, j].double(), None if lse is None else lse[b, j].double()
             if count == 0:
                 assert (got == 0).all() and (gl is None or (gl == -float("inf")).all())
                 continue
-            v, x, y = latents[:count], q[b, j].double(), qr[b, j].double()
+            v, size, x, y = latents[:count], sizes[:count], q[b, j].double(), qr[b, j].double()
             s = a * (x @ v.T + y @ keys[:count].T)
             w = s.softmax(1)
-            want, size = w @ v, w @ v.abs()
-            D = a * ((U + 2.0 ** -13) * (x.abs() @ v.abs().T) + 2.0 ** -13 * (y.abs() @ keys[:count].abs().T)).amax(1, keepdim=True)
-            bound = (2 * D + 2 * D * D + 2 * U + 2.0 ** -12 + count * 2.0 ** -31) * size + count * 2.0 ** -26 * v.abs().max() + step * want.abs()
+            want = w @ v
+            D = a * ((2 * U + 2.0 ** -13) * (x.abs() @ size.T) + 2.0 ** -13 * (y.abs() @ keys[:count].abs().T)).amax(1, keepdim=True)
+            bound = (2 * D + 2 * D * D + 3 * U + 2.0 ** -12 + count * 2.0 ** -31) * (w @ size) + count * 2.0 ** -26 * size.max() + step * want.abs()
             assert ((got - want).abs() <= bound).all(), (b, j, float(((got - want).abs() / bound).max()))
             if gl is not None:
                 l = s.logsumexp(1)
