@@ -18,7 +18,7 @@
 //   warps 8-23       codes to FP16, two sets of eight, in turn 128 channels each: a thread has 32 of two tokens, loaded a group ahead into registers; a piece's
 //                    queries
 //   warps 24, 25     issue every tcgen05.mma: scores, weights times values
-//   warp 26          the tokens' powers of two
+//   warp 26          the tiles' powers of two
 //   warp 27          deals out the pieces
 // The tile's values have one place in shared memory (128 KB, beside queries of 72): a group's 128 channels go there, and to tensor memory as keys, when the
 // same channels of the tile before have been multiplied, so that the products of a tile, the expansion of the next one and its scores follow one another
@@ -73,7 +73,7 @@ template <int NR>
 struct Cfg {
   static constexpr int kPRow = 2 * NR, kPLayout = NR == 16 ? 6 : NR == 32 ? 4 : 2;   // bytes of a token's weights; the descriptor's swizzle of such rows
   static constexpr int kOffV = 0, kOffQ = 131072, kOffP = kOffQ + 9 * NR * 128, kOffFac = kOffP + kTile * kPRow;   // values [8 x 64 channels][128 tokens][128 B]
-  static constexpr int kOffRq = kOffFac + kFac * kTile * 8;          // [kFac][128] {2^e, e}; [2][NR] factors of the rows' scores, tokens they see
+  static constexpr int kOffRq = kOffFac + 16;                        // [kFac] exponents; [2][NR] factors of the rows' scores, tokens they see
   static constexpr int kOffLim = kOffRq + 2 * NR * 4, kOffScale = kOffLim + 2 * NR * 4, kOffRef = kOffScale + NR * 4, kOffFinal = kOffRef + NR * 4;   // [NR] each
   static constexpr int kOffSum = kOffFinal + NR * 4, kOffMax = kOffSum + 4 * NR * 4;                                  // [4][NR]
   static constexpr int kOffItems = kOffMax + 4 * NR * 4, kOffMisc = kOffItems + 2 * 32, kOffBars = kOffMisc + 64;
@@ -438,12 +438,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       wait(qready + qi * 8, (ic >> 1) & 1, ab);
       // (factors and references of pairs of rows stay in shared memory, for want of registers)
       const uint64_t* const rq = reinterpret_cast<const uint64_t*>(rq_s + qi * NR + col0);
-      uint64_t* const ref = reinterpret_cast<uint64_t*>(ref_s + col0);
+      uint64_t* const minus = reinterpret_cast<uint64_t*>(ref_s + col0);   // (references with the opposite sign)
       uint64_t l[NJ];
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         l[j] = 0ull;
-        if (w4 == 0 && lane < 4) ref[4 * j] = 0ull;
+        if (w4 == 0 && lane < 4) minus[4 * j] = 0ull;
       }
       const int id = 1 + wg;
       named_bar(id, 128);
@@ -453,20 +453,17 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         wait(fready + fr.i * 8, fr.ph, ab);
         wait(sfull, gt & 1, ab);
         tc_fence_after();
-        const float2* fac = reinterpret_cast<const float2*>(smem + C::kOffFac) + fr.i * kTile + tok0;
+        const int e = reinterpret_cast<volatile int*>(smem + C::kOffFac)[fr.i];
+        const uint64_t e2 = f2_pack((float)e, (float)e), factor = f2_pack(pow2(e), pow2(e));
         const uint32_t tm_s = tmem0 + C::kTmS + wg * NC + lanes;
         const int first = (u0 + u) * kTile;
         // Scores of this thread's tokens tok0 + 16 h, + 8 and all its pairs of rows, less their references
         auto scores = [&](int h, const uint32_t* s, uint64_t (&x)[2][NJ]) {
-          float2 f[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) f[i] = fac[16 * h + 8 * i];
 #pragma unroll
           for (int j = 0; j < NJ; ++j) {
-            const uint64_t q = rq[4 * j], minus = ref[4 * j] ^ 0x8000000080000000ull;
+            const uint64_t q = f2_mul(rq[4 * j], factor), less = f2_add(e2, minus[4 * j]);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-              x[i][j] = f2_fma(u2_pack(s[4 * j + 2 * i], s[4 * j + 2 * i + 1]), f2_mul(f2_pack(f[i].x, f[i].x), q), f2_add(f2_pack(f[i].y, f[i].y), minus));
+            for (int i = 0; i < 2; ++i) x[i][j] = f2_fma(u2_pack(s[4 * j + 2 * i], s[4 * j + 2 * i + 1]), q, less);
           }
           if (__builtin_expect(first + kTile > clear, 0)) {   // a mask: the sequence's end, and what lies behind a row's position
             const int2* const lim = reinterpret_cast<const int2*>(smem + C::kOffLim) + (qi * NR + col0) / 2;
@@ -483,6 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
             }
           }
         };
+        const uint64_t back = f2_pack(pow2(-e), pow2(-e));
         bool anew = u == 0;   // references are to be set, or raised
         uint32_t w[4][NJ];
         uint64_t sum[NJ];
@@ -527,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
                 const int c = col0 + 8 * (j >> 1) + (j & 1);
                 const float M = fmaxf(fmaxf(max_s[c], max_s[NR + c]), fmaxf(max_s[2 * NR + c], max_s[3 * NR + c]));   // (less the reference)
                 const float more = (u == 0 ? M > -INFINITY : M > kRaise) ? M - kTop : 0.0f, f = u == 0 ? 1.0f : ex2(-more);
-                ref_s[c] += more;
+                ref_s[c] -= more;
                 scale_s[c] = f;
                 rescale = rescale || f != 1.0f;
               }
@@ -560,15 +558,13 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
             scores(h, s, x);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const uint32_t back = 0x7F000000u - __float_as_uint(fac[16 * h + 8 * i].x);   // 2^-e
-              const uint64_t b2 = u2_pack(back, back);
 #pragma unroll
               for (int j = 0; j < NJ; ++j) {
                 float a, c;
                 f2_unpack(x[i][j], a, c);
                 a = ex2(a);
                 c = ex2(c);
-                sum[j] = f2_fma(f2_pack(a, c), b2, sum[j]);
+                sum[j] = f2_add(f2_pack(a, c), sum[j]);
                 v[2 * h + i][j] = pack_f16x2(a, c);
                 asm("max.u16x2 %0, %0, %1;" : "+r"(most) : "r"(v[2 * h + i][j]));
               }
@@ -583,7 +579,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
           anew = true;
         }
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) l[j] = f2_add(l[j], sum[j]);
+        for (int j = 0; j < NJ; ++j) l[j] = f2_fma(sum[j], back, l[j]);
         if (gt > 0) wait(odone, (gt - 1) & 1, ab);   // the weights before have been used
         if constexpr (NJ == 1) {
           stm_x4(p_row + (uint32_t)((wg ^ swz) << 4), w[0][0], w[1][0], w[2][0], w[3][0]);
@@ -619,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             sum_s[w4 * NR + col0 + 8 * j + k] = s[k];
-            if (w4 == 0) final_s[col0 + 8 * j + k] = ref_s[col0 + 8 * j + k];   // (ref_s may be the next piece's while it is read)
+            if (w4 == 0) final_s[col0 + 8 * j + k] = -ref_s[col0 + 8 * j + k];   // (ref_s may be the next piece's while it is read)
           }
         }
       }
@@ -767,13 +763,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       for (int u = 0; u < n; ++u, ++gt, fr.next(kFac)) {
         const bool more = u + 1 < n;
         wait(fready + fr.i * 8, fr.ph, ab);
-        float back[2];     // 2^-e, of a token behind the sequence's end (whose rows may be anything) 0
-        bool live[2];
+        const float back = pow2(-reinterpret_cast<volatile int*>(smem + C::kOffFac)[fr.i]);
+        bool live[2];      // (what lies behind the sequence's end may be anything)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          live[i] = (u0 + u) * kTile + tok + 8 * i < len;
-          back[i] = pow2(-(int)reinterpret_cast<const float2*>(smem + C::kOffFac)[fr.i * kTile + tok + 8 * i].y);
-        }
+        for (int i = 0; i < 2; ++i) live[i] = (u0 + u) * kTile + tok + 8 * i < len;
         __syncwarp();
         if (lane == 0) mbar_arrive(ffree + fr.i * 8);
         Ring k = kp;   // the place at hand
@@ -788,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
           uint32_t o[8];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const uint32_t f2 = live[i] ? (__float_as_uint(back[i]) >> 16) * 0x10001u : 0u, w[4] = {key[i].x, key[i].y, key[i].z, key[i].w};
+            const uint32_t f2 = (__float_as_uint(back) >> 16) * 0x10001u, w[4] = {key[i].x, key[i].y, key[i].z, key[i].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[(j >> 1) * 4 + 2 * i + (j & 1)] = live[i] ? mul_bf16x2(w[j], f2) : 0u;
           }
@@ -806,7 +799,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
           uint32_t o[32];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float s = (live[h] ? m[h][i].x : 0.0f) * back[h], mid = fmaf(128.0f, s, (live[h] ? m[h][i].y : 0.0f) * back[h]);
+            const float s = (live[h] ? m[h][i].x : 0.0f) * back, mid = fmaf(128.0f, s, (live[h] ? m[h][i].y : 0.0f) * back);
             const uint32_t s2 = pack_f16x2(s, s), m2 = pack_f16x2(mid, mid);
             const bool turn = (q4 & 2) != 0;
             const uint4 x = turn ? make_uint4(a[h].z, a[h].w, a[h].x, a[h].y) : a[h], y = turn ? make_uint4(r[h].z, r[h].w, r[h].x, r[h].y) : r[h];
@@ -941,7 +934,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
     bar_arrive(4, kDoneThreads);
     return;
   }
-  // ================================================================================== the tokens' powers of two, four tokens a lane
+  // ================================================================================== the tiles' powers of two, four tokens a lane
   {
     Ring fr;
     fr.ph = 1;   // (empty: the first waits succeed)
@@ -958,20 +951,20 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         int blk[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) blk[i] = len > 0 ? block_id(p, b, min((u0 + u) * kTile + lane + 32 * i, top)) : 0;
+        float big = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int tok = (u0 + u) * kTile + lane + 32 * i, t = min(tok, top);
           const float2* at = p.meta + (int64_t)min(max(blk[i], 0), p.num_blocks - 1) * kGroups * p.bt + (t - quotient(t, p.bt_div) * p.bt);
-          float big = 0.0f;
 #pragma unroll
           for (int g = 0; g < kGroups; ++g) {
             const float2 m = ld_dep(at + g * p.bt);
-            big = fmaxf(big, fmaxf(fabsf(m.y), fabsf(fmaf(255.0f, m.x, m.y))));
+            const float most = fabsf(fmaf(128.0f, m.x, m.y)) + 128.0f * fabsf(m.x);
+            if (tok < len && most < INFINITY) big = fmaxf(big, most);   // (what lies behind the sequence's end may be anything)
           }
-          if (tok >= len) big = 0.0f;   // (what lies behind the sequence's end may be anything)
-          const int e = min(max(exponent_of(big), kMinExp), 113);
-          reinterpret_cast<float2*>(smem + C::kOffFac)[fr.i * kTile + lane + 32 * i] = make_float2(pow2(e), (float)e);
         }
+        big = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big)));
+        if (lane == 0) reinterpret_cast<volatile int*>(smem + C::kOffFac)[fr.i] = min(max(exponent_of(big), kMinExp), 113);
         __syncwarp();
         if (lane == 0) mbar_arrive(fready + fr.i * 8);
       }
