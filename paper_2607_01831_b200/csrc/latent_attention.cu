@@ -43,8 +43,7 @@ constexpr int kPartRow = kLatent + 4;       // floats of a partial row: O[512], 
 constexpr int kThreads = 896;
 constexpr int kRegSoft = 72, kRegCodes = 80, kRegRest = 40;   // per thread; the launch has 72 for each of seven warpgroups
 static_assert(2 * kRegSoft + 4 * kRegCodes + kRegRest <= 7 * 72, "registers");
-constexpr int kFac = 3;                     // places for the powers of two of a tile's tokens
-constexpr int kPlaces = 3;                  // for keys, of a rotary part or of 128 channels: five a tile, in turn
+constexpr int kFac = 4;                     // places for the powers of two of a tile's tokens
 constexpr int kDoneThreads = 256 + 4 * 32;  // softmax, products, powers of two, pieces
 // log2 of a row's largest weight when its reference is set; of what sets it anew when another row's weight has left FP16 (65504)
 constexpr float kTop = 4.0f, kRaise = 9.0f;
@@ -72,35 +71,33 @@ struct LatentParams {
 template <int NR>
 struct Cfg {
   static constexpr int kPRow = 2 * NR, kPLayout = NR == 16 ? 6 : NR == 32 ? 4 : 2;   // bytes of a token's weights; the descriptor's swizzle of such rows
+  // Places in tensor memory: for the keys of 128 channels (a tile's groups in turn) and of the rotary part, for scores.  Few rows leave room for more.
+  static constexpr int kK = NR == 64 ? 2 : 4, kS = NR == 64 ? 1 : 2;
   static constexpr int kOffV = 0, kOffQ = 131072, kOffP = kOffQ + 9 * NR * 128, kOffFac = kOffP + kTile * kPRow;   // values [8 x 64 channels][128 tokens][128 B]
   static constexpr int kOffRq = kOffFac + 16;                        // [kFac] exponents; [2][NR] factors of the rows' scores, tokens they see
   static constexpr int kOffLim = kOffRq + 2 * NR * 4, kOffScale = kOffLim + 2 * NR * 4, kOffRef = kOffScale + NR * 4, kOffFinal = kOffRef + NR * 4;   // [NR] each
   static constexpr int kOffSum = kOffFinal + NR * 4, kOffMax = kOffSum + 4 * NR * 4;                                  // [4][NR]
   static constexpr int kOffItems = kOffMax + 4 * NR * 4, kOffMisc = kOffItems + 2 * 32, kOffBars = kOffMisc + 64;
-  static constexpr int kBars = 2 * kPlaces + 2 * 4 + 2 * kFac + 4 + 7;
+  static constexpr int kBars = 2 * kK + 2 + 2 * kGroups + 2 * kFac + 2 * kS + 2 + 7;
   static constexpr int kSmem = kOffBars + kBars * 8 + 1024;          // + alignment
   static_assert(kSmem <= 227 * 1024 && kOffP % 1024 == 0 && kOffItems % 16 == 0 && kOffBars % 8 == 0, "shared memory");
-  static constexpr int kTmO = 0, kTmS = 4 * NR, kTmK = 5 * NR;       // O^T [4][NR], scores [NR], keys [kPlaces][64]
-  static_assert(kTmK + kPlaces * 64 <= 512, "tensor memory");
+  static constexpr int kTmO = 0, kTmS = 4 * NR, kTmK = kTmS + kS * NR, kTmR = kTmK + kK * 64;   // O^T [4][NR], scores [kS][NR], keys [kK][64], rotary keys [32]
+  static_assert(kTmR + 32 <= 512, "tensor memory");
 };
 
 struct Item {  // a piece: tiles u0 .. u0 + n - 1 of segment (b, rt), none: the end
   int b, rt, len, u0, n, first_cta, n_contrib, pad;
 };
 
-// A place among several in turn, and the parity of its round.
-struct Ring {
-  int i = 0;
-  uint32_t ph = 0;
-  __device__ __forceinline__ void next(int places, int by = 1) {   // (by no more than five times as many)
-    for (i += by; i >= places; ph ^= 1) i -= places;
-  }
-};
+// The t-th use of one of N places that are used in turn, N a power of two: the place, and the parity of its round.
+template <int N>
+__device__ __forceinline__ uint32_t place_of(int t) { return (uint32_t)t & (N - 1); }
+template <int N>
+__device__ __forceinline__ uint32_t round_of(int t) { return ((uint32_t)t / N) & 1u; }
 
 // ------------------------------------------------------------------ PTX
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
-__device__ __forceinline__ void mbar_arrive2(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 2;" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
   uint32_t ok;
@@ -372,14 +369,14 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
   const PieceWait iab = {misc + 1};   // (pieces need no data to arrive and stay in step after a wait for data has given up)
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   const uint32_t bars = sbase + C::kOffBars;
-  // of a place for keys: kready, kfree; of a group of the values: vready, vfree (4); of the powers of two: fready, ffree (kFac); of a tile: sfull, sfree,
-  // pready, odone; of a piece: ifull, iempty, qready (2), qfree
-  const uint32_t kready = bars, kfree = kready + 8 * kPlaces, vready = kfree + 8 * kPlaces, vfree = vready + 32, fready = vfree + 32, ffree = fready + 8 * kFac,
-                 sfull = ffree + 8 * kFac, sfree = sfull + 8, pready = sfree + 8, odone = pready + 8, ifull = odone + 8, iempty = ifull + 16, qready = iempty + 16,
-                 qfree = qready + 16;
+  // of a place for keys: kready, kfree; for rotary keys: rready, rfree; of a group's values: vready, vfree; for the powers of two: fready, ffree; for scores: sfull, sfree; of a tile: pready, odone; of a piece:
+  // ifull, iempty, qready (2), qfree
+  const uint32_t kready = bars, kfree = kready + 8 * C::kK, rready = kfree + 8 * C::kK, rfree = rready + 8, vready = rfree + 8, vfree = vready + 32, fready = vfree + 32, ffree = fready + 8 * kFac,
+                 sfull = ffree + 8 * kFac, sfree = sfull + 8 * C::kS, pready = sfree + 8 * C::kS, odone = pready + 8, ifull = odone + 8, iempty = ifull + 16,
+                 qready = iempty + 16, qfree = qready + 16;
   if (tid == 0) {
-    for (int i = 0; i < kPlaces; ++i) {
-      mbar_init(kready + i * 8, 16);   // (rotary keys by all, 128 channels by eight warps, twice each)
+    for (int i = 0; i < C::kK; ++i) {
+      mbar_init(kready + i * 8, 8);
       mbar_init(kfree + i * 8, 1);
     }
     for (int i = 0; i < kFac; ++i) {
@@ -391,12 +388,16 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       mbar_init(iempty + i * 8, 8 + 16 + 2 + 1);   // softmax, codes, products, powers of two
       mbar_init(qready + i * 8, 16);
     }
-    for (int i = 0; i < 4; ++i) {
+    mbar_init(rready, 16);
+    mbar_init(rfree, 1);
+    for (int i = 0; i < kGroups; ++i) {
       mbar_init(vready + i * 8, 8);
       mbar_init(vfree + i * 8, 1);
     }
-    mbar_init(sfull, 1);
-    mbar_init(sfree, 8);
+    for (int i = 0; i < C::kS; ++i) {
+      mbar_init(sfull + i * 8, 1);
+      mbar_init(sfree + i * 8, 8);
+    }
     mbar_init(pready, 8);
     mbar_init(odone, 1);
     mbar_init(qfree, 1);
@@ -429,7 +430,6 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
     const int pr = lane & 7, pb = lane >> 3, swz = NR == 64 ? pr : NR == 32 ? pr >> 1 : pr >> 2;
     const uint32_t p_row = sbase + C::kOffP + (uint32_t)((32 * w4 + (NJ == 1 ? 8 * pb : 8 * (pb & 1)) + pr) * C::kPRow);
     int gt = 0;   // tiles so far
-    Ring fr;      // place of their powers of two
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
@@ -449,13 +449,14 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       named_bar(id, 128);
       const int clear = p.causal ? len - p.n + 1 : len;   // tokens that every row sees
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt, fr.next(kFac)) {
-        wait(fready + fr.i * 8, fr.ph, ab);
-        wait(sfull, gt & 1, ab);
+      for (int u = 0; u < n; ++u, ++gt) {
+        const uint32_t fi = place_of<kFac>(gt), si = place_of<C::kS>(gt);
+        wait(fready + fi * 8, round_of<kFac>(gt), ab);
+        wait(sfull + si * 8, round_of<C::kS>(gt), ab);
         tc_fence_after();
-        const int e = reinterpret_cast<volatile int*>(smem + C::kOffFac)[fr.i];
+        const int e = reinterpret_cast<volatile int*>(smem + C::kOffFac)[fi];
         const uint64_t e2 = f2_pack((float)e, (float)e), factor = f2_pack(pow2(e), pow2(e));
-        const uint32_t tm_s = tmem0 + C::kTmS + wg * NC + lanes;
+        const uint32_t tm_s = tmem0 + C::kTmS + si * NR + wg * NC + lanes;
         const int first = (u0 + u) * kTile;
         // Scores of this thread's tokens tok0 + 16 h, + 8 and all its pairs of rows, less their references
         auto scores = [&](int h, const uint32_t* s, uint64_t (&x)[2][NJ]) {
@@ -597,8 +598,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(pready);
-          mbar_arrive(sfree);
-          mbar_arrive(ffree + fr.i * 8);
+          mbar_arrive(sfree + si * 8);
+          mbar_arrive(ffree + fi * 8);
         }
       }
       // ---- end of the piece: sums over the warps, then a row's 512 channels by the lanes that hold them
@@ -677,8 +678,6 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
     const uint32_t tm_k = tmem0 + C::kTmK + ((uint32_t)lane0 << 16);
     const uint32_t v_row = sbase + C::kOffV + (uint32_t)(set * 32768 + (q4 >> 1) * 16384 + tok * 128), v_swz = (uint32_t)((((q4 & 1) * 4) ^ (q4 & 2) ^ (tok & 7)) << 4);
     int gt = 0;          // tiles so far
-    Ring kp, fr;         // places of the tile's rotary keys, of the tokens' powers of two
-    kp.ph = 1;           // (empty: the first waits for them succeed)
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
       wait(ifull + qi * 8, (ic >> 1) & 1, iab);
@@ -689,29 +688,32 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       int next_id = len > 0 ? block_id(p, b, min(u0 * kTile + tok, top)) : 0;
       uint4 a[2], r[2], key[2];    // of both tokens: codes of the set's next group, 16 bytes of the rotary key
       float2 m[2][2];              // scalars of the set's groups
-      uint32_t row[2] = {0u, 0u};  // of the loads: group set's (fewer than 2^31)
-      auto place = [&](int u) {    // where tile u's tokens lie (in one block), their scalars and rotary keys; the block after it is looked up
-        const int t = min((u0 + u) * kTile + tok, top), t8 = min((u0 + u) * kTile + tok + 8, top), blk = in_pool(p, next_id), first = quotient(t, p.bt_div) * p.bt;
-        row[0] = (uint32_t)((blk * kGroups + set) * p.bt + t - first);
-        row[1] = row[0] + (uint32_t)(t8 - t);
+      const uint4 *at_a = nullptr, *at_r = nullptr;   // of the loads: group set's codes of token tok; tok + 8 has the next 8 rows (16 tokens lie in one block)
+      const uint32_t next_group = (uint32_t)(2 * p.bt);   // rows from there to group set + 2
+      auto place = [&](int u) {    // where tile u's tokens lie, their scalars and rotary keys; the block after theirs is looked up.  (Behind the sequence's end some row of its last block.)
+        const int t = (u0 + u) * kTile + tok, blk = in_pool(p, next_id), off = t - quotient(t, p.bt_div) * p.bt;
+        const int64_t row = (int64_t)(blk * kGroups + set) * p.bt + off;
+        at_a = reinterpret_cast<const uint4*>(p.anchor) + row * 4 + q4;
+        if (FULL) at_r = reinterpret_cast<const uint4*>(p.residual) + row * 4 + q4;
+        const float2* const at_m = p.meta + row;
+        const uint4* const at_k = p.pages + (int64_t)(blk * p.bt + off) * 8 + set * 4 + q4;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          m[i][0] = ld_dep(p.meta + row[i]);
-          m[i][1] = ld_dep(p.meta + row[i] + 2 * p.bt);
-          key[i] = ld_dep(p.pages + (int64_t)(blk * p.bt + (i ? t8 : t) - first) * 8 + set * 4 + q4);
+          key[i] = ld_dep(at_k + 64 * i);
+          m[i][0] = ld_dep(at_m + 8 * i);
+          m[i][1] = ld_dep(at_m + next_group + 8 * i);
         }
         if (u + 1 < n) next_id = block_id(p, b, min(t + kTile, top));
       };
-      auto load_codes = [&](int i) {   // of group set + 2 i
+      auto load_codes = [&](uint32_t rows) {   // (rows: from the first group's)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const int64_t at = (int64_t)(row[k] + (uint32_t)(2 * i * p.bt)) * 4 + q4;
-          a[k] = ld_dep(reinterpret_cast<const uint4*>(p.anchor) + at);
-          if (FULL) r[k] = ld_dep(reinterpret_cast<const uint4*>(p.residual) + at);
+          a[k] = ld_dep(at_a + rows * 4u + 32 * k);
+          if (FULL) r[k] = ld_dep(at_r + rows * 4u + 32 * k);
         }
       };
       place(0);
-      load_codes(0);
+      load_codes(0u);
       if (ic > 0) wait(qfree, (ic - 1) & 1, ab);
       {   // queries: a row by TPR threads, chunks of 8 channels, 16 at a time
         constexpr int TPR = 512 / NR, kMine = 64 / TPR;
@@ -760,17 +762,16 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         if (lane == 0) mbar_arrive(qready + qi * 8);
       }
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, ++gt, fr.next(kFac)) {
+      for (int u = 0; u < n; ++u, ++gt) {
         const bool more = u + 1 < n;
-        wait(fready + fr.i * 8, fr.ph, ab);
-        const float back = pow2(-reinterpret_cast<volatile int*>(smem + C::kOffFac)[fr.i]);
+        const uint32_t fi = place_of<kFac>(gt);
+        wait(fready + fi * 8, round_of<kFac>(gt), ab);
+        const float back = pow2(-reinterpret_cast<volatile int*>(smem + C::kOffFac)[fi]);
         bool live[2];      // (what lies behind the sequence's end may be anything)
 #pragma unroll
         for (int i = 0; i < 2; ++i) live[i] = (u0 + u) * kTile + tok + 8 * i < len;
         __syncwarp();
-        if (lane == 0) mbar_arrive(ffree + fr.i * 8);
-        Ring k = kp;   // the place at hand
-        kp.next(kPlaces, 5);
+        if (lane == 0) mbar_arrive(ffree + fi * 8);
         auto keys_there = [&]() {
           tc_wait_st();
           tc_fence_before();
@@ -785,17 +786,15 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[(j >> 1) * 4 + 2 * i + (j & 1)] = live[i] ? mul_bf16x2(w[j], f2) : 0u;
           }
-          wait(kfree + k.i * 8, k.ph, ab);
+          if (gt > 0) wait(rfree, (gt - 1) & 1, ab);
           tc_fence_after();
-          st_16x256(tm_k + k.i * 64 + set * 16, o);
+          st_16x256(tm_k + (C::kTmR - C::kTmK) + set * 16, o);
           keys_there();
-          if (lane == 0) mbar_arrive(kready + k.i * 8);
+          if (lane == 0) mbar_arrive(rready);
         }
-        k.next(kPlaces, 1 + set);
         // ---- 128 channels at a time, ready before their places are
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int g = set + 2 * i;
           uint32_t o[32];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -814,27 +813,28 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
               o[8 * w + 4 + 2 * h + 1] = v[3];
             }
           }
-          if (i == 0) load_codes(1);
-          wait(kfree + k.i * 8, k.ph, ab);
+          if (i == 0) load_codes(next_group);
+          const int g = set + 2 * i, use = gt * kGroups + g;   // (of the places for keys)
+          const uint32_t ki = place_of<C::kK>(use);
+          if (use >= C::kK) wait(kfree + ki * 8, round_of<C::kK>(use) ^ 1u, ab);
           tc_fence_after();
-          st_16x256(tm_k + k.i * 64, o);
+          st_16x256(tm_k + ki * 64, o);
+          keys_there();      // (before the values: their scores can begin while the tile before is multiplied)
+          if (lane == 0) mbar_arrive(kready + ki * 8);
           if (gt > 0) wait(vfree + g * 8, (gt - 1) & 1, ab);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int w = 0; w < 4; ++w)
-              sts128((v_row + (uint32_t)(i * 65536 + h * 1024)) + (v_swz ^ (uint32_t)(w << 4)), o[8 * w + 2 * h], o[8 * w + 2 * h + 1], o[8 * w + 4 + 2 * h], o[8 * w + 5 + 2 * h]);
+              sts128((v_row + (uint32_t)(i * 65536 + h * 1024)) + (v_swz ^ (uint32_t)(w << 4)), o[8 * w + 2 * h], o[8 * w + 2 * h + 1], o[8 * w + 4 + 2 * h],
+                     o[8 * w + 5 + 2 * h]);
           }
-          keys_there();
-          if (lane == 0) {
-            mbar_arrive2(kready + k.i * 8);
-            mbar_arrive(vready + g * 8);
-          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(vready + g * 8);
           if (i == 1 && more) {   // (behind the hand-over: loads wait for room in the queue of those under way, which these fill)
             place(u + 1);
-            load_codes(0);
+            load_codes(0u);
           }
-          k.next(kPlaces, 2);
         }
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
@@ -847,7 +847,6 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
     constexpr uint32_t kHi = desc_hi(128u, 2u);
     const bool scores = warp == 24;
     int gt = 0;   // tiles so far
-    Ring kp;      // place of the next keys
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
@@ -856,30 +855,35 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       if (n == 0) break;
       if (scores) {
         constexpr uint32_t kIdesc = tc_idesc(NR, false);
-        const uint32_t q_lo = desc_lo(sbase + C::kOffQ, 16u), d = tmem0 + C::kTmS;
+        const uint32_t q_lo = desc_lo(sbase + C::kOffQ, 16u);
         wait(qready + qi * 8, (ic >> 1) & 1, ab);
 #pragma unroll 1
         for (int u = 0; u < n; ++u, ++gt) {
-          if (gt > 0) wait(sfree, (gt - 1) & 1, ab);
+          const uint32_t si = place_of<C::kS>(gt), d = tmem0 + C::kTmS + si * NR;
+          if (gt >= C::kS) wait(sfree + si * 8, round_of<C::kS>(gt) ^ 1u, ab);
           // The rotary keys', then of 128 channels at a time; the last of a tile makes its scores full, the last of a piece gives up the queries
+          wait(rready, gt & 1, ab);
+          tc_fence_after();
+          if (tc_elect()) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              tc_mma_ts(d, tmem0 + C::kTmR + ks * 8, desc(q_lo + (uint32_t)((8 * NR * 128 + ks * 32) >> 4), kHi), kIdesc | kBf16Operands, ks > 0 ? 1u : 0u);
+            tc_commit(rfree);
+          }
+          __syncwarp();
 #pragma unroll 1
-          for (int g = -1; g < kGroups; ++g, kp.next(kPlaces)) {
-            wait(kready + kp.i * 8, kp.ph, ab);
+          for (int g = 0; g < kGroups; ++g) {
+            const int use = gt * kGroups + g;
+            const uint32_t ki = place_of<C::kK>(use);
+            wait(kready + ki * 8, round_of<C::kK>(use), ab);
             tc_fence_after();
             if (tc_elect()) {
-              const uint32_t a = tmem0 + C::kTmK + kp.i * 64;
-              if (g < 0) {
+              const uint32_t a = tmem0 + C::kTmK + ki * 64, q = q_lo + (uint32_t)((2 * g * NR * 128) >> 4);
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                  tc_mma_ts(d, a + ks * 8, desc(q_lo + (uint32_t)((8 * NR * 128 + ks * 32) >> 4), kHi), kIdesc | kBf16Operands, ks > 0 ? 1u : 0u);
-              } else {
-                const uint32_t q = q_lo + (uint32_t)((2 * g * NR * 128) >> 4);
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                  tc_mma_ts(d, a + ks * 8, desc(q + (uint32_t)(((ks >> 2) * NR * 128 + (ks & 3) * 32) >> 4), kHi), kIdesc, 1u);
-              }
-              tc_commit(kfree + kp.i * 8);
-              if (g == kGroups - 1) tc_commit(sfull);
+              for (int ks = 0; ks < 8; ++ks)
+                tc_mma_ts(d, a + ks * 8, desc(q + (uint32_t)(((ks >> 2) * NR * 128 + (ks & 3) * 32) >> 4), kHi), kIdesc, 1u);
+              tc_commit(kfree + ki * 8);
+              if (g == kGroups - 1) tc_commit(sfull + si * 8);
               if (g == kGroups - 1 && u == n - 1) tc_commit(qfree);
             }
             __syncwarp();
@@ -899,10 +903,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
           if (tc_elect()) {
 #pragma unroll 1
             for (int g = 0; g < kGroups; ++g) {
-              const uint32_t v = v_lo + (uint32_t)((g * 32768) >> 4), d = tmem0 + C::kTmO + g * NR;
+              const uint32_t x = v_lo + (uint32_t)((g * 32768) >> 4), d = tmem0 + C::kTmO + g * NR;
 #pragma unroll
               for (int ks = 0; ks < 8; ++ks)
-                tc_mma_ss(d, desc(v + ks * 128u, kHi), desc(p_lo + (uint32_t)((ks * 16 * C::kPRow) >> 4), kPHi), kIdesc, ks > 0 || u > 0 ? 1u : 0u);
+                tc_mma_ss(d, desc(x + ks * 128u, kHi), desc(p_lo + (uint32_t)((ks * 16 * C::kPRow) >> 4), kPHi), kIdesc, ks > 0 || u > 0 ? 1u : 0u);
               tc_commit(vfree + g * 8);
             }
             tc_commit(odone);
@@ -936,8 +940,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
   }
   // ================================================================================== the tiles' powers of two, four tokens a lane
   {
-    Ring fr;
-    fr.ph = 1;   // (empty: the first waits succeed)
+    int gt = 0;
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
@@ -946,8 +949,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       if (n == 0) break;
       const int top = max(len - 1, 0);
 #pragma unroll 1
-      for (int u = 0; u < n; ++u, fr.next(kFac)) {
-        wait(ffree + fr.i * 8, fr.ph, ab);
+      for (int u = 0; u < n; ++u, ++gt) {
+        const uint32_t fi = place_of<kFac>(gt);
+        if (gt >= kFac) wait(ffree + fi * 8, round_of<kFac>(gt) ^ 1u, ab);
         int blk[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) blk[i] = len > 0 ? block_id(p, b, min((u0 + u) * kTile + lane + 32 * i, top)) : 0;
@@ -964,9 +968,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
           }
         }
         big = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big)));
-        if (lane == 0) reinterpret_cast<volatile int*>(smem + C::kOffFac)[fr.i] = min(max(exponent_of(big), kMinExp), 113);
+        if (lane == 0) reinterpret_cast<volatile int*>(smem + C::kOffFac)[fi] = min(max(exponent_of(big), kMinExp), 113);
         __syncwarp();
-        if (lane == 0) mbar_arrive(fready + fr.i * 8);
+        if (lane == 0) mbar_arrive(fready + fi * 8);
       }
       if (lane == 0) mbar_arrive(iempty + qi * 8);
     }
