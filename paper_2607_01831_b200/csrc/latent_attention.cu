@@ -244,11 +244,18 @@ __device__ __forceinline__ void values8(uint32_t xa, uint32_t xr, uint32_t scale
 // Where channels lie in the contraction of the scores.  Four threads load a token's 64 bytes of a row, 16 each (a warp 8 tokens at a time, 512 bytes), and
 // write what they hold into tensor memory in the accumulator layout of the warp-level products: thread q's channel pairs 2 j, 2 j + 1 are columns 8 j + 2 q, + 1, that
 // is positions 16 j + 4 q .. + 3.  (A thread a token and 32 bytes a load, whose 32 sectors lie in as many lines: 374 instead of 296 us for 128 rows and 16 sequences of 32768
-// tokens.)  q = 2, 3 take their words in the order 2 3 0 1, so that the stores of the values meet in no bank.
+// tokens.)
 __host__ __device__ constexpr int position_of(int chunk) {   // of the first four of 8 channels, chunk 0..15 of a group; the others are 16 further on
-  return 32 * ((chunk & 3) ^ ((chunk >> 3) << 1)) + 4 * (chunk >> 2);
+  return 32 * (chunk & 3) + 4 * (chunk >> 2);
 }
 __host__ __device__ constexpr int rope_position_of(int chunk) { return 32 * (chunk >> 2) + 4 * (chunk & 3); }   // likewise, chunk 0..7 of a rotary key
+
+// Where they lie in the values, from which the outputs have it: 8 bytes a store, two registers that lie side by side there, too (16 bytes, whose registers do not, cost as
+// many moves), thread q's j-th at chunk (j & 3) + 4 (q >> 1) of 16 bytes, half q & 1, of 64 channels j >> 2: the 16 threads of a store's phase meet in no bank.
+__host__ __device__ constexpr int channel_at(int d) {   // of position d of 128
+  const int j = 4 * (d >> 6) + ((d >> 3) & 3), q = ((d >> 4) & 2) + ((d >> 2) & 1);
+  return 32 * q + 8 * (j >> 1) + (((d & 1) << 2) | (d & 2) | (j & 1));
+}
 
 // ------------------------------------------------------------------ the cut
 struct Cursor {   // where a CTA's range begins, and how much of it there is
@@ -630,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       float* const part = p.part + (int64_t)(segment + (int)blockIdx.x) * NR * kPartRow;
 #pragma unroll 1
       for (int i = 0; i < 2 * NR; i += 8) {
-        const int g = 2 * wg + i / NR, c0 = i % NR, d = g * 128 + w4 * 32 + (lane & 24) + ((lane & 1) << 2 | (lane & 2) | (lane & 4) >> 2);   // (see values8)
+        const int g = 2 * wg + i / NR, c0 = i % NR, d = g * 128 + channel_at(w4 * 32 + lane);
         if (c0 >= rows) continue;
         uint32_t o[8];
         TmemRegs<8>::ld(tmem0 + C::kTmO + g * NR + c0 + lanes, o);
@@ -676,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
     reg_inc<kRegCodes>();
     const int set = (warp - 8) >> 3, q4 = lane & 3, lane0 = (warp & 3) * 32 + ((warp >> 2) & 1) * 16, tok = lane0 + (lane >> 2);   // tokens tok, tok + 8 of a tile
     const uint32_t tm_k = tmem0 + C::kTmK + ((uint32_t)lane0 << 16);
-    const uint32_t v_row = sbase + C::kOffV + (uint32_t)(set * 32768 + (q4 >> 1) * 16384 + tok * 128), v_swz = (uint32_t)((((q4 & 1) * 4) ^ (q4 & 2) ^ (tok & 7)) << 4);
+    const uint32_t v_row = sbase + C::kOffV + (uint32_t)(set * 32768 + tok * 128 + (q4 & 1) * 8), v_swz = (uint32_t)((((q4 >> 1) * 4) ^ (tok & 7)) << 4);
     int gt = 0;          // tiles so far
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
@@ -800,9 +807,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
           for (int h = 0; h < 2; ++h) {
             const float s = (live[h] ? m[h][i].x : 0.0f) * back, mid = fmaf(128.0f, s, (live[h] ? m[h][i].y : 0.0f) * back);
             const uint32_t s2 = pack_f16x2(s, s), m2 = pack_f16x2(mid, mid);
-            const bool turn = (q4 & 2) != 0;
-            const uint4 x = turn ? make_uint4(a[h].z, a[h].w, a[h].x, a[h].y) : a[h], y = turn ? make_uint4(r[h].z, r[h].w, r[h].x, r[h].y) : r[h];
-            const uint32_t wa[4] = {x.x, x.y, x.z, x.w}, wr[4] = {y.x, y.y, y.z, y.w};
+            const uint32_t wa[4] = {a[h].x, a[h].y, a[h].z, a[h].w}, wr[4] = {r[h].x, r[h].y, r[h].z, r[h].w};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
               uint32_t v[4];
@@ -823,11 +828,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
           if (lane == 0) mbar_arrive(kready + ki * 8);
           if (gt > 0) wait(vfree + g * 8, (gt - 1) & 1, ab);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
+          for (int j = 0; j < 8; ++j) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-              sts128((v_row + (uint32_t)(i * 65536 + h * 1024)) + (v_swz ^ (uint32_t)(w << 4)), o[8 * w + 2 * h], o[8 * w + 2 * h + 1], o[8 * w + 4 + 2 * h],
-                     o[8 * w + 5 + 2 * h]);
+            for (int h = 0; h < 2; ++h)
+              sts64((v_row + (uint32_t)(i * 65536 + h * 1024 + (j >> 2) * 16384)) + (v_swz ^ (uint32_t)((j & 3) << 4)), o[4 * j + 2 * h], o[4 * j + 2 * h + 1]);
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(vready + g * 8);
