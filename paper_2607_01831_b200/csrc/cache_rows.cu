@@ -90,7 +90,7 @@ struct AppendParams {
 // cost more registers than they hide (149 and 185, 152 and 209), a fifth CTA per SM 144 and 197.  Two turned rows in FP32 and their angles are too many
 // for the 64 registers that four CTAs leave: 60 bytes a thread are spilled (-Xptxas -v), which the rotated keys' time includes.
 template <int kFly, bool TURN, bool NORM>
-__device__ __forceinline__ void append_rows(const RotaryParams& r, const NormParams& norm, const AppendParams& p, int64_t row, int64_t slot, int v, int l, int first, int last) {
+__device__ __forceinline__ void append_rows(const RotaryParams& r, float eps, const float4* weight_s, const AppendParams& p, int64_t row, int64_t slot, int v, int l, int first, int last) {
   static_assert(kFly == 1 || kFly == 2 || kFly == 4, "a division per lane");
   const bool turns = TURN && 8 * l < r.n_pairs, have = row >= 0 && row < p.n_src;
   int c0 = 2 * l, c1 = 2 * l + 1;
@@ -126,9 +126,7 @@ __device__ __forceinline__ void append_rows(const RotaryParams& r, const NormPar
         unpack8(a[u], y[u]);
         unpack8(b[u], y[u] + 8);
         if constexpr (NORM) {
-          float w[16];
-          load_weights(norm, c0, c1, w);
-          norm16<LYNX_D>(y[u], w, norm.eps);
+          norm16<LYNX_D>(y[u], weight_s, c0, c1, eps);
         }
         if (turns) turn16(y[u], t, r.interleaved);
         range[u] = row_range(y[u]);
@@ -171,9 +169,14 @@ __device__ __forceinline__ void append_rows(const RotaryParams& r, const NormPar
   }
 }
 template <int kFly, bool NORM>
-__global__ void __launch_bounds__(kThreads, NORM ? 3 : 4) cache_append_kernel(const __grid_constant__ RotaryParams r, const __grid_constant__ NormParams norm,
+__global__ void __launch_bounds__(kThreads, 4) cache_append_kernel(const __grid_constant__ RotaryParams r, const __grid_constant__ NormParams norm,
                                                                   const __grid_constant__ AppendParams p, int per, int groups) {
+  __shared__ float4 weight_s[NORM ? LYNX_D / 4 : 1];
   pdl_begin();
+  if constexpr (NORM) {
+    if (threadIdx.x < LYNX_D / 8) stage_weights8(norm, threadIdx.x, weight_s);
+    __syncthreads();
+  }
   const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31, l = lane & 7;
   const int64_t quad = w / (2 * groups), token = quad * 4 + (lane >> 3);
@@ -184,8 +187,8 @@ __global__ void __launch_bounds__(kThreads, NORM ? 3 : 4) cache_append_kernel(co
     slot = ld_dep(p.slots + token);
     row = p.rows ? (int64_t)ld_dep(p.rows + token) : token;
   }
-  if ((NORM || p.rotate) && !v) append_rows<kFly, true, NORM>(r, norm, p, row, slot, v, l, first, last);
-  else append_rows<kFly, false, false>(r, norm, p, row, slot, v, l, first, last);
+  if ((NORM || p.rotate) && !v) append_rows<kFly, true, NORM>(r, norm.eps, weight_s, p, row, slot, v, l, first, last);
+  else append_rows<kFly, false, false>(r, 0.0f, weight_s, p, row, slot, v, l, first, last);
 }
 
 // ------------------------------------------------------------------ out of the planes
@@ -317,8 +320,7 @@ static lynx_status cache_append(const lynx_shape* shape, const void* k, int64_t 
   unsigned grid;
   if (!grid_of((n_tokens + 3) / 4 * 2 * groups, &grid)) return LYNX_ERR_UNSUPPORTED;
   if (n.weight)
-    return per > 1 ? launch_pdl(cache_append_kernel<2, true>, grid, kThreads, 0, stream, r, n, p, per, groups)
-                   : launch_pdl(cache_append_kernel<1, true>, grid, kThreads, 0, stream, r, n, p, per, groups);
+    return launch_pdl(cache_append_kernel<1, true>, grid, kThreads, 0, stream, r, n, p, per, groups);   // (two rows at a time spill: 99.6 us for what takes 96.8)
   return per > 1 ? launch_pdl(cache_append_kernel<2, false>, grid, kThreads, 0, stream, r, n, p, per, groups)
                  : launch_pdl(cache_append_kernel<1, false>, grid, kThreads, 0, stream, r, n, p, per, groups);
 }

@@ -104,7 +104,8 @@ __global__ void __launch_bounds__(kThreads, 3) latent_append_kernel(const __grid
     unpack8(b[u], x + 8);
     if (norm.weight) {
       float weight[16];
-      load_weights(norm, (g0 + u) * 16 + 2 * l, (g0 + u) * 16 + 2 * l + 1, weight);
+      load_weights8(norm, (g0 + u) * 16 + 2 * l, weight);
+      load_weights8(norm, (g0 + u) * 16 + 2 * l + 1, weight + 8);
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = x[i] * scale * weight[i];
     }

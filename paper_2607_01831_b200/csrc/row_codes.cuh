@@ -168,19 +168,28 @@ struct NormParams {
   int f32;
   float eps;
 };
-// Weights of the chunks c0 and c1 of 8 channels.  (Few rows of them: they come out of a cache.)
-__device__ __forceinline__ void load_weights(const NormParams& n, int c0, int c1, float* w) {
+// Eight weights, in FP32.
+__device__ __forceinline__ void load_weights8(const NormParams& n, int chunk, float* w) {
   if (n.f32) {
-    const float4* p = static_cast<const float4*>(n.weight);
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const float4 v = ld_dep(p + 2 * (h < 2 ? c0 : c1) + (h & 1));
-      w[4 * h] = v.x; w[4 * h + 1] = v.y; w[4 * h + 2] = v.z; w[4 * h + 3] = v.w;
-    }
+    const float4 lo = ld_dep(static_cast<const float4*>(n.weight) + 2 * chunk), hi = ld_dep(static_cast<const float4*>(n.weight) + 2 * chunk + 1);
+    w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w; w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
   } else {
-    unpack8(ld_dep(static_cast<const uint4*>(n.weight) + c0), w);
-    unpack8(ld_dep(static_cast<const uint4*>(n.weight) + c1), w + 8);
+    unpack8(ld_dep(static_cast<const uint4*>(n.weight) + chunk), w);
   }
+}
+// A lane's 16 values times a factor and the weights of their chunks, which lie in shared memory as FP32.
+__device__ __forceinline__ void times_weights(float* y, float scale, const float4* weight_s, int c0, int c1) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 v = weight_s[2 * (i < 2 ? c0 : c1) + (i & 1)];
+    y[4 * i] *= scale * v.x; y[4 * i + 1] *= scale * v.y; y[4 * i + 2] *= scale * v.z; y[4 * i + 3] *= scale * v.w;
+  }
+}
+__device__ __forceinline__ void stage_weights8(const NormParams& n, int chunk, float4* weight_s) {
+  float x[8];
+  load_weights8(n, chunk, x);
+  weight_s[2 * chunk] = make_float4(x[0], x[1], x[2], x[3]);
+  weight_s[2 * chunk + 1] = make_float4(x[4], x[5], x[6], x[7]);
 }
 // The sum of a lane's 16 squares over the kLanes lanes of its row.
 template <int kLanes>
@@ -194,10 +203,8 @@ __device__ __forceinline__ float sum_squares(const float* x) {
   return v;
 }
 template <int kWidth>
-__device__ __forceinline__ void norm16(float* x, const float* w, float eps) {
-  const float r = rsqrtf(fmaf(sum_squares<kWidth / 16>(x), 1.0f / kWidth, eps));
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
+__device__ __forceinline__ void norm16(float* x, const float4* weight_s, int c0, int c1, float eps) {
+  times_weights(x, rsqrtf(fmaf(sum_squares<kWidth / 16>(x), 1.0f / kWidth, eps)), weight_s, c0, c1);
 }
 
 // ------------------------------------------------------------------ out of the planes
