@@ -442,12 +442,14 @@ lynx_status lynx_latent_read(const lynx_shape* shape, lynx_plane C, const void* 
  * [0, seq_lens[b] - n_q + j + 1); one that sees no token gives zeros and a log-sum-exp of -inf.  softmax_scale 0 means 1/sqrt(192), of heads with 128 + 64
  * channels before they are absorbed.  C with its residual: the full codes; residual NULL: the Anchor's state.
  * out : [batch][n_q][Hq][512], BF16, or float where out_float is set; lse : float [batch][n_q][Hq] (natural log) or NULL.  Pointers 16-byte aligned (meta 8;
- * block_table, seq_lens, lens 4); planes and pages aligned to 32 are read faster.
+ * block_table, seq_lens, lse 4).
  * An infinity or a NaN in a query spoils that row alone, one in the scalars or the rotary key of a token the rows that see it (all of a sequence's may be NaN); what
  * lies behind a sequence's end, in blocks or in the table, is not looked at.
- * Precision: scores, statistics and sums are FP32; a code's value zero + scale c enters both products as FP16 (2^-12 of it; relative to the token's largest, so that
- * any finite scale is handled; channels below 2^-29 of it lose bits), rotary keys and their queries as they are, queries as FP16 relative to their row's largest
- * (exact down to 2^-32 of it), weights as FP16 (2^-12 of one; below 2^-18 of a row's largest they lose bits, below 2^-28 they are left out of the sum's numerator).
+ * Precision: scores, statistics and sums are FP32.  A code's value, middle + scale (c - 128) with middle = zero + 128 scale, enters both products as FP16: scale and middle rounded (2^-11 of
+ * each at most), then the value (2^-11 of it), relative to a power of two of the 128 tokens that the value's token is among (tokens [128 i, 128 i + 128) of a sequence), so that any finite scale is
+ * handled; what is below 2^-29 of the largest of them loses bits, and of tiles whose largest values are further than 2^90 apart the smaller may count as nothing.  Rotary keys enter as they
+ * are, queries relative to their row's largest (exact down to 2^-32 of it), weights as FP16 (2^-11 of one; below 2^-18 of a row's largest they lose bits,
+ * below 2^-28 they are left out of the sum's numerator).
  * Up to 64 rows n_q * Hq of a sequence take one pass over its planes.
  * workspace : lynx_latent_workspace_bytes(shape, batch, n_q) bytes (0: unsupported shape), zero-filled once before its first use (lynx_workspace_init); it serves
  * smaller batches and fewer positions of the same shape, too.  Calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of

@@ -2,17 +2,17 @@
 //
 // A token is four rows of the planes, its latent's channels [128 g, 128 (g + 1)), and a BF16 rotary key of 64.  For R = n_q * Hq rows (positions x heads) per sequence
 //   S = Q C^T + Qr Kr^T,   p = 2^(a S + e - ref_r),   O += P C,   l += sum p 2^-e,   out = O / l:
-// 576 channels into a score, 512 out, and all heads share the token.  A code c stands for zero + scale c; it is computed in FP32 and rounded once, to FP16 relative to a power of two of its
-// token, 2^e, the largest of the token's four rows below 2^15 (2^-12 of a value, independent from channel to channel; BF16 pages have 2^-9).  Both products
-// take these values: tokens' rows are the scores' A operand in tensor memory and, in shared memory, the A operand C^T of the second product.  Scores get
-// the token's power of two back as a factor in FP32, weights carry 2^e in their exponent, and l has it taken out again, so that any finite scale works.
-// Queries are FP16 relative to a power of two of their row (exact down to 2^-32 of its largest), rotary parts BF16 as they are, into an accumulator of their
-// own.  Weights are FP16 relative to a reference per row, set from its first tile and raised (rare) before one would leave FP16; references, sums and
+// 576 channels into a score, 512 out, and all heads share the token.  A code c stands for zero + scale c = middle + scale (c - 128).  It enters both products as FP16 relative to
+// 2^e, a power of two that brings the largest value that a tile of 128 tokens can hold below 2^15: a row's scale and middle are rounded to FP16, and the value once more
+// (half a step, 2^-11, each; BF16 pages have 2^-8).  Tokens' rows are the scores' A operand in tensor memory and, in shared memory, the A operand C^T of the
+// second product.  Scores get 2^e back as a factor in FP32, weights carry it in their exponent, and l has it taken out again, so that any finite scale works.
+// Queries are FP16 relative to a power of two of their row (exact down to 2^-32 of its largest, over latent and rotary part), rotary parts BF16 times the same powers
+// of two (exact).  Weights are FP16 relative to a reference per row, set from its first tile and raised (rare) before one would leave FP16; references, sums and
 // accumulators are FP32.
 //
-// Layout: tokens (scores) and channels (outputs) are the M = 128 lanes of tensor memory, up to 64 rows the N: O^T takes 4 x 64 columns of the 512, scores
-// 64, three places for 128 channels of a tile's keys the rest.  (Rows as lanes would need all 512 columns for O alone.)
-// More rows are more row tiles, each a pass over the planes.
+// Layout: tokens (scores) and channels (outputs) are the M = 128 lanes of tensor memory, up to 64 rows the N: O^T takes 4 x N columns of the 512, and what is left
+// holds N scores of one or two tiles and the keys of two or four groups of 128 channels.  (Rows as lanes would need all 512 columns for O alone.)
+// More rows are more row tiles, each a pass over the planes that expands their codes again (128 rows as two tiles: see below).
 // One CTA per SM, a tile 128 tokens; roles, every hand-off an mbarrier with a bounded wait, nothing waits on another CTA:
 //   warps 0-3, 4-7   softmax, half of the rows each, whole tiles
 //   warps 8-23       codes to FP16, two sets of eight, in turn 128 channels each: a thread has 32 of two tokens, loaded a group ahead into registers; a piece's
@@ -20,11 +20,21 @@
 //   warps 24, 25     issue every tcgen05.mma: scores, weights times values
 //   warp 26          the tiles' powers of two
 //   warp 27          deals out the pieces
-// The tile's values have one place in shared memory (128 KB, beside queries of 72): a group's 128 channels go there, and to tensor memory as keys, when the
+// The tile's values have one place in shared memory (128 KB, beside queries of 18 to 72): a group's 128 channels go there, and to tensor memory as keys, when the
 // same channels of the tile before have been multiplied, so that the products of a tile, the expansion of the next one and its scores follow one another
 // group by group.
 // Work is cut in stream-K form: the (sequence, row tile, tile) list into equal ranges, a piece being a range's part of one segment.  A segment within one
-// CTA is written by it; otherwise partial (O, ref, l) go to the workspace and a dependent kernel joins them.
+// CTA is written by it; otherwise partial (O, ref, l) go to the workspace and a dependent kernel joins them.  Where all sequences are of one length and their segments come to 85 %
+// of the grid or more, each segment has CTAs of its own (a CTA then has one piece: queries and epilogue once).
+//
+// What bounds it.  Few rows: instructions of the warps that expand codes (a token's 512 values cost 3.5 a pair and thread, whatever the rows); 64 rows: the chain keys -> scores -> softmax ->
+// products, of which the second product reads its 128 KB of values at 128 bytes a cycle while expansions write the next ones.  Batches x context, 4 heads' planes, us, with the
+// joining kernel (floor: 326 bytes a token at the copy rate, or 2 x 1088 operations a row and token at the FP16 rate):
+//   16 rows   8 x 4096 15.7 (3.3)   8 x 131072 184 (53; the Anchor 156)   1 x 131072 33 (6.7; the Anchor 29)
+//   64 rows   1 x 131072 50 (11)
+//   128 rows  4 x 32768 80 (22)   16 x 32768 278 (89)
+// Steps that were kept, 16 x 32768 tokens and 128 rows: 417 with eight expanding warps, their values in FP32 and rounded once; 374 with a separate place for the rotary part; 315 with coalesced loads issued behind the
+// hand-over; 301 with FP16 arithmetic; 289 with a power of two per tile in place of one a token; 278 with 8-byte stores whose registers need no moves.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -139,9 +149,6 @@ __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.al
 template <int N>
 __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
-__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
 // 16 lanes of tensor memory x 8 J columns (see tc_ld_16x256)
 template <int J>
 __device__ __forceinline__ void ld_16x256(uint32_t a, uint32_t* r) {
@@ -453,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         if (w4 == 0 && lane < 4) minus[4 * j] = 0ull;
       }
       const int id = 1 + wg;
-      named_bar(id, 128);
+      named_bar(3, 256);   // (of all: what is read at a piece's end, of both halves' rows, is written anew at the next one's, which may be one tile)
       const int clear = p.causal ? len - p.n + 1 : len;   // tokens that every row sees
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gt) {

@@ -138,6 +138,20 @@ def test_many_sequences():
     _check(cache, q, qr, out, lse, True, False)
 
 
+@pytest.mark.parametrize("H,n", [(16, 1), (32, 1), (64, 2)])
+def test_many_pieces_of_one_tile(H, n):
+    """Each CTA takes several pieces, one behind the other: outputs of one are written while the next one's tile is under way."""
+    lens = [i * 53 % 129 for i in range(1100)]
+    cache = Cache(lens, 16, H, seed=15, wide=9)
+    q, qr = _queries(1100, n, H, seed=16)
+    out, lse = _run(cache, q, qr)
+    some = set(range(0, 1100, 7))
+    _check(cache, q, qr, out, lse, True, False, skip=set(range(1100)) - some)
+    for _ in range(5):
+        again, l2 = _run(cache, q, qr)
+        assert torch.equal(again, out) and torch.equal(l2, lse)
+
+
 @pytest.mark.parametrize("spread,qs", [(1e-20, 1.0), (1e-3, 100.0), (300.0, 0.01), (1e15, 1e-15), (1.0, 8.0), (1.0, 1e-30)])
 @pytest.mark.parametrize("H", [16, 64])
 def test_scales_of_any_size(spread, qs, H):
