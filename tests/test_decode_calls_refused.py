@@ -94,6 +94,43 @@ def test_latent_rows():
         assert read(**bad) == want, bad
 
 
+def _attend(shape=None, q=P, qs=576, qr=P, qrs=576, B=2, n=1, C=(P, P, P), pages=P, table=P, lens=P, scale=0.0, out=P, lse=None, ws=P, nbytes=1 << 30):
+    return lynx.load().lynx_latent_attention(_ref(shape or _shape(num_kv_heads=4)), q, qs, qr, qrs, B, n, 1, lynx._Plane(*C), pages, table, lens, scale, 0, out, lse, ws,
+                                             nbytes, None)
+
+
+def test_latent_attention():
+    lat = lambda **kw: _shape(**{"num_kv_heads": 4, **kw})
+    assert _attend(B=0) == OK
+    for bad, want in ((dict(B=-1), SHAPE), (dict(n=0), SHAPE), (dict(shape=lat(num_q_heads=0)), SHAPE), (dict(shape=lat(max_blocks_per_seq=0)), SHAPE),
+                      (dict(shape=_shape()), UNSUPPORTED), (dict(shape=lat(head_dim=64)), UNSUPPORTED), (dict(shape=lat(block_tokens=24)), UNSUPPORTED),
+                      (dict(shape=lat(num_q_heads=129)), UNSUPPORTED), (dict(n=65), UNSUPPORTED), (dict(shape=lat(num_blocks=1 << 26)), UNSUPPORTED),
+                      (dict(shape=lat(max_blocks_per_seq=1 << 26)), UNSUPPORTED), (dict(B=1 << 22), UNSUPPORTED),
+                      (dict(q=None), NULL), (dict(qr=None), NULL), (dict(C=(None, P, P)), NULL), (dict(C=(P, P, None)), NULL), (dict(pages=None), NULL),
+                      (dict(table=None), NULL), (dict(lens=None), NULL), (dict(out=None), NULL), (dict(ws=None), NULL), (dict(qs=504), SHAPE), (dict(qrs=56), SHAPE),
+                      (dict(qs=578), SHAPE), (dict(q=P + 8), ALIGN), (dict(qr=P + 2), ALIGN), (dict(C=(P, P + 8, P)), ALIGN), (dict(C=(P, P, P + 4)), ALIGN),
+                      (dict(pages=P + 8), ALIGN), (dict(out=P + 8), ALIGN), (dict(lse=P + 2), ALIGN), (dict(table=P + 1), ALIGN), (dict(lens=P + 2), ALIGN),
+                      (dict(ws=P + 8), ALIGN)):
+        assert _attend(**bad) == want, bad
+    need = lynx.load().lynx_latent_workspace_bytes(ctypes.byref(lat()), 2, 1)
+    assert need > 0 and _attend(nbytes=need - 1) == 5      # (LYNX_ERR_WORKSPACE)
+
+
+def test_a_latent_workspace_serves_smaller_calls():
+    size = lambda B, n, **kw: lynx.latent_workspace_bytes(lynx.Geometry(**{**dict(num_q_heads=16, num_kv_heads=4, block_tokens=16, num_blocks=99, max_blocks_per_seq=40), **kw}),
+                                                          B, n)
+    for kw in ({}, dict(max_blocks_per_seq=8), dict(num_q_heads=128), dict(num_q_heads=1), dict(max_blocks_per_seq=4000)):
+        for B in (1, 2, 3, 5, 31, 147, 148, 149, 700):
+            for n in (1, 2, 3, 4, 5, 8, 9, 63, 64):
+                here = size(B, n, **kw)
+                assert here > 0 and size(B + 1, n, **kw) >= here
+                if n < 64:
+                    assert size(B, n + 1, **kw) >= here
+    assert size(1, 65) == 0 and size(0, 1) == 0 and size(1, 1, num_kv_heads=2) == 0
+    with pytest.raises(lynx.LynxError, match="unsupported"):
+        lynx.make_latent_workspace(lynx.Geometry(16, 2, 16, 4, 4), 1, 1, "cpu")
+
+
 def test_the_python_bodies():
     E = lynx.LynxError
     bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
@@ -109,6 +146,10 @@ def test_the_python_bodies():
         lynx.HeadNorm(bf(128), eps=-1.0)
     norm = lynx.HeadNorm(bf(128), bf(128), 1)
     assert norm.eps == 1.0
+
+    def attend(geo=lat, q=bf(1, 1, 16, 512), qr=bf(1, 1, 16, 64), C=latents, pages=pages, table=i32(1, 4), lens=i32(1), **kw):
+        return lynx.latent_attention(geo, q, qr, C, pages, table, lens, torch.zeros(1 << 16, dtype=torch.uint8), **kw)
+
     calls = [
         ("device", lambda: lynx.norm_rotary(k, k, norm)),
         ("needed", lambda: lynx.norm_rotary(None, None, norm)),
@@ -132,6 +173,17 @@ def test_the_python_bodies():
         ("rope_pages", lambda: lynx.latent_read(lat, latents, pages[:3], i32(1, 4), None, i32(2), 3)),
         ("Residual", lambda: lynx.latent_read(lat, lynx.Planes(latents.anchor, None, latents.meta), pages, i32(1, 4), None, i32(2), 3)),
         ("n_rows", lambda: lynx.latent_read(lat, latents, pages, i32(1, 4), None, i32(2), -1)),
+        ("device", lambda: attend()),
+        ("q_latent", lambda: attend(q=bf(1, 1, 15, 512))),
+        ("q_latent", lambda: attend(q=torch.zeros(1, 1, 16, 512))),
+        ("device|q_rope", lambda: attend(qr=bf(1, 1, 16, 32))),
+        ("block_table", lambda: attend(table=i32(1, 5))),
+        ("seq_lens", lambda: attend(lens=i32(2))),
+        ("out", lambda: attend(out=torch.zeros(1, 1, 16, 512, dtype=torch.float16))),
+        ("lse", lambda: attend(lse=torch.zeros(1, 16))),
+        ("Residual", lambda: attend(C=lynx.Planes(latents.anchor, None, latents.meta))),
+        ("num_kv_heads", lambda: attend(geo=lynx.Geometry(16, 2, 16, 4, 4))),
+        ("rope_pages", lambda: attend(pages=pages[:3])),
     ]
     for match, call in calls:
         with pytest.raises(E, match=match):
