@@ -27,14 +27,18 @@
 // CTA is written by it; otherwise partial (O, ref, l) go to the workspace and a dependent kernel joins them.  Where all sequences are of one length and their segments come to 85 %
 // of the grid or more, each segment has CTAs of its own (a CTA then has one piece: queries and epilogue once).
 //
-// What bounds it.  Few rows: instructions of the warps that expand codes (a token's 512 values cost 3.5 a pair and thread, whatever the rows); 64 rows: the chain keys -> scores -> softmax ->
-// products, of which the second product reads its 128 KB of values at 128 bytes a cycle while expansions write the next ones.  Batches x context, 4 heads' planes, us, with the
-// joining kernel (floor: 326 bytes a token at the copy rate, or 2 x 1088 operations a row and token at the FP16 rate):
-//   16 rows   8 x 4096 15.7 (3.3)   8 x 131072 184 (53; the Anchor 156)   1 x 131072 33 (6.7; the Anchor 29)
-//   64 rows   1 x 131072 50 (11)
-//   128 rows  4 x 32768 80 (22)   16 x 32768 278 (89)
+// What bounds it.  Few rows: what a warp that expands codes does one step after the other (loads, FP16 values, tensor memory, barriers, 16 stores), four such warps a scheduler for
+// want of registers; instructions issue in 0.53 of the cycles.  64 rows: the chain keys -> scores -> softmax -> products, of which the second product reads its 128 KB of values
+// at 128 bytes a cycle while expansions write the next ones.  Batches x context, one kind of planes' blocks of 16 in random order, us, with the joining kernel (floor: 672 bytes a token, the Anchor
+// 416, at the copy rate, or 2 x 1088 operations a row and token at the FP16 rate where those take longer):
+//   16 rows   8 x 4096 15.9 (3.4)   8 x 131072 164 (108; the Anchor 149, 67)   1 x 131072 31.5 (13.4; the Anchor 29.5, 8.3)
+//   32 rows   8 x 131072 183 (108)
+//   64 rows   1 x 131072 45.4 (13.4)
+//   128 rows  4 x 32768 76 (22)   16 x 32768 272 (89)
 // Steps that were kept, 16 x 32768 tokens and 128 rows: 417 with eight expanding warps, their values in FP32 and rounded once; 374 with a separate place for the rotary part; 315 with coalesced loads issued behind the
-// hand-over; 301 with FP16 arithmetic; 289 with a power of two per tile in place of one a token; 278 with 8-byte stores whose registers need no moves.
+// hand-over; 301 with FP16 arithmetic; 289 with a power of two per tile in place of one a token; 278 with 8-byte stores whose registers need no moves; 270 with loads that take no place in the L1 (8 x 131072
+// and 16 rows: 184 -> 171), barriers asked before the values are computed (171 -> 164).
+// Tried and left: six places for the values (few rows; the L1 is smaller by as much, and loads wait: 184 -> 222), prefetches into the L2 a few tiles ahead (171 -> 198).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -116,6 +120,12 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
       : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
   return ok != 0;
 }
+// Whether a phase is over, without waiting for it.
+__device__ __forceinline__ bool mbar_probe(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ uint64_t globaltimer_ns() {
   uint64_t t;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
@@ -172,6 +182,17 @@ __device__ __forceinline__ void st_16x256(uint32_t a, const uint32_t (&r)[32]) {
       ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
         "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+// What is read once: into no cache line of the L1, which holds up as many loads under way as it has room for beside the shared memory.
+__device__ __forceinline__ uint4 ld_once(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ float2 ld_once(const float2* p) {
+  float2 v;
+  asm volatile("ld.global.L1::no_allocate.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+  return v;
 }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   uint32_t d;
@@ -713,17 +734,17 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         const uint4* const at_k = p.pages + (int64_t)(blk * p.bt + off) * 8 + set * 4 + q4;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          key[i] = ld_dep(at_k + 64 * i);
-          m[i][0] = ld_dep(at_m + 8 * i);
-          m[i][1] = ld_dep(at_m + next_group + 8 * i);
+          key[i] = ld_once(at_k + 64 * i);
+          m[i][0] = ld_once(at_m + 8 * i);
+          m[i][1] = ld_once(at_m + next_group + 8 * i);
         }
         if (u + 1 < n) next_id = block_id(p, b, min(t + kTile, top));
       };
       auto load_codes = [&](uint32_t rows) {   // (rows: from the first group's)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          a[k] = ld_dep(at_a + rows * 4u + 32 * k);
-          if (FULL) r[k] = ld_dep(at_r + rows * 4u + 32 * k);
+          a[k] = ld_once(at_a + rows * 4u + 32 * k);
+          if (FULL) r[k] = ld_once(at_r + rows * 4u + 32 * k);
         }
       };
       place(0);
@@ -809,6 +830,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         // ---- 128 channels at a time, ready before their places are
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+          const int g = set + 2 * i, use = gt * kGroups + g;   // (of the places for keys)
+          const uint32_t ki = place_of<C::kK>(use);
+          // (Asked here, whose answers take 80 cycles each, and waited for only where it was no.)
+          const bool k_free = use < C::kK || mbar_probe(kfree + ki * 8, round_of<C::kK>(use) ^ 1u), v_free = gt == 0 || mbar_probe(vfree + g * 8, (gt - 1) & 1);
           uint32_t o[32];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -826,14 +851,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
             }
           }
           if (i == 0) load_codes(next_group);
-          const int g = set + 2 * i, use = gt * kGroups + g;   // (of the places for keys)
-          const uint32_t ki = place_of<C::kK>(use);
-          if (use >= C::kK) wait(kfree + ki * 8, round_of<C::kK>(use) ^ 1u, ab);
+          if (!k_free) wait(kfree + ki * 8, round_of<C::kK>(use) ^ 1u, ab);
           tc_fence_after();
           st_16x256(tm_k + ki * 64, o);
           keys_there();      // (before the values: their scores can begin while the tile before is multiplied)
           if (lane == 0) mbar_arrive(kready + ki * 8);
-          if (gt > 0) wait(vfree + g * 8, (gt - 1) & 1, ab);
+          if (!v_free) wait(vfree + g * 8, (gt - 1) & 1, ab);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
 #pragma unroll
