@@ -263,3 +263,80 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         _check(cache, q, qr, out, None, True, False)
+
+
+@pytest.mark.parametrize("bt", [48, 112, 128, 400])
+def test_blocks_that_end_inside_a_tile(bt):
+    cache = Cache((1000, 130, 47), bt, 20, seed=18)
+    q, qr = _queries(3, 2, 20, seed=19)
+    out, lse = _run(cache, q, qr)
+    _check(cache, q, qr, out, lse, True, False)
+
+
+def test_lengths_beyond_the_table():
+    cache = Cache((320, 64), 16, 16, seed=20, junk=False)
+    cache.table[1, 4:] = cache.table[1, :1]      # (20 blocks: any will do)
+    cache.d_table = cache.table.cuda()
+    q, qr = _queries(2, 1, 16, seed=21)
+    cache.d_lens.copy_(torch.tensor([320, 320], dtype=torch.int32))
+    want, _ = _run(cache, q, qr)
+    cache.d_lens.copy_(torch.tensor([2 ** 31 - 1, 321], dtype=torch.int32))
+    assert torch.equal(_run(cache, q, qr)[0], want)
+    cache.d_lens.copy_(torch.tensor([-5, 0], dtype=torch.int32))
+    out, lse = _run(cache, q, qr)
+    assert not out.any() and (lse == -float("inf")).all()
+
+
+def test_two_graphs_of_one_workspace_and_two_streams():
+    caches = [Cache((900, 40), 16, 16, seed=22), Cache((333, 2000), 16, 16, seed=23)]
+    queries = [_queries(2, 1, 16, seed=24), _queries(2, 1, 16, seed=25)]
+    want = [_run(c, *x)[0] for c, x in zip(caches, queries)]
+    ws = lynx.make_latent_workspace(lynx.Geometry(16, 4, 16, 9, 200), 2, 1, "cuda")
+    call = lambda i, w, out: lynx.latent_attention(caches[i].geo, *queries[i], caches[i].planes, caches[i].pages, caches[i].d_table, caches[i].d_lens, w, out=out)
+    outs, graphs = [torch.empty_like(x) for x in want], [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for i in range(2):
+        with torch.cuda.graph(graphs[i]):
+            call(i, ws, outs[i])
+    for _ in range(5):
+        for i in (0, 1, 1, 0):
+            outs[i].zero_()
+            graphs[i].replay()
+            assert torch.equal(outs[i], want[i])
+    lynx.check(ws)
+    # a workspace and a stream each
+    streams, spaces = [torch.cuda.Stream(), torch.cuda.Stream()], [lynx.make_latent_workspace(c.geo, 2, 1, "cuda") for c in caches]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                call(i, spaces[i], outs[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    for w in spaces:
+        lynx.check(w)
+
+
+def test_planes_of_more_than_four_gigabytes():
+    """Blocks at the end of a pool whose planes' and pages' offsets pass 32 bits: written, read back and attended to as at its beginning."""
+    bt, tokens = 16, 200
+    nb = (1 << 32) // (4 * bt * 64) + 40000
+    rows = (nb, 4, bt)
+    big = lynx.Planes(torch.empty(*rows, 64, dtype=torch.uint8, device="cuda"), torch.empty(*rows, 64, dtype=torch.uint8, device="cuda"), torch.empty(*rows, 2, device="cuda"))
+    pages = torch.empty(nb, bt, 64, dtype=torch.bfloat16, device="cuda")
+    g = _gen(26)
+    c, k = (torch.randn(tokens, w, generator=g).to(torch.bfloat16).cuda() for w in (512, 64))
+    q, qr = _queries(1, 1, 16, seed=27)
+    results = []
+    for first in (0, nb - 13):
+        geo = lynx.Geometry(16, 4, bt, nb, 13)
+        blocks = first + torch.randperm(13, generator=_gen(28)).cuda()
+        t = torch.arange(tokens, device="cuda")
+        lynx.latent_append(geo, c, k, blocks[t // bt] * bt + t % bt, big, pages)
+        table, lens = blocks.to(torch.int32)[None], torch.tensor([tokens], dtype=torch.int32).cuda()
+        back = lynx.latent_read(geo, big, pages, table, None, torch.tensor([0, tokens], dtype=torch.int32).cuda(), tokens)
+        out = lynx.latent_attention(geo, q, qr, big, pages, table, lens, lynx.make_latent_workspace(geo, 1, 1, "cuda"))
+        results.append((*back, out))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    # (half a step of a row's span, and BF16's rounding)
+    span = (c.view(-1, 4, 128).amax(2) - c.view(-1, 4, 128).amin(2)).double().repeat_interleave(128, 1)
+    assert ((results[1][0].double() - c.double()).abs() <= span * (1 + 2.0 ** -6) / 510 + 2.0 ** -8 * c.double().abs().amax()).all() and torch.equal(results[1][1], k)
