@@ -38,7 +38,9 @@
 // Steps that were kept, 16 x 32768 tokens and 128 rows: 417 with eight expanding warps, their values in FP32 and rounded once; 374 with a separate place for the rotary part; 315 with coalesced loads issued behind the
 // hand-over; 301 with FP16 arithmetic; 289 with a power of two per tile in place of one a token; 278 with 8-byte stores whose registers need no moves; 270 with loads that take no place in the L1 (8 x 131072
 // and 16 rows: 184 -> 171), barriers asked before the values are computed (171 -> 164).
-// Tried and left: six places for the values (few rows; the L1 is smaller by as much, and loads wait: 184 -> 222), prefetches into the L2 a few tiles ahead (171 -> 198).
+// Tried and left: six places for the values (few rows; the L1 is smaller by as much, and loads wait: 184 -> 222), prefetches into the L2 a few tiles ahead (171 -> 198);
+// the next tile's loads in front of the second hand-over (16 x 32768, 128 rows: 271 -> 305); one softmax warpgroup and 88 registers for codes where rows are 16 (164 -> 158, but the Anchor 149 -> 151 and
+// 300 tokens 11.6 -> 12.1).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
