@@ -9,6 +9,7 @@
 #include <ATen/ATen.h>
 #include <ATen/TensorSubclassLikeUtils.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -74,7 +75,7 @@ bool planes_of(PyObject* o, lynx_plane* pl) {
 }
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 at::Tensor empty_like_device(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& on) {
-  return at::empty(sizes, at::TensorOptions().dtype(type).device(on.device()));
+  return at::detail::empty_cuda(sizes, type, on.device(), std::nullopt);   // (without the dispatcher)
 }
 // What a call returns: its result, or its status where it is not LYNX_OK (the caller raises).
 PyObject* status(lynx_status st) { return PyLong_FromLong((long)st); }
