@@ -90,7 +90,8 @@ struct AppendParams {
 // cost more registers than they hide (149 and 185, 152 and 209), a fifth CTA per SM 144 and 197.  Two turned rows in FP32 and their angles are too many
 // for the 64 registers that four CTAs leave: 60 bytes a thread are spilled (-Xptxas -v), which the rotated keys' time includes.
 template <int kFly, bool TURN, bool NORM>
-__device__ __forceinline__ void append_rows(const RotaryParams& r, float eps, const float4* weight_s, const AppendParams& p, int64_t row, int64_t slot, int v, int l, int first, int last) {
+__device__ __forceinline__ void append_rows(const RotaryParams& r, float eps, const float4* weight_s, const AppendParams& p, int64_t row, int64_t slot, int v, int l,
+                                            int first, int last) {
   static_assert(kFly == 1 || kFly == 2 || kFly == 4, "a division per lane");
   const bool turns = TURN && 8 * l < r.n_pairs, have = row >= 0 && row < p.n_src;
   int c0 = 2 * l, c1 = 2 * l + 1;
@@ -283,7 +284,7 @@ extern "C" lynx_status lynx_rotary(const lynx_rotary_spec* spec, const void* q, 
 }
 
 static lynx_status cache_append(const lynx_shape* shape, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t n_src,
-                                         const int32_t* rows, int64_t n_tokens, const int64_t* slots, const lynx_head_norm* norm,
+                                const int32_t* rows, int64_t n_tokens, const int64_t* slots, const lynx_head_norm* norm,
                                 const lynx_rotary_spec* spec, lynx_plane_out K, lynx_plane_out V, void* stream) {
   using namespace lynx;
   if (!shape) return LYNX_ERR_NULL;

@@ -24,8 +24,8 @@
 // same channels of the tile before have been multiplied, so that the products of a tile, the expansion of the next one and its scores follow one another
 // group by group.
 // Work is cut in stream-K form: the (sequence, row tile, tile) list into equal ranges, a piece being a range's part of one segment.  A segment within one
-// CTA is written by it; otherwise partial (O, ref, l) go to the workspace and a dependent kernel joins them.  Where all sequences are of one length and their segments come to 85 %
-// of the grid or more, each segment has CTAs of its own (a CTA then has one piece: queries and epilogue once).
+// CTA is written by it; otherwise partial (O, ref, l) go to the workspace and a dependent kernel joins them.  Several row tiles lie side by side: neighbouring CTAs take the same tokens, whose
+// codes the second one finds in the L2.  One row tile: where all sequences are of one length and come to 85 % of the grid or more, each has CTAs of its own (a CTA then has one piece: queries and epilogue once).
 //
 // What bounds it.  Few rows: what a warp that expands codes does one step after the other (loads, FP16 values, tensor memory, barriers, 16 stores), four such warps a scheduler for
 // want of registers; instructions issue in 0.53 of the cycles.  64 rows: the chain keys -> scores -> softmax -> products, of which the second product reads its 128 KB of values
@@ -34,10 +34,10 @@
 //   16 rows   8 x 4096 15.9 (3.4)   8 x 131072 164 (108; the Anchor 149, 67)   1 x 131072 31.5 (13.4; the Anchor 29.5, 8.3)
 //   32 rows   8 x 131072 183 (108)
 //   64 rows   1 x 131072 45.4 (13.4)
-//   128 rows  4 x 32768 76 (22)   16 x 32768 272 (89)
+//   128 rows  4 x 32768 77 (22)   16 x 32768 245 (89)
 // Steps that were kept, 16 x 32768 tokens and 128 rows: 417 with eight expanding warps, their values in FP32 and rounded once; 374 with a separate place for the rotary part; 315 with coalesced loads issued behind the
 // hand-over; 301 with FP16 arithmetic; 289 with a power of two per tile in place of one a token; 278 with 8-byte stores whose registers need no moves; 270 with loads that take no place in the L1 (8 x 131072
-// and 16 rows: 184 -> 171), barriers asked before the values are computed (171 -> 164).
+// and 16 rows: 184 -> 171), barriers asked before the values are computed (171 -> 164); 245 with row tiles side by side.
 // Tried and left: six places for the values (few rows; the L1 is smaller by as much, and loads wait: 184 -> 222), prefetches into the L2 a few tiles ahead (171 -> 198);
 // the next tile's loads in front of the second hand-over (16 x 32768, 128 rows: 271 -> 305); one softmax warpgroup and 88 registers for codes where rows are 16 (164 -> 158, but the Anchor 149 -> 151 and
 // 300 tokens 11.6 -> 12.1).
@@ -81,6 +81,7 @@ struct LatentParams {
   int B, n, Hq, R, RT, bt, num_blocks, max_blocks, causal, out_f32;
   int whole;                                // CTA i takes segment i
   int per_seg;                              // CTAs per segment where all have as many tiles (else 0)
+  int side_by_side;                         // CTAs RT i .. RT i + RT - 1 take the same tokens, a row tile each
   BlockDiv bt_div;
 };
 
@@ -102,7 +103,7 @@ struct Cfg {
 };
 
 struct Item {  // a piece: tiles u0 .. u0 + n - 1 of segment (b, rt), none: the end
-  int b, rt, len, u0, n, first_cta, n_contrib, pad;
+  int b, rt, len, u0, n, first_cta, n_contrib, slot;   // (slot: of its partial result)
 };
 
 // The t-th use of one of N places that are used in turn, N a power of two: the place, and the parity of its round.
@@ -291,12 +292,22 @@ __host__ __device__ constexpr int channel_at(int d) {   // of position d of 128
 struct Cursor {   // where a CTA's range begins, and how much of it there is
   int left, q, before;   // units (fewer than 2^31 in all); units a CTA; units in front of sequence b
   int b, s, u;           // sequence, row tile of it, tile
+  int cta, fixed;        // its number among those that cut the list (side by side: of row tile `fixed`, behind those of the row tiles before)
 };
 __device__ __forceinline__ int seq_len(const LatentParams& p, int b) { return min(max(ld_dep(p.lens + b), 0), p.max_blocks * p.bt); }
 __device__ __forceinline__ int tiles_of(int len) { return max((len + kTile - 1) / kTile, 1); }   // (a sequence without tokens has one, of none)
 // By one warp.
 __device__ __forceinline__ Cursor first_unit(const LatentParams& p, int cta, int n_cta, int lane) {
-  Cursor c = {0, 0, 0, 0, 0, 0};
+  Cursor c = {0, 0, 0, 0, 0, 0, cta, 0};
+  int RT = p.RT;
+  if (p.side_by_side) {   // the list of one row tile, by the CTAs that have it
+    n_cta /= RT;
+    c.fixed = cta % RT;
+    cta /= RT;
+    c.cta = c.fixed * n_cta + cta;
+    RT = 1;
+    if (cta >= n_cta) return c;
+  }
   if (p.whole) {
     c.b = cta / p.RT;
     c.s = cta - c.b * p.RT;
@@ -321,14 +332,14 @@ __device__ __forceinline__ Cursor first_unit(const LatentParams& p, int cta, int
     c.before = -1;
     return c;
   }
-  const int T = tot * p.RT;
+  const int T = tot * RT;
   c.q = (T - 1) / n_cta + 1;
   const int at = (int)min((long long)cta * c.q, (long long)T);
   c.left = min(c.q, T - at);
   if (c.left == 0) return c;
   int running = 0;
   for (int b0 = 0; b0 < p.B; b0 += 32) {
-    const int u = b0 + lane < p.B ? tiles_of(seq_len(p, b0 + lane)) * p.RT : 0;
+    const int u = b0 + lane < p.B ? tiles_of(seq_len(p, b0 + lane)) * RT : 0;
     int incl = u;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -350,32 +361,35 @@ __device__ __forceinline__ Cursor first_unit(const LatentParams& p, int cta, int
   }
   return c;
 }
+// Segments and partial results: CTAs in their order take segments in theirs, so that segment + CTA names a partial result; of CTAs side by side, those of each row tile by themselves.
+__device__ __forceinline__ int slot_of(const LatentParams& p, int b, int rt, int cta) { return (p.side_by_side ? rt * p.B + b : b * p.RT + rt) + cta; }
 // The piece at the cursor, which moves behind it.
-__device__ __forceinline__ Item next_piece(const LatentParams& p, Cursor& c, int cta) {
+__device__ __forceinline__ Item next_piece(const LatentParams& p, Cursor& c) {
   Item it = {0, 0, 0, 0, 0, 0, 0, 0};
   if (c.left <= 0 || c.b >= p.B) return it;
-  const int len = seq_len(p, c.b), U = tiles_of(len);
+  const int len = seq_len(p, c.b), U = tiles_of(len), RT = p.side_by_side ? 1 : p.RT;
   it.b = c.b;
-  it.rt = c.s;
+  it.rt = p.side_by_side ? c.fixed : c.s;
   it.len = len;
   it.u0 = c.u;
   it.n = min(c.left, U - c.u);
+  it.slot = slot_of(p, it.b, it.rt, c.cta);
   if (p.whole) {
-    it.first_cta = cta;
+    it.first_cta = c.cta;
     it.n_contrib = 1;
   } else if (c.before < 0) {
     it.first_cta = (c.b * p.RT + c.s) * p.per_seg;
     it.n_contrib = (U + c.q - 1) / c.q;
   } else {
-    const int g0 = c.before + c.s * U;
-    it.first_cta = g0 / c.q;
-    it.n_contrib = (g0 + U - 1) / c.q - it.first_cta + 1;
+    const int g0 = c.before + c.s * U, first = g0 / c.q;
+    it.first_cta = first + (p.side_by_side ? c.fixed * ((int)gridDim.x / p.RT) : 0);
+    it.n_contrib = (g0 + U - 1) / c.q - first + 1;
   }
   c.left -= it.n;
   c.u = 0;
-  if (++c.s == p.RT) {
+  if (++c.s == RT) {
     c.s = 0;
-    if (c.before >= 0) c.before += U * p.RT;
+    if (c.before >= 0) c.before += U * RT;
     ++c.b;
   }
   return it;
@@ -664,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       const bool direct = n_contrib == 1;
       const int segment = b * p.RT + rt;
       const int64_t row0 = (int64_t)b * p.R + rt * kMaxRows;
-      float* const part = p.part + (int64_t)(segment + (int)blockIdx.x) * NR * kPartRow;
+      float* const part = p.part + (int64_t)items[qi].slot * NR * kPartRow;
 #pragma unroll 1
       for (int i = 0; i < 2 * NR; i += 8) {
         const int g = 2 * wg + i / NR, c0 = i % NR, d = g * 128 + channel_at(w4 * 32 + lane);
@@ -961,11 +975,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
 #pragma unroll 1
     for (int ic = 0;; ++ic) {
       const int qi = ic & 1;
-      const Item it = next_piece(p, cur, blockIdx.x);
+      const Item it = next_piece(p, cur);
       if (ic > 1) wait(iempty + qi * 8, ((ic >> 1) - 1) & 1, iab);
       if (lane == 0) {
         volatile Item* d = items + qi;
-        d->b = it.b; d->rt = it.rt; d->len = it.len; d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib;
+        d->b = it.b; d->rt = it.rt; d->len = it.len; d->u0 = it.u0; d->n = it.n; d->first_cta = it.first_cta; d->n_contrib = it.n_contrib; d->slot = it.slot;
         mbar_arrive(ifull + qi * 8);
       }
       __syncwarp();
@@ -1029,7 +1043,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) latent_join_kernel(const __gr
   const int first = min((int)(info >> 16), n_cta - 1), n = min((int)(info & 0xFFFFu), n_cta - first);
   if (n <= 1) return;   // written by the attention kernel
   const int64_t slot = (int64_t)part_rows * kPartRow;
-  const float* src = p.part + (int64_t)(segment + first) * slot + (int64_t)(c - rt * kMaxRows) * kPartRow;
+  const float* src = p.part + (int64_t)slot_of(p, b, rt, first) * slot + (int64_t)(c - rt * kMaxRows) * kPartRow;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float M = -INFINITY, L = 0.0f;
   auto join = [&](float2 ml, const float4& o) {   // (M is the larger one's already)
@@ -1091,7 +1105,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) latent_join_kernel(const __gr
 
 // ------------------------------------------------------------------ host side
 struct LatentPlan {
-  int R, RT, NR, whole, grid, per_seg;
+  int R, RT, NR, whole, grid, per_seg, side_by_side;
   int64_t segs;
   size_t off_seg, off_part, bytes;
 };
@@ -1110,11 +1124,15 @@ lynx_status latent_plan(const lynx_shape* s, int B, int n, LatentPlan* pl) {
   if (pl->segs >= (1 << 22) || pl->segs * tiles >= (1ll << 31)) return LYNX_ERR_UNSUPPORTED;
   pl->whole = tiles <= 1;
   pl->per_seg = 0;
+  pl->side_by_side = 0;
   if (pl->whole) {
     pl->grid = (int)pl->segs;
   } else {
     pl->grid = (int)(pl->segs * tiles < sms ? pl->segs * tiles : sms);
-    if (pl->segs <= pl->grid && pl->grid / pl->segs * pl->segs * 100 >= 85ll * pl->grid) pl->per_seg = (int)(pl->grid / pl->segs);
+    // Several row tiles, where nearly all of the grid has one: those of a token side by side, so that its codes come out of the L2 but once.  Else equal segments, where they come
+    // to nearly all of the grid.  (128 rows: 16 x 32768 tokens 271 -> 245 us, with CTAs of their own for 32 segments; 16 sequences of 8192 to 65536 tokens, cut as one list before, 342 -> 326.)
+    if (pl->RT > 1 && pl->grid / pl->RT * pl->RT * 100 >= 95 * pl->grid) pl->side_by_side = 1;
+    else if (pl->segs <= pl->grid && pl->grid / pl->segs * pl->segs * 100 >= 85ll * pl->grid) pl->per_seg = (int)(pl->grid / pl->segs);
   }
   pl->off_seg = kWsHeaderBytes;
   pl->off_part = (pl->off_seg + (size_t)pl->segs * 4 + 255) / 256 * 256;
@@ -1182,7 +1200,7 @@ extern "C" lynx_status lynx_latent_attention(const lynx_shape* shape, const void
   p.B = batch; p.n = n_q; p.Hq = shape->num_q_heads; p.R = pl.R; p.RT = pl.RT;
   p.bt = shape->block_tokens; p.num_blocks = shape->num_blocks; p.max_blocks = shape->max_blocks_per_seq;
   p.causal = causal ? 1 : 0; p.out_f32 = out_float ? 1 : 0;
-  p.whole = pl.whole; p.per_seg = pl.per_seg;
+  p.whole = pl.whole; p.per_seg = pl.per_seg; p.side_by_side = pl.side_by_side;
   p.bt_div = block_div(p.bt);
   const lynx_status st = pl.NR == 16 ? launch_latent<16>(p, pl.grid, stream) : pl.NR == 32 ? launch_latent<32>(p, pl.grid, stream) : launch_latent<64>(p, pl.grid, stream);
   if (st != LYNX_OK || pl.whole) return st;
