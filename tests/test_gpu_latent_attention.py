@@ -340,3 +340,15 @@ def test_planes_of_more_than_four_gigabytes():
     # (half a step of a row's span, and BF16's rounding)
     span = (c.view(-1, 4, 128).amax(2) - c.view(-1, 4, 128).amin(2)).double().repeat_interleave(128, 1)
     assert ((results[1][0].double() - c.double()).abs() <= span * (1 + 2.0 ** -6) / 510 + 2.0 ** -8 * c.double().abs().amax()).all() and torch.equal(results[1][1], k)
+
+
+@pytest.mark.parametrize("zeros", [(0, 128), (128, 256), (100, 400), (0, 700)])
+@pytest.mark.parametrize("H", [16, 64, 100])
+def test_tiles_of_zeros(zeros, H):
+    """Tokens whose latents are zeros, tiles of them: their rotary keys still take weight."""
+    cache = Cache((700,), 16, H, seed=29)
+    t = torch.arange(*zeros)
+    cache.planes.meta[cache.table[0, t // 16].long().cuda(), :, (t % 16).cuda()] = 0.0
+    q, qr = _queries(1, 2, H, seed=30)
+    out, lse = _run(cache, q, qr, out=torch.empty(q.shape, device="cuda"))
+    _check(cache, q, qr, out, lse, True, False)
