@@ -447,9 +447,10 @@ lynx_status lynx_latent_read(const lynx_shape* shape, lynx_plane C, const void* 
  * lies behind a sequence's end, in blocks or in the table, is not looked at.
  * Precision: scores, statistics and sums are FP32.  A code's value, middle + scale (c - 128) with middle = zero + 128 scale, enters both products as FP16: scale and middle rounded (2^-11 of
  * each at most), then the value (2^-11 of it), relative to a power of two of the 128 tokens that the value's token is among (tokens [128 i, 128 i + 128) of a sequence), so that any finite scale is
- * handled; what is below 2^-29 of the largest of them loses bits, and of tiles whose largest values are further than 2^90 apart the smaller may count as nothing.  Rotary keys enter as they
- * are, queries relative to their row's largest (exact down to 2^-32 of it), weights as FP16 (2^-11 of one; below 2^-18 of a row's largest they lose bits,
- * below 2^-28 they are left out of the sum's numerator).
+ * handled.  Among such tokens rows lose bits of their scale where they hold less than 2^-21 of the largest value (2^-25 of it: seven bits are left, 2^-33: none), and values below 2^-29 of it lose bits.
+ * Rotary keys enter as they are, queries relative to their row's largest (exact down to 2^-32 of it), weights as FP16 (2^-11 of one; below 2^-16 of a row's largest they lose bits,
+ * below 2^-26 they are left out of the sum's numerator), whatever the sizes of other tokens' values; only where a set of 128 tokens holds less than 2^-64 of another's largest value its
+ * weights may lose as many bits more as it holds less, and all of them beyond 2^-90.
  * Up to 64 rows n_q * Hq of a sequence take one pass over its planes.
  * workspace : lynx_latent_workspace_bytes(shape, batch, n_q) bytes (0: unsupported shape), zero-filled once before its first use (lynx_workspace_init); it serves
  * smaller batches and fewer positions of the same shape, too.  Calls that share one are ordered on a stream.  lynx_check reads its status word: block ids out of

@@ -7,8 +7,8 @@
 // (half a step, 2^-11, each; BF16 pages have 2^-8).  Tokens' rows are the scores' A operand in tensor memory and, in shared memory, the A operand C^T of the
 // second product.  Scores get 2^e back as a factor in FP32, weights carry it in their exponent, and l has it taken out again, so that any finite scale works.
 // Queries are FP16 relative to a power of two of their row (exact down to 2^-32 of its largest, over latent and rotary part), rotary parts BF16 times the same powers
-// of two (exact).  Weights are FP16 relative to a reference per row, set from its first tile and raised (rare) before one would leave FP16; references, sums and
-// accumulators are FP32.
+// of two (exact).  Weights are FP16 relative to a reference per row, ref = largest score so far + e of the tile that set it - 4: set from a piece's first tile, raised (rare) before a weight would leave FP16, and
+// lowered (rare) with e, since the weights of a tile of smaller values are smaller by as much; references, sums and accumulators are FP32.
 //
 // Layout: tokens (scores) and channels (outputs) are the M = 128 lanes of tensor memory, up to 64 rows the N: O^T takes 4 x N columns of the 512, and what is left
 // holds N scores of one or two tiles and the keys of two or four groups of 128 channels.  (Rows as lanes would need all 512 columns for O alone.)
@@ -59,11 +59,14 @@ constexpr int kPartRow = kLatent + 4;       // floats of a partial row: O[512], 
 constexpr int kThreads = 896;
 constexpr int kRegSoft = 72, kRegCodes = 80, kRegRest = 40;   // per thread; the launch has 72 for each of seven warpgroups
 static_assert(2 * kRegSoft + 4 * kRegCodes + kRegRest <= 7 * 72, "registers");
-constexpr int kFac = 4;                     // places for the powers of two of a tile's tokens
+constexpr int kFac = 4;                     // places for tiles' powers of two
 constexpr int kDoneThreads = 256 + 4 * 32;  // softmax, products, powers of two, pieces
-// log2 of a row's largest weight when its reference is set; of what sets it anew when another row's weight has left FP16 (65504)
-constexpr float kTop = 4.0f, kRaise = 9.0f;
-constexpr int kMinExp = -80;                // smallest exponent of a token's values
+// log2 of a row's largest weight when its reference is set
+constexpr float kTop = 4.0f;
+// References are lowered for a tile whose exponent is smaller than that of the tile that set them by more than kDrop: weights lose bits below 2^-16 of a row's largest, 2^(-14 - kTop + kDrop).  Accumulators grow with
+// that, by 2^kSpan at most: from the largest exponent of a piece on (sums of weights of 2^16, values of 2^16 and 2^31 tokens leave 2^64 of FP32).
+constexpr int kDrop = 2, kSpan = 64;
+constexpr int kMinExp = -80;                // smallest exponent of a tile's values
 
 struct LatentParams {
   const uint4 *q, *qr;                      // rows `q_stride`, `qr_stride` chunks apart
@@ -499,6 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       const int id = 1 + wg;
       named_bar(3, 256);   // (of all: what is read at a piece's end, of both halves' rows, is written anew at the next one's, which may be one tile)
       const int clear = p.causal ? len - p.n + 1 : len;   // tokens that every row sees
+      int e_ref = 0, e_top = kMinExp;   // exponent that the references have in them; the piece's largest
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gt) {
         const uint32_t fi = place_of<kFac>(gt), si = place_of<C::kS>(gt);
@@ -506,6 +510,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
         wait(sfull + si * 8, round_of<C::kS>(gt), ab);
         tc_fence_after();
         const int e = reinterpret_cast<volatile int*>(smem + C::kOffFac)[fi];
+        e_top = max(e_top, e);
+        const int e_new = max(e, e_top - kSpan);   // (for references that are set)
         const uint64_t e2 = f2_pack((float)e, (float)e), factor = f2_pack(pow2(e), pow2(e));
         const uint32_t tm_s = tmem0 + C::kTmS + si * NR + wg * NC + lanes;
         const int first = (u0 + u) * kTile;
@@ -533,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
           }
         };
         const uint64_t back = f2_pack(pow2(-e), pow2(-e));
-        bool anew = u == 0;   // references are to be set, or raised
+        bool anew = u == 0 || e_new < e_ref - kDrop;   // references are to be set, lowered or raised
         uint32_t w[4][NJ];
         uint64_t sum[NJ];
 #pragma unroll 1
@@ -576,12 +582,14 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
               for (int j = 0; j < 2 * NJ; ++j) {
                 const int c = col0 + 8 * (j >> 1) + (j & 1);
                 const float M = fmaxf(fmaxf(max_s[c], max_s[NR + c]), fmaxf(max_s[2 * NR + c], max_s[3 * NR + c]));   // (less the reference)
-                const float more = (u == 0 ? M > -INFINITY : M > kRaise) ? M - kTop : 0.0f, f = u == 0 ? 1.0f : ex2(-more);
+                // (largest score so far, plus e_new: this tile's, or what the reference has in it)
+                const float more = u > 0 ? fmaxf(M + (float)(e_new - e) - kTop, (float)(e_new - e_ref)) : M > -INFINITY ? M - kTop : 0.0f, f = u == 0 ? 1.0f : ex2(-more);
                 ref_s[c] -= more;
                 scale_s[c] = f;
                 rescale = rescale || f != 1.0f;
               }
             }
+            e_ref = e_new;
             if (bar_or(id, 128, rescale)) {   // (not in a piece's first tile: f is 1)
 #pragma unroll
               for (int j = 0; j < NJ; ++j) l[j] = f2_mul(l[j], *reinterpret_cast<const uint64_t*>(scale_s + col0 + 8 * j));
@@ -998,6 +1006,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
       const int n = items[qi].n, len = items[qi].len, u0 = items[qi].u0, b = items[qi].b;
       if (n == 0) break;
       const int top = max(len - 1, 0);
+      int e = 0;
 #pragma unroll 1
       for (int u = 0; u < n; ++u, ++gt) {
         const uint32_t fi = place_of<kFac>(gt);
@@ -1018,7 +1027,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attention_kernel(const __g
           }
         }
         big = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(big)));
-        if (lane == 0) reinterpret_cast<volatile int*>(smem + C::kOffFac)[fi] = min(max(exponent_of(big), kMinExp), 113);
+        if (big > 0.0f) e = min(max(exponent_of(big), kMinExp), 113);   // (any will do for zeros: that of the tile before)
+        if (lane == 0) reinterpret_cast<volatile int*>(smem + C::kOffFac)[fi] = e;
         __syncwarp();
         if (lane == 0) mbar_arrive(fready + fi * 8);
       }
