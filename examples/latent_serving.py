@@ -72,7 +72,8 @@ class Server:
         self.lens = torch.zeros(batch, dtype=torch.int32, device=device)
         self.active = torch.zeros(batch, dtype=torch.int32, device=device)     # 1: the place decodes
         self.last = torch.zeros(batch, dtype=torch.int64, device=device)       # its last token, not in the cache yet
-        self.angles = lynx.rotary_table(capacity, ROPE // 2, device=device)
+        self.capacity = self.geo.max_blocks_per_seq * BLOCK                    # tokens of a place's table: plan_blocks clamps lengths to it
+        self.angles = lynx.rotary_table(self.capacity, ROPE // 2, device=device)
         self.ws_step = lynx.make_latent_workspace(self.geo, batch, 1, device)
         self.ws_chunk = lynx.make_latent_workspace(self.geo, 1, CHUNK, device)
         self.graph = None
@@ -89,6 +90,8 @@ class Server:
     def start(self, at, prompt):
         """Puts a request with prompt [n] into the free place `at`, 64 positions at a time.  False: there are no blocks for it, and nothing has changed."""
         n = len(prompt)
+        if not 1 <= n <= self.capacity:     # (its last token is not in the cache yet, but will be)
+            raise ValueError(f"a prompt must have 1 to {self.capacity} tokens")
         plan = lynx.plan_blocks(self.geo, self.pool, self.table, self.lens, self.grown(at, n - 1), n - 1)
         if int(plan.lens[at]) < n - 1:      # (a request that does not get its blocks stays as it is)
             return False
@@ -153,6 +156,8 @@ class Server:
 
 def serve(server, prompts, n_tokens):
     """Serves all prompts, n_tokens each, as many at a time as there are places and blocks.  -> each prompt's tokens, decode steps."""
+    if any(len(x) - 1 + n_tokens > server.capacity for x in prompts):      # (a place that is full gets no further token)
+        raise ValueError(f"a request must end within {server.capacity} tokens")
     waiting, place, got, steps = list(range(len(prompts))), [None] * server.batch, [[] for _ in prompts], 0
     while waiting or any(r is not None for r in place):
         for at in range(server.batch):
