@@ -8,6 +8,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/TensorSubclassLikeUtils.h>
+#include <ATen/record_function.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
@@ -74,8 +75,10 @@ bool planes_of(PyObject* o, lynx_plane* pl) {
          tensor_attr(o, s_meta, false, (void**)&pl->meta);
 }
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
+// Without the dispatcher (about 1 us less), unless it has something to do: fill fresh memory, for programs that ask for deterministic results, or tell a profiler.
 at::Tensor empty_like_device(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& on) {
-  return at::detail::empty_cuda(sizes, type, on.device(), std::nullopt);   // (without the dispatcher)
+  if (at::globalContext().deterministicAlgorithms() || at::hasCallbacks()) return at::empty(sizes, at::TensorOptions().dtype(type).device(on.device()));
+  return at::detail::empty_cuda(sizes, type, on.device(), std::nullopt);
 }
 // What a call returns: its result, or its status where it is not LYNX_OK (the caller raises).
 PyObject* status(lynx_status st) { return PyLong_FromLong((long)st); }
