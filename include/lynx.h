@@ -338,8 +338,9 @@ typedef struct {
 
 /* Norms of queries and keys for each head and their rotary positions, in one pass: lynx_rotary's arguments, conventions and tensors
  * (in place or not), each head normed before it is turned, one rounding to BF16 behind both.  head_width : 64, 128 or 256 channels (strides at least
- * heads * head_width, weights of as many); 2 n_pairs <= head_width.  norm or spec may be NULL: the rotation alone (of 64-wide rotary keys
- * and queries, say), the norm alone, a copy. */
+ * heads * head_width, weights of as many); 2 n_pairs <= head_width, and n_pairs <= 64 as always: of 256 channels at most 128 turn.  The heads of a token lie one
+ * behind the other: rotary parts that lie between other channels of their heads (64 of every 192, say) are copied or projected apart first.  norm or spec may be
+ * NULL: the rotation alone (of 64-wide rotary keys and queries, say), the norm alone, a copy. */
 lynx_status lynx_norm_rotary(const lynx_head_norm* norm, const lynx_rotary_spec* spec, int32_t head_width, const void* q,
                              int64_t q_stride, int32_t num_q_heads, const void* k, int64_t k_stride, int32_t num_kv_heads,
                              int64_t n_tokens, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,

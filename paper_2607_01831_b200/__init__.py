@@ -691,8 +691,9 @@ class HeadNorm:
 
 def norm_rotary(q: torch.Tensor | None, k: torch.Tensor | None, norm: HeadNorm | None = None, spec: Rotary | None = None,
                 q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
-    """lynx_norm_rotary: q BF16 [T][Hq][W], k BF16 [T][Hkv][W], W = 64, 128 or 256 (either may be None; tokens may lie apart), each head normed
-    and turned in one pass -> (q_out, k_out), which may be the inputs.  norm or spec None: that part is left out."""
+    """lynx_norm_rotary: q BF16 [T][Hq][W], k BF16 [T][Hkv][W], W = 64, 128 or 256 (either may be None; tokens may lie apart, the heads of a token
+    not), each head normed and turned (128 channels of it at most) in one pass -> (q_out, k_out), which may be the inputs.  norm or spec None:
+    that part is left out."""
     r = _fast_norm_rotary(q, k, norm, spec, q_out, k_out)
     if r is not None:
         return _result(r, "lynx_norm_rotary")

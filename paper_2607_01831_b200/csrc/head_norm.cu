@@ -24,7 +24,8 @@ struct HeadRows {
 };
 
 // A warp: 32 / L tokens, `per` of the heads of both tensors.  Weights are read from shared memory row by row: in registers, with two CTAs of 117 to an SM instead
-// of three of 80, 32768 tokens of 72 heads (1.24 GB, 184 us at the copy rate) took 223 us.
+// of three of 80, 32768 tokens of 72 heads (1.21 GB, 184 us at the copy rate) took 223 us.  They take 206 (0.89 of that rate); as many channels in heads of 64 run at 0.85, of 256 at 0.81.  With four
+// heads under way 44 bytes a thread are spilled.
 template <int L, int kFly>
 __global__ void __launch_bounds__(kThreads, 3) norm_rotary_kernel(const __grid_constant__ RotaryParams r, const __grid_constant__ HeadRows q,
                                                                  const __grid_constant__ HeadRows k, int64_t n_tokens, int per, int groups) {

@@ -28,13 +28,15 @@
 // codes the second one finds in the L2.  One row tile: where all sequences are of one length and come to 85 % of the grid or more, each has CTAs of its own (a CTA then has one piece: queries and epilogue once).
 //
 // What bounds it.  Few rows: what a warp that expands codes does one step after the other (loads, FP16 values, tensor memory, barriers, 16 stores), four such warps a scheduler for
-// want of registers; instructions issue in 0.53 of the cycles.  64 rows: the chain keys -> scores -> softmax -> products, of which the second product reads its 128 KB of values
+// want of registers; instructions issue in 0.61 of the cycles (64 rows 0.41, 128 rows 0.46).  64 rows: the chain keys -> scores -> softmax -> products, of which the second product reads its 128 KB of values
 // at 128 bytes a cycle while expansions write the next ones.  Batches x context, one kind of planes' blocks of 16 in random order, us, with the joining kernel (floor: 672 bytes a token, the Anchor
 // 416, at the copy rate, or 2 x 1088 operations a row and token at the FP16 rate where those take longer):
-//   16 rows   8 x 4096 15.9 (3.4)   8 x 131072 164 (108; the Anchor 149, 67)   1 x 131072 31.5 (13.4; the Anchor 29.5, 8.3)
+//   16 rows   8 x 4096 15.6 (3.4)   8 x 131072 164 (108; the Anchor 149, 67)   1 x 131072 32.6 (13.4; the Anchor 29.1, 8.3)
 //   32 rows   8 x 131072 183 (108)
-//   64 rows   1 x 131072 45.4 (13.4)
-//   128 rows  4 x 32768 77 (22)   16 x 32768 245 (89)
+//   64 rows   1 x 131072 45.9 (13.4)
+//   128 rows  4 x 32768 77 (22)   16 x 32768 247 (89)
+//   64 positions of 128 rows, 128 row tiles a sequence, each of which expands the codes again: 1 x 16384 500 (177), 2 x 16384 955 (355)
+// A tile takes a CTA 2.4 (the Anchor) and 2.6 us with 16 rows, 3.1 with 32, 3.9 with 64, beside 12 to 17 of a call: queries, first loads, the joining kernel.
 // Steps that were kept, 16 x 32768 tokens and 128 rows: 417 with eight expanding warps, their values in FP32 and rounded once; 374 with a separate place for the rotary part; 315 with coalesced loads issued behind the
 // hand-over; 301 with FP16 arithmetic; 289 with a power of two per tile in place of one a token; 278 with 8-byte stores whose registers need no moves; 270 with loads that take no place in the L1 (8 x 131072
 // and 16 rows: 184 -> 171), barriers asked before the values are computed (171 -> 164); 245 with row tiles side by side.
@@ -57,7 +59,7 @@ constexpr int kTile = 128, kGroups = 4, kLatent = 512, kRope = 64;
 constexpr int kMaxRows = 64;                // rows of a row tile
 constexpr int kPartRow = kLatent + 4;       // floats of a partial row: O[512], reference, sum, pad
 constexpr int kThreads = 896;
-constexpr int kRegSoft = 72, kRegCodes = 80, kRegRest = 40;   // per thread; the launch has 72 for each of seven warpgroups
+constexpr int kRegSoft = 72, kRegCodes = 80, kRegRest = 40;   // per thread; the launch has 72 for each of seven warpgroups (full codes spill 52 bytes a thread, 32 rows and fewer of the Anchor 4)
 static_assert(2 * kRegSoft + 4 * kRegCodes + kRegRest <= 7 * 72, "registers");
 constexpr int kFac = 4;                     // places for tiles' powers of two
 constexpr int kDoneThreads = 256 + 4 * 32;  // softmax, products, powers of two, pieces

@@ -5,7 +5,8 @@
 //   many tokens: a quarter-warp (8 lanes) owns a token, all four rows in flight; four consecutive tokens a warp, whose rows of a plane lie side by side
 //   few tokens:  a warp owns one, a quarter each row
 // A lane holds 16 channels of a row as two neighbouring chunks of 8, and chunk l of the key's eight.
-// 32768 tokens, out of one projection into scattered blocks and back (60 MB each way: 9.1 us at the copy rate): append with norm and rotation 15.3 us (instructions of the quantiser), read 10.4.
+// 32768 tokens, out of one projection into scattered blocks and back (60 MB each way: 9.1 us at the copy rate): append with norm and rotation 21.3 us (instructions of the quantiser, which issue in
+// half of the cycles, and loads that each warp waits for once), read 11.4; with all of it in the L2 16.2 and 10.7.
 // 16 tokens there and back: 5.2 us (latency).
 #include <cuda_bf16.h>
 
